@@ -454,6 +454,125 @@ relaxkv_status relaxkv_cache_attention(
     void* out, float* lse_out, void* workspace, size_t workspace_bytes, relaxkv_stream stream);
 
 /*
+ * ---- Many continuations of a repaired context.  (The paper answers one query per repair; these calls are for the callers that answer
+ * from one repaired context many times: several samples, beams, follow-up questions.)  The contexts stay where the repair left them, in a
+ * relaxkv_cache_view; every continuation ("sequence") keeps the K/V of its own tokens - the question, the answer so far - in blocks of a
+ * paged store.  One step appends some tokens to some sequences (a "row" each) and attends from those rows.  ----
+ *
+ * In these calls shape->h_ctx_len[b] may be 0 (a sequence without a context), h_q_len is not read, h_tuning neither.
+ */
+
+/* The paged store of one layer.  Token t of block x of KV head g lives at k + x * block_stride + t * token_stride + g * head_stride (in
+ * elements), same for V: [n_blocks, block_size, H_kv, D] and [n_blocks, H_kv, block_size, D] storage.  Strides are multiples of 8. */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t block_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+  int32_t block_size;                  /* tokens of a block: 16, 32, 64 or 128                                  */
+  int32_t n_blocks;
+} relaxkv_paged_cache;
+
+/* The rows of a step.  Sequences are grouped by their context; row r belongs to sequence row_seq[r] and sees the whole context of that
+ * sequence and the first row_len[r] tokens of the sequence's own (itself the last of them, once it has been appended). */
+typedef struct {
+  int32_t n_seq;                       /* sequences                                                             */
+  int32_t table_width;                 /* blocks a row of block_table has room for                              */
+  int64_t table_stride;                /* elements between the rows of block_table                              */
+  int64_t n_rows;                      /* rows allocated in q / out                                             */
+  int32_t max_len;                     /* upper bound of row_len                                                */
+  const int32_t* h_seq_cu;             /* host [n_req+1]: sequences [h_seq_cu[b], h_seq_cu[b+1]) continue context b; from 0 to n_seq */
+  const int32_t* h_max_rows;           /* host [n_req]: upper bound of the rows of context b                    */
+  const int32_t* row_cu;               /* device [n_seq+1]: rows [row_cu[i], row_cu[i+1]) are sequence i's      */
+  const int32_t* row_seq;              /* device [n_rows]; -1: no row (left alone)                              */
+  const int32_t* row_len;              /* device [n_rows]                                                       */
+  const int32_t* block_table;          /* device [n_seq, table_width]: the blocks of every sequence in order    */
+} relaxkv_continuation_rows;
+
+/* Bytes of device scratch that suffice for the three calls below that take a workspace, with these shapes, up to n_rows rows and context
+ * blocks of block_size tokens (0: no block selection).  Returns 0 for an invalid shape.  Host only. */
+size_t relaxkv_continuation_workspace_bytes(const relaxkv_shape* shape, int64_t n_rows, int32_t block_size);
+
+/*
+ * Block tables and slot maps of a step from the sequences' lengths, on the device.  Sequence i holds seq_len[i] tokens in the blocks
+ * block_table[i, 0 .. ceil(seq_len[i] / block_size)); new_len[i] >= 0 tokens are appended to it, new_len[i] < 0 ends it: its blocks are free
+ * again (before new ones are taken) and its length is 0.
+ *   stack     free_blocks[0 .. n_free[0]), then the ended sequences' blocks in sequence order
+ *   taken     from the end of the stack, in sequence order; written to block_table behind the blocks a sequence has
+ *   rows      of sequence i: [row_cu[i], row_cu[i+1]); token j of them has row_seq = i, row_len = seq_len[i] + j + 1,
+ *             row_pos = seq_base[i] + seq_len[i] + j (seq_base NULL: 0) and row_slot = block * block_size + place in the block.
+ *             Rows from row_cu[n_seq] to n_rows: row_seq = row_slot = -1, row_len = row_pos = 0.
+ * seq_len_out and n_free_out receive the lengths and the free blocks left, the next step's inputs (they may not overlap seq_len, new_len and
+ * n_free); the stack that is left stands in free_blocks, which is written from entry n_free[0] on only.  Same inputs, same results: the call
+ * may be repeated.
+ * A sequence with seq_len < 0, more tokens than its row of block_table holds or new_len > n_rows is left as it is; more rows than n_rows, more
+ * blocks than there are: nothing is appended to any sequence (ended ones still end); n_free or the blocks given back beyond free_capacity:
+ * nothing happens at all.  Each is reported in the device status word.  Block numbers are not looked at here (the calls that use them do).
+ * n_seq <= 4096.
+ */
+relaxkv_status relaxkv_build_block_tables(
+    int32_t n_seq, int32_t block_size, const int32_t* seq_len, const int32_t* new_len, const int32_t* seq_base, int32_t* free_blocks,
+    int32_t free_capacity, const int32_t* n_free, int32_t* block_table, int32_t table_width, int64_t table_stride, int64_t n_rows,
+    int32_t* seq_len_out, int32_t* n_free_out, int32_t* row_cu, int32_t* row_seq, int32_t* row_pos, int32_t* row_len, int32_t* row_slot,
+    relaxkv_stream stream);
+
+/* The per-head RMSNorm of the projected queries and keys (weights [head_dim], or both NULL), the rotary embedding at `positions` and the
+ * append of K and V to the paged store in ONE pass: q_out = rotated q (may be q itself), store.k[slot] = rotated k, store.v[slot] = v.
+ * Arithmetic in fp32 (angles in fp64) with one rounding to bf16 at the end.  q, q_out [n_rows, n_q_heads, head_dim], k and v [n_rows, n_kv_heads,
+ * head_dim] (left as they are); positions, slots device int32 [n_rows]; a row with slot -1 is rotated and not stored, another slot outside the
+ * store is reported and not stored.  Slots are distinct. */
+relaxkv_status relaxkv_qk_norm_rope_append_paged(
+    const relaxkv_paged_cache* store, const void* q, const void* k, const void* v, int64_t n_rows, int32_t n_q_heads, int32_t n_kv_heads,
+    int32_t head_dim, const void* w_q_norm, const void* w_k_norm, float eps, const int32_t* positions, const int32_t* slots, float theta,
+    void* q_out, relaxkv_stream stream);
+
+/*
+ * Attention of a step's rows over [the shared context, the sequence's own tokens]: for row r of sequence i of context b
+ *   out[r,h,:] = softmax over j < T_b and t < row_len[r] of scale * <q[r,h,:], K>, times V      K = cache rows of context b, then
+ *                                                                                              the store's tokens of sequence i
+ * A context is read once for all its rows, whatever their number.  cache may be NULL where every context is empty, store NULL where max_len is 0.
+ * A row that sees no key at all gets zeros and lse = -inf.
+ *   q, out  device bf16 [n_rows, H, D] (16-byte aligned); lse_out NULL or device fp32 [H, n_rows]
+ * Rows with row_seq -1 are left alone.  Reported and left alone: row_seq or row_len out of range, rows of a context above h_max_rows.  A block
+ * number out of range is reported, its tokens are passed over.
+ */
+relaxkv_status relaxkv_shared_prefix_attention(
+    const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store, const relaxkv_continuation_rows* rows,
+    const void* q, void* out, float* lse_out, void* workspace, size_t workspace_bytes, relaxkv_stream stream);
+
+/*
+ * 8-bit bounds of the keys of every context block (block x of context b: tokens [x * block_size, (x+1) * block_size) of it, the last one what is
+ * left).  For block x and KV head g, with hi_d and lo_d the largest and the smallest key element of dim d (NaN are passed over):
+ *   scale = the smallest power of two s with |hi_d|, |lo_d| <= 127 s for all d (at least 2^-100; 1 if all are 0)
+ *   bounds[x, g, 0, d] = ceil(hi_d / s), bounds[x, g, 1, d] = floor(lo_d / s)       as int8 (beyond +-127: +-127)
+ * bounds_out int8 [sum_b n_b, H_kv, 2, D] (16-byte aligned), scale_out fp32 [sum_b n_b, H_kv], n_b = ceil(T_b / block_size); only cache->k is read.
+ * block_size 16, 32, 64 or 128.
+ */
+relaxkv_status relaxkv_block_bounds(const relaxkv_shape* shape, const relaxkv_cache_view* cache, int32_t block_size, int8_t* bounds_out,
+                                    float* scale_out, relaxkv_stream stream);
+
+/*
+ * The context blocks that a row may need most: with q_h in 8 bits the way the bounds are (scale s_h per row and head, rounded to nearest even),
+ *   score[x] = scale[x] * max over the heads h of the KV head's group of s_h * sum_d (max(q_hd, 0) * hi_d + min(q_hd, 0) * lo_d),
+ * the largest logit that a key within the bounds could have.  All terms are whole numbers below 2^24 and powers of two, so scores do not depend on
+ * the order of summation.  Selected are the n_select blocks of the highest score, equal scores by the lower number, the first n_first and the last
+ * n_last blocks in any case.
+ * blocks_out device int32 [n_rows, H_kv, n_select]: ascending, -1 behind them.  n_first + n_last <= n_select.
+ * Of rows only h_seq_cu, h_max_rows, n_seq, n_rows, row_cu and row_seq are read; rows with row_seq -1 are left alone.
+ */
+relaxkv_status relaxkv_select_blocks(
+    const relaxkv_shape* shape, int32_t block_size, const int8_t* bounds, const float* scale, const relaxkv_continuation_rows* rows, const void* q,
+    int32_t n_select, int32_t n_first, int32_t n_last, int32_t* blocks_out, void* workspace, size_t workspace_bytes, relaxkv_stream stream);
+
+/* relaxkv_shared_prefix_attention with, of each context, only the tokens of the blocks that `blocks` (device int32 [n_rows, H_kv, n_select]) lists
+ * for the row and KV head: distinct, in any order, entries -1 are passed over; another number without a block is reported and passed over. */
+relaxkv_status relaxkv_block_sparse_attention(
+    const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store, const relaxkv_continuation_rows* rows,
+    int32_t block_size, const int32_t* blocks, int32_t n_select, const void* q, void* out, float* lse_out, void* workspace, size_t workspace_bytes,
+    relaxkv_stream stream);
+
+/*
  * Test utility for the bounded waits (the paper has no counterpart): launches one thread that waits on
  * a barrier nothing will ever complete.  The wait gives up after its limit (0.4 s), the kernel ends
  * normally and RELAXKV_ERR_TIMEOUT is recorded in the device status word - the same path a stuck

@@ -27,6 +27,8 @@ ENTRY_POINTS = (
     "relaxkv_list_attention", "relaxkv_cache_attention",
     "relaxkv_scatter_kv_lists", "relaxkv_mean_scores", "relaxkv_scale_scores", "relaxkv_query_prefill_attention", "relaxkv_rmsnorm", "relaxkv_linear", "relaxkv_linear_qkv", "relaxkv_linear_swiglu", "relaxkv_rope", "relaxkv_qk_norm_rope", "relaxkv_qk_norm_rope_append",
     "relaxkv_swiglu", "relaxkv_target_positions", "relaxkv_carry_rows", "relaxkv_set_chained_launch",
+    "relaxkv_continuation_workspace_bytes", "relaxkv_build_block_tables", "relaxkv_qk_norm_rope_append_paged", "relaxkv_shared_prefix_attention",
+    "relaxkv_block_bounds", "relaxkv_select_blocks", "relaxkv_block_sparse_attention",
 )
 
 
@@ -53,6 +55,17 @@ class _CacheView(ctypes.Structure):
                 ("head_stride", ctypes.c_int64), ("h_req_token_offset", ctypes.POINTER(ctypes.c_int64))]
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class _ContinuationRows(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("table_width", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("n_rows", ctypes.c_int64),
+                ("max_len", ctypes.c_int32), ("h_seq_cu", ctypes.c_void_p), ("h_max_rows", ctypes.c_void_p), ("row_cu", ctypes.c_void_p),
+                ("row_seq", ctypes.c_void_p), ("row_len", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
+
+
 # Argument types of the entry points, declared once so that a call passes plain integers and floats (p pointer or stream,
 # i int32, l int64, z size_t, f float, d double): a ctypes object per argument and a stream object per call were most of
 # the 15 us that a call of a decode step took on the host.
@@ -74,6 +87,11 @@ _SIGNATURES = {
     "relaxkv_qk_norm_rope": (_ST, "pp liii pp f p f p"),
     "relaxkv_qk_norm_rope_append": (_ST, "pp ppp l pp f ppp f p"), "relaxkv_swiglu": (_ST, "pp li p"),
     "relaxkv_target_positions": (_ST, "p pppp p p p"), "relaxkv_carry_rows": (_ST, "p pp i ppp p p"),
+    "relaxkv_continuation_workspace_bytes": (ctypes.c_size_t, "pli"),
+    "relaxkv_build_block_tables": (_ST, "ii pppp i pp i ll pp ppppp p"),
+    "relaxkv_qk_norm_rope_append_paged": (_ST, "p ppp liii pp f pp f pp"),
+    "relaxkv_shared_prefix_attention": (_ST, "pppp ppp pzp"), "relaxkv_block_bounds": (_ST, "pp i pp p"),
+    "relaxkv_select_blocks": (_ST, "p i pp pp iii p pzp"), "relaxkv_block_sparse_attention": (_ST, "pppp ipi ppp pzp"),
     "relaxkv_debug_wait_timeout": (_ST, "p"), "relaxkv_read_device_status": (_ST, "pp p"),
 }
 
@@ -237,6 +255,42 @@ class CacheView:
 
     def ref(self):
         return ctypes.byref(self.c)
+
+
+class PagedStore:
+    """Host-side relaxkv_paged_cache over torch tensors k, v of logical shape [n_blocks, block_size, H_kv, D] (any block, token and head
+    strides, D contiguous)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        assert k.dim() == 4 and k.stride(3) == 1 and k.dtype == torch.bfloat16
+        assert v.shape == k.shape and v.stride() == k.stride() and v.dtype == torch.bfloat16
+        self.k, self.v = k, v
+        self.c = _PagedCache(k.data_ptr(), v.data_ptr(), int(k.stride(0)), int(k.stride(1)), int(k.stride(2)), int(k.shape[1]), int(k.shape[0]))
+
+    @property
+    def block_size(self) -> int:
+        return int(self.k.shape[1])
+
+
+class ContinuationRows:
+    """Host-side relaxkv_continuation_rows: the rows of a step over sequences that continue the contexts (sequences [seq_cu[b], seq_cu[b+1])
+    continue context b; at most max_rows[b] rows of it, max_len own tokens to a row).  The device tensors are those that
+    relaxkv_build_block_tables writes; they are kept alive."""
+
+    def __init__(self, seq_cu: Sequence[int], max_rows: Sequence[int], max_len: int, row_cu: torch.Tensor, row_seq: torch.Tensor,
+                 row_len: Optional[torch.Tensor], block_table: Optional[torch.Tensor]):
+        for t in (row_cu, row_seq, row_len, block_table):
+            assert t is None or t.dtype == torch.int32
+        assert len(max_rows) == len(seq_cu) - 1 and row_cu.numel() == seq_cu[-1] + 1 and row_cu.is_contiguous() and row_seq.is_contiguous()
+        assert row_len is None or (row_len.is_contiguous() and row_len.numel() >= row_seq.numel())
+        assert block_table is None or (block_table.dim() == 2 and block_table.stride(1) == 1 and block_table.shape[0] >= seq_cu[-1])
+        self._keep = (_i32(seq_cu), _i32(max_rows), row_cu, row_seq, row_len, block_table)
+        self.c = _ContinuationRows()
+        self.c.n_seq, self.c.n_rows, self.c.max_len = int(seq_cu[-1]), row_seq.numel(), int(max_len)
+        if block_table is not None:
+            self.c.table_width, self.c.table_stride = int(block_table.shape[1]), max(int(block_table.stride(0)), int(block_table.shape[1]))
+        self.c.h_seq_cu, self.c.h_max_rows = ctypes.addressof(self._keep[0]), ctypes.addressof(self._keep[1])
+        self.c.row_cu, self.c.row_seq, self.c.row_len, self.c.block_table = (_ptr(t) for t in self._keep[2:])
 
 
 def relaxkv_anchor_count(ctx_len: int, ratio: float) -> int:
@@ -460,6 +514,73 @@ def relaxkv_carry_rows(shape: Shape, h_in: torch.Tensor, h_out: torch.Tensor, r_
                        max_next: Sequence[int], stream=None) -> None:
     _check(lib().relaxkv_carry_rows(*_args("spp.ppph.", shape.c, h_in, h_out, int(h_in.shape[1]), r_rank, r_cu_layer, r_cu_next, max_next,
                                            _stream(stream))), "relaxkv_carry_rows")
+
+
+def relaxkv_continuation_workspace_bytes(shape: Shape, n_rows: int, block_size: int = 0) -> int:
+    return int(lib().relaxkv_continuation_workspace_bytes(shape.ref(), int(n_rows), int(block_size)))
+
+
+def relaxkv_build_block_tables(block_size: int, seq_len: torch.Tensor, new_len: torch.Tensor, seq_base: Optional[torch.Tensor],
+                               free_blocks: torch.Tensor, n_free: torch.Tensor, block_table: torch.Tensor, seq_len_out: torch.Tensor,
+                               n_free_out: torch.Tensor, row_cu: torch.Tensor, row_seq: torch.Tensor, row_pos: torch.Tensor,
+                               row_len: torch.Tensor, row_slot: torch.Tensor, stream=None) -> None:
+    """seq_len, new_len, seq_base [n_seq]; block_table [n_seq, width] (rows any distance apart); row_* [n_rows].  All int32."""
+    _check(lib().relaxkv_build_block_tables(*_args("..pppp.pp...ppppppp.", seq_len.numel(), int(block_size), seq_len, new_len, seq_base,
+                                                   free_blocks, free_blocks.numel(), n_free, block_table, block_table.shape[1],
+                                                   max(block_table.stride(0), block_table.shape[1]), row_seq.numel(), seq_len_out, n_free_out,
+                                                   row_cu, row_seq, row_pos, row_len, row_slot, _stream(stream))),
+           "relaxkv_build_block_tables")
+
+
+def relaxkv_qk_norm_rope_append_paged(store: PagedStore, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                                      slots: torch.Tensor, theta: float, q_out: torch.Tensor, w_q_norm: Optional[torch.Tensor] = None,
+                                      w_k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
+    """q_out [n, H, D] = normed and rotated q (may be q); the store receives the normed and rotated k and v [n, H_kv, D] at `slots`."""
+    _check(lib().relaxkv_qk_norm_rope_append_paged(*_args("sppp....pp.pp.p.", store.c, q, k, v, q.shape[0], q.shape[1], k.shape[1], q.shape[2],
+                                                          w_q_norm, w_k_norm, float(eps), positions, slots, float(theta), q_out,
+                                                          _stream(stream))), "relaxkv_qk_norm_rope_append_paged")
+
+
+def _optional(struct):
+    return None if struct is None else struct.c
+
+
+def _codes(before: str, cache, store, behind: str) -> str:
+    """Argument codes with a cache and a store between them that may be missing."""
+    return before + ("." if cache is None else "s") + ("." if store is None else "s") + behind
+
+
+def relaxkv_shared_prefix_attention(shape: Shape, cache: Optional[CacheView], store: Optional[PagedStore], rows: ContinuationRows,
+                                    q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                                    stream=None) -> None:
+    """cache: the contexts (None where all are empty); store: the sequences' own tokens (None where rows.max_len is 0)."""
+    _check(lib().relaxkv_shared_prefix_attention(*_args(_codes("s", cache, store, "spppp.."), shape.c, _optional(cache), _optional(store),
+                                                        rows.c, q, out, lse_out, workspace, workspace.nbytes, _stream(stream))),
+           "relaxkv_shared_prefix_attention")
+
+
+def relaxkv_block_bounds(shape: Shape, cache: CacheView, block_size: int, bounds_out: torch.Tensor, scale_out: torch.Tensor,
+                         stream=None) -> None:
+    """bounds_out int8 [sum of the contexts' blocks, H_kv, 2, D], scale_out fp32 [.., H_kv]."""
+    _check(lib().relaxkv_block_bounds(*_args("ss.pp.", shape.c, cache.c, int(block_size), bounds_out, scale_out, _stream(stream))),
+           "relaxkv_block_bounds")
+
+
+def relaxkv_select_blocks(shape: Shape, block_size: int, bounds: torch.Tensor, scale: torch.Tensor, rows: ContinuationRows, q: torch.Tensor,
+                          n_first: int, n_last: int, blocks_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """blocks_out int32 [n_rows, H_kv, n_select]."""
+    _check(lib().relaxkv_select_blocks(*_args("s.ppsp...pp..", shape.c, int(block_size), bounds, scale, rows.c, q, blocks_out.shape[2],
+                                              int(n_first), int(n_last), blocks_out, workspace, workspace.nbytes, _stream(stream))),
+           "relaxkv_select_blocks")
+
+
+def relaxkv_block_sparse_attention(shape: Shape, cache: Optional[CacheView], store: Optional[PagedStore], rows: ContinuationRows,
+                                   block_size: int, blocks: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                                   lse_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """blocks int32 [n_rows, H_kv, n_select]: the context blocks that each row and KV head reads."""
+    _check(lib().relaxkv_block_sparse_attention(*_args(_codes("s", cache, store, "s.p.pppp.."), shape.c, _optional(cache), _optional(store),
+                                                       rows.c, int(block_size), blocks, blocks.shape[2], q, out, lse_out, workspace,
+                                                       workspace.nbytes, _stream(stream))), "relaxkv_block_sparse_attention")
 
 
 def relaxkv_debug_wait_timeout(stream=None) -> None:

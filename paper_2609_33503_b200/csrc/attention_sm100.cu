@@ -23,6 +23,7 @@
 // device status word and the block tears down normally.
 #include "attention_common.cuh"
 #include "attention_pieces.cuh"
+#include "continuations.cuh"
 #include "decode_attention.cuh"
 #include "sm100_ptx.cuh"
 #include <algorithm>
@@ -1246,6 +1247,19 @@ bool make_map_3d(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uin
   const cuuint32_t box[3] = {64u, b1, b2};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool make_block_map(CUtensorMap* m, const void* base, int D, uint64_t tokens, int n_kv_heads, uint64_t blocks, uint64_t token_stride,
+                    uint64_t head_stride, uint64_t block_stride, uint32_t box) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[5] = {64, tokens, (cuuint64_t)(D / 64), (cuuint64_t)n_kv_heads, blocks};
+  const cuuint64_t strides[4] = {token_stride * 2, 128, head_stride * 2, block_stride * 2};
+  const cuuint32_t sizes[5] = {64u, box, (cuuint32_t)(D / 64), 1u, 1u};
+  const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, sizes, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

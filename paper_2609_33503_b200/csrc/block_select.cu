@@ -1,0 +1,438 @@
+// Context blocks by a cheap score: 8-bit bounds of every block's keys (relaxkv_block_bounds), and the blocks of the highest possible logit for
+// each row and KV head (relaxkv_select_blocks).
+//
+// Bounds: one pass over K, bound by its bytes.  A warp has one (block, KV head): 16 lanes hold the 128 dims of a token as 16-byte pieces, so
+// a load takes two tokens (four of 64 dims); maxima and minima stay packed bf16 pairs and are exact.  The scale is a power of two, so are the
+// quotients, and the rounding is away from the block: the bounds remain bounds.
+// Scores: sum_d max(q_d hi_d, q_d lo_d) = q+ . hi + q- . lo, a product over 2 D bytes on the tensor cores (m16n8k32, s8): rows are the heads of two
+// rows of the step (of one with more than eight heads to a KV head), columns eight blocks.  The product's terms may come in any order as long as both
+// sides agree, so a lane takes D / 2 bytes of its block in 16-byte loads and the queries are laid out to match.  Sums are whole numbers below 2^24:
+// the scores, and with them the lists, do not depend on the order of anything.
+// Selection: one block per (row, KV head); radix passes of 11, 11 and 10 bits find the lowest selected score, then every thread writes its
+// own range's blocks in order.
+#include "continuations.cuh"
+#include <algorithm>
+
+namespace relaxkv {
+
+__device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t bmin2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// Exponent of the smallest power of two s with |x| <= 127 s, for the bits of a finite bf16 |x|: 127 = 1.984375 * 2^6, and the next mantissa after
+// that one is the last (0x7f), so adding one to the bits carries exactly when |x| is above it.  From -100 on; 0 for 0.
+__device__ __forceinline__ int scale_exponent(uint32_t abs_bits) {
+  return abs_bits == 0 ? 0 : max(-100, (int)((abs_bits + 1) >> 7) - 127 - 6);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // -100 <= e <= 127
+
+constexpr int kBndThreads = 256;
+
+// KEYS: key tokens of a block, known at compile time so that the loads of eight steps travel together.
+template <int D>
+__global__ void __launch_bounds__(kBndThreads)
+block_bounds_kernel(const uint16_t* k, long long token_stride, long long head_stride, const __grid_constant__ ContTable ct, int block_size, int Hkv,
+                    int8_t* bounds, float* scale, int heads_outer) {
+  constexpr int kLanes = D / 8, kTok = 32 / kLanes, U = 8;
+  const int lane = threadIdx.x & 31, gl = lane % kLanes, sub = lane / kLanes;
+  const long long w = (long long)blockIdx.x * (kBndThreads / 32) + (threadIdx.x >> 5);
+  const int n_blocks = ct.blk_cu[ct.n_req];
+  griddep_launch();
+  griddep_wait();
+  if (w >= (long long)n_blocks * Hkv) return;
+  // warps side by side read what lies side by side in memory
+  const int x = heads_outer ? (int)(w % n_blocks) : (int)(w / Hkv), g = heads_outer ? (int)(w / n_blocks) : (int)(w % Hkv);
+  int b = 0;
+  for (int hi = ct.n_req; hi - b > 1;) { const int mid = (b + hi) >> 1; if (ct.blk_cu[mid] <= x) b = mid; else hi = mid; }
+  const long long first = (long long)(x - ct.blk_cu[b]) * block_size;
+  const int n = (int)min((long long)block_size, ct.ctx_len[b] - first);
+  const uint16_t* p = k + (ct.tok_off[b] + first) * token_stride + g * head_stride + gl * 8;
+  uint32_t mx[4], mn[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { mx[e] = 0x7fff7fffu; mn[e] = 0x7fff7fffu; }       // NaN: passed over by both
+  for (int t0 = 0; t0 < n; t0 += U * kTok) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * kTok + sub;
+      v[u] = t < n ? *reinterpret_cast<const uint4*>(p + t * token_stride) : make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      mx[0] = bmax2(mx[0], v[u].x); mx[1] = bmax2(mx[1], v[u].y); mx[2] = bmax2(mx[2], v[u].z); mx[3] = bmax2(mx[3], v[u].w);
+      mn[0] = bmin2(mn[0], v[u].x); mn[1] = bmin2(mn[1], v[u].y); mn[2] = bmin2(mn[2], v[u].z); mn[3] = bmin2(mn[3], v[u].w);
+    }
+  }
+#pragma unroll
+  for (int o = kLanes; o < 32; o <<= 1) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      mx[e] = bmax2(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], o));
+      mn[e] = bmin2(mn[e], __shfl_xor_sync(0xffffffffu, mn[e], o));
+    }
+  }
+  // the largest magnitude among all dims (NaN, where a dim has nothing else, counts as 0)
+  uint32_t amax = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const uint32_t m1 = (mx[e] >> h) & 0x7fffu, m2 = (mn[e] >> h) & 0x7fffu;
+      if (m1 <= 0x7f80u) amax = max(amax, m1);
+      if (m2 <= 0x7f80u) amax = max(amax, m2);
+    }
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  const int ex = scale_exponent(min(amax, 0x7f7fu));               // an infinity is clamped below
+  const float inv = power_of_two(-ex);                             // ex <= 122
+  auto quantise = [&](uint32_t bits, bool up) -> uint32_t {
+    const float f = bf16_bits_to_float((uint16_t)bits) * inv;      // exact, or below the smallest normal number times a power of two
+    const float r = up ? ceilf(f) : floorf(f);
+    return (uint32_t)(uint8_t)(int8_t)(int)fminf(fmaxf(r, -127.f), 127.f);
+  };
+  if (sub == 0) {
+    uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bh = (mx[e >> 1] >> ((e & 1) * 16)) & 0xffffu, bl = (mn[e >> 1] >> ((e & 1) * 16)) & 0xffffu;
+      hi[e >> 2] |= ((bh & 0x7fffu) > 0x7f80u ? 0u : quantise(bh, true)) << ((e & 3) * 8);
+      lo[e >> 2] |= ((bl & 0x7fffu) > 0x7f80u ? 0u : quantise(bl, false)) << ((e & 3) * 8);
+    }
+    int8_t* o = bounds + ((long long)x * Hkv + g) * (2 * D) + gl * 8;
+    *reinterpret_cast<uint2*>(o) = make_uint2(hi[0], hi[1]);
+    *reinterpret_cast<uint2*>(o + D) = make_uint2(lo[0], lo[1]);
+    if (gl == 0) scale[(long long)x * Hkv + g] = power_of_two(ex);
+  }
+}
+
+// ---- scores ---------------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void mma_s8_16832(int* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+struct SelectArgs {
+  const int8_t* bounds;
+  const float* scale;
+  const uint16_t* q;
+  const int *row_cu, *row_seq;
+  float* scores;                       // [n_rows, H_kv, most]
+  int* out;                            // [n_rows, H_kv, n_select]
+  long long n_rows;
+  int most, H, Hkv, n_seq, block_size, n_select, n_first, n_last;
+};
+
+// Rows of context b in the step; n < 0: more than the host's bounds.
+struct RowRange { long long first; int n; };
+__device__ __forceinline__ RowRange rows_of(const SelectArgs& a, const ContTable& ct, int b) {
+  const long long r0 = a.row_cu[ct.seq_cu[b]], r1 = a.row_cu[ct.seq_cu[b + 1]];
+  if (r0 < 0 || r1 < r0 || r1 > a.n_rows || r1 - r0 > ct.max_rows[b]) return {0, -1};
+  return {r0, (int)(r1 - r0)};
+}
+
+constexpr int kScoWarps = 4;
+constexpr int kScoPass = 8;             // row tiles whose queries a block holds at once
+
+// A block: eight context blocks per warp, one KV head, all rows of the context.  PAIR: two rows of the step to an MMA (groups of up to eight heads).
+template <int D, bool PAIR>
+__global__ void __launch_bounds__(kScoWarps * 32)
+block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
+  constexpr int kSteps = 2 * D / 32;                                // MMAs of a product
+  constexpr int kRowsPer = PAIR ? 2 : 1, kSlots = PAIR ? 8 : 16;    // rows of the step per tile, fragment rows of each
+  __shared__ __align__(16) uint32_t q_s[kScoPass][16][2 * D / 4 + 4];      // [tile][fragment row][q+ | q-]; the rows 16 bytes apart from whole banks
+  __shared__ float sq_s[kScoPass][16];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const int G = a.H / a.Hkv;
+  const int hd = blockIdx.y;
+  int b = 0;
+  for (int hi = ct.n_req; hi - b > 1;) { const int mid = (b + hi) >> 1; if (ct.tile_cu[mid] <= (int)blockIdx.x) b = mid; else hi = mid; }
+  const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b], x0 = (((int)blockIdx.x - ct.tile_cu[b]) * kScoWarps + warp) * 8;
+  griddep_launch();
+  griddep_wait();
+  const RowRange rr = rows_of(a, ct, b);
+  if (rr.n < 0 && threadIdx.x == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, b, ct.max_rows[b]);
+  if (rr.n <= 0) return;
+  // this lane's share of its block's 2 D bytes: bytes [tig D / 2, + D / 2)
+  const int x = x0 + gid;
+  uint32_t bd[D / 8];
+  {
+    const uint4* p = reinterpret_cast<const uint4*>(a.bounds + ((long long)(ct.blk_cu[b] + min(x, nb - 1)) * a.Hkv + hd) * (2 * D) + tig * (D / 2));
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint4 v = p[i];
+      bd[4 * i] = v.x; bd[4 * i + 1] = v.y; bd[4 * i + 2] = v.z; bd[4 * i + 3] = v.w;
+    }
+  }
+  float sb[2];                                                       // scales of the blocks of this lane's result columns
+#pragma unroll
+  for (int e = 0; e < 2; ++e) sb[e] = a.scale[(long long)(ct.blk_cu[b] + min(x0 + 2 * tig + e, nb - 1)) * a.Hkv + hd];
+  const int n_tiles = (rr.n + kRowsPer - 1) / kRowsPer;
+  for (int p0 = 0; p0 < n_tiles; p0 += kScoPass) {
+    const int here = min(kScoPass, n_tiles - p0);
+    __syncthreads();
+    // queries in 8 bits: a warp per fragment row, D / 32 dims per lane
+    for (int i = warp; i < here * 16; i += kScoWarps) {
+      const int tile = i >> 4, fr = i & 15, r = (p0 + tile) * kRowsPer + (PAIR ? fr >> 3 : 0), h = PAIR ? fr & 7 : fr;
+      constexpr int kPer = D / 32;
+      uint32_t raw[kPer / 2];
+#pragma unroll
+      for (int e = 0; e < kPer / 2; ++e) raw[e] = 0u;
+      const bool live = h < G && r < rr.n;
+      if (live) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q + ((rr.first + r) * a.H + hd * G + h) * D + lane * kPer);
+#pragma unroll
+        for (int e = 0; e < kPer / 2; ++e) raw[e] = p[e];
+      }
+      uint32_t amax = 0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const uint32_t m = (raw[e >> 1] >> ((e & 1) * 16)) & 0x7fffu;
+        if (m <= 0x7f80u) amax = max(amax, m);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      const int ex = scale_exponent(min(amax, 0x7f7fu));
+      const float inv = power_of_two(-ex);
+      uint32_t pos = 0, neg = 0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const uint32_t bits = (raw[e >> 1] >> ((e & 1) * 16)) & 0xffffu;
+        const float f = (bits & 0x7fffu) > 0x7f80u ? 0.f : fminf(fmaxf(rintf(bf16_bits_to_float((uint16_t)bits) * inv), -127.f), 127.f);
+        pos |= (uint32_t)(uint8_t)(int8_t)(int)fmaxf(f, 0.f) << (e * 8);
+        neg |= (uint32_t)(uint8_t)(int8_t)(int)fminf(f, 0.f) << (e * 8);
+      }
+      uint8_t* row = reinterpret_cast<uint8_t*>(q_s[tile][fr]);
+      if constexpr (kPer == 4) {
+        *reinterpret_cast<uint32_t*>(row + lane * 4) = pos;
+        *reinterpret_cast<uint32_t*>(row + D + lane * 4) = neg;
+      } else {
+        *reinterpret_cast<uint16_t*>(row + lane * 2) = (uint16_t)pos;
+        *reinterpret_cast<uint16_t*>(row + D + lane * 2) = (uint16_t)neg;
+      }
+      if (lane == 0) sq_s[tile][fr] = live ? power_of_two(ex) : -1.f;           // no such row or head
+    }
+    __syncthreads();
+    if (x0 >= nb) continue;
+    for (int tile = 0; tile < here; ++tile) {
+      int acc[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const uint2 qa = *reinterpret_cast<const uint2*>(&q_s[tile][gid][tig * (D / 8) + 2 * s]);
+        const uint2 qb = *reinterpret_cast<const uint2*>(&q_s[tile][gid + 8][tig * (D / 8) + 2 * s]);
+        const uint32_t fa[4] = {qa.x, qb.x, qa.y, qb.y};
+        mma_s8_16832(acc, fa, bd[2 * s], bd[2 * s + 1]);
+      }
+      // the largest over the heads of a row: fragment rows lie 4 lanes apart
+      float best[2][2];
+      const float s0 = sq_s[tile][gid], s1 = sq_s[tile][gid + 8];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        best[0][e] = s0 > 0.f ? (float)acc[e] * s0 : -INFINITY;
+        best[1][e] = s1 > 0.f ? (float)acc[2 + e] * s1 : -INFINITY;
+        if (!PAIR) best[0][e] = fmaxf(best[0][e], best[1][e]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          best[0][e] = fmaxf(best[0][e], __shfl_xor_sync(0xffffffffu, best[0][e], o));
+          if (PAIR) best[1][e] = fmaxf(best[1][e], __shfl_xor_sync(0xffffffffu, best[1][e], o));
+        }
+      }
+      if (gid < kRowsPer) {
+        const int r = (p0 + tile) * kRowsPer + gid;
+        if (r < rr.n) {
+          float* o = a.scores + ((rr.first + r) * a.Hkv + hd) * a.most;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int xx = x0 + 2 * tig + e;
+            if (xx < nb) {
+              const bool forced = xx < a.n_first || xx >= nb - a.n_last;
+              o[xx] = forced ? INFINITY : best[gid][e] * sb[e] + 0.f;           // (+ 0: one zero, not two)
+            }
+          }
+        }
+      }
+    }
+  }
+  (void)kSlots;
+}
+
+// ---- the n_select highest scores of a (row, KV head) ------------------------------------------------------------------------------
+
+constexpr int kTopThreads = 256;
+
+// Order-preserving key of a score (no NaN: scores are products of whole numbers and powers of two).
+__device__ __forceinline__ uint32_t score_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(kTopThreads)
+block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
+  constexpr int kBins = 2048, kBinsPer = kBins / kTopThreads, kWarps = kTopThreads / 32;
+  __shared__ int hist[kBins];
+  __shared__ int warp_sum[kWarps], found[2];
+  __shared__ int2 warp_pair[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int hd = (int)(blockIdx.x % a.Hkv);
+  const long long row = blockIdx.x / a.Hkv;
+  griddep_launch();
+  griddep_wait();
+  const int seq = a.row_seq[row];
+  if (seq == -1) return;
+  if (seq < 0 || seq >= a.n_seq) {
+    if (tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, seq, (int)row);
+    return;
+  }
+  const int b = context_of(ct, seq), nb = ct.blk_cu[b + 1] - ct.blk_cu[b];
+  const RowRange rr = rows_of(a, ct, b);
+  if (rr.n < 0 || row < rr.first || row >= rr.first + rr.n) return;             // reported above, or no row of this context
+  int* out = a.out + (row * a.Hkv + hd) * a.n_select;
+  if (nb <= a.n_select) {                                                        // all of them
+    for (int i = tid; i < a.n_select; i += kTopThreads) out[i] = i < nb ? i : -1;
+    return;
+  }
+  const float* score = a.scores + (row * a.Hkv + hd) * a.most;
+  // ---- the n_select-th highest key: 11, 11 and 10 bits at a time ----
+  uint32_t prefix = 0;
+  int want = a.n_select;                                                         // of the keys that share the prefix, the want-th highest
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    for (int i = tid; i < kBins; i += kTopThreads) hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < nb; i += kTopThreads) {
+      const uint32_t key = score_key(score[i]);
+      if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1);
+    }
+    __syncthreads();
+    // bins from the highest: thread t has bins [top - kBinsPer t - kBinsPer + 1, top - kBinsPer t]
+    const int top = (1 << bits) - 1;
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < kBinsPer; ++e) { const int bin = top - tid * kBinsPer - e; mine += bin >= 0 ? hist[bin] : 0; }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int before = incl - mine;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (before < want && before + mine >= want) {                                // exactly one thread
+      int acc = before;
+#pragma unroll
+      for (int e = 0; e < kBinsPer; ++e) {
+        const int bin = top - tid * kBinsPer - e;
+        if (bin < 0) break;
+        if (acc + hist[bin] >= want) { found[0] = bin; found[1] = want - acc; break; }
+        acc += hist[bin];
+      }
+    }
+    __syncthreads();
+    prefix = pass == 0 ? (uint32_t)found[0] : (prefix << bits) | (uint32_t)found[0];
+    want = found[1];
+  }
+  // ---- keys above the last one, and of the equal ones the first `want`: every thread a range in order ----
+  const int per = (nb + kTopThreads - 1) / kTopThreads, i0 = min(nb, tid * per), i1 = min(nb, i0 + per);
+  int above = 0, equal = 0;
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t key = score_key(score[i]);
+    above += key > prefix;
+    equal += key == prefix;
+  }
+  int ia = above, ie = equal;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int va = __shfl_up_sync(0xffffffffu, ia, o), ve = __shfl_up_sync(0xffffffffu, ie, o);
+    if (lane >= o) { ia += va; ie += ve; }
+  }
+  if (lane == 31) warp_pair[warp] = make_int2(ia, ie);
+  __syncthreads();
+  ia -= above; ie -= equal;
+  for (int w = 0; w < warp; ++w) { ia += warp_pair[w].x; ie += warp_pair[w].y; }
+  int at = ia + min(ie, want);
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t key = score_key(score[i]);
+    if (key > prefix) out[at++] = i;
+    else if (key == prefix && ie++ < want) out[at++] = i;
+  }
+}
+
+}  // namespace relaxkv
+
+using namespace relaxkv;
+
+extern "C" relaxkv_status relaxkv_block_bounds(const relaxkv_shape* shape, const relaxkv_cache_view* cache, int32_t block_size, int8_t* bounds_out,
+                                               float* scale_out, relaxkv_stream stream) {
+  RELAXKV_RANGE("relaxkv_block_bounds");
+  relaxkv_status rc = check_contexts(shape);
+  if (rc != RELAXKV_OK) return rc;
+  if (!block_size_ok(block_size)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  long long blocks = 0;
+  for (int b = 0; b < shape->n_req; ++b) blocks += ((long long)shape->h_ctx_len[b] + block_size - 1) / block_size;
+  if (blocks == 0) return RELAXKV_OK;
+  if ((rc = check_cache(shape, cache, false)) != RELAXKV_OK) return rc;
+  if (!bounds_out || !scale_out || !aligned16(bounds_out)) return RELAXKV_ERR_INVALID_ARG;
+  const int Hkv = shape->n_kv_heads, D = shape->head_dim;
+  if (blocks * Hkv > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  ContTable ct;
+  fill_contexts(ct, shape, cache, block_size);
+  const unsigned grid = (unsigned)((blocks * Hkv + kBndThreads / 32 - 1) / (kBndThreads / 32));
+  auto kern = D == 128 ? block_bounds_kernel<128> : block_bounds_kernel<64>;
+  return cuda_ok(launch_chained(kern, dim3(grid), kBndThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const uint16_t*>(cache->k),
+                                (long long)cache->token_stride, (long long)cache->head_stride, ct, block_size, Hkv, bounds_out, scale_out,
+                                cache->head_stride > cache->token_stride ? 1 : 0));
+}
+
+extern "C" relaxkv_status relaxkv_select_blocks(
+    const relaxkv_shape* shape, int32_t block_size, const int8_t* bounds, const float* scale, const relaxkv_continuation_rows* rows, const void* q,
+    int32_t n_select, int32_t n_first, int32_t n_last, int32_t* blocks_out, void* workspace, size_t workspace_bytes, relaxkv_stream stream) {
+  RELAXKV_RANGE("relaxkv_select_blocks");
+  relaxkv_status rc = check_contexts(shape);
+  if (rc != RELAXKV_OK) return rc;
+  if (!block_size_ok(block_size)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  if (n_select < 1 || n_first < 0 || n_last < 0 || (long long)n_first + n_last > n_select) return RELAXKV_ERR_INVALID_ARG;
+  ContTable ct;
+  long long blocks = 0;
+  for (int b = 0; b < shape->n_req; ++b) blocks += ((long long)shape->h_ctx_len[b] + block_size - 1) / block_size;
+  if (blocks * shape->n_kv_heads > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  fill_contexts(ct, shape, nullptr, block_size);
+  if ((rc = check_rows(shape, rows, false, ct)) != RELAXKV_OK) return rc;
+  if (!q || !aligned16(q) || !blocks_out || !workspace || (blocks > 0 && (!bounds || !scale || !aligned16(bounds)))) return RELAXKV_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return RELAXKV_ERR_INVALID_ARG;
+  if (workspace_bytes < cont_ws(shape, rows->n_rows, block_size).total) return RELAXKV_ERR_WORKSPACE_TOO_SMALL;
+  if (rows->n_rows == 0) return RELAXKV_OK;
+  if (rows->n_rows * shape->n_kv_heads > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  DeviceStatus* st = status_word();
+  if (!st) return RELAXKV_ERR_CUDA;
+  SelectArgs a = {};
+  a.bounds = bounds; a.scale = scale; a.q = static_cast<const uint16_t*>(q);
+  a.row_cu = rows->row_cu; a.row_seq = rows->row_seq;
+  a.scores = static_cast<float*>(workspace); a.out = blocks_out; a.n_rows = rows->n_rows;
+  a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.n_seq = rows->n_seq; a.block_size = block_size;
+  a.n_select = n_select; a.n_first = n_first; a.n_last = n_last;
+  for (int b = 0; b < ct.n_req; ++b) {
+    const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b];
+    a.most = std::max(a.most, nb);
+    // contexts of no more blocks than are selected need no scores
+    ct.tile_cu[b + 1] = ct.tile_cu[b] + (nb > n_select && ct.max_rows[b] > 0 ? (nb + 8 * kScoWarps - 1) / (8 * kScoWarps) : 0);
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int D = shape->head_dim;
+  if (a.Hkv > 65535) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  if (ct.tile_cu[ct.n_req] > 0) {
+    const bool pair = a.H / a.Hkv <= 8;
+    auto kern = D == 128 ? (pair ? block_score_kernel<128, true> : block_score_kernel<128, false>)
+                         : (pair ? block_score_kernel<64, true> : block_score_kernel<64, false>);
+    rc = cuda_ok(launch_chained(kern, dim3((unsigned)ct.tile_cu[ct.n_req], (unsigned)a.Hkv), kScoWarps * 32, 0, s, ct, a, st));
+    if (rc != RELAXKV_OK) return rc;
+  }
+  return cuda_ok(launch_chained(block_topk_kernel, dim3((unsigned)(a.n_rows * a.Hkv)), kTopThreads, 0, s, ct, a, st));
+}

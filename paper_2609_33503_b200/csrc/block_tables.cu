@@ -1,0 +1,174 @@
+// Block tables and slot maps of a step over continuations, from the sequences' lengths (relaxkv_build_block_tables).
+//
+// Three running sums over the sequences decide everything: rows appended, blocks needed, blocks given back.  They are a few thousand
+// numbers, so every block of the launch computes them for itself from the lengths (all in L2) and then writes its share of the outputs: rows,
+// new table entries and what is left of the released blocks, each found by bisection in the sums.  No block waits for another and there is one
+// launch.  Entries that are read (blocks a sequence has, free blocks below n_free) are never entries that are written, which is what lets the
+// blocks of the launch run in any order and the call be repeated.
+#include "continuations.cuh"
+#include <algorithm>
+
+namespace relaxkv {
+
+constexpr int kTabMaxSeq = 4096;
+constexpr int kTabThreads = 512;
+
+struct TableArgs {
+  int n_seq, block_size, free_capacity, table_width;
+  long long table_stride, n_rows;
+  const int *seq_len, *new_len, *seq_base, *n_free;
+  int *free_blocks, *table, *seq_len_out, *n_free_out, *row_cu, *row_seq, *row_pos, *row_len, *row_slot;
+};
+
+__device__ __forceinline__ int blocks_of(int tokens, int shift) { return (int)(((long long)tokens + (1 << shift) - 1) >> shift); }
+
+// The segment of cu[0 .. n] that x lies in: the last i with cu[i] <= x (empty segments are passed over).
+__device__ __forceinline__ int bisect(const int* cu, int n, int x) {
+  int lo = 0;
+  for (int hi = n; hi - lo > 1;) { const int mid = (lo + hi) >> 1; if (cu[mid] <= x) lo = mid; else hi = mid; }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kTabThreads)
+block_tables_kernel(const TableArgs a, DeviceStatus* st) {
+  extern __shared__ int cu_s[];
+  int *rows_cu = cu_s, *need_cu = cu_s + a.n_seq + 1, *back_cu = need_cu + a.n_seq + 1;
+  __shared__ long long warp_rows[kTabThreads / 32];
+  __shared__ int warp_need[kTabThreads / 32], warp_back[kTabThreads / 32];
+  griddep_launch();
+  griddep_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = (int)blockDim.x >> 5;
+  const int shift = 31 - __clz(a.block_size);
+  const bool teller = blockIdx.x == 0;
+  const int per = (a.n_seq + (int)blockDim.x - 1) / (int)blockDim.x, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
+  const long long room = min((long long)a.table_width << shift, 0x7fffffffLL);
+  const int n_free = *a.n_free;
+  // a sequence's share of the sums; what it asks for and cannot have counts as nothing
+  auto share = [&](int i, bool tell, int& rows, int& need, int& back) {
+    const int len = a.seq_len[i], add = a.new_len[i];
+    rows = need = back = 0;
+    const bool ok = len >= 0 && len <= room && add <= a.n_rows && (long long)len + max(add, 0) <= room;
+    if (!ok) { if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, i, add); }
+    else if (add < 0) back = blocks_of(len, shift);
+    else { rows = add; need = blocks_of(len + add, shift) - blocks_of(len, shift); }
+  };
+  // ---- the sums: this thread's sequences, its warp's threads, the block's warps ----
+  long long rows_t = 0;
+  int need_t = 0, back_t = 0;
+  for (int i = first; i < last; ++i) {
+    int r, n, k;
+    share(i, teller, r, n, k);
+    rows_t += r; need_t += n; back_t += k;
+  }
+  long long rows_x = rows_t;
+  int need_x = need_t, back_x = back_t;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long r = __shfl_up_sync(0xffffffffu, rows_x, o);
+    const int n = __shfl_up_sync(0xffffffffu, need_x, o), k = __shfl_up_sync(0xffffffffu, back_x, o);
+    if (lane >= o) { rows_x += r; need_x += n; back_x += k; }
+  }
+  if (lane == 31) { warp_rows[warp] = rows_x; warp_need[warp] = need_x; warp_back[warp] = back_x; }
+  __syncthreads();
+  long long rows_before = 0, total_rows = 0;
+  int need_before = 0, back_before = 0, total_need = 0, total_back = 0;
+  for (int w = 0; w < n_warps; ++w) {
+    if (w < warp) { rows_before += warp_rows[w]; need_before += warp_need[w]; back_before += warp_back[w]; }
+    total_rows += warp_rows[w]; total_need += warp_need[w]; total_back += warp_back[w];
+  }
+  // (the sums of the blocks fit 32 bits: a table of 2^31 entries or more is refused on the host)
+  const bool nothing = n_free < 0 || (long long)n_free + total_back > a.free_capacity;
+  const bool full = !nothing && (total_rows > a.n_rows || total_need > n_free + total_back);
+  if (teller && tid == 0 && (nothing || full)) report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, nothing ? -1 : -2, nothing ? n_free : total_need);
+  const bool grow = !nothing && !full;
+  if (nothing) total_back = 0;
+  if (!grow) { total_rows = 0; total_need = 0; }
+  {
+    long long rows_at = rows_before + rows_x - rows_t;
+    int need_at = need_before + need_x - need_t, back_at = back_before + back_x - back_t;
+    for (int i = first; i < last; ++i) {
+      int r, n, k;
+      share(i, false, r, n, k);
+      rows_cu[i] = grow ? (int)rows_at : 0;
+      need_cu[i] = grow ? need_at : 0;
+      back_cu[i] = nothing ? 0 : back_at;
+      rows_at += r; need_at += n; back_at += k;
+      if (teller) {
+        a.row_cu[i] = rows_cu[i];
+        a.seq_len_out[i] = !nothing && k > 0 ? 0 : a.seq_len[i] + (grow ? r : 0);
+      }
+    }
+  }
+  if (tid == 0) { rows_cu[a.n_seq] = (int)total_rows; need_cu[a.n_seq] = total_need; back_cu[a.n_seq] = total_back; }
+  if (teller && tid == 0) { a.row_cu[a.n_seq] = (int)total_rows; *a.n_free_out = nothing ? n_free : n_free + total_back - total_need; }
+  __syncthreads();
+  // ---- the outputs ----
+  const int top = n_free + total_back;
+  auto released = [&](int j) -> int {
+    const int i = bisect(back_cu, a.n_seq, j);
+    return a.table[i * a.table_stride + (j - back_cu[i])];
+  };
+  auto taken = [&](int j) -> int {               // the j-th block of the stack from its end
+    const int at = top - 1 - j;
+    return at < n_free ? a.free_blocks[at] : released(at - n_free);
+  };
+  const long long step = (long long)gridDim.x * blockDim.x, me = (long long)blockIdx.x * blockDim.x + tid;
+  for (long long j = me; j < total_need; j += step) {
+    const int i = bisect(need_cu, a.n_seq, (int)j);
+    a.table[i * a.table_stride + blocks_of(a.seq_len[i], shift) + ((int)j - need_cu[i])] = taken((int)j);
+  }
+  for (long long j = n_free + me; j < top - total_need; j += step) a.free_blocks[j] = released((int)j - n_free);
+  for (long long r = me; r < a.n_rows; r += step) {
+    int seq = -1, pos = 0, len = 0, slot = -1;
+    if (r < total_rows) {
+      seq = bisect(rows_cu, a.n_seq, (int)r);
+      const int had = a.seq_len[seq], at = had + ((int)r - rows_cu[seq]), have = blocks_of(had, shift), j = at >> shift;
+      const int block = j < have ? a.table[seq * a.table_stride + j] : taken(need_cu[seq] + (j - have));
+      len = at + 1;
+      pos = (a.seq_base ? a.seq_base[seq] : 0) + at;
+      slot = block < 0 ? -1 : (int)(((unsigned)block << shift) + (at & ((1 << shift) - 1)));
+      if (block < 0 || ((long long)block << shift) > 0x7fffffffLL - (1 << shift)) {
+        slot = -1;
+        report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, seq, block);
+      }
+    }
+    a.row_seq[r] = seq;
+    a.row_pos[r] = pos;
+    a.row_len[r] = len;
+    a.row_slot[r] = slot;
+  }
+}
+
+}  // namespace relaxkv
+
+using namespace relaxkv;
+
+extern "C" relaxkv_status relaxkv_build_block_tables(
+    int32_t n_seq, int32_t block_size, const int32_t* seq_len, const int32_t* new_len, const int32_t* seq_base, int32_t* free_blocks,
+    int32_t free_capacity, const int32_t* n_free, int32_t* block_table, int32_t table_width, int64_t table_stride, int64_t n_rows,
+    int32_t* seq_len_out, int32_t* n_free_out, int32_t* row_cu, int32_t* row_seq, int32_t* row_pos, int32_t* row_len, int32_t* row_slot,
+    relaxkv_stream stream) {
+  RELAXKV_RANGE("relaxkv_build_block_tables");
+  if (!seq_len || !new_len || !free_blocks || !n_free || !block_table || !seq_len_out || !n_free_out || !row_cu) return RELAXKV_ERR_INVALID_ARG;
+  if (n_seq < 1 || n_rows < 0 || free_capacity < 0 || table_width < 1 || table_stride < table_width) return RELAXKV_ERR_INVALID_ARG;
+  if (n_rows > 0 && (!row_seq || !row_pos || !row_len || !row_slot)) return RELAXKV_ERR_INVALID_ARG;
+  // the blocks of the launch read these while others may already write the results
+  if (seq_len_out == seq_len || seq_len_out == new_len || n_free_out == n_free) return RELAXKV_ERR_INVALID_ARG;
+  if (!block_size_ok(block_size) || n_seq > kTabMaxSeq) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  if (n_rows > 0x7fffffffLL || (long long)n_seq * table_width > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  DeviceStatus* st = status_word();
+  const int sms = sm_count_of_current_device();
+  if (!st || sms <= 0) return RELAXKV_ERR_CUDA;
+  static std::atomic<int> attr_done[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
+  if (!attr_done[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * 4 * (kTabMaxSeq + 1)) != cudaSuccess)
+      return RELAXKV_ERR_CUDA;
+    attr_done[dev].store(1, std::memory_order_release);
+  }
+  const TableArgs a = {n_seq, block_size, free_capacity, table_width, (long long)table_stride, (long long)n_rows, seq_len, new_len, seq_base, n_free,
+                       free_blocks, block_table, seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot};
+  const long long blocks = std::max<long long>(1, std::min<long long>(2LL * sms, (n_rows + kTabThreads - 1) / kTabThreads));
+  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), kTabThreads, 3 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
+}

@@ -47,7 +47,8 @@ struct NvtxRange {
 
 enum KernelId : int {
   KID_SETS = 1, KID_SELECT = 2, KID_SCORE = 3, KID_GATHER = 4, KID_SCATTER = 5,
-  KID_ATTN_SIMT = 6, KID_ATTN_SM100 = 7, KID_SCORE_SM100 = 8, KID_GEMM_SM100 = 9, KID_DENSE = 10
+  KID_ATTN_SIMT = 6, KID_ATTN_SM100 = 7, KID_SCORE_SM100 = 8, KID_GEMM_SM100 = 9, KID_DENSE = 10,
+  KID_TABLES = 11, KID_PAGED_APPEND = 12, KID_PAGED_ATTN = 13, KID_PREFIX_ATTN = 14, KID_SELECT_BLOCKS = 15
 };
 
 __device__ __forceinline__ void report(DeviceStatus* st, int status, int kernel, int v0, int v1) {

@@ -1,0 +1,39 @@
+// Internal: how the attention over continuations cuts keys into pieces (host only, no CUDA).
+#pragma once
+#include <algorithm>
+
+namespace relaxkv {
+
+// Pieces per row so that a launch of `items` (row, KV head) pairs fills the GPU with two blocks per SM, each piece at least two tiles long.
+inline int paged_pieces(long long items, long long tiles, int sms, int most) {
+  const long long want = std::max<long long>(1, 2LL * sms / std::max<long long>(1, items));
+  return (int)std::max<long long>(1, std::min<long long>({want, (tiles + 1) / 2, (long long)most}));
+}
+
+constexpr double kPrefixStartTiles = 3.0;      // start and end of a block of the prefix kernel, in its 128-key tiles
+
+// Key tiles per block for contexts of n_tiles[0 .. n) tiles and row_tiles[0 .. n) tiles of rows, each times `heads` KV heads, one block per SM.
+// Each block takes start + its tiles; blocks that all run at once end with the longest one, more of them when the SMs have worked all of it off
+// (and on average half a block later).  A piece of the longest context is one more slot for the merge: merge_tiles, in the time of a tile.
+inline int prefix_tiles_per_block(const int* n_tiles, const int* row_tiles, int n, int heads, int sms, int most_pieces, double merge_tiles) {
+  int longest = 1;
+  for (int i = 0; i < n; ++i)
+    if (row_tiles[i] > 0) longest = std::max(longest, n_tiles[i]);
+  int best = longest;
+  double best_cost = 0;
+  for (int p = 1; p <= most_pieces && p <= std::max(1, longest / 2); ++p) {
+    const int per = (longest + p - 1) / p;
+    double blocks = 0, all = 0;
+    for (int i = 0; i < n; ++i) {
+      const double k = (double)row_tiles[i] * heads, pieces = (n_tiles[i] + per - 1) / per;
+      blocks += k * pieces;
+      all += k * (pieces * kPrefixStartTiles + n_tiles[i]);
+    }
+    const double block = kPrefixStartTiles + per;
+    const double cost = (blocks <= sms ? block : std::max(block, all / sms + 0.5 * block)) + merge_tiles * (p > 1 ? p : 0);
+    if (p == 1 || cost < best_cost) { best_cost = cost; best = per; }
+  }
+  return best;
+}
+
+}  // namespace relaxkv

@@ -1,0 +1,59 @@
+// Internal: the streaming attention over listed context blocks and paged tokens, and the merge of partial results.
+#pragma once
+#include "continuations.cuh"
+#include "sm100_ptx.cuh"
+
+namespace relaxkv {
+
+// What a row's keys are made of besides its own tokens.
+enum ContextKeys { CTX_KEYS_NONE = 0, CTX_KEYS_LISTED = 1 };
+
+struct PagedAttnArgs {
+  const uint16_t* q;
+  uint16_t* out;
+  float *lse_out, *part_o, *part_lse;
+  const int *row_seq, *row_len, *row_cu, *table, *lists;
+  long long table_stride, n_rows;
+  int table_width, max_len, n_select, n_blocks;
+  int H, Hkv, n_seq;
+  int ctx_keys;                        // ContextKeys
+  int ctx_block, page;                 // tokens of a context block and of a block of the store
+  int n_splits;                        // pieces a row's keys are cut into
+  int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
+  float scale_log2;
+};
+
+// Whether row r is one that the calls work on: its sequence and length in range, its context's rows within the host's bound.
+struct RowCheck { int seq, len, ctx; };
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int token, int head, int block) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(0), "r"(token), "r"(0), "r"(head), "r"(block) : "memory");
+}
+
+// Sequence, length and context of a row; seq -1: nothing to do (tell: and the reason is reported).
+__device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
+  RowCheck r = {a.row_seq[row], a.row_len[row], 0};
+  if (r.seq == -1) return r;
+  const bool known = r.seq >= 0 && r.seq < a.n_seq;
+  if (!known || r.len < 0 || r.len > a.max_len || (a.max_len > 0 && r.len > (long long)a.table_width * a.page)) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, known ? r.len : r.seq, (int)row);
+    r.seq = -1;
+    return r;
+  }
+  r.ctx = context_of(ct, r.seq);
+  const int n = a.row_cu[ct.seq_cu[r.ctx + 1]] - a.row_cu[ct.seq_cu[r.ctx]];
+  if (n > ct.max_rows[r.ctx]) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, n, r.ctx);
+    r.seq = -1;
+  }
+  return r;
+}
+
+relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
+                                      const ContTable& ct, PagedAttnArgs a, cudaStream_t stream);
+// out = sum over the slots of w_s O_s / sum w_s, w_s = exp(lse_s - max)
+relaxkv_status launch_continuation_merge(const ContTable& ct, const PagedAttnArgs& a, int D, cudaStream_t stream);
+
+}  // namespace relaxkv
