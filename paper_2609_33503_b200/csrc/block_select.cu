@@ -147,7 +147,7 @@ template <int D, bool PAIR>
 __global__ void __launch_bounds__(kScoWarps * 32)
 block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
   constexpr int kSteps = 2 * D / 32;                                // MMAs of a product
-  constexpr int kRowsPer = PAIR ? 2 : 1, kSlots = PAIR ? 8 : 16;    // rows of the step per tile, fragment rows of each
+  constexpr int kRowsPer = PAIR ? 2 : 1;                            // rows of the step per tile
   __shared__ __align__(16) uint32_t q_s[kScoPass][16][2 * D / 4 + 4];      // [tile][fragment row][q+ | q-]; the rows 16 bytes apart from whole banks
   __shared__ float sq_s[kScoPass][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
@@ -179,46 +179,59 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
   for (int p0 = 0; p0 < n_tiles; p0 += kScoPass) {
     const int here = min(kScoPass, n_tiles - p0);
     __syncthreads();
-    // queries in 8 bits: a warp per fragment row, D / 32 dims per lane
-    for (int i = warp; i < here * 16; i += kScoWarps) {
-      const int tile = i >> 4, fr = i & 15, r = (p0 + tile) * kRowsPer + (PAIR ? fr >> 3 : 0), h = PAIR ? fr & 7 : fr;
-      constexpr int kPer = D / 32;
-      uint32_t raw[kPer / 2];
+    // queries in 8 bits: eight lanes per fragment row, D / 8 dims each, the loads of four steps side by side
+    constexpr int kVec = D / 64, kStep = 4 * kScoWarps, kBatch = 4;
+    const int ql = lane & 7, sub = lane >> 3;
+    for (int i0 = warp * 4 + sub; i0 < here * 16; i0 += kStep * kBatch) {
+      uint4 raw[kBatch][kVec];
+      bool live[kBatch];
 #pragma unroll
-      for (int e = 0; e < kPer / 2; ++e) raw[e] = 0u;
-      const bool live = h < G && r < rr.n;
-      if (live) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q + ((rr.first + r) * a.H + hd * G + h) * D + lane * kPer);
+      for (int c = 0; c < kBatch; ++c) {
+        const int i = i0 + c * kStep, tile = i >> 4, fr = i & 15, r = (p0 + tile) * kRowsPer + (PAIR ? fr >> 3 : 0), h = PAIR ? fr & 7 : fr;
+        live[c] = i < here * 16 && h < G && r < rr.n;
+        const uint4* p = reinterpret_cast<const uint4*>(a.q + ((rr.first + r) * a.H + hd * G + h) * D + ql * (D / 8));
 #pragma unroll
-        for (int e = 0; e < kPer / 2; ++e) raw[e] = p[e];
-      }
-      uint32_t amax = 0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const uint32_t m = (raw[e >> 1] >> ((e & 1) * 16)) & 0x7fffu;
-        if (m <= 0x7f80u) amax = max(amax, m);
+        for (int e = 0; e < kVec; ++e) raw[c][e] = live[c] ? p[e] : make_uint4(0u, 0u, 0u, 0u);
       }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      const int ex = scale_exponent(min(amax, 0x7f7fu));
-      const float inv = power_of_two(-ex);
-      uint32_t pos = 0, neg = 0;
+      for (int c = 0; c < kBatch; ++c) {
+        const int i = i0 + c * kStep, tile = i >> 4, fr = i & 15;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(raw[c]);
+        uint32_t amax = 0;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const uint32_t bits = (raw[e >> 1] >> ((e & 1) * 16)) & 0xffffu;
-        const float f = (bits & 0x7fffu) > 0x7f80u ? 0.f : fminf(fmaxf(rintf(bf16_bits_to_float((uint16_t)bits) * inv), -127.f), 127.f);
-        pos |= (uint32_t)(uint8_t)(int8_t)(int)fmaxf(f, 0.f) << (e * 8);
-        neg |= (uint32_t)(uint8_t)(int8_t)(int)fminf(f, 0.f) << (e * 8);
+        for (int e = 0; e < 4 * kVec; ++e) {
+#pragma unroll
+          for (int hf = 0; hf < 32; hf += 16) {
+            const uint32_t m = (w[e] >> hf) & 0x7fffu;
+            amax = max(amax, m <= 0x7f80u ? m : 0u);
+          }
+        }
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        const int ex = scale_exponent(min(amax, 0x7f7fu));
+        const float inv = power_of_two(-ex);
+        uint32_t pos[2 * kVec], neg[2 * kVec];
+#pragma unroll
+        for (int e = 0; e < 2 * kVec; ++e) {
+          pos[e] = neg[e] = 0u;
+#pragma unroll
+          for (int b4 = 0; b4 < 4; ++b4) {
+            const uint32_t bits = (w[2 * e + (b4 >> 1)] >> ((b4 & 1) * 16)) & 0xffffu;
+            const float f = (bits & 0x7fffu) > 0x7f80u ? 0.f : rintf(bf16_bits_to_float((uint16_t)bits) * inv);
+            pos[e] |= (uint32_t)(int)fminf(fmaxf(f, 0.f), 127.f) << (b4 * 8);
+            neg[e] |= ((uint32_t)(int)fmaxf(fminf(f, 0.f), -127.f) & 0xffu) << (b4 * 8);
+          }
+        }
+        if (i < here * 16) {
+          uint32_t* row = q_s[tile][fr];
+#pragma unroll
+          for (int e = 0; e < 2 * kVec; ++e) {
+            row[ql * 2 * kVec + e] = pos[e];
+            row[D / 4 + ql * 2 * kVec + e] = neg[e];
+          }
+          if (ql == 0) sq_s[tile][fr] = live[c] ? power_of_two(ex) : -1.f;      // no such row or head
+        }
       }
-      uint8_t* row = reinterpret_cast<uint8_t*>(q_s[tile][fr]);
-      if constexpr (kPer == 4) {
-        *reinterpret_cast<uint32_t*>(row + lane * 4) = pos;
-        *reinterpret_cast<uint32_t*>(row + D + lane * 4) = neg;
-      } else {
-        *reinterpret_cast<uint16_t*>(row + lane * 2) = (uint16_t)pos;
-        *reinterpret_cast<uint16_t*>(row + D + lane * 2) = (uint16_t)neg;
-      }
-      if (lane == 0) sq_s[tile][fr] = live ? power_of_two(ex) : -1.f;           // no such row or head
     }
     __syncthreads();
     if (x0 >= nb) continue;
@@ -261,7 +274,6 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
       }
     }
   }
-  (void)kSlots;
 }
 
 // ---- the n_select highest scores of a (row, KV head) ------------------------------------------------------------------------------

@@ -1,9 +1,11 @@
 // Head norm, rotary embedding and append to the paged store of a step's rows in one pass (relaxkv_qk_norm_rope_append_paged).
 //
 // Reads Q, K, V once and writes rotated Q and the store's K and V once: bound by HBM for many rows and by its latencies (row values, then slot) for
-// few.  16 lanes hold one head of 128 dims as 16-byte pieces (8 lanes one of 64): a warp works on two (four) heads at once, the rotation partner is
-// half of those lanes away.  A block has a few rows; its (cos, sin) table, one angle per thread in double precision, is made while the first
-// heads are on their way.  Values stay in fp32 from the load to the one rounding at the store.
+// few.  D / 8 lanes hold one head, each four dims of its first half and the four that they are rotated with, as two 8-byte pieces: the pair
+// meets in one lane, and a warp works on two heads of 128 dims (four of 64) at once.  All heads of a row turn by the same angles, so a lane keeps
+// its four (cos, sin) in registers; they are made once per row, one angle per thread in double precision, while the first heads are on their
+// way.  (With 16-byte pieces, the partner in another lane and the angles read from shared memory for every head, 8205 rows of 40 / 8 heads of 128 with
+// norms took 101 us, bound by shared memory.)  Values stay in fp32 from the load to the one rounding at the store.
 #include "continuations.cuh"
 
 namespace relaxkv {
@@ -20,77 +22,77 @@ struct PagedAppendArgs {
   double log2_theta;
 };
 
-__device__ __forceinline__ void unpack_8(const uint4& r, float* f) {
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+__device__ __forceinline__ void unpack_4(const uint2& r, float* f) {
+  f[0] = __uint_as_float(r.x << 16); f[1] = __uint_as_float(r.x & 0xffff0000u);
+  f[2] = __uint_as_float(r.y << 16); f[3] = __uint_as_float(r.y & 0xffff0000u);
 }
-__device__ __forceinline__ uint4 pack_8(const float* f) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint2 pack_4(const float* f) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// ROWS rows per block, heads [blockIdx.y * heads_per_block, + heads_per_block) of each, in the order query heads, key heads, value heads.
+// ROWS rows per block, 8 / ROWS warps on each; heads [blockIdx.y * heads_per_block, + heads_per_block) of them, in the order query heads, key heads,
+// value heads.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kPapThreads)
 paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* st) {
   constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, half = D / 2;
-  constexpr int U = 4;                                          // heads a group of lanes has in flight
+  constexpr int kWarps = kPapThreads / 32 / ROWS, kUnits = kWarps * kPerWarp;       // warps of a row, heads that they work on at once
+  constexpr int U = 4;                                          // heads that a group of lanes has in flight
   __shared__ float2 turn_s[ROWS][half];
-  __shared__ long long place_s[ROWS];
-  const int tid = threadIdx.x, lane = tid & 31, gl = lane % kLanes, unit0 = (tid >> 5) * kPerWarp + lane / kLanes;
-  constexpr int kUnits = (kPapThreads / 32) * kPerWarp;         // heads the block works on at once
-  const long long row0 = (long long)blockIdx.x * ROWS;
-  const int n_heads = a.H + 2 * a.Hkv, h0 = blockIdx.y * heads_per_block, n_here = min(heads_per_block, n_heads - h0);
-  const int rows_here = (int)min((long long)ROWS, a.n_rows - row0), total = rows_here * n_here;
-  const bool low = gl < kLanes / 2;
-  auto load = [&](int u) -> uint4 {
-    if (u >= total) return make_uint4(0, 0, 0, 0);
-    const int rr = u / n_here, h = h0 + u - rr * n_here;
-    const long long row = row0 + rr;
+  const int tid = threadIdx.x, lane = tid & 31, gl = lane % kLanes, rr = (tid >> 5) / kWarps;
+  const int unit0 = ((tid >> 5) % kWarps) * kPerWarp + lane / kLanes;
+  const long long row0 = (long long)blockIdx.x * ROWS, row = row0 + rr;
+  const bool here = row < a.n_rows;
+  const int n_heads = a.H + 2 * a.Hkv, h0 = blockIdx.y * heads_per_block, total = here ? min(heads_per_block, n_heads - h0) : 0;
+  auto load = [&](int u, uint2& lo, uint2& hi) {
+    lo = hi = make_uint2(0u, 0u);
+    if (u >= total) return;
+    const int h = h0 + u;
     const uint16_t* p = h < a.H ? a.q + (row * a.H + h) * D : h < a.H + a.Hkv ? a.k + (row * a.Hkv + (h - a.H)) * D : a.v + (row * a.Hkv + (h - a.H - a.Hkv)) * D;
-    return *reinterpret_cast<const uint4*>(p + gl * 8);
+    lo = *reinterpret_cast<const uint2*>(p + gl * 4);
+    hi = *reinterpret_cast<const uint2*>(p + half + gl * 4);
   };
   griddep_launch();
   griddep_wait();
-  uint4 raw[U];
+  uint2 lo[U], hi[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) raw[u] = load(unit0 + u * kUnits);
+  for (int u = 0; u < U; ++u) load(unit0 + u * kUnits, lo[u], hi[u]);
+  const int slot = here ? a.slots[row] : -1;
+  float wq[8], wk[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
+  if (a.wq != nullptr) {
+    unpack_4(*reinterpret_cast<const uint2*>(a.wq + gl * 4), wq); unpack_4(*reinterpret_cast<const uint2*>(a.wq + half + gl * 4), wq + 4);
+    unpack_4(*reinterpret_cast<const uint2*>(a.wk + gl * 4), wk); unpack_4(*reinterpret_cast<const uint2*>(a.wk + half + gl * 4), wk + 4);
+  }
   for (int x = tid; x < ROWS * half; x += kPapThreads) {
-    const int rr = x / half, i = x - rr * half;
-    if (rr < rows_here) {
+    const int r = x / half, i = x - r * half;
+    if (row0 + r < a.n_rows) {
       const double inv_freq = exp2(-a.log2_theta * (2.0 * i / D));
-      double ang = (double)a.positions[row0 + rr] * inv_freq;
+      double ang = (double)a.positions[row0 + r] * inv_freq;
       ang -= 6.283185307179586 * floor(ang * 0.15915494309189535);
-      sincosf((float)ang, &turn_s[rr][i].y, &turn_s[rr][i].x);
+      sincosf((float)ang, &turn_s[r][i].y, &turn_s[r][i].x);
     }
   }
-  if (tid < rows_here) {
-    const int slot = a.slots[row0 + tid];
-    long long place = -1;
-    if (slot >= 0 && (slot >> a.block_shift) < a.n_blocks)
-      place = (long long)(slot >> a.block_shift) * a.block_stride + (slot & ((1 << a.block_shift) - 1)) * a.token_stride;
-    else if (slot != -1 && blockIdx.y == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_APPEND, (int)(row0 + tid), slot);
-    place_s[tid] = place;
-  }
+  long long place = -1;                                         // of the row in the store
+  if (slot >= 0 && (slot >> a.block_shift) < a.n_blocks)
+    place = (long long)(slot >> a.block_shift) * a.block_stride + (slot & ((1 << a.block_shift) - 1)) * a.token_stride;
+  else if (slot != -1 && unit0 == 0 && gl == 0 && blockIdx.y == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_APPEND, (int)row, slot);
   __syncthreads();
-  for (int u0 = unit0; u0 - unit0 < total; u0 += U * kUnits) {              // (the same trips for all lanes: the sums below need whole warps)
-    uint4 next[U];
+  float2 cs[4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = load(u0 + (U + u) * kUnits);
+  for (int e = 0; e < 4; ++e) cs[e] = turn_s[rr][gl * 4 + e];
+  for (int u0 = unit0; u0 - unit0 < total; u0 += U * kUnits) {              // (the same trips for a row's lanes: the sums below need whole warps)
+    uint2 nlo[U], nhi[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(u0 + (U + u) * kUnits, nlo[u], nhi[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int x = u0 + u * kUnits;
-      const bool live = x < total;
-      const int rr = live ? x / n_here : 0, h = live ? h0 + x - rr * n_here : 0;
-      const bool is_v = h >= a.H + a.Hkv;
+      const int x = u0 + u * kUnits, h = h0 + x;
+      const bool live = x < total, is_q = h < a.H, is_v = h >= a.H + a.Hkv;
       float f[8];
-      unpack_8(raw[u], f);
+      unpack_4(lo[u], f); unpack_4(hi[u], f + 4);
       if (a.wq != nullptr) {
         float ss = 0.f;
 #pragma unroll
@@ -98,29 +100,24 @@ paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* 
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const float inv = rsqrtf(ss / (float)D + a.eps);
-        if (live && !is_v) {
-          float w[8];
-          unpack_8(*reinterpret_cast<const uint4*>((h < a.H ? a.wq : a.wk) + gl * 8), w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * w[e];
-        }
-      }
-      float r[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float other = __shfl_xor_sync(0xffffffffu, f[e], kLanes / 2);
-        const float2 cs = turn_s[rr][(gl % (kLanes / 2)) * 8 + e];
-        r[e] = low ? f[e] * cs.x - other * cs.y : f[e] * cs.x + other * cs.y;
+        for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * (is_q ? wq[e] : wk[e]);
       }
       if (live) {
-        const long long place = place_s[rr];
-        if (h < a.H) *reinterpret_cast<uint4*>(a.q_out + ((row0 + rr) * a.H + h) * D + gl * 8) = pack_8(r);
-        else if (place >= 0) {
-          if (is_v) *reinterpret_cast<uint4*>(a.store_v + place + (h - a.H - a.Hkv) * a.head_stride + gl * 8) = raw[u];
-          else *reinterpret_cast<uint4*>(a.store_k + place + (h - a.H) * a.head_stride + gl * 8) = pack_8(r);
+        float r[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          r[e] = f[e] * cs[e].x - f[4 + e] * cs[e].y;
+          r[4 + e] = f[4 + e] * cs[e].x + f[e] * cs[e].y;
+        }
+        const uint2 rlo = is_v ? lo[u] : pack_4(r), rhi = is_v ? hi[u] : pack_4(r + 4);
+        uint16_t* p = is_q ? a.q_out + (row * a.H + h) * D : is_v ? a.store_v + place + (h - a.H - a.Hkv) * a.head_stride : a.store_k + place + (h - a.H) * a.head_stride;
+        if (is_q || place >= 0) {
+          *reinterpret_cast<uint2*>(p + gl * 4) = rlo;
+          *reinterpret_cast<uint2*>(p + half + gl * 4) = rhi;
         }
       }
-      raw[u] = next[u];
+      lo[u] = nlo[u]; hi[u] = nhi[u];
     }
   }
 }
@@ -154,9 +151,9 @@ extern "C" relaxkv_status relaxkv_qk_norm_rope_append_paged(
   a.log2_theta = log2((double)theta);
   const int n_heads = n_q_heads + 2 * n_kv_heads;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (n_rows >= 1024) {                         // four rows per block: every thread makes one angle or two
-    const dim3 grid((unsigned)((n_rows + 3) / 4), 1);
-    auto kern = head_dim == 128 ? paged_append_kernel<128, 4> : paged_append_kernel<64, 4>;
+  if (n_rows >= 1024) {                         // a row per warp, all its heads
+    const dim3 grid((unsigned)((n_rows + 7) / 8), 1);
+    auto kern = head_dim == 128 ? paged_append_kernel<128, 8> : paged_append_kernel<64, 8>;
     return cuda_ok(launch_chained(kern, grid, kPapThreads, 0, s, a, n_heads, st));
   }
   const int per = head_dim == 128 ? 16 : 32;    // one head per group of lanes

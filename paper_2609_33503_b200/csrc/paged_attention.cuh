@@ -18,7 +18,7 @@ struct PagedAttnArgs {
   int H, Hkv, n_seq;
   int ctx_keys;                        // ContextKeys
   int ctx_block, page;                 // tokens of a context block and of a block of the store
-  int n_splits;                        // pieces a row's keys are cut into
+  int n_splits, piece_tiles;           // pieces a row's keys are cut into, 64-key tiles of one
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };
@@ -30,6 +30,12 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* m, 
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(0), "r"(token), "r"(0), "r"(head), "r"(block) : "memory");
+}
+
+// Requests a box into L2 (nothing is written to this SM).
+__device__ __forceinline__ void tma_prefetch_5d(const CUtensorMap* m, int token, int head, int block) {
+  asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global.tile [%0, {%1, %2, %3, %4, %5}];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(0), "r"(token), "r"(0), "r"(head), "r"(block) : "memory");
 }
 
 // Sequence, length and context of a row; seq -1: nothing to do (tell: and the reason is reported).

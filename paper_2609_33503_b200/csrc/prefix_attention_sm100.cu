@@ -1,11 +1,18 @@
 // Attention of a step's rows over the context they share, read once for all of them (relaxkv_shared_prefix_attention).
 //
-// Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of the step),
-// one KV head and a piece of the context, and walks it in 128-key tiles: TMA (128-byte swizzle) -> S = Q K^T (tcgen05, accumulators in tensor
-// memory) -> softmax warps (thread = row), P as bf16 over S -> O += P V (tcgen05, P from tensor memory).  S of the next tile is issued before
-// O of this one, so the tensor pipe works while the softmax does.  With up to 128 rows the kernel is bound by the bytes of K and V (a tile
-// of 64 KB takes an SM's share of HBM 1.5 us, its products and exponentials half of that), with more by the exponentials.  The pieces' results are
-// merged with those of the rows' own tokens by their log-sum-exps.  Every wait is bounded.
+// Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of the
+// step), one KV head and a piece of the context, and walks it in 128-key tiles: TMA (128-byte swizzle) -> S = Q K^T (tcgen05, Q and the
+// accumulators in tensor memory) -> softmax (thread = row) -> P as bf16 in tensor memory -> O += P V (tcgen05).
+// With up to 128 rows the kernel is bound by the bytes of K and V: a tile of 64 KB takes an SM's share of HBM 1.5 us.  With several row tiles to
+// a context a tile's products (2 x 512 clk), its 16 K exponentials (16 per clk) and its way through shared memory (written once and read
+// once at 128 bytes per clk, as long as Q is not read from there, too) all take 1024 clk, so they have to overlap:
+//   two groups of four softmax warps take the even and the odd tiles;
+//   S is double-buffered and free again as soon as a group has it in registers, so S of tile j + 2 is made while P of tile j is;
+//   P and O are single: a group hands its P over when O of the tile before is complete, which is also when O may be rescaled (every barrier
+//   belongs to the even or to the odd tiles, so that nobody who waits for one phase can be two behind);
+//   the running maximum of a row goes from group to group through shared memory (known a third into a group's step); sums stay with the groups.
+// (Each group with an output of its own, S and P in one place, Q in shared memory: 1780 clk per tile.)
+// The pieces' results are merged with those of the rows' own tokens by their log-sum-exps.  Every wait is bounded.
 #include "continuation_splits.cuh"
 #include "paged_attention.cuh"
 #include "sm100_ptx.cuh"
@@ -16,66 +23,68 @@ namespace relaxkv {
 using namespace ptx;
 
 constexpr int kPreTile = 128;                         // keys per tile = rows per block
-constexpr int kPreRing = 6;                           // tile buffers, used in the order K0 V0 K1 V1 ...
-constexpr int kPreThreads = 192;                      // four softmax warps, the TMA warp, the MMA warp
+constexpr int kPreRing = 7;                           // tile buffers, used in the order K0 V0 K1 V1 ...
+constexpr int kPreThreads = 384;                      // two groups of four softmax warps; the TMA warp, the MMA warp, two idle
 constexpr float kPreRescale = 8.0f;                   // log2 units: O is rescaled only when the row maximum grew by more
 constexpr float kLog2ePre = 1.4426950408889634f, kLn2Pre = 0.6931471805599453f;
+
+// p = 2^(s * scale - m) of a row's 128 keys as bf16 pairs, and their sum.
+__device__ __forceinline__ float prefix_exponentials(const uint32_t* s, uint32_t* pk, float scale, float neg_m) {
+  float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPreTile; i += 4) {
+    float y[4], p[4];
+#pragma unroll
+    for (int e = 0; e < 4; e += 2)
+      fma2(y[e], y[e + 1], __uint_as_float(s[i + e]), __uint_as_float(s[i + e + 1]), scale, scale, neg_m, neg_m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = fast_exp2(y[e]);
+    add2(z0, z1, p[0], p[1]);
+    add2(z2, z3, p[2], p[3]);
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(p[e], p[e + 1]);
+      pk[(i + e) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  return (z0 + z1) + (z2 + z3);
+}
 
 template <int D>
 struct PreSmem {
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = kPreTile * 128;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kQ = 0;
-  static constexpr int kKV = kTileBytes;
-  static constexpr int kBar = kKV + kPreRing * kTileBytes;
-  static constexpr int kNumBars = 2 * kPreRing + 9;   // full, empty | q, s[2], p_lo[2], p_hi[2], o, vfix
+  static constexpr int kBar = kPreRing * kTileBytes;
+  static constexpr int kNumBars = 2 * kPreRing + 12;  // full, empty | q, s[2], read[2], p[2], m[2], o[2], vfix
   static constexpr int kMisc = kBar + 8 * kNumBars;   // tensor memory address, abort flag
-  static constexpr int kTotal = kMisc + 16;
+  static constexpr int kMax = kMisc + 8;              // running maximum of every row
+  static constexpr int kSum = kMax + 4 * kPreTile;    // sums of every row, by group
+  static constexpr int kTotal = kSum + 8 * kPreTile;
   static constexpr int kDynamic = kTotal + 1024;
+  static constexpr int kOutStride = D * 2 + 16;       // bytes between the half rows of partial output that threads stage in the ring
+  static_assert(256 * kOutStride <= kBar, "the ring holds them");
+  static_assert(kDynamic <= 232448, "shared memory of a block");
 };
 
-// P of keys [32 C0, 32 C1): p = 2^(s * scale - m) as bf16 over S, and its sum.
-template <int C0, int C1>
-__device__ __forceinline__ float prefix_exponentials(uint32_t t_s, const uint32_t* s, float scale, float neg_m) {
-  float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
-#pragma unroll
-  for (int c = C0; c < C1; ++c) {
-    uint32_t pk[16];
-#pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      float x[4], p[4];
-#pragma unroll
-      for (int e = 0; e < 4; e += 2)
-        fma2(x[e], x[e + 1], __uint_as_float(s[c * 32 + i + e]), __uint_as_float(s[c * 32 + i + e + 1]), scale, scale, neg_m, neg_m);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(x[e]);
-      add2(z0, z1, p[0], p[1]);
-      add2(z2, z3, p[2], p[3]);
-#pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(p[e], p[e + 1]);
-        pk[(i + e) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-    }
-    tmem_st16(t_s + c * 16, pk);
-  }
-  return (z0 + z1) + (z2 + z3);
-}
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 template <int D>
 __global__ void __launch_bounds__(kPreThreads, 1)
 prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ContTable ct,
                         const __grid_constant__ PagedAttnArgs a, int rows_per_tile, DeviceStatus* st) {
   using L = PreSmem<D>;
-  constexpr uint32_t kTmemCols = 512;                   // S of even tiles | S of odd tiles | O
+  // tensor memory: S of even tiles | S of odd tiles | O | P | Q
+  constexpr uint32_t kTmemCols = 512, kO = 256, kP = 384, kQ = 448;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t bar_full = base + L::kBar, bar_empty = bar_full + 8 * kPreRing, bar_q = bar_empty + 8 * kPreRing, bar_s = bar_q + 8,
-                 bar_plo = bar_s + 16, bar_phi = bar_plo + 16, bar_o = bar_phi + 16, bar_vfix = bar_o + 8;
+                 bar_read = bar_s + 16, bar_p = bar_read + 16, bar_m = bar_p + 16, bar_o = bar_m + 16, bar_vfix = bar_o + 16;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + L::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + L::kMisc + 4);
+  volatile float* max_s = reinterpret_cast<volatile float*>(base_ptr + L::kMax);
+  volatile float* sum_s = reinterpret_cast<volatile float*>(base_ptr + L::kSum);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.H / a.Hkv;
   // which context, rows, head and piece: the row tiles of a piece stand side by side and find its keys in L2
@@ -84,46 +93,62 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   const int rt = at % n_rt, hd = at / n_rt % a.Hkv, piece = at / (n_rt * a.Hkv);
   const int ctx_len = ct.ctx_len[b], n_tiles = (ctx_len + kPreTile - 1) / kPreTile;
   const int per = (n_tiles + ct.pieces[b] - 1) / ct.pieces[b], j0 = min(n_tiles, piece * per), n = min(n_tiles, j0 + per) - j0;
-  if (threadIdx.x == 128) { prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v); }
-  if (threadIdx.x == 0) {
+  const int token0 = (int)ct.tok_off[b] + j0 * kPreTile;
+  const int x = (warp >> 2) & 1, t = (int)threadIdx.x & 127, t_local = t / G, head = hd * G + t - t_local * G;      // softmax threads: group, row, of it
+  if (threadIdx.x == 256) {
+    prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     for (int s = 0; s < kPreRing; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
-    mbar_init(bar_q, 128);
-    mbar_init(bar_s, 1); mbar_init(bar_s + 8, 1);
-    for (int x = 0; x < 2; ++x) { mbar_init(bar_plo + 8 * x, 128); mbar_init(bar_phi + 8 * x, 128); }
-    mbar_init(bar_o, 1);
+    mbar_init(bar_q, 256);
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_read + 8 * i, 128); mbar_init(bar_p + 8 * i, 128); mbar_init(bar_m + 8 * i, 128); mbar_init(bar_o + 8 * i, 1); }
     mbar_init(bar_vfix, 32);
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
   }
+  if (warp == 9) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols); tmem_relinquish(); }
+  // What a block needs first into L2 while the kernels in front finish (prefetches only: everything is read after the wait).  The rows are
+  // guessed from the host's bounds: behind the first tiles of all blocks in HBM's queue, their loads took 3 to 5 us.
+  if (warp < 8) {
+    int before = 0;
+    for (int i = 0; i < b; ++i) before += ct.max_rows[i];
+    const long long guess = (long long)before + (long long)rt * rows_per_tile + t_local;
+    if (x < L::kHalves && guess < a.n_rows && t_local < rows_per_tile) prefetch_l2(a.q + (guess * a.H + head) * D + x * 64);
+    if (threadIdx.x == 0) { prefetch_l2(st); prefetch_l2(a.row_cu + ct.seq_cu[b]); prefetch_l2(a.row_cu + ct.seq_cu[b + 1]); }
+  } else if (threadIdx.x == 256) {
+    for (int u = 0; u < min(2 * n, kPreRing); ++u) tma_prefetch_5d((u & 1) ? &tm_v : &tm_k, token0 + (u >> 1) * kPreTile, hd, 0);
+  }
+  if (threadIdx.x < kPreTile) max_s[threadIdx.x] = -1.0e30f;      // (finite, so that logits of -inf leave 2^(-inf) = 0)
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  griddep_launch();                                     // (the block holds its tensor memory)
   griddep_wait();
   const int status = *reinterpret_cast<volatile int*>(&st->status);
   const long long row0 = a.row_cu[ct.seq_cu[b]], row1 = a.row_cu[ct.seq_cu[b + 1]];
   const long long first = row0 + (long long)rt * rows_per_tile;
-  if (row0 < 0 || row1 > a.n_rows || row1 - row0 > ct.max_rows[b]) {        // more rows than the host's bounds: report, touch nothing
-    if (threadIdx.x == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PREFIX_ATTN, (int)(row1 - row0), b);
+  const bool refused = row0 < 0 || row1 > a.n_rows || row1 - row0 > ct.max_rows[b];       // more rows than the host's bounds: report, touch nothing
+  if (refused || first >= row1 || status == RELAXKV_ERR_TIMEOUT) {
+    if (refused && threadIdx.x == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PREFIX_ATTN, (int)(row1 - row0), b);
+    __syncthreads();
+    if (warp == 9) tmem_dealloc(tmem_base, kTmemCols);
     return;
   }
-  if (first >= row1 || status == RELAXKV_ERR_TIMEOUT) return;
   const int n_rows = (int)min((long long)rows_per_tile, row1 - first);
-  if (warp == 5) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols); tmem_relinquish(); }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  griddep_launch();                                     // (the block holds its tensor memory)
-  const uint32_t tmem_base = *tmem_slot;
   const int tail = ctx_len % kPreTile;                  // tokens of the context's last tile, 0: all
   const bool fix_v = tail != 0 && j0 + n == n_tiles && n > 0;
 
-  if (warp == 4) {
-    // ================= TMA producer =================
+  // Registers: 12 warps x 168 at launch = 8 x 224 + 4 x 56.
+  if (warp >= 8) {
+  reg_dealloc<56>();
+  if (warp == 8) {
+    // ================= TMA producer: K_0 V_0 K_1 V_1 ... =================
     if (lane == 0) {
-      const int token0 = (int)ct.tok_off[b] + j0 * kPreTile;
       for (int u = 0; u < 2 * n; ++u) {
         const int s = u % kPreRing;
         if (u >= kPreRing && !mbar_wait(bar_empty + 8 * s, (uint32_t)(u / kPreRing - 1) & 1, abort_flag)) break;
         mbar_expect_tx(bar_full + 8 * s, L::kTileBytes);
-        tma_load_5d(base + L::kKV + s * L::kTileBytes, (u & 1) ? &tm_v : &tm_k, bar_full + 8 * s, token0 + (u >> 1) * kPreTile, hd, 0);
+        tma_load_5d(base + s * L::kTileBytes, (u & 1) ? &tm_v : &tm_k, bar_full + 8 * s, token0 + (u >> 1) * kPreTile, hd, 0);
       }
     }
     __syncwarp();
@@ -131,7 +156,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
       // V rows behind the context belong to nobody (0 x NaN = NaN on the tensor core): zero them once their tile has landed
       const int u = 2 * n - 1, s = u % kPreRing;
       if (mbar_wait(bar_full + 8 * s, (uint32_t)(u / kPreRing) & 1, abort_flag)) {
-        uint8_t* vt = base_ptr + L::kKV + s * L::kTileBytes;
+        uint8_t* vt = base_ptr + s * L::kTileBytes;
         for (int i = lane; i < (kPreTile - tail) * 8 * L::kHalves; i += 32) {
           const int c = i & 7, r = tail + (i >> 3) % (kPreTile - tail), hf = (i >> 3) / (kPreTile - tail);
           *reinterpret_cast<uint4*>(vt + hf * L::kHalfBytes + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
@@ -140,91 +165,116 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
       }
       mbar_arrive(bar_vfix);
     }
-  } else if (warp == 5) {
-    // ================= MMA issuer =================
-    if (lane == 0 && n > 0) {
-      constexpr uint32_t idesc_qk = idesc_bf16_f32(kPreTile, kPreTile, 0), idesc_pv = idesc_bf16_f32(kPreTile, D, 1);
-      const uint32_t hi = desc_hi_sw128(1024);
-      auto issue_qk = [&](int j) -> bool {              // S_j = Q K_j^T
-        const int u = 2 * j, s = u % kPreRing;
-        if (!mbar_wait(bar_full + 8 * s, (uint32_t)(u / kPreRing) & 1, abort_flag)) return false;
-        tc_fence_after();
-#pragma unroll
-        for (int hf = 0; hf < L::kHalves; ++hf)
-          mma_ss_4steps(tmem_base + (j & 1) * 128, desc_lo(base + L::kQ + hf * L::kHalfBytes, 16),
-                        desc_lo(base + L::kKV + s * L::kTileBytes + hf * L::kHalfBytes, 16), hi, idesc_qk, hf > 0 ? 1u : 0u);
-        mma_commit(bar_s + 8 * (j & 1));
-        mma_commit(bar_empty + 8 * s);
-        return true;
-      };
-      bool ok = mbar_wait(bar_q, 0, abort_flag) && issue_qk(0);
-      for (int j = 0; ok && j < n; ++j) {
-        if (j + 1 < n && !(ok = issue_qk(j + 1))) break;
-        const int u = 2 * j + 1, s = u % kPreRing;
-        if (!(ok = mbar_wait(bar_full + 8 * s, (uint32_t)(u / kPreRing) & 1, abort_flag))) break;
-        if (fix_v && j == n - 1 && !(ok = mbar_wait(bar_vfix, 0, abort_flag))) break;
-        if (!(ok = mbar_wait(bar_plo + 8 * (j & 1), (uint32_t)(j >> 1) & 1, abort_flag))) break;
-        tc_fence_after();
-        const uint32_t v_lo = desc_lo(base + L::kKV + s * L::kTileBytes, L::kHalfBytes), p = tmem_base + (j & 1) * 128;
-        mma_ts_steps<6>(tmem_base + 256, p, v_lo, hi, idesc_pv, j > 0 ? 1u : 0u);       // the first 96 keys while the last 32 are worked on
-        if (!(ok = mbar_wait(bar_phi + 8 * (j & 1), (uint32_t)(j >> 1) & 1, abort_flag))) break;
-        tc_fence_after();
-        mma_ts_steps<2>(tmem_base + 256, p + 48, v_lo + 6 * 128, hi, idesc_pv, 1u);
-        mma_commit(bar_empty + 8 * s);
-        mma_commit(bar_o);
-      }
+  } else if (warp == 9) {
+    // ================= MMA issuer: the whole warp, one lane issues =================
+    constexpr uint32_t idesc_qk = idesc_bf16_f32(kPreTile, kPreTile, 0), idesc_pv = idesc_bf16_f32(kPreTile, D, 1);
+    constexpr uint32_t hi = desc_hi_sw128(1024);
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, abort_flag)); };
+    // buffers and phases of the next K tile and of the next V tile; a buffer that no later tile takes is not reported free (an arrival that
+    // nobody waits for could come when the block has gone)
+    int sk = 0, sv = 1;
+    uint32_t pk = 0, pv = 0;
+    auto step = [&](int& s, uint32_t& phase) { s += 2; if (s >= kPreRing) { s -= kPreRing; phase ^= 1u; } };
+    auto issue_qk = [&](int j) -> bool {                // S_j = Q K_j^T
+      if (!wait(bar_full + 8 * sk, pk)) return false;
+      if (j > 1 && !wait(bar_read + 8 * (j & 1), (uint32_t)((j >> 1) - 1))) return false;         // S_{j-2} is in registers
+      tc_fence_after();
+      warp_mma_ts_kmajor<L::kHalves>(tmem_base + (j & 1) * 128, tmem_base + kQ, desc_lo(base + sk * L::kTileBytes, 16), hi, idesc_qk);
+      if (2 * j + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * sk);
+      warp_mma_commit(bar_s + 8 * (j & 1));
+      step(sk, pk);
+      return true;
+    };
+    bool ok = n > 0 && wait(bar_q, 0);
+    for (int j = 0; ok && j < min(n, 2); ++j) ok = issue_qk(j);
+    for (int j = 0; ok && j < n; ++j) {
+      if (j + 2 < n && !(ok = issue_qk(j + 2))) break;
+      if (!(ok = wait(bar_full + 8 * sv, pv))) break;
+      if (fix_v && j == n - 1 && !(ok = wait(bar_vfix, 0))) break;
+      if (!(ok = wait(bar_p + 8 * (j & 1), (uint32_t)(j >> 1)))) break;
+      tc_fence_after();
+      warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + kP, desc_lo(base + sv * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
+      if (2 * j + 1 + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * sv);
+      warp_mma_commit(bar_o + 8 * (j & 1));
+      step(sv, pv);
     }
+  }
   } else {
-    // ================= softmax: thread = (row of the step, head) = TMEM lane =================
-    const int t_local = (int)threadIdx.x / G, head = hd * G + (int)threadIdx.x - t_local * G;
+    reg_alloc<224>();
+    // ================= softmax: thread = (row of the step, head) = TMEM lane; x: even or odd tiles =================
     const bool mine = t_local < n_rows;
     const long long row = first + t_local;
-    {
-      uint8_t* q_s = base_ptr + L::kQ + threadIdx.x * 128;
-      const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D);
+    const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16), t_s = lane_base + x * 128, t_o = lane_base + kO;
+    if (x < L::kHalves) {                               // of Q, each group brings 64 dims
+      uint32_t w[32];
+      const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D + x * 64);
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c)
-        *reinterpret_cast<uint4*>(q_s + (c >> 3) * L::kHalfBytes + (((c & 7) ^ ((int)threadIdx.x & 7)) << 4)) = mine ? q[c] : make_uint4(0, 0, 0, 0);
-      fence_proxy_async_smem();
-      mbar_arrive(bar_q);
+      for (int c = 0; c < 8; ++c) {
+        const uint4 v = mine ? q[c] : make_uint4(0, 0, 0, 0);
+        w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
+      }
+      tmem_st32(lane_base + kQ + x * 32, w);
+      tmem_wait_st();
+      tc_fence_before();
     }
+    mbar_arrive(bar_q);
     const bool busy = __any_sync(0xffffffffu, mine);    // a warp without rows only keeps step
-    const uint32_t lane_base = tmem_base + ((uint32_t)(warp * 32) << 16), t_o = lane_base + 256;
-    float m = -1.0e30f, z = 0.f;                        // (finite, so that logits of -inf leave 2^(-inf) = 0)
+    float m = -1.0e30f, z = 0.f;                        // the row's maximum when this group last saw it, the group's sum relative to that
     bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      ok = mbar_wait(bar_s + 8 * (j & 1), (uint32_t)(j >> 1) & 1, abort_flag);
+    for (int j = x; j < n; j += 2) {
+      ok = mbar_wait(bar_s + 8 * x, (uint32_t)(j >> 1) & 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      if (busy) {
-        const uint32_t t_s = lane_base + (j & 1) * 128;
-        uint32_t s[kPreTile];
+      if (!busy) {                                      // (a warp that ran ahead would arrive twice in one phase of a barrier)
+        mbar_arrive(bar_read + 8 * x);
+        if (j > 0) ok = mbar_wait(bar_m + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
+        if (ok) mbar_arrive(bar_m + 8 * x);
+        if (ok && j > 0) ok = mbar_wait(bar_o + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
+        if (ok) mbar_arrive(bar_p + 8 * x);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        continue;
+      }
+      uint32_t s[kPreTile];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, &s[c * 32]);
-        tmem_wait_ld();
-        const int limit = ctx_len - (j0 + j) * kPreTile;
-        if (limit < kPreTile) {
+      for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, &s[c * 32]);
+      tmem_wait_ld();
+      tc_fence_before();
+      mbar_arrive(bar_read + 8 * x);
+      const int limit = ctx_len - (j0 + j) * kPreTile;
+      if (limit < kPreTile) {
 #pragma unroll
-          for (int i = 0; i < kPreTile; ++i)
-            if (i >= limit) s[i] = 0xff800000u;         // -inf
-        }
-        float mx[8];
+        for (int i = 0; i < kPreTile; ++i)
+          if (i >= limit) s[i] = 0xff800000u;           // -inf
+      }
+      float mx[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+      for (int e = 0; e < 8; ++e) mx[e] = fmaxf(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
 #pragma unroll
-        for (int i = 16; i < kPreTile; i += 2) mx[(i >> 1) & 7] = fmax3(mx[(i >> 1) & 7], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-        const float m_new = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.scale_log2;
-        const float m_old = m;
-        const bool need = m_new > m + kPreRescale;
-        if (need) m = m_new;
-        if (j > 0 && __any_sync(0xffffffffu, need)) {
-          ok = mbar_wait(bar_o, (uint32_t)(j - 1) & 1, abort_flag);           // O of the tile before is complete
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          const float alpha = fast_exp2(m_old - m);
-          z *= alpha;
+      for (int i = 16; i < kPreTile; i += 2) mx[(i >> 1) & 7] = fmax3(mx[(i >> 1) & 7], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+      const float m_tile = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.scale_log2;
+      if (j > 0) {                                      // the other group's maximum of the tile before
+        ok = mbar_wait(bar_m + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+      }
+      const float m_old = max_s[t];
+      const bool need = m_tile > m_old + kPreRescale;
+      const float m_new = need ? m_tile : m_old;
+      if (need) max_s[t] = m_new;
+      mbar_arrive(bar_m + 8 * x);
+      z *= fast_exp2(m - m_new);                        // (1 as long as nothing has changed)
+      m = m_new;
+      uint32_t pk[64];
+      z += prefix_exponentials(s, pk, a.scale_log2, -m);
+      if (j > 0) {                                      // O of the tile before is complete, its P is not needed any more
+        ok = mbar_wait(bar_o + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        if (__any_sync(0xffffffffu, need)) {
+          const float alpha = fast_exp2(m_old - m_new);
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
@@ -235,39 +285,40 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             tmem_st32(t_o + c * 32, o);
           }
         }
-        z += prefix_exponentials<0, 3>(t_s, s, a.scale_log2, -m);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bar_plo + 8 * (j & 1));
-        z += prefix_exponentials<3, 4>(t_s, s, a.scale_log2, -m);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bar_phi + 8 * (j & 1));
-      } else {
-        tc_fence_before();
-        mbar_arrive(bar_plo + 8 * (j & 1));
-        mbar_arrive(bar_phi + 8 * (j & 1));
       }
+      tmem_st32(lane_base + kP, pk);
+      tmem_st32(lane_base + kP + 32, pk + 32);
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(bar_p + 8 * x);
     }
-    if (ok && n > 0) {
-      ok = mbar_wait(bar_o, (uint32_t)(n - 1) & 1, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
-      tc_fence_after();
-    }
+    // ---- the output, each thread half the dims of its row ----
+    if (ok && n > 0) ok = mbar_wait(bar_o, (uint32_t)((n - 1) >> 1) & 1, abort_flag);
+    if (ok && n > 1) ok = mbar_wait(bar_o + 8, (uint32_t)((n - 2) >> 1) & 1, abort_flag);
+    const float m_end = ok ? max_s[t] : m;
+    sum_s[x * kPreTile + t] = z * fast_exp2(m - m_end);
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    ok = __all_sync(0xffffffffu, ok && !*abort_flag);
+    tc_fence_after();
     if (ok && busy) {
-      const bool none = z == 0.f;                       // no key, or none of a logit above -inf (NaN stays NaN)
-      const float inv = none ? 0.f : 1.f / z, lse = none ? -INFINITY : (m + log2f(z)) * kLn2Pre;
+      const float zz = sum_s[t] + sum_s[kPreTile + t];
+      const bool none = zz == 0.f;                      // no key, or none of a logit above -inf (NaN stays NaN)
+      const float inv = none ? 0.f : 1.f / zz, lse = none ? -INFINITY : (m_end + log2f(zz)) * kLn2Pre;
       const bool direct = a.n_slots == 1;
-      const bool store = mine && (!direct || check_row(a, ct, row, true, st).seq >= 0);
+      const bool store = mine && (!direct || check_row(a, ct, row, x == 0, st).seq >= 0);
       const long long slot = ((long long)piece * a.n_rows + row) * a.H + head;
+      uint8_t* stage = base_ptr + threadIdx.x * L::kOutStride;        // (all tiles have been consumed)
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
+      for (int c = 0; c < D / 64; ++c) {
         uint32_t o[32];
-        if (n > 0) { tmem_ld32(t_o + c * 32, o); tmem_wait_ld(); }
+        if (n > 0) { tmem_ld32(t_o + x * (D / 2) + c * 32, o); tmem_wait_ld(); }
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = none ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
-        if (store && direct) {
-          uint16_t* p = a.out + (row * a.H + head) * D + c * 32;
+        if (!direct) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(stage + c * 128 + i * 4) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        } else if (store) {
+          uint16_t* p = a.out + (row * a.H + head) * D + x * (D / 2) + c * 32;
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             uint32_t w[4];
@@ -278,14 +329,15 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             }
             *reinterpret_cast<uint4*>(p + i) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-        } else if (store) {
-          float* p = a.part_o + slot * D + c * 32;
-#pragma unroll
-          for (int i = 0; i < 32; i += 8) st_global_32b(p + i, o + i);        // (the workspace is 256-byte aligned)
         }
       }
-      if (store && direct && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = lse;
-      if (store && !direct) a.part_lse[slot] = lse;
+      if (!direct && store) {                           // a row's half as one copy out of shared memory
+        fence_proxy_async_smem();
+        bulk_store(a.part_o + slot * D + x * (D / 2), smem_u32(stage), D * 2);
+        if (x == 0) a.part_lse[slot] = lse;
+        bulk_store_commit_and_drain();
+      }
+      if (store && x == 0 && direct && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = lse;
     }
   }
   // ---- teardown ----
@@ -297,7 +349,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 5) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
+  if (warp == 9) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
 }
 
 template <int D>
@@ -377,7 +429,8 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // ---- pieces of the rows' own keys (0: there are none), and of the contexts ----
   const bool own = a.max_len > 0;
-  const int own_pieces = own ? paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, sms, std::max(1, slots / 4)) : 0;
+  const PagedPieces cut = paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, 2 * sms, std::max(1, slots / 4), false);
+  const int own_pieces = own ? cut.n : 0;
   int n_tiles[kMaxReqInline], row_tiles[kMaxReqInline], most = 0;
   for (int b = 0; b < ct.n_req; ++b) {
     n_tiles[b] = (int)(((long long)ct.ctx_len[b] + kPreTile - 1) / kPreTile);
@@ -399,6 +452,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   a.slot0 = own ? most : kContSlotsMost;                // without own keys no slot is theirs
   a.n_slots = most + own_pieces;
   a.n_splits = own_pieces;
+  a.piece_tiles = cut.tiles;
   if (a.n_slots <= 1 && !all) a.n_slots = 2;            // rows without any key: the merge writes their zeros
   if (most > 0) {
     rc = D == 128 ? launch_prefix<128>(cache, ct, a, rows_per_tile, s) : launch_prefix<64>(cache, ct, a, rows_per_tile, s);
@@ -428,7 +482,9 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   a.ctx_keys = any_ctx ? CTX_KEYS_LISTED : CTX_KEYS_NONE;
   a.lists = blocks; a.n_select = n_select; a.ctx_block = block_size;
   const long long tiles = ((long long)n_select * block_size + 63) / 64 + (a.max_len + 63) / 64;
-  a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
+  const PagedPieces cut = paged_pieces(a.n_rows * a.Hkv, tiles, 2 * sms, cont_slots(a.n_rows), true);
+  a.n_splits = cut.n;
+  a.piece_tiles = cut.tiles;
   a.slot0 = 0;
   a.n_slots = a.n_splits;
   cudaStream_t s = static_cast<cudaStream_t>(stream);

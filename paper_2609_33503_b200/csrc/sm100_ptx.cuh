@@ -267,6 +267,41 @@ __device__ __forceinline__ void mma_ts_steps(uint32_t d_tmem, uint32_t a_tmem, u
 #undef RELAXKV_MMA_TS_ARGS
 }
 
+// ---- issue by a whole warp -------------------------------------------------------------------------------------
+// The warp executes these with all its lanes and the same operands, one elected lane (always the same) issues.  Inside a branch that one lane
+// takes, the compiler cannot keep operands in uniform registers, where tcgen05.mma wants them, and moves each of them there before every
+// instruction: a 128 x 128 x 16 product then takes some 100 clk to issue, 64 to execute.
+#define RELAXKV_MMA_TS_ELECT(AOFF, BOFF, PRED)                                                 \
+  "add.u32 ta, %1, " #AOFF ";\n\tadd.u32 tb, %2, " #BOFF ";\n\t"                                  \
+  "mov.b64 db, {tb, %3};\n\t"                                                                  \
+  "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, " #PRED ";\n\t"
+#define RELAXKV_MMA_ELECT_HEAD                                                                 \
+  "{\n\t.reg .pred p0, p1, pe;\n\t.reg .b32 ta, tb;\n\t.reg .b64 db;\n\t"                        \
+  "elect.sync _|pe, 0xffffffff;\n\tsetp.ne.b32 p0, %5, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+#define RELAXKV_MMA_ELECT_ARGS "}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc_first) : "memory"
+// D[tmem] = A[tmem] * B[smem] over K = 64 * HALVES: A advances 8 columns per K step of 16, B is K-major (128B swizzle, halves 16 KB apart).
+template <int HALVES>
+__device__ __forceinline__ void warp_mma_ts_kmajor(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc) {
+  constexpr uint32_t acc_first = 0;
+  if (HALVES == 1)
+    asm volatile(RELAXKV_MMA_ELECT_HEAD RELAXKV_MMA_TS_ELECT(0, 0, p0) RELAXKV_MMA_TS_ELECT(8, 2, p1) RELAXKV_MMA_TS_ELECT(16, 4, p1)
+                 RELAXKV_MMA_TS_ELECT(24, 6, p1) RELAXKV_MMA_ELECT_ARGS);
+  else
+    asm volatile(RELAXKV_MMA_ELECT_HEAD RELAXKV_MMA_TS_ELECT(0, 0, p0) RELAXKV_MMA_TS_ELECT(8, 2, p1) RELAXKV_MMA_TS_ELECT(16, 4, p1)
+                 RELAXKV_MMA_TS_ELECT(24, 6, p1) RELAXKV_MMA_TS_ELECT(32, 1024, p1) RELAXKV_MMA_TS_ELECT(40, 1026, p1)
+                 RELAXKV_MMA_TS_ELECT(48, 1028, p1) RELAXKV_MMA_TS_ELECT(56, 1030, p1) RELAXKV_MMA_ELECT_ARGS);
+}
+// D[tmem] (+)= A[tmem] * B[smem] over K = 128, B MN-major (128B swizzle): 2048 bytes per K step.  acc_first = 0: the first one overwrites D.
+__device__ __forceinline__ void warp_mma_ts_mnmajor(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc_first) {
+  asm volatile(RELAXKV_MMA_ELECT_HEAD RELAXKV_MMA_TS_ELECT(0, 0, p0) RELAXKV_MMA_TS_ELECT(8, 128, p1) RELAXKV_MMA_TS_ELECT(16, 256, p1)
+               RELAXKV_MMA_TS_ELECT(24, 384, p1) RELAXKV_MMA_TS_ELECT(32, 512, p1) RELAXKV_MMA_TS_ELECT(40, 640, p1)
+               RELAXKV_MMA_TS_ELECT(48, 768, p1) RELAXKV_MMA_TS_ELECT(56, 896, p1) RELAXKV_MMA_ELECT_ARGS);
+}
+__device__ __forceinline__ void warp_mma_commit(uint32_t bar) {
+  asm volatile("{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
+               "@pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
+
 // ---- CTA pairs (cta_group::2): one MMA instruction drives the tensor cores of two SMs ----------------------
 // A cluster of two CTAs; rank 0 (the leader) issues.  For M = 256 each CTA supplies 128 rows of A (its own shared
 // memory or TMEM, same offsets in both), HALF of B's N rows from its own shared memory, and receives its 128 rows
