@@ -8,8 +8,8 @@
 // rows of the step (of one with more than eight heads to a KV head), columns eight blocks.  The product's terms may come in any order as long as both
 // sides agree, so a lane takes D / 2 bytes of its block in 16-byte loads and the queries are laid out to match.  Sums are whole numbers below 2^24:
 // the scores, and with them the lists, do not depend on the order of anything.
-// Selection: one block per (row, KV head); radix passes of 11, 11 and 10 bits find the lowest selected score, then every thread writes its
-// own range's blocks in order.
+// Selection: one block per (row, KV head); counts of digits find the lowest selected score, then every thread writes its own range's blocks in
+// order.
 #include "continuations.cuh"
 #include <algorithm>
 
@@ -158,9 +158,6 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
   const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b], x0 = (((int)blockIdx.x - ct.tile_cu[b]) * kScoWarps + warp) * 8;
   griddep_launch();
   griddep_wait();
-  const RowRange rr = rows_of(a, ct, b);
-  if (rr.n < 0 && threadIdx.x == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, b, ct.max_rows[b]);
-  if (rr.n <= 0) return;
   // this lane's share of its block's 2 D bytes: bytes [tig D / 2, + D / 2)
   const int x = x0 + gid;
   uint32_t bd[D / 8];
@@ -175,6 +172,10 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
   float sb[2];                                                       // scales of the blocks of this lane's result columns
 #pragma unroll
   for (int e = 0; e < 2; ++e) sb[e] = a.scale[(long long)(ct.blk_cu[b] + min(x0 + 2 * tig + e, nb - 1)) * a.Hkv + hd];
+  // (the bounds are on their way)
+  const RowRange rr = rows_of(a, ct, b);
+  if (rr.n < 0 && threadIdx.x == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, b, ct.max_rows[b]);
+  if (rr.n <= 0) return;
   const int n_tiles = (rr.n + kRowsPer - 1) / kRowsPer;
   for (int p0 = 0; p0 < n_tiles; p0 += kScoPass) {
     const int here = min(kScoPass, n_tiles - p0);
@@ -265,10 +266,7 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int xx = x0 + 2 * tig + e;
-            if (xx < nb) {
-              const bool forced = xx < a.n_first || xx >= nb - a.n_last;
-              o[xx] = forced ? INFINITY : best[gid][e] * sb[e] + 0.f;           // (+ 0: one zero, not two)
-            }
+            if (xx < nb) o[xx] = best[gid][e] * sb[e] + 0.f;                     // (+ 0: one zero, not two)
           }
         }
       }
@@ -279,6 +277,8 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
 // ---- the n_select highest scores of a (row, KV head) ------------------------------------------------------------------------------
 
 constexpr int kTopThreads = 256;
+constexpr int kTopKept = 8192;          // scores that a block keeps in shared memory; more are read again by every pass
+constexpr int kTopBits = 10;
 
 // Order-preserving key of a score (no NaN: scores are products of whole numbers and powers of two).
 __device__ __forceinline__ uint32_t score_key(float f) {
@@ -286,11 +286,16 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+// The first and last blocks are taken in any case; of the others the `want` highest.  Their keys' common leading bits are skipped, then digits of ten
+// bits are counted from the highest on until the digit that the want-th key falls into holds no more keys than are wanted: with spread scores
+// two counts.  A launch of few rows is a chain of latencies and barriers.
 __global__ void __launch_bounds__(kTopThreads)
 block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
-  constexpr int kBins = 2048, kBinsPer = kBins / kTopThreads, kWarps = kTopThreads / 32;
+  constexpr int kBins = 1 << kTopBits, kBinsPer = kBins / kTopThreads, kWarps = kTopThreads / 32, U = 8;
+  extern __shared__ uint32_t key_s[];
   __shared__ int hist[kBins];
   __shared__ int warp_sum[kWarps], found[2];
+  __shared__ uint2 warp_range[kWarps];
   __shared__ int2 warp_pair[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hd = (int)(blockIdx.x % a.Hkv);
@@ -305,60 +310,94 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   }
   const int b = context_of(ct, seq), nb = ct.blk_cu[b + 1] - ct.blk_cu[b];
   const RowRange rr = rows_of(a, ct, b);
-  if (rr.n < 0 || row < rr.first || row >= rr.first + rr.n) return;             // reported above, or no row of this context
+  const float* score = a.scores + (row * a.Hkv + hd) * a.most;
   int* out = a.out + (row * a.Hkv + hd) * a.n_select;
+  const bool mine = rr.n >= 0 && row >= rr.first && row < rr.first + rr.n;      // (too many rows: reported with the scores)
   if (nb <= a.n_select) {                                                        // all of them
-    for (int i = tid; i < a.n_select; i += kTopThreads) out[i] = i < nb ? i : -1;
+    for (int i = tid; mine && i < a.n_select; i += kTopThreads) out[i] = i < nb ? i : -1;
     return;
   }
-  const float* score = a.scores + (row * a.Hkv + hd) * a.most;
-  // ---- the n_select-th highest key: 11, 11 and 10 bits at a time ----
-  uint32_t prefix = 0;
-  int want = a.n_select;                                                         // of the keys that share the prefix, the want-th highest
-#pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < kBins; i += kTopThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < nb; i += kTopThreads) {
-      const uint32_t key = score_key(score[i]);
-      if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1);
+  const int x0 = a.n_first, x1 = nb - a.n_last;                                  // blocks that compete: [x0, x1), more than are wanted
+  const bool kept = nb <= kTopKept;
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  for (int i0 = x0 + tid; i0 < x1; i0 += U * kTopThreads) {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = i0 + u * kTopThreads < x1 ? score[i0 + u * kTopThreads] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kTopThreads;
+      if (i < x1) {
+        const uint32_t k = score_key(v[u]);
+        if (kept) key_s[i] = k;
+        lo = min(lo, k);
+        hi = max(hi, k);
+      }
+    }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) warp_range[warp] = make_uint2(lo, hi);
+  for (int i = tid; i < kBins; i += kTopThreads) hist[i] = 0;
+  if (!mine) return;                                                             // (the whole block)
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) { lo = min(lo, warp_range[w].x); hi = max(hi, warp_range[w].y); }
+  auto key_of = [&](int i) -> uint32_t { return kept ? key_s[i] : score_key(score[i]); };
+  int want = a.n_select - a.n_first - a.n_last;                                  // of the keys in [base, base + 2^left), the want-th highest is looked for
+  int left = 32 - __clz(lo ^ hi);                                                // bits that are not common
+  uint32_t base = left >= 32 ? 0u : lo >> left << left;
+  bool all_in = false;                                                           // every key from base on is taken: no ties to break
+  if (want == 0) { base = 0xffffffffu; all_in = true; left = 0; }
+  while (left > 0) {
+    const int shift = max(0, left - kTopBits);
+    for (int i = x0 + tid; i < x1; i += kTopThreads) {
+      const uint32_t d = key_of(i) - base;
+      if (left >= 32 || (d >> left) == 0) atomicAdd(&hist[d >> shift], 1);       // (keys below base wrap round and fall out)
     }
     __syncthreads();
-    // bins from the highest: thread t has bins [top - kBinsPer t - kBinsPer + 1, top - kBinsPer t]
-    const int top = (1 << bits) - 1;
-    int mine = 0;
+    // bins from the highest: thread t has bins (top - kBinsPer (t + 1), top - kBinsPer t]
+    int cnt[kBinsPer], mine_n = 0;
 #pragma unroll
-    for (int e = 0; e < kBinsPer; ++e) { const int bin = top - tid * kBinsPer - e; mine += bin >= 0 ? hist[bin] : 0; }
-    int incl = mine;
+    for (int e = 0; e < kBinsPer; ++e) {
+      const int bin = kBins - 1 - tid * kBinsPer - e;
+      cnt[e] = hist[bin];
+      hist[bin] = 0;
+      mine_n += cnt[e];
+    }
+    int incl = mine_n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    int before = incl - mine;
+    int before = incl - mine_n;
     for (int w = 0; w < warp; ++w) before += warp_sum[w];
-    if (before < want && before + mine >= want) {                                // exactly one thread
-      int acc = before;
+    if (before < want && before + mine_n >= want) {                              // exactly one thread
 #pragma unroll
       for (int e = 0; e < kBinsPer; ++e) {
-        const int bin = top - tid * kBinsPer - e;
-        if (bin < 0) break;
-        if (acc + hist[bin] >= want) { found[0] = bin; found[1] = want - acc; break; }
-        acc += hist[bin];
+        if (before < want && before + cnt[e] >= want) {
+          found[0] = (kBins - 1 - tid * kBinsPer - e) | (before + cnt[e] == want ? 1 << 30 : 0);
+          found[1] = want - before;
+        }
+        before += cnt[e];
       }
     }
     __syncthreads();
-    prefix = pass == 0 ? (uint32_t)found[0] : (prefix << bits) | (uint32_t)found[0];
+    base += (uint32_t)(found[0] & ((1 << 30) - 1)) << shift;
     want = found[1];
+    left = shift;
+    if (found[0] >> 30) { all_in = true; break; }
+    __syncthreads();
   }
-  // ---- keys above the last one, and of the equal ones the first `want`: every thread a range in order ----
+  // ---- keys above, and of those equal to base the first `want`: every thread a range in order ----
   const int per = (nb + kTopThreads - 1) / kTopThreads, i0 = min(nb, tid * per), i1 = min(nb, i0 + per);
+  auto kind = [&](int i) -> int {                                                // 2: taken, 1: equal to the last one, 0: left
+    if (i < x0 || i >= x1) return 2;
+    const uint32_t k = key_of(i);
+    return all_in ? (k >= base ? 2 : 0) : k > base ? 2 : k == base ? 1 : 0;
+  };
   int above = 0, equal = 0;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = score_key(score[i]);
-    above += key > prefix;
-    equal += key == prefix;
-  }
+  for (int i = i0; i < i1; ++i) { const int k = kind(i); above += k == 2; equal += k == 1; }
   int ia = above, ie = equal;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -369,11 +408,11 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   __syncthreads();
   ia -= above; ie -= equal;
   for (int w = 0; w < warp; ++w) { ia += warp_pair[w].x; ie += warp_pair[w].y; }
+  if (all_in) want = 0;
   int at = ia + min(ie, want);
   for (int i = i0; i < i1; ++i) {
-    const uint32_t key = score_key(score[i]);
-    if (key > prefix) out[at++] = i;
-    else if (key == prefix && ie++ < want) out[at++] = i;
+    const int k = kind(i);
+    if (k == 2 || (k == 1 && ie++ < want)) out[at++] = i;
   }
 }
 
@@ -446,5 +485,6 @@ extern "C" relaxkv_status relaxkv_select_blocks(
     rc = cuda_ok(launch_chained(kern, dim3((unsigned)ct.tile_cu[ct.n_req], (unsigned)a.Hkv), kScoWarps * 32, 0, s, ct, a, st));
     if (rc != RELAXKV_OK) return rc;
   }
-  return cuda_ok(launch_chained(block_topk_kernel, dim3((unsigned)(a.n_rows * a.Hkv)), kTopThreads, 0, s, ct, a, st));
+  const size_t smem = a.most <= kTopKept ? (size_t)a.most * 4 : 0;
+  return cuda_ok(launch_chained(block_topk_kernel, dim3((unsigned)(a.n_rows * a.Hkv)), kTopThreads, smem, s, ct, a, st));
 }

@@ -4,16 +4,10 @@
 
 namespace relaxkv {
 
-struct PagedPieces { int n, tiles; };          // pieces of a row, 64-key tiles of a piece
-
-// How the keys of rows of up to `tiles` tiles are cut, for `items` (row, KV head) pairs and room for `slots` resident blocks.  Rows of one
-// length (even): one piece per block, if there are blocks left over.  Of different lengths: some three pieces per block, so that the blocks that walk them end
-// together.  A piece has two tiles at least.
-inline PagedPieces paged_pieces(long long items, long long tiles, int slots, int most, bool even) {
-  const long long want = (even ? slots : 3LL * slots) / std::max<long long>(1, items);
-  const long long n = std::max<long long>(1, std::min<long long>({want, tiles / 2, (long long)most}));
-  const long long per = std::max<long long>(1, (tiles + n - 1) / n);
-  return {(int)std::max<long long>(1, (tiles + per - 1) / per), (int)per};
+// Pieces per row so that a launch of `items` (row, KV head) pairs fills the GPU with two blocks per SM, each piece at least two tiles long.
+inline int paged_pieces(long long items, long long tiles, int sms, int most) {
+  const long long want = std::max<long long>(1, 2LL * sms / std::max<long long>(1, items));
+  return (int)std::max<long long>(1, std::min<long long>({want, (tiles + 1) / 2, (long long)most}));
 }
 
 constexpr double kPrefixStartTiles = 3.0;      // start and end of a block of the prefix kernel, in its 128-key tiles

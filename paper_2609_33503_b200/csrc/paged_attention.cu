@@ -1,12 +1,17 @@
 // Attention of single rows over listed blocks of their context and over their own tokens in the paged store
 // (relaxkv_block_sparse_attention, and the own tokens of relaxkv_shared_prefix_attention).
 //
-// Every key and value meets the G <= 16 query heads of one KV head once: bound by the bytes of K and V.  An item is (row, KV head, piece of the row's
-// keys); a resident block walks items, two blocks to an SM.  Its producer warp streams 64-key tiles through a ring in shared memory, one TMA box
-// per block of the cache (its lanes look the block numbers up a tile ahead and each issues its own box, K and V), and runs on into the next item
-// while the consumers finish one: started block by block, 512 items of eight tiles on average left HBM idle a third of the time (131 MB in 32 us).  Four
-// consumer warps take 16 keys of a tile each: S = Q K^T and O += P V as warp-level MMAs whose 16 rows are the heads (a 128-row tcgen05
-// tile would be 3 to 6 % full), softmax on the fragments.  16 keys never straddle a block, so a chunk's valid keys are one number.
+// Every key and value meets the G <= 16 query heads of one KV head once: bound by the bytes of K and V.  A block of the launch owns (row, KV
+// head, piece of the row's keys); a producer warp streams 64-key tiles through a ring in shared memory, one TMA box per block of the cache (its
+// lanes look the block numbers up a tile ahead and each issues its own box, K and V), and four consumer warps take 16 keys of a tile each:
+// S = Q K^T and O += P V as warp-level MMAs whose 16 rows are the heads (a 128-row tcgen05 tile would be 3 to 6 % full), softmax on the
+// fragments.  16 keys never straddle a block, so a chunk's valid keys are one number.  Tiles of 64 keys and three stages leave room for two
+// blocks per SM, which hide each other's starts.
+// Measured, own tokens of 64 rows of 40 / 8 heads, 512 on average (131 MB) by themselves 32 us, 128 of 2048 blocks for each of 16 rows 66 us (5.9 TB/s of
+// HBM, rows share blocks in L2).  Whole passes of those two: two stages and three blocks per SM 86.6 and 112 us, 32-key tiles and four blocks 86.9 / 136,
+// 128-key tiles and one 86.4 / 102, this 83.8 / 94.  Resident blocks that walk several items, with the producer running ahead, or that
+// share all tiles evenly by a sum over the lengths: 33 us and 72 / 80 of the 66: neither starts nor uneven lengths are what costs here, and rows
+// that start together find shared blocks in L2.
 // Every wait is bounded.
 #include "paged_attention.cuh"
 #include "sm100_ptx.cuh"
@@ -19,22 +24,19 @@ using namespace ptx;
 constexpr int kPagWarps = 4;                          // consumer warps
 constexpr int kPagThreads = (kPagWarps + 1) * 32;
 constexpr int kPagTile = 16 * kPagWarps;              // keys per tile
+constexpr int kPagStages = 3;
 constexpr int kPagEntries = kPagTile / 16;            // boxes of a tile, at most
 constexpr float kLog2eP = 1.4426950408889634f, kLn2P = 0.6931471805599453f;
 
-template <int D, int GMAX>
+template <int D>
 struct PagSmem {
-  static constexpr int kStages = GMAX > 8 && D > 64 ? 2 : 3;      // what leaves two blocks per SM room
   static constexpr int kTileBytes = kPagTile * D * 2;
   static constexpr int kStageBytes = 2 * kTileBytes;              // K tile | V tile
-  static constexpr int kOut = kStages * kStageBytes;              // the warps' partial outputs, for the merge
-  static constexpr int kBar = kOut + (kPagWarps - 1) * GMAX * D * 4;      // full[stages], empty[stages]
-  static constexpr int kStat = kBar + 16 * kStages;               // their maxima and sums
-  static constexpr int kValid = kStat + 8 * kPagWarps * GMAX;     // valid keys of each box of a stage
-  static constexpr int kMisc = kValid + 4 * kStages * kPagEntries;
+  static constexpr int kBar = kPagStages * kStageBytes;           // full[stages], empty[stages]
+  static constexpr int kValid = kBar + 16 * kPagStages;           // valid keys of each box of a stage
+  static constexpr int kMisc = kValid + 4 * kPagStages * kPagEntries;
   static constexpr int kTotal = kMisc + 16;
   static constexpr int kDynamic = kTotal + 1024;
-  static_assert(2 * (kDynamic + 1024) <= 233472, "two blocks per SM: 228 KB, 1 KB of each for the system");
 };
 
 __device__ __forceinline__ void ldsm_x4(uint32_t* r, uint32_t smem_addr) {
@@ -49,51 +51,27 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// An item's row and tiles: [listed context blocks | own tokens], of which this piece has [t0, t1).  A piece is a fixed number of tiles, so that
-// items are alike whatever the rows' lengths; a short row's last pieces are empty.
-struct PagItem { int row, hd, split, n_ctx, t0, t1; RowCheck rc; };
-__device__ __forceinline__ PagItem paged_item(const PagedAttnArgs& a, const ContTable& ct, long long item, int seq, int len) {
-  PagItem p;
-  p.hd = (int)(item % a.Hkv);
-  const long long x = item / a.Hkv;
-  p.row = (int)(x % a.n_rows);
-  p.split = (int)(x / a.n_rows);
-  p.rc = {seq, len, 0};
-  p.n_ctx = p.t0 = p.t1 = 0;
-  if (seq < 0 || seq >= a.n_seq || len < 0 || len > a.max_len || (a.max_len > 0 && len > (long long)a.table_width * a.page)) { p.rc.seq = -1; return p; }
-  p.rc.ctx = context_of(ct, seq);
-  const int box = min(a.ctx_block, kPagTile), per = kPagTile / box;
-  if (a.ctx_keys == CTX_KEYS_LISTED && ct.ctx_len[p.rc.ctx] > 0) p.n_ctx = (a.n_select * (a.ctx_block / box) + per - 1) / per;
-  const int n_tiles = p.n_ctx + (len + kPagTile - 1) / kPagTile;
-  p.t0 = min(n_tiles, p.split * a.piece_tiles);
-  p.t1 = min(n_tiles, p.t0 + a.piece_tiles);
-  return p;
-}
-
 // GMAX: heads of a KV head's group, at most (8 or 16).
 template <int D, int GMAX>
 __global__ void __launch_bounds__(kPagThreads, 2)
 paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_constant__ CUtensorMap tm_cv,
                        const __grid_constant__ CUtensorMap tm_pk, const __grid_constant__ CUtensorMap tm_pv,
                        const __grid_constant__ ContTable ct, const __grid_constant__ PagedAttnArgs a, DeviceStatus* st) {
-  using L = PagSmem<D, GMAX>;
-  constexpr int kStages = L::kStages;
+  using L = PagSmem<D>;
   constexpr int kRowsUsed = GMAX > 8 ? 2 : 1;          // fragment rows gid (and gid + 8) that hold heads
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t bar_full = base + L::kBar, bar_empty = bar_full + 8 * kStages;
+  const uint32_t bar_full = base + L::kBar, bar_empty = bar_full + 8 * kPagStages;
   volatile int* valid_s = reinterpret_cast<volatile int*>(base_ptr + L::kValid);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + L::kMisc);
+  __shared__ float m_s[kPagWarps][GMAX], z_s[kPagWarps][GMAX];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kOwn = D / 8 / kPagWarps;              // of the 8-dim column tiles of O, a warp adds these up
-  auto part_s = [&](int owner, int from, int i) -> float2* {          // warp `from`'s fragment of them: this lane's place
-    return reinterpret_cast<float2*>(base_ptr + L::kOut) + (((owner * (kPagWarps - 1) + from - (from > owner ? 1 : 0)) * kOwn + i) * 32 + lane) * kRowsUsed;
-  };
-  float (*m_s)[GMAX] = reinterpret_cast<float (*)[GMAX]>(base_ptr + L::kStat), (*z_s)[GMAX] = m_s + kPagWarps;
   const int G = a.H / a.Hkv;
+  const int hd = (int)(blockIdx.x % a.Hkv), split = (int)(blockIdx.x / a.Hkv) % a.n_splits;
+  const long long row = blockIdx.x / (a.Hkv * a.n_splits);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, kPagWarps); }
+    for (int s = 0; s < kPagStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, kPagWarps); }
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
@@ -102,252 +80,256 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     if (a.ctx_keys == CTX_KEYS_LISTED) { prefetch_tensormap(&tm_ck); prefetch_tensormap(&tm_cv); }
     if (a.max_len > 0) { prefetch_tensormap(&tm_pk); prefetch_tensormap(&tm_pv); }
   }
+  // what the chain row -> block numbers -> keys begins with, into L2 while the kernels in front finish (prefetches only)
+  if (warp == 0) {
+    if (lane == 0) { prefetch_l2(a.row_seq + row); prefetch_l2(a.row_len + row); prefetch_l2(st); }
+    if (lane < G) prefetch_l2(a.q + (row * a.H + hd * G + lane) * D);
+    if (a.ctx_keys == CTX_KEYS_LISTED && lane * 32 < a.n_select) prefetch_l2(a.lists + (row * a.Hkv + hd) * a.n_select + lane * 32);
+  }
   griddep_launch();
   __syncthreads();
   griddep_wait();                                       // q, the rows and the appended tokens come from the kernels before
   const int status = *reinterpret_cast<volatile int*>(&st->status);
-  const long long n_items = status == RELAXKV_ERR_TIMEOUT ? 0 : a.n_rows * a.Hkv * a.n_splits;
-  auto row_of = [&](long long item) -> long long { return item / a.Hkv % a.n_rows; };
-  int seq = 0, len = 0;                                 // of the item to come
-  if (blockIdx.x < n_items) { const long long r = row_of(blockIdx.x); seq = a.row_seq[r]; len = a.row_len[r]; }
+  const bool teller = threadIdx.x == 0 && split == 0 && hd == 0;
+  const RowCheck rc = known_row(a, ct, row, teller, st);
+  if (rc.seq < 0 || status == RELAXKV_ERR_TIMEOUT) return;
+  // looked at when the results are written: more rows than the host's bound
+  const int rows_first = a.row_cu[ct.seq_cu[rc.ctx]], rows_end = a.row_cu[ct.seq_cu[rc.ctx + 1]];
+  // ---- this piece's tiles: the row's are [listed context blocks | own tokens] ----
+  const int ctx_box = min(a.ctx_block, kPagTile), page_box = min(a.page, kPagTile);
+  const int ctx_sub = a.ctx_block / ctx_box, page_sub = a.page / page_box;             // boxes of a block
+  const int ctx_per = kPagTile / ctx_box, page_per = kPagTile / page_box;              // boxes of a tile
+  const int n_ctx = a.ctx_keys == CTX_KEYS_LISTED && ct.ctx_len[rc.ctx] > 0 ? (a.n_select * ctx_sub + ctx_per - 1) / ctx_per : 0;
+  const int n_tiles = n_ctx + (rc.len + kPagTile - 1) / kPagTile;
+  const int per = (n_tiles + a.n_splits - 1) / a.n_splits;
+  const int t0 = min(n_tiles, split * per), t1 = min(n_tiles, t0 + per);
 
+  float frag_m[2] = {-INFINITY, -INFINITY}, frag_z[2] = {0.f, 0.f}, frag_o[D / 8][4];
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) frag_o[d][0] = frag_o[d][1] = frag_o[d][2] = frag_o[d][3] = 0.f;
   if (warp == kPagWarps) {
     // ================= producer: one lane per box =================
-    const int ctx_box = min(a.ctx_block, kPagTile), page_box = min(a.page, kPagTile);
-    const int ctx_sub = a.ctx_block / ctx_box, page_sub = a.page / page_box;           // boxes of a block
-    const int ctx_per = kPagTile / ctx_box, page_per = kPagTile / page_box;            // boxes of a tile
-    int s = 0;
-    uint32_t phase = 1;                                 // of the stage's empty barrier (the first round does not wait)
-    bool ok = true;
-    for (long long item = blockIdx.x; ok && item < n_items; item += gridDim.x) {
-      const PagItem p = paged_item(a, ct, item, seq, len);
-      if (item + gridDim.x < n_items) { const long long r = row_of(item + gridDim.x); seq = a.row_seq[r]; len = a.row_len[r]; }
-      const int* list = a.ctx_keys == CTX_KEYS_LISTED ? a.lists + ((long long)p.row * a.Hkv + p.hd) * a.n_select : nullptr;
-      const int ctx_len = ct.ctx_len[p.rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
-      auto block_number = [&](int t) -> int {           // of this lane's box of tile t; -1: none
-        if (t >= p.t1) return -1;
-        if (t < p.n_ctx) {
-          const int u = t * ctx_per + lane;
-          return lane < ctx_per && u < a.n_select * ctx_sub ? list[u / ctx_sub] : -1;
-        }
-        const int u = (t - p.n_ctx) * page_per + lane;
-        return lane < page_per && u * page_box < p.rc.len ? a.table[p.rc.seq * a.table_stride + u / page_sub] : -1;
-      };
-      int id = block_number(p.t0);
-      for (int t = p.t0; t < p.t1; ++t) {
-        const int id_next = block_number(t + 1);        // on its way while the ring is full
-        const bool of_ctx = t < p.n_ctx;
-        const int box = of_ctx ? ctx_box : page_box;
-        int valid = 0, token = 0, block = 0;
+    const int* list = a.ctx_keys == CTX_KEYS_LISTED ? a.lists + (row * a.Hkv + hd) * a.n_select : nullptr;
+    const int ctx_len = ct.ctx_len[rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
+    auto block_number = [&](int t) -> int {             // of this lane's box of tile t; -1: none
+      if (t >= t1) return -1;
+      if (t < n_ctx) {
+        const int u = t * ctx_per + lane;
+        return lane < ctx_per && u < a.n_select * ctx_sub ? list[u / ctx_sub] : -1;
+      }
+      const int u = (t - n_ctx) * page_per + lane;
+      return lane < page_per && u * page_box < rc.len ? a.table[rc.seq * a.table_stride + u / page_sub] : -1;
+    };
+    int id = block_number(t0);
+    for (int t = t0, it = 0; t < t1; ++t, ++it) {
+      const int s = it % kPagStages;
+      const int id_next = block_number(t + 1);          // on its way while the ring is full
+      if (it >= kPagStages) {
+        const bool ok = mbar_wait(bar_empty + 8 * s, (uint32_t)((it / kPagStages) - 1) & 1, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) break;
+      }
+      const bool of_ctx = t < n_ctx;
+      const int box = of_ctx ? ctx_box : page_box;
+      int valid = 0, token = 0, block = 0;
+      if (lane < (of_ctx ? ctx_per : page_per)) {
         if (of_ctx) {
           const int off = (t * ctx_per + lane) % ctx_sub * box;
           if (id >= 0 && id < ctx_blocks) {
             valid = max(0, min(box, ctx_len - (id * a.ctx_block + off)));
-            token = (int)(ct.tok_off[p.rc.ctx] + (long long)id * a.ctx_block + off);
+            token = (int)(ct.tok_off[rc.ctx] + (long long)id * a.ctx_block + off);
           } else if (id != -1) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, id, ctx_blocks);
-        } else if (lane < page_per) {
-          const int u = (t - p.n_ctx) * page_per + lane, left = p.rc.len - u * box;
+        } else {
+          const int u = (t - n_ctx) * page_per + lane, left = rc.len - u * box;
           token = u % page_sub * box;
           if (left > 0) {
             if (id >= 0 && id < a.n_blocks) { valid = min(box, left); block = id; }
             else report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, id, a.n_blocks);
           }
         }
-        ok = mbar_wait(bar_empty + 8 * s, phase, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane < kPagEntries) valid_s[s * kPagEntries + lane] = valid;
-        const int n_boxes = __popc(__ballot_sync(0xffffffffu, valid > 0));
-        __syncwarp();                                   // the valid keys of all boxes are written
-        if (lane == 0) mbar_expect_tx(bar_full + 8 * s, (uint32_t)(n_boxes * box * D * 4));
-        __syncwarp();
-        if (valid > 0) {
-          const uint32_t dst = base + s * L::kStageBytes + lane * box * D * 2;
-          tma_load_5d(dst, of_ctx ? &tm_ck : &tm_pk, bar_full + 8 * s, token, p.hd, block);
-          tma_load_5d(dst + L::kTileBytes, of_ctx ? &tm_cv : &tm_pv, bar_full + 8 * s, token, p.hd, block);
-        }
-        id = id_next;
-        if (++s == kStages) { s = 0; phase ^= 1u; }
+        valid_s[s * kPagEntries + lane] = valid;
       }
+      const int n_boxes = __popc(__ballot_sync(0xffffffffu, valid > 0));
+      __syncwarp();                                     // the valid keys of all boxes are written
+      if (lane == 0) mbar_expect_tx(bar_full + 8 * s, (uint32_t)(n_boxes * box * D * 4));
+      __syncwarp();
+      if (valid > 0) {
+        const uint32_t dst = base + s * L::kStageBytes + lane * box * D * 2;
+        tma_load_5d(dst, of_ctx ? &tm_ck : &tm_pk, bar_full + 8 * s, token, hd, block);
+        tma_load_5d(dst + L::kTileBytes, of_ctx ? &tm_cv : &tm_pv, bar_full + 8 * s, token, hd, block);
+      }
+      id = id_next;
     }
   } else {
     // ================= consumers =================
     const int gid = lane >> 2, tig = lane & 3;                        // fragment coordinates: row gid (and gid + 8), column pair tig
-    int s = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (long long item = blockIdx.x; ok && item < n_items; item += gridDim.x) {
-      const PagItem p = paged_item(a, ct, item, seq, len);
-      const long long row = p.row;
-      const bool teller = threadIdx.x == 0 && p.split == 0 && p.hd == 0;
-      if (p.rc.seq < 0) {                                             // no row, or one that the calls refuse
-        if (teller && seq != -1) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, seq >= 0 && seq < a.n_seq ? len : seq, (int)row);
-        if (item + gridDim.x < n_items) { const long long r = row_of(item + gridDim.x); seq = a.row_seq[r]; len = a.row_len[r]; }
-        continue;
+    uint32_t qa[D / 16][4];                                           // the heads as A fragments, the bf16 pairs as stored (the scale goes on S)
+    const uint16_t* q_head = a.q + (row * a.H + hd * G) * D + tig * 2;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2) {
+        qa[ks][h2 * 2] = gid < G ? *reinterpret_cast<const uint32_t*>(q_head + gid * D + ks * 16 + h2 * 8) : 0u;
+        qa[ks][h2 * 2 + 1] = (GMAX > 8 && gid + 8 < G) ? *reinterpret_cast<const uint32_t*>(q_head + (gid + 8) * D + ks * 16 + h2 * 8) : 0u;
       }
-      // looked at when the results are written: more rows than the host's bound
-      const int rows_first = a.row_cu[ct.seq_cu[p.rc.ctx]], rows_end = a.row_cu[ct.seq_cu[p.rc.ctx + 1]];
-      uint32_t qa[D / 16][4];                                         // the heads as A fragments, the bf16 pairs as stored (the scale goes on S)
-      const uint16_t* q_head = a.q + (row * a.H + p.hd * G) * D + tig * 2;
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-          qa[ks][h2 * 2] = gid < G ? *reinterpret_cast<const uint32_t*>(q_head + gid * D + ks * 16 + h2 * 8) : 0u;
-          qa[ks][h2 * 2 + 1] = (GMAX > 8 && gid + 8 < G) ? *reinterpret_cast<const uint32_t*>(q_head + (gid + 8) * D + ks * 16 + h2 * 8) : 0u;
-        }
-      }
-      if (item + gridDim.x < n_items) { const long long r = row_of(item + gridDim.x); seq = a.row_seq[r]; len = a.row_len[r]; }
-      float frag_m[2] = {-INFINITY, -INFINITY}, frag_z[2] = {0.f, 0.f}, frag_o[D / 8][4];
-#pragma unroll
-      for (int d = 0; d < D / 8; ++d) frag_o[d][0] = frag_o[d][1] = frag_o[d][2] = frag_o[d][3] = 0.f;
-      for (int t = p.t0; t < p.t1; ++t) {
-        ok = mbar_wait(bar_full + 8 * s, phase, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const int box = min(t < p.n_ctx ? a.ctx_block : a.page, kPagTile), entry = warp * 16 / box, off = warp * 16 - entry * box;
-        const int n_here = min(16, valid_s[s * kPagEntries + entry] - off);               // keys of this warp's chunk that count
-        if (n_here > 0) {
-          const uint32_t half = (uint32_t)box * 128, chunk = (uint32_t)(entry * box * D * 2 + off * 128);
-          const uint32_t kt = base + s * L::kStageBytes + chunk, vt = kt + L::kTileBytes;
-          if (n_here < 16) {
-            // V rows behind the valid ones belong to nobody (they may hold NaN, and 0 x NaN = NaN on the tensor core): zero them
-            uint8_t* vrows = base_ptr + s * L::kStageBytes + L::kTileBytes + chunk;
-            for (int i = lane; i < (16 - n_here) * (D / 8); i += 32) {
-              const int r = n_here + i / (D / 8), c16 = i % (D / 8);
-              *reinterpret_cast<uint4*>(vrows + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-            }
-            fence_proxy_async_smem();                                 // (the stage's next copy comes through the other proxy)
-            __syncwarp();
+    }
+    for (int t = t0, it = 0; t < t1; ++t, ++it) {
+      const int s = it % kPagStages;
+      bool ok = mbar_wait(bar_full + 8 * s, (uint32_t)(it / kPagStages) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const int box = t < n_ctx ? ctx_box : page_box, entry = warp * 16 / box, off = warp * 16 - entry * box;
+      const int n_here = min(16, valid_s[s * kPagEntries + entry] - off);                 // keys of this warp's chunk that count
+      if (n_here > 0) {
+        const uint32_t half = (uint32_t)box * 128, chunk = (uint32_t)(entry * box * D * 2 + off * 128);
+        const uint32_t kt = base + s * L::kStageBytes + chunk, vt = kt + L::kTileBytes;
+        if (n_here < 16) {
+          // V rows behind the valid ones belong to nobody (they may hold NaN, and 0 x NaN = NaN on the tensor core): zero them
+          uint8_t* vrows = base_ptr + s * L::kStageBytes + L::kTileBytes + chunk;
+          for (int i = lane; i < (16 - n_here) * (D / 8); i += 32) {
+            const int r = n_here + i / (D / 8), c16 = i % (D / 8);
+            *reinterpret_cast<uint4*>(vrows + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
           }
-          // ---- S = Q K^T: two 8-key column tiles ----
-          float sacc[2][4];
+          fence_proxy_async_smem();                                   // (the stage's next copy comes through the other proxy)
+          __syncwarp();
+        }
+        // ---- S = Q K^T: two 8-key column tiles ----
+        float sacc[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          sacc[j][0] = sacc[j][1] = sacc[j][2] = sacc[j][3] = 0.f;
+          const int r = j * 8 + (lane & 7);
+#pragma unroll
+          for (int q4 = 0; q4 < D / 32; ++q4) {
+            const int c16 = 4 * q4 + (lane >> 3);
+            uint32_t kb[4];
+            ldsm_x4(kb, kt + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
+            mma_16816(sacc[j], qa[2 * q4], kb[0], kb[1]);
+            mma_16816(sacc[j], qa[2 * q4 + 1], kb[2], kb[3]);
+          }
+        }
+        // ---- online softmax: this lane holds, of rows gid (and gid + 8), keys 8 j + 2 tig (+ 1) ----
+        uint32_t pa[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int rr = 0; rr < kRowsUsed; ++rr) {
+          float mx = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            sacc[j][0] = sacc[j][1] = sacc[j][2] = sacc[j][3] = 0.f;
-            const int r = j * 8 + (lane & 7);
 #pragma unroll
-            for (int q4 = 0; q4 < D / 32; ++q4) {
-              const int c16 = 4 * q4 + (lane >> 3);
-              uint32_t kb[4];
-              ldsm_x4(kb, kt + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
-              mma_16816(sacc[j], qa[2 * q4], kb[0], kb[1]);
-              mma_16816(sacc[j], qa[2 * q4 + 1], kb[2], kb[3]);
+            for (int e = 0; e < 2; ++e) {
+              const float v = j * 8 + tig * 2 + e < n_here ? sacc[j][2 * rr + e] * a.scale_log2 : -INFINITY;
+              sacc[j][2 * rr + e] = v;
+              mx = fmaxf(mx, v);
             }
           }
-          // ---- online softmax: this lane holds, of rows gid (and gid + 8), keys 8 j + 2 tig (+ 1) ----
-          uint32_t pa[4] = {0u, 0u, 0u, 0u};
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float m_new = fmaxf(frag_m[rr], mx), m_ref = m_new == -INFINITY ? 0.f : m_new;      // (every logit so far may be -inf)
+          const float alpha = fast_exp2(frag_m[rr] - m_ref);
+          frag_m[rr] = m_new;
+          float z = 0.f;
 #pragma unroll
-          for (int rr = 0; rr < kRowsUsed; ++rr) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float v = j * 8 + tig * 2 + e < n_here ? sacc[j][2 * rr + e] * a.scale_log2 : -INFINITY;
-                sacc[j][2 * rr + e] = v;
-                mx = fmaxf(mx, v);
-              }
-            }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const float m_new = fmaxf(frag_m[rr], mx), m_ref = m_new == -INFINITY ? 0.f : m_new;     // (every logit so far may be -inf)
-            const float alpha = fast_exp2(frag_m[rr] - m_ref);
-            frag_m[rr] = m_new;
-            float z = 0.f;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float p0 = fast_exp2(sacc[j][2 * rr] - m_ref), p1 = fast_exp2(sacc[j][2 * rr + 1] - m_ref);
-              z += p0 + p1;
-              const __nv_bfloat162 p01 = __floats2bfloat162_rn(p0, p1);
-              pa[j * 2 + rr] = *reinterpret_cast<const uint32_t*>(&p01);
-            }
-            frag_z[rr] = frag_z[rr] * alpha + z;                      // this lane's keys; the quad is added up at the end
-#pragma unroll
-            for (int d = 0; d < D / 8; ++d) { frag_o[d][2 * rr] *= alpha; frag_o[d][2 * rr + 1] *= alpha; }
+          for (int j = 0; j < 2; ++j) {
+            const float p0 = fast_exp2(sacc[j][2 * rr] - m_ref), p1 = fast_exp2(sacc[j][2 * rr + 1] - m_ref);
+            z += p0 + p1;
+            const __nv_bfloat162 p01 = __floats2bfloat162_rn(p0, p1);
+            pa[j * 2 + rr] = *reinterpret_cast<const uint32_t*>(&p01);
           }
-          // ---- O += P V: V fragments transposed out of the tile, two 8-dim column tiles per load ----
-          const int r = ((lane >> 3) & 1) * 8 + (lane & 7);
+          frag_z[rr] = frag_z[rr] * alpha + z;                        // this lane's keys; the quad is added up at the end
 #pragma unroll
-          for (int dp = 0; dp < D / 16; ++dp) {
-            const int c16 = 2 * dp + (lane >> 4);
-            uint32_t vb[4];
-            ldsm_x4_trans(vb, vt + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
-            mma_16816(frag_o[2 * dp], pa, vb[0], vb[1]);
-            mma_16816(frag_o[2 * dp + 1], pa, vb[2], vb[3]);
-          }
+          for (int d = 0; d < D / 8; ++d) { frag_o[d][2 * rr] *= alpha; frag_o[d][2 * rr + 1] *= alpha; }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_empty + 8 * s);                // this warp is through with the stage
-        if (++s == kStages) { s = 0; phase ^= 1u; }
-      }
-      if (!ok) break;
-      // ---- the warps' results, added up in a fixed order: every warp adds up a quarter of the dims, the others' come through shared memory ----
-      float own[kOwn][2 * kRowsUsed];
+        // ---- O += P V: V fragments transposed out of the tile, two 8-dim column tiles per load ----
+        const int r = ((lane >> 3) & 1) * 8 + (lane & 7);
 #pragma unroll
-      for (int d = 0; d < D / 8; ++d) {
-        if (d / kOwn == warp) {
-#pragma unroll
-          for (int e = 0; e < 2 * kRowsUsed; ++e) own[d % kOwn][e] = frag_o[d][e];
-        } else {
-#pragma unroll
-          for (int rr = 0; rr < kRowsUsed; ++rr) part_s(d / kOwn, warp, d % kOwn)[rr] = make_float2(frag_o[d][2 * rr], frag_o[d][2 * rr + 1]);
+        for (int dp = 0; dp < D / 16; ++dp) {
+          const int c16 = 2 * dp + (lane >> 4);
+          uint32_t vb[4];
+          ldsm_x4_trans(vb, vt + (c16 >> 3) * half + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
+          mma_16816(frag_o[2 * dp], pa, vb[0], vb[1]);
+          mma_16816(frag_o[2 * dp + 1], pa, vb[2], vb[3]);
         }
       }
-#pragma unroll
-      for (int rr = 0; rr < kRowsUsed; ++rr) {
-        frag_z[rr] += __shfl_xor_sync(0xffffffffu, frag_z[rr], 1);
-        frag_z[rr] += __shfl_xor_sync(0xffffffffu, frag_z[rr], 2);
-        if (tig == 0 && gid + 8 * rr < G) { m_s[warp][gid + 8 * rr] = frag_m[rr]; z_s[warp][gid + 8 * rr] = frag_z[rr]; }
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(kPagWarps * 32) : "memory");
-      const bool store = rows_end - rows_first <= ct.max_rows[p.rc.ctx];
-      if (!store && teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, rows_end - rows_first, p.rc.ctx);
-#pragma unroll
-      for (int rr = 0; rr < kRowsUsed; ++rr) {
-        const int g = gid + 8 * rr;
-        if (g < G && store) {
-          float mb = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < kPagWarps; ++w) mb = fmaxf(mb, m_s[w][g]);
-          float wgt[kPagWarps], zb = 0.f;
-#pragma unroll
-          for (int w = 0; w < kPagWarps; ++w) {
-            wgt[w] = mb == -INFINITY ? 0.f : fast_exp2(m_s[w][g] - mb);         // (0 for a warp without keys)
-            zb = fmaf(z_s[w][g], wgt[w], zb);
-          }
-          const bool none = zb == 0.f;                                // no key at all, or none above -inf (NaN stays NaN)
-          const float inv = none ? 0.f : 1.f / zb;
-          const int h = p.hd * G + g;
-          const long long slot = ((long long)(a.slot0 + p.split) * a.n_rows + row) * a.H + h;
-#pragma unroll
-          for (int i = 0; i < kOwn; ++i) {
-            float a0 = 0.f, a1 = 0.f;
-#pragma unroll
-            for (int w = 0; w < kPagWarps; ++w) {
-              const float2 v = w == warp ? make_float2(own[i][2 * rr], own[i][2 * rr + 1]) : part_s(warp, w, i)[rr];
-              a0 = fmaf(v.x, wgt[w], a0);
-              a1 = fmaf(v.y, wgt[w], a1);
-            }
-            const int d = (warp * kOwn + i) * 8 + tig * 2;
-            if (a.n_slots == 1) *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
-            else *reinterpret_cast<float2*>(a.part_o + slot * D + d) = make_float2(a0 * inv, a1 * inv);
-          }
-          if (warp == 0 && tig == 0) {
-            const float lse = none ? -INFINITY : (mb + log2f(zb)) * kLn2P;
-            if (a.n_slots > 1) a.part_lse[slot] = lse;
-            else if (a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = lse;
-          }
-        }
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(kPagWarps * 32) : "memory");      // (the next item's results come into the same place)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_empty + 8 * s);                  // this warp is through with the stage
     }
+#pragma unroll
+    for (int rr = 0; rr < kRowsUsed; ++rr) {
+      frag_z[rr] += __shfl_xor_sync(0xffffffffu, frag_z[rr], 1);
+      frag_z[rr] += __shfl_xor_sync(0xffffffffu, frag_z[rr], 2);
+    }
+  }
+  __syncthreads();                                                    // every tile consumed: the ring is free
+  // ---- the warps' results, added up in a fixed order: every warp adds up a quarter of the dims, the others' come through the ring's place
+  // in fragment order (written head by head, a warp's stores met in eight banks and this took 1.3 us) ----
+  constexpr int kOwn = D / 8 / kPagWarps;                             // of the 8-dim column tiles of O
+  static_assert(kPagWarps * (kPagWarps - 1) * kOwn * 32 * kRowsUsed * 8 <= L::kBar, "they fit the ring");
+  auto part_s = [&](int owner, int from, int i) -> float2* {          // warp `from`'s fragment of tile i of `owner`: this lane's place
+    return reinterpret_cast<float2*>(base_ptr) + (((owner * (kPagWarps - 1) + from - (from > owner ? 1 : 0)) * kOwn + i) * 32 + lane) * kRowsUsed;
+  };
+  const int gid = lane >> 2, tig = lane & 3;
+  float own[kOwn][2 * kRowsUsed];
+  if (warp < kPagWarps && !*abort_flag) {
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) {
+      if (d / kOwn == warp) {
+#pragma unroll
+        for (int e = 0; e < 2 * kRowsUsed; ++e) own[d % kOwn][e] = frag_o[d][e];
+      } else {
+#pragma unroll
+        for (int rr = 0; rr < kRowsUsed; ++rr) part_s(d / kOwn, warp, d % kOwn)[rr] = make_float2(frag_o[d][2 * rr], frag_o[d][2 * rr + 1]);
+      }
+    }
+#pragma unroll
+    for (int rr = 0; rr < kRowsUsed; ++rr)
+      if (tig == 0 && gid + 8 * rr < G) { m_s[warp][gid + 8 * rr] = frag_m[rr]; z_s[warp][gid + 8 * rr] = frag_z[rr]; }
   }
   __syncthreads();
   if (*abort_flag) {
-    if (threadIdx.x == 0) report(st, RELAXKV_ERR_TIMEOUT, KID_PAGED_ATTN, (int)blockIdx.x, 0);
+    if (threadIdx.x == 0) report(st, RELAXKV_ERR_TIMEOUT, KID_PAGED_ATTN, (int)row, hd);
     const uint64_t tw = global_timer_ns();                            // copies still in flight: let them land
     while (global_timer_ns() - tw < 200000ull) __nanosleep(1000);
+    return;
+  }
+  if (rows_end - rows_first > ct.max_rows[rc.ctx]) {
+    if (teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, rows_end - rows_first, rc.ctx);
+    return;
+  }
+  if (warp == kPagWarps) return;
+#pragma unroll
+  for (int rr = 0; rr < kRowsUsed; ++rr) {
+    const int g = gid + 8 * rr;
+    if (g >= G) continue;
+    float mb = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kPagWarps; ++w) mb = fmaxf(mb, m_s[w][g]);
+    float wgt[kPagWarps], zb = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPagWarps; ++w) {
+      wgt[w] = mb == -INFINITY ? 0.f : fast_exp2(m_s[w][g] - mb);     // (0 for a warp without keys)
+      zb = fmaf(z_s[w][g], wgt[w], zb);
+    }
+    const bool none = zb == 0.f;                                      // no key at all, or none above -inf (NaN stays NaN)
+    const float inv = none ? 0.f : 1.f / zb;
+    const int h = hd * G + g;
+    const long long slot = ((long long)(a.slot0 + split) * a.n_rows + row) * a.H + h;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < kPagWarps; ++w) {
+        const float2 v = w == warp ? make_float2(own[i][2 * rr], own[i][2 * rr + 1]) : part_s(warp, w, i)[rr];
+        a0 = fmaf(v.x, wgt[w], a0);
+        a1 = fmaf(v.y, wgt[w], a1);
+      }
+      const int d = (warp * kOwn + i) * 8 + tig * 2;
+      if (a.n_slots == 1) *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
+      else *reinterpret_cast<float2*>(a.part_o + slot * D + d) = make_float2(a0 * inv, a1 * inv);
+    }
+    if (warp == 0 && tig == 0) {
+      const float lse = none ? -INFINITY : (mb + log2f(zb)) * kLn2P;
+      if (a.n_slots > 1) a.part_lse[slot] = lse;
+      else if (a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = lse;
+    }
   }
 }
 
@@ -424,13 +406,12 @@ static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& c
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
   auto kern = paged_attention_kernel<D, GMAX>;
   if (!attr_done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PagSmem<D, GMAX>::kDynamic) != cudaSuccess) return RELAXKV_ERR_CUDA;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PagSmem<D>::kDynamic) != cudaSuccess) return RELAXKV_ERR_CUDA;
     attr_done[dev].store(1, std::memory_order_release);
   }
-  const int sms = sm_count_of_current_device();
-  if (sms <= 0) return RELAXKV_ERR_CUDA;
-  const long long blocks = std::min<long long>(a.n_rows * a.n_splits * a.Hkv, 2LL * sms);
-  return cuda_ok(launch_chained(kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D, GMAX>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
+  const long long blocks = a.n_rows * a.n_splits * a.Hkv;
+  if (blocks > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  return cuda_ok(launch_chained(kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
 }
 
 relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,

@@ -18,7 +18,7 @@ struct PagedAttnArgs {
   int H, Hkv, n_seq;
   int ctx_keys;                        // ContextKeys
   int ctx_block, page;                 // tokens of a context block and of a block of the store
-  int n_splits, piece_tiles;           // pieces a row's keys are cut into, 64-key tiles of one
+  int n_splits;                        // pieces a row's keys are cut into
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };
@@ -38,8 +38,10 @@ __device__ __forceinline__ void tma_prefetch_5d(const CUtensorMap* m, int token,
                ::"l"(reinterpret_cast<uint64_t>(m)), "r"(0), "r"(token), "r"(0), "r"(head), "r"(block) : "memory");
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // Sequence, length and context of a row; seq -1: nothing to do (tell: and the reason is reported).
-__device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
+__device__ __forceinline__ RowCheck known_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
   RowCheck r = {a.row_seq[row], a.row_len[row], 0};
   if (r.seq == -1) return r;
   const bool known = r.seq >= 0 && r.seq < a.n_seq;
@@ -49,6 +51,12 @@ __device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const Cont
     return r;
   }
   r.ctx = context_of(ct, r.seq);
+  return r;
+}
+// And whether its context has no more rows than the host's bound.
+__device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
+  RowCheck r = known_row(a, ct, row, tell, st);
+  if (r.seq < 0) return r;
   const int n = a.row_cu[ct.seq_cu[r.ctx + 1]] - a.row_cu[ct.seq_cu[r.ctx]];
   if (n > ct.max_rows[r.ctx]) {
     if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, n, r.ctx);

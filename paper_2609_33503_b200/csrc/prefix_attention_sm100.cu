@@ -67,8 +67,6 @@ struct PreSmem {
   static_assert(kDynamic <= 232448, "shared memory of a block");
 };
 
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
 template <int D>
 __global__ void __launch_bounds__(kPreThreads, 1)
 prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ContTable ct,
@@ -429,8 +427,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // ---- pieces of the rows' own keys (0: there are none), and of the contexts ----
   const bool own = a.max_len > 0;
-  const PagedPieces cut = paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, 2 * sms, std::max(1, slots / 4), false);
-  const int own_pieces = own ? cut.n : 0;
+  const int own_pieces = own ? paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, sms, std::max(1, slots / 4)) : 0;
   int n_tiles[kMaxReqInline], row_tiles[kMaxReqInline], most = 0;
   for (int b = 0; b < ct.n_req; ++b) {
     n_tiles[b] = (int)(((long long)ct.ctx_len[b] + kPreTile - 1) / kPreTile);
@@ -452,7 +449,6 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   a.slot0 = own ? most : kContSlotsMost;                // without own keys no slot is theirs
   a.n_slots = most + own_pieces;
   a.n_splits = own_pieces;
-  a.piece_tiles = cut.tiles;
   if (a.n_slots <= 1 && !all) a.n_slots = 2;            // rows without any key: the merge writes their zeros
   if (most > 0) {
     rc = D == 128 ? launch_prefix<128>(cache, ct, a, rows_per_tile, s) : launch_prefix<64>(cache, ct, a, rows_per_tile, s);
@@ -482,9 +478,7 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   a.ctx_keys = any_ctx ? CTX_KEYS_LISTED : CTX_KEYS_NONE;
   a.lists = blocks; a.n_select = n_select; a.ctx_block = block_size;
   const long long tiles = ((long long)n_select * block_size + 63) / 64 + (a.max_len + 63) / 64;
-  const PagedPieces cut = paged_pieces(a.n_rows * a.Hkv, tiles, 2 * sms, cont_slots(a.n_rows), true);
-  a.n_splits = cut.n;
-  a.piece_tiles = cut.tiles;
+  a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
   a.slot0 = 0;
   a.n_slots = a.n_splits;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
