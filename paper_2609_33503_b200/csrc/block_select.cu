@@ -300,7 +300,8 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hd = (int)(blockIdx.x % a.Hkv);
   const long long row = blockIdx.x / a.Hkv;
-  griddep_launch();
+  // (No early call for the next kernel: the attention's clusters, placed while these blocks are still there, ran 6 us longer, 29.4 / 35.8 for a
+  // pass over four rows of 32 K.)
   griddep_wait();
   const int seq = a.row_seq[row];
   if (seq == -1) return;

@@ -10,6 +10,13 @@ inline int paged_pieces(long long items, long long tiles, int sms, int most) {
   return (int)std::max<long long>(1, std::min<long long>({want, (tiles + 1) / 2, (long long)most}));
 }
 
+// Pieces that merge among themselves as one cluster of blocks: no launch behind them and no way through memory.  Taken where `most` of
+// them make the launch at least three quarters full, or all there are tiles for.  0: pieces for the merge are better.
+inline int paged_cluster(long long items, long long tiles, int sms, int most) {
+  const int want = paged_pieces(items, tiles, sms, 64);
+  return want <= most ? want : 4 * items * most >= 3LL * 2 * sms ? most : 0;
+}
+
 constexpr double kPrefixStartTiles = 3.0;      // start and end of a block of the prefix kernel, in its 128-key tiles
 
 // Key tiles per block for contexts of n_tiles[0 .. n) tiles and row_tiles[0 .. n) tiles of rows, each times `heads` KV heads, one block per SM.

@@ -26,7 +26,7 @@ constexpr int kPagThreads = (kPagWarps + 1) * 32;
 constexpr int kPagTile = 16 * kPagWarps;              // keys per tile
 constexpr int kPagStages = 3;
 constexpr int kPagEntries = kPagTile / 16;            // boxes of a tile, at most
-constexpr float kLog2eP = 1.4426950408889634f, kLn2P = 0.6931471805599453f;
+constexpr float kLn2P = 0.6931471805599453f;
 
 template <int D>
 struct PagSmem {
@@ -68,7 +68,9 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   __shared__ float m_s[kPagWarps][GMAX], z_s[kPagWarps][GMAX];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.H / a.Hkv;
-  const int hd = (int)(blockIdx.x % a.Hkv), split = (int)(blockIdx.x / a.Hkv) % a.n_splits;
+  // KV heads fastest; with clusters, whose blocks stand side by side, the pieces
+  const int unit = a.cluster ? (int)blockIdx.x / a.n_splits : 0;
+  const int hd = (int)((a.cluster ? unit : blockIdx.x) % a.Hkv), split = (int)(a.cluster ? blockIdx.x - unit * a.n_splits : blockIdx.x / a.Hkv % a.n_splits);
   const long long row = blockIdx.x / (a.Hkv * a.n_splits);
   if (threadIdx.x == 0) {
     for (int s = 0; s < kPagStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, kPagWarps); }
@@ -77,7 +79,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     fence_proxy_async_smem();
   }
   if (threadIdx.x == kPagWarps * 32) {                  // (of maps that there are)
-    if (a.ctx_keys == CTX_KEYS_LISTED) { prefetch_tensormap(&tm_ck); prefetch_tensormap(&tm_cv); }
+    if (a.ctx_keys != CTX_KEYS_NONE) { prefetch_tensormap(&tm_ck); prefetch_tensormap(&tm_cv); }
     if (a.max_len > 0) { prefetch_tensormap(&tm_pk); prefetch_tensormap(&tm_pv); }
   }
   // what the chain row -> block numbers -> keys begins with, into L2 while the kernels in front finish (prefetches only)
@@ -86,21 +88,24 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     if (lane < G) prefetch_l2(a.q + (row * a.H + hd * G + lane) * D);
     if (a.ctx_keys == CTX_KEYS_LISTED && lane * 32 < a.n_select) prefetch_l2(a.lists + (row * a.Hkv + hd) * a.n_select + lane * 32);
   }
-  griddep_launch();
   __syncthreads();
   griddep_wait();                                       // q, the rows and the appended tokens come from the kernels before
   const int status = *reinterpret_cast<volatile int*>(&st->status);
   const bool teller = threadIdx.x == 0 && split == 0 && hd == 0;
   const RowCheck rc = known_row(a, ct, row, teller, st);
-  if (rc.seq < 0 || status == RELAXKV_ERR_TIMEOUT) return;
+  // (a block of a cluster stays to the end: the others read its shared memory)
+  const bool live = rc.seq >= 0 && status != RELAXKV_ERR_TIMEOUT;
+  if (!live && !a.cluster) return;
   // looked at when the results are written: more rows than the host's bound
   const int rows_first = a.row_cu[ct.seq_cu[rc.ctx]], rows_end = a.row_cu[ct.seq_cu[rc.ctx + 1]];
   // ---- this piece's tiles: the row's are [listed context blocks | own tokens] ----
   const int ctx_box = min(a.ctx_block, kPagTile), page_box = min(a.page, kPagTile);
   const int ctx_sub = a.ctx_block / ctx_box, page_sub = a.page / page_box;             // boxes of a block
   const int ctx_per = kPagTile / ctx_box, page_per = kPagTile / page_box;              // boxes of a tile
-  const int n_ctx = a.ctx_keys == CTX_KEYS_LISTED && ct.ctx_len[rc.ctx] > 0 ? (a.n_select * ctx_sub + ctx_per - 1) / ctx_per : 0;
-  const int n_tiles = n_ctx + (rc.len + kPagTile - 1) / kPagTile;
+  const int ctx_len = ct.ctx_len[rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
+  const int listed = a.ctx_keys == CTX_KEYS_NONE || ctx_len == 0 ? 0 : a.ctx_keys == CTX_KEYS_ALL ? ctx_blocks : a.n_select;      // blocks
+  const int n_ctx = (listed * ctx_sub + ctx_per - 1) / ctx_per;
+  const int n_tiles = live ? n_ctx + (rc.len + kPagTile - 1) / kPagTile : 0;
   const int per = (n_tiles + a.n_splits - 1) / a.n_splits;
   const int t0 = min(n_tiles, split * per), t1 = min(n_tiles, t0 + per);
 
@@ -110,12 +115,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   if (warp == kPagWarps) {
     // ================= producer: one lane per box =================
     const int* list = a.ctx_keys == CTX_KEYS_LISTED ? a.lists + (row * a.Hkv + hd) * a.n_select : nullptr;
-    const int ctx_len = ct.ctx_len[rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
     auto block_number = [&](int t) -> int {             // of this lane's box of tile t; -1: none
       if (t >= t1) return -1;
       if (t < n_ctx) {
         const int u = t * ctx_per + lane;
-        return lane < ctx_per && u < a.n_select * ctx_sub ? list[u / ctx_sub] : -1;
+        return lane < ctx_per && u < listed * ctx_sub ? (list ? list[u / ctx_sub] : u / ctx_sub) : -1;
       }
       const int u = (t - n_ctx) * page_per + lane;
       return lane < page_per && u * page_box < rc.len ? a.table[rc.seq * a.table_stride + u / page_sub] : -1;
@@ -259,6 +263,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     }
   }
   __syncthreads();                                                    // every tile consumed: the ring is free
+  griddep_launch();                                                   // (called first thing, sixteen rows of 16 K took 30.1 us, 29.4 so)
   // ---- the warps' results, added up in a fixed order: every warp adds up a quarter of the dims, the others' come through the ring's place
   // in fragment order (written head by head, a warp's stores met in eight banks and this took 1.3 us) ----
   constexpr int kOwn = D / 8 / kPagWarps;                             // of the 8-dim column tiles of O
@@ -284,53 +289,89 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
       if (tig == 0 && gid + 8 * rr < G) { m_s[warp][gid + 8 * rr] = frag_m[rr]; z_s[warp][gid + 8 * rr] = frag_z[rr]; }
   }
   __syncthreads();
-  if (*abort_flag) {
+  const bool aborted = *abort_flag != 0;
+  if (aborted) {
     if (threadIdx.x == 0) report(st, RELAXKV_ERR_TIMEOUT, KID_PAGED_ATTN, (int)row, hd);
     const uint64_t tw = global_timer_ns();                            // copies still in flight: let them land
     while (global_timer_ns() - tw < 200000ull) __nanosleep(1000);
-    return;
+    if (!a.cluster) return;
   }
-  if (rows_end - rows_first > ct.max_rows[rc.ctx]) {
-    if (teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, rows_end - rows_first, rc.ctx);
-    return;
-  }
-  if (warp == kPagWarps) return;
+  const bool fits = rows_end - rows_first <= ct.max_rows[rc.ctx];
+  if (live && !fits && teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, rows_end - rows_first, rc.ctx);
+  if (!fits && !a.cluster) return;
+  // where a cluster's blocks find each other's results: [G][D] normalised, behind them the log-sum-exps (in log2 units; NaN: given up)
+  constexpr int kResult = L::kBar / 2, kResultLse = kResult + GMAX * D * 4;
+  static_assert(kPagWarps * (kPagWarps - 1) * kOwn * 32 * kRowsUsed * 8 <= kResult && kResultLse + GMAX * 4 <= L::kBar, "side by side in the ring");
+  if (warp < kPagWarps) {
 #pragma unroll
-  for (int rr = 0; rr < kRowsUsed; ++rr) {
-    const int g = gid + 8 * rr;
-    if (g >= G) continue;
-    float mb = -INFINITY;
+    for (int rr = 0; rr < kRowsUsed; ++rr) {
+      const int g = gid + 8 * rr;
+      if (g >= G) continue;
+      float mb = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kPagWarps; ++w) mb = fmaxf(mb, m_s[w][g]);
-    float wgt[kPagWarps], zb = 0.f;
-#pragma unroll
-    for (int w = 0; w < kPagWarps; ++w) {
-      wgt[w] = mb == -INFINITY ? 0.f : fast_exp2(m_s[w][g] - mb);     // (0 for a warp without keys)
-      zb = fmaf(z_s[w][g], wgt[w], zb);
-    }
-    const bool none = zb == 0.f;                                      // no key at all, or none above -inf (NaN stays NaN)
-    const float inv = none ? 0.f : 1.f / zb;
-    const int h = hd * G + g;
-    const long long slot = ((long long)(a.slot0 + split) * a.n_rows + row) * a.H + h;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      float a0 = 0.f, a1 = 0.f;
+      for (int w = 0; w < kPagWarps; ++w) mb = fmaxf(mb, m_s[w][g]);
+      float wgt[kPagWarps], zb = 0.f;
 #pragma unroll
       for (int w = 0; w < kPagWarps; ++w) {
-        const float2 v = w == warp ? make_float2(own[i][2 * rr], own[i][2 * rr + 1]) : part_s(warp, w, i)[rr];
-        a0 = fmaf(v.x, wgt[w], a0);
-        a1 = fmaf(v.y, wgt[w], a1);
+        wgt[w] = mb == -INFINITY ? 0.f : fast_exp2(m_s[w][g] - mb);   // (0 for a warp without keys)
+        zb = fmaf(z_s[w][g], wgt[w], zb);
       }
-      const int d = (warp * kOwn + i) * 8 + tig * 2;
-      if (a.n_slots == 1) *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
-      else *reinterpret_cast<float2*>(a.part_o + slot * D + d) = make_float2(a0 * inv, a1 * inv);
-    }
-    if (warp == 0 && tig == 0) {
-      const float lse = none ? -INFINITY : (mb + log2f(zb)) * kLn2P;
-      if (a.n_slots > 1) a.part_lse[slot] = lse;
-      else if (a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = lse;
+      const bool none = zb == 0.f;                                    // no key at all, or none above -inf (NaN stays NaN)
+      const float inv = none ? 0.f : 1.f / zb, lse2 = none ? -INFINITY : mb + log2f(zb);
+      const int h = hd * G + g;
+      const long long slot = ((long long)(a.slot0 + split) * a.n_rows + row) * a.H + h;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPagWarps; ++w) {
+          const float2 v = w == warp ? make_float2(own[i][2 * rr], own[i][2 * rr + 1]) : part_s(warp, w, i)[rr];
+          a0 = fmaf(v.x, wgt[w], a0);
+          a1 = fmaf(v.y, wgt[w], a1);
+        }
+        const int d = (warp * kOwn + i) * 8 + tig * 2;
+        if (a.cluster) *reinterpret_cast<float2*>(base_ptr + kResult + (g * D + d) * 4) = make_float2(a0 * inv, a1 * inv);
+        else if (a.n_slots == 1) *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
+        else *reinterpret_cast<float2*>(a.part_o + slot * D + d) = make_float2(a0 * inv, a1 * inv);
+      }
+      if (warp == 0 && tig == 0) {
+        if (a.cluster) *reinterpret_cast<float*>(base_ptr + kResultLse + g * 4) = aborted ? __uint_as_float(0x7fc00000u) : lse2;
+        else if (a.n_slots > 1) a.part_lse[slot] = lse2 * kLn2P;
+        else if (a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = lse2 * kLn2P;
+      }
     }
   }
+  if (!a.cluster) return;
+  // ---- the cluster's merge: two dims of a head per thread, over the blocks in their order ----
+  cluster_sync();
+  for (int i = split * kPagThreads + (int)threadIdx.x; live && fits && i < G * D / 2; i += a.n_splits * kPagThreads) {
+    const int g = i / (D / 2), d = 2 * (i - g * (D / 2)), h = hd * G + g;
+    float lse[kPagCluster], mx = -INFINITY;
+    float2 v[kPagCluster];
+#pragma unroll
+    for (int r = 0; r < kPagCluster; ++r) {
+      lse[r] = -INFINITY;
+      v[r] = make_float2(0.f, 0.f);
+      if (r < a.n_splits) {
+        const uint32_t peer = mapa_shared(base, (uint32_t)r);
+        lse[r] = ld_cluster_f32(peer + kResultLse + g * 4);
+        v[r] = ld_cluster_f32x2(peer + kResult + (g * D + d) * 4);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kPagCluster; ++r) mx = fmaxf(mx, lse[r]);
+    float a0 = 0.f, a1 = 0.f, den = 0.f;
+#pragma unroll
+    for (int r = 0; r < kPagCluster; ++r) {
+      const float w = lse[r] == -INFINITY ? 0.f : fast_exp2(lse[r] - mx);      // (NaN stays NaN: logits that were, or a block that gave up)
+      den += w;
+      if (w != 0.f) { a0 = fmaf(w, v[r].x, a0); a1 = fmaf(w, v[r].y, a1); }
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
+    if (d == 0 && a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = den == 0.f ? -INFINITY : (mx + log2f(den)) * kLn2P;
+  }
+  cluster_sync();                                                     // nobody leaves while its results are read
 }
 
 // One warp per (row, head): the slots' weights from their log-sum-exps, then their outputs in slot order.  A launch of few rows is a chain of
@@ -411,7 +452,8 @@ static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& c
   }
   const long long blocks = a.n_rows * a.n_splits * a.Hkv;
   if (blocks > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
-  return cuda_ok(launch_chained(kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
+  const int pieces = a.cluster ? a.n_splits : 1;
+  return cuda_ok(launch_chained_clusters(pieces, kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
 }
 
 relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
@@ -420,7 +462,7 @@ relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_
   if (!st) return RELAXKV_ERR_CUDA;
   const int D = shape->head_dim;
   CUtensorMap maps[4] = {};
-  if (a.ctx_keys == CTX_KEYS_LISTED) {
+  if (a.ctx_keys != CTX_KEYS_NONE) {
     long long tokens = 0;
     for (int b = 0; b < ct.n_req; ++b) tokens = std::max(tokens, ct.ctx_len[b] ? ct.tok_off[b] + ct.ctx_len[b] : 0);
     const uint32_t box = (uint32_t)std::min(a.ctx_block, kPagTile);

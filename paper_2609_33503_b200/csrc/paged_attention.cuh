@@ -6,7 +6,9 @@
 namespace relaxkv {
 
 // What a row's keys are made of besides its own tokens.
-enum ContextKeys { CTX_KEYS_NONE = 0, CTX_KEYS_LISTED = 1 };
+enum ContextKeys { CTX_KEYS_NONE = 0, CTX_KEYS_LISTED = 1, CTX_KEYS_ALL = 2 };
+
+constexpr int kPagCluster = 8;         // blocks of a cluster, at most
 
 struct PagedAttnArgs {
   const uint16_t* q;
@@ -19,6 +21,7 @@ struct PagedAttnArgs {
   int ctx_keys;                        // ContextKeys
   int ctx_block, page;                 // tokens of a context block and of a block of the store
   int n_splits;                        // pieces a row's keys are cut into
+  int cluster;                         // 1: the pieces' blocks are a cluster and merge among themselves (n_slots is 1)
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };

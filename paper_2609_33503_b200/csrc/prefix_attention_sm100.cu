@@ -425,6 +425,21 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   if (sms <= 0) return RELAXKV_ERR_CUDA;
   const int D = shape->head_dim, rows_per_tile = kPreTile / (a.H / a.Hkv), slots = cont_slots(a.n_rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // ---- few rows and short contexts: one launch, each row by itself ----
+  // One cluster per (row, KV head), all at once and eight tiles to a block at most: the launches are what such a call takes (four rows of 4 / 1
+  // heads over 1 K, three launches 12.8 us).
+  int longest = 0;
+  for (int b = 0; b < ct.n_req; ++b)
+    if (ct.max_rows[b] > 0) longest = std::max(longest, ct.ctx_len[b]);
+  const long long all_tiles = ((long long)longest + 63) / 64 + (a.max_len + 63) / 64;
+  if (a.n_rows * a.Hkv * kPagCluster <= 2LL * sms && all_tiles <= 8 * kPagCluster) {
+    a.ctx_keys = longest > 0 ? CTX_KEYS_ALL : CTX_KEYS_NONE;
+    a.ctx_block = 64;
+    a.n_splits = (int)std::max<long long>(1, std::min<long long>(kPagCluster, all_tiles / 2));
+    a.cluster = a.n_splits > 1;
+    a.n_slots = 1;
+    return launch_paged_attention(shape, cache, store, ct, a, s);
+  }
   // ---- pieces of the rows' own keys (0: there are none), and of the contexts ----
   const bool own = a.max_len > 0;
   const int own_pieces = own ? paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, sms, std::max(1, slots / 4)) : 0;
@@ -478,9 +493,11 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   a.ctx_keys = any_ctx ? CTX_KEYS_LISTED : CTX_KEYS_NONE;
   a.lists = blocks; a.n_select = n_select; a.ctx_block = block_size;
   const long long tiles = ((long long)n_select * block_size + 63) / 64 + (a.max_len + 63) / 64;
-  a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
+  a.n_splits = paged_cluster(a.n_rows * a.Hkv, tiles, sms, kPagCluster);
+  a.cluster = a.n_splits > 1;
+  if (a.n_splits == 0) a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
   a.slot0 = 0;
-  a.n_slots = a.n_splits;
+  a.n_slots = a.cluster ? 1 : a.n_splits;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((rc = launch_paged_attention(shape, cache, store, ct, a, s)) != RELAXKV_OK) return rc;
   return a.n_slots == 1 ? RELAXKV_OK : launch_continuation_merge(ct, a, shape->head_dim, s);
