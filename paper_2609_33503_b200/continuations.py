@@ -1,0 +1,160 @@
+"""Many continuations of repaired contexts: several samples, beams or follow-up questions that share what a repair has paid for.
+(The paper answers one query per repair; this is its decode step for callers that answer from one repaired context many times.)
+
+The contexts stay in the caches the repair loop leaves them in.  What a continuation ("sequence") adds of its own - a question, the
+answer so far - lives in blocks of a paged store, one per layer, handed out on the GPU.  A step appends some tokens to some sequences: block
+tables and slot maps once for all layers, then per layer the decoder block, with norm, rotation and append of the rows' K/V in one
+launch and attention over [the shared context, the sequence's own tokens].  The context is read once for all its rows; with
+`n_select` only the blocks that each row may need most are read (8-bit bounds of the keys' blocks choose them).
+
+Call sequencing over torch buffers only; every operation runs in the CUDA kernels behind `binding`.
+"""
+from __future__ import annotations
+
+from typing import Dict, List, Optional, Sequence
+
+import torch
+
+from . import binding as B
+from .inputs import BlockShape
+
+
+class Continuations:
+    """Sequences over the contexts of a batch: `seqs[b]` of them continue context b (`ctx_lens[b]` tokens; 0: none).  Room for
+    `n_blocks` blocks of `block_size` own tokens in all, `max_len` to a sequence, and steps of up to `max_rows` rows."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, ctx_lens: Sequence[int], seqs: Sequence[int], n_layers: int,
+                 blk: BlockShape, n_blocks: int, max_len: int, block_size: int = 64, max_rows: Optional[int] = None, n_select: int = 0,
+                 n_first: int = 1, n_last: int = 2, ctx_block: int = 64, device="cuda", softmax_scale: Optional[float] = None):
+        self.H, self.Hkv, self.D, self.blk, self.n_layers = n_q_heads, n_kv_heads, head_dim, blk, int(n_layers)
+        self.device = torch.device(device)
+        self.ctx_lens, self.seqs = [int(x) for x in ctx_lens], [int(x) for x in seqs]
+        self.seq_cu = [sum(self.seqs[:b]) for b in range(len(self.seqs) + 1)]
+        n_seq = self.n_seq = self.seq_cu[-1]
+        self.max_rows = n_seq if max_rows is None else int(max_rows)
+        self.block_size, self.ctx_block = int(block_size), int(ctx_block)
+        self.n_select, self.n_first, self.n_last = int(n_select), int(n_first), int(n_last)
+        self.shape = B.Shape(self.H, self.Hkv, self.D, self.ctx_lens, None, softmax_scale)
+        bf = dict(dtype=torch.bfloat16, device=self.device)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        self.stores = [B.PagedStore(*(torch.empty(n_blocks, self.block_size, self.Hkv, self.D, **bf) for _ in range(2)))
+                       for _ in range(self.n_layers)]
+        self.width = -(-int(max_len) // self.block_size)
+        self.table = torch.full((n_seq, self.width), -1, **i32)
+        self.free = torch.arange(n_blocks - 1, -1, -1, **i32)
+        self._n_free = [torch.full((1,), n_blocks, **i32), torch.empty(1, **i32)]          # before and after a step, in turn
+        self._len = [torch.zeros(n_seq, **i32), torch.empty(n_seq, **i32)]
+        self.base = torch.cat([torch.full((n,), t, **i32) for t, n in zip(self.ctx_lens, self.seqs)] or [torch.empty(0, **i32)])
+        self.lens = [0] * n_seq                        # the host's copy of the lengths: what it asks for is what it gets
+        self.n_free = int(n_blocks)
+        self._new: Dict[tuple, torch.Tensor] = {}
+        R = self.max_rows
+        self.row_cu = torch.empty(n_seq + 1, **i32)
+        self.row_seq, self.row_pos, self.row_len, self.row_slot = (torch.empty(R, **i32) for _ in range(4))
+        e = lambda *s: torch.empty(*s, **bf)
+        C, I = blk.hidden, blk.inter
+        self.x, self.a, self.h = e(R, C), e(R, C), [e(R, C), e(R, C)]
+        self.q, self.k, self.v, self.o = e(R, self.H, self.D), e(R, self.Hkv, self.D), e(R, self.Hkv, self.D), e(R, self.H, self.D)
+        self.gu, self.m = e(R, 2 * I), e(R, I)
+        self.bounds = self.scale = self.blocks = None
+        if self.n_select > 0:
+            nb = sum(-(-t // self.ctx_block) for t in self.ctx_lens)
+            self.bounds = [torch.empty(nb, self.Hkv, 2, self.D, dtype=torch.int8, device=self.device) for _ in range(self.n_layers)]
+            self.scale = [torch.empty(nb, self.Hkv, dtype=torch.float32, device=self.device) for _ in range(self.n_layers)]
+            self.blocks = torch.empty(R, self.Hkv, self.n_select, **i32)
+        nbytes = B.relaxkv_continuation_workspace_bytes(self.shape, R, self.ctx_block if self.n_select else 0)
+        if nbytes == 0:
+            raise B.RelaxKVError(B.ERR_INVALID_ARG, "relaxkv_continuation_workspace_bytes")
+        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        off = (-ws.data_ptr()) % 256
+        self.workspace = ws[off:off + nbytes]
+        self.rows: Optional[B.ContinuationRows] = None
+        self.n_rows = 0
+
+    def context_bounds(self, caches: Sequence[B.CacheView], stream=None) -> None:
+        """Bounds of the context blocks of every layer, for `n_select`: once, when the repair has left the caches as they are to be read."""
+        for l in range(self.n_layers if self.n_select else 0):
+            B.relaxkv_block_bounds(self.shape, caches[l], self.ctx_block, self.bounds[l], self.scale[l], stream=stream)
+
+    def _blocks(self, tokens: int) -> int:
+        return -(-tokens // self.block_size)
+
+    def begin(self, new: Sequence[int], stream=None) -> int:
+        """Begins a step: new[i] tokens of sequence i follow (0: it waits, -1: it ends and gives its blocks back).  Block tables, positions and
+        slots of the rows are made on the device; the rows are those of the sequences in order.  Returns their number."""
+        new = [int(x) for x in new]
+        if len(new) != self.n_seq or any(n < -1 for n in new):
+            raise ValueError(f"a step of {self.n_seq} sequences takes as many counts, -1 or more each")
+        lens = [0 if n < 0 else t + n for t, n in zip(self.lens, new)]
+        rows = sum(n for n in new if n > 0)
+        # what the device would refuse is refused here, before anything has changed
+        if rows > self.max_rows:
+            raise ValueError(f"{rows} rows in a step of at most {self.max_rows}")
+        if any(t > self.width * self.block_size for t in lens):
+            raise ValueError(f"a sequence of {max(lens)} tokens with room for {self.width * self.block_size}")
+        n_free = self.n_free + sum(self._blocks(t) for t in self.lens) - sum(self._blocks(t) for t in lens)
+        if n_free < 0:
+            raise ValueError(f"{-n_free} blocks short: let sequences end, or give the store more")
+        key = tuple(new)
+        if key not in self._new:
+            if len(self._new) > 64:
+                self._new.clear()
+            self._new[key] = torch.tensor(new, dtype=torch.int32, device=self.device)
+        B.relaxkv_build_block_tables(self.block_size, self._len[0], self._new[key], self.base, self.free, self._n_free[0], self.table,
+                                     self._len[1], self._n_free[1], self.row_cu, self.row_seq[:rows], self.row_pos[:rows],
+                                     self.row_len[:rows], self.row_slot[:rows], stream=stream)
+        self._len.reverse()
+        self._n_free.reverse()
+        self.lens, self.n_free, self.n_rows = lens, n_free, rows
+        per_ctx = [sum(n for n in new[a:b] if n > 0) for a, b in zip(self.seq_cu, self.seq_cu[1:])]
+        longest = max([t for t, n in zip(lens, new) if n > 0], default=0)
+        self.rows = B.ContinuationRows(self.seq_cu, per_ctx, longest, self.row_cu, self.row_seq[:rows], self.row_len[:rows], self.table)
+        return rows
+
+    def attention(self, layer: int, cache: Optional[B.CacheView], q: torch.Tensor, out: torch.Tensor, lse_out=None, stream=None) -> None:
+        """Attention of the step's rows at one layer, their own K/V appended: over the whole contexts, or over n_select blocks of them."""
+        if self.n_select == 0:
+            B.relaxkv_shared_prefix_attention(self.shape, cache, self.stores[layer], self.rows, q, out, self.workspace, lse_out=lse_out, stream=stream)
+            return
+        blocks = self.blocks[:q.shape[0]]
+        B.relaxkv_select_blocks(self.shape, self.ctx_block, self.bounds[layer], self.scale[layer], self.rows, q, self.n_first, self.n_last, blocks,
+                                self.workspace, stream=stream)
+        B.relaxkv_block_sparse_attention(self.shape, cache, self.stores[layer], self.rows, self.ctx_block, blocks, q, out, self.workspace,
+                                         lse_out=lse_out, stream=stream)
+
+    def run(self, h0: torch.Tensor, weights: List[Dict[str, torch.Tensor]], caches: Sequence[Optional[B.CacheView]]) -> torch.Tensor:
+        """The step's rows through the decoder: h0 [n_rows, hidden] = their input representations.  Returns the hidden rows
+        after the last layer (one of this object's buffers)."""
+        n, blk = self.n_rows, self.blk
+        if n == 0:
+            return h0
+        x, a, q, k, v, o, gu, m = (t[:n] for t in (self.x, self.a, self.q, self.k, self.v, self.o, self.gu, self.m))
+        h = h0
+        for l, w in enumerate(weights):
+            if "w_qkv" not in w:                        # weight-loading steps, once per layer
+                w["w_qkv"] = B.stack_qkv(w["wq"], w["wk"], w["wv"])
+            if blk.inter % 128 == 0 and "w_gate_up_tiled" not in w:
+                w["w_gate_up_tiled"] = B.tile_gate_up(w["w_gate_up"])
+            h_out = self.h[l % 2][:n]
+            B.relaxkv_rmsnorm(h, w["w_in_norm"], x, blk.eps)
+            B.relaxkv_linear_qkv(x, w["w_qkv"], q, k, v)
+            B.relaxkv_qk_norm_rope_append_paged(self.stores[l], q, k, v, self.row_pos, self.row_slot, blk.rope_theta, q, w.get("w_q_norm"),
+                                                w.get("w_k_norm"), blk.eps)
+            self.attention(l, caches[l], q, o)
+            B.relaxkv_linear(o, w["wo"], a, residual=h)
+            B.relaxkv_rmsnorm(a, w["w_post_norm"], x, blk.eps)
+            if blk.inter % 128 == 0:
+                B.relaxkv_linear_swiglu(x, w["w_gate_up_tiled"], m)
+            else:
+                B.relaxkv_linear(x, w["w_gate_up"], gu)
+                B.relaxkv_swiglu(gu, m)
+            B.relaxkv_linear(m, w["w_down"], h_out, residual=a)
+            h = h_out
+        return h
+
+    def output_head(self, h: torch.Tensor, final_norm: torch.Tensor, w_head: torch.Tensor, logits: torch.Tensor) -> torch.Tensor:
+        """Final RMSNorm and output projection of the given rows: logits [rows, vocab]."""
+        x = self.x[:h.shape[0]]
+        B.relaxkv_rmsnorm(h, final_norm, x, self.blk.eps)
+        B.relaxkv_linear(x, w_head, logits)
+        return logits
