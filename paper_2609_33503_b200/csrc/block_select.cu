@@ -40,7 +40,7 @@ template <int D>
 __global__ void __launch_bounds__(kBndThreads)
 block_bounds_kernel(const uint16_t* k, long long token_stride, long long head_stride, const __grid_constant__ ContTable ct, int block_size, int Hkv,
                     int8_t* bounds, float* scale, int heads_outer) {
-  constexpr int kLanes = D / 8, kTok = 32 / kLanes, U = 8;
+    constexpr int kLanes = D / 8, kTok = 32 / kLanes, U = 8;
   const int lane = threadIdx.x & 31, gl = lane % kLanes, sub = lane / kLanes;
   const long long w = (long long)blockIdx.x * (kBndThreads / 32) + (threadIdx.x >> 5);
   const int n_blocks = ct.blk_cu[ct.n_req];

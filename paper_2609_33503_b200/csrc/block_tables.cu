@@ -11,7 +11,8 @@
 namespace relaxkv {
 
 constexpr int kTabMaxSeq = 4096;
-constexpr int kTabThreads = 512;
+constexpr int kTabThreads = 1024, kTabFew = 512;
+constexpr int kTabPer = kTabMaxSeq / kTabFew;           // sequences of a thread, at most
 
 struct TableArgs {
   int n_seq, block_size, free_capacity, table_width;
@@ -32,7 +33,7 @@ __device__ __forceinline__ int bisect(const int* cu, int n, int x) {
 __global__ void __launch_bounds__(kTabThreads)
 block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   extern __shared__ int cu_s[];
-  int *rows_cu = cu_s, *need_cu = cu_s + a.n_seq + 1, *back_cu = need_cu + a.n_seq + 1;
+  int *rows_cu = cu_s, *need_cu = cu_s + a.n_seq + 1, *back_cu = need_cu + a.n_seq + 1, *had_s = back_cu + a.n_seq + 1;
   __shared__ long long warp_rows[kTabThreads / 32];
   __shared__ int warp_need[kTabThreads / 32], warp_back[kTabThreads / 32];
   griddep_launch();
@@ -43,22 +44,30 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   const int per = (a.n_seq + (int)blockDim.x - 1) / (int)blockDim.x, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
   const long long room = min((long long)a.table_width << shift, 0x7fffffffLL);
   const int n_free = *a.n_free;
-  // a sequence's share of the sums; what it asks for and cannot have counts as nothing
-  auto share = [&](int i, bool tell, int& rows, int& need, int& back) {
-    const int len = a.seq_len[i], add = a.new_len[i];
-    rows = need = back = 0;
-    const bool ok = len >= 0 && len <= room && add <= a.n_rows && (long long)len + max(add, 0) <= room;
-    if (!ok) { if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, i, add); }
-    else if (add < 0) back = blocks_of(len, shift);
-    else { rows = add; need = blocks_of(len + add, shift) - blocks_of(len, shift); }
-  };
+  // lengths and requests by way of shared memory (the requests in the place of a sum that comes later), then a thread's own in registers: what
+  // one asks for and cannot have counts as nothing
+  for (int i = tid; i < a.n_seq; i += (int)blockDim.x) { had_s[i] = a.seq_len[i]; rows_cu[i] = a.new_len[i]; }
+  __syncthreads();
+  int had_[kTabPer], rows_[kTabPer], need_[kTabPer], back_[kTabPer];
+#pragma unroll
+  for (int e = 0; e < kTabPer; ++e) {
+    had_[e] = first + e < last ? had_s[first + e] : 0;
+    rows_[e] = first + e < last ? rows_cu[first + e] : 0;
+  }
   // ---- the sums: this thread's sequences, its warp's threads, the block's warps ----
   long long rows_t = 0;
   int need_t = 0, back_t = 0;
-  for (int i = first; i < last; ++i) {
-    int r, n, k;
-    share(i, teller, r, n, k);
-    rows_t += r; need_t += n; back_t += k;
+#pragma unroll
+  for (int e = 0; e < kTabPer; ++e) {
+    need_[e] = back_[e] = 0;
+    if (e >= per) continue;                             // (the same for all threads)
+    const int len = had_[e], add = rows_[e];
+    const bool ok = len >= 0 && len <= room && add <= a.n_rows && (long long)len + max(add, 0) <= room;
+    if (!ok && teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, first + e, add);
+    rows_[e] = ok ? max(add, 0) : 0;
+    need_[e] = ok && add > 0 ? blocks_of(len + add, shift) - blocks_of(len, shift) : 0;
+    back_[e] = ok && add < 0 ? blocks_of(len, shift) : 0;
+    rows_t += rows_[e]; need_t += need_[e]; back_t += back_[e];
   }
   long long rows_x = rows_t;
   int need_x = need_t, back_x = back_t;
@@ -70,11 +79,23 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   }
   if (lane == 31) { warp_rows[warp] = rows_x; warp_need[warp] = need_x; warp_back[warp] = back_x; }
   __syncthreads();
-  long long rows_before = 0, total_rows = 0;
-  int need_before = 0, back_before = 0, total_need = 0, total_back = 0;
-  for (int w = 0; w < n_warps; ++w) {
-    if (w < warp) { rows_before += warp_rows[w]; need_before += warp_need[w]; back_before += warp_back[w]; }
-    total_rows += warp_rows[w]; total_need += warp_need[w]; total_back += warp_back[w];
+  long long rows_before, total_rows;
+  int need_before, back_before, total_need, total_back;
+  {                                                     // every warp adds up the warps' sums, a warp per lane
+    long long r = lane < n_warps ? warp_rows[lane] : 0;
+    int n = lane < n_warps ? warp_need[lane] : 0, k = lane < n_warps ? warp_back[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long r2 = __shfl_up_sync(0xffffffffu, r, o);
+      const int n2 = __shfl_up_sync(0xffffffffu, n, o), k2 = __shfl_up_sync(0xffffffffu, k, o);
+      if (lane >= o) { r += r2; n += n2; k += k2; }
+    }
+    total_rows = __shfl_sync(0xffffffffu, r, 31);
+    total_need = __shfl_sync(0xffffffffu, n, 31);
+    total_back = __shfl_sync(0xffffffffu, k, 31);
+    rows_before = warp == 0 ? 0 : __shfl_sync(0xffffffffu, r, max(warp - 1, 0));
+    need_before = warp == 0 ? 0 : __shfl_sync(0xffffffffu, n, max(warp - 1, 0));
+    back_before = warp == 0 ? 0 : __shfl_sync(0xffffffffu, k, max(warp - 1, 0));
   }
   // (the sums of the blocks fit 32 bits: a table of 2^31 entries or more is refused on the host)
   const bool nothing = n_free < 0 || (long long)n_free + total_back > a.free_capacity;
@@ -86,16 +107,17 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   {
     long long rows_at = rows_before + rows_x - rows_t;
     int need_at = need_before + need_x - need_t, back_at = back_before + back_x - back_t;
-    for (int i = first; i < last; ++i) {
-      int r, n, k;
-      share(i, false, r, n, k);
+#pragma unroll
+    for (int e = 0; e < kTabPer; ++e) {
+      const int i = first + e;
+      if (i >= last) break;
       rows_cu[i] = grow ? (int)rows_at : 0;
       need_cu[i] = grow ? need_at : 0;
       back_cu[i] = nothing ? 0 : back_at;
-      rows_at += r; need_at += n; back_at += k;
+      rows_at += rows_[e]; need_at += need_[e]; back_at += back_[e];
       if (teller) {
         a.row_cu[i] = rows_cu[i];
-        a.seq_len_out[i] = !nothing && k > 0 ? 0 : a.seq_len[i] + (grow ? r : 0);
+        a.seq_len_out[i] = !nothing && back_[e] > 0 ? 0 : had_[e] + (grow ? rows_[e] : 0);
       }
     }
   }
@@ -104,33 +126,30 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   __syncthreads();
   // ---- the outputs ----
   const int top = n_free + total_back;
-  auto released = [&](int j) -> int {
+  auto released = [&](int j) -> const int* {     // where the j-th released block's number stands
     const int i = bisect(back_cu, a.n_seq, j);
-    return a.table[i * a.table_stride + (j - back_cu[i])];
+    return a.table + i * a.table_stride + (j - back_cu[i]);
   };
-  auto taken = [&](int j) -> int {               // the j-th block of the stack from its end
+  auto taken = [&](int j) -> const int* {        // and that of the j-th block of the stack from its end
     const int at = top - 1 - j;
-    return at < n_free ? a.free_blocks[at] : released(at - n_free);
+    return at < n_free ? a.free_blocks + at : released(at - n_free);
   };
   const long long step = (long long)gridDim.x * blockDim.x, me = (long long)blockIdx.x * blockDim.x + tid;
   for (long long j = me; j < total_need; j += step) {
     const int i = bisect(need_cu, a.n_seq, (int)j);
-    a.table[i * a.table_stride + blocks_of(a.seq_len[i], shift) + ((int)j - need_cu[i])] = taken((int)j);
+    a.table[i * a.table_stride + blocks_of(had_s[i], shift) + ((int)j - need_cu[i])] = *taken((int)j);
   }
-  for (long long j = n_free + me; j < top - total_need; j += step) a.free_blocks[j] = released((int)j - n_free);
+  for (long long j = n_free + me; j < top - total_need; j += step) a.free_blocks[j] = *released((int)j - n_free);
   for (long long r = me; r < a.n_rows; r += step) {
     int seq = -1, pos = 0, len = 0, slot = -1;
     if (r < total_rows) {
       seq = bisect(rows_cu, a.n_seq, (int)r);
-      const int had = a.seq_len[seq], at = had + ((int)r - rows_cu[seq]), have = blocks_of(had, shift), j = at >> shift;
-      const int block = j < have ? a.table[seq * a.table_stride + j] : taken(need_cu[seq] + (j - have));
-      len = at + 1;
+      const int had = had_s[seq], at = had + ((int)r - rows_cu[seq]), have = blocks_of(had, shift), j = at >> shift;
+      const int block = *(j < have ? a.table + seq * a.table_stride + j : taken(need_cu[seq] + (j - have)));
       pos = (a.seq_base ? a.seq_base[seq] : 0) + at;
-      slot = block < 0 ? -1 : (int)(((unsigned)block << shift) + (at & ((1 << shift) - 1)));
-      if (block < 0 || ((long long)block << shift) > 0x7fffffffLL - (1 << shift)) {
-        slot = -1;
-        report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, seq, block);
-      }
+      len = at + 1;
+      if (block >= 0 && ((long long)block << shift) <= 0x7fffffffLL - (1 << shift)) slot = (int)(((unsigned)block << shift) + (at & ((1 << shift) - 1)));
+      else report(st, RELAXKV_ERR_BAD_INDEX, KID_TABLES, seq, block);
     }
     a.row_seq[r] = seq;
     a.row_pos[r] = pos;
@@ -163,12 +182,15 @@ extern "C" relaxkv_status relaxkv_build_block_tables(
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
   if (!attr_done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * 4 * (kTabMaxSeq + 1)) != cudaSuccess)
+    if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * 4 * (kTabMaxSeq + 1)) != cudaSuccess)
       return RELAXKV_ERR_CUDA;
     attr_done[dev].store(1, std::memory_order_release);
   }
   const TableArgs a = {n_seq, block_size, free_capacity, table_width, (long long)table_stride, (long long)n_rows, seq_len, new_len, seq_base, n_free,
                        free_blocks, block_table, seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot};
-  const long long blocks = std::max<long long>(1, std::min<long long>(2LL * sms, (n_rows + kTabThreads - 1) / kTabThreads));
-  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), kTabThreads, 3 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
+  // One block per SM at most: more of them repeat the sums for less than they bring (452 K rows of 1600 sequences: 12.1 us with blocks of 512 threads and two to an SM, 11.8 so).
+  // Few rows: half as many threads, whose sums are ready sooner.
+  const int threads = n_rows > kTabFew && n_seq > kTabFew ? kTabThreads : kTabFew;
+  const long long blocks = std::max<long long>(1, std::min<long long>(sms, (n_rows + threads - 1) / threads));
+  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), (unsigned)threads, 4 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
 }

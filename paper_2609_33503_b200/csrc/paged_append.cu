@@ -5,7 +5,8 @@
 // meets in one lane, and a warp works on two heads of 128 dims (four of 64) at once.  All heads of a row turn by the same angles, so a lane keeps
 // its four (cos, sin) in registers; they are made once per row, one angle per thread in double precision, while the first heads are on their
 // way.  (With 16-byte pieces, the partner in another lane and the angles read from shared memory for every head, 8205 rows of 40 / 8 heads of 128 with
-// norms took 101 us, bound by shared memory.)  Values stay in fp32 from the load to the one rounding at the store.
+// norms took 101 us, bound by shared memory.  Many rows want many warps more than loads in flight per warp: two heads and four blocks per SM 50.4
+// us = 4.7 TB/s, four heads and three 52.6, seven heads and two 53.6.)  Values stay in fp32 from the load to the one rounding at the store.
 #include "continuations.cuh"
 
 namespace relaxkv {
@@ -34,11 +35,11 @@ __device__ __forceinline__ uint2 pack_4(const float* f) {
 // ROWS rows per block, 8 / ROWS warps on each; heads [blockIdx.y * heads_per_block, + heads_per_block) of them, in the order query heads, key heads,
 // value heads.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(kPapThreads)
+__global__ void __launch_bounds__(kPapThreads, ROWS > 1 ? 4 : 1)
 paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* st) {
   constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, half = D / 2;
   constexpr int kWarps = kPapThreads / 32 / ROWS, kUnits = kWarps * kPerWarp;       // warps of a row, heads that they work on at once
-  constexpr int U = 4;                                          // heads that a group of lanes has in flight
+  constexpr int U = ROWS > 1 ? 2 : 4;                           // heads that a group of lanes has in flight
   __shared__ float2 turn_s[ROWS][half];
   const int tid = threadIdx.x, lane = tid & 31, gl = lane % kLanes, rr = (tid >> 5) / kWarps;
   const int unit0 = ((tid >> 5) % kWarps) * kPerWarp + lane / kLanes;
@@ -54,6 +55,7 @@ paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* 
     hi = *reinterpret_cast<const uint2*>(p + half + gl * 4);
   };
   griddep_launch();
+  const double inv_freq = exp2(-a.log2_theta * (2.0 * (tid % half) / D));       // (depends on no earlier kernel)
   griddep_wait();
   uint2 lo[U], hi[U];
 #pragma unroll
@@ -67,9 +69,8 @@ paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* 
     unpack_4(*reinterpret_cast<const uint2*>(a.wk + gl * 4), wk); unpack_4(*reinterpret_cast<const uint2*>(a.wk + half + gl * 4), wk + 4);
   }
   for (int x = tid; x < ROWS * half; x += kPapThreads) {
-    const int r = x / half, i = x - r * half;
+    const int r = x / half, i = x - r * half;                   // (the same dim every time: the block has a multiple of D / 2 threads)
     if (row0 + r < a.n_rows) {
-      const double inv_freq = exp2(-a.log2_theta * (2.0 * i / D));
       double ang = (double)a.positions[row0 + r] * inv_freq;
       ang -= 6.283185307179586 * floor(ang * 0.15915494309189535);
       sincosf((float)ang, &turn_s[r][i].y, &turn_s[r][i].x);

@@ -26,7 +26,7 @@ constexpr int kPagThreads = (kPagWarps + 1) * 32;
 constexpr int kPagTile = 16 * kPagWarps;              // keys per tile
 constexpr int kPagStages = 3;
 constexpr int kPagEntries = kPagTile / 16;            // boxes of a tile, at most
-constexpr float kLn2P = 0.6931471805599453f;
+constexpr float kLog2eP = 1.4426950408889634f, kLn2P = 0.6931471805599453f;
 
 template <int D>
 struct PagSmem {
@@ -342,33 +342,51 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     }
   }
   if (!a.cluster) return;
-  // ---- the cluster's merge: two dims of a head per thread, over the blocks in their order ----
+  // ---- the merge, four dims of a head per thread: the cluster's blocks in their order, then the pieces of the row's context that the kernel
+  // before has left.  In batches whose loads travel together. ----
   cluster_sync();
-  for (int i = split * kPagThreads + (int)threadIdx.x; live && fits && i < G * D / 2; i += a.n_splits * kPagThreads) {
-    const int g = i / (D / 2), d = 2 * (i - g * (D / 2)), h = hd * G + g;
-    float lse[kPagCluster], mx = -INFINITY;
-    float2 v[kPagCluster];
+  const int pieces = ct.pieces[rc.ctx], sources = a.n_splits + pieces;
+  const long long stride = a.n_rows * a.H;
+  for (int i = split * kPagThreads + (int)threadIdx.x; live && fits && i < G * D / 4; i += a.n_splits * kPagThreads) {
+    constexpr int U = 10;
+    const int g = i / (D / 4), d = 4 * (i - g * (D / 4)), h = hd * G + g;
+    const long long at = row * a.H + h;
+    float mx = -INFINITY, den = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < sources; s0 += U) {
+      float lse[U];
+      float4 v[U];
 #pragma unroll
-    for (int r = 0; r < kPagCluster; ++r) {
-      lse[r] = -INFINITY;
-      v[r] = make_float2(0.f, 0.f);
-      if (r < a.n_splits) {
-        const uint32_t peer = mapa_shared(base, (uint32_t)r);
-        lse[r] = ld_cluster_f32(peer + kResultLse + g * 4);
-        v[r] = ld_cluster_f32x2(peer + kResult + (g * D + d) * 4);
+      for (int u = 0; u < U; ++u) {
+        const int r = s0 + u;
+        lse[u] = -INFINITY;
+        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < a.n_splits) {
+          const uint32_t peer = mapa_shared(base, (uint32_t)r);
+          lse[u] = ld_cluster_f32(peer + kResultLse + g * 4);
+          v[u] = ld_cluster_f32x4(peer + kResult + (g * D + d) * 4);
+        } else if (r < sources) {
+          lse[u] = a.part_lse[(r - a.n_splits) * stride + at] * kLog2eP;
+          v[u] = *reinterpret_cast<const float4*>(a.part_o + ((r - a.n_splits) * stride + at) * D + d);
+        }
+      }
+      float m_new = mx;
+#pragma unroll
+      for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, lse[u]);
+      const float alpha = mx == -INFINITY ? 0.f : fast_exp2(mx - m_new);
+      mx = m_new;
+      den *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = lse[u] == -INFINITY ? 0.f : fast_exp2(lse[u] - mx);      // (NaN stays NaN: logits that were, or a block that gave up)
+        den += w;
+        if (w != 0.f) { acc[0] = fmaf(w, v[u].x, acc[0]); acc[1] = fmaf(w, v[u].y, acc[1]); acc[2] = fmaf(w, v[u].z, acc[2]); acc[3] = fmaf(w, v[u].w, acc[3]); }
       }
     }
-#pragma unroll
-    for (int r = 0; r < kPagCluster; ++r) mx = fmaxf(mx, lse[r]);
-    float a0 = 0.f, a1 = 0.f, den = 0.f;
-#pragma unroll
-    for (int r = 0; r < kPagCluster; ++r) {
-      const float w = lse[r] == -INFINITY ? 0.f : fast_exp2(lse[r] - mx);      // (NaN stays NaN: logits that were, or a block that gave up)
-      den += w;
-      if (w != 0.f) { a0 = fmaf(w, v[r].x, a0); a1 = fmaf(w, v[r].y, a1); }
-    }
     const float inv = den == 0.f ? 0.f : 1.f / den;
-    *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + h) * D + d) = __floats2bfloat162_rn(a0 * inv, a1 * inv);
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
+    *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
     if (d == 0 && a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = den == 0.f ? -INFINITY : (mx + log2f(den)) * kLn2P;
   }
   cluster_sync();                                                     // nobody leaves while its results are read

@@ -21,7 +21,7 @@ struct PagedAttnArgs {
   int ctx_keys;                        // ContextKeys
   int ctx_block, page;                 // tokens of a context block and of a block of the store
   int n_splits;                        // pieces a row's keys are cut into
-  int cluster;                         // 1: the pieces' blocks are a cluster and merge among themselves (n_slots is 1)
+  int cluster;                         // 1: a row's pieces are a cluster of blocks, which merges them and what the prefix kernel has left
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };

@@ -442,7 +442,12 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   }
   // ---- pieces of the rows' own keys (0: there are none), and of the contexts ----
   const bool own = a.max_len > 0;
-  const int own_pieces = own ? paged_pieces(a.n_rows * a.Hkv, (a.max_len + 63) / 64, sms, std::max(1, slots / 4)) : 0;
+  // Up to eight pieces of a row's own keys are a cluster that merges them and the pieces of its context, too; more go through slots and the
+  // merge behind.
+  const long long own_tiles = ((long long)a.max_len + 63) / 64;
+  a.n_splits = own ? paged_cluster(a.n_rows * a.Hkv, own_tiles, sms, kPagCluster) : 0;
+  a.cluster = a.n_splits > 0;
+  const int own_pieces = !own || a.cluster ? 0 : paged_pieces(a.n_rows * a.Hkv, own_tiles, sms, std::max(1, slots / 4));
   int n_tiles[kMaxReqInline], row_tiles[kMaxReqInline], most = 0;
   for (int b = 0; b < ct.n_req; ++b) {
     n_tiles[b] = (int)(((long long)ct.ctx_len[b] + kPreTile - 1) / kPreTile);
@@ -461,16 +466,18 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
     most = std::max(most, ct.pieces[b]);
     all &= own || ct.pieces[b] > 0 || ct.max_rows[b] == 0;
   }
-  a.slot0 = own ? most : kContSlotsMost;                // without own keys no slot is theirs
+  a.slot0 = own_pieces > 0 ? most : kContSlotsMost;     // without such pieces no slot is theirs
   a.n_slots = most + own_pieces;
-  a.n_splits = own_pieces;
+  if (own_pieces > 0) a.n_splits = own_pieces;
+  if (a.cluster && most == 0 && a.n_splits == 1) a.cluster = 0, a.n_slots = 1;        // nothing to merge
+  if (a.cluster && a.n_slots == 1) a.n_slots = 2;       // (the prefix kernel is not the last)
   if (a.n_slots <= 1 && !all) a.n_slots = 2;            // rows without any key: the merge writes their zeros
   if (most > 0) {
     rc = D == 128 ? launch_prefix<128>(cache, ct, a, rows_per_tile, s) : launch_prefix<64>(cache, ct, a, rows_per_tile, s);
     if (rc != RELAXKV_OK) return rc;
   }
   if (own && (rc = launch_paged_attention(shape, cache, store, ct, a, s)) != RELAXKV_OK) return rc;
-  return a.n_slots == 1 ? RELAXKV_OK : launch_continuation_merge(ct, a, D, s);
+  return a.n_slots == 1 || a.cluster ? RELAXKV_OK : launch_continuation_merge(ct, a, D, s);
 }
 
 extern "C" relaxkv_status relaxkv_block_sparse_attention(
