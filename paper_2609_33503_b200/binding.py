@@ -272,6 +272,10 @@ class PagedStore:
         return int(self.k.shape[1])
 
 
+def _is_table(t: torch.Tensor) -> bool:
+    return t.dim() == 2 and t.stride(1) == 1 and (t.shape[0] == 1 or t.stride(0) >= t.shape[1])
+
+
 class ContinuationRows:
     """Host-side relaxkv_continuation_rows: the rows of a step over sequences that continue the contexts (sequences [seq_cu[b], seq_cu[b+1])
     continue context b; at most max_rows[b] rows of it, max_len own tokens to a row).  The device tensors are those that
@@ -283,7 +287,7 @@ class ContinuationRows:
             assert t is None or t.dtype == torch.int32
         assert len(max_rows) == len(seq_cu) - 1 and row_cu.numel() == seq_cu[-1] + 1 and row_cu.is_contiguous() and row_seq.is_contiguous()
         assert row_len is None or (row_len.is_contiguous() and row_len.numel() >= row_seq.numel())
-        assert block_table is None or (block_table.dim() == 2 and block_table.stride(1) == 1 and block_table.shape[0] >= seq_cu[-1])
+        assert block_table is None or (_is_table(block_table) and block_table.shape[0] >= seq_cu[-1])
         self._keep = (_i32(seq_cu), _i32(max_rows), row_cu, row_seq, row_len, block_table)
         self.c = _ContinuationRows()
         self.c.n_seq, self.c.n_rows, self.c.max_len = int(seq_cu[-1]), row_seq.numel(), int(max_len)
@@ -525,6 +529,7 @@ def relaxkv_build_block_tables(block_size: int, seq_len: torch.Tensor, new_len: 
                                n_free_out: torch.Tensor, row_cu: torch.Tensor, row_seq: torch.Tensor, row_pos: torch.Tensor,
                                row_len: torch.Tensor, row_slot: torch.Tensor, stream=None) -> None:
     """seq_len, new_len, seq_base [n_seq]; block_table [n_seq, width] (rows any distance apart); row_* [n_rows].  All int32."""
+    assert _is_table(block_table)
     _check(lib().relaxkv_build_block_tables(*_args("..pppp.pp...ppppppp.", seq_len.numel(), int(block_size), seq_len, new_len, seq_base,
                                                    free_blocks, free_blocks.numel(), n_free, block_table, block_table.shape[1],
                                                    max(block_table.stride(0), block_table.shape[1]), row_seq.numel(), seq_len_out, n_free_out,

@@ -313,7 +313,8 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   const RowRange rr = rows_of(a, ct, b);
   const float* score = a.scores + (row * a.Hkv + hd) * a.most;
   int* out = a.out + (row * a.Hkv + hd) * a.n_select;
-  const bool mine = rr.n >= 0 && row >= rr.first && row < rr.first + rr.n;      // (too many rows: reported with the scores)
+  const bool mine = rr.n >= 0 && row >= rr.first && row < rr.first + rr.n;
+  if (!mine && tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, (int)row, b);
   if (nb <= a.n_select) {                                                        // all of them
     for (int i = tid; mine && i < a.n_select; i += kTopThreads) out[i] = i < nb ? i : -1;
     return;

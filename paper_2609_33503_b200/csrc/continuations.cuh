@@ -25,6 +25,9 @@ __device__ __forceinline__ int context_of(const ContTable& ct, int seq) {
   return b;
 }
 
+// Tokens of a context or of a sequence, at most: what a tile adds still fits 32 bits.
+constexpr int kContTokensMost = 0x7fffff00;
+
 inline bool block_size_ok(int32_t bs) { return bs == 16 || bs == 32 || bs == 64 || bs == 128; }
 
 // check_shape, with contexts of no token
@@ -34,8 +37,10 @@ inline relaxkv_status check_contexts(const relaxkv_shape* s) {
   if (s->n_q_heads % s->n_kv_heads != 0) return RELAXKV_ERR_INVALID_ARG;
   if (s->head_dim != 64 && s->head_dim != 128) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (s->n_q_heads / s->n_kv_heads > 16 || s->n_req > kMaxReqInline) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
-  for (int b = 0; b < s->n_req; ++b)
+  for (int b = 0; b < s->n_req; ++b) {
     if (s->h_ctx_len[b] < 0) return RELAXKV_ERR_INVALID_ARG;
+    if (s->h_ctx_len[b] > kContTokensMost) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  }
   if (!(s->softmax_scale > 0.f)) return RELAXKV_ERR_INVALID_ARG;
   return RELAXKV_OK;
 }
@@ -68,6 +73,7 @@ inline relaxkv_status check_rows(const relaxkv_shape* s, const relaxkv_continuat
   if (r->n_rows > 0x7fffffffLL / (s->n_q_heads * 2)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (attend) {
     if (!r->row_len || r->max_len < 0) return RELAXKV_ERR_INVALID_ARG;
+    if (r->max_len > kContTokensMost) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
     if (r->max_len > 0 && (!r->block_table || r->table_width < 1 || r->table_stride < r->table_width)) return RELAXKV_ERR_INVALID_ARG;
   }
   t.n_seq = r->n_seq;

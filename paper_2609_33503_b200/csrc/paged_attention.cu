@@ -7,11 +7,14 @@
 // S = Q K^T and O += P V as warp-level MMAs whose 16 rows are the heads (a 128-row tcgen05 tile would be 3 to 6 % full), softmax on the
 // fragments.  16 keys never straddle a block, so a chunk's valid keys are one number.  Tiles of 64 keys and three stages leave room for two
 // blocks per SM, which hide each other's starts.
-// Measured, own tokens of 64 rows of 40 / 8 heads, 512 on average (131 MB) by themselves 32 us, 128 of 2048 blocks for each of 16 rows 66 us (5.9 TB/s of
-// HBM, rows share blocks in L2).  Whole passes of those two: two stages and three blocks per SM 86.6 and 112 us, 32-key tiles and four blocks 86.9 / 136,
-// 128-key tiles and one 86.4 / 102, this 83.8 / 94.  Resident blocks that walk several items, with the producer running ahead, or that
-// share all tiles evenly by a sum over the lengths: 33 us and 72 / 80 of the 66: neither starts nor uneven lengths are what costs here, and rows
-// that start together find shared blocks in L2.
+// A row's pieces merge among themselves where a cluster of up to eight blocks is enough (four rows of 32 K, 64 blocks each: 15.9 us, 18.1 with a merge
+// behind), and with what the prefix kernel has left of the row's context.
+// Measured, 128 of 2048 blocks for each of 16 rows 66 us (5.9 TB/s of HBM; rows share blocks in L2); own tokens of 64 rows of 40 / 8 heads, 512 on
+// average (131 MB), 33 us: a block's chain row -> block number -> first tile takes 3.4 us and its results 1, between them it has its tiles at the rate
+// of HBM, and blocks of 1 to 17 tiles do not end together.  Whole passes of those two when they took 94 and 83.8: two stages and three blocks per SM
+// 112 and 86.6, 32-key tiles and four blocks 136 / 86.9, 128-key tiles and one 102 / 86.4.  Resident blocks that walk several items, with the
+// producer running ahead (a fixed share of items; items by cluster launch control; an equal share of tiles, found by a sum over the lengths) hid
+// the chain but not the tail, or lost the rows' shared blocks in L2: the first kernel 72 / 71 / 80 us of the 66, the second 33 / 37 / 33.
 // Every wait is bounded.
 #include "paged_attention.cuh"
 #include "sm100_ptx.cuh"
@@ -51,6 +54,7 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+
 // GMAX: heads of a KV head's group, at most (8 or 16).
 template <int D, int GMAX>
 __global__ void __launch_bounds__(kPagThreads, 2)
@@ -296,7 +300,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     while (global_timer_ns() - tw < 200000ull) __nanosleep(1000);
     if (!a.cluster) return;
   }
-  const bool fits = rows_end - rows_first <= ct.max_rows[rc.ctx];
+  const bool fits = rows_fit(a, ct, rc.ctx, rows_first, rows_end, row);
   if (live && !fits && teller) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, rows_end - rows_first, rc.ctx);
   if (!fits && !a.cluster) return;
   // where a cluster's blocks find each other's results: [G][D] normalised, behind them the log-sum-exps (in log2 units; NaN: given up)

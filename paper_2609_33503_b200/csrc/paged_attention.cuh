@@ -56,13 +56,16 @@ __device__ __forceinline__ RowCheck known_row(const PagedAttnArgs& a, const Cont
   r.ctx = context_of(ct, r.seq);
   return r;
 }
-// And whether its context has no more rows than the host's bound.
+// Whether the rows [first, end) of a context are what the host's bounds and the step's rows allow, and this row is one of them.
+__device__ __forceinline__ bool rows_fit(const PagedAttnArgs& a, const ContTable& ct, int ctx, int first, int end, long long row) {
+  return first >= 0 && end <= a.n_rows && end - first <= ct.max_rows[ctx] && row >= first && row < end;
+}
 __device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
   RowCheck r = known_row(a, ct, row, tell, st);
   if (r.seq < 0) return r;
-  const int n = a.row_cu[ct.seq_cu[r.ctx + 1]] - a.row_cu[ct.seq_cu[r.ctx]];
-  if (n > ct.max_rows[r.ctx]) {
-    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, n, r.ctx);
+  const int first = a.row_cu[ct.seq_cu[r.ctx]], end = a.row_cu[ct.seq_cu[r.ctx + 1]];
+  if (!rows_fit(a, ct, r.ctx, first, end, row)) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, end - first, r.ctx);
     r.seq = -1;
   }
   return r;

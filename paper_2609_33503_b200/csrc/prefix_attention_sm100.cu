@@ -374,14 +374,16 @@ static relaxkv_status launch_prefix(const relaxkv_cache_view* cache, const ContT
 
 // Checks that the attention calls share.  Fills ct and what of `a` does not depend on how the keys are cut.
 static relaxkv_status prepare_continuations(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
-                                            const relaxkv_continuation_rows* rows, int ctx_block, const void* q, void* out, float* lse_out,
+                                            const relaxkv_continuation_rows* rows, const void* q, void* out, float* lse_out,
                                             void* workspace, size_t workspace_bytes, ContTable& ct, PagedAttnArgs& a) {
   relaxkv_status rc = check_contexts(shape);
   if (rc != RELAXKV_OK) return rc;
   bool any_ctx = false;
   for (int b = 0; b < shape->n_req; ++b) any_ctx |= shape->h_ctx_len[b] > 0;
   if (any_ctx && (rc = check_cache(shape, cache, true)) != RELAXKV_OK) return rc;
-  fill_contexts(ct, shape, any_ctx ? cache : nullptr, ctx_block);
+  fill_contexts(ct, shape, any_ctx ? cache : nullptr, 0);
+  for (int b = 0; b < ct.n_req; ++b)
+    if (ct.ctx_len[b] > 0 && ct.tok_off[b] > kContTokensMost - ct.ctx_len[b]) return RELAXKV_ERR_UNSUPPORTED_SHAPE;      // a tile's place is 32 bits
   if ((rc = check_rows(shape, rows, true, ct)) != RELAXKV_OK) return rc;
   if (rows->max_len > 0 && (rc = check_store(store, shape->head_dim)) != RELAXKV_OK) return rc;
   if (!q || !out || !workspace || !aligned16(q) || !aligned16(out)) return RELAXKV_ERR_INVALID_ARG;
@@ -419,7 +421,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   RELAXKV_RANGE("relaxkv_shared_prefix_attention");
   ContTable ct;
   PagedAttnArgs a = {};
-  relaxkv_status rc = prepare_continuations(shape, cache, store, rows, 0, q, out, lse_out, workspace, workspace_bytes, ct, a);
+  relaxkv_status rc = prepare_continuations(shape, cache, store, rows, q, out, lse_out, workspace, workspace_bytes, ct, a);
   if (rc != RELAXKV_OK || rows->n_rows == 0) return rc;
   const int sms = sm_count_of_current_device();
   if (sms <= 0) return RELAXKV_ERR_CUDA;
@@ -469,7 +471,10 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   a.slot0 = own_pieces > 0 ? most : kContSlotsMost;     // without such pieces no slot is theirs
   a.n_slots = most + own_pieces;
   if (own_pieces > 0) a.n_splits = own_pieces;
-  if (a.cluster && most == 0 && a.n_splits == 1) a.cluster = 0, a.n_slots = 1;        // nothing to merge
+  if (a.cluster && most == 0 && a.n_splits == 1) {      // nothing to merge
+    a.cluster = 0;
+    a.n_slots = 1;
+  }
   if (a.cluster && a.n_slots == 1) a.n_slots = 2;       // (the prefix kernel is not the last)
   if (a.n_slots <= 1 && !all) a.n_slots = 2;            // rows without any key: the merge writes their zeros
   if (most > 0) {
@@ -489,7 +494,7 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   PagedAttnArgs a = {};
   if (!block_size_ok(block_size)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (!blocks || n_select < 1) return RELAXKV_ERR_INVALID_ARG;
-  relaxkv_status rc = prepare_continuations(shape, cache, store, rows, block_size, q, out, lse_out, workspace, workspace_bytes, ct, a);
+  relaxkv_status rc = prepare_continuations(shape, cache, store, rows, q, out, lse_out, workspace, workspace_bytes, ct, a);
   if (rc != RELAXKV_OK) return rc;
   if (n_select > 0x7fffffff / block_size) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (rows->n_rows == 0) return RELAXKV_OK;

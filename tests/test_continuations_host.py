@@ -72,7 +72,7 @@ ATTEND = [
     (dict(r=rows(max_rows=(2, 6))), INVALID), (dict(r=rows(row_cu=None)), INVALID), (dict(r=rows(row_seq=None)), INVALID),
     (dict(r=rows(row_len=None)), INVALID), (dict(r=rows(block_table=None)), INVALID), (dict(r=rows(table_stride=3)), INVALID),
     (dict(r=rows(table_width=0)), INVALID), (dict(r=rows(max_len=-1)), INVALID), (dict(r=rows(n_rows=-1)), INVALID),
-    (dict(r=rows(n_rows=1 << 30)), SHAPE), (dict(q=None), INVALID), (dict(q=ODD), INVALID), (dict(out=ODD), INVALID), (dict(ws=None), INVALID),
+    (dict(r=rows(n_rows=1 << 30)), SHAPE), (dict(r=rows(max_len=0x7fffffff)), SHAPE), (dict(s=shape(ctx=(0x7fffffff, 0))), SHAPE), (dict(q=None), INVALID), (dict(q=ODD), INVALID), (dict(out=ODD), INVALID), (dict(ws=None), INVALID),
     (dict(ws=0x10010), INVALID), (dict(nbytes=1000), SMALL),
 ]
 

@@ -288,6 +288,13 @@ ATTEND = {
     "contexts of very different length": dict(H=4, Hkv=1, D=128, ctx=[5000, 100, 1, 2500], seqs=[2, 40, 1, 3], own=300, new=1, bs=32),
     "long own, short context": dict(H=8, Hkv=8, D=64, ctx=[20], seqs=[1], own=[1500], new=1, bs=16),
     "a context nobody continues": dict(H=8, Hkv=2, D=64, ctx=[400, 900], seqs=[0, 2], own=20, new=1, bs=16),
+    # (more (row, KV head) pairs than the one-launch form takes)
+    "sixteen heads, many rows": dict(H=32, Hkv=2, D=64, ctx=[500, 129], seqs=[10, 15], own=150, new=1, bs=16, layout="head"),
+    "nine heads, many rows": dict(H=9, Hkv=1, D=128, ctx=[1260], seqs=[45], own=30, new=1, bs=64, ctx_layout="gaps"),
+    "multi head, many rows": dict(H=3, Hkv=3, D=128, ctx=[383, 640], seqs=[12, 5], own=129, new=1, bs=128, ctx_layout="gaps", layout="gaps"),
+    "dim 64, long": dict(H=4, Hkv=4, D=64, ctx=[4500], seqs=[12], own=40, new=1, bs=32, ctx_layout="head"),
+    "several tokens each, many rows": dict(H=8, Hkv=2, D=128, ctx=[700, 64, 0], seqs=[4, 3, 2], own=100, new=[9, 0, 11, 7, 2, 0, 1, 3, 1], bs=16, len_slack=9, bound_slack=3),
+    "large logits, many rows": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[24], own=60, new=1, bs=16, q_scale=12.0),
     "large logits": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[4], own=60, new=1, bs=16, q_scale=12.0),
 }
 
@@ -330,17 +337,19 @@ def test_one_piece_goes_straight_to_the_output():
     s.check()
 
 
-def test_row_maxima_that_grow_along_the_context():
-    s = Step(8, 2, 128, [1500], [6], 40, 1, 16, seed=5)
+@pytest.mark.parametrize("rows", [6, 25])
+def test_row_maxima_that_grow_along_the_context(rows):
+    s = Step(8, 2, 128, [1500], [rows], 40, 1, 16, seed=5)
     ramp = torch.linspace(0.01, 6.0, 1500, device="cuda")[:, None, None]
     s.k[s.at[0]:s.at[0] + 1500] = (s.k[s.at[0]:s.at[0] + 1500].float() * ramp).to(torch.bfloat16)
     s.shared()
     s.check()
 
 
-def test_infinite_keys_give_their_rows_the_weight_they_ask_for():
+@pytest.mark.parametrize("rows", [2, 50])
+def test_infinite_keys_give_their_rows_the_weight_they_ask_for(rows):
     """A key of -inf in a dim where the query is positive has weight zero; where all logits are -inf the row is defined as empty."""
-    s = Step(4, 1, 64, [200], [2], [0, 20], 1, 16, seed=6)
+    s = Step(4, 1, 64, [200], [rows], [0, 20] + [1] * (rows - 2), 1, 16, seed=6)
     s.q[:] = s.q.abs() + 0.1
     s.k[s.at[0] + 3:s.at[0] + 9, 0, 5] = float("-inf")
     s.k[s.at[0] + 150:s.at[0] + 200, 0, 7] = float("-inf")
@@ -348,9 +357,11 @@ def test_infinite_keys_give_their_rows_the_weight_they_ask_for():
     s.check()
 
 
+@pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("what", ["seq", "len", "bound", "block", "gone"])
-def test_shared_prefix_device_refusals(what):
-    s = Step(8, 2, 128, [300, 200], [3, 4], 50, 1, 16, seed=7)
+def test_shared_prefix_device_refusals(what, many):
+    """many: a third context with rows of its own, so that the call takes the prefix kernel."""
+    s = Step(8, 2, 128, [300, 200] + [150] * many, [3, 4] + [20] * many, 50, 1, 16, seed=7)
     skip, want = (), B().ERR_BAD_INDEX
     if what == "seq":
         s.t["row_seq"][2] = 7
@@ -385,8 +396,9 @@ def test_shared_prefix_device_refusals(what):
     s.check(skip=skip)
 
 
-def test_other_stream_and_graph():
-    s = Step(8, 2, 128, [700], [5], 90, 1, 16, seed=8)
+@pytest.mark.parametrize("rows", [5, 30])
+def test_other_stream_and_graph(rows):
+    s = Step(8, 2, 128, [700], [rows], 90, 1, 16, seed=8)
     s.shared()
     ref = s.out.clone()
     rows, ws, side = s.rows(), s.ws(), torch.cuda.Stream()
@@ -406,6 +418,48 @@ def test_other_stream_and_graph():
     torch.cuda.synchronize()
     s.check()
     assert not torch.equal(ref, s.out)
+
+
+@pytest.mark.parametrize("rows", [5, 30])
+def test_plain_launches_and_an_expired_wait(rows):
+    """The same bits with plain launches; after an expired wait nothing is written until the status word has been read."""
+    b = B()
+    s = Step(8, 2, 128, [700], [rows], 90, 1, 16, seed=15)
+    s.shared()
+    ref = s.out.clone()
+    before = b.relaxkv_set_chained_launch(False)
+    try:
+        s.out.fill_(3)
+        s.shared()
+        assert torch.equal(s.out, ref)
+    finally:
+        b.relaxkv_set_chained_launch(before)
+    s.out.fill_(3)
+    b.relaxkv_debug_wait_timeout()
+    lists = torch.zeros(rows, 2, 3, dtype=torch.int32, device="cuda")
+    lists[:, :, 1], lists[:, :, 2] = 2, -1
+    s.shared()
+    s.sparse(64, lists)
+    torch.cuda.synchronize()
+    assert (s.out == 3).all()
+    assert status() == b.ERR_TIMEOUT
+    s.shared()
+    assert torch.equal(s.out, ref) and status() == b.OK
+
+
+def test_rows_that_their_offsets_do_not_hold():
+    """row_cu and row_seq that contradict each other: reported, nothing outside the step's rows is touched."""
+    b = B()
+    for what in ("end", "elsewhere"):
+        s = Step(8, 2, 128, [300, 200], [12, 14], 50, 1, 16, seed=16)
+        if what == "end":
+            s.t["row_cu"][-1] = 27
+        else:
+            s.t["row_seq"][3] = 20
+        s.max_rows = [26, 26]
+        s.shared()
+        assert status() == b.ERR_BAD_INDEX
+        s.check(skip=tuple(range(12, 26)) if what == "end" else (3,))
 
 
 # ---- bounds, selection, sparse attention ----------------------------------------------------------------------------------------------
@@ -481,6 +535,41 @@ def test_select_and_sparse_attention(name, block, n_select, n_first, n_last):
     s.sparse(block, lists)
     assert status() == b.OK
     s.check(block, lists.cpu().numpy())
+
+
+@pytest.mark.parametrize("n_select,n_first,n_last", [(300, 1, 2), (2, 1, 1), (8700, 0, 3)])
+def test_selection_among_very_many_blocks(n_select, n_first, n_last):
+    """8750 blocks: more than a block of the launch keeps in shared memory."""
+    b = B()
+    s = Step(2, 1, 64, [140000], [3], 3, 1, 16, seed=17)
+    bounds, scale = get_bounds(s, 16)
+    lists = torch.full((3, 1, n_select), -9, dtype=torch.int32, device="cuda")
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, n_first, n_last, lists, s.ws(16))
+    assert status() == b.OK
+    bi, sc, q = bounds.cpu().numpy().astype(np.int64), f64(scale), f64(s.q)
+    for r in range(3):
+        assert np.array_equal(lists[r].cpu().numpy(), orc.select(q[r], bi, sc, n_select, n_first, n_last))
+
+
+@pytest.mark.parametrize("what", ["bound", "seq", "gone"])
+def test_selection_device_refusals(what):
+    b = B()
+    s = Step(8, 2, 64, [900, 200], [3, 4], 5, 1, 16, seed=18)
+    bounds, scale = get_bounds(s, 16)
+    good = torch.full((7, 2, 20), -9, dtype=torch.int32, device="cuda")
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, 1, 1, good, s.ws(16))
+    lists, skip, want = torch.full_like(good, -9), [2], b.ERR_BAD_INDEX
+    if what == "bound":
+        s.max_rows[0], skip = 2, [0, 1, 2]
+    elif what == "seq":
+        s.t["row_seq"][2] = 9
+    else:
+        s.t["row_seq"][2], want = -1, b.OK
+    assert status() == b.OK
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, 1, 1, lists, s.ws(16))
+    assert status() == want
+    keep = [r for r in range(7) if r not in skip]
+    assert (lists[skip] == -9).all() and torch.equal(lists[keep], good[keep])
 
 
 def test_equal_scores_go_to_the_lower_block():
