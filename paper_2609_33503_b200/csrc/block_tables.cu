@@ -11,8 +11,8 @@
 namespace relaxkv {
 
 constexpr int kTabMaxSeq = 4096;
-constexpr int kTabThreads = 1024, kTabFew = 512;
-constexpr int kTabPer = kTabMaxSeq / kTabFew;           // sequences of a thread, at most
+constexpr int kTabThreads = 1024;
+constexpr int kTabPer = kTabMaxSeq / kTabThreads;           // sequences of a thread, at most
 
 struct TableArgs {
   int n_seq, block_size, free_capacity, table_width;
@@ -38,15 +38,15 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   __shared__ int warp_need[kTabThreads / 32], warp_back[kTabThreads / 32];
   griddep_launch();
   griddep_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = (int)blockDim.x >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = kTabThreads / 32;
   const int shift = 31 - __clz(a.block_size);
   const bool teller = blockIdx.x == 0;
-  const int per = (a.n_seq + (int)blockDim.x - 1) / (int)blockDim.x, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
+  const int per = (a.n_seq + kTabThreads - 1) / kTabThreads, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
   const long long room = min((long long)a.table_width << shift, 0x7fffffffLL);
   const int n_free = *a.n_free;
   // lengths and requests by way of shared memory (the requests in the place of a sum that comes later), then a thread's own in registers: what
   // one asks for and cannot have counts as nothing
-  for (int i = tid; i < a.n_seq; i += (int)blockDim.x) { had_s[i] = a.seq_len[i]; rows_cu[i] = a.new_len[i]; }
+  for (int i = tid; i < a.n_seq; i += kTabThreads) { had_s[i] = a.seq_len[i]; rows_cu[i] = a.new_len[i]; }
   __syncthreads();
   int had_[kTabPer], rows_[kTabPer], need_[kTabPer], back_[kTabPer];
 #pragma unroll
@@ -134,7 +134,7 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
     const int at = top - 1 - j;
     return at < n_free ? a.free_blocks + at : released(at - n_free);
   };
-  const long long step = (long long)gridDim.x * blockDim.x, me = (long long)blockIdx.x * blockDim.x + tid;
+  const long long step = (long long)gridDim.x * kTabThreads, me = (long long)blockIdx.x * kTabThreads + tid;
   for (long long j = me; j < total_need; j += step) {
     const int i = bisect(need_cu, a.n_seq, (int)j);
     a.table[i * a.table_stride + blocks_of(had_s[i], shift) + ((int)j - need_cu[i])] = *taken((int)j);
@@ -188,9 +188,8 @@ extern "C" relaxkv_status relaxkv_build_block_tables(
   }
   const TableArgs a = {n_seq, block_size, free_capacity, table_width, (long long)table_stride, (long long)n_rows, seq_len, new_len, seq_base, n_free,
                        free_blocks, block_table, seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot};
-  // One block per SM at most: more of them repeat the sums for less than they bring (452 K rows of 1600 sequences: 12.1 us with blocks of 512 threads and two to an SM, 11.8 so).
-  // Few rows: half as many threads, whose sums are ready sooner.
-  const int threads = n_rows > kTabFew && n_seq > kTabFew ? kTabThreads : kTabFew;
-  const long long blocks = std::max<long long>(1, std::min<long long>(sms, (n_rows + threads - 1) / threads));
-  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), (unsigned)threads, 4 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
+  // One block per SM at most: more of them repeat the sums for less than they bring (452 K rows of 1600 sequences: 12.1 us with blocks of 512
+  // threads and two to an SM, 11.8 so; a million rows of 4096 sequences 17.9 with 512 threads, 14.0 so; few rows make no difference).
+  const long long blocks = std::max<long long>(1, std::min<long long>(sms, (n_rows + kTabThreads - 1) / kTabThreads));
+  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), kTabThreads, 4 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
 }

@@ -109,6 +109,8 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // call in front of the barrier the warps that had nothing to do let the next kernels come at once.  Their blocks then crowd onto the SMs that
 // the first finished blocks leave (40 requests of up to 5 K, gather and attention 49.7 us, now 39; scoring one 16 K layer
 // 65.9 / 62.9, a query pass over 8 K 1383 / 1336).
+// One kernel reads before its wait: the attention over a row's own tokens behind the prefix kernel, which calls griddep_launch() after its own
+// griddep_wait().  What the kernels in front of these two have written is complete by then; the prefix kernel's results are read after the wait.
 // Both instructions do nothing in a kernel that was launched the plain way.
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -5,13 +5,14 @@
 // meets in one lane, and a warp works on two heads of 128 dims (four of 64) at once.  All heads of a row turn by the same angles, so a lane keeps
 // its four (cos, sin) in registers; they are made once per row, one angle per thread in double precision, while the first heads are on their
 // way.  (With 16-byte pieces, the partner in another lane and the angles read from shared memory for every head, 8205 rows of 40 / 8 heads of 128 with
-// norms took 101 us, bound by shared memory.  Many rows want many warps more than loads in flight per warp: two heads and four blocks per SM 50.4
-// us = 4.7 TB/s, four heads and three 52.6, seven heads and two 53.6.)  Values stay in fp32 from the load to the one rounding at the store.
+// norms took 101 us, bound by shared memory.)  Now 49 us = 4.8 TB/s.  Two heads per group of lanes are on their way while two are worked on, and four
+// blocks share an SM: with four heads and three blocks 53 us, with one and six 78.  Values stay in fp32 from the load to the one rounding at the
+// store.
 #include "continuations.cuh"
 
 namespace relaxkv {
 
-constexpr int kPapThreads = 256;
+constexpr int kPapThreads = 256, kPapAhead = 2;
 
 struct PagedAppendArgs {
   const uint16_t *q, *k, *v, *wq, *wk;
@@ -32,24 +33,22 @@ __device__ __forceinline__ uint2 pack_4(const float* f) {
   return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// ROWS rows per block, 8 / ROWS warps on each; heads [blockIdx.y * heads_per_block, + heads_per_block) of them, in the order query heads, key heads,
-// value heads.
+// ROWS rows per block, 8 / ROWS warps on each, all heads in the order query heads, key heads, value heads.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(kPapThreads, ROWS > 1 ? 4 : 1)
-paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* st) {
+__global__ void __launch_bounds__(kPapThreads, 4)
+paged_append_kernel(const PagedAppendArgs a, DeviceStatus* st) {
   constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, half = D / 2;
   constexpr int kWarps = kPapThreads / 32 / ROWS, kUnits = kWarps * kPerWarp;       // warps of a row, heads that they work on at once
-  constexpr int U = ROWS > 1 ? 2 : 4;                           // heads that a group of lanes has in flight
+  constexpr int U = kPapAhead;                                  // heads that a group of lanes has in flight
   __shared__ float2 turn_s[ROWS][half];
   const int tid = threadIdx.x, lane = tid & 31, gl = lane % kLanes, rr = (tid >> 5) / kWarps;
   const int unit0 = ((tid >> 5) % kWarps) * kPerWarp + lane / kLanes;
   const long long row0 = (long long)blockIdx.x * ROWS, row = row0 + rr;
   const bool here = row < a.n_rows;
-  const int n_heads = a.H + 2 * a.Hkv, h0 = blockIdx.y * heads_per_block, total = here ? min(heads_per_block, n_heads - h0) : 0;
-  auto load = [&](int u, uint2& lo, uint2& hi) {
+  const int total = here ? a.H + 2 * a.Hkv : 0;
+  auto load = [&](int h, uint2& lo, uint2& hi) {
     lo = hi = make_uint2(0u, 0u);
-    if (u >= total) return;
-    const int h = h0 + u;
+    if (h >= total) return;
     const uint16_t* p = h < a.H ? a.q + (row * a.H + h) * D : h < a.H + a.Hkv ? a.k + (row * a.Hkv + (h - a.H)) * D : a.v + (row * a.Hkv + (h - a.H - a.Hkv)) * D;
     lo = *reinterpret_cast<const uint2*>(p + gl * 4);
     hi = *reinterpret_cast<const uint2*>(p + half + gl * 4);
@@ -79,7 +78,7 @@ paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* 
   long long place = -1;                                         // of the row in the store
   if (slot >= 0 && (slot >> a.block_shift) < a.n_blocks)
     place = (long long)(slot >> a.block_shift) * a.block_stride + (slot & ((1 << a.block_shift) - 1)) * a.token_stride;
-  else if (slot != -1 && unit0 == 0 && gl == 0 && blockIdx.y == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_APPEND, (int)row, slot);
+  else if (slot != -1 && unit0 == 0 && gl == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_APPEND, (int)row, slot);
   __syncthreads();
   float2 cs[4];
 #pragma unroll
@@ -90,8 +89,8 @@ paged_append_kernel(const PagedAppendArgs a, int heads_per_block, DeviceStatus* 
     for (int u = 0; u < U; ++u) load(u0 + (U + u) * kUnits, nlo[u], nhi[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int x = u0 + u * kUnits, h = h0 + x;
-      const bool live = x < total, is_q = h < a.H, is_v = h >= a.H + a.Hkv;
+      const int h = u0 + u * kUnits;
+      const bool live = h < total, is_q = h < a.H, is_v = h >= a.H + a.Hkv;
       float f[8];
       unpack_4(lo[u], f); unpack_4(hi[u], f + 4);
       if (a.wq != nullptr) {
@@ -140,7 +139,8 @@ extern "C" relaxkv_status relaxkv_qk_norm_rope_append_paged(
   if (rc != RELAXKV_OK) return rc;
   if (n_rows == 0) return RELAXKV_OK;
   DeviceStatus* st = status_word();
-  if (!st) return RELAXKV_ERR_CUDA;
+  const int sms = sm_count_of_current_device();
+  if (!st || sms <= 0) return RELAXKV_ERR_CUDA;
   PagedAppendArgs a = {};
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
   a.wq = static_cast<const uint16_t*>(w_q_norm); a.wk = static_cast<const uint16_t*>(w_k_norm);
@@ -152,13 +152,12 @@ extern "C" relaxkv_status relaxkv_qk_norm_rope_append_paged(
   a.log2_theta = log2((double)theta);
   const int n_heads = n_q_heads + 2 * n_kv_heads;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (n_rows >= 1024) {                         // a row per warp, all its heads
-    const dim3 grid((unsigned)((n_rows + 7) / 8), 1);
-    auto kern = head_dim == 128 ? paged_append_kernel<128, 8> : paged_append_kernel<64, 8>;
-    return cuda_ok(launch_chained(kern, grid, kPapThreads, 0, s, a, n_heads, st));
-  }
-  const int per = head_dim == 128 ? 16 : 32;    // one head per group of lanes
-  const dim3 grid((unsigned)n_rows, (unsigned)((n_heads + per - 1) / per));
-  auto kern = head_dim == 128 ? paged_append_kernel<128, 1> : paged_append_kernel<64, 1>;
-  return cuda_ok(launch_chained(kern, grid, kPapThreads, 0, s, a, per, st));
+  // Rows of a block: eight of so few heads that a warp has them all at once (8205 rows of 4 / 1 heads of 64: 5.2 us, 7.8 with four rows); else one
+  // while the SMs hold the launch's blocks in two turns or less (40 / 8 heads, 64 rows 4.8 us, 1024 rows 8.5; with four 8.4 and 15.0), four for
+  // more (4096 rows 26.8, 8205 rows 49.2; with one 32.5 and 61.3, with two 29.3 and 54.3, with eight 31.0 and 50.3).
+  const bool small = n_heads <= kPapAhead * (256 / head_dim);
+  const int per = small ? 8 : n_rows <= 8LL * sms ? 1 : 4;
+  auto kern = head_dim == 128 ? (per == 8 ? paged_append_kernel<128, 8> : per == 4 ? paged_append_kernel<128, 4> : paged_append_kernel<128, 1>)
+                              : (per == 8 ? paged_append_kernel<64, 8> : per == 4 ? paged_append_kernel<64, 4> : paged_append_kernel<64, 1>);
+  return cuda_ok(launch_chained(kern, dim3((unsigned)((n_rows + per - 1) / per)), kPapThreads, 0, s, a, st));
 }

@@ -22,11 +22,12 @@ struct PagedAttnArgs {
   int ctx_block, page;                 // tokens of a context block and of a block of the store
   int n_splits;                        // pieces a row's keys are cut into
   int cluster;                         // 1: a row's pieces are a cluster of blocks, which merges them and what the prefix kernel has left
+  int behind_prefix;                   // 1: launched by the prefix kernel, once the kernels in front of that one are complete
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };
 
-// Whether row r is one that the calls work on: its sequence and length in range, its context's rows within the host's bound.
+// A row's sequence (-1: not one to work on), its own tokens and its context.
 struct RowCheck { int seq, len, ctx; };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int token, int head, int block) {
@@ -43,7 +44,7 @@ __device__ __forceinline__ void tma_prefetch_5d(const CUtensorMap* m, int token,
 
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// Sequence, length and context of a row; seq -1: nothing to do (tell: and the reason is reported).
+// tell: the reason why a row is left out is reported.
 __device__ __forceinline__ RowCheck known_row(const PagedAttnArgs& a, const ContTable& ct, long long row, bool tell, DeviceStatus* st) {
   RowCheck r = {a.row_seq[row], a.row_len[row], 0};
   if (r.seq == -1) return r;

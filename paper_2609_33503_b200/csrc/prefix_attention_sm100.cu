@@ -11,8 +11,12 @@
 //   P and O are single: a group hands its P over when O of the tile before is complete, which is also when O may be rescaled (every barrier
 //   belongs to the even or to the odd tiles, so that nobody who waits for one phase can be two behind);
 //   the running maximum of a row goes from group to group through shared memory (known a third into a group's step); sums stay with the groups.
-// (Each group with an output of its own, S and P in one place, Q in shared memory: 1780 clk per tile.)
-// The pieces' results are merged with those of the rows' own tokens by their log-sum-exps.  Every wait is bounded.
+// Measured: 1700 clk per tile.  (Each group with an output of its own, S and P in one place, Q in shared memory: 1780.)  64 rows of 40 / 8 heads over
+// 32 K, three row tiles: 50 us of the 21 that the keys take and the 30 of the products.  16 rows of 32 / 8 heads over 16 K, where a block has eight
+// tiles and its start and end count: 14 us of 10.
+// A row's pieces are merged with its own tokens by their log-sum-exps: by the clusters of the kernel over those (paged_attention.cu), or by a kernel
+// behind it.  That kernel begins when every block here has passed its wait, and reads what this one writes only after its own: 83.8 -> 80.6 and
+// 31.0 -> 29.5 us for whole calls of those two sizes.  Every wait is bounded.
 #include "continuation_splits.cuh"
 #include "paged_attention.cuh"
 #include "sm100_ptx.cuh"
@@ -120,8 +124,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  griddep_launch();                                     // (the block holds its tensor memory)
   griddep_wait();
+  griddep_launch();                                     // (behind the wait: the next kernel relies on what is in front of this one being complete)
   const int status = *reinterpret_cast<volatile int*>(&st->status);
   const long long row0 = a.row_cu[ct.seq_cu[b]], row1 = a.row_cu[ct.seq_cu[b + 1]];
   const long long first = row0 + (long long)rt * rows_per_tile;
@@ -428,13 +432,14 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   const int D = shape->head_dim, rows_per_tile = kPreTile / (a.H / a.Hkv), slots = cont_slots(a.n_rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // ---- few rows and short contexts: one launch, each row by itself ----
-  // One cluster per (row, KV head), all at once and eight tiles to a block at most: the launches are what such a call takes (four rows of 4 / 1
-  // heads over 1 K, three launches 12.8 us).
+  // One cluster per (row, KV head), all at once and twelve tiles to a block at most: the launches are what such a call takes.  One and four rows of 32 / 8
+  // heads over 3 K tokens 10.7 and 11.8 us (14.2 and 14.7 the other way), 6 K 14.2 and 16.6 (15.5 and 19.5), 10 K 19.5 and 23.0 (18.8 and 21.3); eight
+  // rows over 3 K, not all at once, 22.8 (18.7).
   int longest = 0;
   for (int b = 0; b < ct.n_req; ++b)
     if (ct.max_rows[b] > 0) longest = std::max(longest, ct.ctx_len[b]);
   const long long all_tiles = ((long long)longest + 63) / 64 + (a.max_len + 63) / 64;
-  if (a.n_rows * a.Hkv * kPagCluster <= 2LL * sms && all_tiles <= 8 * kPagCluster) {
+  if (a.n_rows * a.Hkv * kPagCluster <= 2LL * sms && all_tiles <= 12 * kPagCluster) {
     a.ctx_keys = longest > 0 ? CTX_KEYS_ALL : CTX_KEYS_NONE;
     a.ctx_block = 64;
     a.n_splits = (int)std::max<long long>(1, std::min<long long>(kPagCluster, all_tiles / 2));
@@ -481,6 +486,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
     rc = D == 128 ? launch_prefix<128>(cache, ct, a, rows_per_tile, s) : launch_prefix<64>(cache, ct, a, rows_per_tile, s);
     if (rc != RELAXKV_OK) return rc;
   }
+  a.behind_prefix = most > 0;
   if (own && (rc = launch_paged_attention(shape, cache, store, ct, a, s)) != RELAXKV_OK) return rc;
   return a.n_slots == 1 || a.cluster ? RELAXKV_OK : launch_continuation_merge(ct, a, D, s);
 }

@@ -132,7 +132,8 @@ def randn(shape, seed):
 
 
 @pytest.mark.parametrize("n,H,Hkv,D,bs,layout,norm", [(1, 4, 1, 64, 16, "token", False), (3, 5, 5, 128, 32, "gaps", True), (64, 32, 8, 128, 16, "token", False),
-                                                      (77, 40, 8, 128, 64, "head", True), (1500, 8, 2, 64, 128, "head", True), (1027, 6, 3, 128, 16, "gaps", False)])
+                                                      (77, 40, 8, 128, 64, "head", True), (1500, 8, 2, 64, 128, "head", True), (1027, 6, 3, 128, 16, "gaps", False),
+                                                      (1203, 5, 5, 128, 32, "token", True), (9, 2, 1, 128, 16, "gaps", True), (1185, 1, 1, 64, 64, "head", False)])
 def test_norm_rope_append(n, H, Hkv, D, bs, layout, norm):
     nb = -(-n // bs) + 2
     q, k, v = randn((n, H, D), 1), randn((n, Hkv, D), 2), randn((n, Hkv, D), 3)
