@@ -4,15 +4,17 @@
 // Bounds: one pass over K, bound by its bytes.  A warp has one (block, KV head): 16 lanes hold the 128 dims of a token as 16-byte pieces, so
 // a load takes two tokens (four of 64 dims); maxima and minima stay packed bf16 pairs and are exact.  The scale is a power of two, so are the
 // quotients, and the rounding is away from the block: the bounds remain bounds.
-// Scores: sum_d max(q_d hi_d, q_d lo_d) = q+ . hi + q- . lo, a product over 2 D bytes on the tensor cores (m16n8k32, s8): rows are the heads of two
-// rows of the step (of one with more than eight heads to a KV head), columns eight blocks.  The product's terms may come in any order as long as both
-// sides agree, so a lane takes D / 2 bytes of its block in 16-byte loads and the queries are laid out to match.  Sums are whole numbers below 2^24:
-// the scores, and with them the lists, do not depend on the order of anything.
-// Selection: one block per (row, KV head); counts of digits find the lowest selected score, then every thread writes its own range's blocks in
-// order.  Both launches: 4 rows of 40 / 8 heads, 512 blocks 10.3 us, 16 rows of 32 / 8 heads in two contexts of 2048 blocks 22.8: latencies
-// (row -> query -> product -> score -> counts), not bytes.
+// Scores: sum_d max(q_d hi_d, q_d lo_d) = q+ . hi + q- . lo, a product over 2 D whole numbers of 8 bits, as halves on the tensor cores with sums in
+// 32 bits: rows are the heads of one, two or four rows of the step, columns eight blocks.  All are whole numbers below 2^24, so the scores, and with them
+// the lists, do not depend on the order of anything; it may be any as long as both sides agree, so a lane takes D / 2 bytes of its block in
+// 16-byte loads and the queries are laid out to match.  Up to four tiles of rows go to a block, so that rows and context blocks both spread
+// over the SMs: with all rows in one block, 64 rows of 40 / 8 heads over 938 blocks took 33 us, so 27.
+// Selection: one block per (row, KV head); counts of digits find the lowest selected score, then every warp writes its own range's blocks in
+// order.  Both launches: 4 rows of 40 / 8 heads, 512 blocks 8.3 us, 16 rows of 32 / 8 heads in two contexts of some 2000 blocks 14.1: latencies
+// (row -> query -> product -> score -> counts), not bytes; 64 rows in one context of 8192 blocks 89.
 #include "continuations.cuh"
 #include <algorithm>
+#include <cuda_fp16.h>
 
 namespace relaxkv {
 
@@ -36,13 +38,13 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 
 constexpr int kBndThreads = 256;
 
-// U: loads of a lane that travel together.  131 K tokens of 8 heads of 128 dims (268 MB) 46.4 us = 5.8 TB/s, 16 K (33.5 MB) 12.0; with sixteen loads
-// 48.6 and 10.9, with thirty-two 85.2 and 12.9.
-template <int D>
+// U: loads of a lane that travel together, 16 where a block has as many.  Blocks of 64 tokens, 8 heads of 128 dims: 16 K tokens (33.5 MB) 7.2 us,
+// 131 K (268 MB) 43.6 = 6.2 TB/s, with eight loads 9.7 and 44.4; blocks of 16 tokens, 16 K: 8.8 with eight, 11.7 with sixteen, half of them empty.
+template <int D, int U>
 __global__ void __launch_bounds__(kBndThreads)
 block_bounds_kernel(const uint16_t* k, long long token_stride, long long head_stride, const __grid_constant__ ContTable ct, int block_size, int Hkv,
                     int8_t* bounds, float* scale, int heads_outer) {
-  constexpr int kLanes = D / 8, kTok = 32 / kLanes, U = 8;
+  constexpr int kLanes = D / 8, kTok = 32 / kLanes;
   const int lane = threadIdx.x & 31, gl = lane % kLanes, sub = lane / kLanes;
   const long long w = (long long)blockIdx.x * (kBndThreads / 32) + (threadIdx.x >> 5);
   const int n_blocks = ct.blk_cu[ct.n_req];
@@ -117,9 +119,17 @@ block_bounds_kernel(const uint16_t* k, long long token_stride, long long head_st
 
 // ---- scores ---------------------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ void mma_s8_16832(int* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+__device__ __forceinline__ void mma_f16_16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+// Four whole numbers of 8 bits as halves: with 128 added, a byte behind 0x64 is the half 1024 + byte.
+__device__ __forceinline__ void halves_of(uint32_t bytes, uint32_t* h) {
+  const uint32_t u = bytes ^ 0x80808080u, lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+  const __half2 off = __float2half2_rn(1152.f);
+  h[0] = h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&lo), off));
+  h[1] = h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&hi), off));
 }
 
 struct SelectArgs {
@@ -142,135 +152,143 @@ __device__ __forceinline__ RowRange rows_of(const SelectArgs& a, const ContTable
 }
 
 constexpr int kScoWarps = 4;
-constexpr int kScoPass = 8;             // row tiles whose queries a block holds at once
+constexpr int kScoCols = 2;             // times eight context blocks of a warp
+constexpr int kScoPass = 4;             // row tiles of a block
 
-// A block: eight context blocks per warp, one KV head, all rows of the context.  PAIR: two rows of the step to an MMA (groups of up to eight heads).
-template <int D, bool PAIR>
+// A block: sixteen context blocks per warp, one KV head, up to kScoPass tiles of the context's rows.  ROWS: rows of the step to an MMA, 16 / ROWS heads of each.
+template <int D, int ROWS>
 __global__ void __launch_bounds__(kScoWarps * 32)
 block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
-  constexpr int kSteps = 2 * D / 32;                                // MMAs of a product
-  constexpr int kRowsPer = PAIR ? 2 : 1;                            // rows of the step per tile
-  __shared__ __align__(16) uint32_t q_s[kScoPass][16][2 * D / 4 + 4];      // [tile][fragment row][q+ | q-]; the rows 16 bytes apart from whole banks
+  constexpr int kSteps = 2 * D / 16;                                // MMAs of a product
+  constexpr int kHeads = 16 / ROWS;                                 // fragment rows of a row of the step
+  __shared__ __align__(16) uint32_t q_s[kScoPass][16][D + 8];       // [tile][fragment row][step][lane of four] four halves of (q+ | q-)
   __shared__ float sq_s[kScoPass][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const int G = a.H / a.Hkv;
   const int hd = blockIdx.y;
   int b = 0;
   for (int hi = ct.n_req; hi - b > 1;) { const int mid = (b + hi) >> 1; if (ct.tile_cu[mid] <= (int)blockIdx.x) b = mid; else hi = mid; }
-  const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b], x0 = (((int)blockIdx.x - ct.tile_cu[b]) * kScoWarps + warp) * 8;
+  const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b], across = (nb + 8 * kScoCols * kScoWarps - 1) / (8 * kScoCols * kScoWarps);
+  const int p0 = ((int)blockIdx.x - ct.tile_cu[b]) / across * kScoPass;
+  const int x0 = (((int)blockIdx.x - ct.tile_cu[b]) % across * kScoWarps + warp) * (8 * kScoCols);
   griddep_launch();
   griddep_wait();
-  // this lane's share of its block's 2 D bytes: bytes [tig D / 2, + D / 2)
-  const int x = x0 + gid;
-  uint32_t bd[D / 8];
-  {
-    const uint4* p = reinterpret_cast<const uint4*>(a.bounds + ((long long)(ct.blk_cu[b] + min(x, nb - 1)) * a.Hkv + hd) * (2 * D) + tig * (D / 2));
+  // this lane's share of its blocks' 2 D bytes: bytes [tig D / 2, + D / 2) of block x0 + gid (and of the eight behind)
+  uint4 bytes[kScoCols][D / 32];
+  float sb[kScoCols][2];                                             // scales of the blocks of this lane's result columns
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      const uint4 v = p[i];
-      bd[4 * i] = v.x; bd[4 * i + 1] = v.y; bd[4 * i + 2] = v.z; bd[4 * i + 3] = v.w;
-    }
+  for (int c = 0; c < kScoCols; ++c) {
+    const uint4* p = reinterpret_cast<const uint4*>(a.bounds + ((long long)(ct.blk_cu[b] + min(x0 + 8 * c + gid, nb - 1)) * a.Hkv + hd) * (2 * D) + tig * (D / 2));
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) bytes[c][i] = p[i];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) sb[c][e] = a.scale[(long long)(ct.blk_cu[b] + min(x0 + 8 * c + 2 * tig + e, nb - 1)) * a.Hkv + hd];
   }
-  float sb[2];                                                       // scales of the blocks of this lane's result columns
-#pragma unroll
-  for (int e = 0; e < 2; ++e) sb[e] = a.scale[(long long)(ct.blk_cu[b] + min(x0 + 2 * tig + e, nb - 1)) * a.Hkv + hd];
   // (the bounds are on their way)
   const RowRange rr = rows_of(a, ct, b);
-  if (rr.n < 0 && threadIdx.x == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, b, ct.max_rows[b]);
-  if (rr.n <= 0) return;
-  const int n_tiles = (rr.n + kRowsPer - 1) / kRowsPer;
-  for (int p0 = 0; p0 < n_tiles; p0 += kScoPass) {
-    const int here = min(kScoPass, n_tiles - p0);
-    __syncthreads();
-    // queries in 8 bits: eight lanes per fragment row, D / 8 dims each, the loads of four steps side by side
-    constexpr int kVec = D / 64, kStep = 4 * kScoWarps, kBatch = 4;
-    const int ql = lane & 7, sub = lane >> 3;
-    for (int i0 = warp * 4 + sub; i0 < here * 16; i0 += kStep * kBatch) {
-      uint4 raw[kBatch][kVec];
-      bool live[kBatch];
+  if (rr.n < 0 && threadIdx.x == 0 && hd == 0 && p0 == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, b, ct.max_rows[b]);
+  const int here = min(kScoPass, (rr.n + ROWS - 1) / ROWS - p0);
+  if (rr.n < 0 || here <= 0) return;
+  // queries in 8 bits: eight lanes per fragment row, D / 8 dims each, all loads side by side
+  constexpr int kVec = D / 64, kStep = 4 * kScoWarps, kBatch = 16 * kScoPass / kStep;
+  const int ql = lane & 7, sub = lane >> 3;
+  uint4 raw[kBatch][kVec];
+  bool live[kBatch];
 #pragma unroll
-      for (int c = 0; c < kBatch; ++c) {
-        const int i = i0 + c * kStep, tile = i >> 4, fr = i & 15, r = (p0 + tile) * kRowsPer + (PAIR ? fr >> 3 : 0), h = PAIR ? fr & 7 : fr;
-        live[c] = i < here * 16 && h < G && r < rr.n;
-        const uint4* p = reinterpret_cast<const uint4*>(a.q + ((rr.first + r) * a.H + hd * G + h) * D + ql * (D / 8));
+  for (int c = 0; c < kBatch; ++c) {
+    const int i = warp * 4 + sub + c * kStep, tile = i >> 4, fr = i & 15, r = (p0 + tile) * ROWS + fr / kHeads, h = fr % kHeads;
+    live[c] = i < here * 16 && h < G && r < rr.n;
+    const uint4* p = reinterpret_cast<const uint4*>(a.q + ((rr.first + r) * a.H + hd * G + h) * D + ql * (D / 8));
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) raw[c][e] = live[c] ? p[e] : make_uint4(0u, 0u, 0u, 0u);
+    for (int e = 0; e < kVec; ++e) raw[c][e] = live[c] ? p[e] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  uint32_t bd[kScoCols][D / 4];
+#pragma unroll
+  for (int c = 0; c < kScoCols; ++c) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      halves_of(bytes[c][i].x, &bd[c][8 * i]);
+      halves_of(bytes[c][i].y, &bd[c][8 * i + 2]);
+      halves_of(bytes[c][i].z, &bd[c][8 * i + 4]);
+      halves_of(bytes[c][i].w, &bd[c][8 * i + 6]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kBatch; ++c) {
+    const int i = warp * 4 + sub + c * kStep, tile = i >> 4, fr = i & 15;
+    if (i >= here * 16) break;                        // (the same for a warp's lanes)
+    if (ql == 0 && !live[c]) sq_s[tile][fr] = -1.f;   // no such row or head: its scores are passed over, whatever they are
+    if (!__any_sync(0xffffffffu, live[c])) continue;
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(raw[c]);
+    uint32_t top = w[0] & 0x7fff7fffu;
+#pragma unroll
+    for (int e = 1; e < 4 * kVec; ++e) top = bmax2(top, w[e] & 0x7fff7fffu);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) top = bmax2(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // the larger half; NaN is left only where there is nothing else
+    const uint32_t t0 = top & 0xffffu, t1 = top >> 16, amax = max(t0 > 0x7f80u ? 0u : t0, t1 > 0x7f80u ? 0u : t1);
+    const int ex = scale_exponent(min(amax, 0x7f7fu));
+    const float inv = power_of_two(-ex);
+    // to the nearest whole number, ties to the even one; NaN is neither above nor below zero
+    uint2* row = reinterpret_cast<uint2*>(q_s[tile][fr]);
+    constexpr float kWhole = 12582912.f;
+    const __half2 zero = __float2half2_rn(0.f), most = __float2half2_rn(127.f), least = __float2half2_rn(-127.f);
+#pragma unroll
+    for (int e = 0; e < 2 * kVec; ++e) {
+      uint32_t pos[2], neg[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t bits = w[2 * e + u];
+        const __half2 v = __floats2half2_rn((__uint_as_float(bits << 16) * inv + kWhole) - kWhole, (__uint_as_float(bits & 0xffff0000u) * inv + kWhole) - kWhole);
+        pos[u] = h2_bits(__hmin2(__hmax2(v, zero), most));
+        neg[u] = h2_bits(__hmax2(__hmin2(v, zero), least));
       }
+      const int at = ((ql & 3) * 2 * kVec + e) * 4 + (ql >> 2);            // [step][lane of the four]
+      row[at] = make_uint2(pos[0], pos[1]);
+      row[at + 2] = make_uint2(neg[0], neg[1]);
+    }
+    if (ql == 0 && live[c]) sq_s[tile][fr] = power_of_two(ex);
+  }
+  __syncthreads();
+  if (x0 >= nb) return;
+  for (int tile = 0; tile < here; ++tile) {
+    // (sums of an even and an odd half of the steps, so that they need not wait for each other)
+    float acc[kScoCols][2][4];
 #pragma unroll
-      for (int c = 0; c < kBatch; ++c) {
-        const int i = i0 + c * kStep, tile = i >> 4, fr = i & 15;
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(raw[c]);
-        uint32_t amax = 0;
+    for (int c = 0; c < kScoCols; ++c) {
 #pragma unroll
-        for (int e = 0; e < 4 * kVec; ++e) {
+      for (int e = 0; e < 4; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
+    }
 #pragma unroll
-          for (int hf = 0; hf < 32; hf += 16) {
-            const uint32_t m = (w[e] >> hf) & 0x7fffu;
-            amax = max(amax, m <= 0x7f80u ? m : 0u);
-          }
-        }
+    for (int s = 0; s < kSteps; ++s) {
+      const uint2 qa = *reinterpret_cast<const uint2*>(&q_s[tile][gid][8 * s + 2 * tig]);
+      const uint2 qb = *reinterpret_cast<const uint2*>(&q_s[tile][gid + 8][8 * s + 2 * tig]);
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const int ex = scale_exponent(min(amax, 0x7f7fu));
-        const float inv = power_of_two(-ex);
-        uint32_t pos[2 * kVec], neg[2 * kVec];
+      for (int c = 0; c < kScoCols; ++c) mma_f16_16816(acc[c][s & 1], qa.x, qb.x, qa.y, qb.y, bd[c][2 * s], bd[c][2 * s + 1]);
+    }
+    // the largest over the heads of a row: fragment rows lie 4 lanes apart
+    float best[2][2 * kScoCols];
+    const float s0 = sq_s[tile][gid], s1 = sq_s[tile][gid + 8];
 #pragma unroll
-        for (int e = 0; e < 2 * kVec; ++e) {
-          pos[e] = neg[e] = 0u;
+    for (int e = 0; e < 2 * kScoCols; ++e) {
+      const float *even = acc[e >> 1][0], *odd = acc[e >> 1][1];
+      best[0][e] = s0 > 0.f ? (even[e & 1] + odd[e & 1]) * s0 : -INFINITY;
+      best[1][e] = s1 > 0.f ? (even[2 + (e & 1)] + odd[2 + (e & 1)]) * s1 : -INFINITY;
+      if (ROWS == 1) best[0][e] = fmaxf(best[0][e], best[1][e]);
 #pragma unroll
-          for (int b4 = 0; b4 < 4; ++b4) {
-            const uint32_t bits = (w[2 * e + (b4 >> 1)] >> ((b4 & 1) * 16)) & 0xffffu;
-            const float f = (bits & 0x7fffu) > 0x7f80u ? 0.f : rintf(bf16_bits_to_float((uint16_t)bits) * inv);
-            pos[e] |= (uint32_t)(int)fminf(fmaxf(f, 0.f), 127.f) << (b4 * 8);
-            neg[e] |= ((uint32_t)(int)fmaxf(fminf(f, 0.f), -127.f) & 0xffu) << (b4 * 8);
-          }
-        }
-        if (i < here * 16) {
-          uint32_t* row = q_s[tile][fr];
-#pragma unroll
-          for (int e = 0; e < 2 * kVec; ++e) {
-            row[ql * 2 * kVec + e] = pos[e];
-            row[D / 4 + ql * 2 * kVec + e] = neg[e];
-          }
-          if (ql == 0) sq_s[tile][fr] = live[c] ? power_of_two(ex) : -1.f;      // no such row or head
-        }
+      for (int o = 4; o < 4 * min(kHeads, 8); o <<= 1) {
+        best[0][e] = fmaxf(best[0][e], __shfl_xor_sync(0xffffffffu, best[0][e], o));
+        if (ROWS > 1) best[1][e] = fmaxf(best[1][e], __shfl_xor_sync(0xffffffffu, best[1][e], o));
       }
     }
-    __syncthreads();
-    if (x0 >= nb) continue;
-    for (int tile = 0; tile < here; ++tile) {
-      int acc[4] = {0, 0, 0, 0};
+    // of the fragment rows that hold a row's result, one writes it: gid from the first half, gid + 1 from the second
+    const int half = gid % min(kHeads, 8), r = (p0 + tile) * ROWS + (ROWS == 4 ? 2 * half + (gid >> 2) : half);
+    if (half < min(ROWS, 2) && r < rr.n) {
+      float* o = a.scores + ((rr.first + r) * a.Hkv + hd) * a.most;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const uint2 qa = *reinterpret_cast<const uint2*>(&q_s[tile][gid][tig * (D / 8) + 2 * s]);
-        const uint2 qb = *reinterpret_cast<const uint2*>(&q_s[tile][gid + 8][tig * (D / 8) + 2 * s]);
-        const uint32_t fa[4] = {qa.x, qb.x, qa.y, qb.y};
-        mma_s8_16832(acc, fa, bd[2 * s], bd[2 * s + 1]);
-      }
-      // the largest over the heads of a row: fragment rows lie 4 lanes apart
-      float best[2][2];
-      const float s0 = sq_s[tile][gid], s1 = sq_s[tile][gid + 8];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        best[0][e] = s0 > 0.f ? (float)acc[e] * s0 : -INFINITY;
-        best[1][e] = s1 > 0.f ? (float)acc[2 + e] * s1 : -INFINITY;
-        if (!PAIR) best[0][e] = fmaxf(best[0][e], best[1][e]);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          best[0][e] = fmaxf(best[0][e], __shfl_xor_sync(0xffffffffu, best[0][e], o));
-          if (PAIR) best[1][e] = fmaxf(best[1][e], __shfl_xor_sync(0xffffffffu, best[1][e], o));
-        }
-      }
-      if (gid < kRowsPer) {
-        const int r = (p0 + tile) * kRowsPer + gid;
-        if (r < rr.n) {
-          float* o = a.scores + ((rr.first + r) * a.Hkv + hd) * a.most;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int xx = x0 + 2 * tig + e;
-            if (xx < nb) o[xx] = best[gid][e] * sb[e] + 0.f;                     // (+ 0: one zero, not two)
-          }
-        }
+      for (int e = 0; e < 2 * kScoCols; ++e) {
+        const int xx = x0 + 8 * (e >> 1) + 2 * tig + (e & 1);
+        if (xx < nb) o[xx] = (half ? best[1][e] : best[0][e]) * sb[e >> 1][e & 1] + 0.f;   // (+ 0: one zero, not two)
       }
     }
   }
@@ -278,9 +296,7 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
 
 // ---- the n_select highest scores of a (row, KV head) ------------------------------------------------------------------------------
 
-constexpr int kTopThreads = 256;
 constexpr int kTopKept = 8192;          // scores that a block keeps in shared memory; more are read again by every pass
-constexpr int kTopBits = 10;
 
 // Order-preserving key of a score (no NaN: scores are products of whole numbers and powers of two).
 __device__ __forceinline__ uint32_t score_key(float f) {
@@ -288,14 +304,16 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// The first and last blocks are taken in any case; of the others the `want` highest.  Their keys' common leading bits are skipped, then digits of ten
-// bits are counted from the highest on until the digit that the want-th key falls into holds no more keys than are wanted: with spread scores
-// two counts.  A launch of few rows is a chain of latencies and barriers.
-__global__ void __launch_bounds__(kTopThreads)
+// The first and last blocks are taken in any case; of the others the `want` highest.  Their keys' common leading bits are skipped, then digits are
+// counted from the highest on, a digit's value per thread, until the one that the want-th key falls into holds no more keys than are wanted: with
+// spread scores two counts.  A launch of few rows is a chain of latencies and barriers.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
-  constexpr int kBins = 1 << kTopBits, kBinsPer = kBins / kTopThreads, kWarps = kTopThreads / 32, U = 8;
+  constexpr int kBits = THREADS > 256 ? 9 : 8, kWarps = THREADS / 32, U = 8;
   extern __shared__ uint32_t key_s[];
-  __shared__ int hist[kBins];
+  static_assert(THREADS == 1 << kBits, "a bin per thread");
+  __shared__ int hist[THREADS];
   __shared__ int warp_sum[kWarps], found[2];
   __shared__ uint2 warp_range[kWarps];
   __shared__ int2 warp_pair[kWarps];
@@ -318,19 +336,19 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   const bool mine = rr.n >= 0 && row >= rr.first && row < rr.first + rr.n;
   if (!mine && tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_SELECT_BLOCKS, (int)row, b);
   if (nb <= a.n_select) {                                                        // all of them
-    for (int i = tid; mine && i < a.n_select; i += kTopThreads) out[i] = i < nb ? i : -1;
+    for (int i = tid; mine && i < a.n_select; i += THREADS) out[i] = i < nb ? i : -1;
     return;
   }
   const int x0 = a.n_first, x1 = nb - a.n_last;                                  // blocks that compete: [x0, x1), more than are wanted
   const bool kept = nb <= kTopKept;
   uint32_t lo = 0xffffffffu, hi = 0u;
-  for (int i0 = x0 + tid; i0 < x1; i0 += U * kTopThreads) {
+  for (int i0 = x0 + tid; i0 < x1; i0 += U * THREADS) {
     float v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = i0 + u * kTopThreads < x1 ? score[i0 + u * kTopThreads] : 0.f;
+    for (int u = 0; u < U; ++u) v[u] = i0 + u * THREADS < x1 ? score[i0 + u * THREADS] : 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kTopThreads;
+      const int i = i0 + u * THREADS;
       if (i < x1) {
         const uint32_t k = score_key(v[u]);
         if (kept) key_s[i] = k;
@@ -342,7 +360,7 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   if (lane == 0) warp_range[warp] = make_uint2(lo, hi);
-  for (int i = tid; i < kBins; i += kTopThreads) hist[i] = 0;
+  hist[tid] = 0;
   if (!mine) return;                                                             // (the whole block)
   __syncthreads();
 #pragma unroll
@@ -354,37 +372,25 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   bool all_in = false;                                                           // every key from base on is taken: no ties to break
   if (want == 0) { base = 0xffffffffu; all_in = true; left = 0; }
   while (left > 0) {
-    const int shift = max(0, left - kTopBits);
-    for (int i = x0 + tid; i < x1; i += kTopThreads) {
+    const int shift = max(0, left - kBits);
+    for (int i = x0 + tid; i < x1; i += THREADS) {
       const uint32_t d = key_of(i) - base;
       if (left >= 32 || (d >> left) == 0) atomicAdd(&hist[d >> shift], 1);       // (keys below base wrap round and fall out)
     }
     __syncthreads();
-    // bins from the highest: thread t has bins (top - kBinsPer (t + 1), top - kBinsPer t]
-    int cnt[kBinsPer], mine_n = 0;
-#pragma unroll
-    for (int e = 0; e < kBinsPer; ++e) {
-      const int bin = kBins - 1 - tid * kBinsPer - e;
-      cnt[e] = hist[bin];
-      hist[bin] = 0;
-      mine_n += cnt[e];
-    }
-    int incl = mine_n;
+    // thread t has bin THREADS - 1 - t: the sums run from the highest on
+    const int bin = THREADS - 1 - tid, n = hist[bin];
+    hist[bin] = 0;
+    int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    int before = incl - mine_n;
+    int before = incl - n;
     for (int w = 0; w < warp; ++w) before += warp_sum[w];
-    if (before < want && before + mine_n >= want) {                              // exactly one thread
-#pragma unroll
-      for (int e = 0; e < kBinsPer; ++e) {
-        if (before < want && before + cnt[e] >= want) {
-          found[0] = (kBins - 1 - tid * kBinsPer - e) | (before + cnt[e] == want ? 1 << 30 : 0);
-          found[1] = want - before;
-        }
-        before += cnt[e];
-      }
+    if (before < want && before + n >= want) {                                   // exactly one thread
+      found[0] = bin | (before + n == want ? 1 << 30 : 0);
+      found[1] = want - before;
     }
     __syncthreads();
     base += (uint32_t)(found[0] & ((1 << 30) - 1)) << shift;
@@ -393,30 +399,34 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
     if (found[0] >> 30) { all_in = true; break; }
     __syncthreads();
   }
-  // ---- keys above, and of those equal to base the first `want`: every thread a range in order ----
-  const int per = (nb + kTopThreads - 1) / kTopThreads, i0 = min(nb, tid * per), i1 = min(nb, i0 + per);
+  // ---- keys above, and of those equal to base the first `want`: every warp a range in order, 32 keys at a time ----
+  const int per = (nb + 32 * kWarps - 1) / (32 * kWarps) * 32, i0 = min(nb, warp * per), i1 = min(nb, i0 + per);
   auto kind = [&](int i) -> int {                                                // 2: taken, 1: equal to the last one, 0: left
+    if (i >= i1) return 0;
     if (i < x0 || i >= x1) return 2;
     const uint32_t k = key_of(i);
     return all_in ? (k >= base ? 2 : 0) : k > base ? 2 : k == base ? 1 : 0;
   };
   int above = 0, equal = 0;
-  for (int i = i0; i < i1; ++i) { const int k = kind(i); above += k == 2; equal += k == 1; }
-  int ia = above, ie = equal;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int va = __shfl_up_sync(0xffffffffu, ia, o), ve = __shfl_up_sync(0xffffffffu, ie, o);
-    if (lane >= o) { ia += va; ie += ve; }
+  for (int i = i0; i < i1; i += 32) {
+    const int k = kind(i + lane);
+    above += __popc(__ballot_sync(0xffffffffu, k == 2));
+    equal += __popc(__ballot_sync(0xffffffffu, k == 1));
   }
-  if (lane == 31) warp_pair[warp] = make_int2(ia, ie);
+  if (lane == 0) warp_pair[warp] = make_int2(above, equal);
   __syncthreads();
-  ia -= above; ie -= equal;
+  int ia = 0, ie = 0;
   for (int w = 0; w < warp; ++w) { ia += warp_pair[w].x; ie += warp_pair[w].y; }
   if (all_in) want = 0;
   int at = ia + min(ie, want);
-  for (int i = i0; i < i1; ++i) {
-    const int k = kind(i);
-    if (k == 2 || (k == 1 && ie++ < want)) out[at++] = i;
+  const uint32_t lower = (1u << lane) - 1u;
+  for (int i = i0; i < i1; i += 32) {
+    const int k = kind(i + lane);
+    const uint32_t ties = __ballot_sync(0xffffffffu, k == 1);
+    const uint32_t taken = __ballot_sync(0xffffffffu, k == 2 || (k == 1 && ie + __popc(ties & lower) < want));
+    if ((taken >> lane) & 1u) out[at + __popc(taken & lower)] = i + lane;
+    at += __popc(taken);
+    ie += __popc(ties);
   }
 }
 
@@ -440,7 +450,9 @@ extern "C" relaxkv_status relaxkv_block_bounds(const relaxkv_shape* shape, const
   ContTable ct;
   fill_contexts(ct, shape, cache, block_size);
   const unsigned grid = (unsigned)((blocks * Hkv + kBndThreads / 32 - 1) / (kBndThreads / 32));
-  auto kern = D == 128 ? block_bounds_kernel<128> : block_bounds_kernel<64>;
+  const bool wide = block_size >= 16 * (256 / D);      // sixteen loads are no more than a block has
+  auto kern = D == 128 ? (wide ? block_bounds_kernel<128, 16> : block_bounds_kernel<128, 8>)
+                       : (wide ? block_bounds_kernel<64, 16> : block_bounds_kernel<64, 8>);
   return cuda_ok(launch_chained(kern, dim3(grid), kBndThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const uint16_t*>(cache->k),
                                 (long long)cache->token_stride, (long long)cache->head_stride, ct, block_size, Hkv, bounds_out, scale_out,
                                 cache->head_stride > cache->token_stride ? 1 : 0));
@@ -473,22 +485,28 @@ extern "C" relaxkv_status relaxkv_select_blocks(
   a.scores = static_cast<float*>(workspace); a.out = blocks_out; a.n_rows = rows->n_rows;
   a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.n_seq = rows->n_seq; a.block_size = block_size;
   a.n_select = n_select; a.n_first = n_first; a.n_last = n_last;
+  const int G = a.H / a.Hkv, rows_per = (G <= 4 ? 4 : G <= 8 ? 2 : 1) * kScoPass;
+  long long tiles = 0;
   for (int b = 0; b < ct.n_req; ++b) {
     const int nb = ct.blk_cu[b + 1] - ct.blk_cu[b];
     a.most = std::max(a.most, nb);
     // contexts of no more blocks than are selected need no scores
-    ct.tile_cu[b + 1] = ct.tile_cu[b] + (nb > n_select && ct.max_rows[b] > 0 ? (nb + 8 * kScoWarps - 1) / (8 * kScoWarps) : 0);
+    const long long across = (nb + 8 * kScoCols * kScoWarps - 1) / (8 * kScoCols * kScoWarps);
+    tiles += nb > n_select ? across * ((ct.max_rows[b] + rows_per - 1) / rows_per) : 0;
+    if (tiles > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+    ct.tile_cu[b + 1] = (int)tiles;
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int D = shape->head_dim;
   if (a.Hkv > 65535) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (ct.tile_cu[ct.n_req] > 0) {
-    const bool pair = a.H / a.Hkv <= 8;
-    auto kern = D == 128 ? (pair ? block_score_kernel<128, true> : block_score_kernel<128, false>)
-                         : (pair ? block_score_kernel<64, true> : block_score_kernel<64, false>);
+    auto kern = D == 128 ? (G <= 4 ? block_score_kernel<128, 4> : G <= 8 ? block_score_kernel<128, 2> : block_score_kernel<128, 1>)
+                         : (G <= 4 ? block_score_kernel<64, 4> : G <= 8 ? block_score_kernel<64, 2> : block_score_kernel<64, 1>);
     rc = cuda_ok(launch_chained(kern, dim3((unsigned)ct.tile_cu[ct.n_req], (unsigned)a.Hkv), kScoWarps * 32, 0, s, ct, a, st));
     if (rc != RELAXKV_OK) return rc;
   }
   const size_t smem = a.most <= kTopKept ? (size_t)a.most * 4 : 0;
-  return cuda_ok(launch_chained(block_topk_kernel, dim3((unsigned)(a.n_rows * a.Hkv)), kTopThreads, smem, s, ct, a, st));
+  const bool many = a.most > 1024;
+  auto kern = many ? block_topk_kernel<512> : block_topk_kernel<256>;
+  return cuda_ok(launch_chained(kern, dim3((unsigned)(a.n_rows * a.Hkv)), many ? 512 : 256, smem, s, ct, a, st));
 }

@@ -573,6 +573,40 @@ def test_selection_device_refusals(what):
     assert (lists[skip] == -9).all() and torch.equal(lists[keep], good[keep])
 
 
+@pytest.mark.parametrize("H,Hkv,D,rows", [(4, 2, 128, [37, 3]), (6, 2, 64, [16, 17]), (10, 2, 128, [8, 19]), (8, 1, 64, [9, 7]), (24, 2, 128, [9, 4]),
+                                          (16, 1, 64, [5, 8]), (3, 3, 128, [33, 1])])
+def test_selection_for_many_rows(H, Hkv, D, rows):
+    """More rows in a context than a block of the launch takes at once, for every way that rows and heads share a product."""
+    b = B()
+    s = Step(H, Hkv, D, [2100, 1040], rows, 3, 1, 16, seed=19)
+    bounds, scale = get_bounds(s, 16)
+    n = sum(rows)
+    lists = torch.full((n, Hkv, 9), -9, dtype=torch.int32, device="cuda")
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, 1, 2, lists, s.ws(16))
+    assert status() == b.OK
+    bi, sc, q, first = bounds.cpu().numpy().astype(np.int64), f64(scale), f64(s.q), [0, 132, 197]
+    for r in range(n):
+        c = 0 if r < rows[0] else 1
+        assert np.array_equal(lists[r].cpu().numpy(), orc.select(q[r], bi[first[c]:first[c + 1]], sc[first[c]:first[c + 1]], 9, 1, 2)), r
+
+
+def test_scores_are_exact_up_to_their_largest_value():
+    """Sums of 128 products of 127 x 127 that differ by one part in 16129."""
+    b = B()
+    s = Step(8, 2, 128, [1600], [3], 5, 1, 16, seed=20)
+    k = torch.full((100, 16, 2, 128), 127.0, device="cuda")
+    k[..., 5] -= (torch.arange(100, device="cuda") * 37 % 101)[:, None, None].float()
+    s.k[s.at[0]:s.at[0] + 1600] = k.reshape(1600, 2, 128).to(torch.bfloat16)
+    s.q.fill_(127)
+    s.q[1, :, 0] = 1                                         # (a lower score for all blocks)
+    s.q[2, :, 5] = 2
+    bounds, scale = get_bounds(s, 16)
+    lists = torch.empty(3, 2, 40, dtype=torch.int32, device="cuda")
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, 0, 0, lists, s.ws(16))
+    want = torch.argsort(torch.arange(100) * 37 % 101, stable=True)[:40].sort().values
+    assert (lists.cpu() == want).all()
+
+
 def test_equal_scores_go_to_the_lower_block():
     b = B()
     s = Step(8, 2, 64, [1600], [2], 5, 1, 16, seed=12)
