@@ -353,52 +353,97 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
     }
   }
   if (!a.cluster) return;
-  // ---- the merge, four dims of a head per thread: the cluster's blocks in their order, then the pieces of the row's context that the kernel
-  // before has left.  In batches whose loads travel together. ----
+  // ---- the merge, four dims of a head per thread, 32 threads to a unit: the cluster's blocks in their order, and the pieces of the row's context
+  // that the kernel before has left, in batches whose loads travel together.  The cluster's blocks take the units in turn; warps that are left
+  // share a unit's sources where these are more than a batch.  (All of them in the first block's warps: 30 rows of 8 / 2 heads over 59 pieces each 45 us,
+  // so 32; 16 rows of 32 / 8 heads over 16 pieces 29.8 and 26.9.) ----
   cluster_sync();
-  const int pieces = ct.pieces[rc.ctx], sources = a.n_splits + pieces;
+  constexpr int kWarpsAll = kPagThreads / 32, kBatch = 10, kOwnBatch = 4;
+  struct Merged { float mx, den, acc[4]; };
+  Merged* merged_s = reinterpret_cast<Merged*>(base_ptr);             // (the ring, and what was exchanged through it, has been read)
+  static_assert(kWarpsAll * 32 * sizeof(Merged) <= kResult, "in front of the results");
+  const int pieces = ct.pieces[rc.ctx], quads = G * D / 4, per_block = a.merge_units, across = a.merge_across, groups = a.merge_groups;
+  const int group = (a.merge_group_of >> (4 * warp)) & 15;
   const long long stride = a.n_rows * a.H;
-  for (int i = split * kPagThreads + (int)threadIdx.x; live && fits && !gave_up && i < G * D / 4; i += a.n_splits * kPagThreads) {
-    constexpr int U = 10;
+  for (int u0 = 0; u0 < per_block; u0 += across) {                    // (once, unless there are more units than warps)
+    const int unit_in = u0 + warp - group * across, i = (split * per_block + unit_in) * 32 + lane;
+    const bool has = live && fits && !gave_up && group < groups && unit_in < per_block && i < quads;
     const int g = i / (D / 4), d = 4 * (i - g * (D / 4)), h = hd * G + g;
     const long long at = row * a.H + h;
-    float mx = -INFINITY, den = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < sources; s0 += U) {
-      float lse[U];
-      float4 v[U];
+    Merged r = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    auto take = [&](const float* lse, const float4* v, auto count) {
+      constexpr int N = decltype(count)::value;
+      float m_new = r.mx;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = s0 + u;
-        lse[u] = -INFINITY;
-        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < a.n_splits) {
-          const uint32_t peer = mapa_shared(base, (uint32_t)r);
-          lse[u] = ld_cluster_f32(peer + kResultLse + g * 4);
-          v[u] = ld_cluster_f32x4(peer + kResult + (g * D + d) * 4);
-        } else if (r < sources) {
-          lse[u] = a.part_lse[(r - a.n_splits) * stride + at] * kLog2eP;
-          v[u] = *reinterpret_cast<const float4*>(a.part_o + ((r - a.n_splits) * stride + at) * D + d);
+      for (int u = 0; u < N; ++u) m_new = fmaxf(m_new, lse[u]);
+      const float alpha = r.mx == -INFINITY ? 0.f : fast_exp2(r.mx - m_new);
+      r.mx = m_new;
+      r.den *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.acc[e] *= alpha;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const float w = lse[u] == -INFINITY ? 0.f : fast_exp2(lse[u] - r.mx);    // (NaN stays NaN: logits that were, or a block that gave up)
+        r.den += w;
+        if (w != 0.f) {
+          r.acc[0] = fmaf(w, v[u].x, r.acc[0]); r.acc[1] = fmaf(w, v[u].y, r.acc[1]);
+          r.acc[2] = fmaf(w, v[u].z, r.acc[2]); r.acc[3] = fmaf(w, v[u].w, r.acc[3]);
         }
       }
-      float m_new = mx;
+    };
+    // (the first batch of pieces is asked for before the cluster's results are read)
+    for (int s0 = group; has && (s0 == group || s0 < pieces); s0 += kBatch * groups) {
+      float lse[kBatch];
+      float4 v[kBatch];
+      if (pieces > 0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, lse[u]);
-      const float alpha = mx == -INFINITY ? 0.f : fast_exp2(mx - m_new);
-      mx = m_new;
-      den *= alpha;
+        for (int u = 0; u < kBatch; ++u) {
+          const int s = s0 + u * groups;
+          lse[u] = s < pieces ? a.part_lse[s * stride + at] * kLog2eP : -INFINITY;
+          v[u] = s < pieces ? *reinterpret_cast<const float4*>(a.part_o + (s * stride + at) * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+      if (s0 == group) {
+        for (int q0 = group; q0 < a.n_splits; q0 += kOwnBatch * groups) {
+          float own_lse[kOwnBatch];
+          float4 own_v[kOwnBatch];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+          for (int u = 0; u < kOwnBatch; ++u) {
+            const int s = q0 + u * groups;
+            own_lse[u] = -INFINITY;
+            own_v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s < a.n_splits) {
+              const uint32_t peer = mapa_shared(base, (uint32_t)s);
+              own_lse[u] = ld_cluster_f32(peer + kResultLse + g * 4);
+              own_v[u] = ld_cluster_f32x4(peer + kResult + (g * D + d) * 4);
+            }
+          }
+          take(own_lse, own_v, std::integral_constant<int, kOwnBatch>{});
+        }
+      }
+      if (pieces > 0) take(lse, v, std::integral_constant<int, kBatch>{});
+    }
+    if (groups > 1) {                                                 // (then this loop has one trip)
+      if (group > 0) merged_s[threadIdx.x] = r;
+      __syncthreads();
+      if (has && group == 0) {
+        for (int x = 1; x < groups; ++x) {
+          const Merged& o = merged_s[threadIdx.x + 32 * across * x];
+          const float m_new = fmaxf(r.mx, o.mx);
+          const float wr = r.mx == -INFINITY ? 0.f : fast_exp2(r.mx - m_new), wo = o.mx == -INFINITY ? 0.f : fast_exp2(o.mx - m_new);
+          r.mx = m_new;
+          r.den = r.den * wr + o.den * wo;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float w = lse[u] == -INFINITY ? 0.f : fast_exp2(lse[u] - mx);      // (NaN stays NaN: logits that were, or a block that gave up)
-        den += w;
-        if (w != 0.f) { acc[0] = fmaf(w, v[u].x, acc[0]); acc[1] = fmaf(w, v[u].y, acc[1]); acc[2] = fmaf(w, v[u].z, acc[2]); acc[3] = fmaf(w, v[u].w, acc[3]); }
+          for (int e = 0; e < 4; ++e) r.acc[e] = r.acc[e] * wr + o.acc[e] * wo;
+        }
       }
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
-    *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-    if (d == 0 && a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = den == 0.f ? -INFINITY : (mx + log2f(den)) * kLn2P;
+    if (has && group == 0) {
+      const float inv = r.den == 0.f ? 0.f : 1.f / r.den;
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(r.acc[0] * inv, r.acc[1] * inv), hi = __floats2bfloat162_rn(r.acc[2] * inv, r.acc[3] * inv);
+      *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      if (d == 0 && a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = r.den == 0.f ? -INFINITY : (r.mx + log2f(r.den)) * kLn2P;
+    }
   }
   cluster_sync();                                                     // nobody leaves while its results are read
 }
@@ -471,7 +516,7 @@ continuation_merge_kernel(const __grid_constant__ ContTable ct, const __grid_con
 }
 
 template <int D, int GMAX>
-static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& ct, const PagedAttnArgs& a, DeviceStatus* st, cudaStream_t stream) {
+static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& ct, PagedAttnArgs a, DeviceStatus* st, cudaStream_t stream) {
   static std::atomic<int> attr_done[kMaxDevices];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
@@ -482,6 +527,15 @@ static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& c
   }
   const long long blocks = a.n_rows * a.n_splits * a.Hkv;
   if (blocks > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  if (a.cluster) {                                       // who merges what: the kernel's divisions
+    constexpr int kWarpsAll = kPagThreads / 32;
+    int most = 0;
+    for (int b = 0; b < ct.n_req; ++b) most = std::max(most, ct.pieces[b]);
+    a.merge_units = ((a.H / a.Hkv * D / 4 + 31) / 32 + a.n_splits - 1) / a.n_splits;
+    a.merge_across = std::min(a.merge_units, kWarpsAll);
+    a.merge_groups = std::max(1, std::min(kWarpsAll / a.merge_units, (a.n_splits + most + 9) / 10));
+    for (int w = 0; w < kWarpsAll; ++w) a.merge_group_of |= (uint32_t)(w / a.merge_across) << (4 * w);
+  }
   const int pieces = a.cluster ? a.n_splits : 1;
   return cuda_ok(launch_chained_clusters(pieces, kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
 }

@@ -23,6 +23,9 @@ struct PagedAttnArgs {
   int n_splits;                        // pieces a row's keys are cut into
   int cluster;                         // 1: a row's pieces are a cluster of blocks, which merges them and what the prefix kernel has left
   int behind_prefix;                   // 1: launched by the prefix kernel, once the kernels in front of that one are complete
+  // clusters: a block's units of 32 threads' worth of results, units at once, groups of warps that share one, and every warp's group (4 bits each)
+  int merge_units, merge_across, merge_groups;
+  uint32_t merge_group_of;
   int slot0, n_slots;                  // first slot of these pieces, slots in all; one in all: results go to out
   float scale_log2;
 };
