@@ -295,6 +295,8 @@ ATTEND = {
     "multi head, many rows": dict(H=3, Hkv=3, D=128, ctx=[383, 640], seqs=[12, 5], own=129, new=1, bs=128, ctx_layout="gaps", layout="gaps"),
     "dim 64, long": dict(H=4, Hkv=4, D=64, ctx=[4500], seqs=[12], own=40, new=1, bs=32, ctx_layout="head"),
     "several tokens each, many rows": dict(H=8, Hkv=2, D=128, ctx=[700, 64, 0], seqs=[4, 3, 2], own=100, new=[9, 0, 11, 7, 2, 0, 1, 3, 1], bs=16, len_slack=9, bound_slack=3),
+    "sixty pieces": dict(H=2, Hkv=1, D=64, ctx=[16500, 300], seqs=[30, 9], own=90, new=1, bs=16),
+    "sixty pieces, wide groups": dict(H=14, Hkv=1, D=128, ctx=[9000], seqs=[60], own=200, new=1, bs=32),
     "large logits, many rows": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[24], own=60, new=1, bs=16, q_scale=12.0),
     "large logits": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[4], own=60, new=1, bs=16, q_scale=12.0),
 }
