@@ -17,6 +17,7 @@
 // the chain but not the tail, or lost the rows' shared blocks in L2: the first kernel 72 / 71 / 80 us of the 66, the second 33 / 37 / 33.
 // Every wait is bounded.
 #include "paged_attention.cuh"
+#include "continuation_splits.cuh"
 #include "sm100_ptx.cuh"
 #include <atomic>
 
@@ -24,20 +25,21 @@ namespace relaxkv {
 
 using namespace ptx;
 
-constexpr int kPagWarps = 4;                          // consumer warps
-constexpr int kPagThreads = (kPagWarps + 1) * 32;
-constexpr int kPagTile = 16 * kPagWarps;              // keys per tile
 constexpr int kPagStages = 3;
-constexpr int kPagEntries = kPagTile / 16;            // boxes of a tile, at most
 constexpr float kLog2eP = 1.4426950408889634f, kLn2P = 0.6931471805599453f;
 
-template <int D>
+// WARPS: consumer warps, sixteen keys of a tile each.
+template <int D, int WARPS>
 struct PagSmem {
-  static constexpr int kTileBytes = kPagTile * D * 2;
+  static constexpr int kThreads = (WARPS + 1) * 32;
+  static constexpr int kTile = 16 * WARPS;                        // keys per tile
+  static constexpr int kEntries = WARPS;                          // boxes of a tile, at most
+  static constexpr int kBlocksPerSm = WARPS == 4 ? 2 : WARPS == 2 ? 4 : 6;
+  static constexpr int kTileBytes = kTile * D * 2;
   static constexpr int kStageBytes = 2 * kTileBytes;              // K tile | V tile
   static constexpr int kBar = kPagStages * kStageBytes;           // full[stages], empty[stages]
   static constexpr int kValid = kBar + 16 * kPagStages;           // valid keys of each box of a stage
-  static constexpr int kMisc = kValid + 4 * kPagStages * kPagEntries;
+  static constexpr int kMisc = kValid + 4 * kPagStages * kEntries;
   static constexpr int kTotal = kMisc + 16;
   static constexpr int kDynamic = kTotal + 1024;
 };
@@ -56,12 +58,13 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
 }
 
 // GMAX: heads of a KV head's group, at most (8 or 16).
-template <int D, int GMAX>
-__global__ void __launch_bounds__(kPagThreads, 2)
+template <int D, int GMAX, int WARPS>
+__global__ void __launch_bounds__(PagSmem<D, WARPS>::kThreads, PagSmem<D, WARPS>::kBlocksPerSm)
 paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_constant__ CUtensorMap tm_cv,
                        const __grid_constant__ CUtensorMap tm_pk, const __grid_constant__ CUtensorMap tm_pv,
                        const __grid_constant__ ContTable ct, const __grid_constant__ PagedAttnArgs a, DeviceStatus* st) {
-  using L = PagSmem<D>;
+  using L = PagSmem<D, WARPS>;
+  constexpr int kThreads = L::kThreads, kTile = L::kTile, kEntries = L::kEntries;
   constexpr int kRowsUsed = GMAX > 8 ? 2 : 1;          // fragment rows gid (and gid + 8) that hold heads
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -69,7 +72,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   const uint32_t bar_full = base + L::kBar, bar_empty = bar_full + 8 * kPagStages;
   volatile int* valid_s = reinterpret_cast<volatile int*>(base_ptr + L::kValid);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + L::kMisc);
-  __shared__ float m_s[kPagWarps][GMAX], z_s[kPagWarps][GMAX];
+  __shared__ float m_s[WARPS][GMAX], z_s[WARPS][GMAX];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.H / a.Hkv;
   // KV heads fastest; with clusters, whose blocks stand side by side, the pieces
@@ -77,12 +80,12 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   const int hd = (int)((a.cluster ? unit : blockIdx.x) % a.Hkv), split = (int)(a.cluster ? blockIdx.x - unit * a.n_splits : blockIdx.x / a.Hkv % a.n_splits);
   const long long row = blockIdx.x / (a.Hkv * a.n_splits);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kPagStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, kPagWarps); }
+    for (int s = 0; s < kPagStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, WARPS); }
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
   }
-  if (threadIdx.x == kPagWarps * 32) {                  // (of maps that there are)
+  if (threadIdx.x == WARPS * 32) {                  // (of maps that there are)
     if (a.ctx_keys != CTX_KEYS_NONE) { prefetch_tensormap(&tm_ck); prefetch_tensormap(&tm_cv); }
     if (a.max_len > 0) { prefetch_tensormap(&tm_pk); prefetch_tensormap(&tm_pv); }
   }
@@ -108,20 +111,20 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   // looked at when the results are written: more rows than the host's bound
   const int rows_first = a.row_cu[ct.seq_cu[rc.ctx]], rows_end = a.row_cu[ct.seq_cu[rc.ctx + 1]];
   // ---- this piece's tiles: the row's are [listed context blocks | own tokens] ----
-  const int ctx_box = min(a.ctx_block, kPagTile), page_box = min(a.page, kPagTile);
+  const int ctx_box = min(a.ctx_block, kTile), page_box = min(a.page, kTile);
   const int ctx_sub = a.ctx_block / ctx_box, page_sub = a.page / page_box;             // boxes of a block
-  const int ctx_per = kPagTile / ctx_box, page_per = kPagTile / page_box;              // boxes of a tile
+  const int ctx_per = kTile / ctx_box, page_per = kTile / page_box;              // boxes of a tile
   const int ctx_len = ct.ctx_len[rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
   const int listed = a.ctx_keys == CTX_KEYS_NONE || ctx_len == 0 ? 0 : a.ctx_keys == CTX_KEYS_ALL ? ctx_blocks : a.n_select;      // blocks
   const int n_ctx = (listed * ctx_sub + ctx_per - 1) / ctx_per;
-  const int n_tiles = live ? n_ctx + (rc.len + kPagTile - 1) / kPagTile : 0;
+  const int n_tiles = live ? n_ctx + (rc.len + kTile - 1) / kTile : 0;
   const int per = (n_tiles + a.n_splits - 1) / a.n_splits;
   const int t0 = min(n_tiles, split * per), t1 = min(n_tiles, t0 + per);
 
   float frag_m[2] = {-INFINITY, -INFINITY}, frag_z[2] = {0.f, 0.f}, frag_o[D / 8][4];
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) frag_o[d][0] = frag_o[d][1] = frag_o[d][2] = frag_o[d][3] = 0.f;
-  if (warp == kPagWarps) {
+  if (warp == WARPS) {
     // ================= producer: one lane per box =================
     const int* list = a.ctx_keys == CTX_KEYS_LISTED ? a.lists + (row * a.Hkv + hd) * a.n_select : nullptr;
     auto block_number = [&](int t) -> int {             // of this lane's box of tile t; -1: none
@@ -159,7 +162,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
             else report(st, RELAXKV_ERR_BAD_INDEX, KID_PAGED_ATTN, id, a.n_blocks);
           }
         }
-        valid_s[s * kPagEntries + lane] = valid;
+        valid_s[s * kEntries + lane] = valid;
       }
       const int n_boxes = __popc(__ballot_sync(0xffffffffu, valid > 0));
       __syncwarp();                                     // the valid keys of all boxes are written
@@ -191,7 +194,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       const int box = t < n_ctx ? ctx_box : page_box, entry = warp * 16 / box, off = warp * 16 - entry * box;
-      const int n_here = min(16, valid_s[s * kPagEntries + entry] - off);                 // keys of this warp's chunk that count
+      const int n_here = min(16, valid_s[s * kEntries + entry] - off);                 // keys of this warp's chunk that count
       if (n_here > 0) {
         const uint32_t half = (uint32_t)box * 128, chunk = (uint32_t)(entry * box * D * 2 + off * 128);
         const uint32_t kt = base + s * L::kStageBytes + chunk, vt = kt + L::kTileBytes;
@@ -275,14 +278,14 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   griddep_launch();                                                   // (called first thing, sixteen rows of 16 K took 30.1 us, 29.4 so)
   // ---- the warps' results, added up in a fixed order: every warp adds up a quarter of the dims, the others' come through the ring's place
   // in fragment order (written head by head, a warp's stores met in eight banks and this took 1.3 us) ----
-  constexpr int kOwn = D / 8 / kPagWarps;                             // of the 8-dim column tiles of O
-  static_assert(kPagWarps * (kPagWarps - 1) * kOwn * 32 * kRowsUsed * 8 <= L::kBar, "they fit the ring");
+  constexpr int kOwn = D / 8 / WARPS;                             // of the 8-dim column tiles of O
+  static_assert(WARPS * (WARPS - 1) * kOwn * 32 * kRowsUsed * 8 <= L::kBar, "they fit the ring");
   auto part_s = [&](int owner, int from, int i) -> float2* {          // warp `from`'s fragment of tile i of `owner`: this lane's place
-    return reinterpret_cast<float2*>(base_ptr) + (((owner * (kPagWarps - 1) + from - (from > owner ? 1 : 0)) * kOwn + i) * 32 + lane) * kRowsUsed;
+    return reinterpret_cast<float2*>(base_ptr) + (((owner * (WARPS - 1) + from - (from > owner ? 1 : 0)) * kOwn + i) * 32 + lane) * kRowsUsed;
   };
   const int gid = lane >> 2, tig = lane & 3;
   float own[kOwn][2 * kRowsUsed];
-  if (warp < kPagWarps && !*abort_flag) {
+  if (warp < WARPS && !*abort_flag) {
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
       if (d / kOwn == warp) {
@@ -312,18 +315,18 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   if (!a.cluster && (gave_up || !fits)) return;
   // where a cluster's blocks find each other's results: [G][D] normalised, behind them the log-sum-exps (in log2 units; NaN: given up)
   constexpr int kResult = L::kBar / 2, kResultLse = kResult + GMAX * D * 4;
-  static_assert(kPagWarps * (kPagWarps - 1) * kOwn * 32 * kRowsUsed * 8 <= kResult && kResultLse + GMAX * 4 <= L::kBar, "side by side in the ring");
-  if (warp < kPagWarps) {
+  static_assert(WARPS * (WARPS - 1) * kOwn * 32 * kRowsUsed * 8 <= kResult && kResultLse + GMAX * 4 <= L::kBar, "side by side in the ring");
+  if (warp < WARPS) {
 #pragma unroll
     for (int rr = 0; rr < kRowsUsed; ++rr) {
       const int g = gid + 8 * rr;
       if (g >= G) continue;
       float mb = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kPagWarps; ++w) mb = fmaxf(mb, m_s[w][g]);
-      float wgt[kPagWarps], zb = 0.f;
+      for (int w = 0; w < WARPS; ++w) mb = fmaxf(mb, m_s[w][g]);
+      float wgt[WARPS], zb = 0.f;
 #pragma unroll
-      for (int w = 0; w < kPagWarps; ++w) {
+      for (int w = 0; w < WARPS; ++w) {
         wgt[w] = mb == -INFINITY ? 0.f : fast_exp2(m_s[w][g] - mb);   // (0 for a warp without keys)
         zb = fmaf(z_s[w][g], wgt[w], zb);
       }
@@ -335,7 +338,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
       for (int i = 0; i < kOwn; ++i) {
         float a0 = 0.f, a1 = 0.f;
 #pragma unroll
-        for (int w = 0; w < kPagWarps; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
           const float2 v = w == warp ? make_float2(own[i][2 * rr], own[i][2 * rr + 1]) : part_s(warp, w, i)[rr];
           a0 = fmaf(v.x, wgt[w], a0);
           a1 = fmaf(v.y, wgt[w], a1);
@@ -358,7 +361,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   // share a unit's sources where these are more than a batch.  (All of them in the first block's warps: 30 rows of 8 / 2 heads over 59 pieces each 45 us,
   // so 32; 16 rows of 32 / 8 heads over 16 pieces 29.8 and 26.9.) ----
   cluster_sync();
-  constexpr int kWarpsAll = kPagThreads / 32, kBatch = 10, kOwnBatch = 4;
+  constexpr int kWarpsAll = kThreads / 32, kBatch = 10, kOwnBatch = 4;
   struct Merged { float mx, den, acc[4]; };
   Merged* merged_s = reinterpret_cast<Merged*>(base_ptr);             // (the ring, and what was exchanged through it, has been read)
   static_assert(kWarpsAll * 32 * sizeof(Merged) <= kResult, "in front of the results");
@@ -515,20 +518,21 @@ continuation_merge_kernel(const __grid_constant__ ContTable ct, const __grid_con
   if (lane == 0 && a.lse_out) a.lse_out[(long long)h * a.n_rows + row] = den != 0.f ? mx + logf(den) : -INFINITY;
 }
 
-template <int D, int GMAX>
+template <int D, int GMAX, int WARPS>
 static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& ct, PagedAttnArgs a, DeviceStatus* st, cudaStream_t stream) {
   static std::atomic<int> attr_done[kMaxDevices];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
-  auto kern = paged_attention_kernel<D, GMAX>;
+  using L = PagSmem<D, WARPS>;
+  auto kern = paged_attention_kernel<D, GMAX, WARPS>;
   if (!attr_done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PagSmem<D>::kDynamic) != cudaSuccess) return RELAXKV_ERR_CUDA;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic) != cudaSuccess) return RELAXKV_ERR_CUDA;
     attr_done[dev].store(1, std::memory_order_release);
   }
   const long long blocks = a.n_rows * a.n_splits * a.Hkv;
   if (blocks > 0x7fffffffLL) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
   if (a.cluster) {                                       // who merges what: the kernel's divisions
-    constexpr int kWarpsAll = kPagThreads / 32;
+    constexpr int kWarpsAll = L::kThreads / 32;
     int most = 0;
     for (int b = 0; b < ct.n_req; ++b) most = std::max(most, ct.pieces[b]);
     a.merge_units = ((a.H / a.Hkv * D / 4 + 31) / 32 + a.n_splits - 1) / a.n_splits;
@@ -537,7 +541,16 @@ static relaxkv_status launch_paged_g(const CUtensorMap* maps, const ContTable& c
     for (int w = 0; w < kWarpsAll; ++w) a.merge_group_of |= (uint32_t)(w / a.merge_across) << (4 * w);
   }
   const int pieces = a.cluster ? a.n_splits : 1;
-  return cuda_ok(launch_chained_clusters(pieces, kern, dim3((unsigned)blocks), kPagThreads, PagSmem<D>::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
+  return cuda_ok(launch_chained_clusters(pieces, kern, dim3((unsigned)blocks), L::kThreads, L::kDynamic, stream, maps[0], maps[1], maps[2], maps[3], ct, a, st));
+}
+
+template <int D>
+static relaxkv_status launch_paged_d(int warps, const CUtensorMap* maps, const ContTable& ct, const PagedAttnArgs& a, DeviceStatus* st, cudaStream_t stream) {
+  if (a.H / a.Hkv > 8)
+    return warps == 1 ? launch_paged_g<D, 16, 1>(maps, ct, a, st, stream)
+                      : warps == 2 ? launch_paged_g<D, 16, 2>(maps, ct, a, st, stream) : launch_paged_g<D, 16, 4>(maps, ct, a, st, stream);
+  return warps == 1 ? launch_paged_g<D, 8, 1>(maps, ct, a, st, stream)
+                    : warps == 2 ? launch_paged_g<D, 8, 2>(maps, ct, a, st, stream) : launch_paged_g<D, 8, 4>(maps, ct, a, st, stream);
 }
 
 relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
@@ -545,24 +558,25 @@ relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_
   DeviceStatus* st = status_word();
   if (!st) return RELAXKV_ERR_CUDA;
   const int D = shape->head_dim;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return RELAXKV_ERR_CUDA;
+  const int warps = a.ctx_keys == CTX_KEYS_NONE && a.n_splits == 1 ? paged_warps(a.n_rows * a.Hkv, a.max_len, sms) : 4;
   CUtensorMap maps[4] = {};
   if (a.ctx_keys != CTX_KEYS_NONE) {
     long long tokens = 0;
     for (int b = 0; b < ct.n_req; ++b) tokens = std::max(tokens, ct.ctx_len[b] ? ct.tok_off[b] + ct.ctx_len[b] : 0);
-    const uint32_t box = (uint32_t)std::min(a.ctx_block, kPagTile);
+    const uint32_t box = (uint32_t)std::min(a.ctx_block, 16 * warps);
     for (int i = 0; i < 2; ++i)
       if (!make_block_map(&maps[i], i ? cache->v : cache->k, D, (uint64_t)tokens, a.Hkv, 1, (uint64_t)cache->token_stride, (uint64_t)cache->head_stride,
                           (uint64_t)cache->token_stride, box)) return RELAXKV_ERR_CUDA;
   }
   if (a.max_len > 0) {
-    const uint32_t box = (uint32_t)std::min(a.page, kPagTile);
+    const uint32_t box = (uint32_t)std::min(a.page, 16 * warps);
     for (int i = 0; i < 2; ++i)
       if (!make_block_map(&maps[2 + i], i ? store->v : store->k, D, (uint64_t)store->block_size, a.Hkv, (uint64_t)store->n_blocks,
                           (uint64_t)store->token_stride, (uint64_t)store->head_stride, (uint64_t)store->block_stride, box)) return RELAXKV_ERR_CUDA;
   }
-  const bool wide = a.H / a.Hkv > 8;
-  if (D == 128) return wide ? launch_paged_g<128, 16>(maps, ct, a, st, stream) : launch_paged_g<128, 8>(maps, ct, a, st, stream);
-  return wide ? launch_paged_g<64, 16>(maps, ct, a, st, stream) : launch_paged_g<64, 8>(maps, ct, a, st, stream);
+  return D == 128 ? launch_paged_d<128>(warps, maps, ct, a, st, stream) : launch_paged_d<64>(warps, maps, ct, a, st, stream);
 }
 
 relaxkv_status launch_continuation_merge(const ContTable& ct, const PagedAttnArgs& a, int D, cudaStream_t stream) {

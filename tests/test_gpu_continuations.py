@@ -297,6 +297,14 @@ ATTEND = {
     "several tokens each, many rows": dict(H=8, Hkv=2, D=128, ctx=[700, 64, 0], seqs=[4, 3, 2], own=100, new=[9, 0, 11, 7, 2, 0, 1, 3, 1], bs=16, len_slack=9, bound_slack=3),
     "sixty pieces": dict(H=2, Hkv=1, D=64, ctx=[16500, 300], seqs=[30, 9], own=90, new=1, bs=16),
     "sixty pieces, wide groups": dict(H=14, Hkv=1, D=128, ctx=[9000], seqs=[60], own=200, new=1, bs=32),
+    # (so many (row, KV head) pairs that blocks of one or two consumer warps are taken)
+    "a warp per row": dict(H=16, Hkv=8, D=128, ctx=[300, 40], seqs=[70, 45], own=100, new=1, bs=16, ctx_layout="head"),
+    "a warp per row, blocks of 128": dict(H=8, Hkv=8, D=64, ctx=[130, 0], seqs=[25, 8], own=200, new=4, bs=128, layout="head"),
+    "a warp per row, nine heads": dict(H=18, Hkv=2, D=64, ctx=[70], seqs=[450], own=30, new=1, bs=32),
+    "a warp per row, sixteen heads": dict(H=128, Hkv=8, D=128, ctx=[200], seqs=[112], own=20, new=1, bs=16, layout="gaps"),
+    "two warps per row": dict(H=8, Hkv=8, D=128, ctx=[500], seqs=[60], own=600, new=1, bs=64, layout="head"),
+    "two warps per row, no context": dict(H=48, Hkv=3, D=64, ctx=[0], seqs=[150], own=150, new=1, bs=128),
+    "two warps per row, nine heads": dict(H=72, Hkv=8, D=128, ctx=[100], seqs=[57], own=90, new=1, bs=16),
     "large logits, many rows": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[24], own=60, new=1, bs=16, q_scale=12.0),
     "large logits": dict(H=8, Hkv=2, D=128, ctx=[900], seqs=[4], own=60, new=1, bs=16, q_scale=12.0),
 }
