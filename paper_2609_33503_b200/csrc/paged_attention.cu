@@ -6,7 +6,8 @@
 // lanes look the block numbers up a tile ahead and each issues its own box, K and V), and four consumer warps take 16 keys of a tile each:
 // S = Q K^T and O += P V as warp-level MMAs whose 16 rows are the heads (a 128-row tcgen05 tile would be 3 to 6 % full), softmax on the
 // fragments.  16 keys never straddle a block, so a chunk's valid keys are one number.  Tiles of 64 keys and three stages leave room for two
-// blocks per SM, which hide each other's starts.
+// blocks per SM, which hide each other's starts; many rows of few keys go to blocks of two consumer warps or one, with tiles as much smaller (the
+// rule and its figures: continuation_splits.cuh).
 // A row's pieces merge among themselves where a cluster of up to eight blocks is enough (four rows of 32 K, 64 blocks each: 15.9 us, 18.1 with a merge
 // behind), and with what the prefix kernel has left of the row's context.
 // Measured, 128 of 2048 blocks for each of 16 rows 66 us (5.9 TB/s of HBM; rows share blocks in L2); own tokens of 64 rows of 40 / 8 heads, 512 on
@@ -560,7 +561,7 @@ relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_
   const int D = shape->head_dim;
   const int sms = sm_count_of_current_device();
   if (sms <= 0) return RELAXKV_ERR_CUDA;
-  const int warps = a.ctx_keys == CTX_KEYS_NONE && a.n_splits == 1 ? paged_warps(a.n_rows * a.Hkv, a.max_len, sms) : 4;
+  const int warps = a.n_splits == 1 ? paged_warps(a.n_rows * a.Hkv, (long long)a.n_select * a.ctx_block + a.max_len, sms) : 4;
   CUtensorMap maps[4] = {};
   if (a.ctx_keys != CTX_KEYS_NONE) {
     long long tokens = 0;

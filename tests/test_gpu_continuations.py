@@ -524,6 +524,8 @@ SPARSE = {
     "sixteen heads": dict(H=16, Hkv=1, D=64, ctx=[2000, 2500], seqs=[2, 5], own=40, new=1, bs=128, ctx_layout="gaps"),
     "eight heads": dict(H=8, Hkv=1, D=128, ctx=[4000], seqs=[21], own=20, new=1, bs=16),
     "single heads": dict(H=2, Hkv=2, D=64, ctx=[900], seqs=[3], own=20, new=[1, 0, 3], bs=16, layout="gaps"),
+    "two warps per row": dict(H=16, Hkv=8, D=128, ctx=[600, 0], seqs=[50, 10], own=30, new=1, bs=32, ctx_layout="head"),
+    "a warp per row": dict(H=8, Hkv=8, D=64, ctx=[400], seqs=[115], own=20, new=1, bs=64, layout="head"),
 }
 
 
