@@ -11,8 +11,10 @@
 //   P and O are single: a group hands its P over when O of the tile before is complete, which is also when O may be rescaled (every barrier
 //   belongs to the even or to the odd tiles, so that nobody who waits for one phase can be two behind);
 //   the running maximum of a row goes from group to group through shared memory (known a third into a group's step); sums stay with the groups.
-// Measured: 1700 clk per tile.  (Each group with an output of its own, S and P in one place, Q in shared memory: 1780.)  64 rows of 40 / 8 heads over
-// 32 K, three row tiles: 50 us of the 21 that the keys take and the 30 of the products.  16 rows of 32 / 8 heads over 16 K, where a block has eight
+// Tiles are loaded in the order of the products, K two tiles ahead of V: with K0 V0 K1 V1 ... a V tile waits in its buffer for two tiles' time, and five
+// buffers were too few (64 rows of 40 / 8 heads over 32 K without own tokens 80 us, seven 59; in this order five 55.5, six 57, seven 58).
+// Measured: some 1700 clk per tile.  (Each group with an output of its own, S and P in one place, Q in shared memory: 1780.)  64 rows of 40 / 8 heads over
+// 32 K, three row tiles: 47 us of the 21 that the keys take and the 30 of the products.  16 rows of 32 / 8 heads over 16 K, where a block has eight
 // tiles and its start and end count: 14 us of 10.
 // A row's pieces are merged with its own tokens by their log-sum-exps: by the clusters of the kernel over those (paged_attention.cu), or by a kernel
 // behind it.  That kernel begins when every block here has passed its wait, and reads what this one writes only after its own: 83.8 -> 80.6 and
@@ -27,7 +29,7 @@ namespace relaxkv {
 using namespace ptx;
 
 constexpr int kPreTile = 128;                         // keys per tile = rows per block
-constexpr int kPreRing = 7;                           // tile buffers, used in the order K0 V0 K1 V1 ...
+constexpr int kPreRing = 5;                           // tile buffers, used in the order of the products: K0 K1 K2 V0 K3 V1 ...
 constexpr int kPreThreads = 384;                      // two groups of four softmax warps; the TMA warp, the MMA warp, two idle
 constexpr float kPreRescale = 8.0f;                   // log2 units: O is rescaled only when the row maximum grew by more
 constexpr float kLog2ePre = 1.4426950408889634f, kLn2Pre = 0.6931471805599453f;
@@ -52,6 +54,14 @@ __device__ __forceinline__ float prefix_exponentials(const uint32_t* s, uint32_t
     }
   }
   return (z0 + z1) + (z2 + z3);
+}
+
+// The u-th of a block's 2 n loads: Q K^T is two tiles ahead of P V.
+struct PreLoad { int tile; bool v; };
+__device__ __forceinline__ PreLoad prefix_load(int u, int n) {
+  if (u < min(n, 2)) return {u, false};
+  if (u >= 2 * n - 2) return {u - n, true};
+  return u & 1 ? PreLoad{(u - 3) >> 1, true} : PreLoad{(u + 2) >> 1, false};
 }
 
 template <int D>
@@ -117,7 +127,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     if (x < L::kHalves && guess < a.n_rows && t_local < rows_per_tile) prefetch_l2(a.q + (guess * a.H + head) * D + x * 64);
     if (threadIdx.x == 0) { prefetch_l2(st); prefetch_l2(a.row_cu + ct.seq_cu[b]); prefetch_l2(a.row_cu + ct.seq_cu[b + 1]); }
   } else if (threadIdx.x == 256) {
-    for (int u = 0; u < min(2 * n, kPreRing); ++u) tma_prefetch_5d((u & 1) ? &tm_v : &tm_k, token0 + (u >> 1) * kPreTile, hd, 0);
+    for (int u = 0; u < min(2 * n, kPreRing); ++u) {
+      const PreLoad ld = prefix_load(u, n);
+      tma_prefetch_5d(ld.v ? &tm_v : &tm_k, token0 + ld.tile * kPreTile, hd, 0);
+    }
   }
   if (threadIdx.x < kPreTile) max_s[threadIdx.x] = -1.0e30f;      // (finite, so that logits of -inf leave 2^(-inf) = 0)
   tc_fence_before();
@@ -144,13 +157,14 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   if (warp >= 8) {
   reg_dealloc<56>();
   if (warp == 8) {
-    // ================= TMA producer: K_0 V_0 K_1 V_1 ... =================
+    // ================= TMA producer =================
     if (lane == 0) {
       for (int u = 0; u < 2 * n; ++u) {
         const int s = u % kPreRing;
         if (u >= kPreRing && !mbar_wait(bar_empty + 8 * s, (uint32_t)(u / kPreRing - 1) & 1, abort_flag)) break;
         mbar_expect_tx(bar_full + 8 * s, L::kTileBytes);
-        tma_load_5d(base + s * L::kTileBytes, (u & 1) ? &tm_v : &tm_k, bar_full + 8 * s, token0 + (u >> 1) * kPreTile, hd, 0);
+        const PreLoad ld = prefix_load(u, n);
+        tma_load_5d(base + s * L::kTileBytes, ld.v ? &tm_v : &tm_k, bar_full + 8 * s, token0 + ld.tile * kPreTile, hd, 0);
       }
     }
     __syncwarp();
@@ -172,33 +186,33 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     constexpr uint32_t idesc_qk = idesc_bf16_f32(kPreTile, kPreTile, 0), idesc_pv = idesc_bf16_f32(kPreTile, D, 1);
     constexpr uint32_t hi = desc_hi_sw128(1024);
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, abort_flag)); };
-    // buffers and phases of the next K tile and of the next V tile; a buffer that no later tile takes is not reported free (an arrival that
-    // nobody waits for could come when the block has gone)
-    int sk = 0, sv = 1;
-    uint32_t pk = 0, pv = 0;
-    auto step = [&](int& s, uint32_t& phase) { s += 2; if (s >= kPreRing) { s -= kPreRing; phase ^= 1u; } };
+    // number, buffer and phase of the next load, which is always the next to be used; a buffer that no later tile takes is not reported free (an
+    // arrival that nobody waits for could come when the block has gone)
+    int at_u = 0, s = 0;
+    uint32_t phase = 0;
+    auto step = [&]() { ++at_u; if (++s == kPreRing) { s = 0; phase ^= 1u; } };
     auto issue_qk = [&](int j) -> bool {                // S_j = Q K_j^T
-      if (!wait(bar_full + 8 * sk, pk)) return false;
+      if (!wait(bar_full + 8 * s, phase)) return false;
       if (j > 1 && !wait(bar_read + 8 * (j & 1), (uint32_t)((j >> 1) - 1))) return false;         // S_{j-2} is in registers
       tc_fence_after();
-      warp_mma_ts_kmajor<L::kHalves>(tmem_base + (j & 1) * 128, tmem_base + kQ, desc_lo(base + sk * L::kTileBytes, 16), hi, idesc_qk);
-      if (2 * j + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * sk);
+      warp_mma_ts_kmajor<L::kHalves>(tmem_base + (j & 1) * 128, tmem_base + kQ, desc_lo(base + s * L::kTileBytes, 16), hi, idesc_qk);
+      if (at_u + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * s);
       warp_mma_commit(bar_s + 8 * (j & 1));
-      step(sk, pk);
+      step();
       return true;
     };
     bool ok = n > 0 && wait(bar_q, 0);
     for (int j = 0; ok && j < min(n, 2); ++j) ok = issue_qk(j);
     for (int j = 0; ok && j < n; ++j) {
       if (j + 2 < n && !(ok = issue_qk(j + 2))) break;
-      if (!(ok = wait(bar_full + 8 * sv, pv))) break;
+      if (!(ok = wait(bar_full + 8 * s, phase))) break;
       if (fix_v && j == n - 1 && !(ok = wait(bar_vfix, 0))) break;
       if (!(ok = wait(bar_p + 8 * (j & 1), (uint32_t)(j >> 1)))) break;
       tc_fence_after();
-      warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + kP, desc_lo(base + sv * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
-      if (2 * j + 1 + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * sv);
+      warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + kP, desc_lo(base + s * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
+      if (at_u + kPreRing < 2 * n) warp_mma_commit(bar_empty + 8 * s);
       warp_mma_commit(bar_o + 8 * (j & 1));
-      step(sv, pv);
+      step();
     }
   }
   } else {
