@@ -272,8 +272,13 @@ class PagedStore:
         return int(self.k.shape[1])
 
 
-def _is_table(t: torch.Tensor) -> bool:
-    return t.dim() == 2 and t.stride(1) == 1 and (t.shape[0] == 1 or t.stride(0) >= t.shape[1])
+def _table_layout(t: torch.Tensor):
+    """Width and row distance of a block table."""
+    n, width = t.shape
+    distance, one = t.stride()
+    if one != 1 or (distance < width and n > 1):
+        raise AssertionError("a block table's rows are contiguous and do not overlap")
+    return width, max(distance, width)
 
 
 class ContinuationRows:
@@ -287,7 +292,7 @@ class ContinuationRows:
             assert t is None or t.dtype == torch.int32
         assert len(max_rows) == len(seq_cu) - 1 and row_cu.numel() == seq_cu[-1] + 1 and row_cu.is_contiguous() and row_seq.is_contiguous()
         assert row_len is None or (row_len.is_contiguous() and row_len.numel() >= row_seq.numel())
-        assert block_table is None or (_is_table(block_table) and block_table.shape[0] >= seq_cu[-1])
+        assert block_table is None or (_table_layout(block_table) and block_table.shape[0] >= seq_cu[-1])
         self._keep = (_i32(seq_cu), _i32(max_rows), row_cu, row_seq, row_len, block_table)
         self.c = _ContinuationRows()
         self.c.n_seq, self.c.n_rows, self.c.max_len = int(seq_cu[-1]), row_seq.numel(), int(max_len)
@@ -529,11 +534,10 @@ def relaxkv_build_block_tables(block_size: int, seq_len: torch.Tensor, new_len: 
                                n_free_out: torch.Tensor, row_cu: torch.Tensor, row_seq: torch.Tensor, row_pos: torch.Tensor,
                                row_len: torch.Tensor, row_slot: torch.Tensor, stream=None) -> None:
     """seq_len, new_len, seq_base [n_seq]; block_table [n_seq, width] (rows any distance apart); row_* [n_rows].  All int32."""
-    assert _is_table(block_table)
+    width, distance = _table_layout(block_table)
     _check(lib().relaxkv_build_block_tables(*_args("..pppp.pp...ppppppp.", seq_len.numel(), int(block_size), seq_len, new_len, seq_base,
-                                                   free_blocks, free_blocks.numel(), n_free, block_table, block_table.shape[1],
-                                                   max(block_table.stride(0), block_table.shape[1]), row_seq.numel(), seq_len_out, n_free_out,
-                                                   row_cu, row_seq, row_pos, row_len, row_slot, _stream(stream))),
+                                                   free_blocks, free_blocks.numel(), n_free, block_table, width, distance, row_seq.numel(),
+                                                   seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot, _stream(stream))),
            "relaxkv_build_block_tables")
 
 
@@ -541,9 +545,10 @@ def relaxkv_qk_norm_rope_append_paged(store: PagedStore, q: torch.Tensor, k: tor
                                       slots: torch.Tensor, theta: float, q_out: torch.Tensor, w_q_norm: Optional[torch.Tensor] = None,
                                       w_k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
     """q_out [n, H, D] = normed and rotated q (may be q); the store receives the normed and rotated k and v [n, H_kv, D] at `slots`."""
-    _check(lib().relaxkv_qk_norm_rope_append_paged(*_args("sppp....pp.pp.p.", store.c, q, k, v, q.shape[0], q.shape[1], k.shape[1], q.shape[2],
-                                                          w_q_norm, w_k_norm, float(eps), positions, slots, float(theta), q_out,
-                                                          _stream(stream))), "relaxkv_qk_norm_rope_append_paged")
+    n, heads, dim = q.shape
+    _check(lib().relaxkv_qk_norm_rope_append_paged(*_args("sppp....pp.pp.p.", store.c, q, k, v, n, heads, k.shape[1], dim, w_q_norm, w_k_norm,
+                                                          float(eps), positions, slots, float(theta), q_out, _stream(stream))),
+           "relaxkv_qk_norm_rope_append_paged")
 
 
 def _optional(struct):

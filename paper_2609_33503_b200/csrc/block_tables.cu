@@ -11,8 +11,6 @@
 namespace relaxkv {
 
 constexpr int kTabMaxSeq = 4096;
-constexpr int kTabThreads = 1024;
-constexpr int kTabPer = kTabMaxSeq / kTabThreads;           // sequences of a thread, at most
 
 struct TableArgs {
   int n_seq, block_size, free_capacity, table_width;
@@ -30,27 +28,29 @@ __device__ __forceinline__ int bisect(const int* cu, int n, int x) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kTabThreads)
+// PER: sequences of a thread, at most.
+template <int THREADS, int PER>
+__global__ void __launch_bounds__(THREADS)
 block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   extern __shared__ int cu_s[];
   int *rows_cu = cu_s, *need_cu = cu_s + a.n_seq + 1, *back_cu = need_cu + a.n_seq + 1, *had_s = back_cu + a.n_seq + 1;
-  __shared__ long long warp_rows[kTabThreads / 32];
-  __shared__ int warp_need[kTabThreads / 32], warp_back[kTabThreads / 32];
+  __shared__ long long warp_rows[THREADS / 32];
+  __shared__ int warp_need[THREADS / 32], warp_back[THREADS / 32];
   griddep_launch();
   griddep_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = kTabThreads / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = THREADS / 32;
   const int shift = 31 - __clz(a.block_size);
   const bool teller = blockIdx.x == 0;
-  const int per = (a.n_seq + kTabThreads - 1) / kTabThreads, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
+  const int per = (a.n_seq + THREADS - 1) / THREADS, first = min(a.n_seq, tid * per), last = min(a.n_seq, first + per);
   const long long room = min((long long)a.table_width << shift, 0x7fffffffLL);
   const int n_free = *a.n_free;
   // lengths and requests by way of shared memory (the requests in the place of a sum that comes later), then a thread's own in registers: what
   // one asks for and cannot have counts as nothing
-  for (int i = tid; i < a.n_seq; i += kTabThreads) { had_s[i] = a.seq_len[i]; rows_cu[i] = a.new_len[i]; }
+  for (int i = tid; i < a.n_seq; i += THREADS) { had_s[i] = a.seq_len[i]; rows_cu[i] = a.new_len[i]; }
   __syncthreads();
-  int had_[kTabPer], rows_[kTabPer], need_[kTabPer], back_[kTabPer];
+  int had_[PER], rows_[PER], need_[PER], back_[PER];
 #pragma unroll
-  for (int e = 0; e < kTabPer; ++e) {
+  for (int e = 0; e < PER; ++e) {
     had_[e] = first + e < last ? had_s[first + e] : 0;
     rows_[e] = first + e < last ? rows_cu[first + e] : 0;
   }
@@ -58,7 +58,7 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
   long long rows_t = 0;
   int need_t = 0, back_t = 0;
 #pragma unroll
-  for (int e = 0; e < kTabPer; ++e) {
+  for (int e = 0; e < PER; ++e) {
     need_[e] = back_[e] = 0;
     if (e >= per) continue;                             // (the same for all threads)
     const int len = had_[e], add = rows_[e];
@@ -108,7 +108,7 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
     long long rows_at = rows_before + rows_x - rows_t;
     int need_at = need_before + need_x - need_t, back_at = back_before + back_x - back_t;
 #pragma unroll
-    for (int e = 0; e < kTabPer; ++e) {
+    for (int e = 0; e < PER; ++e) {
       const int i = first + e;
       if (i >= last) break;
       rows_cu[i] = grow ? (int)rows_at : 0;
@@ -134,7 +134,7 @@ block_tables_kernel(const TableArgs a, DeviceStatus* st) {
     const int at = top - 1 - j;
     return at < n_free ? a.free_blocks + at : released(at - n_free);
   };
-  const long long step = (long long)gridDim.x * kTabThreads, me = (long long)blockIdx.x * kTabThreads + tid;
+  const long long step = (long long)gridDim.x * THREADS, me = (long long)blockIdx.x * THREADS + tid;
   for (long long j = me; j < total_need; j += step) {
     const int i = bisect(need_cu, a.n_seq, (int)j);
     a.table[i * a.table_stride + blocks_of(had_s[i], shift) + ((int)j - need_cu[i])] = *taken((int)j);
@@ -178,18 +178,24 @@ extern "C" relaxkv_status relaxkv_build_block_tables(
   DeviceStatus* st = status_word();
   const int sms = sm_count_of_current_device();
   if (!st || sms <= 0) return RELAXKV_ERR_CUDA;
-  static std::atomic<int> attr_done[kMaxDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
-  if (!attr_done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * 4 * (kTabMaxSeq + 1)) != cudaSuccess)
-      return RELAXKV_ERR_CUDA;
-    attr_done[dev].store(1, std::memory_order_release);
-  }
   const TableArgs a = {n_seq, block_size, free_capacity, table_width, (long long)table_stride, (long long)n_rows, seq_len, new_len, seq_base, n_free,
                        free_blocks, block_table, seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot};
-  // One block per SM at most: more of them repeat the sums for less than they bring (452 K rows of 1600 sequences: 12.1 us with blocks of 512
-  // threads and two to an SM, 11.8 so; a million rows of 4096 sequences 17.9 with 512 threads, 14.0 so; few rows make no difference).
-  const long long blocks = std::max<long long>(1, std::min<long long>(sms, (n_rows + kTabThreads - 1) / kTabThreads));
-  return cuda_ok(launch_chained(block_tables_kernel, dim3((unsigned)blocks), kTabThreads, 4 * 4 * (size_t)(n_seq + 1), static_cast<cudaStream_t>(stream), a, st));
+  // One block per SM at most: more of them repeat the sums for less than they bring (452 K rows of 1600 sequences: 12.1 us with two of 512 threads, 11.8
+  // so; a million rows of 4096 17.9 and 14.0; 320 K rows of 64 5.3 so, 6.8 with four of 256).  Few rows: a block for the sums, as small as the sequences
+  // allow (graph replay, 64 sequences of a token each: 2.9 us with 256 threads, 3.9 with 1024; 500 of four tokens 5.2 with 512, 6.4).
+  const int threads = n_rows > 256LL * sms || n_seq > 1024 ? 1024 : n_seq > 256 ? 512 : 256;
+  auto kern = threads == 256 ? block_tables_kernel<256, 1> : threads == 512 ? block_tables_kernel<512, 2> : block_tables_kernel<1024, 4>;
+  const size_t smem = 4 * 4 * (size_t)(n_seq + 1);
+  if (threads == 1024) {                                 // (the others stay below what a launch may have without asking)
+    static std::atomic<int> attr_done[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RELAXKV_ERR_CUDA;
+    if (!attr_done[dev].load(std::memory_order_acquire)) {
+      if (cudaFuncSetAttribute(block_tables_kernel<1024, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * 4 * (kTabMaxSeq + 1)) != cudaSuccess)
+        return RELAXKV_ERR_CUDA;
+      attr_done[dev].store(1, std::memory_order_release);
+    }
+  }
+  const long long blocks = std::max<long long>(1, std::min<long long>(sms, (n_rows + threads - 1) / threads));
+  return cuda_ok(launch_chained(kern, dim3((unsigned)blocks), (unsigned)threads, smem, static_cast<cudaStream_t>(stream), a, st));
 }

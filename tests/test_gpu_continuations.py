@@ -61,7 +61,8 @@ def random_state(rng, n, bs, longest, width=None):
 
 
 @pytest.mark.parametrize("n,bs,longest,most,seed", [(1, 16, 0, 1, 0), (1, 16, 100, 1, 1), (5, 128, 300, 3, 2), (64, 16, 900, 1, 3), (33, 32, 77, 90, 4),
-                                                    (777, 16, 200, 40, 5), (4096, 64, 500, 9, 6)])
+                                                    (777, 16, 200, 40, 5), (4096, 64, 500, 9, 6),
+                                                    (120, 128, 100, 1000, 7), (256, 32, 60, 2, 8), (257, 32, 60, 2, 9), (1025, 16, 40, 3, 10)])
 def test_block_tables(n, bs, longest, most, seed):
     rng = np.random.default_rng(seed)
     lens, table, free = random_state(rng, n, bs, longest)
