@@ -79,9 +79,9 @@ class Continuations:
     def _blocks(self, tokens: int) -> int:
         return -(-tokens // self.block_size)
 
-    def begin(self, new: Sequence[int], stream=None) -> int:
+    def begin(self, new: Sequence[int]) -> int:
         """Begins a step: new[i] tokens of sequence i follow (0: it waits, -1: it ends and gives its blocks back).  Block tables, positions and
-        slots of the rows are made on the device; the rows are those of the sequences in order.  Returns their number."""
+        slots of the rows are made on the device, on the current stream; the rows are those of the sequences in order.  Returns their number."""
         new = [int(x) for x in new]
         if len(new) != self.n_seq or any(n < -1 for n in new):
             raise ValueError(f"a step of {self.n_seq} sequences takes as many counts, -1 or more each")
@@ -102,7 +102,7 @@ class Continuations:
             self._new[key] = torch.tensor(new, dtype=torch.int32, device=self.device)
         B.relaxkv_build_block_tables(self.block_size, self._len[0], self._new[key], self.base, self.free, self._n_free[0], self.table,
                                      self._len[1], self._n_free[1], self.row_cu, self.row_seq[:rows], self.row_pos[:rows],
-                                     self.row_len[:rows], self.row_slot[:rows], stream=stream)
+                                     self.row_len[:rows], self.row_slot[:rows])
         self._len.reverse()
         self._n_free.reverse()
         self.lens, self.n_free, self.n_rows = lens, n_free, rows

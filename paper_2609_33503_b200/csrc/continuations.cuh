@@ -96,7 +96,8 @@ struct ContWs { size_t part_o, part_lse, scores, total; };
 inline ContWs cont_ws(const relaxkv_shape* s, int64_t n_rows, int block_size) {
   ContWs w{};
   size_t a = 0;
-  const size_t row_slots = (size_t)std::max<int64_t>(1, n_rows) * cont_slots(n_rows);
+  // (the most that this many rows or fewer can ask for)
+  const size_t row_slots = (size_t)std::min<int64_t>(std::max<int64_t>(kContRowSlots, 4 * n_rows), kContSlotsMost * std::max<int64_t>(1, n_rows));
   w.part_o = a; a = align_up(a + row_slots * s->n_q_heads * s->head_dim * 4, 256);
   w.part_lse = a; a = align_up(a + row_slots * s->n_q_heads * 4, 256);
   w.total = a;

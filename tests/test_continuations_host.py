@@ -191,3 +191,11 @@ def test_how_keys_are_cut(tmp_path):
     subprocess.check_call([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-I", CSRC, str(src), "-o", str(exe)])
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_the_room_of_a_step_holds_every_smaller_one():
+    s, before = B.Shape(4, 2, 64, [1000]), 0
+    for n in list(range(0, 1200)) + [4095, 4096, 4097, 20000]:
+        nbytes = B.relaxkv_continuation_workspace_bytes(s, n, 0)
+        assert nbytes >= before, n
+        before = nbytes

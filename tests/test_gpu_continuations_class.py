@@ -66,6 +66,27 @@ def test_question_and_answers_match_the_query_pass(n_select):
     assert c.lens == [q + 3 for q in qn] == c._len[0].tolist() and c._n_free[0].tolist() == [c.n_free]
 
 
+def test_a_step_of_fewer_rows_fits_the_room_of_the_largest():
+    """Steps of every size that the object was made for, on a stream of their own as well."""
+    from paper_2609_33503_b200.continuations import Continuations
+    ctx = (200,)
+    weights, caches = setup(ctx, 0)
+    c = Continuations(H, HKV, D, ctx, (1,), L, BLK, n_blocks=16, max_len=256, block_size=16, max_rows=100)
+    for n in (100, 1, 64):
+        x = rnd(n, BLK.hidden, seed=n)
+        c.begin([-1])
+        assert c.begin([n]) == n
+        want = c.run(x, weights, caches).clone()
+        c.begin([-1])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            assert c.begin([n]) == n
+            got = c.run(x, weights, caches)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want) and status() == B().OK
+
+
 def test_samples_do_not_disturb_each_other():
     """Four samples of two contexts: the same tokens give the same rows whatever the others do, through ends, waits and blocks used again."""
     from paper_2609_33503_b200.continuations import Continuations
