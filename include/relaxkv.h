@@ -534,8 +534,9 @@ relaxkv_status relaxkv_qk_norm_rope_append_paged(
  * A context is read once for all its rows, whatever their number.  cache may be NULL where every context is empty, store NULL where max_len is 0.
  * A row that sees no key at all gets zeros and lse = -inf.
  *   q, out  device bf16 [n_rows, H, D] (16-byte aligned); lse_out NULL or device fp32 [H, n_rows]
- * Rows with row_seq -1 are left alone.  Reported and left alone: row_seq or row_len out of range, rows of a context above h_max_rows.  A block
- * number out of range is reported, its tokens are passed over.
+ * Rows with row_seq -1 are left alone.  Reported and left alone: row_seq or row_len out of range, rows of a context above h_max_rows, rows that
+ * row_cu does not count among those of their sequence's context.  A block number out of range is reported, its tokens are passed over.
+ * T_b, max_len and the cache rows that a context spans: up to 2^31 - 256 tokens, more is refused.
  */
 relaxkv_status relaxkv_shared_prefix_attention(
     const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store, const relaxkv_continuation_rows* rows,
