@@ -320,8 +320,8 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hd = (int)(blockIdx.x % a.Hkv);
   const long long row = blockIdx.x / a.Hkv;
-  // (No early call for the next kernel: the attention's clusters, placed while these blocks are still there, ran 6 us longer, 29.4 / 35.8 for a
-  // pass over four rows of 32 K.)
+  // (No early call for the next kernel: the attention's clusters cannot come to the SMs of these blocks, whose shared memory is set up otherwise, and
+  // crowd onto the rest: 36.7 us for a pass over four rows of 32 K.  With the same set-up for all kernels 29.5, like this 29.0.)
   griddep_wait();
   const int seq = a.row_seq[row];
   if (seq == -1) return;
