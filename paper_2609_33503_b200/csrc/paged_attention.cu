@@ -116,7 +116,21 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tm_ck, const __grid_c
   const int ctx_sub = a.ctx_block / ctx_box, page_sub = a.page / page_box;             // boxes of a block
   const int ctx_per = kTile / ctx_box, page_per = kTile / page_box;              // boxes of a tile
   const int ctx_len = ct.ctx_len[rc.ctx], ctx_blocks = (int)(((long long)ctx_len + a.ctx_block - 1) / a.ctx_block);
-  const int listed = a.ctx_keys == CTX_KEYS_NONE || ctx_len == 0 ? 0 : a.ctx_keys == CTX_KEYS_ALL ? ctx_blocks : a.n_select;      // blocks
+  int listed = a.ctx_keys == CTX_KEYS_NONE || ctx_len == 0 ? 0 : a.ctx_keys == CTX_KEYS_ALL ? ctx_blocks : a.n_select;      // blocks
+  if (live && listed > ctx_blocks) {                    // a list longer than its context ends with entries that are none: only up to the last one that is
+    const int* list = a.lists + (row * a.Hkv + hd) * a.n_select;
+    for (bool any = false; listed > 0 && !any;) {
+      int id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) id[u] = listed > 32 * u + lane ? list[listed - 1 - 32 * u - lane] : -1;
+#pragma unroll
+      for (int u = 0; u < 4 && !any; ++u) {
+        const uint32_t some = __ballot_sync(0xffffffffu, id[u] != -1);
+        any = some != 0;
+        listed -= any ? __ffs((int)some) - 1 : min(listed, 32);
+      }
+    }
+  }
   const int n_ctx = (listed * ctx_sub + ctx_per - 1) / ctx_per;
   const int n_tiles = live ? n_ctx + (rc.len + kTile - 1) / kTile : 0;
   const int per = (n_tiles + a.n_splits - 1) / a.n_splits;
@@ -561,7 +575,7 @@ relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_
   const int D = shape->head_dim;
   const int sms = sm_count_of_current_device();
   if (sms <= 0) return RELAXKV_ERR_CUDA;
-  const int warps = a.n_splits == 1 ? paged_warps(a.n_rows * a.Hkv, (long long)a.n_select * a.ctx_block + a.max_len, sms) : 4;
+  const int warps = a.n_splits == 1 ? paged_warps(a.n_rows * a.Hkv, (long long)a.listed_most * a.ctx_block + a.max_len, sms) : 4;
   CUtensorMap maps[4] = {};
   if (a.ctx_keys != CTX_KEYS_NONE) {
     long long tokens = 0;

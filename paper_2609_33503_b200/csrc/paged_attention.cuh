@@ -17,6 +17,7 @@ struct PagedAttnArgs {
   const int *row_seq, *row_len, *row_cu, *table, *lists;
   long long table_stride, n_rows;
   int table_width, max_len, n_select, n_blocks;
+  int listed_most;                     // entries of a list that are blocks, at most
   int H, Hkv, n_seq;
   int ctx_keys;                        // ContextKeys
   int ctx_block, page;                 // tokens of a context block and of a block of the store

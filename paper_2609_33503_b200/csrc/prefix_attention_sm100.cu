@@ -524,7 +524,9 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   for (int b = 0; b < ct.n_req; ++b) any_ctx |= ct.ctx_len[b] > 0;
   a.ctx_keys = any_ctx ? CTX_KEYS_LISTED : CTX_KEYS_NONE;
   a.lists = blocks; a.n_select = n_select; a.ctx_block = block_size;
-  const long long tiles = ((long long)n_select * block_size + 63) / 64 + (a.max_len + 63) / 64;
+  for (int b = 0; b < ct.n_req; ++b)
+    if (ct.max_rows[b] > 0) a.listed_most = std::max(a.listed_most, (int)std::min<long long>(n_select, ((long long)ct.ctx_len[b] + block_size - 1) / block_size));
+  const long long tiles = ((long long)a.listed_most * block_size + 63) / 64 + (a.max_len + 63) / 64;
   a.n_splits = paged_cluster(a.n_rows * a.Hkv, tiles, sms, kPagCluster);
   a.cluster = a.n_splits > 1;
   if (a.n_splits == 0) a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
