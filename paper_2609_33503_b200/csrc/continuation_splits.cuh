@@ -20,11 +20,11 @@ inline int paged_cluster(long long items, long long tiles, int sms, int most) {
 // Consumer warps (and sixteenths of a tile's keys) of a block that streams a row's keys, listed and own, for launches of one piece per row.  A block
 // takes some 7 us whatever it reads, so launches of several turns of them are better off with more and smaller ones: 6 blocks of one warp to an SM, 4
 // of two or 2 of four.  (row, KV head) pairs, keys up to: 512, 16: 18.3 us with one warp, 18.5 two, 23.4 four; 512, 600: 43.8 / 35.5 / 38.7; 1024, 256:
-// 38.7 / 39.5 / 46.3; 2048, 128: 48 / 54 / 69; 2048, 600: 89.3 / 87.7 / 96.2; 512, 1024: - / 81.5 / 81.1; 320, 256: 27.3 / 22.9 / 22.5.  With listed blocks
+// 38.7 / 39.5 / 46.3; 2048, 128: 48 / 54 / 69; 2048, 600: 89.3 / 87.7 / 96.2; 512, 1024: - / 81.5 / 81.1; 320, 256: 27.3 / 22.9 / 22.5; 320, 128: 21.5 / 19.7 / 21.1.  With listed blocks
 // (selection included): 512, 164 34.4 / 32.7 / 36.0; 1200, 612 80.6 / 71.1 / 76.0; 1200, 2148 206 / 175 / 168.
 inline int paged_warps(long long items, long long keys, int sms) {
   if (items > 6LL * sms && keys <= 256) return 1;
-  return items > 3LL * sms && keys <= 640 ? 2 : 4;
+  return (items > 3LL * sms && keys <= 640) || (items > 2LL * sms && keys <= 128) ? 2 : 4;
 }
 
 constexpr double kPrefixStartTiles = 3.0;      // start and end of a block of the prefix kernel, in its 128-key tiles

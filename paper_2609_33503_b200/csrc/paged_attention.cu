@@ -568,6 +568,45 @@ static relaxkv_status launch_paged_d(int warps, const CUtensorMap* maps, const C
                     : warps == 2 ? launch_paged_g<D, 8, 2>(maps, ct, a, st, stream) : launch_paged_g<D, 8, 4>(maps, ct, a, st, stream);
 }
 
+template <int D, int GMAX>
+static int clusters_at_once(int n, int sms) {
+  static std::atomic<int> known[kMaxDevices][kPagCluster + 1];
+  int dev = 0;
+  const int guess = std::max(1, 2 * sms / n - sms / 16);
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return guess;
+  int k = known[dev][n].load(std::memory_order_acquire);
+  if (k > 0) return k;
+  using L = PagSmem<D, 4>;
+  auto kern = paged_attention_kernel<D, GMAX, 4>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(n * sms));
+  cfg.blockDim = L::kThreads;
+  cfg.dynamicSmemBytes = L::kDynamic;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&k, kern, &cfg) != cudaSuccess || k < 1) {
+    (void)cudaGetLastError();
+    k = guess;
+  }
+  known[dev][n].store(k, std::memory_order_release);
+  return k;
+}
+
+int cluster_that_fits(const relaxkv_shape* shape, int n, long long items) {
+  const int sms = std::max(1, sm_count_of_current_device());
+  const bool wide = shape->n_q_heads / shape->n_kv_heads > 8;
+  for (; n > 1; --n) {
+    const int room = shape->head_dim == 128 ? (wide ? clusters_at_once<128, 16>(n, sms) : clusters_at_once<128, 8>(n, sms))
+                                            : (wide ? clusters_at_once<64, 16>(n, sms) : clusters_at_once<64, 8>(n, sms));
+    if (items <= room) break;
+  }
+  return n;
+}
+
 relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
                                       const ContTable& ct, PagedAttnArgs a, cudaStream_t stream) {
   DeviceStatus* st = status_word();

@@ -76,6 +76,10 @@ __device__ __forceinline__ RowCheck check_row(const PagedAttnArgs& a, const Cont
   return r;
 }
 
+// The largest cluster of at most n blocks of which `items` run at once (of blocks of four consumer warps).  Clusters live within a GPC, so they fill the
+// GPU less than their blocks by themselves: 72 clusters of four are one more than fit, and took twice as long as 71.
+int cluster_that_fits(const relaxkv_shape* shape, int n, long long items);
+
 relaxkv_status launch_paged_attention(const relaxkv_shape* shape, const relaxkv_cache_view* cache, const relaxkv_paged_cache* store,
                                       const ContTable& ct, PagedAttnArgs a, cudaStream_t stream);
 // out = sum over the slots of w_s O_s / sum w_s, w_s = exp(lse_s - max)

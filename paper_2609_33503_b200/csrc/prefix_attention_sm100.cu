@@ -456,7 +456,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   if (a.n_rows * a.Hkv * kPagCluster <= 2LL * sms && all_tiles <= 12 * kPagCluster) {
     a.ctx_keys = longest > 0 ? CTX_KEYS_ALL : CTX_KEYS_NONE;
     a.ctx_block = 64;
-    a.n_splits = (int)std::max<long long>(1, std::min<long long>(kPagCluster, all_tiles / 2));
+    a.n_splits = cluster_that_fits(shape, (int)std::max<long long>(1, std::min<long long>(kPagCluster, all_tiles / 2)), a.n_rows * a.Hkv);
     a.cluster = a.n_splits > 1;
     a.n_slots = 1;
     return launch_paged_attention(shape, cache, store, ct, a, s);
@@ -466,7 +466,7 @@ extern "C" relaxkv_status relaxkv_shared_prefix_attention(
   // Up to eight pieces of a row's own keys are a cluster that merges them and the pieces of its context, too; more go through slots and the
   // merge behind.
   const long long own_tiles = ((long long)a.max_len + 63) / 64;
-  a.n_splits = own ? paged_cluster(a.n_rows * a.Hkv, own_tiles, sms, kPagCluster) : 0;
+  a.n_splits = own ? cluster_that_fits(shape, paged_cluster(a.n_rows * a.Hkv, own_tiles, sms, kPagCluster), a.n_rows * a.Hkv) : 0;
   a.cluster = a.n_splits > 0;
   const int own_pieces = !own || a.cluster ? 0 : paged_pieces(a.n_rows * a.Hkv, own_tiles, sms, std::max(1, slots / 4));
   int n_tiles[kMaxReqInline], row_tiles[kMaxReqInline], most = 0;
@@ -527,7 +527,7 @@ extern "C" relaxkv_status relaxkv_block_sparse_attention(
   for (int b = 0; b < ct.n_req; ++b)
     if (ct.max_rows[b] > 0) a.listed_most = std::max(a.listed_most, (int)std::min<long long>(n_select, ((long long)ct.ctx_len[b] + block_size - 1) / block_size));
   const long long tiles = ((long long)a.listed_most * block_size + 63) / 64 + (a.max_len + 63) / 64;
-  a.n_splits = paged_cluster(a.n_rows * a.Hkv, tiles, sms, kPagCluster);
+  a.n_splits = cluster_that_fits(shape, paged_cluster(a.n_rows * a.Hkv, tiles, sms, kPagCluster), a.n_rows * a.Hkv);
   a.cluster = a.n_splits > 1;
   if (a.n_splits == 0) a.n_splits = paged_pieces(a.n_rows * a.Hkv, tiles, sms, cont_slots(a.n_rows));
   a.slot0 = 0;
