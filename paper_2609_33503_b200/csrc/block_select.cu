@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kScoWarps * 32)
 block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ SelectArgs a, DeviceStatus* st) {
   constexpr int kSteps = 2 * D / 16;                                // MMAs of a product
   constexpr int kHeads = 16 / ROWS;                                 // fragment rows of a row of the step
-  __shared__ __align__(16) uint32_t q_s[kScoPass][16][D + 8];       // [tile][fragment row][step][lane of four] four halves of (q+ | q-)
+  __shared__ __align__(16) uint32_t q_s[kScoPass][16][D + 8];       // [tile][fragment row][step, in an order][lane of four] four halves of (q+ | q-)
   __shared__ float sq_s[kScoPass][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const int G = a.H / a.Hkv;
@@ -243,7 +243,7 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
         pos[u] = h2_bits(__hmin2(__hmax2(v, zero), most));
         neg[u] = h2_bits(__hmax2(__hmin2(v, zero), least));
       }
-      const int at = ((ql & 3) * 2 * kVec + e) * 4 + (ql >> 2);            // [step][lane of the four]
+      const int at = (4 * e + (ql & 3)) * 4 + (ql >> 2);                  // step 2 kVec (ql & 3) + e, lane of the four: steps apart by banks
       row[at] = make_uint2(pos[0], pos[1]);
       row[at + 2] = make_uint2(neg[0], neg[1]);
     }
@@ -261,8 +261,9 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
     }
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const uint2 qa = *reinterpret_cast<const uint2*>(&q_s[tile][gid][8 * s + 2 * tig]);
-      const uint2 qb = *reinterpret_cast<const uint2*>(&q_s[tile][gid + 8][8 * s + 2 * tig]);
+      const int at = 8 * (s % (2 * kVec) * 4 + s / (2 * kVec)) + 2 * tig;
+      const uint2 qa = *reinterpret_cast<const uint2*>(&q_s[tile][gid][at]);
+      const uint2 qb = *reinterpret_cast<const uint2*>(&q_s[tile][gid + 8][at]);
 #pragma unroll
       for (int c = 0; c < kScoCols; ++c) mma_f16_16816(acc[c][s & 1], qa.x, qb.x, qa.y, qb.y, bd[c][2 * s], bd[c][2 * s + 1]);
     }
