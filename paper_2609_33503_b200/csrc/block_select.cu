@@ -8,10 +8,10 @@
 // 32 bits: rows are the heads of one, two or four rows of the step, columns eight blocks.  All are whole numbers below 2^24, so the scores, and with them
 // the lists, do not depend on the order of anything; it may be any as long as both sides agree, so a lane takes D / 2 bytes of its block in
 // 16-byte loads and the queries are laid out to match.  Up to four tiles of rows go to a block, so that rows and context blocks both spread
-// over the SMs: with all rows in one block, 64 rows of 40 / 8 heads over 938 blocks took 33 us, so 27.
+// over the SMs: with all rows in one block, 64 rows of 40 / 8 heads over 938 blocks took 33 us, so 27 (24.5 by now).
 // Selection: one block per (row, KV head); counts of digits find the lowest selected score, then every warp writes its own range's blocks in
-// order.  Both launches: 4 rows of 40 / 8 heads, 512 blocks 8.3 us, 16 rows of 32 / 8 heads in two contexts of some 2000 blocks 14.1: latencies
-// (row -> query -> product -> score -> counts), not bytes; 64 rows in one context of 8192 blocks 89.
+// order.  Both launches: 4 rows of 40 / 8 heads, 512 blocks 8.0 us, 16 rows of 32 / 8 heads in two contexts of some 2000 blocks 13.6: latencies
+// (row -> query -> product -> score -> counts), not bytes; 64 rows in one context of 8192 blocks 81.
 #include "continuations.cuh"
 #include <algorithm>
 #include <cuda_fp16.h>
@@ -267,29 +267,40 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
 #pragma unroll
       for (int c = 0; c < kScoCols; ++c) mma_f16_16816(acc[c][s & 1], qa.x, qb.x, qa.y, qb.y, bd[c][2 * s], bd[c][2 * s + 1]);
     }
-    // the largest over the heads of a row: fragment rows lie 4 lanes apart
-    float best[2][2 * kScoCols];
+    // the largest over the heads of a row, whose fragment rows lie 4 lanes apart: of the values (half of the fragment rows, column tile, column)
+    // a lane keeps one side of each in turn and hands over the other
+    static_assert(kScoCols == 2, "two column tiles");
+    float v[8];
     const float s0 = sq_s[tile][gid], s1 = sq_s[tile][gid + 8];
 #pragma unroll
-    for (int e = 0; e < 2 * kScoCols; ++e) {
+    for (int e = 0; e < 4; ++e) {
       const float *even = acc[e >> 1][0], *odd = acc[e >> 1][1];
-      best[0][e] = s0 > 0.f ? (even[e & 1] + odd[e & 1]) * s0 : -INFINITY;
-      best[1][e] = s1 > 0.f ? (even[2 + (e & 1)] + odd[2 + (e & 1)]) * s1 : -INFINITY;
-      if (ROWS == 1) best[0][e] = fmaxf(best[0][e], best[1][e]);
-#pragma unroll
-      for (int o = 4; o < 4 * min(kHeads, 8); o <<= 1) {
-        best[0][e] = fmaxf(best[0][e], __shfl_xor_sync(0xffffffffu, best[0][e], o));
-        if (ROWS > 1) best[1][e] = fmaxf(best[1][e], __shfl_xor_sync(0xffffffffu, best[1][e], o));
-      }
+      v[e] = s0 > 0.f ? (even[e & 1] + odd[e & 1]) * s0 : -INFINITY;
+      v[4 + e] = s1 > 0.f ? (even[2 + (e & 1)] + odd[2 + (e & 1)]) * s1 : -INFINITY;
+      if (ROWS == 1) v[e] = fmaxf(v[e], v[4 + e]);
     }
-    // of the fragment rows that hold a row's result, one writes it: gid from the first half, gid + 1 from the second
-    const int half = gid % min(kHeads, 8), r = (p0 + tile) * ROWS + (ROWS == 4 ? 2 * half + (gid >> 2) : half);
-    if (half < min(ROWS, 2) && r < rr.n) {
-      float* o = a.scores + ((rr.first + r) * a.Hkv + hd) * a.most;
+    int o = 4;
+    auto halve = [&](int n) {                                            // of 2 n values, this lane keeps n
+      const bool up = (lane & o) != 0;
 #pragma unroll
-      for (int e = 0; e < 2 * kScoCols; ++e) {
-        const int xx = x0 + 8 * (e >> 1) + 2 * tig + (e & 1);
-        if (xx < nb) o[xx] = (half ? best[1][e] : best[0][e]) * sb[e >> 1][e & 1] + 0.f;   // (+ 0: one zero, not two)
+      for (int e = 0; e < n; ++e) {
+        const float keep = up ? v[n + e] : v[e], give = up ? v[e] : v[n + e];
+        v[e] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+      }
+      o <<= 1;
+    };
+    if (ROWS > 1) halve(4);
+    halve(2);
+    if (ROWS < 4) halve(1);
+    if (ROWS == 1) v[0] = fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
+    const int half = ROWS > 1 ? gid & 1 : 0, c = ROWS > 1 ? (gid >> 1) & 1 : gid & 1, r = (p0 + tile) * ROWS + (ROWS == 4 ? 2 * half + (gid >> 2) : half);
+    if (r < rr.n && (ROWS > 1 || gid < 4)) {
+      float* out = a.scores + ((rr.first + r) * a.Hkv + hd) * a.most;
+#pragma unroll
+      for (int e = 0; e < (ROWS == 4 ? 2 : 1); ++e) {
+        const int col = ROWS == 4 ? e : ROWS == 2 ? gid >> 2 : (gid >> 1) & 1, xx = x0 + 8 * c + 2 * tig + col;
+        const float scale = c ? (col ? sb[1][1] : sb[1][0]) : (col ? sb[0][1] : sb[0][0]);
+        if (xx < nb) out[xx] = v[e] * scale + 0.f;                        // (+ 0: one zero, not two)
       }
     }
   }
