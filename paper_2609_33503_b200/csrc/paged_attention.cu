@@ -5,7 +5,7 @@
 // head, piece of the row's keys); a producer warp streams 64-key tiles through a ring in shared memory, one TMA box per block of the cache (its
 // lanes look the block numbers up a tile ahead and each issues its own box, K and V), and four consumer warps take 16 keys of a tile each:
 // S = Q K^T and O += P V as warp-level MMAs whose 16 rows are the heads (a 128-row tcgen05 tile would be 3 to 6 % full), softmax on the
-// fragments.  16 keys never straddle a block, so a chunk's valid keys are one number.  Tiles of 64 keys and three stages leave room for two
+// fragments (weights are rounded to bf16 for the product with V, their sums are of the unrounded ones in fp32).  16 keys never straddle a block, so a chunk's valid keys are one number.  Tiles of 64 keys and three stages leave room for two
 // blocks per SM, which hide each other's starts; many rows of few keys go to blocks of two consumer warps or one, with tiles as much smaller (the
 // rule and its figures: continuation_splits.cuh).
 // A row's pieces merge among themselves where a cluster of up to eight blocks is enough (four rows of 32 K, 64 blocks each: 15.9 us, 18.1 with a merge

@@ -34,7 +34,8 @@ constexpr int kPreThreads = 384;                      // two groups of four soft
 constexpr float kPreRescale = 8.0f;                   // log2 units: O is rescaled only when the row maximum grew by more
 constexpr float kLog2ePre = 1.4426950408889634f, kLn2Pre = 0.6931471805599453f;
 
-// p = 2^(s * scale - m) of a row's 128 keys as bf16 pairs, and their sum.
+// p = 2^(s * scale - m) of a row's 128 keys as bf16 pairs, and their sum.  bf16 is what the product with V takes beside bf16 values: its rounding
+// errors (2^-9 of a weight, of either sign) average out over the keys; the sum is that of the unrounded weights, in fp32.
 __device__ __forceinline__ float prefix_exponentials(const uint32_t* s, uint32_t* pk, float scale, float neg_m) {
   float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
 #pragma unroll
