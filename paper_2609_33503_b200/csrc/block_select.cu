@@ -12,6 +12,7 @@
 // Selection: one block per (row, KV head); counts of digits find the lowest selected score, then every warp writes its own range's blocks in
 // order.  Both launches: 4 rows of 40 / 8 heads, 512 blocks 8.0 us, 16 rows of 32 / 8 heads in two contexts of some 2000 blocks 13.6: latencies
 // (row -> query -> product -> score -> counts), not bytes; 64 rows in one context of 8192 blocks 81.
+#include "continuation_splits.cuh"
 #include "continuations.cuh"
 #include <algorithm>
 #include <cuda_fp16.h>
@@ -141,6 +142,7 @@ struct SelectArgs {
   int* out;                            // [n_rows, H_kv, n_select]
   long long n_rows;
   int most, H, Hkv, n_seq, block_size, n_select, n_first, n_last;
+  int kept;                            // scores that a block of the selection has shared memory for
 };
 
 // Rows of context b in the step; n < 0: more than the host's bounds.
@@ -308,7 +310,7 @@ block_score_kernel(const __grid_constant__ ContTable ct, const __grid_constant__
 
 // ---- the n_select highest scores of a (row, KV head) ------------------------------------------------------------------------------
 
-constexpr int kTopKept = 8192;          // scores that a block keeps in shared memory; more are read again by every pass
+constexpr int kTopKept = 8192;          // scores that a block keeps in shared memory, at most; more are read again by every pass
 
 // Order-preserving key of a score (no NaN: scores are products of whole numbers and powers of two).
 __device__ __forceinline__ uint32_t score_key(float f) {
@@ -352,7 +354,7 @@ block_topk_kernel(const __grid_constant__ ContTable ct, const __grid_constant__ 
     return;
   }
   const int x0 = a.n_first, x1 = nb - a.n_last;                                  // blocks that compete: [x0, x1), more than are wanted
-  const bool kept = nb <= kTopKept;
+  const bool kept = nb <= a.kept;                                                // (the launch's shared memory: contexts of a call differ)
   uint32_t lo = 0xffffffffu, hi = 0u;
   for (int i0 = x0 + tid; i0 < x1; i0 += U * THREADS) {
     float v[U];
@@ -517,7 +519,8 @@ extern "C" relaxkv_status relaxkv_select_blocks(
     rc = cuda_ok(launch_chained(kern, dim3((unsigned)ct.tile_cu[ct.n_req], (unsigned)a.Hkv), kScoWarps * 32, 0, s, ct, a, st));
     if (rc != RELAXKV_OK) return rc;
   }
-  const size_t smem = a.most <= kTopKept ? (size_t)a.most * 4 : 0;
+  a.kept = kept_scores(ct.blk_cu, ct.n_req, n_select, kTopKept);
+  const size_t smem = (size_t)a.kept * 4;
   const bool many = a.most > 1024;
   auto kern = many ? block_topk_kernel<512> : block_topk_kernel<256>;
   return cuda_ok(launch_chained(kern, dim3((unsigned)(a.n_rows * a.Hkv)), many ? 512 : 256, smem, s, ct, a, st));

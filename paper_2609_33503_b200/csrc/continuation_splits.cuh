@@ -1,4 +1,4 @@
-// Internal: how the attention over continuations cuts keys into pieces (host only, no CUDA).
+// Internal: how the attention over continuations cuts keys into pieces, and what its launches need (host only, no CUDA).
 #pragma once
 #include <algorithm>
 
@@ -25,6 +25,17 @@ inline int paged_cluster(long long items, long long tiles, int sms, int most) {
 inline int paged_warps(long long items, long long keys, int sms) {
   if (items > 6LL * sms && keys <= 256) return 1;
   return (items > 3LL * sms && keys <= 640) || (items > 2LL * sms && keys <= 128) ? 2 : 4;
+}
+
+// Scores that a block of the selection needs room for, contexts of blocks [blk_cu[b], blk_cu[b+1]) in one call: the longest context that competes (has
+// more blocks than are selected) and whose scores are kept at all.  A longer one beside it takes none of that room, and must not take it away.
+inline int kept_scores(const int* blk_cu, int n, int n_select, int most) {
+  int kept = 0;
+  for (int b = 0; b < n; ++b) {
+    const int nb = blk_cu[b + 1] - blk_cu[b];
+    if (nb > n_select && nb <= most) kept = std::max(kept, nb);
+  }
+  return kept;
 }
 
 constexpr double kPrefixStartTiles = 3.0;      // start and end of a block of the prefix kernel, in its 128-key tiles

@@ -1,0 +1,28 @@
+"""Continuations on the GPU over ranges that meet in one call: contexts of very different length, logits and values of very different size."""
+import numpy as np
+import pytest
+import torch
+
+from tests import continuation_oracle as orc
+from tests.test_gpu_continuations import B, Step, f64, get_bounds, status
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("ctx", [(140000, 3000), (3000, 140000), (300, 131200, 0, 140000, 9000)])
+@pytest.mark.parametrize("n_select,n_first,n_last", [(9, 1, 2), (200, 0, 3), (3, 1, 2)])
+def test_selection_in_contexts_beside_one_of_very_many_blocks(ctx, n_select, n_first, n_last):
+    """140000 tokens in blocks of 16: more blocks than the selection keeps the scores of, beside contexts of fewer."""
+    b = B()
+    s = Step(2, 1, 64, list(ctx), [2] * len(ctx), 3, 1, 16, seed=21)
+    bounds, scale = get_bounds(s, 16)
+    n = len(s.row_seq)
+    lists = torch.full((n, 1, n_select), -9, dtype=torch.int32, device="cuda")
+    b.relaxkv_select_blocks(s.shape, 16, bounds, scale, s.rows(), s.q, n_first, n_last, lists, s.ws(16))
+    assert status() == b.OK
+    at = np.concatenate([[0], np.cumsum([-(-t // 16) for t in ctx])])
+    bi, sc, q = bounds.cpu().numpy().astype(np.int64), f64(scale), f64(s.q)
+    for r in range(n):
+        c = s.context_of(r)
+        want = orc.select(q[r], bi[at[c]:at[c + 1]], sc[at[c]:at[c + 1]], n_select, n_first, n_last)
+        assert np.array_equal(lists[r].cpu().numpy(), want), r
