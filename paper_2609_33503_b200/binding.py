@@ -160,7 +160,9 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _args(codes: str, *args):
     """The arguments of an entry point as its bound form takes them, one code each: p a tensor (or None), h host integers (or None), s a
-    ctypes structure, . a plain value.  The first call puts the native function in this one's place."""
+    ctypes structure, . a plain value.  # is a number of elements, not passed on: I, W, F and C behind it are tensors of int32, bfloat16, float32
+    or int8 that have to hold as many (ValueError); i, w, f and c have to be contiguous whatever their size.  The first call puts the native
+    function in this one's place."""
     global _args
     _args = _native().marshal
     return _args(codes, *args)
@@ -272,9 +274,14 @@ class PagedStore:
         return int(self.k.shape[1])
 
 
-def _table_layout(t: torch.Tensor):
-    """Width and row distance of a block table."""
+_INT32 = torch.int32
+
+
+def _table_layout(t: torch.Tensor, n_seq: int):
+    """Width and row distance of a block table of that many sequences."""
     n, width = t.shape
+    if n < n_seq or t.dtype is not _INT32:
+        raise ValueError(f"a block table of {n_seq} rows of int32 expected, not {n} of {t.dtype}")
     distance, one = t.stride()
     if one != 1 or (distance < width and n > 1):
         raise AssertionError("a block table's rows are contiguous and do not overlap")
@@ -292,7 +299,7 @@ class ContinuationRows:
             assert t is None or t.dtype == torch.int32
         assert len(max_rows) == len(seq_cu) - 1 and row_cu.numel() == seq_cu[-1] + 1 and row_cu.is_contiguous() and row_seq.is_contiguous()
         assert row_len is None or (row_len.is_contiguous() and row_len.numel() >= row_seq.numel())
-        assert block_table is None or (_table_layout(block_table) and block_table.shape[0] >= seq_cu[-1])
+        assert block_table is None or (block_table.shape[0] >= seq_cu[-1] and _table_layout(block_table, seq_cu[-1]))
         self._keep = (_i32(seq_cu), _i32(max_rows), row_cu, row_seq, row_len, block_table)
         self.c = _ContinuationRows()
         self.c.n_seq, self.c.n_rows, self.c.max_len = int(seq_cu[-1]), row_seq.numel(), int(max_len)
@@ -534,10 +541,11 @@ def relaxkv_build_block_tables(block_size: int, seq_len: torch.Tensor, new_len: 
                                n_free_out: torch.Tensor, row_cu: torch.Tensor, row_seq: torch.Tensor, row_pos: torch.Tensor,
                                row_len: torch.Tensor, row_slot: torch.Tensor, stream=None) -> None:
     """seq_len, new_len, seq_base [n_seq]; block_table [n_seq, width] (rows any distance apart); row_* [n_rows].  All int32."""
-    width, distance = _table_layout(block_table)
-    _check(lib().relaxkv_build_block_tables(*_args("..pppp.pp...ppppppp.", seq_len.numel(), int(block_size), seq_len, new_len, seq_base,
-                                                   free_blocks, free_blocks.numel(), n_free, block_table, width, distance, row_seq.numel(),
-                                                   seq_len_out, n_free_out, row_cu, row_seq, row_pos, row_len, row_slot, _stream(stream))),
+    n, n_rows, n_stack = seq_len.numel(), row_seq.numel(), free_blocks.numel()
+    width, distance = _table_layout(block_table, n)
+    _check(lib().relaxkv_build_block_tables(*_args("..#Iii#I.#Ip...#I#I#I#IIII.", n, int(block_size), n, seq_len, new_len, seq_base, n_stack,
+                                                   free_blocks, n_stack, 1, n_free, block_table, width, distance, n_rows, n, seq_len_out,
+                                                   1, n_free_out, n + 1, row_cu, n_rows, row_seq, row_pos, row_len, row_slot, _stream(stream))),
            "relaxkv_build_block_tables")
 
 
