@@ -266,7 +266,7 @@ class PagedStore:
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         assert k.dim() == 4 and k.stride(3) == 1 and k.dtype == torch.bfloat16
         assert v.shape == k.shape and v.stride() == k.stride() and v.dtype == torch.bfloat16
-        self.k, self.v = k, v
+        self.k, self.v, self.heads, self.dim = k, v, int(k.shape[2]), int(k.shape[3])
         self.c = _PagedCache(k.data_ptr(), v.data_ptr(), int(k.stride(0)), int(k.stride(1)), int(k.stride(2)), int(k.shape[1]), int(k.shape[0]))
 
     @property
@@ -554,9 +554,14 @@ def relaxkv_qk_norm_rope_append_paged(store: PagedStore, q: torch.Tensor, k: tor
                                       w_k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
     """q_out [n, H, D] = normed and rotated q (may be q); the store receives the normed and rotated k and v [n, H_kv, D] at `slots`."""
     n, heads, dim = q.shape
-    _check(lib().relaxkv_qk_norm_rope_append_paged(*_args("sppp....pp.pp.p.", store.c, q, k, v, n, heads, k.shape[1], dim, w_q_norm, w_k_norm,
-                                                          float(eps), positions, slots, float(theta), q_out, _stream(stream))),
-           "relaxkv_qk_norm_rope_append_paged")
+    kv_heads = k.shape[1]
+    if kv_heads > store.heads or dim != store.dim:
+        raise ValueError(f"{kv_heads} heads of {dim} for a store of {store.heads} heads of {store.dim}")
+    size = n * heads * dim
+    kv_size = n * kv_heads * dim
+    _check(lib().relaxkv_qk_norm_rope_append_paged(*_args("s#w#ww....#WW.#II.#W.", store.c, size, q, kv_size, k, v, n, heads, kv_heads, dim, dim,
+                                                          w_q_norm, w_k_norm, float(eps), n, positions, slots, float(theta), size, q_out,
+                                                          _stream(stream))), "relaxkv_qk_norm_rope_append_paged")
 
 
 def _optional(struct):

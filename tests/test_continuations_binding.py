@@ -67,3 +67,34 @@ def test_block_tables_take_what_they_took(calls):
     assert a[12:19] == tuple(t[k].data_ptr() for k in ("seq_len_out", "n_free_out", "row_cu", "row_seq", "row_pos", "row_len", "row_slot"))
     B.relaxkv_build_block_tables(16, **tables(**{k: i32(0) for k in ("row_seq", "row_pos", "row_len", "row_slot")}), stream=0)
     assert calls[1][1][11] == 0
+
+
+def append(**kw):
+    n, H, Hkv, D = 5, 8, 2, 64
+    a = dict(store=B.PagedStore(bf(4, 16, Hkv, D), bf(4, 16, Hkv, D)), q=bf(n, H, D), k=bf(n, Hkv, D), v=bf(n, Hkv, D), positions=i32(n), slots=i32(n), theta=1e4,
+             q_out=bf(n, H, D))
+    a.update(kw)
+    return a
+
+
+APPEND = [dict(store=B.PagedStore(bf(4, 16, 1, 64), bf(4, 16, 1, 64))), dict(store=B.PagedStore(bf(4, 16, 2, 128), bf(4, 16, 2, 128))),
+          dict(store=B.PagedStore(bf(4, 16, 4, 32), bf(4, 16, 4, 32))), dict(k=bf(5, 3, 64)), dict(k=bf(4, 2, 64)), dict(v=bf(5, 1, 64)), dict(v=bf(4, 2, 64)),
+          dict(q=bf(5, 12, 64)[:, :8]), dict(q=bf(5, 8, 64).float()), dict(k=bf(5, 12, 64)[:, 8:10]), dict(v=bf(5, 12, 64)[:, 10:]), dict(q_out=bf(4, 8, 64)),
+          dict(positions=i32(4)), dict(slots=i32(4)), dict(slots=torch.zeros(5, dtype=torch.int64)), dict(positions=torch.zeros(5, dtype=torch.int64)),
+          dict(w_q_norm=bf(32), w_k_norm=bf(64)), dict(w_q_norm=bf(64), w_k_norm=bf(64).float())]
+
+
+@pytest.mark.parametrize("i", range(len(APPEND)))
+def test_append_refuses_what_does_not_fit_the_rows_or_the_store(calls, i):
+    with pytest.raises(ValueError):
+        B.relaxkv_qk_norm_rope_append_paged(**append(**APPEND[i]), stream=0)
+    assert not calls
+
+
+def test_append_takes_what_it_took(calls):
+    for kw in (dict(), dict(k=bf(9, 1, 64)), dict(w_q_norm=bf(64), w_k_norm=bf(64)), dict(slots=i32(9)), dict(q_out=bf(9, 8, 64))):
+        a = append(**kw)
+        B.relaxkv_qk_norm_rope_append_paged(**a, stream=0)
+        got = calls[-1][1]
+        assert got[1:8] == (a["q"].data_ptr(), a["k"].data_ptr(), a["v"].data_ptr(), 5, 8, a["k"].shape[1], 64) and len(got) == 16
+        assert got[11:13] == (a["positions"].data_ptr(), a["slots"].data_ptr()) and got[14] == a["q_out"].data_ptr()
