@@ -8,6 +8,7 @@ fails with an error.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import List, Optional, Sequence
 
@@ -219,6 +220,8 @@ class Shape:
         self.c.h_ctx_len = ctypes.cast(self._ctx, ctypes.POINTER(ctypes.c_int32))
         self.c.h_q_len = ctypes.cast(self._q, ctypes.POINTER(ctypes.c_int32)) if self._q is not None else None
         self.c.softmax_scale = float(softmax_scale if softmax_scale is not None else head_dim ** -0.5)
+        self.heads, self.kv_heads, self.dim = int(n_q_heads), int(n_kv_heads), int(head_dim)
+        self._blocks = {}
         self._tuning = None
         self.set_tuning(attention_ctx_splits, attention_persistent, attention_grid_blocks)
 
@@ -235,6 +238,13 @@ class Shape:
     def n_req(self) -> int:
         return len(self.ctx_lens)
 
+    def context_blocks(self, block_size: int) -> int:
+        """Blocks of that many tokens in all contexts."""
+        n = self._blocks.get(block_size)
+        if n is None:
+            n = self._blocks[block_size] = sum(-(-t // block_size) for t in self._ctx)
+        return n
+
     def ref(self):
         return ctypes.byref(self.c)
 
@@ -249,6 +259,8 @@ class CacheView:
             assert v.shape == k.shape and v.stride() == k.stride() and v.dtype == torch.bfloat16
         self.k, self.v = k, v
         self._off = (ctypes.c_int64 * len(req_token_offsets))(*[int(x) for x in req_token_offsets])
+        self.heads, self.dim = int(k.shape[1]), int(k.shape[2])
+        self.room = [max(0, int(k.shape[0]) - x) for x in self._off]       # tokens behind each request's start
         self.c = _CacheView()
         self.c.k = k.data_ptr()
         self.c.v = v.data_ptr() if v is not None else None
@@ -301,6 +313,7 @@ class ContinuationRows:
         assert row_len is None or (row_len.is_contiguous() and row_len.numel() >= row_seq.numel())
         assert block_table is None or (block_table.shape[0] >= seq_cu[-1] and _table_layout(block_table, seq_cu[-1]))
         self._keep = (_i32(seq_cu), _i32(max_rows), row_cu, row_seq, row_len, block_table)
+        self.n_req, self.n_rows = len(max_rows), row_seq.numel()
         self.c = _ContinuationRows()
         self.c.n_seq, self.c.n_rows, self.c.max_len = int(seq_cu[-1]), row_seq.numel(), int(max_len)
         if block_table is not None:
@@ -564,6 +577,19 @@ def relaxkv_qk_norm_rope_append_paged(store: PagedStore, q: torch.Tensor, k: tor
                                                           _stream(stream))), "relaxkv_qk_norm_rope_append_paged")
 
 
+def _fit(shape: Shape, cache: Optional[CacheView], store: Optional[PagedStore], rows: Optional[ContinuationRows]) -> None:
+    """Whether a call's cache, store and rows hold what its shape says that they do."""
+    if cache is not None:
+        if cache.dim != shape.dim or cache.heads < shape.kv_heads:
+            raise ValueError(f"a cache of {cache.heads} heads of {cache.dim} for a shape of {shape.kv_heads} heads of {shape.dim}")
+        if len(cache.room) < len(shape.ctx_lens) or not all(map(operator.le, shape.ctx_lens, cache.room)):
+            raise ValueError(f"contexts of {shape.ctx_lens} tokens in a cache with room for {cache.room}")
+    if store is not None and (store.dim != shape.dim or store.heads < shape.kv_heads):
+        raise ValueError(f"a store of {store.heads} heads of {store.dim} for a shape of {shape.kv_heads} heads of {shape.dim}")
+    if rows is not None and rows.n_req != len(shape.ctx_lens):
+        raise ValueError(f"rows over {rows.n_req} contexts for a shape of {len(shape.ctx_lens)}")
+
+
 def _optional(struct):
     return None if struct is None else struct.c
 
@@ -577,23 +603,35 @@ def relaxkv_shared_prefix_attention(shape: Shape, cache: Optional[CacheView], st
                                     q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
                                     stream=None) -> None:
     """cache: the contexts (None where all are empty); store: the sequences' own tokens (None where rows.max_len is 0)."""
-    _check(lib().relaxkv_shared_prefix_attention(*_args(_codes("s", cache, store, "spppp.."), shape.c, _optional(cache), _optional(store),
-                                                        rows.c, q, out, lse_out, workspace, workspace.nbytes, _stream(stream))),
-           "relaxkv_shared_prefix_attention")
+    _fit(shape, cache, store, rows)
+    heads = rows.n_rows * shape.heads
+    _check(lib().relaxkv_shared_prefix_attention(*_args(_codes("s", cache, store, "s#ww#fp.."), shape.c, _optional(cache), _optional(store),
+                                                        rows.c, heads * shape.dim, q, out, heads, lse_out, workspace, workspace.nbytes,
+                                                        _stream(stream))), "relaxkv_shared_prefix_attention")
+
+
+def _bounds_of(shape: Shape, block_size: int) -> int:
+    """(block, KV head) pairs of the contexts (0 for a size that the library refuses)."""
+    return shape.context_blocks(int(block_size)) * shape.kv_heads if block_size > 0 else 0
 
 
 def relaxkv_block_bounds(shape: Shape, cache: CacheView, block_size: int, bounds_out: torch.Tensor, scale_out: torch.Tensor,
                          stream=None) -> None:
     """bounds_out int8 [sum of the contexts' blocks, H_kv, 2, D], scale_out fp32 [.., H_kv]."""
-    _check(lib().relaxkv_block_bounds(*_args("ss.pp.", shape.c, cache.c, int(block_size), bounds_out, scale_out, _stream(stream))),
-           "relaxkv_block_bounds")
+    _fit(shape, cache, None, None)
+    n = _bounds_of(shape, block_size)
+    _check(lib().relaxkv_block_bounds(*_args("ss.#c#f.", shape.c, cache.c, int(block_size), 2 * shape.dim * n, bounds_out, n, scale_out,
+                                             _stream(stream))), "relaxkv_block_bounds")
 
 
 def relaxkv_select_blocks(shape: Shape, block_size: int, bounds: torch.Tensor, scale: torch.Tensor, rows: ContinuationRows, q: torch.Tensor,
                           n_first: int, n_last: int, blocks_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """blocks_out int32 [n_rows, H_kv, n_select]."""
-    _check(lib().relaxkv_select_blocks(*_args("s.ppsp...pp..", shape.c, int(block_size), bounds, scale, rows.c, q, blocks_out.shape[2],
-                                              int(n_first), int(n_last), blocks_out, workspace, workspace.nbytes, _stream(stream))),
+    _fit(shape, None, None, rows)
+    n, n_select, n_rows = _bounds_of(shape, block_size), blocks_out.shape[2], rows.n_rows
+    _check(lib().relaxkv_select_blocks(*_args("s.#c#fs#w...#ip..", shape.c, int(block_size), 2 * shape.dim * n, bounds, n, scale, rows.c,
+                                              n_rows * shape.heads * shape.dim, q, n_select, int(n_first), int(n_last),
+                                              n_rows * shape.kv_heads * n_select, blocks_out, workspace, workspace.nbytes, _stream(stream))),
            "relaxkv_select_blocks")
 
 
@@ -601,9 +639,12 @@ def relaxkv_block_sparse_attention(shape: Shape, cache: Optional[CacheView], sto
                                    block_size: int, blocks: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
                                    lse_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """blocks int32 [n_rows, H_kv, n_select]: the context blocks that each row and KV head reads."""
-    _check(lib().relaxkv_block_sparse_attention(*_args(_codes("s", cache, store, "s.p.pppp.."), shape.c, _optional(cache), _optional(store),
-                                                       rows.c, int(block_size), blocks, blocks.shape[2], q, out, lse_out, workspace,
-                                                       workspace.nbytes, _stream(stream))), "relaxkv_block_sparse_attention")
+    _fit(shape, cache, store, rows)
+    n_select, heads = blocks.shape[2], rows.n_rows * shape.heads
+    _check(lib().relaxkv_block_sparse_attention(*_args(_codes("s", cache, store, "s.#i.#ww#fp.."), shape.c, _optional(cache), _optional(store),
+                                                       rows.c, int(block_size), rows.n_rows * shape.kv_heads * n_select, blocks, n_select,
+                                                       heads * shape.dim, q, out, heads, lse_out, workspace, workspace.nbytes,
+                                                       _stream(stream))), "relaxkv_block_sparse_attention")
 
 
 def relaxkv_debug_wait_timeout(stream=None) -> None:

@@ -98,3 +98,74 @@ def test_append_takes_what_it_took(calls):
         got = calls[-1][1]
         assert got[1:8] == (a["q"].data_ptr(), a["k"].data_ptr(), a["v"].data_ptr(), 5, 8, a["k"].shape[1], 64) and len(got) == 16
         assert got[11:13] == (a["positions"].data_ptr(), a["slots"].data_ptr()) and got[14] == a["q_out"].data_ptr()
+
+
+def step(n_rows=7, H=8, Hkv=2, D=64, ctx=(100, 0, 33), seqs=(2, 1, 2)):
+    """What the attention calls take, by name."""
+    cu = [sum(seqs[:i]) for i in range(len(seqs) + 1)]
+    shape = B.Shape(H, Hkv, D, ctx)
+    at = [sum(ctx[:i]) for i in range(len(ctx))]
+    nb = sum(-(-t // 16) for t in ctx)
+    rows = B.ContinuationRows(cu, [n_rows] * len(ctx), 40, i32(cu[-1] + 1), i32(n_rows), i32(n_rows), i32(cu[-1], 3))
+    return dict(shape=shape, cache=B.CacheView(bf(sum(ctx), Hkv, D), bf(sum(ctx), Hkv, D), at), store=B.PagedStore(bf(9, 16, Hkv, D), bf(9, 16, Hkv, D)), rows=rows,
+                q=bf(n_rows, H, D), out=bf(n_rows, H, D), lse_out=torch.zeros(H, n_rows), blocks=i32(n_rows, Hkv, 4), bounds=torch.zeros(nb, Hkv, 2, D, dtype=torch.int8),
+                scale=torch.zeros(nb, Hkv), workspace=torch.zeros(512, dtype=torch.uint8))
+
+
+def shared(a):
+    B.relaxkv_shared_prefix_attention(*(a[k] for k in ("shape", "cache", "store", "rows", "q", "out", "workspace", "lse_out")), stream=0)
+
+
+def sparse(a):
+    B.relaxkv_block_sparse_attention(a["shape"], a["cache"], a["store"], a["rows"], 16, a["blocks"], a["q"], a["out"], a["workspace"], a["lse_out"], stream=0)
+
+
+def select(a):
+    B.relaxkv_select_blocks(a["shape"], 16, a["bounds"], a["scale"], a["rows"], a["q"], 1, 1, a["blocks"], a["workspace"], stream=0)
+
+
+def bounds(a):
+    B.relaxkv_block_bounds(a["shape"], a["cache"], 16, a["bounds"], a["scale"], stream=0)
+
+
+FITS = {
+    "rows of q": (dict(q=bf(6, 8, 64)), (shared, sparse, select)), "heads of q": (dict(q=bf(7, 4, 64)), (shared, sparse, select)),
+    "type of q": (dict(q=bf(7, 8, 64).float()), (shared, sparse, select)), "order of q": (dict(q=bf(7, 12, 64)[:, :8]), (shared, sparse, select)),
+    "rows of out": (dict(out=bf(6, 8, 64)), (shared, sparse)), "order of out": (dict(out=bf(8, 7, 64).transpose(0, 1)), (shared, sparse)),
+    "rows of lse": (dict(lse_out=torch.zeros(8, 6)), (shared, sparse)), "order of lse": (dict(lse_out=torch.zeros(7, 8).t()), (shared, sparse)),
+    "type of lse": (dict(lse_out=torch.zeros(8, 7, dtype=torch.float64)), (shared, sparse)),
+    "rows of blocks": (dict(blocks=i32(6, 2, 4)), (sparse, select)), "heads of blocks": (dict(blocks=i32(7, 1, 4)), (sparse, select)),
+    "type of blocks": (dict(blocks=torch.zeros(7, 2, 4, dtype=torch.int64)), (sparse, select)), "order of blocks": (dict(blocks=i32(7, 2, 6)[..., :4]), (sparse, select)),
+    "bounds": (dict(bounds=torch.zeros(9, 2, 2, 64, dtype=torch.int8)), (select, bounds)), "scales": (dict(scale=torch.zeros(9, 2)), (select, bounds)),
+    "type of bounds": (dict(bounds=torch.zeros(10, 2, 2, 64)), (select, bounds)),
+    "contexts of rows": (dict(rows=step(ctx=(100, 33), seqs=(2, 3))["rows"]), (shared, sparse, select)),
+    "heads of the cache": (dict(cache=step(Hkv=1)["cache"]), (shared, sparse, bounds)), "dim of the cache": (dict(cache=step(D=128)["cache"]), (shared, sparse, bounds)),
+    "tokens of the cache": (dict(cache=step(ctx=(100, 0, 32))["cache"]), (shared, sparse, bounds)),
+    "requests of the cache": (dict(cache=step(ctx=(100, 33), seqs=(2, 3))["cache"]), (shared, sparse, bounds)),
+    "heads of the store": (dict(store=step(Hkv=1)["store"]), (shared, sparse)), "dim of the store": (dict(store=step(D=128)["store"]), (shared, sparse)),
+}
+
+
+@pytest.mark.parametrize("name", list(FITS))
+def test_attention_refuses_what_does_not_fit_the_step(calls, name):
+    kw, entries = FITS[name]
+    for entry in entries:
+        with pytest.raises(ValueError):
+            entry(dict(step(), **kw))
+    assert not calls
+
+
+def test_attention_takes_what_it_took(calls):
+    more = step(n_rows=9, Hkv=4)
+    for kw in (dict(), dict(lse_out=None), dict(store=None), {k: more[k] for k in ("q", "out", "cache", "store")}, dict(bounds=torch.zeros(30, 2, 2, 64, dtype=torch.int8))):
+        a = dict(step(), **kw)
+        for entry, n in ((shared, 10), (sparse, 13), (select, 13), (bounds, 6)):
+            entry(a)
+            assert len(calls[-1][1]) == n
+        assert calls[-4][1][4:7] == tuple(None if a[k] is None else a[k].data_ptr() for k in ("q", "out", "lse_out"))
+        assert calls[-2][1][2:4] == (a["bounds"].data_ptr(), a["scale"].data_ptr()) and calls[-2][1][5:10] == (a["q"].data_ptr(), 4, 1, 1, a["blocks"].data_ptr())
+        assert calls[-3][1][4:8] == (16, a["blocks"].data_ptr(), 4, a["q"].data_ptr()) and calls[-1][1][3:5] == (a["bounds"].data_ptr(), a["scale"].data_ptr())
+    none = dict(step(ctx=(0, 0, 0)), cache=None)
+    shared(none)
+    sparse(none)
+    assert [c[1][1] for c in calls[-2:]] == [None, None]
