@@ -76,6 +76,12 @@ class Continuations:
         for l in range(self.n_layers if self.n_select else 0):
             B.relaxkv_block_bounds(self.shape, caches[l], self.ctx_block, self.bounds[l], self.scale[l], stream=stream)
 
+    def _rows(self, h: torch.Tensor, n: int) -> torch.Tensor:
+        """The first n hidden rows of h: the kernels take as many as the buffers beside them have."""
+        if h.dim() != 2 or h.shape[0] < n or h.shape[1] != self.blk.hidden or h.dtype != torch.bfloat16 or not h.is_contiguous():
+            raise ValueError(f"{n} contiguous bf16 rows of {self.blk.hidden} expected, not {tuple(h.shape)} of {h.dtype}")
+        return h if h.shape[0] == n else h[:n]
+
     def _blocks(self, tokens: int) -> int:
         return -(-tokens // self.block_size)
 
@@ -116,20 +122,20 @@ class Continuations:
         if self.n_select == 0:
             B.relaxkv_shared_prefix_attention(self.shape, cache, self.stores[layer], self.rows, q, out, self.workspace, lse_out=lse_out, stream=stream)
             return
-        blocks = self.blocks[:q.shape[0]]
+        blocks = self.blocks[:self.n_rows]
         B.relaxkv_select_blocks(self.shape, self.ctx_block, self.bounds[layer], self.scale[layer], self.rows, q, self.n_first, self.n_last, blocks,
                                 self.workspace, stream=stream)
         B.relaxkv_block_sparse_attention(self.shape, cache, self.stores[layer], self.rows, self.ctx_block, blocks, q, out, self.workspace,
                                          lse_out=lse_out, stream=stream)
 
     def run(self, h0: torch.Tensor, weights: List[Dict[str, torch.Tensor]], caches: Sequence[Optional[B.CacheView]]) -> torch.Tensor:
-        """The step's rows through the decoder: h0 [n_rows, hidden] = their input representations.  Returns the hidden rows
-        after the last layer (one of this object's buffers)."""
+        """The step's rows through the decoder: h0 [n_rows, hidden] = their input representations (rows behind them are not looked
+        at).  Returns the hidden rows after the last layer (one of this object's buffers)."""
         n, blk = self.n_rows, self.blk
         if n == 0:
             return h0
         x, a, q, k, v, o, gu, m = (t[:n] for t in (self.x, self.a, self.q, self.k, self.v, self.o, self.gu, self.m))
-        h = h0
+        h = self._rows(h0, n)
         for l, w in enumerate(weights):
             if "w_qkv" not in w:                        # weight-loading steps, once per layer
                 w["w_qkv"] = B.stack_qkv(w["wq"], w["wk"], w["wv"])
@@ -154,7 +160,12 @@ class Continuations:
 
     def output_head(self, h: torch.Tensor, final_norm: torch.Tensor, w_head: torch.Tensor, logits: torch.Tensor) -> torch.Tensor:
         """Final RMSNorm and output projection of the given rows: logits [rows, vocab]."""
-        x = self.x[:h.shape[0]]
+        n, vocab = h.shape[0], w_head.shape[0]
+        if n > self.max_rows or w_head.shape[1] != self.blk.hidden:
+            raise ValueError(f"{n} rows of at most {self.max_rows} by a head {tuple(w_head.shape)}")
+        if logits.numel() < n * vocab or logits.dtype != torch.bfloat16 or not logits.is_contiguous():
+            raise ValueError(f"logits of {n} contiguous bf16 rows of {vocab} expected, not {tuple(logits.shape)} of {logits.dtype}")
+        h, x = self._rows(h, n), self.x[:n]
         B.relaxkv_rmsnorm(h, final_norm, x, self.blk.eps)
         B.relaxkv_linear(x, w_head, logits)
         return logits
