@@ -615,13 +615,13 @@ def _bounds_of(shape: Shape, block_size: int) -> int:
     return shape.context_blocks(int(block_size)) * shape.kv_heads if block_size > 0 else 0
 
 
-def relaxkv_block_bounds(shape: Shape, cache: CacheView, block_size: int, bounds_out: torch.Tensor, scale_out: torch.Tensor,
+def relaxkv_block_bounds(shape: Shape, cache: Optional[CacheView], block_size: int, bounds_out: torch.Tensor, scale_out: torch.Tensor,
                          stream=None) -> None:
-    """bounds_out int8 [sum of the contexts' blocks, H_kv, 2, D], scale_out fp32 [.., H_kv]."""
+    """bounds_out int8 [sum of the contexts' blocks, H_kv, 2, D], scale_out fp32 [.., H_kv].  cache: None where all contexts are empty."""
     _fit(shape, cache, None, None)
     n = _bounds_of(shape, block_size)
-    _check(lib().relaxkv_block_bounds(*_args("ss.#c#f.", shape.c, cache.c, int(block_size), 2 * shape.dim * n, bounds_out, n, scale_out,
-                                             _stream(stream))), "relaxkv_block_bounds")
+    _check(lib().relaxkv_block_bounds(*_args(("s." if cache is None else "ss") + ".#c#f.", shape.c, _optional(cache), int(block_size),
+                                             2 * shape.dim * n, bounds_out, n, scale_out, _stream(stream))), "relaxkv_block_bounds")
 
 
 def relaxkv_select_blocks(shape: Shape, block_size: int, bounds: torch.Tensor, scale: torch.Tensor, rows: ContinuationRows, q: torch.Tensor,

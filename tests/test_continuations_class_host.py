@@ -71,3 +71,15 @@ def test_the_output_head_refuses_more_rows_than_its_buffers_hold(monkeypatch, h,
     assert not calls
     c.output_head(bf(12, 256), bf(256), bf(104, 256), bf(20, 104))
     assert len(calls) == 2
+
+
+def test_sequences_without_contexts_have_no_bounds_to_make(monkeypatch):
+    """No context, no cache: as the attention calls take it."""
+    c = Continuations(H, HKV, D, (0, 0), (1, 2), L, BLK, n_blocks=20, max_len=40, block_size=16, device="cpu", n_select=4)
+    r = Recorder()
+    monkeypatch.setattr(B, "lib", lambda: r)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    c.context_bounds([None] * L)
+    assert [(name, a[1]) for name, a in r.calls] == [("relaxkv_block_bounds", None)] * L
+    c.begin([1, 1, 1])
+    assert c.run(bf(3, 256), weights(), [None] * L).shape == (3, 256)

@@ -26,3 +26,26 @@ def test_selection_in_contexts_beside_one_of_very_many_blocks(ctx, n_select, n_f
         c = s.context_of(r)
         want = orc.select(q[r], bi[at[c]:at[c + 1]], sc[at[c]:at[c + 1]], n_select, n_first, n_last)
         assert np.array_equal(lists[r].cpu().numpy(), want), r
+
+
+def test_block_selection_without_any_context():
+    """Sequences without a context: with and without block selection they attend over their own tokens alone."""
+    from paper_2609_33503_b200 import inputs
+    from paper_2609_33503_b200.continuations import Continuations
+    blk = inputs.BlockShape(hidden=256, inter=384, rope_theta=1.0e4, eps=1.0e-5)
+    w = inputs.Workload("continuations", 2, 8, 2, 64, 64, (1,), (1,), 0.15, base_seed=3, planted_chunks=((0,),))
+    weights = [inputs.block_weights(w, blk, l, "cuda") for l in range(2)]
+    outs = []
+    for n_select in (0, 4):
+        c = Continuations(8, 2, 64, (0, 0), (1, 2), 2, blk, n_blocks=20, max_len=40, block_size=16, max_rows=24, n_select=n_select)
+        c.context_bounds([None] * 2)
+        for i, new in enumerate(([20, 1, 3], [1, 1, 0])):
+            c.begin(new)
+            x = torch.randn(sum(new), 256, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda").to(torch.bfloat16)
+            outs.append(c.run(x, weights, [None] * 2).clone())
+        assert n_select == 0 or (c.blocks[:2] == -1).all()
+    assert status() == B().OK
+    for a, b in zip(outs[:2], outs[2:]):
+        # two orders of the same bf16 chain: each is some 8e-3 of the exact rows away
+        a, b = a.double(), b.double()
+        assert torch.isfinite(a).all() and float((a - b).norm() / b.norm()) <= 1.6e-2
