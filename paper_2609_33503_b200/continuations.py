@@ -85,6 +85,17 @@ class Continuations:
     def _blocks(self, tokens: int) -> int:
         return -(-tokens // self.block_size)
 
+    def _counts(self, new: List[int]) -> torch.Tensor:
+        """The counts on the device, by way of pinned memory: the host waits for nothing.  Those of the last steps are kept for the stream that
+        they were uploaded on (a stream's memory is handed out again in its own order)."""
+        key = (B._stream(None), *new)
+        if key not in self._new:
+            if len(self._new) >= 64:
+                del self._new[next(iter(self._new))]
+            host = torch.tensor(new, dtype=torch.int32, pin_memory=self.device.type == "cuda")
+            self._new[key] = host.to(self.device, non_blocking=True)
+        return self._new[key]
+
     def begin(self, new: Sequence[int]) -> int:
         """Begins a step: new[i] tokens of sequence i follow (0: it waits, -1: it ends and gives its blocks back).  Block tables, positions and
         slots of the rows are made on the device, on the current stream; the rows are those of the sequences in order.  Returns their number."""
@@ -101,12 +112,7 @@ class Continuations:
         n_free = self.n_free + sum(self._blocks(t) for t in self.lens) - sum(self._blocks(t) for t in lens)
         if n_free < 0:
             raise ValueError(f"{-n_free} blocks short: let sequences end, or give the store more")
-        key = tuple(new)
-        if key not in self._new:
-            if len(self._new) > 64:
-                self._new.clear()
-            self._new[key] = torch.tensor(new, dtype=torch.int32, device=self.device)
-        B.relaxkv_build_block_tables(self.block_size, self._len[0], self._new[key], self.base, self.free, self._n_free[0], self.table,
+        B.relaxkv_build_block_tables(self.block_size, self._len[0], self._counts(new), self.base, self.free, self._n_free[0], self.table,
                                      self._len[1], self._n_free[1], self.row_cu, self.row_seq[:rows], self.row_pos[:rows],
                                      self.row_len[:rows], self.row_slot[:rows])
         self._len.reverse()

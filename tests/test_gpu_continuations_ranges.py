@@ -49,3 +49,48 @@ def test_block_selection_without_any_context():
         # two orders of the same bf16 chain: each is some 8e-3 of the exact rows away
         a, b = a.double(), b.double()
         assert torch.isfinite(a).all() and float((a - b).norm() / b.norm()) <= 1.6e-2
+
+
+def small(seqs=(3,), **kw):
+    from paper_2609_33503_b200 import inputs
+    from paper_2609_33503_b200.continuations import Continuations
+    blk = inputs.BlockShape(hidden=256, inter=384, rope_theta=1.0e4, eps=1.0e-5)
+    return Continuations(8, 2, 64, (40,) * len(seqs), seqs, 1, blk, **dict(dict(n_blocks=300, max_len=600, block_size=16, max_rows=40), **kw))
+
+
+def test_a_step_begins_without_waiting_for_the_steps_before():
+    """New counts behind work that takes a quarter of a second: the host goes on at once, and the device's state is the host's copy."""
+    c = small()
+    c.begin([1, 1, 1])
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    torch.cuda._sleep(500_000_000)
+    done.record()
+    for new in ([2, 1, 1], [1, 3, 0], [0, 0, 5]):
+        c.begin(new)
+        assert not done.query()
+    torch.cuda.synchronize()
+    assert c._len[0].tolist() == c.lens == [4, 5, 7] and c._n_free[0].tolist() == [c.n_free] and status() == B().OK
+
+
+def test_counts_on_one_stream_are_not_another_streams():
+    """Steps on two streams in turn, each behind the other's; what the first stream allocates meanwhile takes no counts' place."""
+    c = small()
+    side = torch.cuda.Stream()
+    main = torch.cuda.current_stream()
+    junk = []
+    for i in range(150):
+        new = [1 + i % 3, (i // 3) % 4, (i // 12) % 5] if i % 10 < 9 else [-1, -1, -1]
+        if i % 2:
+            side.wait_stream(main)
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(200_000)
+                c.begin(new)
+            main.wait_stream(side)
+        else:
+            c.begin(new)
+        if i % 2:
+            junk.append(torch.full((3,), 77, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert c._len[0].tolist() == c.lens and c._n_free[0].tolist() == [c.n_free] and status() == B().OK
+    assert len(c._new) <= 64
