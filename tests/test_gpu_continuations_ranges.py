@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests import continuation_oracle as orc
-from tests.test_gpu_continuations import B, Step, f64, get_bounds, status
+from tests.test_gpu_continuations import B, Step, f64, get_bounds, i32, status
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,32 @@ def test_counts_on_one_stream_are_not_another_streams():
     torch.cuda.synchronize()
     assert c._len[0].tolist() == c.lens and c._n_free[0].tolist() == [c.n_free] and status() == B().OK
     assert len(c._new) <= 64
+
+
+@pytest.mark.parametrize("rows,own", [(3, True), (30, True), (30, False)])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("mantissa", [1.0, 1.3203125])
+@pytest.mark.parametrize("exponent", [10, 21, 33, 60, 104, 124])
+def test_the_highest_of_very_large_logits_takes_its_row(rows, own, sign, exponent, mantissa):
+    """Logits of some 2^exponent (whose products with the scale are exact in fp32, or are not), one above all others: whatever the number of rows, that key has the weight 1 and its logit is the row's lse.  (The products
+    are exact, logits differ by a quarter of their size at least: no rounding can bring another key near.)"""
+    b = B()
+    D, n = 128, 1500
+    for key in (0, 700, n - 1):
+        s = Step(8, 2, D, [n], [rows], [17] * rows if own else [0] * rows, 1, 16, seed=22)
+        big = 2.0 ** (exponent // 2)
+        s.q.zero_()
+        s.q[..., 0] = mantissa * 2.0 ** (exponent - exponent // 2)
+        k = s.k[s.at[0]:s.at[0] + n]
+        k[..., 0] = (sign * big * (1.5 if sign < 0 else 0.5) * (1 + torch.arange(n, device="cuda") % 32 / 128)[:, None]).to(torch.bfloat16)
+        k[key, :, 0] = sign * big
+        s.ks[..., 0] = sign * big * (1.5 if sign < 0 else 0.5)
+        if not own:
+            s.row_len = [0] * rows
+            s.t["row_len"], s.max_len = i32(s.row_len), 0
+        b.relaxkv_shared_prefix_attention(s.shape, s.view, s.store if own else None, s.rows(), s.q, s.out, s.ws(), lse_out=s.lse)
+        assert status() == b.OK
+        assert torch.equal(s.out.view(rows, 2, 4, D), s.v[s.at[0] + key][None, :, None].expand(rows, 2, 4, D)), key
+        want = sign * mantissa * 2.0 ** exponent * float(np.float32(D ** -0.5))
+        # fp32: the scale in log2 units, the product, the way back to natural units, twice where pieces are merged; 2^-24 each, with the constants'
+        assert float((s.lse.double() / want - 1).abs().max()) <= 8 * 2.0 ** -24, key
