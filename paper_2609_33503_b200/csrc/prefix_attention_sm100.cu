@@ -35,13 +35,15 @@ constexpr float kPreRescale = 8.0f;                   // log2 units: O is rescal
 // What a row's maximum begins with: the lowest finite number, so that logits of -inf leave 2^(-inf) = 0 and any finite logit more.
 constexpr float kPreLowest = -3.402823466e38f;
 // s * scale - m in one rounding keeps what the rounding of m has cut off: the same factor, up to 2^(|m| 2^-24), on all weights of a row, which their
-// sum takes out again.  Beyond this |m| (2^-9 of a weight) the logits are rounded first, as m is: the factor would take a lone weight off 1 as a bf16,
-// and leave the range of numbers where |m| is 2^31.  (By thread: by vote of the warp 64 rows over 32 K took 90.8 us, 90.3 so, 89.7 without.)
+// sum takes out again.  Where the largest logit of a tile is beyond this (2^-9 of a weight), its logits are rounded first, as m is: the factor would
+// take a lone weight off 1 as a bf16, and leave the range of numbers where |m| is 2^31.  (A tile below it beside such an m has weights of zero, or
+// makes the next m itself.)  Looked at before the other group's maximum is waited for: 64 rows over 32 K 80.7 us, behind it 81.0, without 79.8; 16 over
+// 16 K 26.4, 26.7 and 26.4.
 constexpr float kPreExact = 32768.f;
 constexpr float kLog2ePre = 1.4426950408889634f, kLn2Pre = 0.6931471805599453f;
 
 // p = 2^(s * scale - m) of a row's 128 keys as bf16 pairs, and their sum.  bf16 is what the product with V takes beside bf16 values: its rounding
-// errors (2^-9 of a weight, of either sign) average out over the keys; the sum is that of the unrounded weights, in fp32.
+// errors (up to 2^-8 of a weight, of either sign) average out over the keys; the sum is that of the unrounded weights, in fp32.
 __device__ __forceinline__ float prefix_exponentials(const uint32_t* s, uint32_t* pk, float scale, float neg_m) {
   float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
 #pragma unroll
@@ -277,6 +279,12 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
 #pragma unroll
       for (int i = 16; i < kPreTile; i += 2) mx[(i >> 1) & 7] = fmax3(mx[(i >> 1) & 7], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
       const float m_tile = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.scale_log2;
+      float scale = a.scale_log2;
+      if (__any_sync(0xffffffffu, fabsf(m_tile) > kPreExact)) {
+#pragma unroll
+        for (int i = 0; i < kPreTile; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * scale);
+        scale = 1.f;
+      }
       if (j > 0) {                                      // the other group's maximum of the tile before
         ok = mbar_wait(bar_m + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
@@ -290,12 +298,6 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
       z *= fast_exp2(m - m_new);                        // (1 as long as nothing has changed)
       m = m_new;
       uint32_t pk[64];
-      float scale = a.scale_log2;
-      if (__builtin_expect(fabsf(m) > kPreExact, 0)) {
-#pragma unroll
-        for (int i = 0; i < kPreTile; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * scale);
-        scale = 1.f;
-      }
       z += prefix_exponentials(s, pk, scale, -m);
       if (j > 0) {                                      // O of the tile before is complete, its P is not needed any more
         ok = mbar_wait(bar_o + 8 * (x ^ 1), (uint32_t)((j - 1) >> 1) & 1, abort_flag);
