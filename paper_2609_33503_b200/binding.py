@@ -239,10 +239,10 @@ class Shape:
         return len(self.ctx_lens)
 
     def context_blocks(self, block_size: int) -> int:
-        """Blocks of that many tokens in all contexts."""
+        """Blocks of that many tokens in all contexts (0 for a size that the library refuses)."""
         n = self._blocks.get(block_size)
         if n is None:
-            n = self._blocks[block_size] = sum(-(-t // block_size) for t in self._ctx)
+            n = self._blocks[block_size] = sum(-(-t // block_size) for t in self._ctx) if block_size > 0 else 0
         return n
 
     def ref(self):
@@ -582,8 +582,9 @@ def _fit(shape: Shape, cache: Optional[CacheView], store: Optional[PagedStore], 
     if cache is not None:
         if cache.dim != shape.dim or cache.heads < shape.kv_heads:
             raise ValueError(f"a cache of {cache.heads} heads of {cache.dim} for a shape of {shape.kv_heads} heads of {shape.dim}")
-        if len(cache.room) < len(shape.ctx_lens) or not all(map(operator.le, shape.ctx_lens, cache.room)):
-            raise ValueError(f"contexts of {shape.ctx_lens} tokens in a cache with room for {cache.room}")
+        lens, room = shape.ctx_lens, cache.room
+        if len(room) < len(lens) or False in map(operator.le, lens, room):
+            raise ValueError(f"contexts of {lens} tokens in a cache with room for {room}")
     if store is not None and (store.dim != shape.dim or store.heads < shape.kv_heads):
         raise ValueError(f"a store of {store.heads} heads of {store.dim} for a shape of {shape.kv_heads} heads of {shape.dim}")
     if rows is not None and rows.n_req != len(shape.ctx_lens):
@@ -610,17 +611,12 @@ def relaxkv_shared_prefix_attention(shape: Shape, cache: Optional[CacheView], st
                                                         _stream(stream))), "relaxkv_shared_prefix_attention")
 
 
-def _bounds_of(shape: Shape, block_size: int) -> int:
-    """(block, KV head) pairs of the contexts (0 for a size that the library refuses)."""
-    return shape.context_blocks(int(block_size)) * shape.kv_heads if block_size > 0 else 0
-
-
 def relaxkv_block_bounds(shape: Shape, cache: Optional[CacheView], block_size: int, bounds_out: torch.Tensor, scale_out: torch.Tensor,
                          stream=None) -> None:
     """bounds_out int8 [sum of the contexts' blocks, H_kv, 2, D], scale_out fp32 [.., H_kv].  cache: None where all contexts are empty."""
     _fit(shape, cache, None, None)
-    n = _bounds_of(shape, block_size)
-    _check(lib().relaxkv_block_bounds(*_args(("s." if cache is None else "ss") + ".#c#f.", shape.c, _optional(cache), int(block_size),
+    n = shape.context_blocks(block_size) * shape.kv_heads
+    _check(lib().relaxkv_block_bounds(*_args(("s." if cache is None else "ss") + ".#C#F.", shape.c, _optional(cache), int(block_size),
                                              2 * shape.dim * n, bounds_out, n, scale_out, _stream(stream))), "relaxkv_block_bounds")
 
 
@@ -628,7 +624,7 @@ def relaxkv_select_blocks(shape: Shape, block_size: int, bounds: torch.Tensor, s
                           n_first: int, n_last: int, blocks_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """blocks_out int32 [n_rows, H_kv, n_select]."""
     _fit(shape, None, None, rows)
-    n, n_select, n_rows = _bounds_of(shape, block_size), blocks_out.shape[2], rows.n_rows
+    n, n_select, n_rows = shape.context_blocks(block_size) * shape.kv_heads, blocks_out.shape[2], rows.n_rows
     _check(lib().relaxkv_select_blocks(*_args("s.#c#fs#w...#ip..", shape.c, int(block_size), 2 * shape.dim * n, bounds, n, scale, rows.c,
                                               n_rows * shape.heads * shape.dim, q, n_select, int(n_first), int(n_last),
                                               n_rows * shape.kv_heads * n_select, blocks_out, workspace, workspace.nbytes, _stream(stream))),

@@ -9,7 +9,7 @@
 //                                that many elements of int32, bfloat16, float32 or int8 side by side: what a kernel reads or writes of
 //                                it.  Where its bytes are just those, the capitals ask nothing more (50 ns a tensor); 'i', 'w', 'f', 'c' ask
 //                                for the order of its elements in any case (another 60).  An object that only has an address is taken at
-//                                its word.  (Block tables of a decode step, twelve tensors: 5.3 us a call without, 6.2 with.)
+//                                its word.  (Block tables of a decode step, twelve tensors: 5.2 us a call without, 5.8 with.)
 //   bind(name, address, other)   the entry point at `address` as a callable over integers, floats, bytes and None.  A call with
 //                                anything else among its arguments (a ctypes reference, a wrong count) is `other`'s.
 // The interpreter's lock is released during the call, as ctypes does it.  Python 3.10 or newer.
