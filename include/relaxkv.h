@@ -455,7 +455,7 @@ relaxkv_status relaxkv_cache_attention(
 
 /*
  * ---- Many continuations of a repaired context.  (The paper answers one query per repair; these calls are for the callers that answer
- * from one repaired context many times: several samples, beams, follow-up questions.)  The contexts stay where the repair left them, in a
+ * from one repaired context many times: several samples, follow-up questions.)  The contexts stay where the repair left them, in a
  * relaxkv_cache_view; every continuation ("sequence") keeps the K/V of its own tokens - the question, the answer so far - in blocks of a
  * paged store.  One step appends some tokens to some sequences (a "row" each) and attends from those rows.  ----
  *
@@ -509,6 +509,7 @@ size_t relaxkv_continuation_workspace_bytes(const relaxkv_shape* shape, int64_t 
  * A sequence with seq_len < 0, more tokens than its row of block_table holds or new_len > n_rows is left as it is; more rows than n_rows, more
  * blocks than there are: nothing is appended to any sequence (ended ones still end); n_free or the blocks given back beyond free_capacity:
  * nothing happens at all.  Each is reported in the device status word.  Block numbers are not looked at here (the calls that use them do).
+ * A block is one sequence's: one that stands in two rows of block_table is given back by each of them when it ends.
  * n_seq <= 4096.
  */
 relaxkv_status relaxkv_build_block_tables(
@@ -556,7 +557,7 @@ relaxkv_status relaxkv_block_bounds(const relaxkv_shape* shape, const relaxkv_ca
 /*
  * The context blocks that a row may need most: with q_h in 8 bits the way the bounds are (scale s_h per row and head, rounded to nearest even),
  *   score[x] = scale[x] * max over the heads h of the KV head's group of s_h * sum_d (max(q_hd, 0) * hi_d + min(q_hd, 0) * lo_d),
- * the largest logit that a key within the bounds could have.  All terms are whole numbers below 2^24 and powers of two, so scores do not depend on
+ * the largest logit that a key within the bounds could have with this rounded query (of the query itself a logit may lie above).  All terms are whole numbers below 2^24 and powers of two, so scores do not depend on
  * the order of summation.  Selected are the n_select blocks of the highest score, equal scores by the lower number, the first n_first and the last
  * n_last blocks in any case.
  * blocks_out device int32 [n_rows, H_kv, n_select]: ascending, -1 behind them.  n_first + n_last <= n_select.

@@ -1,4 +1,4 @@
-"""Many continuations of repaired contexts: several samples, beams or follow-up questions that share what a repair has paid for.
+"""Many continuations of repaired contexts: several samples or follow-up questions that share what a repair has paid for.
 (The paper answers one query per repair; this is its decode step for callers that answer from one repaired context many times.)
 
 The contexts stay in the caches the repair loop leaves them in.  What a continuation ("sequence") adds of its own - a question, the

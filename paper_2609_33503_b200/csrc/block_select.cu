@@ -1,9 +1,10 @@
-// Context blocks by a cheap score: 8-bit bounds of every block's keys (relaxkv_block_bounds), and the blocks of the highest possible logit for
-// each row and KV head (relaxkv_select_blocks).
+// Context blocks by a cheap score: 8-bit bounds of every block's keys (relaxkv_block_bounds), and the blocks of the highest score for each row
+// and KV head (relaxkv_select_blocks): the largest logit of a key within the bounds, of the query as it is in 8 bits.
 //
 // Bounds: one pass over K, bound by its bytes.  A warp has one (block, KV head): 16 lanes hold the 128 dims of a token as 16-byte pieces, so
 // a load takes two tokens (four of 64 dims); maxima and minima stay packed bf16 pairs and are exact.  The scale is a power of two, so are the
-// quotients, and the rounding is away from the block: the bounds remain bounds.
+// quotients, and the rounding is away from the block: the bounds remain bounds (but for infinite keys, which are clamped).  The query is rounded to
+// the nearest number, so a score may lie below a logit of the query itself.
 // Scores: sum_d max(q_d hi_d, q_d lo_d) = q+ . hi + q- . lo, a product over 2 D whole numbers of 8 bits, as halves on the tensor cores with sums in
 // 32 bits: rows are the heads of one, two or four rows of the step, columns eight blocks.  All are whole numbers below 2^24, so the scores, and with them
 // the lists, do not depend on the order of anything; it may be any as long as both sides agree, so a lane takes D / 2 bytes of its block in
@@ -141,7 +142,7 @@ struct SelectArgs {
   float* scores;                       // [n_rows, H_kv, most]
   int* out;                            // [n_rows, H_kv, n_select]
   long long n_rows;
-  int most, H, Hkv, n_seq, block_size, n_select, n_first, n_last;
+  int most, H, Hkv, n_seq, n_select, n_first, n_last;
   int kept;                            // scores that a block of the selection has shared memory for
 };
 
@@ -497,7 +498,7 @@ extern "C" relaxkv_status relaxkv_select_blocks(
   a.bounds = bounds; a.scale = scale; a.q = static_cast<const uint16_t*>(q);
   a.row_cu = rows->row_cu; a.row_seq = rows->row_seq;
   a.scores = static_cast<float*>(workspace); a.out = blocks_out; a.n_rows = rows->n_rows;
-  a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.n_seq = rows->n_seq; a.block_size = block_size;
+  a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.n_seq = rows->n_seq;
   a.n_select = n_select; a.n_first = n_first; a.n_last = n_last;
   const int G = a.H / a.Hkv, rows_per = (G <= 4 ? 4 : G <= 8 ? 2 : 1) * kScoPass;
   long long tiles = 0;
