@@ -48,6 +48,7 @@ class Continuations:
         self.lens = [0] * n_seq                        # the host's copy of the lengths: what it asks for is what it gets
         self.n_free = int(n_blocks)
         self._new: Dict[tuple, torch.Tensor] = {}
+        self._captured: List[torch.Tensor] = []
         R = self.max_rows
         self.row_cu = torch.empty(n_seq + 1, **i32)
         self.row_seq, self.row_pos, self.row_len, self.row_slot = (torch.empty(R, **i32) for _ in range(4))
@@ -89,6 +90,13 @@ class Continuations:
         """The counts on the device, by way of pinned memory: the host waits for nothing.  Those of the last steps are kept for the stream that
         they were uploaded on (a stream's memory is handed out again in its own order)."""
         key = (B._stream(None), *new)
+        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            # a graph reads what an earlier step has uploaded, as long as this object lives: its own copy would read pinned memory that is used again
+            known = next((t for k, t in self._new.items() if k[1:] == key[1:]), None)
+            if known is None:
+                raise RuntimeError("a step whose counts are new cannot begin in a graph's capture: begin one of the same counts before")
+            self._captured.append(known)
+            return known
         if key not in self._new:
             if len(self._new) >= 64:
                 del self._new[next(iter(self._new))]

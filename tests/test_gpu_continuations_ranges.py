@@ -123,3 +123,25 @@ def test_the_highest_of_very_large_logits_takes_its_row(rows, own, sign, exponen
         want = sign * mantissa * 2.0 ** exponent * float(np.float32(D ** -0.5))
         # fp32: the scale in log2 units, the product, the way back to natural units, twice where pieces are merged; 2^-24 each, with the constants'
         assert float((s.lse.double() / want - 1).abs().max()) <= 8 * 2.0 ** -24, key
+
+
+def test_steps_in_a_graph_read_counts_that_were_uploaded_before():
+    """Two steps as a graph (they use the two sets of lengths in turn); counts that are new to the object are refused while it is captured."""
+    c = small()
+    for new in ([2, 0, 1], [1, 1, 1]):
+        c.begin(new)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.begin([1, 1, 1])
+        c.begin([2, 0, 1])
+        before = (list(c.lens), c.n_free, c.n_rows, list(c._len))
+        with pytest.raises(RuntimeError, match="capture"):
+            c.begin([3, 0, 0])
+        assert before[:3] == (c.lens, c.n_free, c.n_rows) and all(x is y for x, y in zip(before[3], c._len))
+    for i in range(100):                                     # other counts push these out of those that are kept
+        c._counts([5 + i, 0, 0])
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert c._len[0].tolist() == c.lens == [6, 2, 4] and c._n_free[0].tolist() == [c.n_free] and status() == B().OK
