@@ -30,6 +30,8 @@ ENTRY_POINTS = (
     "relaxkv_swiglu", "relaxkv_target_positions", "relaxkv_carry_rows", "relaxkv_set_chained_launch",
     "relaxkv_continuation_workspace_bytes", "relaxkv_build_block_tables", "relaxkv_qk_norm_rope_append_paged", "relaxkv_shared_prefix_attention",
     "relaxkv_block_bounds", "relaxkv_select_blocks", "relaxkv_block_sparse_attention",
+    "relaxkv_rotary_frequencies", "relaxkv_qk_norm_rotate", "relaxkv_append_quantized", "relaxkv_read_quantized",
+    "relaxkv_quantized_workspace_bytes", "relaxkv_quantized_attention",
 )
 
 
@@ -59,6 +61,16 @@ class _CacheView(ctypes.Structure):
 class _PagedCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64), ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class _QuantizedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("block_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("block_size", ctypes.c_int32),
+                ("n_blocks", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float)]
 
 
 class _ContinuationRows(ctypes.Structure):
@@ -93,6 +105,9 @@ _SIGNATURES = {
     "relaxkv_qk_norm_rope_append_paged": (_ST, "p ppp liii pp f pp f pp"),
     "relaxkv_shared_prefix_attention": (_ST, "pppp ppp pzp"), "relaxkv_block_bounds": (_ST, "pp i pp p"),
     "relaxkv_select_blocks": (_ST, "p i pp pp iii p pzp"), "relaxkv_block_sparse_attention": (_ST, "pppp ipi ppp pzp"),
+    "relaxkv_rotary_frequencies": (_ST, "id id i dd pp"), "relaxkv_qk_norm_rotate": (_ST, "ppll ppll liii pp f pp p"),
+    "relaxkv_append_quantized": (_ST, "p ppll ppll liii pp f pp p p"), "relaxkv_read_quantized": (_ST, "pp lii pp pp ll p"),
+    "relaxkv_quantized_workspace_bytes": (ctypes.c_size_t, "iii"), "relaxkv_quantized_attention": (_ST, "pp iii f ppp pzp"),
     "relaxkv_debug_wait_timeout": (_ST, "p"), "relaxkv_read_device_status": (_ST, "pp p"),
 }
 
@@ -284,6 +299,46 @@ class PagedStore:
     @property
     def block_size(self) -> int:
         return int(self.k.shape[1])
+
+
+class QuantizedStore:
+    """Host-side relaxkv_quantized_cache over torch tensors: k, v of logical shape [n_blocks, block_size, H_kv, D], int8 or float8_e4m3fn (any block,
+    token and head strides, D contiguous), their exponents k_exp, v_exp int8 [n_blocks, H_kv, block_size]."""
+
+    TYPES = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
+        assert k.dim() == 4 and k.stride(3) == 1 and k.dtype in self.TYPES
+        assert v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype
+        n, block, heads, dim = (int(x) for x in k.shape)
+        for e in (k_exp, v_exp):
+            assert e.shape == (n, heads, block) and e.dtype == torch.int8 and e.is_contiguous()
+        self.k, self.v, self.k_exp, self.v_exp, self.block_size, self.heads, self.dim = k, v, k_exp, v_exp, block, heads, dim
+        self.c = _QuantizedCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), int(k.stride(0)), int(k.stride(1)), int(k.stride(2)),
+                                 block, n, heads, self.TYPES[k.dtype])
+
+    @classmethod
+    def empty(cls, n_blocks: int, block_size: int, kv_heads: int, dim: int, dtype=torch.int8, device="cuda") -> "QuantizedStore":
+        values = [torch.empty(n_blocks, block_size, kv_heads, dim, dtype=dtype, device=device) for _ in range(2)]
+        return cls(*values, *(torch.empty(n_blocks, kv_heads, block_size, dtype=torch.int8, device=device) for _ in range(2)))
+
+
+class Rotary:
+    """Host-side relaxkv_rotary: freq float64 [rotated dims / 2] on the device."""
+
+    SCALINGS = {"none": 0, "linear": 1, "bands": 2, "ramp": 3}
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
+        assert freq.dim() == 1 and freq.dtype == torch.float64 and freq.is_contiguous()
+        self.freq, self.dims, self.interleaved, self.amplitude = freq, 2 * int(freq.numel()), bool(interleaved), float(amplitude)
+        self.c = _Rotary(freq.data_ptr(), self.dims, int(self.interleaved), self.amplitude)
+
+    @classmethod
+    def scaled(cls, dims: int, theta: float, scaling: str = "none", factor: float = 1.0, original_len: int = 0, low: float = 1.0, high: float = 4.0,
+               interleaved: bool = False, device="cuda") -> "Rotary":
+        """Frequencies theta^(-2i / dims), scaled as relaxkv_rotary_frequencies says."""
+        freq, amplitude = relaxkv_rotary_frequencies(dims, theta, scaling, factor, original_len, low, high)
+        return cls(torch.tensor(freq, dtype=torch.float64, device=device), interleaved, amplitude)
 
 
 _INT32 = torch.int32
@@ -641,6 +696,87 @@ def relaxkv_block_sparse_attention(shape: Shape, cache: Optional[CacheView], sto
                                                        rows.c, int(block_size), rows.n_rows * shape.kv_heads * n_select, blocks, n_select,
                                                        heads * shape.dim, q, out, heads, lse_out, workspace, workspace.nbytes,
                                                        _stream(stream))), "relaxkv_block_sparse_attention")
+
+
+def relaxkv_rotary_frequencies(dims: int, theta: float, scaling: str = "none", factor: float = 1.0, original_len: int = 0, low: float = 1.0,
+                               high: float = 4.0):
+    """The dims / 2 frequencies and the amplitude (scaling: a name of Rotary.SCALINGS)."""
+    freq, amplitude = (ctypes.c_double * max(1, int(dims) // 2))(), ctypes.c_float()
+    _check(lib().relaxkv_rotary_frequencies(int(dims), float(theta), Rotary.SCALINGS[scaling], float(factor), int(original_len), float(low), float(high),
+                                            ctypes.byref(freq), ctypes.byref(amplitude)), "relaxkv_rotary_frequencies")
+    return list(freq), float(amplitude.value)
+
+
+_BF16 = torch.bfloat16
+
+
+def _head_rows(x: torch.Tensor, like: Optional[torch.Tensor], n: Optional[int], heads: Optional[int], dim: Optional[int]):
+    """Rows, heads, dims, token and head stride of bf16 head rows [n, heads, dim], which are laid out like `like`."""
+    shape, strides = x.shape, x.stride()
+    if (len(shape) != 3 or x.dtype is not _BF16 or strides[2] != 1 or (n is not None and shape[0] != n) or (heads is not None and shape[1] != heads)
+            or (dim is not None and shape[2] != dim)):
+        raise ValueError(f"bf16 rows [{n}, {heads}, {dim}] with contiguous heads expected, not {tuple(shape)} of {x.dtype}, strides {strides}")
+    if like is not None and (like.shape != shape or like.stride() != strides or like.dtype is not _BF16):
+        raise ValueError(f"rows laid out like {tuple(shape)}, strides {strides}, expected, not {tuple(like.shape)} of {like.dtype}, strides {like.stride()}")
+    return shape[0], shape[1], shape[2], max(strides[0], shape[2]) if shape[0] == 1 else strides[0], max(strides[1], shape[2]) if shape[1] == 1 else strides[1]
+
+
+def relaxkv_qk_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, rotary: Rotary, q_out: Optional[torch.Tensor] = None,
+                           k_out: Optional[torch.Tensor] = None, w_q_norm: Optional[torch.Tensor] = None, w_k_norm: Optional[torch.Tensor] = None,
+                           eps: float = 1e-6, stream=None) -> None:
+    """Per-head RMSNorm (when weights are given) and any rotary embedding of q [n, H, D] and k [n, H_kv, D] (either may be None), into q_out and k_out, which are laid
+    out like them, or in place where these are None."""
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    n = dim = None
+    heads = kv_heads = q_token = q_head = k_token = k_head = 0
+    if q is not None:
+        n, heads, dim, q_token, q_head = _head_rows(q, q_out, None, None, None)
+    if k is not None:
+        n, kv_heads, dim, k_token, k_head = _head_rows(k, k_out, n, None, dim)
+    if n is None:
+        raise ValueError("neither q nor k")
+    _check(lib().relaxkv_qk_norm_rotate(*_args("pp..pp......#WW.#Is.", q, q_out, q_token, q_head, k, k_out, k_token, k_head, n, heads, kv_heads, dim, dim,
+                                               w_q_norm, w_k_norm, float(eps), n, positions, rotary.c, _stream(stream))), "relaxkv_qk_norm_rotate")
+
+
+def relaxkv_append_quantized(store: QuantizedStore, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, q: Optional[torch.Tensor] = None,
+                             q_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                             w_q_norm: Optional[torch.Tensor] = None, w_k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
+    """The store receives k (normed where weights are given, turned where a rotary is) and v [n, H_kv, D] at `slots`; q_out (None: q itself) = q likewise."""
+    n, kv_heads, dim, k_token, k_head = _head_rows(k, v, None, store.heads, store.dim)
+    heads = q_token = q_head = 0
+    if q is not None:
+        q_out = q if q_out is None else q_out
+        _, heads, _, q_token, q_head = _head_rows(q, q_out, n, None, dim)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(lib().relaxkv_append_quantized(*_args("spp..pp......#WW.#I" + ("." if rotary is None else "s") + "I.", store.c, q, q_out, q_token, q_head, k, v, k_token,
+                                                 k_head, n, heads, kv_heads, dim, dim, w_q_norm, w_k_norm, float(eps), n, positions,
+                                                 None if rotary is None else rotary.c, slots, _stream(stream))), "relaxkv_append_quantized")
+
+
+def relaxkv_read_quantized(store: QuantizedStore, slots: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                           rotary: Optional[Rotary] = None, stream=None) -> None:
+    """k_out, v_out [n, H_kv, D] = the store's rows at `slots`, the keys turned by `positions` more."""
+    n, kv_heads, dim, token, head = _head_rows(k_out, v_out, None, store.heads, store.dim)
+    _check(lib().relaxkv_read_quantized(*_args("s#I...I" + ("." if rotary is None else "s") + "pp...", store.c, n, slots, n, kv_heads, dim, positions,
+                                               None if rotary is None else rotary.c, k_out, v_out, token, head, _stream(stream))), "relaxkv_read_quantized")
+
+
+def relaxkv_quantized_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().relaxkv_quantized_workspace_bytes(int(n_q_heads), int(n_kv_heads), int(head_dim)))
+
+
+def relaxkv_quantized_attention(store: QuantizedStore, rows: ContinuationRows, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                                lse_out: Optional[torch.Tensor] = None, softmax_scale: Optional[float] = None, stream=None) -> None:
+    """q, out [n_rows, H, D], contiguous; softmax_scale: D^-1/2 where None."""
+    n, heads, dim = q.shape
+    if dim != store.dim or n != rows.n_rows:
+        raise ValueError(f"{n} rows of heads of {dim} for {rows.n_rows} rows over a store of heads of {store.dim}")
+    size = n * heads * dim
+    _check(lib().relaxkv_quantized_attention(*_args("ss....#ww#fp..", store.c, rows.c, heads, store.heads, dim,
+                                                    float(dim ** -0.5 if softmax_scale is None else softmax_scale), size, q, out, n * heads, lse_out, workspace,
+                                                    workspace.nbytes, _stream(stream))), "relaxkv_quantized_attention")
 
 
 def relaxkv_debug_wait_timeout(stream=None) -> None:

@@ -223,7 +223,8 @@ const Known kKnown[] = {
     KNOWN(relaxkv_linear), KNOWN(relaxkv_linear_qkv), KNOWN(relaxkv_linear_swiglu), KNOWN(relaxkv_qk_norm_rope),
     KNOWN(relaxkv_qk_norm_rope_append), KNOWN(relaxkv_swiglu), KNOWN(relaxkv_target_positions), KNOWN(relaxkv_carry_rows),
     KNOWN(relaxkv_build_block_tables), KNOWN(relaxkv_qk_norm_rope_append_paged), KNOWN(relaxkv_shared_prefix_attention), KNOWN(relaxkv_block_bounds),
-    KNOWN(relaxkv_select_blocks), KNOWN(relaxkv_block_sparse_attention),
+    KNOWN(relaxkv_select_blocks), KNOWN(relaxkv_block_sparse_attention), KNOWN(relaxkv_qk_norm_rotate), KNOWN(relaxkv_append_quantized),
+    KNOWN(relaxkv_read_quantized), KNOWN(relaxkv_quantized_attention),
 };
 
 void entry_dealloc(PyObject* self) {

@@ -1,0 +1,745 @@
+// Attention of a step's rows over their sequence's tokens in the 8-bit store (relaxkv_quantized_attention).
+//
+// Every key and value meets the few rows and heads that read its KV head once: bound by the bytes of K and V.  Tokens are the 16 rows of the warp-level MMA and
+// (row, head) pairs its 8 columns, S^T = K Q^T and O^T += V^T P^T: a group of 4 or 5 heads fills half of it (as the 16 rows of the usual order a quarter), and what
+// is made of a byte of K or V is used for NT column tiles.  Bytes become fp16 in registers, exactly: two instructions for two of them (the byte under the exponent of
+// 1024, minus that; or the hardware's conversion of e4m3).  Q becomes fp16 exactly, too, scaled by a power of two per head; scores get the exponent
+// of their token's keys behind the product.  The exponents of the values are weighed with the scores: p'_t = 2^(s_t + e_t - max of that + 14), so that weights stay within
+// fp16 whatever the exponents are, and are rounded to 11 bits; the sum of the weights is kept beside it in fp32, with a maximum of its own.  P^T comes out of the first
+// product as rows of tokens and goes into the second as columns of them: one 8 x 8 transposition per 8 tokens.
+//
+// A warp streams 32 tokens at a time through a ring of its own in shared memory (16-byte asynchronous copies, no barrier between warps; what lies behind a
+// sequence's end is filled with zeros and never read), eight warps to an SM with two tiles of 8 KB in flight each.  The work of a call - (sequence, KV head, row tile, 32
+// tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths: a block's first and last task may be
+// parts of one, whose results a second small kernel joins in the order of the blocks.
+#include "quantized_cache.cuh"
+#include "sm100_ptx.cuh"
+
+namespace relaxkv {
+
+constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaStages = 3, kQaTile = 32;
+constexpr int kQaBlocks = 2 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
+constexpr int kQaLeastTiles = 2 * kQaWarps;      // tiles of a block's share, at least
+constexpr int kQaColsMost = 32;                  // (row, head) columns of a block, at most
+constexpr int kQaSeqsMost = 4096;
+constexpr int kNoKey = -127;                     // exponent in shared memory of a token whose block does not exist
+constexpr float kPShift = 14.f;                  // the largest weight is 2^14
+
+struct QuantAttnArgs {
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse_out;
+  const uint8_t *k, *v;
+  const int8_t *k_exp, *v_exp;
+  const int *row_cu, *row_seq, *row_len, *table;
+  float *part_o, *part_s;
+  int4* chain;
+  long long block_stride, token_stride, head_stride, table_stride, n_rows;
+  int table_width, n_seq, n_blocks, block_shift, max_len;
+  int H, Hkv, G, rows_per_tile;
+  float scale_log2;
+};
+
+template <int D>
+struct QaSmem {
+  static constexpr int kHalf = 16 * D;                               // bytes of 16 tokens
+  static constexpr int kV = 2 * kHalf, kExp = 4 * kHalf;             // K | V | exponents of K, of V
+  static constexpr int kStage = kExp + 128;
+  static constexpr int kWarp = kQaStages * kStage;
+  static constexpr int kTotal = kQaWarps * kWarp;
+};
+
+// Place of 16-byte piece c of token t (of 16) so that eight tokens' pieces lie in eight different groups of banks.
+template <int D>
+__device__ __forceinline__ int swizzled(int t, int c) {
+  return D == 128 ? t * 128 + ((c ^ (t & 7)) << 4) : t * 64 + ((c ^ ((t >> 1) & 3)) << 4);
+}
+
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {       // bytes 16, or 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void load_matrices(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void load_matrices_trans(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t r) {
+  uint32_t t;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(r));
+  return t;
+}
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Bytes 0, 1 and 2, 3 of w as fp16 pairs (keys), bytes 0, 2 and 1, 3 (values, after the transposition of pairs of dims).
+template <int TYPE>
+__device__ __forceinline__ void key_pairs(uint32_t w, uint32_t* lo, uint32_t* hi) {
+  if constexpr (TYPE == RELAXKV_INT8) {
+    w ^= 0x80808080u;
+    *lo = int8_to_half2<0x4140>(w); *hi = int8_to_half2<0x4342>(w);
+  } else { *lo = e4m3_to_half2(w, 0); *hi = e4m3_to_half2(w, 1); }
+}
+template <int TYPE>
+__device__ __forceinline__ void value_pairs(uint32_t w, uint32_t* even, uint32_t* odd) {
+  if constexpr (TYPE == RELAXKV_INT8) {
+    w ^= 0x80808080u;
+    *even = int8_to_half2<0x4240>(w); *odd = int8_to_half2<0x4341>(w);
+  } else {
+    w = __byte_perm(w, 0, 0x3120);
+    *even = e4m3_to_half2(w, 0); *odd = e4m3_to_half2(w, 1);
+  }
+}
+
+__device__ __forceinline__ float max_over_tokens(float x) {              // lanes of one column
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+}
+__device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
+
+// Rows and tokens of a sequence; rows 0: none to work on.
+struct SeqRows { int first, n, len; };
+__device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, bool tell, DeviceStatus* st) {
+  SeqRows s = {a.row_cu[seq], 0, 0};
+  const int end = a.row_cu[seq + 1];
+  if (s.first < 0 || end < s.first || end > a.n_rows) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, end, seq);
+    return s;
+  }
+  if (end == s.first) return s;
+  s.len = a.row_len[end - 1];
+  if (s.len < 0 || s.len > a.max_len || s.len > ((long long)a.table_width << a.block_shift)) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, s.len, seq);
+    return s;
+  }
+  s.n = end - s.first;
+  return s;
+}
+// Tokens that a row of a sequence sees; -1: the row is left alone.
+__device__ __forceinline__ int row_tokens(const QuantAttnArgs& a, int seq, const SeqRows& s, long long row, bool tell, DeviceStatus* st) {
+  const int rs = a.row_seq[row], len = a.row_len[row];
+  if (rs == seq && len >= 0 && len <= s.len) return len;
+  if (tell && rs != -1) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, rs == seq ? len : rs, (int)row);
+  return -1;
+}
+
+__device__ __forceinline__ int tiles_of(int len) { return max(1, (int)(((long long)len + kQaTile - 1) / kQaTile)); }      // (one without tokens writes the zeros)
+
+// What is known of a column: maxima of the scores and of scores + exponents of the values (in log2 units), sum of the weights.
+struct ColStats { float m, mp, z; };
+
+template <int D, int TYPE, int NT, bool WHOLE>
+__global__ void __launch_bounds__(kQaThreads, 2)
+quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
+  using L = QaSmem<D>;
+  constexpr int kCols = 8 * NT, kChunks = D / 16;                     // columns of the block; 16-dim pieces of a head
+  constexpr bool kQInRegs = NT <= 2;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ ColStats stats_s[kQaWarps][kCols];
+  __shared__ int len_s[kCols];
+  __shared__ float qscale_s[kCols];
+  __shared__ __align__(16) uint2 q_s[kQInRegs ? 1 : kChunks][kQInRegs ? 1 : NT][32];
+  __shared__ long long sums_s[kQaWarps];
+  __shared__ long long start_s;
+  __shared__ int seq_s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const uint32_t ring = ptx::smem_u32(smem) + warp * L::kWarp;
+  uint8_t* ring_ptr = smem + warp * L::kWarp;
+  const int G = a.G, rpt = a.rows_per_tile, bs_mask = (1 << a.block_shift) - 1;
+  griddep_wait();
+
+  // ---- this block's share ----
+  int seq = 0;
+  SeqRows s = {0, 0, 0};
+  long long f = 0, f1 = 1, per = 1, seq_start = 0;                    // units of the call: where the block is, where it ends, share, first unit of the sequence
+  int hd = 0, tile = 0;
+  if constexpr (WHOLE) {                                              // a block per row and KV head: the first of a tile's rows takes them all
+    const long long row = blockIdx.x / a.Hkv;
+    hd = (int)(blockIdx.x - row * a.Hkv);
+    seq = a.row_seq[row];
+    bool mine = row < a.row_cu[a.n_seq] && seq != -1;
+    if (mine && (seq < 0 || seq >= a.n_seq)) {
+      if (tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, seq, (int)row);
+      mine = false;
+    }
+    if (!mine) return;
+    s = rows_of(a, seq, tid == 0 && hd == 0, st);
+    if (s.n == 0) return;
+    if (row < s.first || row >= s.first + s.n) {
+      if (tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, seq, (int)row);
+      return;
+    }
+    tile = (int)(row - s.first) / rpt;
+    for (long long r = s.first + (long long)tile * rpt; r < row; ++r)
+      if (a.row_seq[r] == seq) return;
+  } else {
+    const int per_thread = (a.n_seq + kQaThreads - 1) / kQaThreads, i0 = tid * per_thread, i1 = min(a.n_seq, i0 + per_thread);
+    auto units = [&](int i, bool tell) -> long long {
+      const SeqRows x = rows_of(a, i, tell, st);
+      return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * tiles_of(x.len);
+    };
+    long long mine = 0;
+    for (int i = i0; i < i1; ++i) mine += units(i, blockIdx.x == 0);
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 31) sums_s[warp] = upto;
+    __syncthreads();
+    long long all = 0;
+#pragma unroll
+    for (int w = 0; w < kQaWarps; ++w) {
+      if (w < warp) upto += sums_s[w];
+      all += sums_s[w];
+    }
+    per = max((all + gridDim.x - 1) / gridDim.x, (long long)kQaLeastTiles);
+    f = blockIdx.x * per;
+    f1 = min(all, f + per);
+    if (f >= f1) {
+      if (tid == 0) a.chain[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      return;
+    }
+    if (f >= upto - mine && f < upto) {                               // the share begins in one of this thread's sequences
+      long long at = upto - mine;
+      int i = i0;
+      for (long long n = units(i, false); f >= at + n && i + 1 < i1; n = units(i, false)) { at += n; ++i; }
+      seq_s = i;
+      start_s = at;
+    }
+    __syncthreads();
+    seq = seq_s;
+    seq_start = start_s;
+    s = rows_of(a, seq, false, st);
+  }
+
+  while (true) {
+    // ---- the task: (sequence, KV head, row tile), its 32-token tiles [j0, j1) ----
+    const int tiles = tiles_of(s.len), row_tiles = (s.n + rpt - 1) / rpt;
+    int j0 = 0, j1 = tiles;
+    long long task_start = 0;
+    if constexpr (!WHOLE) {
+      const long long task = (f - seq_start) / tiles;
+      task_start = seq_start + task * tiles;
+      hd = (int)(task / row_tiles);
+      tile = (int)(task - (long long)hd * row_tiles);
+      j0 = (int)(f - task_start);
+      j1 = (int)min((long long)tiles, j0 + (f1 - f));
+    }
+    const long long row_first = s.first + (long long)tile * rpt;
+    const int rows_here = min(rpt, s.n - tile * rpt), cols = rows_here * G;
+    if (tid < kCols) {
+      const int r = tid / G;
+      len_s[tid] = tid < cols ? row_tokens(a, seq, s, row_first + r, tid % G == 0 && hd == 0 && j0 == 0, st) : -1;
+    }
+
+    // ---- copies: lane l has piece l % (D / 16) of every (512 / D)-th token; block numbers of sixteen tiles at a time, one lane each half ----
+    const int* pages = a.table + seq * a.table_stride;
+    constexpr int kPieces = D / 16, kTokensAtOnce = 32 / kPieces, kCopies = 16 / kTokensAtOnce;
+    const int my_token = lane / kPieces, my_piece = lane % kPieces;
+    const uint8_t *k_lane = a.k + hd * a.head_stride + my_token * a.token_stride + my_piece * 16, *v_lane = a.v + (k_lane - a.k);
+    const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kQaWarps - 1) / kQaWarps : 0;        // this warp's tiles: j0 + warp, + 4, ..
+    int page = 0;
+    auto issue = [&](int it) {
+      if ((it & 15) == 0) {
+        const int mine = it + (lane >> 1);
+        page = 0;
+        if (mine < n_mine) {                                          // (its tokens' numbers fit 32 bits: see the host's limit)
+          const int t = (j0 + warp + mine * kQaWarps) * kQaTile + (lane & 1) * 16;
+          if (t < s.len) page = pages[t >> a.block_shift];
+        }
+      }
+      const uint32_t dst = ring + (it % kQaStages) * L::kStage;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h);
+        if (it >= n_mine) continue;
+        const int t = (j0 + warp + it * kQaWarps) * kQaTile + h * 16, left = s.len - t;
+        const bool there = left > 0 && id >= 0 && id < a.n_blocks;
+        if (left > 0 && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+        const int valid = there ? min(16, left) : 0;
+        const long long at = there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const int token = my_token + i * kTokensAtOnce, bytes = token < valid ? 16 : 0;
+          const long long off = at + (long long)(bytes ? i * kTokensAtOnce : -my_token) * a.token_stride;      // (nothing is read where bytes is 0: the block's first token)
+          const uint32_t d = dst + h * L::kHalf + swizzled<D>(token, my_piece);
+          copy_16(d, k_lane + off, bytes);
+          copy_16(d + L::kV, v_lane + off, bytes);
+        }
+        if (lane < 2) {
+          const uint32_t e = L::kExp + lane * 32 + h * 16;
+          if (there) copy_16(dst + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + hd) << a.block_shift) + (t & bs_mask)), 16);
+          else *reinterpret_cast<uint4*>(ring_ptr + (it % kQaStages) * L::kStage + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
+        }
+      }
+    };
+#pragma unroll
+    for (int it = 0; it < kQaStages - 1; ++it) { issue(it); copies_commit(); }
+
+    // ---- the columns of Q as fragments: 16-dim piece c, dims 4 tig .. 4 tig + 3 of it, as fp16 times 2^-exponent ----
+    uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];
+    if (kQInRegs || warp == 0) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int col = nt * 8 + gid, r = col / G;
+        const uint16_t* q = a.q + ((row_first + r) * a.H + hd * G + col - r * G) * D + tig * 4;
+        uint2 raw[kChunks];
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          raw[c] = col < cols ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
+          top = max(top, max(max(raw[c].x & 0x7fffu, (raw[c].x >> 16) & 0x7fffu), max(raw[c].y & 0x7fffu, (raw[c].y >> 16) & 0x7fffu)));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const bool finite = top < 0x7f80u;
+        const int e = max((int)(top >> 7) - 127 - 14, -120);          // the largest element comes to lie in [2^14, 2^15)
+        const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.f;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          uint2 h2 = make_uint2(0u, 0u);
+          if (finite) {
+            const __half2 x = __floats2half2_rn(__uint_as_float(raw[c].x << 16) * inv, __uint_as_float(raw[c].x & 0xffff0000u) * inv);
+            const __half2 y = __floats2half2_rn(__uint_as_float(raw[c].y << 16) * inv, __uint_as_float(raw[c].y & 0xffff0000u) * inv);
+            h2 = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+          }
+          if constexpr (kQInRegs) qf[c][nt] = h2;
+          else q_s[c][nt][lane] = h2;
+        }
+        if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
+      }
+    }
+    __syncthreads();
+    float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
+    int seen[NT][2], seen_all = s.len;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int col = nt * 8 + tig * 2 + x;
+        qs[nt][x] = qscale_s[col];
+        seen[nt][x] = len_s[col];
+        if (col < cols) seen_all = min(seen_all, seen[nt][x]);
+        m[nt][x] = mp[nt][x] = -INFINITY;
+        z[nt][x] = 0.f;
+      }
+    seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 1));
+    seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 2));
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) o[c][nt][0] = o[c][nt][1] = o[c][nt][2] = o[c][nt][3] = 0.f;
+
+    for (int it = 0; it < n_mine; ++it) {
+      __syncwarp();                                                   // everyone is through with the stage that is filled now
+      issue(it + kQaStages - 1);
+      copies_commit();
+      copies_wait<kQaStages - 1>();
+      __syncwarp();
+      const uint32_t kt = ring + (it % kQaStages) * L::kStage, vt = kt + L::kV;
+      const int8_t* exps = reinterpret_cast<const int8_t*>(ring_ptr + (it % kQaStages) * L::kStage + L::kExp);
+      const int t0 = (j0 + warp + it * kQaWarps) * kQaTile;
+      // ---- S^T = K Q^T: 16 tokens by the columns, twice ----
+      float sc[2][NT][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[h][nt][0] = sc[h][nt][1] = sc[h][nt][2] = sc[h][nt][3] = 0.f;
+#pragma unroll
+        for (int c4 = 0; c4 < kChunks / 4; ++c4) {
+          uint32_t lo[4], hi[4];                                      // tokens 0 to 7, 8 to 15
+          const int t = lane & 7, c = c4 * 4 + (lane >> 3);
+          load_matrices(lo, kt + h * L::kHalf + swizzled<D>(t, c));
+          load_matrices(hi, kt + h * L::kHalf + swizzled<D>(t + 8, c));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t frag[4];
+            key_pairs<TYPE>(lo[i], &frag[0], &frag[2]);
+            key_pairs<TYPE>(hi[i], &frag[1], &frag[3]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              uint2 b;
+              if constexpr (kQInRegs) b = qf[c4 * 4 + i][nt]; else b = q_s[c4 * 4 + i][nt][lane];
+              mma_f16(sc[h][nt], frag, b.x, b.y);
+            }
+          }
+        }
+      }
+      // ---- scores of this lane: tokens gid (+ 8) of either half, columns 2 tig (+ 1) ----
+      float ve[2][2];
+      const bool all_seen = t0 + kQaTile <= seen_all;
+      bool some_missing = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int at = h * 16 + y * 8 + gid, ek = exps[at], ev = exps[32 + at];
+          const float ks = exp_scale(ek);
+          ve[h][y] = ev == kExpNone ? __uint_as_float(0x7fc00000u) : (float)ev;
+          some_missing |= ek == kNoKey;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) sc[h][nt][2 * y + x] = sc[h][nt][2 * y + x] * qs[nt][x] * ks;
+        }
+      if (!all_seen || __any_sync(0xffffffffu, some_missing)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int at = h * 16 + y * 8 + gid;
+            const bool gone = exps[at] == kNoKey;
+            if (gone) ve[h][y] = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                if (gone || t0 + at >= seen[nt][x]) sc[h][nt][2 * y + x] = -INFINITY;
+          }
+      }
+      uint32_t pb[2][NT][2];                                          // P^T as fragments: tokens 0 to 7, 8 to 15 of a half
+      bool grown = false;
+      float alpha[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float w[2][2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float ms = fmaxf(fmaxf(sc[0][nt][x], sc[0][nt][2 + x]), fmaxf(sc[1][nt][x], sc[1][nt][2 + x]));
+          float mt = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const float v = sc[h][nt][2 * y + x];
+              w[h][y][x] = v == -INFINITY ? v : v + ve[h][y];         // (the exponent of a token that is not seen may be that of NaN)
+              mt = fmaxf(mt, w[h][y][x]);
+            }
+          const float m_new = fmaxf(m[nt][x], max_over_tokens(ms)), mp_new = fmaxf(mp[nt][x], max_over_tokens(mt));
+          const float ref = no_inf(m_new), refp = no_inf(mp_new) - kPShift;
+          z[nt][x] *= ptx::fast_exp2(m[nt][x] - ref);
+          alpha[nt][x] = ptx::fast_exp2(mp[nt][x] - no_inf(mp_new));
+          grown |= mp_new > mp[nt][x];
+          m[nt][x] = m_new; mp[nt][x] = mp_new;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              z[nt][x] += ptx::fast_exp2(sc[h][nt][2 * y + x] - ref);
+              w[h][y][x] = ptx::fast_exp2(w[h][y][x] - refp);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const __half2 p = __floats2half2_rn(w[h][y][0], w[h][y][1]);
+            pb[h][nt][y] = transposed(*reinterpret_cast<const uint32_t*>(&p));
+          }
+      }
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            o[c][nt][0] *= alpha[nt][0]; o[c][nt][1] *= alpha[nt][1]; o[c][nt][2] *= alpha[nt][0]; o[c][nt][3] *= alpha[nt][1];
+          }
+      }
+      // ---- O^T += V^T P^T: rows of the fragment are dims 2 gid, then 2 gid + 1 of a 16-dim piece ----
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c2 = 0; c2 < kChunks / 2; ++c2) {
+          uint32_t w[4];                                              // (tokens 0 to 7, 8 to 15) of two pieces
+          load_matrices_trans(w, vt + h * L::kHalf + swizzled<D>(((lane >> 3) & 1) * 8 + (lane & 7), c2 * 2 + (lane >> 4)));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t frag[4];
+            value_pairs<TYPE>(w[2 * i], &frag[0], &frag[1]);
+            value_pairs<TYPE>(w[2 * i + 1], &frag[2], &frag[3]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(o[c2 * 2 + i][nt], frag, pb[h][nt][0], pb[h][nt][1]);
+          }
+        }
+    }
+    copies_wait<0>();
+    // ---- the warps' results, added up in their order: every warp adds up a quarter of the pieces, the others' come through the rings' place ----
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 4);
+        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 8);
+        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 16);
+        if (gid == 0) stats_s[warp][nt * 8 + tig * 2 + x] = {m[nt][x], mp[nt][x], z[nt][x]};
+      }
+    __syncthreads();                                                  // the rings are free
+    constexpr int kOwn = kChunks / kQaWarps;
+    static_assert(kQaWarps * kChunks * NT * 512 <= L::kTotal, "every warp's result fits the rings");
+    float4* all_s = reinterpret_cast<float4*>(smem);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        if (c / kOwn != warp) all_s[((warp * kChunks + c) * NT + nt) * 32 + lane] = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
+    __syncthreads();
+    const bool whole = WHOLE || (j0 == 0 && j1 == tiles);
+    const int slot = 2 * (int)blockIdx.x + (j0 == 0 ? 1 : 0);         // a task's first part, a later one
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float big[2], bigp[2], zs[2], wgt[kQaWarps][2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int col = nt * 8 + tig * 2 + x;
+        big[x] = bigp[x] = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kQaWarps; ++w) { big[x] = fmaxf(big[x], stats_s[w][col].m); bigp[x] = fmaxf(bigp[x], stats_s[w][col].mp); }
+        zs[x] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kQaWarps; ++w) {
+          zs[x] = fmaf(stats_s[w][col].z, ptx::fast_exp2(stats_s[w][col].m - no_inf(big[x])), zs[x]);
+          wgt[w][x] = ptx::fast_exp2(stats_s[w][col].mp - no_inf(bigp[x]));
+        }
+        if (!whole && warp == 0 && gid == 0) {
+          float* p = a.part_s + ((long long)slot * kQaColsMost + col) * 3;
+          p[0] = big[x]; p[1] = bigp[x]; p[2] = zs[x];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        if (i / kOwn != warp) continue;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kQaWarps; ++w) {
+          const float4 v = w == warp ? make_float4(o[i][nt][0], o[i][nt][1], o[i][nt][2], o[i][nt][3]) : all_s[((w * kChunks + i) * NT + nt) * 32 + lane];
+          acc[0] = fmaf(v.x, wgt[w][0], acc[0]); acc[1] = fmaf(v.y, wgt[w][1], acc[1]);
+          acc[2] = fmaf(v.z, wgt[w][0], acc[2]); acc[3] = fmaf(v.w, wgt[w][1], acc[3]);
+        }
+        if (!whole) {
+          *reinterpret_cast<float4*>(a.part_o + (((long long)slot * kChunks + i) * NT + nt) * 128 + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          continue;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int col = nt * 8 + tig * 2 + x, r = col / G;
+          if (col >= cols || len_s[col] < 0) continue;
+          const bool none = zs[x] == 0.f;                             // no token at all, or none above -inf (NaN stays NaN)
+          const float norm = none ? 0.f : 1.f / (zs[x] * 16384.f), grow = none ? 0.f : exp2f(bigp[x] - big[x]);
+          const long long at = (row_first + r) * a.H + hd * G + col - r * G;
+          *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + i * 16 + gid * 2) = __floats2bfloat162_rn(acc[x] * norm * grow, acc[2 + x] * norm * grow);
+          if (i == 0 && gid == 0 && a.lse_out)
+            a.lse_out[(long long)(hd * G + col - r * G) * a.n_rows + row_first + r] = none ? -INFINITY : (big[x] + log2f(zs[x])) * 0.6931471805599453f;
+        }
+      }
+    }
+    if constexpr (WHOLE) break;
+    else {
+      f += j1 - j0;
+      if (f >= f1) {
+        if (tid == 0)                                                 // a task that goes on in the next blocks
+          a.chain[blockIdx.x] = j1 < tiles ? make_int4(seq, tile * a.Hkv + hd, (int)(task_start / per), (int)((task_start + tiles - 1) / per)) : make_int4(-1, 0, 0, 0);
+        break;
+      }
+      if (f - seq_start >= (long long)tiles * row_tiles * a.Hkv) {
+        seq_start = f;
+        do s = rows_of(a, ++seq, false, st); while (s.n == 0 && seq + 1 < a.n_seq);      // (there is one: the share goes on)
+      }
+      __syncthreads();                                                // what the next task writes into shared memory has been read
+    }
+  }
+  __syncthreads();
+  griddep_launch();
+}
+
+// The parts of tasks that went over several blocks, joined in their order.  The blocks c0 <= b < c1 that such a task leaves share its (16 dims, 8 columns) units; a block's
+// warps share a unit's parts where there are fewer units than warps.
+constexpr int kQjWarps = 16, kQjBatch = 8;
+template <int D, int NT>
+__global__ void __launch_bounds__(kQjWarps * 32)
+quantized_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
+  constexpr int kChunks = D / 16, kUnits = kChunks * NT;
+  struct Joined { float m[2], mp[2], z[2], acc[4]; };
+  __shared__ Joined join_s[kQjWarps][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, G = a.G;
+  griddep_launch();
+  griddep_wait();
+  const int4 ch = a.chain[blockIdx.x];
+  if (ch.x < 0) return;
+  const int seq = ch.x, hd = ch.y % a.Hkv, tile = ch.y / a.Hkv, c0 = ch.z, parts = ch.w - ch.z + 1;
+  const int blocks = parts - 1, me = (int)blockIdx.x - c0, mine = (kUnits - me + blocks - 1) / blocks;      // units me, me + blocks, ..
+  if (me >= kUnits) return;
+  const int groups = max(1, kQjWarps / mine);                         // warps of a unit
+  for (int u0 = 0; u0 < mine; u0 += kQjWarps / groups) {
+    const int in = warp / groups, g = warp - in * groups, u = me + (u0 + in) * blocks;
+    const bool has = in < kQjWarps / groups && u0 + in < mine;
+    const int c = has ? u / NT : 0, nt = has ? u - c * NT : 0;
+    Joined r = {{-INFINITY, -INFINITY}, {-INFINITY, -INFINITY}, {0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int p0 = g; has && p0 < parts; p0 += groups * kQjBatch) {
+      float sv[kQjBatch][6];
+      float4 v[kQjBatch];
+#pragma unroll
+      for (int b = 0; b < kQjBatch; ++b) {
+        const int p = p0 + b * groups;
+        sv[b][0] = sv[b][1] = sv[b][3] = sv[b][4] = -INFINITY;
+        sv[b][2] = sv[b][5] = 0.f;
+        v[b] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p < parts) {
+          const long long slot = p == 0 ? 2 * c0 + 1 : 2 * (c0 + p);
+          const float* sp = a.part_s + (slot * kQaColsMost + nt * 8 + tig * 2) * 3;
+#pragma unroll
+          for (int e = 0; e < 6; e += 2) {
+            const float2 y = *reinterpret_cast<const float2*>(sp + e);
+            sv[b][e] = y.x; sv[b][e + 1] = y.y;
+          }
+          v[b] = *reinterpret_cast<const float4*>(a.part_o + ((slot * kChunks + c) * NT + nt) * 128 + lane * 4);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float m = r.m[x], mp = r.mp[x];
+#pragma unroll
+        for (int b = 0; b < kQjBatch; ++b) { m = fmaxf(m, sv[b][3 * x]); mp = fmaxf(mp, sv[b][3 * x + 1]); }
+        r.z[x] *= ptx::fast_exp2(r.m[x] - no_inf(m));
+        const float al = ptx::fast_exp2(r.mp[x] - no_inf(mp));
+        r.acc[x] *= al; r.acc[2 + x] *= al;
+        r.m[x] = m; r.mp[x] = mp;
+#pragma unroll
+        for (int b = 0; b < kQjBatch; ++b) {
+          r.z[x] = fmaf(sv[b][3 * x + 2], ptx::fast_exp2(sv[b][3 * x] - no_inf(m)), r.z[x]);
+          const float w = ptx::fast_exp2(sv[b][3 * x + 1] - no_inf(mp));
+          r.acc[x] = fmaf(w, x ? v[b].y : v[b].x, r.acc[x]);
+          r.acc[2 + x] = fmaf(w, x ? v[b].w : v[b].z, r.acc[2 + x]);
+        }
+      }
+    }
+    if (groups > 1) {                                                 // (then this loop has one trip)
+      join_s[warp][lane] = r;
+      __syncthreads();
+      if (has && g == 0) {
+        for (int y = 1; y < groups; ++y) {
+          const Joined& n = join_s[warp + y][lane];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float m = fmaxf(r.m[x], n.m[x]), mp = fmaxf(r.mp[x], n.mp[x]);
+            const float wr = ptx::fast_exp2(r.mp[x] - no_inf(mp)), wn = ptx::fast_exp2(n.mp[x] - no_inf(mp));
+            r.z[x] = r.z[x] * ptx::fast_exp2(r.m[x] - no_inf(m)) + n.z[x] * ptx::fast_exp2(n.m[x] - no_inf(m));
+            r.acc[x] = r.acc[x] * wr + n.acc[x] * wn;
+            r.acc[2 + x] = r.acc[2 + x] * wr + n.acc[2 + x] * wn;
+            r.m[x] = m; r.mp[x] = mp;
+          }
+        }
+      }
+    }
+    if (!has || g != 0) continue;
+    const SeqRows s = rows_of(a, seq, false, st);
+    const long long row_first = s.first + (long long)tile * a.rows_per_tile;
+    const int cols = min(a.rows_per_tile, s.n - tile * a.rows_per_tile) * G;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int col = nt * 8 + tig * 2 + x, rr = col / G, head = hd * G + col - rr * G;
+      if (col >= cols || row_tokens(a, seq, s, row_first + rr, false, st) < 0) continue;
+      const bool none = r.z[x] == 0.f;
+      const float norm = none ? 0.f : 1.f / (r.z[x] * 16384.f), grow = none ? 0.f : exp2f(r.mp[x] - r.m[x]);
+      *reinterpret_cast<__nv_bfloat162*>(a.out + ((row_first + rr) * a.H + head) * D + c * 16 + gid * 2) =
+          __floats2bfloat162_rn(r.acc[x] * norm * grow, r.acc[2 + x] * norm * grow);
+      if (c == 0 && gid == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row_first + rr] = none ? -INFINITY : (r.m[x] + log2f(r.z[x])) * 0.6931471805599453f;
+    }
+  }
+}
+
+struct QuantWs { size_t part_o, part_s, chain, total; };
+static QuantWs quant_ws(int D) {
+  QuantWs w{};
+  size_t at = 0;
+  w.part_o = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * D * 4, 256);
+  w.part_s = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * 12, 256);
+  w.chain = at; at = align_up(at + (size_t)kQaBlocks * 16, 256);
+  w.total = at;
+  return w;
+}
+
+template <int D, int TYPE, int NT, bool WHOLE>
+static cudaError_t launch_attend(const QuantAttnArgs& a, long long blocks, DeviceStatus* st, cudaStream_t stream) {
+  static std::atomic<int> attr_done[kMaxDevices];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+  auto kern = quantized_attention_kernel<D, TYPE, NT, WHOLE>;
+  if (!attr_done[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, QaSmem<D>::kTotal);
+    if (e != cudaSuccess) return e;
+    attr_done[dev].store(1, std::memory_order_release);
+  }
+  return launch_chained(kern, dim3((unsigned)blocks), kQaThreads, QaSmem<D>::kTotal, stream, a, st);
+}
+template <int D, int NT>
+static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
+  const long long blocks = whole ? a.n_rows * a.Hkv : std::min(kQaBlocks, 2 * sms);
+  cudaError_t e;
+  if (type == RELAXKV_INT8) e = whole ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream);
+  else e = whole ? launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
+  if (e != cudaSuccess || whole) return e;
+  auto kern = quantized_join_kernel<D, NT>;
+  return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a, st);
+}
+template <int D>
+static cudaError_t launch_attend_d(int nt, int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
+  return nt == 1 ? launch_attend_n<D, 1>(type, whole, a, sms, st, stream)
+                 : nt == 2 ? launch_attend_n<D, 2>(type, whole, a, sms, st, stream) : launch_attend_n<D, 4>(type, whole, a, sms, st, stream);
+}
+
+}  // namespace relaxkv
+
+using namespace relaxkv;
+
+extern "C" size_t relaxkv_quantized_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128)) return 0;
+  return quant_ws(head_dim).total;
+}
+
+extern "C" relaxkv_status relaxkv_quantized_attention(
+    const relaxkv_quantized_cache* store, const relaxkv_continuation_rows* r, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale,
+    const void* q, void* out, float* lse_out, void* workspace, size_t workspace_bytes, relaxkv_stream stream) {
+  RELAXKV_RANGE("relaxkv_quantized_attention");
+  if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || !(softmax_scale > 0.f)) return RELAXKV_ERR_INVALID_ARG;
+  if (n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  const relaxkv_status rc = check_quantized(store, n_kv_heads, head_dim);
+  if (rc != RELAXKV_OK) return rc;
+  if (!r || !r->row_cu || !r->row_seq || !r->row_len || r->n_seq < 1 || r->n_rows < 0 || r->max_len < 0) return RELAXKV_ERR_INVALID_ARG;
+  if (r->n_seq > kQaSeqsMost || r->max_len > kContTokensMost || r->n_rows > 0x7fffffffLL / (n_q_heads * 2)) return RELAXKV_ERR_UNSUPPORTED_SHAPE;
+  if (r->max_len > 0 && (!r->block_table || r->table_width < 1 || r->table_stride < r->table_width)) return RELAXKV_ERR_INVALID_ARG;
+  if (!q || !out || q == out || !aligned16(q) || !aligned16(out)) return RELAXKV_ERR_INVALID_ARG;
+  const QuantWs ws = quant_ws(head_dim);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return RELAXKV_ERR_INVALID_ARG;
+  if (workspace_bytes < ws.total) return RELAXKV_ERR_WORKSPACE_TOO_SMALL;
+  if (r->n_rows == 0) return RELAXKV_OK;
+  DeviceStatus* st = status_word();
+  const int sms = sm_count_of_current_device();
+  if (!st || sms <= 0) return RELAXKV_ERR_CUDA;
+  QuantAttnArgs a = {};
+  a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse_out = lse_out;
+  a.k = static_cast<const uint8_t*>(store->k); a.v = static_cast<const uint8_t*>(store->v); a.k_exp = store->k_exp; a.v_exp = store->v_exp;
+  a.row_cu = r->row_cu; a.row_seq = r->row_seq; a.row_len = r->row_len; a.table = r->block_table;
+  uint8_t* w = static_cast<uint8_t*>(workspace);
+  a.part_o = reinterpret_cast<float*>(w + ws.part_o); a.part_s = reinterpret_cast<float*>(w + ws.part_s); a.chain = reinterpret_cast<int4*>(w + ws.chain);
+  a.block_stride = store->block_stride; a.token_stride = store->token_stride; a.head_stride = store->head_stride;
+  a.table_stride = r->table_stride; a.n_rows = r->n_rows;
+  a.table_width = r->table_width; a.n_seq = r->n_seq; a.n_blocks = store->n_blocks; a.block_shift = 31 - __builtin_clz((unsigned)store->block_size);
+  a.max_len = r->max_len; a.H = n_q_heads; a.Hkv = n_kv_heads; a.G = n_q_heads / n_kv_heads;
+  a.scale_log2 = softmax_scale * 1.4426950408889634f;
+  // Column tiles by the rows of a sequence, on average: as few as hold them.
+  const long long cols = (long long)a.G * ((r->n_rows + r->n_seq - 1) / r->n_seq);
+  const int nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
+  a.rows_per_tile = 8 * nt / a.G;
+  const bool whole = r->max_len <= 1024 && r->n_rows * a.Hkv <= 0x7fffffffLL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return cuda_ok(head_dim == 128 ? launch_attend_d<128>(nt, store->type, whole, a, sms, st, s) : launch_attend_d<64>(nt, store->type, whole, a, sms, st, s));
+}
