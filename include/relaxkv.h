@@ -658,7 +658,8 @@ size_t relaxkv_quantized_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, 
 /*
  * Attention of a step's rows over their sequence's tokens in the 8-bit store: row r of sequence i sees the first row_len[r] tokens of the blocks block_table[i, ..],
  *   out[r,h,:] = softmax over t < row_len[r] of softmax_scale * <q[r,h,:], K[t]>, times V        (keys and values as the store's bytes stand for them)
- * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits before they meet the values.  Any number of rows to a sequence; a sequence's tokens are
+ * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits, and to 2^-38 of the
+ * row's largest (weight times value's scale), before they meet the values.  Any number of rows to a sequence; a sequence's tokens are
  * read once for 8 / G to 32 / G rows of it, G = n_q_heads / n_kv_heads <= 16.  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
  * n_seq <= 4096; row_len does not fall within a sequence.  A row that sees no token gets zeros and lse = -inf.
  *   q, out  device bf16 [n_rows, n_q_heads, head_dim] (16-byte aligned); lse_out NULL or device fp32 [n_q_heads, n_rows]

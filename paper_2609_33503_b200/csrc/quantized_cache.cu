@@ -184,7 +184,8 @@ turn_rows_kernel(const TurnArgs a, DeviceStatus* st) {
       if (STORE == STORE_BF16 || first < a.H) {
         if (h < total && (STORE == STORE_BF16 || h < a.H)) {
           uint16_t* p = const_cast<uint16_t*>(place(h, a.q_out, a.k_out, nullptr));
-          const uint2 r0 = pack_bf16(f), r1 = pack_bf16(f + 4);
+          const bool changed = turned || a.wq != nullptr;        // (what stays keeps every bit, those of a NaN too)
+          const uint2 r0 = changed ? pack_bf16(f) : lo[u], r1 = changed ? pack_bf16(f + 4) : hi[u];
           if constexpr (HALF) {
             *reinterpret_cast<uint2*>(p + dlo) = r0;
             *reinterpret_cast<uint2*>(p + dhi) = r1;

@@ -56,12 +56,13 @@ def values(v, e):
     return np.where((e == -128)[..., None], np.nan, v * 2.0 ** np.where(e == -128, 0, e)[..., None].astype(np.float64))
 
 
-def attention(q, k, v, lens, scale):
-    """q [rows, H, D], k, v [T, H_kv, D], lens [rows]: (out, lse, sum of weights times |v|, largest sum of |q k| scale)."""
+def attention(q, k, v, lens, scale, v_scale=None):
+    """q [rows, H, D], k, v [T, H_kv, D], lens [rows]: (out, lse, sum of weights times |v|, largest sum of |q k| scale, what weights of 16 bits may lose); v_scale [T, H_kv]: what
+    a value's one stands for."""
     rows, H, D = q.shape
     G = H // k.shape[1] if k.shape[0] else H
     out, mass = np.zeros((rows, H, D)), np.zeros((rows, H, D))
-    lse, most = np.full((H, rows), -np.inf), np.zeros((H, rows))
+    lse, most, lost = np.full((H, rows), -np.inf), np.zeros((H, rows)), np.zeros((H, rows))
     for r in range(rows):
         for h in range(H):
             n = lens[r]
@@ -74,15 +75,19 @@ def attention(q, k, v, lens, scale):
             z = p.sum()
             out[r, h], mass[r, h] = p @ vv / z, p @ np.abs(vv) / z
             lse[h, r], most[h, r] = m + math.log(z), (np.abs(kk) @ np.abs(q[r, h])).max() * scale
-    return out, lse, mass, most
+            if v_scale is not None:
+                lost[h, r] = 2.0 ** -39 * n * 448 * np.nanmax(p / z * v_scale[:n, h // G])
+    return out, lse, mass, most, lost
 
 
-def attention_tolerance(want, lse, mass, most, D):
+def attention_tolerance(want, lse, mass, most, lost, D):
     """(of the output, of lse).  A score is a sum of D exact products in fp32, off by at most D 2^-24 of the sum of their sizes, and rounded a few times behind it: 'a'.
     exp2 and log2 of the hardware: 2^-21 each with the rounding of their arguments' products.  A weight is rounded to fp16 (2^-11); weights are summed in fp32 by 32 and by parts:
-    2^-18 for up to 2^6 roundings of the sum in turn.  The output is rounded to bf16 (2^-8)."""
+    2^-18 for up to 2^6 roundings of the sum in turn.  The output is rounded to bf16 (2^-8).
+    Where scores are off by a, a weight over the sum of all is off by a factor between e^-2a and e^2a.  And fp16 has no steps below 2^-24: with the largest weight times its value's scale at
+    2^14, a weight is off by up to 2^-25 all the same, 2^-39 of that largest, for each of n tokens and values of up to 448 ('lost')."""
     a = (D + 8) * 2.0 ** -24 * most
-    rel = 2.0 ** -11 + 4 * a.T[..., None] + 2.0 ** -18
+    rel = 2.0 ** -11 + np.maximum(4 * a, np.expm1(2 * a)).T[..., None] + 2.0 ** -18
     with np.errstate(invalid="ignore"):
         lse_tol = np.where(np.isfinite(lse), a + 2.0 ** -18 + 2.0 ** -21 * np.abs(np.where(np.isfinite(lse), lse, 0)), 0.0)
-    return rel * mass + 2.0 ** -8 * np.abs(want) + 1e-37, lse_tol
+    return rel * mass + 2.0 ** -8 * np.abs(want) + 2 * lost.T[..., None] + 1e-37, lse_tol

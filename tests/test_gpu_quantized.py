@@ -60,6 +60,11 @@ def store_values(store):
     return out
 
 
+def value_scale(store):
+    """2^exponent of the values, [n_blocks * block, H_kv]."""
+    return 2.0 ** store.v_exp.cpu().numpy().astype(np.float64).transpose(0, 2, 1).reshape(-1, store.heads)
+
+
 def store_bytes(store):
     return [x.view(torch.int8).clone() for x in (store.k, store.v, store.k_exp, store.v_exp)]
 
@@ -323,19 +328,20 @@ def attend(store, lens, new, H, block, seed=0, scale=None, width=None, q=None, g
     run = lambda: B().relaxkv_quantized_attention(store, rows, q, out, ws, lse_out=lse, softmax_scale=scale)
     run()
     kk, vv = store_values(store)
+    vs = value_scale(store)
     wants = []
     for i, t in enumerate(lens):
         slots = (table[i, :have[i], None] * block + np.arange(block)).reshape(-1)[:t].astype(int)
         r = slice(cu[i], cu[i + 1])
-        wants.append(orc.attention(f64(q[r]), kk[slots], vv[slots], row_len[r], scale))
+        wants.append(orc.attention(f64(q[r]), kk[slots], vv[slots], row_len[r], scale, vs[slots]))
     return dict(out=out, lse=lse, wants=wants, cu=cu, left=left, n=n, run=run, q=q, rows=rows, ws=ws, keep=(table,))
 
 
 def check(r, D):
     out, lse = f64(r["out"]), f64(r["lse"])
     assert (out[r["n"]:] == 7).all() and (lse[:, r["n"]:] == 7).all()
-    for (want, want_lse, mass, most), a, b in zip(r["wants"], r["cu"], r["cu"][1:]):
-        tol, lse_tol = orc.attention_tolerance(want, want_lse, mass, most, D)
+    for (want, want_lse, *sizes), a, b in zip(r["wants"], r["cu"], r["cu"][1:]):
+        tol, lse_tol = orc.attention_tolerance(want, want_lse, *sizes, D)
         for j, row in enumerate(range(a, b)):
             if row in r["left"]:
                 assert (out[row] == 7).all() and (lse[:, row] == 7).all()
@@ -558,7 +564,7 @@ def test_graphs_and_streams_share_a_workspace():
     kk, vv = store_values(store)
     slots = (a["keep"][0][0, :313, None] * block + np.arange(block)).reshape(-1)[:1234].astype(int)
     want = orc.attention(f64(a["q"][:1]), kk[slots], vv[slots], [1234], D ** -0.5)
-    none = (np.zeros((1, H, D)), np.full((H, 1), -np.inf), np.zeros((1, H, D)), np.zeros((H, 1)))
+    none = (np.zeros((1, H, D)), np.full((H, 1), -np.inf), np.zeros((1, H, D)), np.zeros((H, 1)), np.zeros((H, 1)))
     check(dict(a, wants=[want, none]), D)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -587,8 +593,8 @@ def test_a_step_as_it_is_used():
     out = torch.empty_like(q)
     B().relaxkv_quantized_attention(ctx, rows, q, out, workspace(H, Hkv, D))
     kk, vv = (x[:n + 1] for x in store_values(ctx))
-    want, lse, mass, most = orc.attention(f64(q), kk, vv, [n + 1], D ** -0.5)
-    assert (np.abs(f64(out) - want) <= orc.attention_tolerance(want, lse, mass, most, D)[0]).all()
+    want, lse, *sizes = orc.attention(f64(q), kk, vv, [n + 1], D ** -0.5)
+    assert (np.abs(f64(out) - want) <= orc.attention_tolerance(want, lse, *sizes, D)[0]).all()
     # against the same in 64 bits without any rounding to 8: a key's or value's step is 2^-6 of its largest element at most, half of that is the error, twice for keys
     ang = lambda x, p: orc.turned(x, None, 0, p, rot.freq.cpu().numpy(), True, 1.0)
     full_k = np.concatenate([ang(f64(k), np.full(n, 500)), ang(f64(kn), [500 + n])])

@@ -56,7 +56,7 @@ def test_oracle_rounds_like_the_type():
 def test_oracle_attention_is_a_softmax():
     g = np.random.default_rng(3)
     q, k, v = g.normal(size=(3, 4, 8)), g.normal(size=(9, 2, 8)), g.normal(size=(9, 2, 8))
-    out, lse, _, _ = orc.attention(q, k, v, [9, 0, 4], 0.5)
+    out, lse, *_ = orc.attention(q, k, v, [9, 0, 4], 0.5)
     kk, vv = torch.tensor(k).repeat_interleave(2, 1)[:4], torch.tensor(v).repeat_interleave(2, 1)[:4]
     s = torch.einsum("hd,thd->ht", torch.tensor(q[2]), kk) * 0.5
     assert np.allclose(out[2], torch.einsum("ht,thd->hd", s.softmax(-1), vv).numpy()) and np.allclose(lse[:, 2], s.logsumexp(-1).numpy())
