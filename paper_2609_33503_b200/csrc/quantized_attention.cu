@@ -17,8 +17,8 @@
 
 namespace relaxkv {
 
-constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaStages = 3, kQaTile = 32;
-constexpr int kQaBlocks = 2 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
+constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaTile = 32;
+constexpr int kQaBlocks = 3 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
 constexpr int kQaLeastTiles = 2 * kQaWarps;      // tiles of a block's share, at least
 constexpr int kQaColsMost = 32;                  // (row, head) columns of a block, at most
 constexpr int kQaSeqsMost = 4096;
@@ -40,19 +40,21 @@ struct QuantAttnArgs {
   float scale_log2;
 };
 
-template <int D>
+template <int D, int NT>
 struct QaSmem {
-  static constexpr int kHalf = 16 * D;                               // bytes of 16 tokens
-  static constexpr int kV = 2 * kHalf, kExp = 4 * kHalf;             // K | V | exponents of K, of V
+  static constexpr int kBlocksPerSm = NT == 1 ? 3 : 2, kStages = NT == 1 ? 2 : 3;
+  static constexpr int kTile = kQaTile * D;                          // bytes of a tile of keys
+  static constexpr int kV = kTile, kExp = 2 * kTile;                 // K | V | exponents of K, of V
   static constexpr int kStage = kExp + 128;
-  static constexpr int kWarp = kQaStages * kStage;
+  static constexpr int kWarp = kStages * kStage;
   static constexpr int kTotal = kQaWarps * kWarp;
 };
 
-// Place of 16-byte piece c of token t (of 16) so that eight tokens' pieces lie in eight different groups of banks.
+// Place of 16-byte piece c of token t of a tile.  The eight rows of a matrix are tokens 4 r + j, so that a lane's four tokens are neighbours (their exponents are one
+// word); the same piece of them lies in eight different groups of banks.
 template <int D>
 __device__ __forceinline__ int swizzled(int t, int c) {
-  return D == 128 ? t * 128 + ((c ^ (t & 7)) << 4) : t * 64 + ((c ^ ((t >> 1) & 3)) << 4);
+  return D == 128 ? t * 128 + ((c ^ ((t >> 2) & 7)) << 4) : ((t & ~1) | ((t ^ (t >> 4)) & 1)) * 64 + ((c ^ ((t >> 2) & 3)) << 4);
 }
 
 __device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {       // bytes 16, or 0: zeros
@@ -131,13 +133,19 @@ __device__ __forceinline__ int row_tokens(const QuantAttnArgs& a, int seq, const
 
 __device__ __forceinline__ int tiles_of(int len) { return max(1, (int)(((long long)len + kQaTile - 1) / kQaTile)); }      // (one without tokens writes the zeros)
 
-// What is known of a column: maxima of the scores and of scores + exponents of the values (in log2 units), sum of the weights.
+// What is known of a column: a maximum of the scores, the reference of scores + exponents of the values (in log2 units), sum of the weights.
 struct ColStats { float m, mp, z; };
 
+__device__ __forceinline__ bool some_byte_below_2(uint32_t w) {
+  const uint32_t x = w & 0xfefefefeu;
+  return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+}
+
 template <int D, int TYPE, int NT, bool WHOLE>
-__global__ void __launch_bounds__(kQaThreads, 2)
+__global__ void __launch_bounds__(kQaThreads, QaSmem<D, NT>::kBlocksPerSm)
 quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
-  using L = QaSmem<D>;
+  using L = QaSmem<D, NT>;
+  constexpr int kStages = L::kStages;
   constexpr int kCols = 8 * NT, kChunks = D / 16;                     // columns of the block; 16-dim pieces of a head
   constexpr bool kQInRegs = NT <= 2;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -148,6 +156,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   __shared__ long long sums_s[kQaWarps];
   __shared__ long long start_s;
   __shared__ int seq_s;
+  __shared__ SeqRows rows_s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * L::kWarp;
   uint8_t* ring_ptr = smem + warp * L::kWarp;
@@ -180,12 +189,13 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       if (a.row_seq[r] == seq) return;
   } else {
     const int per_thread = (a.n_seq + kQaThreads - 1) / kQaThreads, i0 = tid * per_thread, i1 = min(a.n_seq, i0 + per_thread);
-    auto units = [&](int i, bool tell) -> long long {
-      const SeqRows x = rows_of(a, i, tell, st);
-      return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * tiles_of(x.len);
-    };
+    auto units = [&](const SeqRows& x) -> long long { return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * tiles_of(x.len); };
     long long mine = 0;
-    for (int i = i0; i < i1; ++i) mine += units(i, blockIdx.x == 0);
+    SeqRows x = s;                                                    // (the last of this thread's sequences: the only one, mostly)
+    for (int i = i0; i < i1; ++i) {
+      x = rows_of(a, i, blockIdx.x == 0, st);
+      mine += units(x);
+    }
     long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -210,14 +220,21 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     if (f >= upto - mine && f < upto) {                               // the share begins in one of this thread's sequences
       long long at = upto - mine;
       int i = i0;
-      for (long long n = units(i, false); f >= at + n && i + 1 < i1; n = units(i, false)) { at += n; ++i; }
+      if (i + 1 < i1) {
+        x = rows_of(a, i, false, st);
+        for (long long n = units(x); f >= at + n && i + 1 < i1; n = units(x)) {
+          at += n;
+          x = rows_of(a, ++i, false, st);
+        }
+      }
       seq_s = i;
       start_s = at;
+      rows_s = x;
     }
     __syncthreads();
     seq = seq_s;
     seq_start = start_s;
-    s = rows_of(a, seq, false, st);
+    s = rows_s;
   }
 
   while (true) {
@@ -244,10 +261,11 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     const int* pages = a.table + seq * a.table_stride;
     constexpr int kPieces = D / 16, kTokensAtOnce = 32 / kPieces, kCopies = 16 / kTokensAtOnce;
     const int my_token = lane / kPieces, my_piece = lane % kPieces;
-    const uint8_t *k_lane = a.k + hd * a.head_stride + my_token * a.token_stride + my_piece * 16, *v_lane = a.v + (k_lane - a.k);
+    const uint8_t* k_lane = a.k + hd * a.head_stride + my_token * a.token_stride + my_piece * 16;
+    const long long v_off = a.v - a.k, step = kTokensAtOnce * a.token_stride;
     const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kQaWarps - 1) / kQaWarps : 0;        // this warp's tiles: j0 + warp, + 4, ..
     int page = 0;
-    auto issue = [&](int it) {
+    auto issue = [&](int it, int stage) {
       if ((it & 15) == 0) {
         const int mine = it + (lane >> 1);
         page = 0;
@@ -256,33 +274,43 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           if (t < s.len) page = pages[t >> a.block_shift];
         }
       }
-      const uint32_t dst = ring + (it % kQaStages) * L::kStage;
+      if (it >= n_mine) return;
+      const uint32_t dst = ring + stage * L::kStage;
+      const int t0 = (j0 + warp + it * kQaWarps) * kQaTile;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h);
-        if (it >= n_mine) continue;
-        const int t = (j0 + warp + it * kQaWarps) * kQaTile + h * 16, left = s.len - t;
-        const bool there = left > 0 && id >= 0 && id < a.n_blocks;
-        if (left > 0 && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
-        const int valid = there ? min(16, left) : 0;
-        const long long at = there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0;
+        const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h), t = t0 + h * 16;
+        const bool there = t < s.len && (unsigned)id < (unsigned)a.n_blocks;
+        const uint8_t* p = k_lane + (there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0);
+        if (there && s.len - t >= 16) {
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int token = my_token + i * kTokensAtOnce, bytes = token < valid ? 16 : 0;
-          const long long off = at + (long long)(bytes ? i * kTokensAtOnce : -my_token) * a.token_stride;      // (nothing is read where bytes is 0: the block's first token)
-          const uint32_t d = dst + h * L::kHalf + swizzled<D>(token, my_piece);
-          copy_16(d, k_lane + off, bytes);
-          copy_16(d + L::kV, v_lane + off, bytes);
+          for (int i = 0; i < kCopies; ++i) {
+            const uint32_t d = dst + swizzled<D>(my_token + h * 16 + i * kTokensAtOnce, my_piece);
+            copy_16(d, p, 16);
+            copy_16(d + L::kV, p + v_off, 16);
+            p += step;
+          }
+        } else {                                                      // the end of the sequence, or no such block: zeros for what is not there (and nothing is read)
+          if (t < s.len && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+          const int valid = there ? s.len - t : 0;
+#pragma unroll
+          for (int i = 0; i < kCopies; ++i) {
+            const int token = my_token + i * kTokensAtOnce;
+            const uint32_t d = dst + swizzled<D>(token + h * 16, my_piece);
+            const uint8_t* q = token < valid ? p + i * step : a.k;
+            copy_16(d, q, token < valid ? 16 : 0);
+            copy_16(d + L::kV, q + v_off, token < valid ? 16 : 0);
+          }
         }
         if (lane < 2) {
-          const uint32_t e = L::kExp + lane * 32 + h * 16;
-          if (there) copy_16(dst + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + hd) << a.block_shift) + (t & bs_mask)), 16);
-          else *reinterpret_cast<uint4*>(ring_ptr + (it % kQaStages) * L::kStage + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
+          const uint32_t e = stage * L::kStage + L::kExp + lane * 32 + h * 16;
+          if (there) copy_16(ring + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + hd) << a.block_shift) + (t & bs_mask)), 16);
+          else *reinterpret_cast<uint4*>(ring_ptr + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
         }
       }
     };
 #pragma unroll
-    for (int it = 0; it < kQaStages - 1; ++it) { issue(it); copies_commit(); }
+    for (int it = 0; it < kStages - 1; ++it) { issue(it, it); copies_commit(); }
 
     // ---- the columns of Q as fragments: 16-dim piece c, dims 4 tig .. 4 tig + 3 of it, as fp16 times 2^-exponent ----
     uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];
@@ -314,10 +342,12 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           if constexpr (kQInRegs) qf[c][nt] = h2;
           else q_s[c][nt][lane] = h2;
         }
-        if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
+        // (half of it: the scale of a key is made with one more)
+        if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
       }
     }
     __syncthreads();
+    // m and z are this lane's own, of its tokens; mp is the column's: all weights of the column that meet values are 2^(s + e - mp + 14)
     float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
     int seen[NT][2], seen_all = s.len;
 #pragma unroll
@@ -338,15 +368,18 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[c][nt][0] = o[c][nt][1] = o[c][nt][2] = o[c][nt][3] = 0.f;
 
-    for (int it = 0; it < n_mine; ++it) {
+    for (int it = 0, stage = 0, fill = kStages - 1; it < n_mine; ++it) {
       __syncwarp();                                                   // everyone is through with the stage that is filled now
-      issue(it + kQaStages - 1);
+      issue(it + kStages - 1, fill);
       copies_commit();
-      copies_wait<kQaStages - 1>();
+      copies_wait<kStages - 1>();
       __syncwarp();
-      const uint32_t kt = ring + (it % kQaStages) * L::kStage, vt = kt + L::kV;
-      const int8_t* exps = reinterpret_cast<const int8_t*>(ring_ptr + (it % kQaStages) * L::kStage + L::kExp);
+      const uint32_t kt = ring + stage * L::kStage, vt = kt + L::kV;
+      const uint8_t* exps = ring_ptr + stage * L::kStage + L::kExp;
+      fill = stage;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
       const int t0 = (j0 + warp + it * kQaWarps) * kQaTile;
+      const uint32_t ke = *reinterpret_cast<const uint32_t*>(exps + gid * 4) ^ 0x80808080u, ve = *reinterpret_cast<const uint32_t*>(exps + 32 + gid * 4) ^ 0x80808080u;
       // ---- S^T = K Q^T: 16 tokens by the columns, twice ----
       float sc[2][NT][4];
 #pragma unroll
@@ -355,10 +388,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         for (int nt = 0; nt < NT; ++nt) sc[h][nt][0] = sc[h][nt][1] = sc[h][nt][2] = sc[h][nt][3] = 0.f;
 #pragma unroll
         for (int c4 = 0; c4 < kChunks / 4; ++c4) {
-          uint32_t lo[4], hi[4];                                      // tokens 0 to 7, 8 to 15
-          const int t = lane & 7, c = c4 * 4 + (lane >> 3);
-          load_matrices(lo, kt + h * L::kHalf + swizzled<D>(t, c));
-          load_matrices(hi, kt + h * L::kHalf + swizzled<D>(t + 8, c));
+          uint32_t lo[4], hi[4];                                      // tokens 4 r + 2 h, 4 r + 2 h + 1
+          const int t = (lane & 7) * 4 + 2 * h, c = c4 * 4 + (lane >> 3);
+          load_matrices(lo, kt + swizzled<D>(t, c));
+          load_matrices(hi, kt + swizzled<D>(t + 1, c));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t frag[4];
@@ -373,93 +406,86 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           }
         }
       }
-      // ---- scores of this lane: tokens gid (+ 8) of either half, columns 2 tig (+ 1) ----
-      float ve[2][2];
-      const bool all_seen = t0 + kQaTile <= seen_all;
-      bool some_missing = false;
+      // ---- scores of this lane: tokens 4 gid + i, i = 2 h + y, columns 2 tig (+ 1); w: with the exponents of the values ----
+      float vexp[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < 4; ++i) {
+        const float ks = __uint_as_float(__byte_perm(ke, 0, 0x0444 | i << 12) >> 1);         // 2^(e + 1)
+        vexp[i] = __uint_as_float(__byte_perm(ve, 0x4b000000u, 0x7550 | i)) - 8388736.f;     // 2^23 + byte, less 2^23 + 128
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int at = h * 16 + y * 8 + gid, ek = exps[at], ev = exps[32 + at];
-          const float ks = exp_scale(ek);
-          ve[h][y] = ev == kExpNone ? __uint_as_float(0x7fc00000u) : (float)ev;
-          some_missing |= ek == kNoKey;
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) sc[i >> 1][nt][2 * (i & 1) + x] = sc[i >> 1][nt][2 * (i & 1) + x] * qs[nt][x] * ks;
+      }
+      if (__any_sync(0xffffffffu, t0 + kQaTile > seen_all || some_byte_below_2(ke) || some_byte_below_2(ve))) {      // tokens that are not seen, NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = gid * 4 + i, ek = (ke >> (8 * i)) & 255u, ev = (ve >> (8 * i)) & 255u;
+          const bool gone = ek == kNoKey + 128;
+          if (gone) vexp[i] = 0.f;
+          else if (ev == kExpNone + 128) vexp[i] = __uint_as_float(0x7fc00000u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) sc[h][nt][2 * y + x] = sc[h][nt][2 * y + x] * qs[nt][x] * ks;
+            for (int x = 0; x < 2; ++x) {
+              float& v = sc[i >> 1][nt][2 * (i & 1) + x];
+              if (ek == kExpNone + 128) v = __uint_as_float(0x7fc00000u);
+              if (gone || t0 + at >= seen[nt][x]) v = -INFINITY;
+            }
         }
-      if (!all_seen || __any_sync(0xffffffffu, some_missing)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int at = h * 16 + y * 8 + gid;
-            const bool gone = exps[at] == kNoKey;
-            if (gone) ve[h][y] = 0.f;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int x = 0; x < 2; ++x)
-                if (gone || t0 + at >= seen[nt][x]) sc[h][nt][2 * y + x] = -INFINITY;
-          }
       }
-      uint32_t pb[2][NT][2];                                          // P^T as fragments: tokens 0 to 7, 8 to 15 of a half
+      uint32_t pb[2][NT][2];                                          // P^T as fragments: tokens 4 r + 2 h, 4 r + 2 h + 1
+      float w[NT][2][4];
       bool grown = false;
-      float alpha[NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float w[2][2][2];
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          float ms = fmaxf(fmaxf(sc[0][nt][x], sc[0][nt][2 + x]), fmaxf(sc[1][nt][x], sc[1][nt][2 + x]));
-          float mt = -INFINITY;
+          float ms = m[nt][x], mt = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const float v = sc[h][nt][2 * y + x];
-              w[h][y][x] = v == -INFINITY ? v : v + ve[h][y];         // (the exponent of a token that is not seen may be that of NaN)
-              mt = fmaxf(mt, w[h][y][x]);
-            }
-          const float m_new = fmaxf(m[nt][x], max_over_tokens(ms)), mp_new = fmaxf(mp[nt][x], max_over_tokens(mt));
-          const float ref = no_inf(m_new), refp = no_inf(mp_new) - kPShift;
-          z[nt][x] *= ptx::fast_exp2(m[nt][x] - ref);
-          alpha[nt][x] = ptx::fast_exp2(mp[nt][x] - no_inf(mp_new));
-          grown |= mp_new > mp[nt][x];
-          m[nt][x] = m_new; mp[nt][x] = mp_new;
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              z[nt][x] += ptx::fast_exp2(sc[h][nt][2 * y + x] - ref);
-              w[h][y][x] = ptx::fast_exp2(w[h][y][x] - refp);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const __half2 p = __floats2half2_rn(w[h][y][0], w[h][y][1]);
-            pb[h][nt][y] = transposed(*reinterpret_cast<const uint32_t*>(&p));
+          for (int i = 0; i < 4; ++i) {
+            const float v = sc[i >> 1][nt][2 * (i & 1) + x];
+            ms = fmaxf(ms, v);
+            w[nt][x][i] = v == -INFINITY ? v : v + vexp[i];           // (the exponent of a token that is not seen may be that of NaN)
+            mt = fmaxf(mt, w[nt][x][i]);
           }
-      }
+          const float ref = no_inf(ms);
+          float zz = z[nt][x] * ptx::fast_exp2(m[nt][x] - ref);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) zz += ptx::fast_exp2(sc[i >> 1][nt][2 * (i & 1) + x] - ref);
+          z[nt][x] = zz;
+          m[nt][x] = ms;
+          grown |= mt > mp[nt][x] + 1.f;                              // (weights up to 2^15 are fine)
+        }
       if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            o[c][nt][0] *= alpha[nt][0]; o[c][nt][1] *= alpha[nt][1]; o[c][nt][2] *= alpha[nt][0]; o[c][nt][3] *= alpha[nt][1];
+          for (int x = 0; x < 2; ++x) {
+            const float mt = fmaxf(fmaxf(w[nt][x][0], w[nt][x][1]), fmaxf(w[nt][x][2], w[nt][x][3]));
+            const float top = max_over_tokens(mt), now = top > mp[nt][x] + 1.f ? top : mp[nt][x];      // (what its neighbours do is nothing to a column)
+            const float alpha = now == mp[nt][x] ? 1.f : ptx::fast_exp2(mp[nt][x] - now);
+            mp[nt][x] = now;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) { o[c][nt][x] *= alpha; o[c][nt][2 + x] *= alpha; }
           }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float ref0 = no_inf(mp[nt][0]) - kPShift, ref1 = no_inf(mp[nt][1]) - kPShift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __half2 p = __floats2half2_rn(ptx::fast_exp2(w[nt][0][i] - ref0), ptx::fast_exp2(w[nt][1][i] - ref1));
+          pb[i >> 1][nt][i & 1] = transposed(*reinterpret_cast<const uint32_t*>(&p));
+        }
       }
       // ---- O^T += V^T P^T: rows of the fragment are dims 2 gid, then 2 gid + 1 of a 16-dim piece ----
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int c2 = 0; c2 < kChunks / 2; ++c2) {
-          uint32_t w[4];                                              // (tokens 0 to 7, 8 to 15) of two pieces
-          load_matrices_trans(w, vt + h * L::kHalf + swizzled<D>(((lane >> 3) & 1) * 8 + (lane & 7), c2 * 2 + (lane >> 4)));
+          uint32_t w[4];                                              // (tokens 4 r + 2 h, 4 r + 2 h + 1) of two pieces
+          load_matrices_trans(w, vt + swizzled<D>((lane & 7) * 4 + 2 * h + ((lane >> 3) & 1), c2 * 2 + (lane >> 4)));
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             uint32_t frag[4];
@@ -476,6 +502,9 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        const float all = max_over_tokens(m[nt][x]);
+        z[nt][x] *= ptx::fast_exp2(m[nt][x] - no_inf(all));
+        m[nt][x] = all;
         z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 4);
         z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 8);
         z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 16);
@@ -674,15 +703,15 @@ static cudaError_t launch_attend(const QuantAttnArgs& a, long long blocks, Devic
   if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
   auto kern = quantized_attention_kernel<D, TYPE, NT, WHOLE>;
   if (!attr_done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, QaSmem<D>::kTotal);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (QaSmem<D, NT>::kTotal));
     if (e != cudaSuccess) return e;
     attr_done[dev].store(1, std::memory_order_release);
   }
-  return launch_chained(kern, dim3((unsigned)blocks), kQaThreads, QaSmem<D>::kTotal, stream, a, st);
+  return launch_chained(kern, dim3((unsigned)blocks), kQaThreads, (QaSmem<D, NT>::kTotal), stream, a, st);
 }
 template <int D, int NT>
 static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
-  const long long blocks = whole ? a.n_rows * a.Hkv : std::min(kQaBlocks, 2 * sms);
+  const long long blocks = whole ? a.n_rows * a.Hkv : std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
   cudaError_t e;
   if (type == RELAXKV_INT8) e = whole ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream);
   else e = whole ? launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
