@@ -25,6 +25,9 @@ constexpr int kQaSeqsMost = 4096;
 constexpr int kNoKey = -127;                     // exponent in shared memory of a token whose block does not exist
 constexpr float kPShift = 14.f;                  // the largest weight is 2^14
 
+// A task that goes on in the next blocks, as the join finds it: blocks c0 to c1, its first row, KV head, columns, and which of them are written.
+struct __align__(16) Chain { int c0, c1, row, head, cols; uint32_t live; int none[2]; };
+
 struct QuantAttnArgs {
   const uint16_t* q;
   uint16_t* out;
@@ -33,7 +36,7 @@ struct QuantAttnArgs {
   const int8_t *k_exp, *v_exp;
   const int *row_cu, *row_seq, *row_len, *table;
   float *part_o, *part_s;
-  int4* chain;
+  struct Chain* chain;
   long long block_stride, token_stride, head_stride, table_stride, n_rows;
   int table_width, n_seq, n_blocks, block_shift, max_len;
   int H, Hkv, G, rows_per_tile;
@@ -161,6 +164,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   const uint32_t ring = ptx::smem_u32(smem) + warp * L::kWarp;
   uint8_t* ring_ptr = smem + warp * L::kWarp;
   const int G = a.G, rpt = a.rows_per_tile, bs_mask = (1 << a.block_shift) - 1;
+  if (!WHOLE) griddep_launch();                                       // (the join's blocks come as these leave, and wait)
   griddep_wait();
 
   // ---- this block's share ----
@@ -214,7 +218,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     f = blockIdx.x * per;
     f1 = min(all, f + per);
     if (f >= f1) {
-      if (tid == 0) a.chain[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      if (tid == 0) a.chain[blockIdx.x].c0 = -1;
       return;
     }
     if (f >= upto - mine && f < upto) {                               // the share begins in one of this thread's sequences
@@ -573,8 +577,14 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     else {
       f += j1 - j0;
       if (f >= f1) {
-        if (tid == 0)                                                 // a task that goes on in the next blocks
-          a.chain[blockIdx.x] = j1 < tiles ? make_int4(seq, tile * a.Hkv + hd, (int)(task_start / per), (int)((task_start + tiles - 1) / per)) : make_int4(-1, 0, 0, 0);
+        if (warp == 0) {
+          const uint32_t live = __ballot_sync(0xffffffffu, lane < kCols && len_s[lane < kCols ? lane : 0] >= 0);
+          if (lane == 0) {
+            Chain c = {-1, 0, (int)row_first, hd, cols, live, {0, 0}};
+            if (j1 < tiles) { c.c0 = (int)(task_start / per); c.c1 = (int)((task_start + tiles - 1) / per); }
+            a.chain[blockIdx.x] = c;
+          }
+        }
         break;
       }
       if (f - seq_start >= (long long)tiles * row_tiles * a.Hkv) {
@@ -584,26 +594,27 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       __syncthreads();                                                // what the next task writes into shared memory has been read
     }
   }
-  __syncthreads();
-  griddep_launch();
+  if (WHOLE) {
+    __syncthreads();
+    griddep_launch();
+  }
 }
 
 // The parts of tasks that went over several blocks, joined in their order.  The blocks c0 <= b < c1 that such a task leaves share its (16 dims, 8 columns) units; a block's
 // warps share a unit's parts where there are fewer units than warps.
-constexpr int kQjWarps = 16, kQjBatch = 8;
+constexpr int kQjWarps = 4, kQjBatch = 4;
 template <int D, int NT>
 __global__ void __launch_bounds__(kQjWarps * 32)
-quantized_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
+quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
   constexpr int kChunks = D / 16, kUnits = kChunks * NT;
   struct Joined { float m[2], mp[2], z[2], acc[4]; };
   __shared__ Joined join_s[kQjWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, G = a.G;
   griddep_launch();
   griddep_wait();
-  const int4 ch = a.chain[blockIdx.x];
-  if (ch.x < 0) return;
-  const int seq = ch.x, hd = ch.y % a.Hkv, tile = ch.y / a.Hkv, c0 = ch.z, parts = ch.w - ch.z + 1;
-  const int blocks = parts - 1, me = (int)blockIdx.x - c0, mine = (kUnits - me + blocks - 1) / blocks;      // units me, me + blocks, ..
+  const Chain ch = a.chain[blockIdx.x];
+  if (ch.c0 < 0) return;
+  const int parts = ch.c1 - ch.c0 + 1, blocks = parts - 1, me = (int)blockIdx.x - ch.c0, mine = (kUnits - me + blocks - 1) / blocks;      // units me, me + blocks, ..
   if (me >= kUnits) return;
   const int groups = max(1, kQjWarps / mine);                         // warps of a unit
   for (int u0 = 0; u0 < mine; u0 += kQjWarps / groups) {
@@ -617,35 +628,27 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
 #pragma unroll
       for (int b = 0; b < kQjBatch; ++b) {
         const int p = p0 + b * groups;
-        sv[b][0] = sv[b][1] = sv[b][3] = sv[b][4] = -INFINITY;
-        sv[b][2] = sv[b][5] = 0.f;
-        v[b] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p < parts) {
-          const long long slot = p == 0 ? 2 * c0 + 1 : 2 * (c0 + p);
-          const float* sp = a.part_s + (slot * kQaColsMost + nt * 8 + tig * 2) * 3;
+        if (p >= parts) break;
+        const long long slot = p == 0 ? 2 * ch.c0 + 1 : 2 * (ch.c0 + p);
+        const float* sp = a.part_s + (slot * kQaColsMost + nt * 8 + tig * 2) * 3;
 #pragma unroll
-          for (int e = 0; e < 6; e += 2) {
-            const float2 y = *reinterpret_cast<const float2*>(sp + e);
-            sv[b][e] = y.x; sv[b][e + 1] = y.y;
-          }
-          v[b] = *reinterpret_cast<const float4*>(a.part_o + ((slot * kChunks + c) * NT + nt) * 128 + lane * 4);
+        for (int e = 0; e < 6; e += 2) {
+          const float2 y = *reinterpret_cast<const float2*>(sp + e);
+          sv[b][e] = y.x; sv[b][e + 1] = y.y;
         }
+        v[b] = *reinterpret_cast<const float4*>(a.part_o + ((slot * kChunks + c) * NT + nt) * 128 + lane * 4);
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float m = r.m[x], mp = r.mp[x];
+      for (int b = 0; b < kQjBatch; ++b) {
+        if (p0 + b * groups >= parts) break;
 #pragma unroll
-        for (int b = 0; b < kQjBatch; ++b) { m = fmaxf(m, sv[b][3 * x]); mp = fmaxf(mp, sv[b][3 * x + 1]); }
-        r.z[x] *= ptx::fast_exp2(r.m[x] - no_inf(m));
-        const float al = ptx::fast_exp2(r.mp[x] - no_inf(mp));
-        r.acc[x] *= al; r.acc[2 + x] *= al;
-        r.m[x] = m; r.mp[x] = mp;
-#pragma unroll
-        for (int b = 0; b < kQjBatch; ++b) {
-          r.z[x] = fmaf(sv[b][3 * x + 2], ptx::fast_exp2(sv[b][3 * x] - no_inf(m)), r.z[x]);
-          const float w = ptx::fast_exp2(sv[b][3 * x + 1] - no_inf(mp));
-          r.acc[x] = fmaf(w, x ? v[b].y : v[b].x, r.acc[x]);
-          r.acc[2 + x] = fmaf(w, x ? v[b].w : v[b].z, r.acc[2 + x]);
+        for (int x = 0; x < 2; ++x) {
+          const float m = fmaxf(r.m[x], sv[b][3 * x]), mp = fmaxf(r.mp[x], sv[b][3 * x + 1]);
+          r.z[x] = fmaf(sv[b][3 * x + 2], ptx::fast_exp2(sv[b][3 * x] - no_inf(m)), r.z[x] * ptx::fast_exp2(r.m[x] - no_inf(m)));
+          const float al = ptx::fast_exp2(r.mp[x] - no_inf(mp)), w = ptx::fast_exp2(sv[b][3 * x + 1] - no_inf(mp));
+          r.acc[x] = fmaf(w, x ? v[b].y : v[b].x, r.acc[x] * al);
+          r.acc[2 + x] = fmaf(w, x ? v[b].w : v[b].z, r.acc[2 + x] * al);
+          r.m[x] = m; r.mp[x] = mp;
         }
       }
     }
@@ -668,18 +671,15 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       }
     }
     if (!has || g != 0) continue;
-    const SeqRows s = rows_of(a, seq, false, st);
-    const long long row_first = s.first + (long long)tile * a.rows_per_tile;
-    const int cols = min(a.rows_per_tile, s.n - tile * a.rows_per_tile) * G;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int col = nt * 8 + tig * 2 + x, rr = col / G, head = hd * G + col - rr * G;
-      if (col >= cols || row_tokens(a, seq, s, row_first + rr, false, st) < 0) continue;
+      const int col = nt * 8 + tig * 2 + x, rr = col / G, head = ch.head * G + col - rr * G;
+      if (col >= ch.cols || !(ch.live >> col & 1)) continue;
       const bool none = r.z[x] == 0.f;
       const float norm = none ? 0.f : 1.f / (r.z[x] * 16384.f), grow = none ? 0.f : exp2f(r.mp[x] - r.m[x]);
-      *reinterpret_cast<__nv_bfloat162*>(a.out + ((row_first + rr) * a.H + head) * D + c * 16 + gid * 2) =
-          __floats2bfloat162_rn(r.acc[x] * norm * grow, r.acc[2 + x] * norm * grow);
-      if (c == 0 && gid == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row_first + rr] = none ? -INFINITY : (r.m[x] + log2f(r.z[x])) * 0.6931471805599453f;
+      const long long row = ch.row + rr;
+      *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + head) * D + c * 16 + gid * 2) = __floats2bfloat162_rn(r.acc[x] * norm * grow, r.acc[2 + x] * norm * grow);
+      if (c == 0 && gid == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = none ? -INFINITY : (r.m[x] + log2f(r.z[x])) * 0.6931471805599453f;
     }
   }
 }
@@ -690,7 +690,7 @@ static QuantWs quant_ws(int D) {
   size_t at = 0;
   w.part_o = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * D * 4, 256);
   w.part_s = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * 12, 256);
-  w.chain = at; at = align_up(at + (size_t)kQaBlocks * 16, 256);
+  w.chain = at; at = align_up(at + (size_t)kQaBlocks * sizeof(Chain), 256);
   w.total = at;
   return w;
 }
@@ -717,7 +717,7 @@ static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a,
   else e = whole ? launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
   if (e != cudaSuccess || whole) return e;
   auto kern = quantized_join_kernel<D, NT>;
-  return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a, st);
+  return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
 }
 template <int D>
 static cudaError_t launch_attend_d(int nt, int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
@@ -758,7 +758,7 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   a.k = static_cast<const uint8_t*>(store->k); a.v = static_cast<const uint8_t*>(store->v); a.k_exp = store->k_exp; a.v_exp = store->v_exp;
   a.row_cu = r->row_cu; a.row_seq = r->row_seq; a.row_len = r->row_len; a.table = r->block_table;
   uint8_t* w = static_cast<uint8_t*>(workspace);
-  a.part_o = reinterpret_cast<float*>(w + ws.part_o); a.part_s = reinterpret_cast<float*>(w + ws.part_s); a.chain = reinterpret_cast<int4*>(w + ws.chain);
+  a.part_o = reinterpret_cast<float*>(w + ws.part_o); a.part_s = reinterpret_cast<float*>(w + ws.part_s); a.chain = reinterpret_cast<Chain*>(w + ws.chain);
   a.block_stride = store->block_stride; a.token_stride = store->token_stride; a.head_stride = store->head_stride;
   a.table_stride = r->table_stride; a.n_rows = r->n_rows;
   a.table_width = r->table_width; a.n_seq = r->n_seq; a.n_blocks = store->n_blocks; a.block_shift = 31 - __builtin_clz((unsigned)store->block_size);
