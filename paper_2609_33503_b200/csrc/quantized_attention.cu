@@ -19,7 +19,8 @@ namespace relaxkv {
 
 constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaTile = 32;
 constexpr int kQaBlocks = 3 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
-constexpr int kQaLeastTiles = 2 * kQaWarps;      // tiles of a block's share, at least
+constexpr int kQaLeastTiles = kQaWarps;          // tiles of a block's share, at least
+constexpr int kQaTaskUnits = 4;                  // what the start and the end of a task take, in tiles of a block
 constexpr int kQaColsMost = 32;                  // (row, head) columns of a block, at most
 constexpr int kQaSeqsMost = 4096;
 constexpr int kNoKey = -127;                     // exponent in shared memory of a token whose block does not exist
@@ -110,7 +111,8 @@ __device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f :
 
 // Rows and tokens of a sequence; rows 0: none to work on.
 struct SeqRows { int first, n, len; };
-__device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, bool tell, DeviceStatus* st) {
+// guess_len: row_len[guess], read before it is known to be the last row's.
+__device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, int guess, int guess_len, bool tell, DeviceStatus* st) {
   SeqRows s = {a.row_cu[seq], 0, 0};
   const int end = a.row_cu[seq + 1];
   if (s.first < 0 || end < s.first || end > a.n_rows) {
@@ -118,7 +120,7 @@ __device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, bool
     return s;
   }
   if (end == s.first) return s;
-  s.len = a.row_len[end - 1];
+  s.len = end - 1 == guess ? guess_len : a.row_len[end - 1];
   if (s.len < 0 || s.len > a.max_len || s.len > ((long long)a.table_width << a.block_shift)) {
     if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, s.len, seq);
     return s;
@@ -144,6 +146,13 @@ __device__ __forceinline__ bool some_byte_below_2(uint32_t w) {
   return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
 }
 
+__device__ __forceinline__ long long quotient(long long a, long long b) {      // of numbers from 0 on; in 32 bits where these hold them
+  return ((a | b) >> 31) == 0 ? (long long)((int)a / (int)b) : a / b;
+}
+
+// A block's share of a task: (sequence, KV head, row tile) and the 32-token tiles [j0, j1) of it.
+struct Segment { int seq, hd, tile, j0, j1, tiles; SeqRows s; long long task_start; };
+
 template <int D, int TYPE, int NT, bool WHOLE>
 __global__ void __launch_bounds__(kQaThreads, QaSmem<D, NT>::kBlocksPerSm)
 quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
@@ -151,10 +160,11 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   constexpr int kStages = L::kStages;
   constexpr int kCols = 8 * NT, kChunks = D / 16;                     // columns of the block; 16-dim pieces of a head
   constexpr bool kQInRegs = NT <= 2;
+  constexpr bool kAhead = NT <= 2 && !WHOLE;                          // the next task's first copies are asked for before a task's results are added up
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ ColStats stats_s[kQaWarps][kCols];
-  __shared__ int len_s[kCols];
-  __shared__ float qscale_s[kCols];
+  __shared__ int len_s[2][kCols];
+  __shared__ float qscale_s[2][kCols];
   __shared__ __align__(16) uint2 q_s[kQInRegs ? 1 : kChunks][kQInRegs ? 1 : NT][32];
   __shared__ long long sums_s[kQaWarps];
   __shared__ long long start_s;
@@ -167,37 +177,38 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   if (!WHOLE) griddep_launch();                                       // (the join's blocks come as these leave, and wait)
   griddep_wait();
 
-  // ---- this block's share ----
-  int seq = 0;
-  SeqRows s = {0, 0, 0};
-  long long f = 0, f1 = 1, per = 1, seq_start = 0;                    // units of the call: where the block is, where it ends, share, first unit of the sequence
-  int hd = 0, tile = 0;
+  // ---- this block's share: units [f, f1) of the call, `per` to a block; a task counts kQaTaskUnits more than it has tiles, the time that its start and end take ----
+  Segment g = {};
+  long long f = 0, f1 = 0, per = 1, seq_start = 0;
   if constexpr (WHOLE) {                                              // a block per row and KV head: the first of a tile's rows takes them all
     const long long row = blockIdx.x / a.Hkv;
-    hd = (int)(blockIdx.x - row * a.Hkv);
-    seq = a.row_seq[row];
-    bool mine = row < a.row_cu[a.n_seq] && seq != -1;
-    if (mine && (seq < 0 || seq >= a.n_seq)) {
-      if (tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, seq, (int)row);
+    g.hd = (int)(blockIdx.x - row * a.Hkv);
+    g.seq = a.row_seq[row];
+    bool mine = row < a.row_cu[a.n_seq] && g.seq != -1;
+    if (mine && (g.seq < 0 || g.seq >= a.n_seq)) {
+      if (tid == 0 && g.hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
       mine = false;
     }
     if (!mine) return;
-    s = rows_of(a, seq, tid == 0 && hd == 0, st);
-    if (s.n == 0) return;
-    if (row < s.first || row >= s.first + s.n) {
-      if (tid == 0 && hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, seq, (int)row);
+    g.s = rows_of(a, g.seq, -1, 0, tid == 0 && g.hd == 0, st);
+    if (g.s.n == 0) return;
+    if (row < g.s.first || row >= g.s.first + g.s.n) {
+      if (tid == 0 && g.hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
       return;
     }
-    tile = (int)(row - s.first) / rpt;
-    for (long long r = s.first + (long long)tile * rpt; r < row; ++r)
-      if (a.row_seq[r] == seq) return;
+    g.tile = (int)(row - g.s.first) / rpt;
+    for (long long r = g.s.first + (long long)g.tile * rpt; r < row; ++r)
+      if (a.row_seq[r] == g.seq) return;
+    g.tiles = g.j1 = tiles_of(g.s.len);
   } else {
     const int per_thread = (a.n_seq + kQaThreads - 1) / kQaThreads, i0 = tid * per_thread, i1 = min(a.n_seq, i0 + per_thread);
-    auto units = [&](const SeqRows& x) -> long long { return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * tiles_of(x.len); };
+    auto units = [&](const SeqRows& x) -> long long { return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * (tiles_of(x.len) + kQaTaskUnits); };
     long long mine = 0;
-    SeqRows x = s;                                                    // (the last of this thread's sequences: the only one, mostly)
+    SeqRows x = {0, 0, 0};                                            // (the last of this thread's sequences: the only one, mostly)
+    const int each = (int)(a.n_rows / a.n_seq);                       // where all sequences have as many rows, the last one's length comes with the row numbers
     for (int i = i0; i < i1; ++i) {
-      x = rows_of(a, i, blockIdx.x == 0, st);
+      const int guess = max(0, (i + 1) * each - 1);
+      x = rows_of(a, i, guess, a.row_len[guess], blockIdx.x == 0, st);
       mine += units(x);
     }
     long long upto = mine;
@@ -214,7 +225,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       if (w < warp) upto += sums_s[w];
       all += sums_s[w];
     }
-    per = max((all + gridDim.x - 1) / gridDim.x, (long long)kQaLeastTiles);
+    per = max(quotient(all + gridDim.x - 1, gridDim.x), (long long)(kQaTaskUnits + kQaLeastTiles));
     f = blockIdx.x * per;
     f1 = min(all, f + per);
     if (f >= f1) {
@@ -225,10 +236,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       long long at = upto - mine;
       int i = i0;
       if (i + 1 < i1) {
-        x = rows_of(a, i, false, st);
+        x = rows_of(a, i, -1, 0, false, st);
         for (long long n = units(x); f >= at + n && i + 1 < i1; n = units(x)) {
           at += n;
-          x = rows_of(a, ++i, false, st);
+          x = rows_of(a, ++i, -1, 0, false, st);
         }
       }
       seq_s = i;
@@ -236,86 +247,90 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       rows_s = x;
     }
     __syncthreads();
-    seq = seq_s;
+    g.seq = seq_s;
     seq_start = start_s;
-    s = rows_s;
+    g.s = rows_s;
   }
-
-  while (true) {
-    // ---- the task: (sequence, KV head, row tile), its 32-token tiles [j0, j1) ----
-    const int tiles = tiles_of(s.len), row_tiles = (s.n + rpt - 1) / rpt;
-    int j0 = 0, j1 = tiles;
-    long long task_start = 0;
+  // The part of the task at f that belongs to this block (no tiles: its share ends before the task's first).
+  auto cut = [&]() {
     if constexpr (!WHOLE) {
-      const long long task = (f - seq_start) / tiles;
-      task_start = seq_start + task * tiles;
-      hd = (int)(task / row_tiles);
-      tile = (int)(task - (long long)hd * row_tiles);
-      j0 = (int)(f - task_start);
-      j1 = (int)min((long long)tiles, j0 + (f1 - f));
+      g.tiles = tiles_of(g.s.len);
+      const int row_tiles = (g.s.n + rpt - 1) / rpt, task_units = g.tiles + kQaTaskUnits;
+      const long long task = quotient(f - seq_start, task_units);
+      g.task_start = seq_start + task * task_units;
+      g.hd = (int)quotient(task, row_tiles);
+      g.tile = (int)(task - (long long)g.hd * row_tiles);
+      const int o0 = (int)(f - g.task_start), o1 = (int)min((long long)task_units, o0 + (f1 - f));
+      g.j0 = max(0, o0 - kQaTaskUnits);
+      g.j1 = max(0, o1 - kQaTaskUnits);
+      f += o1 - o0;
     }
-    const long long row_first = s.first + (long long)tile * rpt;
-    const int rows_here = min(rpt, s.n - tile * rpt), cols = rows_here * G;
-    if (tid < kCols) {
-      const int r = tid / G;
-      len_s[tid] = tid < cols ? row_tokens(a, seq, s, row_first + r, tid % G == 0 && hd == 0 && j0 == 0, st) : -1;
-    }
+  };
+  cut();
 
-    // ---- copies: lane l has piece l % (D / 16) of every (512 / D)-th token; block numbers of sixteen tiles at a time, one lane each half ----
-    const int* pages = a.table + seq * a.table_stride;
-    constexpr int kPieces = D / 16, kTokensAtOnce = 32 / kPieces, kCopies = 16 / kTokensAtOnce;
-    const int my_token = lane / kPieces, my_piece = lane % kPieces;
-    const uint8_t* k_lane = a.k + hd * a.head_stride + my_token * a.token_stride + my_piece * 16;
-    const long long v_off = a.v - a.k, step = kTokensAtOnce * a.token_stride;
-    const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kQaWarps - 1) / kQaWarps : 0;        // this warp's tiles: j0 + warp, + 4, ..
-    int page = 0;
-    auto issue = [&](int it, int stage) {
-      if ((it & 15) == 0) {
-        const int mine = it + (lane >> 1);
-        page = 0;
-        if (mine < n_mine) {                                          // (its tokens' numbers fit 32 bits: see the host's limit)
-          const int t = (j0 + warp + mine * kQaWarps) * kQaTile + (lane & 1) * 16;
-          if (t < s.len) page = pages[t >> a.block_shift];
+  // ---- copies: lane l has piece l % (D / 16) of every (512 / D)-th token; block numbers of sixteen tiles at a time, one lane each half ----
+  constexpr int kPieces = D / 16, kTokensAtOnce = 32 / kPieces, kCopies = 16 / kTokensAtOnce;
+  const int my_token = lane / kPieces, my_piece = lane % kPieces;
+  const long long v_off = a.v - a.k, step = kTokensAtOnce * a.token_stride;
+  const uint8_t* k_all = a.k + my_token * a.token_stride + my_piece * 16;
+  auto tiles_mine = [&]() { return g.j1 - g.j0 > warp ? (g.j1 - g.j0 - warp + kQaWarps - 1) / kQaWarps : 0; };      // tiles j0 + warp, + 4, ..
+  int page = 0;
+  auto issue = [&](int it, int n_mine, int stage) {
+    if ((it & 15) == 0) {
+      const int mine = it + (lane >> 1);
+      page = 0;
+      if (mine < n_mine) {                                            // (its tokens' numbers fit 32 bits: see the host's limit)
+        const int t = (g.j0 + warp + mine * kQaWarps) * kQaTile + (lane & 1) * 16;
+        if (t < g.s.len) page = a.table[g.seq * a.table_stride + (t >> a.block_shift)];
+      }
+    }
+    if (it >= n_mine) return;
+    const uint8_t* k_lane = k_all + g.hd * a.head_stride;
+    const uint32_t dst = ring + stage * L::kStage;
+    const int t0 = (g.j0 + warp + it * kQaWarps) * kQaTile;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h), t = t0 + h * 16;
+      const bool there = t < g.s.len && (unsigned)id < (unsigned)a.n_blocks;
+      const uint8_t* p = k_lane + (there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0);
+      if (there && g.s.len - t >= 16) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const uint32_t d = dst + swizzled<D>(my_token + h * 16 + i * kTokensAtOnce, my_piece);
+          copy_16(d, p, 16);
+          copy_16(d + L::kV, p + v_off, 16);
+          p += step;
+        }
+      } else {                                                        // the end of the sequence, or no such block: zeros for what is not there (and nothing is read)
+        if (t < g.s.len && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+        const int valid = there ? g.s.len - t : 0;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const int token = my_token + i * kTokensAtOnce;
+          const uint32_t d = dst + swizzled<D>(token + h * 16, my_piece);
+          const uint8_t* q = token < valid ? p + i * step : a.k;
+          copy_16(d, q, token < valid ? 16 : 0);
+          copy_16(d + L::kV, q + v_off, token < valid ? 16 : 0);
         }
       }
-      if (it >= n_mine) return;
-      const uint32_t dst = ring + stage * L::kStage;
-      const int t0 = (j0 + warp + it * kQaWarps) * kQaTile;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h), t = t0 + h * 16;
-        const bool there = t < s.len && (unsigned)id < (unsigned)a.n_blocks;
-        const uint8_t* p = k_lane + (there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0);
-        if (there && s.len - t >= 16) {
-#pragma unroll
-          for (int i = 0; i < kCopies; ++i) {
-            const uint32_t d = dst + swizzled<D>(my_token + h * 16 + i * kTokensAtOnce, my_piece);
-            copy_16(d, p, 16);
-            copy_16(d + L::kV, p + v_off, 16);
-            p += step;
-          }
-        } else {                                                      // the end of the sequence, or no such block: zeros for what is not there (and nothing is read)
-          if (t < s.len && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
-          const int valid = there ? s.len - t : 0;
-#pragma unroll
-          for (int i = 0; i < kCopies; ++i) {
-            const int token = my_token + i * kTokensAtOnce;
-            const uint32_t d = dst + swizzled<D>(token + h * 16, my_piece);
-            const uint8_t* q = token < valid ? p + i * step : a.k;
-            copy_16(d, q, token < valid ? 16 : 0);
-            copy_16(d + L::kV, q + v_off, token < valid ? 16 : 0);
-          }
-        }
-        if (lane < 2) {
-          const uint32_t e = stage * L::kStage + L::kExp + lane * 32 + h * 16;
-          if (there) copy_16(ring + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + hd) << a.block_shift) + (t & bs_mask)), 16);
-          else *reinterpret_cast<uint4*>(ring_ptr + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
-        }
+      if (lane < 2) {
+        const uint32_t e = stage * L::kStage + L::kExp + lane * 32 + h * 16;
+        if (there) copy_16(ring + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + g.hd) << a.block_shift) + (t & bs_mask)), 16);
+        else *reinterpret_cast<uint4*>(ring_ptr + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
       }
-    };
+    }
+  };
+  auto first_copies = [&](int n_mine) {
 #pragma unroll
-    for (int it = 0; it < kStages - 1; ++it) { issue(it, it); copies_commit(); }
+    for (int it = 0; it < kStages - 1; ++it) { issue(it, n_mine, it); copies_commit(); }
+  };
+  int n_mine = tiles_mine();
+  if (g.j1 > g.j0) first_copies(n_mine);
 
+  for (int turn = 0; WHOLE || g.j1 > g.j0; turn ^= 1) {
+    const long long row_first = g.s.first + (long long)g.tile * rpt;
+    const int cols = min(rpt, g.s.n - g.tile * rpt) * G, hd = g.hd;
+    if (tid < kCols) len_s[turn][tid] = tid < cols ? row_tokens(a, g.seq, g.s, row_first + tid / G, tid % G == 0 && hd == 0 && g.j0 == 0, st) : -1;
     // ---- the columns of Q as fragments: 16-dim piece c, dims 4 tig .. 4 tig + 3 of it, as fp16 times 2^-exponent ----
     uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];
     if (kQInRegs || warp == 0) {
@@ -326,10 +341,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         uint2 raw[kChunks];
         uint32_t top = 0;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-          raw[c] = col < cols ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
+        for (int c = 0; c < kChunks; ++c) raw[c] = col < cols ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
           top = max(top, max(max(raw[c].x & 0x7fffu, (raw[c].x >> 16) & 0x7fffu), max(raw[c].y & 0x7fffu, (raw[c].y >> 16) & 0x7fffu)));
-        }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const bool finite = top < 0x7f80u;
@@ -347,20 +362,20 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           else q_s[c][nt][lane] = h2;
         }
         // (half of it: the scale of a key is made with one more)
-        if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
+        if (warp == 0 && tig == 0) qscale_s[turn][col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
       }
     }
-    __syncthreads();
+    __syncthreads();                                                  // (and what the last task's exchange has left in the rings has been read)
     // m and z are this lane's own, of its tokens; mp is the column's: all weights of the column that meet values are 2^(s + e - mp + 14)
     float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
-    int seen[NT][2], seen_all = s.len;
+    int seen[NT][2], seen_all = g.s.len;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int col = nt * 8 + tig * 2 + x;
-        qs[nt][x] = qscale_s[col];
-        seen[nt][x] = len_s[col];
+        qs[nt][x] = qscale_s[turn][col];
+        seen[nt][x] = len_s[turn][col];
         if (col < cols) seen_all = min(seen_all, seen[nt][x]);
         m[nt][x] = mp[nt][x] = -INFINITY;
         z[nt][x] = 0.f;
@@ -372,9 +387,13 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[c][nt][0] = o[c][nt][1] = o[c][nt][2] = o[c][nt][3] = 0.f;
 
+    SeqRows next = {0, 0, 0};                                         // the sequence behind this one, for when the share goes on there
+    if constexpr (!WHOLE)
+      if (f < f1 && g.seq + 1 < a.n_seq && f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) next = rows_of(a, g.seq + 1, -1, 0, false, st);
+
     for (int it = 0, stage = 0, fill = kStages - 1; it < n_mine; ++it) {
       __syncwarp();                                                   // everyone is through with the stage that is filled now
-      issue(it + kStages - 1, fill);
+      issue(it + kStages - 1, n_mine, fill);
       copies_commit();
       copies_wait<kStages - 1>();
       __syncwarp();
@@ -382,7 +401,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       const uint8_t* exps = ring_ptr + stage * L::kStage + L::kExp;
       fill = stage;
       stage = stage + 1 == kStages ? 0 : stage + 1;
-      const int t0 = (j0 + warp + it * kQaWarps) * kQaTile;
+      const int t0 = (g.j0 + warp + it * kQaWarps) * kQaTile;
       const uint32_t ke = *reinterpret_cast<const uint32_t*>(exps + gid * 4) ^ 0x80808080u, ve = *reinterpret_cast<const uint32_t*>(exps + 32 + gid * 4) ^ 0x80808080u;
       // ---- S^T = K Q^T: 16 tokens by the columns, twice ----
       float sc[2][NT][4];
@@ -500,8 +519,32 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           }
         }
     }
+
+    // ---- the next task's first copies, while this one's results are added up ----
+    const bool whole = WHOLE || (g.j0 == 0 && g.j1 == g.tiles);
+    const int slot = 2 * (int)blockIdx.x + (g.j0 == 0 ? 1 : 0);       // a task's first part, a later one
     copies_wait<0>();
-    // ---- the warps' results, added up in their order: every warp adds up a quarter of the pieces, the others' come through the rings' place ----
+    __syncwarp();
+    Chain left = {-1, 0, (int)row_first, hd, cols, 0u, {0, 0}};
+    bool more = false;
+    if constexpr (!WHOLE) {
+      if (g.j1 < g.tiles) { left.c0 = (int)quotient(g.task_start + kQaTaskUnits, per); left.c1 = (int)quotient(g.task_start + kQaTaskUnits + g.tiles - 1, per); }
+      if (f < f1) {
+        if (f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) {
+          seq_start = f;
+          g.s = next;
+          for (++g.seq; g.s.n == 0 && g.seq + 1 < a.n_seq;) g.s = rows_of(a, ++g.seq, -1, 0, false, st);      // (there is one: the share goes on)
+        }
+        if (g.s.n > 0) {
+          cut();
+          more = g.j1 > g.j0;
+          n_mine = tiles_mine();
+          if (kAhead && more) first_copies(n_mine);
+        }
+      }
+    }
+    // ---- the warps' results, added up in their order: every warp adds up a quarter of the pieces, the others' come through the rings' last stage (all of them
+    // where no copies are on their way) ----
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -514,18 +557,17 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 16);
         if (gid == 0) stats_s[warp][nt * 8 + tig * 2 + x] = {m[nt][x], mp[nt][x], z[nt][x]};
       }
-    __syncthreads();                                                  // the rings are free
-    constexpr int kOwn = kChunks / kQaWarps;
-    static_assert(kQaWarps * kChunks * NT * 512 <= L::kTotal, "every warp's result fits the rings");
-    float4* all_s = reinterpret_cast<float4*>(smem);
+    constexpr int kOwn = kChunks / kQaWarps, kOthers = kChunks - kOwn, kExchange = kAhead ? (kStages - 1) * L::kStage : 0;
+    static_assert(kOthers * NT * 512 <= (kAhead ? L::kStage : L::kWarp), "a warp's results fit");
+    auto place = [&](int w, int c, int nt) -> float4& {               // warp w's result of piece c, which is another's
+      return reinterpret_cast<float4*>(smem + w * L::kWarp + kExchange)[((c - (c >= (w + 1) * kOwn ? kOwn : 0)) * NT + nt) * 32 + lane];
+    };
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-        if (c / kOwn != warp) all_s[((warp * kChunks + c) * NT + nt) * 32 + lane] = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
+        if (c / kOwn != warp) place(warp, c, nt) = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
     __syncthreads();
-    const bool whole = WHOLE || (j0 == 0 && j1 == tiles);
-    const int slot = 2 * (int)blockIdx.x + (j0 == 0 ? 1 : 0);         // a task's first part, a later one
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float big[2], bigp[2], zs[2], wgt[kQaWarps][2];
@@ -552,7 +594,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kQaWarps; ++w) {
-          const float4 v = w == warp ? make_float4(o[i][nt][0], o[i][nt][1], o[i][nt][2], o[i][nt][3]) : all_s[((w * kChunks + i) * NT + nt) * 32 + lane];
+          const float4 v = w == warp ? make_float4(o[i][nt][0], o[i][nt][1], o[i][nt][2], o[i][nt][3]) : place(w, i, nt);
           acc[0] = fmaf(v.x, wgt[w][0], acc[0]); acc[1] = fmaf(v.y, wgt[w][1], acc[1]);
           acc[2] = fmaf(v.z, wgt[w][0], acc[2]); acc[3] = fmaf(v.w, wgt[w][1], acc[3]);
         }
@@ -563,7 +605,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int col = nt * 8 + tig * 2 + x, r = col / G;
-          if (col >= cols || len_s[col] < 0) continue;
+          if (col >= cols || len_s[turn][col] < 0) continue;
           const bool none = zs[x] == 0.f;                             // no token at all, or none above -inf (NaN stays NaN)
           const float norm = none ? 0.f : 1.f / (zs[x] * 16384.f), grow = none ? 0.f : exp2f(bigp[x] - big[x]);
           const long long at = (row_first + r) * a.H + hd * G + col - r * G;
@@ -574,35 +616,26 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       }
     }
     if constexpr (WHOLE) break;
-    else {
-      f += j1 - j0;
-      if (f >= f1) {
-        if (warp == 0) {
-          const uint32_t live = __ballot_sync(0xffffffffu, lane < kCols && len_s[lane < kCols ? lane : 0] >= 0);
-          if (lane == 0) {
-            Chain c = {-1, 0, (int)row_first, hd, cols, live, {0, 0}};
-            if (j1 < tiles) { c.c0 = (int)(task_start / per); c.c1 = (int)((task_start + tiles - 1) / per); }
-            a.chain[blockIdx.x] = c;
-          }
-        }
-        break;
+    else if (!more) {
+      if (warp == 0) {
+        left.live = __ballot_sync(0xffffffffu, lane < kCols && len_s[turn][lane < kCols ? lane : 0] >= 0);
+        if (lane == 0) a.chain[blockIdx.x] = left;
       }
-      if (f - seq_start >= (long long)tiles * row_tiles * a.Hkv) {
-        seq_start = f;
-        do s = rows_of(a, ++seq, false, st); while (s.n == 0 && seq + 1 < a.n_seq);      // (there is one: the share goes on)
-      }
-      __syncthreads();                                                // what the next task writes into shared memory has been read
+      return;
+    } else if (!kAhead) {
+      __syncthreads();                                                // the exchange has been read
+      first_copies(n_mine);
     }
   }
   if (WHOLE) {
     __syncthreads();
     griddep_launch();
-  }
+  } else if (tid == 0) a.chain[blockIdx.x].c0 = -1;                   // (a share that ends before the first tile of its only task)
 }
 
 // The parts of tasks that went over several blocks, joined in their order.  The blocks c0 <= b < c1 that such a task leaves share its (16 dims, 8 columns) units; a block's
 // warps share a unit's parts where there are fewer units than warps.
-constexpr int kQjWarps = 4, kQjBatch = 4;
+constexpr int kQjWarps = 8, kQjBatch = 8;
 template <int D, int NT>
 __global__ void __launch_bounds__(kQjWarps * 32)
 quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
