@@ -52,6 +52,10 @@ struct QaSmem {
   static constexpr int kStage = kExp + 128;
   static constexpr int kWarp = kStages * kStage;
   static constexpr int kTotal = kQaWarps * kWarp;
+  // Where the warps exchange their results: the last stages of every ring, while the first kBefore are filled for the next task.
+  static constexpr int kResult = (D / 16 - D / 16 / kQaWarps) * NT * 512;
+  static constexpr int kBefore = kStages - (kResult + kStage - 1) / kStage;
+  static_assert(kBefore >= 1, "a warp's results leave a stage");
 };
 
 // Place of 16-byte piece c of token t of a tile.  The eight rows of a matrix are tokens 4 r + j, so that a lane's four tokens are neighbours (their exponents are one
@@ -107,7 +111,18 @@ __device__ __forceinline__ float max_over_tokens(float x) {              // lane
   x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
   return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
 }
-__device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
+// A maximum of nothing: no score lies below it, and what is taken from it stays a number (scores of -inf weigh nothing beside it, either).
+constexpr float kNothing = -3.4028234663852886e38f;
+__device__ __forceinline__ float log2_of(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float one_over(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // Rows and tokens of a sequence; rows 0: none to work on.
 struct SeqRows { int first, n, len; };
@@ -160,11 +175,12 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   constexpr int kStages = L::kStages;
   constexpr int kCols = 8 * NT, kChunks = D / 16;                     // columns of the block; 16-dim pieces of a head
   constexpr bool kQInRegs = NT <= 2;
-  constexpr bool kAhead = NT <= 2 && !WHOLE;                          // the next task's first copies are asked for before a task's results are added up
+  constexpr int kOwn = kChunks / kQaWarps;                            // pieces of the result that a warp adds up
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ ColStats stats_s[kQaWarps][kCols];
-  __shared__ int len_s[2][kCols];
-  __shared__ float qscale_s[2][kCols];
+  __shared__ int len_s[kCols];                                        // tokens that a column sees; -1: none, and it is not written
+  __shared__ float qscale_s[kCols];
+  __shared__ int at_s[kCols];                                         // its row * H + head (less than 2^31: see the host's limit); -1: not written
   __shared__ __align__(16) uint2 q_s[kQInRegs ? 1 : kChunks][kQInRegs ? 1 : NT][32];
   __shared__ long long sums_s[kQaWarps];
   __shared__ long long start_s;
@@ -267,6 +283,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     }
   };
   cut();
+  if (!WHOLE && g.j1 <= g.j0) {                                       // (the share ends before the first tile of its only task)
+    if (tid == 0) a.chain[blockIdx.x].c0 = -1;
+    return;
+  }
 
   // ---- copies: lane l has piece l % (D / 16) of every (512 / D)-th token; block numbers of sixteen tiles at a time, one lane each half ----
   constexpr int kPieces = D / 16, kTokensAtOnce = 32 / kPieces, kCopies = 16 / kTokensAtOnce;
@@ -274,133 +294,25 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   const long long v_off = a.v - a.k, step = kTokensAtOnce * a.token_stride;
   const uint8_t* k_all = a.k + my_token * a.token_stride + my_piece * 16;
   auto tiles_mine = [&]() { return g.j1 - g.j0 > warp ? (g.j1 - g.j0 - warp + kQaWarps - 1) / kQaWarps : 0; };      // tiles j0 + warp, + 4, ..
-  int page = 0;
-  auto issue = [&](int it, int n_mine, int stage) {
-    if ((it & 15) == 0) {
-      const int mine = it + (lane >> 1);
-      page = 0;
-      if (mine < n_mine) {                                            // (its tokens' numbers fit 32 bits: see the host's limit)
-        const int t = (g.j0 + warp + mine * kQaWarps) * kQaTile + (lane & 1) * 16;
-        if (t < g.s.len) page = a.table[g.seq * a.table_stride + (t >> a.block_shift)];
-      }
-    }
-    if (it >= n_mine) return;
-    const uint8_t* k_lane = k_all + g.hd * a.head_stride;
-    const uint32_t dst = ring + stage * L::kStage;
-    const int t0 = (g.j0 + warp + it * kQaWarps) * kQaTile;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int id = __shfl_sync(0xffffffffu, page, (it & 15) * 2 + h), t = t0 + h * 16;
-      const bool there = t < g.s.len && (unsigned)id < (unsigned)a.n_blocks;
-      const uint8_t* p = k_lane + (there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0);
-      if (there && g.s.len - t >= 16) {
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const uint32_t d = dst + swizzled<D>(my_token + h * 16 + i * kTokensAtOnce, my_piece);
-          copy_16(d, p, 16);
-          copy_16(d + L::kV, p + v_off, 16);
-          p += step;
-        }
-      } else {                                                        // the end of the sequence, or no such block: zeros for what is not there (and nothing is read)
-        if (t < g.s.len && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
-        const int valid = there ? g.s.len - t : 0;
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int token = my_token + i * kTokensAtOnce;
-          const uint32_t d = dst + swizzled<D>(token + h * 16, my_piece);
-          const uint8_t* q = token < valid ? p + i * step : a.k;
-          copy_16(d, q, token < valid ? 16 : 0);
-          copy_16(d + L::kV, q + v_off, token < valid ? 16 : 0);
-        }
-      }
-      if (lane < 2) {
-        const uint32_t e = stage * L::kStage + L::kExp + lane * 32 + h * 16;
-        if (there) copy_16(ring + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + g.hd) << a.block_shift) + (t & bs_mask)), 16);
-        else *reinterpret_cast<uint4*>(ring_ptr + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
-      }
-    }
-  };
-  auto first_copies = [&](int n_mine) {
-#pragma unroll
-    for (int it = 0; it < kStages - 1; ++it) { issue(it, n_mine, it); copies_commit(); }
-  };
-  int n_mine = tiles_mine();
-  if (g.j1 > g.j0) first_copies(n_mine);
+  int n_mine = tiles_mine(), page = 0;
 
-  for (int turn = 0; WHOLE || g.j1 > g.j0; turn ^= 1) {
-    const long long row_first = g.s.first + (long long)g.tile * rpt;
-    const int cols = min(rpt, g.s.n - g.tile * rpt) * G, hd = g.hd;
-    if (tid < kCols) len_s[turn][tid] = tid < cols ? row_tokens(a, g.seq, g.s, row_first + tid / G, tid % G == 0 && hd == 0 && g.j0 == 0, st) : -1;
-    // ---- the columns of Q as fragments: 16-dim piece c, dims 4 tig .. 4 tig + 3 of it, as fp16 times 2^-exponent ----
-    uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];
-    if (kQInRegs || warp == 0) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int col = nt * 8 + gid, r = col / G;
-        const uint16_t* q = a.q + ((row_first + r) * a.H + hd * G + col - r * G) * D + tig * 4;
-        uint2 raw[kChunks];
-        uint32_t top = 0;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) raw[c] = col < cols ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-          top = max(top, max(max(raw[c].x & 0x7fffu, (raw[c].x >> 16) & 0x7fffu), max(raw[c].y & 0x7fffu, (raw[c].y >> 16) & 0x7fffu)));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const bool finite = top < 0x7f80u;
-        const int e = max((int)(top >> 7) - 127 - 14, -120);          // the largest element comes to lie in [2^14, 2^15)
-        const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.f;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-          uint2 h2 = make_uint2(0u, 0u);
-          if (finite) {
-            const __half2 x = __floats2half2_rn(__uint_as_float(raw[c].x << 16) * inv, __uint_as_float(raw[c].x & 0xffff0000u) * inv);
-            const __half2 y = __floats2half2_rn(__uint_as_float(raw[c].y << 16) * inv, __uint_as_float(raw[c].y & 0xffff0000u) * inv);
-            h2 = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-          }
-          if constexpr (kQInRegs) qf[c][nt] = h2;
-          else q_s[c][nt][lane] = h2;
-        }
-        // (half of it: the scale of a key is made with one more)
-        if (warp == 0 && tig == 0) qscale_s[turn][col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
-      }
-    }
-    __syncthreads();                                                  // (and what the last task's exchange has left in the rings has been read)
-    // m and z are this lane's own, of its tokens; mp is the column's: all weights of the column that meet values are 2^(s + e - mp + 14)
-    float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
-    int seen[NT][2], seen_all = g.s.len;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int col = nt * 8 + tig * 2 + x;
-        qs[nt][x] = qscale_s[turn][col];
-        seen[nt][x] = len_s[turn][col];
-        if (col < cols) seen_all = min(seen_all, seen[nt][x]);
-        m[nt][x] = mp[nt][x] = -INFINITY;
-        z[nt][x] = 0.f;
-      }
-    seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 1));
-    seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 2));
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) o[c][nt][0] = o[c][nt][1] = o[c][nt][2] = o[c][nt][3] = 0.f;
+  // What has been weighed of the task's tokens.  m and z are this lane's own, of its tokens; mp is the column's: all weights of the column that meet values are 2^(s + e - mp + 14)
+  float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
+  uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];                // the columns of Q as fragments
+  int seen[NT][2], seen_all = 0;
+  // The task before, whose results are still to be added up.
+  bool pending = false, pending_whole = false, more = true;
+  int pending_slot = 0;
+  Chain left = {-1, 0, 0, 0, 0, 0u, {0, 0}};
 
-    SeqRows next = {0, 0, 0};                                         // the sequence behind this one, for when the share goes on there
-    if constexpr (!WHOLE)
-      if (f < f1 && g.seq + 1 < a.n_seq && f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) next = rows_of(a, g.seq + 1, -1, 0, false, st);
-
-    for (int it = 0, stage = 0, fill = kStages - 1; it < n_mine; ++it) {
-      __syncwarp();                                                   // everyone is through with the stage that is filled now
-      issue(it + kStages - 1, n_mine, fill);
-      copies_commit();
+  // One trip per tile: its products, then the copies of the tile that takes its place in the ring.  A task's first trips have copies only; between them the results of the task
+  // before are added up and the rows of this one fetched.  (Every part of the code stands here once: the instructions of a short call come from far.)
+  for (int it = -kStages, stage = 0;; ++it) {
+    if (it >= 0) {
       copies_wait<kStages - 1>();
       __syncwarp();
       const uint32_t kt = ring + stage * L::kStage, vt = kt + L::kV;
       const uint8_t* exps = ring_ptr + stage * L::kStage + L::kExp;
-      fill = stage;
-      stage = stage + 1 == kStages ? 0 : stage + 1;
       const int t0 = (g.j0 + warp + it * kQaWarps) * kQaTile;
       const uint32_t ke = *reinterpret_cast<const uint32_t*>(exps + gid * 4) ^ 0x80808080u, ve = *reinterpret_cast<const uint32_t*>(exps + 32 + gid * 4) ^ 0x80808080u;
       // ---- S^T = K Q^T: 16 tokens by the columns, twice ----
@@ -430,7 +342,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         }
       }
       // ---- scores of this lane: tokens 4 gid + i, i = 2 h + y, columns 2 tig (+ 1); w: with the exponents of the values ----
-      float vexp[4];
+      float vexp[4], w[NT][2][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float ks = __uint_as_float(__byte_perm(ke, 0, 0x0444 | i << 12) >> 1);         // 2^(e + 1)
@@ -438,56 +350,49 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) sc[i >> 1][nt][2 * (i & 1) + x] = sc[i >> 1][nt][2 * (i & 1) + x] * qs[nt][x] * ks;
+          for (int x = 0; x < 2; ++x) {
+            float& v = sc[i >> 1][nt][2 * (i & 1) + x];
+            v = v * qs[nt][x] * ks;
+            w[nt][x][i] = v + vexp[i];
+          }
       }
       if (__any_sync(0xffffffffu, t0 + kQaTile > seen_all || some_byte_below_2(ke) || some_byte_below_2(ve))) {      // tokens that are not seen, NaN
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int at = gid * 4 + i, ek = (ke >> (8 * i)) & 255u, ev = (ve >> (8 * i)) & 255u;
-          const bool gone = ek == kNoKey + 128;
-          if (gone) vexp[i] = 0.f;
-          else if (ev == kExpNone + 128) vexp[i] = __uint_as_float(0x7fc00000u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               float& v = sc[i >> 1][nt][2 * (i & 1) + x];
-              if (ek == kExpNone + 128) v = __uint_as_float(0x7fc00000u);
-              if (gone || t0 + at >= seen[nt][x]) v = -INFINITY;
+              if (ek == kExpNone + 128) v = w[nt][x][i] = __uint_as_float(0x7fc00000u);
+              if (ev == kExpNone + 128) w[nt][x][i] = __uint_as_float(0x7fc00000u);
+              if (ek == kNoKey + 128 || t0 + at >= seen[nt][x]) v = w[nt][x][i] = -INFINITY;
             }
         }
       }
       uint32_t pb[2][NT][2];                                          // P^T as fragments: tokens 4 r + 2 h, 4 r + 2 h + 1
-      float w[NT][2][4];
       bool grown = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          float ms = m[nt][x], mt = -INFINITY;
+          const float ms = ptx::fmax3(ptx::fmax3(sc[0][nt][x], sc[0][nt][2 + x], sc[1][nt][x]), sc[1][nt][2 + x], m[nt][x]);
+          float zz = z[nt][x] * ptx::fast_exp2(m[nt][x] - ms);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = sc[i >> 1][nt][2 * (i & 1) + x];
-            ms = fmaxf(ms, v);
-            w[nt][x][i] = v == -INFINITY ? v : v + vexp[i];           // (the exponent of a token that is not seen may be that of NaN)
-            mt = fmaxf(mt, w[nt][x][i]);
-          }
-          const float ref = no_inf(ms);
-          float zz = z[nt][x] * ptx::fast_exp2(m[nt][x] - ref);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) zz += ptx::fast_exp2(sc[i >> 1][nt][2 * (i & 1) + x] - ref);
+          for (int i = 0; i < 4; ++i) zz += ptx::fast_exp2(sc[i >> 1][nt][2 * (i & 1) + x] - ms);
           z[nt][x] = zz;
           m[nt][x] = ms;
-          grown |= mt > mp[nt][x] + 1.f;                              // (weights up to 2^15 are fine)
+          grown |= ptx::fmax3(w[nt][x][0], w[nt][x][1], fmaxf(w[nt][x][2], w[nt][x][3])) > mp[nt][x] + 1.f;       // (weights up to 2^15 are fine)
         }
       if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float mt = fmaxf(fmaxf(w[nt][x][0], w[nt][x][1]), fmaxf(w[nt][x][2], w[nt][x][3]));
+            const float mt = ptx::fmax3(w[nt][x][0], w[nt][x][1], fmaxf(w[nt][x][2], w[nt][x][3]));
             const float top = max_over_tokens(mt), now = top > mp[nt][x] + 1.f ? top : mp[nt][x];      // (what its neighbours do is nothing to a column)
-            const float alpha = now == mp[nt][x] ? 1.f : ptx::fast_exp2(mp[nt][x] - now);
+            const float alpha = ptx::fast_exp2(mp[nt][x] - now);
             mp[nt][x] = now;
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) { o[c][nt][x] *= alpha; o[c][nt][2 + x] *= alpha; }
@@ -495,7 +400,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float ref0 = no_inf(mp[nt][0]) - kPShift, ref1 = no_inf(mp[nt][1]) - kPShift;
+        const float ref0 = mp[nt][0] - kPShift, ref1 = mp[nt][1] - kPShift;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const __half2 p = __floats2half2_rn(ptx::fast_exp2(w[nt][0][i] - ref0), ptx::fast_exp2(w[nt][1][i] - ref1));
@@ -518,119 +423,225 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
             for (int nt = 0; nt < NT; ++nt) mma_f16(o[c2 * 2 + i][nt], frag, pb[h][nt][0], pb[h][nt][1]);
           }
         }
-    }
-
-    // ---- the next task's first copies, while this one's results are added up ----
-    const bool whole = WHOLE || (g.j0 == 0 && g.j1 == g.tiles);
-    const int slot = 2 * (int)blockIdx.x + (g.j0 == 0 ? 1 : 0);       // a task's first part, a later one
-    copies_wait<0>();
-    __syncwarp();
-    Chain left = {-1, 0, (int)row_first, hd, cols, 0u, {0, 0}};
-    bool more = false;
-    if constexpr (!WHOLE) {
-      if (g.j1 < g.tiles) { left.c0 = (int)quotient(g.task_start + kQaTaskUnits, per); left.c1 = (int)quotient(g.task_start + kQaTaskUnits + g.tiles - 1, per); }
-      if (f < f1) {
-        if (f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) {
-          seq_start = f;
-          g.s = next;
-          for (++g.seq; g.s.n == 0 && g.seq + 1 < a.n_seq;) g.s = rows_of(a, ++g.seq, -1, 0, false, st);      // (there is one: the share goes on)
+      __syncwarp();                                                   // everyone is through with the stage
+    } else if (it == L::kBefore - kStages) {
+      if (pending) {
+        // ---- the warps' results of the task before, added up in their order: every warp adds up a quarter of the pieces, the others' come through the rings ----
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float all = max_over_tokens(m[nt][x]);
+            float zz = z[nt][x] * ptx::fast_exp2(m[nt][x] - all);
+            zz += __shfl_xor_sync(0xffffffffu, zz, 4);
+            zz += __shfl_xor_sync(0xffffffffu, zz, 8);
+            zz += __shfl_xor_sync(0xffffffffu, zz, 16);
+            if (gid == 0) stats_s[warp][nt * 8 + tig * 2 + x] = {all, mp[nt][x], zz};
+          }
+        auto place = [&](int w, int c, int nt) -> float4& {           // warp w's result of piece c, which is another's
+          return reinterpret_cast<float4*>(smem + w * L::kWarp + L::kBefore * L::kStage)[((c - (c >= (w + 1) * kOwn ? kOwn : 0)) * NT + nt) * 32 + lane];
+        };
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            if (c / kOwn != warp) place(warp, c, nt) = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
+        __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float big[2], bigp[2], zs[2], wgt[kQaWarps][2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int col = nt * 8 + tig * 2 + x;
+            big[x] = bigp[x] = kNothing;
+#pragma unroll
+            for (int w = 0; w < kQaWarps; ++w) { big[x] = fmaxf(big[x], stats_s[w][col].m); bigp[x] = fmaxf(bigp[x], stats_s[w][col].mp); }
+            zs[x] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kQaWarps; ++w) {
+              zs[x] = fmaf(stats_s[w][col].z, ptx::fast_exp2(stats_s[w][col].m - big[x]), zs[x]);
+              wgt[w][x] = ptx::fast_exp2(stats_s[w][col].mp - bigp[x]);
+            }
+            if (!pending_whole && warp == 0 && gid == 0) {
+              float* p = a.part_s + ((long long)pending_slot * kQaColsMost + col) * 3;
+              p[0] = big[x]; p[1] = bigp[x]; p[2] = zs[x];
+            }
+          }
+          float acc[kOwn][4];
+#pragma unroll
+          for (int i = 0; i < kOwn; ++i) {
+            acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kQaWarps; ++w) {
+              float4 v;
+              if (w != warp) v = place(w, warp * kOwn + i, nt);
+              else {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+                  if (c == warp * kOwn + i) v = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
+              }
+              acc[i][0] = fmaf(v.x, wgt[w][0], acc[i][0]); acc[i][1] = fmaf(v.y, wgt[w][1], acc[i][1]);
+              acc[i][2] = fmaf(v.z, wgt[w][0], acc[i][2]); acc[i][3] = fmaf(v.w, wgt[w][1], acc[i][3]);
+            }
+          }
+          if (!pending_whole) {
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i)
+              *reinterpret_cast<float4*>(a.part_o + (((long long)pending_slot * kChunks + warp * kOwn + i) * NT + nt) * 128 + lane * 4) =
+                  make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int at = at_s[nt * 8 + tig * 2 + x];
+              if (at < 0) continue;
+              const bool none = zs[x] == 0.f;                         // no token at all, or none above -inf (NaN stays NaN)
+              const float norm = none ? 0.f : one_over(zs[x] * 16384.f), grow = none ? 0.f : ptx::fast_exp2(bigp[x] - big[x]);
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i)
+                *reinterpret_cast<__nv_bfloat162*>(a.out + (long long)at * D + (warp * kOwn + i) * 16 + gid * 2) =
+                    __floats2bfloat162_rn(acc[i][x] * norm * grow, acc[i][2 + x] * norm * grow);
+              if (warp == 0 && gid == 0 && a.lse_out) {
+                const int row = at / a.H;
+                a.lse_out[(at - row * a.H) * a.n_rows + row] = none ? -INFINITY : (big[x] + log2_of(zs[x])) * 0.6931471805599453f;
+              }
+            }
+          }
         }
-        if (g.s.n > 0) {
-          cut();
-          more = g.j1 > g.j0;
-          n_mine = tiles_mine();
-          if (kAhead && more) first_copies(n_mine);
+        if (!more) break;
+        __syncthreads();                                              // all of that has been read
+      }
+      // ---- the rows of this task: 16-dim piece c of a column, dims 4 tig .. 4 tig + 3 of it, as fp16 times 2^-exponent ----
+      const long long row_first = g.s.first + (long long)g.tile * rpt;
+      const int cols = min(rpt, g.s.n - g.tile * rpt) * G;
+      if (tid < kCols) {
+        const int r = tid / G, len = tid < cols ? row_tokens(a, g.seq, g.s, row_first + r, tid - r * G == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
+        len_s[tid] = len;
+        at_s[tid] = len < 0 ? -1 : (int)(row_first + r) * a.H + g.hd * G + tid - r * G;
+      }
+      if (kQInRegs || warp == 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int col = nt * 8 + gid, r = col / G;
+          const uint16_t* q = a.q + ((row_first + r) * a.H + g.hd * G + col - r * G) * D + tig * 4;
+          uint2 raw[kChunks];
+          uint32_t top = 0;
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) raw[c] = col < cols ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) top = __vmaxu2(top, __vmaxu2(raw[c].x & 0x7fff7fffu, raw[c].y & 0x7fff7fffu));
+          top = max(top & 0xffffu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const bool finite = top < 0x7f80u;
+          const int e = max((int)(top >> 7) - 127 - 14, -120);        // the largest element comes to lie in [2^14, 2^15)
+          const float inv = __uint_as_float((uint32_t)(127 - (finite ? e : 0)) << 23);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) {
+            const __half2 x = __floats2half2_rn(__uint_as_float(raw[c].x << 16) * inv, __uint_as_float(raw[c].x & 0xffff0000u) * inv);
+            const __half2 y = __floats2half2_rn(__uint_as_float(raw[c].y << 16) * inv, __uint_as_float(raw[c].y & 0xffff0000u) * inv);
+            const uint2 h2 = finite ? make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y)) : make_uint2(0u, 0u);
+            if constexpr (kQInRegs) qf[c][nt] = h2;
+            else q_s[c][nt][lane] = h2;
+          }
+          // (half of it: the scale of a key is made with one more)
+          if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
         }
       }
-    }
-    // ---- the warps' results, added up in their order: every warp adds up a quarter of the pieces, the others' come through the rings' last stage (all of them
-    // where no copies are on their way) ----
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float all = max_over_tokens(m[nt][x]);
-        z[nt][x] *= ptx::fast_exp2(m[nt][x] - no_inf(all));
-        m[nt][x] = all;
-        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 4);
-        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 8);
-        z[nt][x] += __shfl_xor_sync(0xffffffffu, z[nt][x], 16);
-        if (gid == 0) stats_s[warp][nt * 8 + tig * 2 + x] = {m[nt][x], mp[nt][x], z[nt][x]};
-      }
-    constexpr int kOwn = kChunks / kQaWarps, kOthers = kChunks - kOwn, kExchange = kAhead ? (kStages - 1) * L::kStage : 0;
-    static_assert(kOthers * NT * 512 <= (kAhead ? L::kStage : L::kWarp), "a warp's results fit");
-    auto place = [&](int w, int c, int nt) -> float4& {               // warp w's result of piece c, which is another's
-      return reinterpret_cast<float4*>(smem + w * L::kWarp + kExchange)[((c - (c >= (w + 1) * kOwn ? kOwn : 0)) * NT + nt) * 32 + lane];
-    };
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
+      __syncthreads();
+      seen_all = g.s.len;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-        if (c / kOwn != warp) place(warp, c, nt) = make_float4(o[c][nt][0], o[c][nt][1], o[c][nt][2], o[c][nt][3]);
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float big[2], bigp[2], zs[2], wgt[kQaWarps][2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int col = nt * 8 + tig * 2 + x;
-        big[x] = bigp[x] = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kQaWarps; ++w) { big[x] = fmaxf(big[x], stats_s[w][col].m); bigp[x] = fmaxf(bigp[x], stats_s[w][col].mp); }
-        zs[x] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kQaWarps; ++w) {
-          zs[x] = fmaf(stats_s[w][col].z, ptx::fast_exp2(stats_s[w][col].m - no_inf(big[x])), zs[x]);
-          wgt[w][x] = ptx::fast_exp2(stats_s[w][col].mp - no_inf(bigp[x]));
-        }
-        if (!whole && warp == 0 && gid == 0) {
-          float* p = a.part_s + ((long long)slot * kQaColsMost + col) * 3;
-          p[0] = big[x]; p[1] = bigp[x]; p[2] = zs[x];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        if (i / kOwn != warp) continue;
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kQaWarps; ++w) {
-          const float4 v = w == warp ? make_float4(o[i][nt][0], o[i][nt][1], o[i][nt][2], o[i][nt][3]) : place(w, i, nt);
-          acc[0] = fmaf(v.x, wgt[w][0], acc[0]); acc[1] = fmaf(v.y, wgt[w][1], acc[1]);
-          acc[2] = fmaf(v.z, wgt[w][0], acc[2]); acc[3] = fmaf(v.w, wgt[w][1], acc[3]);
-        }
-        if (!whole) {
-          *reinterpret_cast<float4*>(a.part_o + (((long long)slot * kChunks + i) * NT + nt) * 128 + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-          continue;
-        }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int col = nt * 8 + tig * 2 + x, r = col / G;
-          if (col >= cols || len_s[turn][col] < 0) continue;
-          const bool none = zs[x] == 0.f;                             // no token at all, or none above -inf (NaN stays NaN)
-          const float norm = none ? 0.f : 1.f / (zs[x] * 16384.f), grow = none ? 0.f : exp2f(bigp[x] - big[x]);
-          const long long at = (row_first + r) * a.H + hd * G + col - r * G;
-          *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + i * 16 + gid * 2) = __floats2bfloat162_rn(acc[x] * norm * grow, acc[2 + x] * norm * grow);
-          if (i == 0 && gid == 0 && a.lse_out)
-            a.lse_out[(long long)(hd * G + col - r * G) * a.n_rows + row_first + r] = none ? -INFINITY : (big[x] + log2f(zs[x])) * 0.6931471805599453f;
+          const int col = nt * 8 + tig * 2 + x;
+          qs[nt][x] = qscale_s[col];
+          seen[nt][x] = len_s[col];
+          if (col < cols) seen_all = min(seen_all, seen[nt][x]);
+          m[nt][x] = mp[nt][x] = kNothing;
+          z[nt][x] = 0.f;
+        }
+      seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 1));
+      seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 2));
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[c][nt][0] = o[c][nt][1] = o[c][nt][2] = o[c][nt][3] = 0.f;
+    }
+
+    // ---- copies of tile it + kStages ----
+    const int ahead = it + kStages;
+    if ((ahead & 15) == 0) {
+      const int mine = ahead + (lane >> 1);
+      page = -1;
+      if (mine < n_mine) {                                            // (its tokens' numbers fit 32 bits: see the host's limit)
+        const int t = (g.j0 + warp + mine * kQaWarps) * kQaTile + (lane & 1) * 16;
+        if (t < g.s.len) page = a.table[g.seq * a.table_stride + (t >> a.block_shift)];
+      }
+    }
+    if (ahead < n_mine) {
+      const uint32_t dst = ring + stage * L::kStage;
+      const int t0 = (g.j0 + warp + ahead * kQaWarps) * kQaTile;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int id = __shfl_sync(0xffffffffu, page, (ahead & 15) * 2 + h), t = t0 + h * 16;
+        const bool there = t < g.s.len && (unsigned)id < (unsigned)a.n_blocks;
+        const int valid = there ? min(16, g.s.len - t) : 0;
+        const uint8_t* p = k_all + g.hd * a.head_stride + (there ? id * a.block_stride + (t & bs_mask) * a.token_stride : 0);
+        if (t < g.s.len && !there && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+        // behind the end of the sequence, and where there is no such block: zeros, and nothing is read
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const bool some = my_token + i * kTokensAtOnce < valid;
+          const uint32_t d = dst + swizzled<D>(my_token + h * 16 + i * kTokensAtOnce, my_piece);
+          copy_16(d, p, some ? 16 : 0);                               // (a block has these sixteen tokens in any case)
+          copy_16(d + L::kV, p + v_off, some ? 16 : 0);
+          p += step;
+        }
+        if (lane < 2) {
+          const uint32_t e = stage * L::kStage + L::kExp + lane * 32 + h * 16;
+          if (there) copy_16(ring + e, (lane ? a.v_exp : a.k_exp) + ((((long long)id * a.Hkv + g.hd) << a.block_shift) + (t & bs_mask)), 16);
+          else *reinterpret_cast<uint4*>(ring_ptr + e) = make_uint4(0x81818181u, 0x81818181u, 0x81818181u, 0x81818181u);
         }
       }
     }
-    if constexpr (WHOLE) break;
-    else if (!more) {
-      if (warp == 0) {
-        left.live = __ballot_sync(0xffffffffu, lane < kCols && len_s[turn][lane < kCols ? lane : 0] >= 0);
-        if (lane == 0) a.chain[blockIdx.x] = left;
+    copies_commit();
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+
+    // ---- the task ends: what comes behind it ----
+    if (it >= -1 && it >= n_mine - 1) {
+      copies_wait<0>();
+      __syncwarp();
+      pending = true;
+      pending_whole = WHOLE || (g.j0 == 0 && g.j1 == g.tiles);
+      pending_slot = 2 * (int)blockIdx.x + (g.j0 == 0 ? 1 : 0);       // a task's first part, a later one
+      more = false;
+      if constexpr (!WHOLE) {
+        left.row = g.s.first + g.tile * rpt;
+        left.head = g.hd;
+        left.cols = min(rpt, g.s.n - g.tile * rpt) * G;
+        left.live = __ballot_sync(0xffffffffu, lane < kCols && len_s[lane < kCols ? lane : 0] >= 0);
+        left.c0 = -1;
+        if (g.j1 < g.tiles) { left.c0 = (int)quotient(g.task_start + kQaTaskUnits, per); left.c1 = (int)quotient(g.task_start + kQaTaskUnits + g.tiles - 1, per); }
+        if (f < f1) {
+          if (f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) {
+            seq_start = f;
+            do g.s = rows_of(a, ++g.seq, -1, 0, false, st); while (g.s.n == 0 && g.seq + 1 < a.n_seq);      // (there is one: the share goes on)
+          }
+          if (g.s.n > 0) {
+            cut();
+            more = g.j1 > g.j0;
+          }
+        }
       }
-      return;
-    } else if (!kAhead) {
-      __syncthreads();                                                // the exchange has been read
-      first_copies(n_mine);
+      n_mine = more ? tiles_mine() : 0;
+      stage = 0;
+      it = -kStages - 1;
     }
   }
-  if (WHOLE) {
+  if constexpr (WHOLE) {
     __syncthreads();
     griddep_launch();
-  } else if (tid == 0) a.chain[blockIdx.x].c0 = -1;                   // (a share that ends before the first tile of its only task)
+  } else if (tid == 0) a.chain[blockIdx.x] = left;
 }
 
 // The parts of tasks that went over several blocks, joined in their order.  The blocks c0 <= b < c1 that such a task leaves share its (16 dims, 8 columns) units; a block's
@@ -654,7 +665,7 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
     const int in = warp / groups, g = warp - in * groups, u = me + (u0 + in) * blocks;
     const bool has = in < kQjWarps / groups && u0 + in < mine;
     const int c = has ? u / NT : 0, nt = has ? u - c * NT : 0;
-    Joined r = {{-INFINITY, -INFINITY}, {-INFINITY, -INFINITY}, {0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    Joined r = {{kNothing, kNothing}, {kNothing, kNothing}, {0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     for (int p0 = g; has && p0 < parts; p0 += groups * kQjBatch) {
       float sv[kQjBatch][6];
       float4 v[kQjBatch];
@@ -677,8 +688,8 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const float m = fmaxf(r.m[x], sv[b][3 * x]), mp = fmaxf(r.mp[x], sv[b][3 * x + 1]);
-          r.z[x] = fmaf(sv[b][3 * x + 2], ptx::fast_exp2(sv[b][3 * x] - no_inf(m)), r.z[x] * ptx::fast_exp2(r.m[x] - no_inf(m)));
-          const float al = ptx::fast_exp2(r.mp[x] - no_inf(mp)), w = ptx::fast_exp2(sv[b][3 * x + 1] - no_inf(mp));
+          r.z[x] = fmaf(sv[b][3 * x + 2], ptx::fast_exp2(sv[b][3 * x] - m), r.z[x] * ptx::fast_exp2(r.m[x] - m));
+          const float al = ptx::fast_exp2(r.mp[x] - mp), w = ptx::fast_exp2(sv[b][3 * x + 1] - mp);
           r.acc[x] = fmaf(w, x ? v[b].y : v[b].x, r.acc[x] * al);
           r.acc[2 + x] = fmaf(w, x ? v[b].w : v[b].z, r.acc[2 + x] * al);
           r.m[x] = m; r.mp[x] = mp;
@@ -694,8 +705,8 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const float m = fmaxf(r.m[x], n.m[x]), mp = fmaxf(r.mp[x], n.mp[x]);
-            const float wr = ptx::fast_exp2(r.mp[x] - no_inf(mp)), wn = ptx::fast_exp2(n.mp[x] - no_inf(mp));
-            r.z[x] = r.z[x] * ptx::fast_exp2(r.m[x] - no_inf(m)) + n.z[x] * ptx::fast_exp2(n.m[x] - no_inf(m));
+            const float wr = ptx::fast_exp2(r.mp[x] - mp), wn = ptx::fast_exp2(n.mp[x] - mp);
+            r.z[x] = r.z[x] * ptx::fast_exp2(r.m[x] - m) + n.z[x] * ptx::fast_exp2(n.m[x] - m);
             r.acc[x] = r.acc[x] * wr + n.acc[x] * wn;
             r.acc[2 + x] = r.acc[2 + x] * wr + n.acc[2 + x] * wn;
             r.m[x] = m; r.mp[x] = mp;
@@ -709,10 +720,10 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
       const int col = nt * 8 + tig * 2 + x, rr = col / G, head = ch.head * G + col - rr * G;
       if (col >= ch.cols || !(ch.live >> col & 1)) continue;
       const bool none = r.z[x] == 0.f;
-      const float norm = none ? 0.f : 1.f / (r.z[x] * 16384.f), grow = none ? 0.f : exp2f(r.mp[x] - r.m[x]);
+      const float norm = none ? 0.f : one_over(r.z[x] * 16384.f), grow = none ? 0.f : ptx::fast_exp2(r.mp[x] - r.m[x]);
       const long long row = ch.row + rr;
       *reinterpret_cast<__nv_bfloat162*>(a.out + (row * a.H + head) * D + c * 16 + gid * 2) = __floats2bfloat162_rn(r.acc[x] * norm * grow, r.acc[2 + x] * norm * grow);
-      if (c == 0 && gid == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = none ? -INFINITY : (r.m[x] + log2f(r.z[x])) * 0.6931471805599453f;
+      if (c == 0 && gid == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = none ? -INFINITY : (r.m[x] + log2_of(r.z[x])) * 0.6931471805599453f;
     }
   }
 }
