@@ -19,8 +19,8 @@ namespace relaxkv {
 
 constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaTile = 32;
 constexpr int kQaBlocks = 3 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
-constexpr int kQaLeastTiles = kQaWarps;          // tiles of a block's share, at least
-constexpr int kQaTaskUnits = 4;                  // what the start and the end of a task take, in tiles of a block
+constexpr int kQaLeast = 8;                      // units of a block's share, at least
+constexpr int kQaTaskUnits = 8;                  // what the start and the end of a task take, in tiles of a block
 constexpr int kQaColsMost = 32;                  // (row, head) columns of a block, at most
 constexpr int kQaSeqsMost = 4096;
 constexpr int kNoKey = -127;                     // exponent in shared memory of a token whose block does not exist
@@ -241,7 +241,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       if (w < warp) upto += sums_s[w];
       all += sums_s[w];
     }
-    per = max(quotient(all + gridDim.x - 1, gridDim.x), (long long)(kQaTaskUnits + kQaLeastTiles));
+    per = max(quotient(all + gridDim.x - 1, gridDim.x), (long long)kQaLeast);
     f = blockIdx.x * per;
     f1 = min(all, f + per);
     if (f >= f1) {
