@@ -586,7 +586,7 @@ typedef enum {
 } relaxkv_quantized_type;
 
 /* The 8-bit store of one layer.  Token t of block x of KV head g: values at k + x * block_stride + t * token_stride + g * head_stride (bytes = elements;
- * head_dim of them side by side), same for V, strides multiples of 16; exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V.
+ * head_dim of them side by side), same for V, strides multiples of 16, that of heads below 2^31; exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V.
  * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN.  All pointers 16-byte aligned. */
 typedef struct {
   void* k;
@@ -628,7 +628,7 @@ relaxkv_status relaxkv_rotary_frequencies(int32_t dims, double theta, int32_t sc
 /* relaxkv_qk_norm_rope for any rotary embedding and any strides: q_out = rotated norm of q, k_out likewise, one rounding to bf16 (angles in fp64 up to their
  * remainder, the rest in fp32).  Head h of row r: q + r * q_token_stride + h * q_head_stride, head_dim elements side by side; q_out is laid out like q and may be q
  * itself, k_out like k.  q or k may be NULL, its output with it (only the other one is turned).  Norm weights [head_dim] as in relaxkv_qk_norm_rope.  head_dim 64 or 128,
- * strides multiples of 8, positions device int32 [n_rows], negative ones turn backwards. */
+ * strides multiples of 8, those of heads below 2^31; positions device int32 [n_rows], negative ones turn backwards. */
 relaxkv_status relaxkv_qk_norm_rotate(
     const void* q, void* q_out, int64_t q_token_stride, int64_t q_head_stride, const void* k, void* k_out, int64_t k_token_stride, int64_t k_head_stride,
     int64_t n_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* w_q_norm, const void* w_k_norm, float eps, const int32_t* positions,

@@ -24,8 +24,9 @@ struct TurnArgs {
   int8_t *exp_k, *exp_v;
   const int *positions, *slots;
   const double* freq;
-  long long q_token, q_head, k_token, k_head;            // strides of the bf16 rows
-  long long block_stride, token_stride, head_stride;     // of the store
+  long long q_token, k_token;                            // strides of the bf16 rows
+  long long block_stride, token_stride;                  // of the store
+  int q_head, k_head, head_stride;                       // from head to head
   long long n_rows;
   int n_blocks, block_shift, H, Hkv;
   int part;                                              // dims that turn, 0: none
@@ -50,15 +51,25 @@ __device__ __forceinline__ void lane_dims(int gl, int part, int* lo, int* hi) {
   *hi = turned ? part / 2 + 4 * gl : 8 * gl + 4;
 }
 
-// Eight elements by the four angles (cosine c, sine s) of their pairs: element i and i + 4, or 2 i and 2 i + 1.
+// Eight elements by the four angles (cosine c, sine s, -s) of their pairs: element i and i + 4, or 2 i and 2 i + 1.
 template <bool HALF>
-__device__ __forceinline__ void turn_8(float* f, const float* c, const float* s) {
+__device__ __forceinline__ void turn_8(float* f, const float* c, const float* s, const float* ns) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float &a = f[HALF ? i : 2 * i], &b = f[HALF ? i + 4 : 2 * i + 1];
-    const float x = a * c[i] - b * s[i], y = b * c[i] + a * s[i];
-    a = x; b = y;
+  for (int i = 0; i < 4; i += 2) {
+    float &a0 = f[HALF ? i : 2 * i], &b0 = f[HALF ? i + 4 : 2 * i + 1], &a1 = f[HALF ? i + 1 : 2 * i + 2], &b1 = f[HALF ? i + 5 : 2 * i + 3];
+    float x0, x1, y0, y1;
+    ptx::mul2(x0, x1, b0, b1, ns[i], ns[i + 1]);
+    ptx::fma2(x0, x1, a0, a1, c[i], c[i + 1], x0, x1);
+    ptx::mul2(y0, y1, a0, a1, s[i], s[i + 1]);
+    ptx::fma2(y0, y1, b0, b1, c[i], c[i + 1], y0, y1);
+    a0 = x0; a1 = x1; b0 = y0; b1 = y1;
   }
+}
+
+__device__ __forceinline__ float largest_3(float a, float b, float c) {        // of absolute values; NaN where one is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return d;
 }
 
 // Cosines and sines of the block's rows, [ROWS][part / 2], one per thread at a time.
@@ -118,18 +129,20 @@ turn_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   int dlo, dhi;
   lane_dims<HALF>(gl, a.part, &dlo, &dhi);
   const bool turned = gl < a.part / 8;
-  auto place = [&](int h, const uint16_t* q, const uint16_t* k, const uint16_t* v) -> const uint16_t* {      // of head h of this row
-    return h < a.H ? q + row * a.q_token + h * a.q_head : (h < heads ? k + (h - a.H) * a.k_head : v + (h - heads) * a.k_head) + row * a.k_token;
-  };
+  // where this lane's part of head 0 would be, of the inputs and outputs, if all heads stood there one behind the other
+  const long long q_at = row * a.q_token + dlo, k_at = row * a.k_token - (long long)a.H * a.k_head + dlo;
+  const uint16_t *pq = a.q + q_at, *pk = a.k + k_at, *pv = a.v + k_at - (long long)a.Hkv * a.k_head;
+  const int dd = dhi - dlo;
   auto load = [&](int h, uint2& lo, uint2& hi) {
     lo = hi = make_uint2(0u, 0u);
     if (h >= total) return;
-    const uint16_t* p = place(h, a.q, a.k, a.v);
+    const bool of_q = h < a.H;
+    const uint16_t* p = (of_q ? pq : h < heads ? pk : pv) + (long long)h * (of_q ? a.q_head : a.k_head);
     if constexpr (HALF) {
-      lo = *reinterpret_cast<const uint2*>(p + dlo);
-      hi = *reinterpret_cast<const uint2*>(p + dhi);
+      lo = *reinterpret_cast<const uint2*>(p);
+      hi = *reinterpret_cast<const uint2*>(p + dd);
     } else {
-      const uint4 w = *reinterpret_cast<const uint4*>(p + dlo);
+      const uint4 w = *reinterpret_cast<const uint4*>(p);
       lo = make_uint2(w.x, w.y); hi = make_uint2(w.z, w.w);
     }
   };
@@ -149,12 +162,16 @@ turn_rows_kernel(const TurnArgs a, DeviceStatus* st) {
     at = block * a.block_stride + token * a.token_stride;
     exp_at = (((long long)block * a.Hkv) << a.block_shift) + token;
   } else if (STORE != STORE_BF16 && slot != -1 && unit0 == 0 && gl == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ROWS, (int)row, slot);
+  uint16_t *oq = a.q_out + q_at, *ok = a.k_out + k_at;
+  uint8_t *sk = a.store_k + at - (long long)a.H * a.head_stride + dlo, *sv = a.store_v + at - (long long)heads * a.head_stride + dlo;
   __syncthreads();
-  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f}, ns[4];
   if (turned) {
     *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(&cos_s[rr][gl * 4]);
     *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(&sin_s[rr][gl * 4]);
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ns[e] = -s[e];
   // (a warp's trips depend on its first head alone: the sums below need whole warps)
   for (int p0 = pair0; p0 < total; p0 += U * kUnits) {
     uint2 nlo[U], nhi[U];
@@ -166,49 +183,55 @@ turn_rows_kernel(const TurnArgs a, DeviceStatus* st) {
       float f[8];
       unpack_8(lo[u], hi[u], f);
       if (first < heads && a.wq != nullptr) {
-        float ss = 0.f;
+        float s0, s1;
+        ptx::mul2(s0, s1, f[0], f[1], f[0], f[1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
+        for (int e = 2; e < 8; e += 2) ptx::fma2(s0, s1, f[e], f[e + 1], f[e], f[e + 1], s0, s1);
+        float ss = s0 + s1;
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         if (h < heads) {
           const float inv = rsqrtf(ss * (1.f / D) + a.eps);
           const float* w = w_s[h < a.H ? 0 : 1];
-          const float4 w0 = *reinterpret_cast<const float4*>(w + dlo), w1 = *reinterpret_cast<const float4*>(w + dhi);
-          const float wv[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * wv[e];
+          for (int hf = 0; hf < 2; ++hf) {
+            const float4 wv = *reinterpret_cast<const float4*>(w + (hf ? dhi : dlo));
+            float* x = f + 4 * hf;
+            ptx::mul2(x[0], x[1], x[0], x[1], inv, inv);
+            ptx::mul2(x[2], x[3], x[2], x[3], inv, inv);
+            ptx::mul2(x[0], x[1], x[0], x[1], wv.x, wv.y);
+            ptx::mul2(x[2], x[3], x[2], x[3], wv.z, wv.w);
+          }
         }
       }
-      if (turned && h < heads) turn_8<HALF>(f, c, s);
+      if (turned && h < heads) turn_8<HALF>(f, c, s, ns);
       if (STORE == STORE_BF16 || first < a.H) {
         if (h < total && (STORE == STORE_BF16 || h < a.H)) {
-          uint16_t* p = const_cast<uint16_t*>(place(h, a.q_out, a.k_out, nullptr));
+          uint16_t* p = (STORE != STORE_BF16 || h < a.H ? oq : ok) + (long long)h * (STORE != STORE_BF16 || h < a.H ? a.q_head : a.k_head);
           const bool changed = turned || a.wq != nullptr;        // (what stays keeps every bit, those of a NaN too)
           const uint2 r0 = changed ? pack_bf16(f) : lo[u], r1 = changed ? pack_bf16(f + 4) : hi[u];
           if constexpr (HALF) {
-            *reinterpret_cast<uint2*>(p + dlo) = r0;
-            *reinterpret_cast<uint2*>(p + dhi) = r1;
-          } else *reinterpret_cast<uint4*>(p + dlo) = make_uint4(r0.x, r0.y, r1.x, r1.y);
+            *reinterpret_cast<uint2*>(p) = r0;
+            *reinterpret_cast<uint2*>(p + dd) = r1;
+          } else *reinterpret_cast<uint4*>(p) = make_uint4(r0.x, r0.y, r1.x, r1.y);
         }
       }
       if (STORE != STORE_BF16 && first + kPerWarp > a.H) {     // some of this warp's heads go to the store
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+        const float t0 = largest_3(fabsf(f[0]), f[1], f[2]), t1 = largest_3(fabsf(f[3]), f[4], f[5]);
+        uint32_t top = __float_as_uint(largest_3(largest_3(t0, f[6], f[7]), t1, t1));       // (the order of bits is that of numbers, infinity, NaN)
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
         if (stored && h >= a.H && h < total) {
-          const int e = store_exponent<STORE>(top), g = h < heads ? h - a.H : h - heads;
+          const int e = store_exponent<STORE>(top);
           const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
           uint32_t b0 = 0, b1 = 0;
           if (e != kExpNone) { b0 = store_bytes<STORE>(f, inv); b1 = store_bytes<STORE>(f + 4, inv); }
-          uint8_t* p = (h < heads ? a.store_k : a.store_v) + at + g * a.head_stride;
+          uint8_t* p = (h < heads ? sk : sv) + (long long)h * a.head_stride;
           if constexpr (HALF) {
-            *reinterpret_cast<uint32_t*>(p + dlo) = b0;
-            *reinterpret_cast<uint32_t*>(p + dhi) = b1;
-          } else *reinterpret_cast<uint2*>(p + dlo) = make_uint2(b0, b1);
-          if (gl == 0) (h < heads ? a.exp_k : a.exp_v)[exp_at + ((long long)g << a.block_shift)] = (int8_t)e;
+            *reinterpret_cast<uint32_t*>(p) = b0;
+            *reinterpret_cast<uint32_t*>(p + dd) = b1;
+          } else *reinterpret_cast<uint2*>(p) = make_uint2(b0, b1);
+          if (gl == 0) (h < heads ? a.exp_k : a.exp_v)[exp_at + ((h < heads ? h - a.H : h - heads) << a.block_shift)] = (int8_t)e;
         }
       }
       lo[u] = nlo[u]; hi[u] = nhi[u];
@@ -237,19 +260,21 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   const int block = stored ? slot >> a.block_shift : 0, token = stored ? slot & ((1 << a.block_shift) - 1) : 0;
   const long long at = block * a.block_stride + token * a.token_stride, exp_at = (((long long)block * a.Hkv) << a.block_shift) + token;
   if (!stored && slot != -1 && unit0 == 0 && gl == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ROWS, (int)row, slot);
+  const uint8_t *pk = a.store_k + at + dlo, *pv = a.store_v + at - (long long)a.Hkv * a.head_stride + dlo;      // (value heads behind the key heads)
+  const int8_t *ek = a.exp_k + exp_at, *ev = a.exp_v + exp_at - (a.Hkv << a.block_shift);
+  const int dd = dhi - dlo;
   auto load = [&](int u, uint32_t& w0, uint32_t& w1, int& e) {
     w0 = w1 = 0u; e = 0;
     if (u >= total) return;
-    const int g = u < a.Hkv ? u : u - a.Hkv;
-    const uint8_t* p = (u < a.Hkv ? a.store_k : a.store_v) + at + g * a.head_stride;
+    const uint8_t* p = (u < a.Hkv ? pk : pv) + (long long)u * a.head_stride;
     if constexpr (HALF) {
-      w0 = *reinterpret_cast<const uint32_t*>(p + dlo);
-      w1 = *reinterpret_cast<const uint32_t*>(p + dhi);
+      w0 = *reinterpret_cast<const uint32_t*>(p);
+      w1 = *reinterpret_cast<const uint32_t*>(p + dd);
     } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(p + dlo);
+      const uint2 w = *reinterpret_cast<const uint2*>(p);
       w0 = w.x; w1 = w.y;
     }
-    e = (u < a.Hkv ? a.exp_k : a.exp_v)[exp_at + ((long long)g << a.block_shift)];
+    e = (u < a.Hkv ? ek : ev)[u << a.block_shift];
   };
   uint32_t w0[U], w1[U];
   int e[U];
@@ -259,11 +284,15 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
     make_angles<ROWS>(a.positions, a.freq, a.part / 2, a.amplitude, row0, a.n_rows, cos_s, sin_s);
     __syncthreads();
   }
-  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f}, ns[4];
   if (turned) {
     *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(&cos_s[rr][gl * 4]);
     *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(&sin_s[rr][gl * 4]);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ns[i] = -s[i];
+  const long long k_at = row * a.k_token + dlo;
+  uint16_t *ok = a.k_out + k_at, *ov = a.v_out + k_at - (long long)a.Hkv * a.k_head;
   for (int u0 = unit0; u0 < total; u0 += U * kUnits) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -274,23 +303,27 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
       const uint32_t w[2] = {w0[u], w1[u]};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        uint32_t p[2];
-        if constexpr (TYPE == RELAXKV_INT8) { p[0] = int8_to_half2<0x4140>(w[i] ^ 0x80808080u); p[1] = int8_to_half2<0x4342>(w[i] ^ 0x80808080u); }
-        else { p[0] = e4m3_to_half2(w[i], 0); p[1] = e4m3_to_half2(w[i], 1); }
+        if constexpr (TYPE == RELAXKV_INT8) {                  // 2^23 + 128 + value, less 2^23 + 128, times the scale: products and sum are exact
+          const uint32_t b = w[i] ^ 0x80808080u;
+          const float less = -8388736.f * scale;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&p[j]));
-          f[4 * i + 2 * j] = v.x * scale; f[4 * i + 2 * j + 1] = v.y * scale;
+          for (int j = 0; j < 4; ++j) f[4 * i + j] = fmaf(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7550 | j)), scale, less);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t p = e4m3_to_half2(w[i], j);
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&p));
+            f[4 * i + 2 * j] = v.x * scale; f[4 * i + 2 * j + 1] = v.y * scale;
+          }
         }
       }
-      if (turned && h < a.Hkv) turn_8<HALF>(f, c, s);
-      const int g = h < a.Hkv ? h : h - a.Hkv;
-      uint16_t* out = (h < a.Hkv ? a.k_out : a.v_out) + row * a.k_token + g * a.k_head;
+      if (turned && h < a.Hkv) turn_8<HALF>(f, c, s, ns);
+      uint16_t* out = (h < a.Hkv ? ok : ov) + (long long)h * a.k_head;
       const uint2 r0 = pack_bf16(f), r1 = pack_bf16(f + 4);
       if constexpr (HALF) {
-        *reinterpret_cast<uint2*>(out + dlo) = r0;
-        *reinterpret_cast<uint2*>(out + dhi) = r1;
-      } else *reinterpret_cast<uint4*>(out + dlo) = make_uint4(r0.x, r0.y, r1.x, r1.y);
+        *reinterpret_cast<uint2*>(out) = r0;
+        *reinterpret_cast<uint2*>(out + dd) = r1;
+      } else *reinterpret_cast<uint4*>(out) = make_uint4(r0.x, r0.y, r1.x, r1.y);
       load(h + U * kUnits, w0[u], w1[u], e[u]);
     }
   }
@@ -320,7 +353,7 @@ static relaxkv_status check_rotary(const relaxkv_rotary* r, const int32_t* posit
   return RELAXKV_OK;
 }
 static bool bf16_rows_ok(const void* p, const void* out, int64_t token, int64_t head, int head_dim) {
-  return p && out && aligned16(p) && aligned16(out) && token >= head_dim && head >= head_dim && token % 8 == 0 && head % 8 == 0;
+  return p && out && aligned16(p) && aligned16(out) && token >= head_dim && head >= head_dim && head <= 0x7fffffff && token % 8 == 0 && head % 8 == 0;
 }
 static void set_rotary(TurnArgs& a, const relaxkv_rotary* r, const int32_t* positions) {
   if (!r) return;
@@ -328,7 +361,7 @@ static void set_rotary(TurnArgs& a, const relaxkv_rotary* r, const int32_t* posi
 }
 static void set_store(TurnArgs& a, const relaxkv_quantized_cache* c) {
   a.store_k = static_cast<uint8_t*>(c->k); a.store_v = static_cast<uint8_t*>(c->v); a.exp_k = c->k_exp; a.exp_v = c->v_exp;
-  a.block_stride = c->block_stride; a.token_stride = c->token_stride; a.head_stride = c->head_stride;
+  a.block_stride = c->block_stride; a.token_stride = c->token_stride; a.head_stride = (int)c->head_stride;
   a.n_blocks = c->n_blocks; a.block_shift = 31 - __builtin_clz((unsigned)c->block_size);
 }
 // Rows of a block: eight of so few heads that a warp has them in four trips, else one while the SMs hold the launch's blocks in two turns or less, four for more.
@@ -387,7 +420,7 @@ extern "C" relaxkv_status relaxkv_qk_norm_rotate(
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k);
   a.q_out = static_cast<uint16_t*>(q_out); a.k_out = static_cast<uint16_t*>(k_out);
   a.wq = static_cast<const uint16_t*>(w_q_norm); a.wk = static_cast<const uint16_t*>(w_k_norm);
-  a.q_token = q_token_stride; a.q_head = q_head_stride; a.k_token = k_token_stride; a.k_head = k_head_stride;
+  a.q_token = q_token_stride; a.q_head = (int)q_head_stride; a.k_token = k_token_stride; a.k_head = (int)k_head_stride;
   a.n_rows = n_rows; a.H = q ? n_q_heads : 0; a.Hkv = k ? n_kv_heads : 0; a.eps = eps;
   set_rotary(a, rotary, positions);
   const int per = rows_per_block(n_rows, a.H + a.Hkv, head_dim, sms);
@@ -415,7 +448,7 @@ extern "C" relaxkv_status relaxkv_append_quantized(
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
   a.q_out = static_cast<uint16_t*>(q_out);
   a.wq = static_cast<const uint16_t*>(w_q_norm); a.wk = static_cast<const uint16_t*>(w_k_norm);
-  a.q_token = q_token_stride; a.q_head = q_head_stride; a.k_token = k_token_stride; a.k_head = k_head_stride;
+  a.q_token = q_token_stride; a.q_head = (int)q_head_stride; a.k_token = k_token_stride; a.k_head = (int)k_head_stride;
   a.slots = slots; a.n_rows = n_rows; a.H = q ? n_q_heads : 0; a.Hkv = n_kv_heads; a.eps = eps;
   set_rotary(a, rotary, positions);
   set_store(a, store);
@@ -442,7 +475,7 @@ extern "C" relaxkv_status relaxkv_read_quantized(
   if (!st || sms <= 0) return RELAXKV_ERR_CUDA;
   TurnArgs a = {};
   a.k_out = static_cast<uint16_t*>(k_out); a.v_out = static_cast<uint16_t*>(v_out);
-  a.k_token = token_stride; a.k_head = head_stride;
+  a.k_token = token_stride; a.k_head = (int)head_stride;
   a.slots = slots; a.n_rows = n_rows; a.Hkv = n_kv_heads;
   set_rotary(a, rotary, positions);
   set_store(a, store);

@@ -16,7 +16,7 @@ inline relaxkv_status check_quantized(const relaxkv_quantized_cache* c, int32_t 
   if (n_kv_heads < 1 || n_kv_heads != c->n_kv_heads) return RELAXKV_ERR_INVALID_ARG;
   if (c->n_blocks < 1 || (long long)c->n_blocks * c->block_size > 0x7fffffffLL) return RELAXKV_ERR_INVALID_ARG;     // slots are int32
   if (c->block_stride < head_dim || c->token_stride < head_dim || c->head_stride < head_dim) return RELAXKV_ERR_INVALID_ARG;
-  if (c->block_stride % 16 || c->token_stride % 16 || c->head_stride % 16) return RELAXKV_ERR_INVALID_ARG;
+  if (c->block_stride % 16 || c->token_stride % 16 || c->head_stride % 16 || c->head_stride > 0x7fffffff) return RELAXKV_ERR_INVALID_ARG;
   return RELAXKV_OK;
 }
 
