@@ -41,6 +41,7 @@ struct QuantAttnArgs {
   long long block_stride, token_stride, head_stride, table_stride, n_rows;
   int table_width, n_seq, n_blocks, block_shift, max_len;
   int H, Hkv, G, rows_per_tile;
+  int split;                             // blocks of a cluster that share a row tile and KV head
   float scale_log2;
 };
 
@@ -177,7 +178,8 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   constexpr bool kQInRegs = NT <= 2;
   constexpr int kOwn = kChunks / kQaWarps;                            // pieces of the result that a warp adds up
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ ColStats stats_s[kQaWarps][kCols];
+  __shared__ ColStats stats_s[kQaWarps][kCols], result_s[WHOLE ? kCols : 1];
+  static_assert(kOwn * NT * 512 <= L::kBefore * L::kStage, "a warp's pieces of a cluster's part");
   __shared__ int len_s[kCols];                                        // tokens that a column sees; -1: none, and it is not written
   __shared__ float qscale_s[kCols];
   __shared__ int at_s[kCols];                                         // its row * H + head (less than 2^31: see the host's limit); -1: not written
@@ -196,26 +198,33 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   // ---- this block's share: units [f, f1) of the call, `per` to a block; a task counts kQaTaskUnits more than it has tiles, the time that its start and end take ----
   Segment g = {};
   long long f = 0, f1 = 0, per = 1, seq_start = 0;
-  if constexpr (WHOLE) {                                              // a block per row and KV head: the first of a tile's rows takes them all
-    const long long row = blockIdx.x / a.Hkv;
-    g.hd = (int)(blockIdx.x - row * a.Hkv);
+  int rank = 0;                                                       // of this block in its cluster
+  if constexpr (WHOLE) {                                              // a block, or a cluster, per row and KV head: the first of a tile's rows takes them all
+    const int unit = (int)blockIdx.x / a.split;
+    const long long row = unit / a.Hkv;
+    rank = (int)blockIdx.x - unit * a.split;
+    g.hd = unit - (int)row * a.Hkv;
     g.seq = a.row_seq[row];
+    const bool tell = tid == 0 && g.hd == 0 && rank == 0;
     bool mine = row < a.row_cu[a.n_seq] && g.seq != -1;
     if (mine && (g.seq < 0 || g.seq >= a.n_seq)) {
-      if (tid == 0 && g.hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
+      if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
       mine = false;
     }
     if (!mine) return;
-    g.s = rows_of(a, g.seq, -1, 0, tid == 0 && g.hd == 0, st);
+    g.s = rows_of(a, g.seq, -1, 0, tell, st);
     if (g.s.n == 0) return;
     if (row < g.s.first || row >= g.s.first + g.s.n) {
-      if (tid == 0 && g.hd == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
-      return;
+      if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
+      return;                                                         // (with it the other blocks of its cluster)
     }
     g.tile = (int)(row - g.s.first) / rpt;
     for (long long r = g.s.first + (long long)g.tile * rpt; r < row; ++r)
       if (a.row_seq[r] == g.seq) return;
-    g.tiles = g.j1 = tiles_of(g.s.len);
+    g.tiles = tiles_of(g.s.len);
+    const int each = (g.tiles + a.split - 1) / a.split;
+    g.j0 = min(g.tiles, rank * each);
+    g.j1 = min(g.tiles, g.j0 + each);
   } else {
     const int per_thread = (a.n_seq + kQaThreads - 1) / kQaThreads, i0 = tid * per_thread, i1 = min(a.n_seq, i0 + per_thread);
     auto units = [&](const SeqRows& x) -> long long { return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * (tiles_of(x.len) + kQaTaskUnits); };
@@ -463,8 +472,11 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
               wgt[w][x] = ptx::fast_exp2(stats_s[w][col].mp - bigp[x]);
             }
             if (!pending_whole && warp == 0 && gid == 0) {
-              float* p = a.part_s + ((long long)pending_slot * kQaColsMost + col) * 3;
-              p[0] = big[x]; p[1] = bigp[x]; p[2] = zs[x];
+              if constexpr (WHOLE) result_s[col] = {big[x], bigp[x], zs[x]};
+              else {
+                float* p = a.part_s + ((long long)pending_slot * kQaColsMost + col) * 3;
+                p[0] = big[x]; p[1] = bigp[x]; p[2] = zs[x];
+              }
             }
           }
           float acc[kOwn][4];
@@ -487,7 +499,8 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           if (!pending_whole) {
 #pragma unroll
             for (int i = 0; i < kOwn; ++i)
-              *reinterpret_cast<float4*>(a.part_o + (((long long)pending_slot * kChunks + warp * kOwn + i) * NT + nt) * 128 + lane * 4) =
+              *(WHOLE ? reinterpret_cast<float4*>(ring_ptr) + (i * NT + nt) * 32 + lane       // (in front of the exchange)
+                      : reinterpret_cast<float4*>(a.part_o + (((long long)pending_slot * kChunks + warp * kOwn + i) * NT + nt) * 128 + lane * 4)) =
                   make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
           } else {
 #pragma unroll
@@ -514,7 +527,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       const long long row_first = g.s.first + (long long)g.tile * rpt;
       const int cols = min(rpt, g.s.n - g.tile * rpt) * G;
       if (tid < kCols) {
-        const int r = tid / G, len = tid < cols ? row_tokens(a, g.seq, g.s, row_first + r, tid - r * G == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
+        const int r = tid / G, len = tid < cols ? row_tokens(a, g.seq, g.s, row_first + r, tid - r * G == 0 && g.hd == 0 && g.j0 == 0 && rank == 0, st) : -1;
         len_s[tid] = len;
         at_s[tid] = len < 0 ? -1 : (int)(row_first + r) * a.H + g.hd * G + tid - r * G;
       }
@@ -612,7 +625,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       copies_wait<0>();
       __syncwarp();
       pending = true;
-      pending_whole = WHOLE || (g.j0 == 0 && g.j1 == g.tiles);
+      pending_whole = WHOLE ? a.split == 1 : g.j0 == 0 && g.j1 == g.tiles;
       pending_slot = 2 * (int)blockIdx.x + (g.j0 == 0 ? 1 : 0);       // a task's first part, a later one
       more = false;
       if constexpr (!WHOLE) {
@@ -639,6 +652,43 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     }
   }
   if constexpr (WHOLE) {
+    if (a.split > 1) {
+      // ---- the parts of the cluster's blocks, added up in their order: unit u = (16 dims, 8 columns), the warps of all blocks take them in turn ----
+      ptx::cluster_sync();
+      for (int u = rank * kQaWarps + warp; u < kChunks * NT; u += a.split * kQaWarps) {
+        const int nt = u % NT, c = u / NT, owner = c / kOwn;
+        const uint32_t from = ptx::smem_u32(smem) + owner * L::kWarp + (((c - owner * kOwn) * NT + nt) * 32 + lane) * 16;
+        const uint32_t stats = ptx::smem_u32(&result_s[nt * 8 + tig * 2]);
+        float sm[2] = {kNothing, kNothing}, smp[2] = {kNothing, kNothing}, sz[2] = {0.f, 0.f}, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int b = 0; b < a.split; ++b) {
+          const uint32_t there = ptx::mapa_shared(from, b), of = ptx::mapa_shared(stats, b);
+          const float4 v = ptx::ld_cluster_f32x4(there);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float m1 = ptx::ld_cluster_f32(of + 12 * x), mp1 = ptx::ld_cluster_f32(of + 12 * x + 4), z1 = ptx::ld_cluster_f32(of + 12 * x + 8);
+            const float big = fmaxf(sm[x], m1), bigp = fmaxf(smp[x], mp1), was = ptx::fast_exp2(smp[x] - bigp), w1 = ptx::fast_exp2(mp1 - bigp);
+            sz[x] = sz[x] * ptx::fast_exp2(sm[x] - big) + z1 * ptx::fast_exp2(m1 - big);
+            acc[x] = acc[x] * was + (x ? v.y : v.x) * w1;
+            acc[2 + x] = acc[2 + x] * was + (x ? v.w : v.z) * w1;
+            sm[x] = big; smp[x] = bigp;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int at = at_s[nt * 8 + tig * 2 + x];
+          if (at < 0) continue;
+          const bool none = sz[x] == 0.f;
+          const float norm = none ? 0.f : one_over(sz[x] * 16384.f), grow = none ? 0.f : ptx::fast_exp2(smp[x] - sm[x]);
+          *reinterpret_cast<__nv_bfloat162*>(a.out + (long long)at * D + c * 16 + gid * 2) = __floats2bfloat162_rn(acc[x] * norm * grow, acc[2 + x] * norm * grow);
+          if (c == 0 && gid == 0 && a.lse_out) {
+            const int row = at / a.H;
+            a.lse_out[(at - row * a.H) * a.n_rows + row] = none ? -INFINITY : (sm[x] + log2_of(sz[x])) * 0.6931471805599453f;
+          }
+        }
+      }
+      ptx::cluster_sync();                                                 // nobody leaves while its part is read
+    }
     __syncthreads();
     griddep_launch();
   } else if (tid == 0) a.chain[blockIdx.x] = left;
@@ -751,11 +801,11 @@ static cudaError_t launch_attend(const QuantAttnArgs& a, long long blocks, Devic
     if (e != cudaSuccess) return e;
     attr_done[dev].store(1, std::memory_order_release);
   }
-  return launch_chained(kern, dim3((unsigned)blocks), kQaThreads, (QaSmem<D, NT>::kTotal), stream, a, st);
+  return launch_chained_clusters(WHOLE ? a.split : 1, kern, dim3((unsigned)blocks), kQaThreads, (QaSmem<D, NT>::kTotal), stream, a, st);
 }
 template <int D, int NT>
 static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
-  const long long blocks = whole ? a.n_rows * a.Hkv : std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
+  const long long blocks = whole ? a.n_rows * a.Hkv * a.split : std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
   cudaError_t e;
   if (type == RELAXKV_INT8) e = whole ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream);
   else e = whole ? launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
@@ -812,7 +862,11 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   const long long cols = (long long)a.G * ((r->n_rows + r->n_seq - 1) / r->n_seq);
   const int nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
   a.rows_per_tile = 8 * nt / a.G;
-  const bool whole = r->max_len <= 1024 && r->n_rows * a.Hkv <= 0x7fffffffLL;
+  // Blocks of a row tile and KV head: as many as leave each warp two tiles, where that many run at once.
+  const long long items = r->n_rows * a.Hkv, tiles = (r->max_len + kQaTile - 1LL) / kQaTile;
+  a.split = 1;
+  while (a.split < 8 && 2 * a.split * items <= 2 * sms && 2 * a.split * kQaWarps <= tiles) a.split *= 2;
+  const bool whole = tiles <= (a.split > 1 ? 16LL * a.split : 32) && items * a.split <= 0x7fffffffLL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return cuda_ok(head_dim == 128 ? launch_attend_d<128>(nt, store->type, whole, a, sms, st, s) : launch_attend_d<64>(nt, store->type, whole, a, sms, st, s));
 }
