@@ -12,38 +12,14 @@
 // sequence's end is filled with zeros and never read), eight warps to an SM with two tiles of 8 KB in flight each.  The work of a call - (sequence, KV head, row tile, 32
 // tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths: a block's first and last task may be
 // parts of one, whose results a second small kernel joins in the order of the blocks.
-#include "quantized_cache.cuh"
-#include "sm100_ptx.cuh"
+#include "quantized_attention.cuh"
 
 namespace relaxkv {
 
 constexpr int kQaWarps = 4, kQaThreads = kQaWarps * 32, kQaTile = 32;
 constexpr int kQaBlocks = 3 * 148;               // blocks that a call is cut into, at most (a workspace size does not depend on the device asked)
-constexpr int kQaLeast = 8;                      // units of a block's share, at least
-constexpr int kQaTaskUnits = 8;                  // what the start and the end of a task take, in tiles of a block
 constexpr int kQaColsMost = 32;                  // (row, head) columns of a block, at most
-constexpr int kQaSeqsMost = 4096;
-constexpr int kNoKey = -127;                     // exponent in shared memory of a token whose block does not exist
 constexpr float kPShift = 14.f;                  // the largest weight is 2^14
-
-// A task that goes on in the next blocks, as the join finds it: blocks c0 to c1, its first row, KV head, columns, and which of them are written.
-struct __align__(16) Chain { int c0, c1, row, head, cols; uint32_t live; int none[2]; };
-
-struct QuantAttnArgs {
-  const uint16_t* q;
-  uint16_t* out;
-  float* lse_out;
-  const uint8_t *k, *v;
-  const int8_t *k_exp, *v_exp;
-  const int *row_cu, *row_seq, *row_len, *table;
-  float *part_o, *part_s;
-  struct Chain* chain;
-  long long block_stride, token_stride, head_stride, table_stride, n_rows;
-  int table_width, n_seq, n_blocks, block_shift, max_len;
-  int H, Hkv, G, rows_per_tile;
-  int split;                             // blocks of a cluster that share a row tile and KV head
-  float scale_log2;
-};
 
 template <int D, int NT>
 struct QaSmem {
@@ -112,47 +88,7 @@ __device__ __forceinline__ float max_over_tokens(float x) {              // lane
   x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
   return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
 }
-// A maximum of nothing: no score lies below it, and what is taken from it stays a number (scores of -inf weigh nothing beside it, either).
-constexpr float kNothing = -3.4028234663852886e38f;
-__device__ __forceinline__ float log2_of(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float one_over(float x) {
-  float y;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Rows and tokens of a sequence; rows 0: none to work on.
-struct SeqRows { int first, n, len; };
-// guess_len: row_len[guess], read before it is known to be the last row's.
-__device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, int guess, int guess_len, bool tell, DeviceStatus* st) {
-  SeqRows s = {a.row_cu[seq], 0, 0};
-  const int end = a.row_cu[seq + 1];
-  if (s.first < 0 || end < s.first || end > a.n_rows) {
-    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, end, seq);
-    return s;
-  }
-  if (end == s.first) return s;
-  s.len = end - 1 == guess ? guess_len : a.row_len[end - 1];
-  if (s.len < 0 || s.len > a.max_len || s.len > ((long long)a.table_width << a.block_shift)) {
-    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, s.len, seq);
-    return s;
-  }
-  s.n = end - s.first;
-  return s;
-}
-// Tokens that a row of a sequence sees; -1: the row is left alone.
-__device__ __forceinline__ int row_tokens(const QuantAttnArgs& a, int seq, const SeqRows& s, long long row, bool tell, DeviceStatus* st) {
-  const int rs = a.row_seq[row], len = a.row_len[row];
-  if (rs == seq && len >= 0 && len <= s.len) return len;
-  if (tell && rs != -1) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, rs == seq ? len : rs, (int)row);
-  return -1;
-}
-
-__device__ __forceinline__ int tiles_of(int len) { return max(1, (int)(((long long)len + kQaTile - 1) / kQaTile)); }      // (one without tokens writes the zeros)
+using QaWalk = Walk<kQaTile, 8, 8, kQaThreads>;
 
 // What is known of a column: a maximum of the scores, the reference of scores + exponents of the values (in log2 units), sum of the weights.
 struct ColStats { float m, mp, z; };
@@ -161,13 +97,6 @@ __device__ __forceinline__ bool some_byte_below_2(uint32_t w) {
   const uint32_t x = w & 0xfefefefeu;
   return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
 }
-
-__device__ __forceinline__ long long quotient(long long a, long long b) {      // of numbers from 0 on; in 32 bits where these hold them
-  return ((a | b) >> 31) == 0 ? (long long)((int)a / (int)b) : a / b;
-}
-
-// A block's share of a task: (sequence, KV head, row tile) and the 32-token tiles [j0, j1) of it.
-struct Segment { int seq, hd, tile, j0, j1, tiles; SeqRows s; long long task_start; };
 
 template <int D, int TYPE, int NT, bool WHOLE>
 __global__ void __launch_bounds__(kQaThreads, QaSmem<D, NT>::kBlocksPerSm)
@@ -184,10 +113,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   __shared__ float qscale_s[kCols];
   __shared__ int at_s[kCols];                                         // its row * H + head (less than 2^31: see the host's limit); -1: not written
   __shared__ __align__(16) uint2 q_s[kQInRegs ? 1 : kChunks][kQInRegs ? 1 : NT][32];
-  __shared__ long long sums_s[kQaWarps];
-  __shared__ long long start_s;
-  __shared__ int seq_s;
-  __shared__ SeqRows rows_s;
+  __shared__ QaWalk::Shared walk_s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * L::kWarp;
   uint8_t* ring_ptr = smem + warp * L::kWarp;
@@ -195,9 +121,8 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   if (!WHOLE) griddep_launch();                                       // (the join's blocks come as these leave, and wait)
   griddep_wait();
 
-  // ---- this block's share: units [f, f1) of the call, `per` to a block; a task counts kQaTaskUnits more than it has tiles, the time that its start and end take ----
-  Segment g = {};
-  long long f = 0, f1 = 0, per = 1, seq_start = 0;
+  // ---- this block's share ----
+  QaWalk g;
   int rank = 0;                                                       // of this block in its cluster
   if constexpr (WHOLE) {                                              // a block, or a cluster, per row and KV head: the first of a tile's rows takes them all
     const int unit = (int)blockIdx.x / a.split;
@@ -221,80 +146,15 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     g.tile = (int)(row - g.s.first) / rpt;
     for (long long r = g.s.first + (long long)g.tile * rpt; r < row; ++r)
       if (a.row_seq[r] == g.seq) return;
-    g.tiles = tiles_of(g.s.len);
+    g.tiles = QaWalk::tiles_of(g.s.len);
     const int each = (g.tiles + a.split - 1) / a.split;
     g.j0 = min(g.tiles, rank * each);
     g.j1 = min(g.tiles, g.j0 + each);
   } else {
-    const int per_thread = (a.n_seq + kQaThreads - 1) / kQaThreads, i0 = tid * per_thread, i1 = min(a.n_seq, i0 + per_thread);
-    auto units = [&](const SeqRows& x) -> long long { return x.n == 0 ? 0 : (long long)((x.n + rpt - 1) / rpt) * a.Hkv * (tiles_of(x.len) + kQaTaskUnits); };
-    long long mine = 0;
-    SeqRows x = {0, 0, 0};                                            // (the last of this thread's sequences: the only one, mostly)
-    const int each = (int)(a.n_rows / a.n_seq);                       // where all sequences have as many rows, the last one's length comes with the row numbers
-    for (int i = i0; i < i1; ++i) {
-      const int guess = max(0, (i + 1) * each - 1);
-      x = rows_of(a, i, guess, a.row_len[guess], blockIdx.x == 0, st);
-      mine += units(x);
-    }
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 31) sums_s[warp] = upto;
-    __syncthreads();
-    long long all = 0;
-#pragma unroll
-    for (int w = 0; w < kQaWarps; ++w) {
-      if (w < warp) upto += sums_s[w];
-      all += sums_s[w];
-    }
-    per = max(quotient(all + gridDim.x - 1, gridDim.x), (long long)kQaLeast);
-    f = blockIdx.x * per;
-    f1 = min(all, f + per);
-    if (f >= f1) {
+    if (!g.begin(a, walk_s, st)) {                                    // (or it ends before the first tile of its only task)
       if (tid == 0) a.chain[blockIdx.x].c0 = -1;
       return;
     }
-    if (f >= upto - mine && f < upto) {                               // the share begins in one of this thread's sequences
-      long long at = upto - mine;
-      int i = i0;
-      if (i + 1 < i1) {
-        x = rows_of(a, i, -1, 0, false, st);
-        for (long long n = units(x); f >= at + n && i + 1 < i1; n = units(x)) {
-          at += n;
-          x = rows_of(a, ++i, -1, 0, false, st);
-        }
-      }
-      seq_s = i;
-      start_s = at;
-      rows_s = x;
-    }
-    __syncthreads();
-    g.seq = seq_s;
-    seq_start = start_s;
-    g.s = rows_s;
-  }
-  // The part of the task at f that belongs to this block (no tiles: its share ends before the task's first).
-  auto cut = [&]() {
-    if constexpr (!WHOLE) {
-      g.tiles = tiles_of(g.s.len);
-      const int row_tiles = (g.s.n + rpt - 1) / rpt, task_units = g.tiles + kQaTaskUnits;
-      const long long task = quotient(f - seq_start, task_units);
-      g.task_start = seq_start + task * task_units;
-      g.hd = (int)quotient(task, row_tiles);
-      g.tile = (int)(task - (long long)g.hd * row_tiles);
-      const int o0 = (int)(f - g.task_start), o1 = (int)min((long long)task_units, o0 + (f1 - f));
-      g.j0 = max(0, o0 - kQaTaskUnits);
-      g.j1 = max(0, o1 - kQaTaskUnits);
-      f += o1 - o0;
-    }
-  };
-  cut();
-  if (!WHOLE && g.j1 <= g.j0) {                                       // (the share ends before the first tile of its only task)
-    if (tid == 0) a.chain[blockIdx.x].c0 = -1;
-    return;
   }
 
   // ---- copies: lane l has piece l % (D / 16) of every (512 / D)-th token; block numbers of sixteen tiles at a time, one lane each half ----
@@ -312,7 +172,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   // The task before, whose results are still to be added up.
   bool pending = false, pending_whole = false, more = true;
   int pending_slot = 0;
-  Chain left = {-1, 0, 0, 0, 0, 0u, {0, 0}};
+  Chain left = {-1};
 
   // One trip per tile: its products, then the copies of the tile that takes its place in the ring.  A task's first trips have copies only; between them the results of the task
   // before are added up and the rows of this one fetched.  (Every part of the code stands here once: the instructions of a short call come from far.)
@@ -625,26 +485,17 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       copies_wait<0>();
       __syncwarp();
       pending = true;
-      pending_whole = WHOLE ? a.split == 1 : g.j0 == 0 && g.j1 == g.tiles;
-      pending_slot = 2 * (int)blockIdx.x + (g.j0 == 0 ? 1 : 0);       // a task's first part, a later one
+      pending_whole = WHOLE ? a.split == 1 : g.whole();
+      pending_slot = g.slot();
       more = false;
       if constexpr (!WHOLE) {
         left.row = g.s.first + g.tile * rpt;
         left.head = g.hd;
         left.cols = min(rpt, g.s.n - g.tile * rpt) * G;
-        left.live = __ballot_sync(0xffffffffu, lane < kCols && len_s[lane < kCols ? lane : 0] >= 0);
+        left.live[0] = __ballot_sync(0xffffffffu, lane < kCols && len_s[lane < kCols ? lane : 0] >= 0);
         left.c0 = -1;
-        if (g.j1 < g.tiles) { left.c0 = (int)quotient(g.task_start + kQaTaskUnits, per); left.c1 = (int)quotient(g.task_start + kQaTaskUnits + g.tiles - 1, per); }
-        if (f < f1) {
-          if (f - seq_start >= (long long)(g.tiles + kQaTaskUnits) * ((g.s.n + rpt - 1) / rpt) * a.Hkv) {
-            seq_start = f;
-            do g.s = rows_of(a, ++g.seq, -1, 0, false, st); while (g.s.n == 0 && g.seq + 1 < a.n_seq);      // (there is one: the share goes on)
-          }
-          if (g.s.n > 0) {
-            cut();
-            more = g.j1 > g.j0;
-          }
-        }
+        if (g.j1 < g.tiles) g.blocks_of(&left.c0, &left.c1);
+        more = g.next(a, st);
       }
       n_mine = more ? tiles_mine() : 0;
       stage = 0;
@@ -768,7 +619,7 @@ quantized_join_kernel(const __grid_constant__ QuantAttnArgs a) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int col = nt * 8 + tig * 2 + x, rr = col / G, head = ch.head * G + col - rr * G;
-      if (col >= ch.cols || !(ch.live >> col & 1)) continue;
+      if (col >= ch.cols || !(ch.live[0] >> col & 1)) continue;
       const bool none = r.z[x] == 0.f;
       const float norm = none ? 0.f : one_over(r.z[x] * 16384.f), grow = none ? 0.f : ptx::fast_exp2(r.mp[x] - r.m[x]);
       const long long row = ch.row + rr;
@@ -782,8 +633,9 @@ struct QuantWs { size_t part_o, part_s, chain, total; };
 static QuantWs quant_ws(int D) {
   QuantWs w{};
   size_t at = 0;
-  w.part_o = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * D * 4, 256);
-  w.part_s = at; at = align_up(at + (size_t)2 * kQaBlocks * kQaColsMost * 12, 256);
+  const size_t cols = 2 * std::max<size_t>(kQaBlocks * kQaColsMost, kQrBlocks * kQrRows);       // two parts of a block
+  w.part_o = at; at = align_up(at + cols * D * 4, 256);
+  w.part_s = at; at = align_up(at + cols * 12, 256);
   w.chain = at; at = align_up(at + (size_t)kQaBlocks * sizeof(Chain), 256);
   w.total = at;
   return w;
@@ -805,13 +657,17 @@ static cudaError_t launch_attend(const QuantAttnArgs& a, long long blocks, Devic
 }
 template <int D, int NT>
 static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
-  const long long blocks = whole ? a.n_rows * a.Hkv * a.split : std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
-  cudaError_t e;
-  if (type == RELAXKV_INT8) e = whole ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream);
-  else e = whole ? launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
-  if (e != cudaSuccess || whole) return e;
-  auto kern = quantized_join_kernel<D, NT>;
-  return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
+  const bool int8 = type == RELAXKV_INT8;
+  if constexpr (NT < 4)                                    // (more columns of long sequences go to the kernel of many rows)
+    if (!whole) {
+      const int blocks = std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
+      const cudaError_t e = int8 ? launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
+      if (e != cudaSuccess) return e;
+      auto kern = quantized_join_kernel<D, NT>;
+      return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
+    }
+  const long long blocks = a.n_rows * a.Hkv * a.split;
+  return int8 ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream);
 }
 template <int D>
 static cudaError_t launch_attend_d(int nt, int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
@@ -868,5 +724,9 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   while (a.split < 8 && 2 * a.split * items <= 2 * sms && 2 * a.split * kQaWarps <= tiles) a.split *= 2;
   const bool whole = tiles <= (a.split > 1 ? 16LL * a.split : 32) && items * a.split <= 0x7fffffffLL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (!whole && cols > 16) {
+    a.rows_per_tile = kQrRows / a.G;
+    return cuda_ok(launch_quantized_rows(a, head_dim, store->type, sms, st, s));
+  }
   return cuda_ok(head_dim == 128 ? launch_attend_d<128>(nt, store->type, whole, a, sms, st, s) : launch_attend_d<64>(nt, store->type, whole, a, sms, st, s));
 }

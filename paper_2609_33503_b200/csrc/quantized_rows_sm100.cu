@@ -1,0 +1,553 @@
+// Attention of many rows of a sequence over its tokens in the 8-bit store: a question, a long draft (relaxkv_quantized_attention).
+//
+// Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of one sequence), one KV head and a run of
+// 128-token tiles.  Four warps bring a tile: 8-bit values out of the pages in 16-byte pieces, made fp16 in registers, exactly, and written where the tensor cores read them
+// (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); one thread per row makes
+// weights of it, which go back to tensor memory as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest
+// of the sequence so far: p = 2^(s - m + 11 + e_t - E).  S is double-buffered, and so are the tiles; P and O are single.
+// Bound by the exponentials (16 K of a tile at 16 per clk, 1024 clk) and what stands around them; a tile's products take 512 clk, its conversion about as much on the same
+// schedulers.  Every wait is bounded.
+#include "quantized_attention.cuh"
+#include <atomic>
+
+namespace relaxkv {
+
+using namespace ptx;
+
+constexpr int kQrTile = 128, kQrThreads = 384;           // tokens of a tile; warps 0-3: a row per thread, 4-7: tiles, 8: products, three idle
+constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
+constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
+using QrWalk = Walk<kQrTile, 2, 2, 128>;
+
+template <int D>
+struct QrSmem {
+  static constexpr int kHalves = D / 64, kHalfBytes = kQrTile * 128, kTileBytes = kHalves * kHalfBytes;
+  static constexpr int kV = 2 * kTileBytes;              // K[2] | V[2]
+  static constexpr int kScale = 4 * kTileBytes;          // of the last four tiles: factors of the keys' scores, of the values' weights
+  static constexpr int kBar = kScale + 4 * 2 * kQrTile * 4;
+  // full_k[2], full_v[2], empty_k[2], empty_v[2], s[2], free[2], scale[4], p, o, q
+  static constexpr int kNumBars = 19;
+  static constexpr int kTotal = kBar + 8 * kNumBars;
+  static constexpr int kDynamic = kTotal + 1024;
+};
+
+// f16 x f16 -> fp32, A K-major.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int m, int n, int b_mn_major) {
+  return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+// Sixteen 8-bit values as fp16, in their order.
+template <int TYPE>
+__device__ __forceinline__ void to_half_16(const uint4& r, uint4* out) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  uint32_t h[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TYPE == RELAXKV_INT8) {
+      const uint32_t b = w[i] ^ 0x80808080u;
+      h[2 * i] = int8_to_half2<0x4140>(b); h[2 * i + 1] = int8_to_half2<0x4342>(b);
+    } else { h[2 * i] = e4m3_to_half2(w[i], 0); h[2 * i + 1] = e4m3_to_half2(w[i], 1); }
+  }
+  out[0] = make_uint4(h[0], h[1], h[2], h[3]);
+  out[1] = make_uint4(h[4], h[5], h[6], h[7]);
+}
+
+template <int D, int TYPE>
+__global__ void __launch_bounds__(kQrThreads, 1)
+quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
+  using L = QrSmem<D>;
+  constexpr uint32_t kTmemCols = 512, kO = 256, kP = 384, kQ = 448;      // tensor memory: S of even tiles | of odd tiles | O | P | Q
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ QrWalk::Shared walk_s;
+  __shared__ volatile uint32_t tmem_slot;
+  __shared__ volatile int abort_s;
+  __shared__ int largest_s[2][4], e_s[4];                  // largest exponents: of each of the four warps' tokens; of the values up to the last four tiles
+  __shared__ uint32_t gone_s[4][4];                      // tokens of the last four tiles whose blocks do not exist, or that are NaN
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t full_k = base + L::kBar, full_v = full_k + 16, empty_k = full_v + 16, empty_v = empty_k + 16, bar_s = empty_v + 16, bar_free = bar_s + 16,
+                 bar_scale = bar_free + 16, bar_p = bar_scale + 32, bar_o = bar_p + 8, bar_q = bar_o + 8;
+  volatile int* abort_flag = &abort_s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(full_k + 8 * i, 128); mbar_init(full_v + 8 * i, 128); mbar_init(empty_k + 8 * i, 1); mbar_init(empty_v + 8 * i, 1);
+      mbar_init(bar_s + 8 * i, 1); mbar_init(bar_free + 8 * i, 128);
+    }
+    for (int i = 0; i < 4; ++i) mbar_init(bar_scale + 8 * i, 128);
+    mbar_init(bar_p, 128); mbar_init(bar_o, 1); mbar_init(bar_q, 128);
+    abort_s = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 8) { tmem_alloc(smem_u32(const_cast<uint32_t*>(&tmem_slot)), kTmemCols); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  griddep_launch();                                      // (behind the allocation: the join's blocks take none)
+  griddep_wait();
+  QrWalk g;
+  const bool any = g.begin(a, walk_s, st);
+  const int status = *reinterpret_cast<volatile int*>(&st->status);
+  if (!any || status == RELAXKV_ERR_TIMEOUT) {
+    if (tid == 0) a.chain[blockIdx.x].c0 = -1;
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem_base, kTmemCols);
+    return;
+  }
+  const int G = a.G, rpt = a.rows_per_tile, bs_mask = (1 << a.block_shift) - 1;
+
+  // Registers: 12 warps x 168 at launch = 4 x 240 + 4 x 200 + 4 x 64.
+  if (warp < 4) {
+    reg_alloc<240>();
+    // ================= weights: thread = (row of the sequence, head) = lane of tensor memory =================
+    const int t_local = tid / G, in_group = tid - t_local * G;
+    const uint32_t lane_base = tmem_base + ((uint32_t)(warp * 32) << 16), t_o = lane_base + kO;
+    bool ok = true;
+    uint32_t jj = 0;                                     // tiles so far, over all tasks
+    for (bool more = true; more && ok;) {
+      const long long row = (long long)g.s.first + (long long)g.tile * rpt + t_local;
+      const int head = g.hd * G + in_group;
+      const bool exists = t_local < min(rpt, g.s.n - g.tile * rpt);
+      const int seen = exists ? row_tokens(a, g.seq, g.s, row, in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
+      // ---- Q: as fp16 times 2^-exponent, two dims to a word ----
+      float qs;
+      {
+        uint32_t w[D / 2], top = 0;
+        const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          const uint4 v = exists ? q[c] : make_uint4(0, 0, 0, 0);
+          w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
+        }
+#pragma unroll
+        for (int c = 0; c < D / 2; ++c) top = __vmaxu2(top, w[c] & 0x7fff7fffu);
+        top = max(top & 0xffffu, top >> 16);
+        const bool finite = top < 0x7f80u;
+        const int e = max((int)(top >> 7) - 127 - 14, -120);
+        const float inv = __uint_as_float((uint32_t)(127 - (finite ? e : 0)) << 23);
+#pragma unroll
+        for (int c = 0; c < D / 2; ++c) {
+          const __half2 x = __floats2half2_rn(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xffff0000u) * inv);
+          w[c] = finite ? *reinterpret_cast<const uint32_t*>(&x) : 0u;
+        }
+        qs = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) tmem_st32(lane_base + kQ + 32 * c, w + 32 * c);
+        tmem_wait_st();
+        tc_fence_before();
+      }
+      mbar_arrive(bar_q);
+      const bool busy = __any_sync(0xffffffffu, seen >= 0);          // a warp without rows only keeps step
+      float m = kNothing, z = 0.f;
+      int e_last = 0;
+      for (int j = g.j0; j < g.j1; ++j, ++jj) {
+        const uint32_t x = jj & 1, ph = (jj >> 1) & 1;
+        const int ring = jj & 3;
+        ok = mbar_wait(bar_scale + 8 * ring, (jj >> 2) & 1, abort_flag) && mbar_wait(bar_s + 8 * x, ph, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const int e_now = e_s[ring];
+        if (!busy) {
+          mbar_arrive(bar_free + 8 * x);
+          if (jj > 0) ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
+          if (ok) mbar_arrive(bar_p);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          e_last = e_now;
+          continue;
+        }
+        const float* ks = reinterpret_cast<const float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
+        const float* vs = ks + kQrTile;
+        const int limit = seen - j * kQrTile;
+        const bool slow = __any_sync(0xffffffffu, limit < kQrTile || (gone_s[ring][0] | gone_s[ring][1] | gone_s[ring][2] | gone_s[ring][3]) != 0);
+        // 32 scores times their keys' scales; what the row does not see (its tokens from `limit` on, tokens without a block) becomes -inf
+        auto scores = [&](int c, float* y) -> uint32_t {
+          uint32_t w[32];
+          tmem_ld32(lane_base + x * 128 + c * 32, w);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 k4 = *reinterpret_cast<const float4*>(ks + c * 32 + i);
+            mul2(y[i], y[i + 1], __uint_as_float(w[i]), __uint_as_float(w[i + 1]), k4.x, k4.y);
+            mul2(y[i + 2], y[i + 3], __uint_as_float(w[i + 2]), __uint_as_float(w[i + 3]), k4.z, k4.w);
+          }
+          uint32_t hidden = 0;
+          if (slow) {
+            hidden = limit >= 32 * (c + 1) ? 0u : limit <= 32 * c ? 0xffffffffu : 0xffffffffu << (limit - 32 * c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              if (ks[c * 32 + i] == -INFINITY) hidden |= 1u << i;
+              if (hidden >> i & 1) y[i] = -INFINITY;
+            }
+          }
+          return hidden;
+        };
+        float top = kNothing;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float y[32];
+          scores(c, y);
+          float mx[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(y[2 * e], y[2 * e + 1]);
+#pragma unroll
+          for (int i = 8; i < 32; i += 2) mx[(i >> 1) & 3] = fmax3(mx[(i >> 1) & 3], y[i], y[i + 1]);
+          top = fmax3(top, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        }
+        const float m_tile = top * qs, m_old = m;        // (qs > 0)
+        const bool grows = m_tile > m + kQrGrow;
+        if (grows) m = m_tile;
+        z *= fast_exp2(m_old - m);
+        // s * qs - m in one rounding keeps what the rounding of m has cut off: the same factor on all weights of the row, which their sum takes out again; very large logits are
+        // rounded first, or the factor would leave the range of fp16
+        const bool large = __any_sync(0xffffffffu, fabsf(m_tile) > kQrExact);
+        const float q2 = large ? 1.f : qs;
+        uint32_t pk[kQrTile / 2];
+        float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float y[32];
+          const uint32_t hidden = scores(c, y);
+          if (large) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] *= qs;
+          }
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float p[4];
+            const float4 v4 = *reinterpret_cast<const float4*>(vs + c * 32 + i);
+            fma2(p[0], p[1], y[i], y[i + 1], q2, q2, -m, -m);
+            fma2(p[2], p[3], y[i + 2], y[i + 3], q2, q2, -m, -m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = fast_exp2(p[e]);
+            add2(z0, z1, p[0], p[1]);
+            add2(z2, z3, p[2], p[3]);
+            mul2(p[0], p[1], p[0], p[1], v4.x, v4.y);
+            mul2(p[2], p[3], p[2], p[3], v4.z, v4.w);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+              const __half2 h = __floats2half2_rn(p[e], p[e + 1]);
+              pk[c * 16 + ((i + e) >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+          }
+          if (slow) {                                    // what is not seen weighs nothing, whatever its factor
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (hidden >> i & 1) pk[c * 16 + (i >> 1)] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+          }
+        }
+        z += (z0 + z1) + (z2 + z3);
+        tc_fence_before();
+        mbar_arrive(bar_free + 8 * x);                   // S and the factors have been read
+        if (jj > 0) {                                    // O of the tile before is complete, its P is not needed any more
+          ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        if (j > g.j0 && __any_sync(0xffffffffu, grows || e_now != e_last)) {
+          const float alpha = fast_exp2(m_old - m + (float)(e_last - e_now));
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+            tmem_st32(t_o + c * 32, o);
+          }
+        }
+        e_last = e_now;
+        tmem_st32(lane_base + kP, pk);
+        tmem_st32(lane_base + kP + 32, pk + 32);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p);
+      }
+      // ---- the results ----
+      if (ok) ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      const bool whole = g.whole();
+      const int slot = g.slot();
+      if (tid == 0) {
+        Chain c = {-1, 0, g.s.first + g.tile * rpt, g.hd, min(rpt, g.s.n - g.tile * rpt) * G};
+        if (g.j1 < g.tiles) g.blocks_of(&c.c0, &c.c1);
+        a.chain[blockIdx.x] = c;                         // (the last task's stays)
+      }
+      if (ok && busy) {
+        tc_fence_after();
+        const bool none = z == 0.f;                      // no token, or none of a logit above -inf (NaN stays NaN)
+        const float inv = none ? 0.f : __uint_as_float((uint32_t)(127 - (int)kQrShift) << 23) / z, grow = __uint_as_float((uint32_t)(e_last + 127) << 23);
+        const float lse2 = none ? -INFINITY : m + log2_of(z);
+        const int col = tid;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(t_o + c * 32, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = none ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv * grow);
+          if (seen >= 0 && !whole) {
+            float* p = a.part_o + ((long long)slot * kQrRows + col) * D + c * 32;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(p + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          } else if (seen >= 0) {
+            uint16_t* p = a.out + (row * a.H + head) * D + c * 32;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
+                w[e] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+              *reinterpret_cast<uint4*>(p + i) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        if (seen >= 0) {
+          if (!whole) a.part_s[(long long)slot * kQrRows + col] = lse2;
+          else if (a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = lse2 * 0.6931471805599453f;
+        }
+        tc_fence_before();
+      }
+      more = g.next(a, st);
+    }
+  } else if (warp < 8) {
+    reg_alloc<200>();
+    // ================= tiles: 8 bits -> fp16 in shared memory =================
+    constexpr int kPieces = D / 16, kAtOnce = 128 / kPieces, kTrips = kQrTile / kAtOnce;      // 16-byte pieces of a token; tokens that four warps bring at once
+    const int ct = tid - 128, my_token = ct / kPieces, my_piece = ct % kPieces, cw = ct >> 5;
+    // a piece is two chunks of 16 bytes; the lanes of the upper dims write theirs the other way round, so that eight lanes meet in no bank
+    const int half = my_piece / 4, c0 = (my_piece & 3) * 2;
+    bool ok = true;
+    uint32_t jj = 0;
+    int e_run = 0;
+    uint4 kr[kTrips], vr[kTrips];
+    for (bool more = true; more && ok; more = ok && g.next(a, st)) {
+      const int* pages = a.table + g.seq * a.table_stride;
+      const long long to_lane = (long long)g.hd * a.head_stride + my_piece * 16;
+      const long long exp_head = (long long)g.hd << a.block_shift;
+      auto block_numbers = [&](int j) -> int {           // of 16 tokens of tile j, for lanes 0 to 7; -1: behind the end
+        const long long t = (long long)j * kQrTile + lane * 16;
+        return lane < 8 && j < g.j1 && t < g.s.len ? pages[t >> a.block_shift] : -1;
+      };
+      auto load = [&](int j, int ids, const uint8_t* from, uint4* r) {
+#pragma unroll
+        for (int i = 0; i < kTrips; ++i) {
+          const int token = i * kAtOnce + my_token, id = __shfl_sync(0xffffffffu, ids, token >> 4);
+          const long long t = (long long)j * kQrTile + token;
+          const bool there = t < g.s.len && (unsigned)id < (unsigned)a.n_blocks;
+          r[i] = there ? *reinterpret_cast<const uint4*>(from + to_lane + id * a.block_stride + ((int)t & bs_mask) * a.token_stride) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      };
+      auto write = [&](uint32_t at, const uint4* r) {
+#pragma unroll
+        for (int i = 0; i < kTrips; ++i) {
+          uint4 h[2];
+          const int token = i * kAtOnce + my_token;
+          if (TYPE == RELAXKV_INT8) to_half_16<RELAXKV_INT8>(r[i], h); else to_half_16<RELAXKV_E4M3>(r[i], h);
+          uint8_t* p = base_ptr + at + half * L::kHalfBytes + token * 128;
+          const int f = half & 1;
+          *reinterpret_cast<uint4*>(p + (((c0 + f) ^ (token & 7)) << 4)) = f ? h[1] : h[0];
+          *reinterpret_cast<uint4*>(p + (((c0 + 1 - f) ^ (token & 7)) << 4)) = f ? h[0] : h[1];
+        }
+      };
+      int ids = block_numbers(g.j0);
+      load(g.j0, ids, a.k, kr);
+      e_run = -200;
+      for (int j = g.j0; j < g.j1; ++j, ++jj) {
+        const uint32_t x = jj & 1, ph = (jj >> 1) & 1;
+        const int ring = jj & 3;
+        load(j, ids, a.v, vr);
+        // ---- exponents: token ct ----
+        const int id = __shfl_sync(0xffffffffu, ids, ct >> 4);
+        const long long t = (long long)j * kQrTile + ct;
+        const bool inside = t < g.s.len, there = inside && (unsigned)id < (unsigned)a.n_blocks;
+        if (inside && !there && (ct & 15) == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+        int ek = 0, ev = -200;
+        if (there) {
+          const long long at = (((long long)id * a.Hkv) << a.block_shift) + exp_head + ((int)t & bs_mask);
+          ek = a.k_exp[at];
+          ev = a.v_exp[at];
+        }
+        ids = block_numbers(j + 1);
+        const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
+        if (lane == 0) largest_s[x][cw] = ev_max;        // (two: a warp may be a tile ahead)
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
+        const int e_now = max(e_run, kExpLeast);         // (no token yet: anything)
+        if (jj > 1) {
+          ok = mbar_wait(empty_k + 8 * x, ph ^ 1u, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+        }
+        if (!ok) break;
+        write(x * L::kTileBytes, kr);
+        float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
+        const float nan = __uint_as_float(0x7fc00000u);
+        const int down = ev - e_now + (int)kQrShift;     // (far below: nothing)
+        ks[ct] = there ? exp_scale(ek) : -INFINITY;
+        ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
+        const uint32_t odd = __ballot_sync(0xffffffffu, !there || ek == kExpNone || ev == kExpNone);
+        if (lane == 0) gone_s[ring][cw] = odd;
+        if (ct == 0) e_s[ring] = e_now;
+        mbar_arrive(bar_scale + 8 * ring);
+        fence_proxy_async_smem();
+        mbar_arrive(full_k + 8 * x);
+        load(j + 1, ids, a.k, kr);
+        if (jj > 1) {
+          ok = mbar_wait(empty_v + 8 * x, ph ^ 1u, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+        }
+        if (!ok) break;
+        write(L::kV + x * L::kTileBytes, vr);
+        fence_proxy_async_smem();
+        mbar_arrive(full_v + 8 * x);
+      }
+    }
+    // the last products' arrivals come before the block goes
+    for (uint32_t b = jj > 2 ? jj - 2 : 0; ok && b < jj; ++b)
+      ok = mbar_wait(empty_k + 8 * (b & 1), (b >> 1) & 1, abort_flag) && mbar_wait(empty_v + 8 * (b & 1), (b >> 1) & 1, abort_flag);
+  } else {
+    reg_dealloc<64>();
+    if (warp == 8) {
+    // ================= products: the whole warp, one lane issues =================
+    constexpr uint32_t idesc_qk = idesc_f16_f32(kQrRows, kQrTile, 0), idesc_pv = idesc_f16_f32(kQrRows, D, 1);
+    constexpr uint32_t hi = desc_hi_sw128(1024);
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, abort_flag)); };
+    uint32_t jj = 0, task = 0;
+    bool ok = true;
+    for (bool more = true; more && ok; ++task) {
+      const int n = g.j1 - g.j0;
+      auto scores = [&](uint32_t u) -> bool {             // S = Q K^T of tile u
+        const uint32_t x = u & 1, ph = u >> 1;
+        if (!wait(full_k + 8 * x, ph)) return false;
+        if (u > 1 && !wait(bar_free + 8 * x, ph - 1u)) return false;
+        tc_fence_after();
+        warp_mma_ts_kmajor<L::kHalves>(tmem_base + x * 128, tmem_base + kQ, desc_lo(base + x * L::kTileBytes, 16), hi, idesc_qk);
+        warp_mma_commit(empty_k + 8 * x);
+        warp_mma_commit(bar_s + 8 * x);
+        return true;
+      };
+      ok = wait(bar_q, task);
+      if (ok) ok = scores(jj);
+      for (int j = 0; ok && j < n; ++j, ++jj) {
+        if (j + 1 < n && !(ok = scores(jj + 1))) break;
+        const uint32_t x = jj & 1, ph = jj >> 1;
+        if (!(ok = wait(full_v + 8 * x, ph))) break;
+        if (!(ok = wait(bar_p, jj))) break;
+        tc_fence_after();
+        warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + kP, desc_lo(base + L::kV + x * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
+        warp_mma_commit(empty_v + 8 * x);
+        warp_mma_commit(bar_o);
+      }
+      more = g.next(a, st);
+    }
+    }
+  }
+  // ---- teardown ----
+  tc_fence_before();
+  __syncthreads();
+  if (abort_s) {
+    if (tid == 0) { report(st, RELAXKV_ERR_TIMEOUT, KID_QUANTIZED_ATTN, (int)blockIdx.x, 0); a.chain[blockIdx.x].c0 = -1; }
+    const uint64_t t0 = global_timer_ns();               // products still in flight: let them land
+    while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 8) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
+}
+
+// The parts of tasks that went over several blocks: a row's parts weighed by their log-sum-exps, one warp per row at a time.  The blocks c0 <= b < c1 of a task share its rows.
+constexpr int kQrJoinWarps = 8, kQrJoinBatch = 4;
+template <int D>
+__global__ void __launch_bounds__(kQrJoinWarps * 32)
+quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
+  constexpr int kPer = D / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  griddep_launch();
+  griddep_wait();
+  const Chain ch = a.chain[blockIdx.x];
+  if (ch.c0 < 0 || *reinterpret_cast<volatile int*>(&st->status) == RELAXKV_ERR_TIMEOUT) return;
+  const int parts = ch.c1 - ch.c0 + 1, step = (parts - 1) * kQrJoinWarps;
+  for (int col = ((int)blockIdx.x - ch.c0) * kQrJoinWarps + warp; col < ch.cols; col += step) {
+    float m = kNothing, den = 0.f, acc[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
+    const int r = col / a.G, head = ch.head * a.G + col - r * a.G;
+    const long long row = ch.row + r;
+    bool live = false;
+    for (int p0 = 0; p0 < parts; p0 += kQrJoinBatch) {
+      float l[kQrJoinBatch], v[kQrJoinBatch][kPer];
+#pragma unroll
+      for (int b = 0; b < kQrJoinBatch; ++b) {
+        const int p = p0 + b;
+        if (p >= parts) break;
+        const long long at = ((long long)(p == 0 ? 2 * ch.c0 + 1 : 2 * (ch.c0 + p))) * kQrRows + col;
+        l[b] = a.part_s[at];
+        if constexpr (kPer == 4) *reinterpret_cast<float4*>(v[b]) = *reinterpret_cast<const float4*>(a.part_o + at * D + lane * kPer);
+        else *reinterpret_cast<float2*>(v[b]) = *reinterpret_cast<const float2*>(a.part_o + at * D + lane * kPer);
+      }
+      if (p0 == 0) {                                     // (rows that are left alone have no parts: what was read is not looked at)
+        const int seq = a.row_seq[row];
+        live = seq >= 0 && seq < a.n_seq;
+        if (live) {
+          const SeqRows s = rows_of(a, seq, -1, 0, false, st);
+          live = row >= s.first && row < s.first + s.n && row_tokens(a, seq, s, row, false, st) >= 0;
+        }
+        if (!live) break;
+      }
+#pragma unroll
+      for (int b = 0; b < kQrJoinBatch; ++b) {
+        if (p0 + b >= parts) break;
+        if (l[b] == -INFINITY) continue;
+        const float now = fmaxf(m, l[b]), was = fast_exp2(m - now), w = fast_exp2(l[b] - now);
+        den = den * was + w;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = acc[e] * was + v[b][e] * w;
+        m = now;
+      }
+    }
+    if (!live) continue;
+    const bool none = den == 0.f;
+    const float inv = none ? 0.f : one_over(den);
+    uint32_t packed[kPer / 2];
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) {
+      const __nv_bfloat162 h2 = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+      packed[e / 2] = *reinterpret_cast<const uint32_t*>(&h2);
+    }
+    uint16_t* o = a.out + (row * a.H + head) * D + lane * kPer;
+    if constexpr (kPer == 4) *reinterpret_cast<uint2*>(o) = make_uint2(packed[0], packed[1]);
+    else *reinterpret_cast<uint32_t*>(o) = packed[0];
+    if (lane == 0 && a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = none ? -INFINITY : (m + log2_of(den)) * 0.6931471805599453f;
+  }
+}
+
+template <int D, int TYPE>
+static cudaError_t launch_rows(const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
+  static std::atomic<int> attr_done[kMaxDevices];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+  auto kern = quantized_rows_kernel<D, TYPE>;
+  if (!attr_done[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, QrSmem<D>::kDynamic);
+    if (e != cudaSuccess) return e;
+    attr_done[dev].store(1, std::memory_order_release);
+  }
+  const int blocks = std::min(sms, kQrBlocks);
+  e = launch_chained(kern, dim3((unsigned)blocks), kQrThreads, QrSmem<D>::kDynamic, stream, a, st);
+  if (e != cudaSuccess) return e;
+  auto join = quantized_rows_join_kernel<D>;
+  return launch_chained(join, dim3((unsigned)blocks), kQrJoinWarps * 32, 0, stream, a, st);
+}
+
+cudaError_t launch_quantized_rows(const QuantAttnArgs& a, int head_dim, int type, int sms, DeviceStatus* st, cudaStream_t stream) {
+  if (head_dim == 128) return type == RELAXKV_INT8 ? launch_rows<128, RELAXKV_INT8>(a, sms, st, stream) : launch_rows<128, RELAXKV_E4M3>(a, sms, st, stream);
+  return type == RELAXKV_INT8 ? launch_rows<64, RELAXKV_INT8>(a, sms, st, stream) : launch_rows<64, RELAXKV_E4M3>(a, sms, st, stream);
+}
+
+}  // namespace relaxkv
