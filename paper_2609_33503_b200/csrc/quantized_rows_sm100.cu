@@ -185,8 +185,9 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           }
           return hidden;
         };
+        // (chunk by chunk: unrolled over the tile, the code of a warp that has its scheduler almost for itself came from far, 16 K clk a tile)
         float top = kNothing;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           float y[32];
           scores(c, y);
@@ -205,11 +206,30 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         // rounded first, or the factor would leave the range of fp16
         const bool large = __any_sync(0xffffffffu, fabsf(m_tile) > kQrExact);
         const float q2 = large ? 1.f : qs;
-        uint32_t pk[kQrTile / 2];
-        float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
+        if (jj > 0) {                                    // O of the tile before is complete, its P is not needed any more
+          ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        if (j > g.j0 && __any_sync(0xffffffffu, grows || e_now != e_last)) {
+          const float alpha = fast_exp2(m_old - m + (float)(e_last - e_now));
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c * 32, o);
+            tmem_wait_ld();
 #pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+            tmem_st32(t_o + c * 32, o);
+          }
+        }
+        e_last = e_now;
+        float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           float y[32];
+          uint32_t pk[16];
           const uint32_t hidden = scores(c, y);
           if (large) {
 #pragma unroll
@@ -230,41 +250,20 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
               const __half2 h = __floats2half2_rn(p[e], p[e + 1]);
-              pk[c * 16 + ((i + e) >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
+              pk[(i + e) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
           }
           if (slow) {                                    // what is not seen weighs nothing, whatever its factor
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (hidden >> i & 1) pk[c * 16 + (i >> 1)] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+              if (hidden >> i & 1) pk[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
           }
+          tmem_st16(lane_base + kP + c * 16, pk);
         }
         z += (z0 + z1) + (z2 + z3);
-        tc_fence_before();
-        mbar_arrive(bar_free + 8 * x);                   // S and the factors have been read
-        if (jj > 0) {                                    // O of the tile before is complete, its P is not needed any more
-          ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-        }
-        if (j > g.j0 && __any_sync(0xffffffffu, grows || e_now != e_last)) {
-          const float alpha = fast_exp2(m_old - m + (float)(e_last - e_now));
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(t_o + c * 32, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-            tmem_st32(t_o + c * 32, o);
-          }
-        }
-        e_last = e_now;
-        tmem_st32(lane_base + kP, pk);
-        tmem_st32(lane_base + kP + 32, pk + 32);
         tmem_wait_st();
         tc_fence_before();
+        mbar_arrive(bar_free + 8 * x);                   // S and the factors have been read
         mbar_arrive(bar_p);
       }
       // ---- the results ----
