@@ -42,12 +42,6 @@ __device__ __forceinline__ int swizzled(int t, int c) {
   return D == 128 ? t * 128 + ((c ^ ((t >> 2) & 7)) << 4) : ((t & ~1) | ((t ^ (t >> 4)) & 1)) * 64 + ((c ^ ((t >> 2) & 3)) << 4);
 }
 
-__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {       // bytes 16, or 0: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void load_matrices(uint32_t* r, uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }

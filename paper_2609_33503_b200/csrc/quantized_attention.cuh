@@ -37,6 +37,12 @@ __device__ __forceinline__ float one_over(float x) {
   asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {       // bytes 16, or 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // A maximum of nothing: no score lies below it, and what is taken from it stays a number (scores of -inf weigh nothing beside it, either).
 constexpr float kNothing = -3.4028234663852886e38f;
 

@@ -24,11 +24,14 @@ struct QrSmem {
   static constexpr int kHalves = D / 64, kHalfBytes = kQrTile * 128, kTileBytes = kHalves * kHalfBytes;
   static constexpr int kV = 2 * kTileBytes;              // K[2] | V[2]
   static constexpr int kScale = 4 * kTileBytes;          // of the last four tiles: factors of the keys' scores, of the values' weights
-  static constexpr int kBar = kScale + 4 * 2 * kQrTile * 4;
+  static constexpr int kRaw = kScale + 4 * 2 * kQrTile * 4;      // 8-bit values of two tiles as they come, K and V: every piece is one thread's
+  static constexpr int kRawTile = 2 * kQrTile * D;
+  static constexpr int kBar = kRaw + 2 * kRawTile;
   // full_k[2], full_v[2], empty_k[2], empty_v[2], s[2], free[2], scale[4], p, o, q
   static constexpr int kNumBars = 19;
   static constexpr int kTotal = kBar + 8 * kNumBars;
   static constexpr int kDynamic = kTotal + 1024;
+  static_assert(kDynamic <= 232448 - 1024, "shared memory of a block");
 };
 
 // f16 x f16 -> fp32, A K-major.
@@ -320,71 +323,81 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
     // ================= tiles: 8 bits -> fp16 in shared memory =================
     constexpr int kPieces = D / 16, kAtOnce = 128 / kPieces, kTrips = kQrTile / kAtOnce;      // 16-byte pieces of a token; tokens that four warps bring at once
     const int ct = tid - 128, my_token = ct / kPieces, my_piece = ct % kPieces, cw = ct >> 5;
-    // a piece is two chunks of 16 bytes; the lanes of the upper dims write theirs the other way round, so that eight lanes meet in no bank
-    const int half = my_piece / 4, c0 = (my_piece & 3) * 2;
+    // a piece becomes two chunks of 16 bytes; the lanes of the upper dims write theirs the other way round, so that eight lanes meet in no bank
+    static_assert(kAtOnce % 8 == 0, "rows of the same swizzle");
+    const int half = my_piece / 4, place0 = (((my_piece & 3) * 2 + half) ^ (my_token & 7)) << 4, place1 = place0 ^ 16;
+    const uint32_t raw = base + L::kRaw + ct * 16;        // this thread's pieces: kTrips of K, kTrips of V, 128 x 16 bytes apart
+    const uint8_t* raw_ptr = base_ptr + L::kRaw + ct * 16;
     bool ok = true;
     uint32_t jj = 0;
-    int e_run = 0;
-    uint4 kr[kTrips], vr[kTrips];
     for (bool more = true; more && ok; more = ok && g.next(a, st)) {
       const int* pages = a.table + g.seq * a.table_stride;
-      const long long to_lane = (long long)g.hd * a.head_stride + my_piece * 16;
-      const long long exp_head = (long long)g.hd << a.block_shift;
+      const uint8_t* k_lane = a.k + g.hd * a.head_stride + my_piece * 16;
+      const long long v_off = a.v - a.k;
       auto block_numbers = [&](int j) -> int {           // of 16 tokens of tile j, for lanes 0 to 7; -1: behind the end
         const long long t = (long long)j * kQrTile + lane * 16;
         return lane < 8 && j < g.j1 && t < g.s.len ? pages[t >> a.block_shift] : -1;
       };
-      auto load = [&](int j, int ids, const uint8_t* from, uint4* r) {
-#pragma unroll
+      auto issue = [&](int j, int ids, uint32_t buffer) {
+        const uint32_t dst = raw + buffer * L::kRawTile;
+        const int left = (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile);
+#pragma unroll 1
         for (int i = 0; i < kTrips; ++i) {
           const int token = i * kAtOnce + my_token, id = __shfl_sync(0xffffffffu, ids, token >> 4);
-          const long long t = (long long)j * kQrTile + token;
-          const bool there = t < g.s.len && (unsigned)id < (unsigned)a.n_blocks;
-          r[i] = there ? *reinterpret_cast<const uint4*>(from + to_lane + id * a.block_stride + ((int)t & bs_mask) * a.token_stride) : make_uint4(0u, 0u, 0u, 0u);
+          const bool there = token < left && (unsigned)id < (unsigned)a.n_blocks;
+          const uint8_t* p = there ? k_lane + id * a.block_stride + ((j * kQrTile + token) & bs_mask) * a.token_stride : a.k;
+          copy_16(dst + i * 2048, p, there ? 16 : 0);
+          copy_16(dst + (kTrips + i) * 2048, p + v_off, there ? 16 : 0);
         }
+        copies_commit();
       };
-      auto write = [&](uint32_t at, const uint4* r) {
-#pragma unroll
-        for (int i = 0; i < kTrips; ++i) {
+      auto write = [&](uint32_t at, const uint8_t* from) {
+        uint8_t* to = base_ptr + at + half * L::kHalfBytes + my_token * 128;
+#pragma unroll 2
+        for (int i = 0; i < kTrips; ++i) {               // (kAtOnce tokens on, a row's chunks lie in the same order)
           uint4 h[2];
-          const int token = i * kAtOnce + my_token;
-          if (TYPE == RELAXKV_INT8) to_half_16<RELAXKV_INT8>(r[i], h); else to_half_16<RELAXKV_E4M3>(r[i], h);
-          uint8_t* p = base_ptr + at + half * L::kHalfBytes + token * 128;
-          const int f = half & 1;
-          *reinterpret_cast<uint4*>(p + (((c0 + f) ^ (token & 7)) << 4)) = f ? h[1] : h[0];
-          *reinterpret_cast<uint4*>(p + (((c0 + 1 - f) ^ (token & 7)) << 4)) = f ? h[0] : h[1];
+          to_half_16<TYPE>(*reinterpret_cast<const uint4*>(from + i * 2048), h);
+          *reinterpret_cast<uint4*>(to + place0) = half ? h[1] : h[0];
+          *reinterpret_cast<uint4*>(to + place1) = half ? h[0] : h[1];
+          to += kAtOnce * 128;
         }
       };
-      int ids = block_numbers(g.j0);
-      load(g.j0, ids, a.k, kr);
-      e_run = -200;
+      auto exponents = [&](int j, int ids, int* ek, int* ev) -> bool {       // of token ct; false: none
+        const int id = __shfl_sync(0xffffffffu, ids, ct >> 4);
+        const long long t = (long long)j * kQrTile + ct;
+        const bool inside = j < g.j1 && t < g.s.len, there = inside && (unsigned)id < (unsigned)a.n_blocks;
+        if (inside && !there && (ct & 15) == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
+        *ek = 0; *ev = -200;
+        if (there) {
+          const long long at = (((long long)id * a.Hkv + g.hd) << a.block_shift) + ((int)t & bs_mask);
+          *ek = a.k_exp[at];
+          *ev = a.v_exp[at];
+        }
+        return there;
+      };
+      int ids0 = block_numbers(g.j0), ids1 = block_numbers(g.j0 + 1), ids2;
+      issue(g.j0, ids0, jj & 1);
+      int ek, ev, ek_next, ev_next;
+      bool there = exponents(g.j0, ids0, &ek, &ev), there_next;
+      issue(g.j0 + 1, ids1, (jj + 1) & 1);
+      int e_run = -200;
       for (int j = g.j0; j < g.j1; ++j, ++jj) {
         const uint32_t x = jj & 1, ph = (jj >> 1) & 1;
         const int ring = jj & 3;
-        load(j, ids, a.v, vr);
-        // ---- exponents: token ct ----
-        const int id = __shfl_sync(0xffffffffu, ids, ct >> 4);
-        const long long t = (long long)j * kQrTile + ct;
-        const bool inside = t < g.s.len, there = inside && (unsigned)id < (unsigned)a.n_blocks;
-        if (inside && !there && (ct & 15) == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, id, a.n_blocks);
-        int ek = 0, ev = -200;
-        if (there) {
-          const long long at = (((long long)id * a.Hkv) << a.block_shift) + exp_head + ((int)t & bs_mask);
-          ek = a.k_exp[at];
-          ev = a.v_exp[at];
-        }
-        ids = block_numbers(j + 1);
+        ids2 = block_numbers(j + 2);
+        there_next = exponents(j + 1, ids1, &ek_next, &ev_next);
         const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
         if (lane == 0) largest_s[x][cw] = ev_max;        // (two: a warp may be a tile ahead)
         asm volatile("bar.sync 1, 128;" ::: "memory");
         e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
         const int e_now = max(e_run, kExpLeast);         // (no token yet: anything)
+        copies_wait<1>();                                // (of this thread's own pieces)
         if (jj > 1) {
           ok = mbar_wait(empty_k + 8 * x, ph ^ 1u, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok) break;
-        write(x * L::kTileBytes, kr);
+        write(x * L::kTileBytes, raw_ptr + x * L::kRawTile);
         float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
         const float nan = __uint_as_float(0x7fc00000u);
         const int down = ev - e_now + (int)kQrShift;     // (far below: nothing)
@@ -396,16 +409,19 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         mbar_arrive(bar_scale + 8 * ring);
         fence_proxy_async_smem();
         mbar_arrive(full_k + 8 * x);
-        load(j + 1, ids, a.k, kr);
         if (jj > 1) {
           ok = mbar_wait(empty_v + 8 * x, ph ^ 1u, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok) break;
-        write(L::kV + x * L::kTileBytes, vr);
+        write(L::kV + x * L::kTileBytes, raw_ptr + x * L::kRawTile + kTrips * 2048);
         fence_proxy_async_smem();
         mbar_arrive(full_v + 8 * x);
+        issue(j + 2, ids2, x);                           // (behind the end: zeros)
+        ids1 = ids2;
+        ek = ek_next; ev = ev_next; there = there_next;
       }
+      copies_wait<0>();
     }
     // the last products' arrivals come before the block goes
     for (uint32_t b = jj > 2 ? jj - 2 : 0; ok && b < jj; ++b)
