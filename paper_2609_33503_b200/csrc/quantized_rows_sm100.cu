@@ -1,12 +1,14 @@
 // Attention of many rows of a sequence over its tokens in the 8-bit store: a question, a long draft (relaxkv_quantized_attention).
 //
 // Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of one sequence), one KV head and a run of
-// 128-token tiles.  Four warps bring a tile: 8-bit values out of the pages in 16-byte pieces, made fp16 in registers, exactly, and written where the tensor cores read them
-// (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); one thread per row makes
-// weights of it, which go back to tensor memory as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest
-// of the sequence so far: p = 2^(s - m + 11 + e_t - E).  S is double-buffered, and so are the tiles; P and O are single.
-// Bound by the exponentials (16 K of a tile at 16 per clk, 1024 clk) and what stands around them; a tile's products take 512 clk, its conversion about as much on the same
-// schedulers.  Every wait is bounded.
+// 128-token tiles.  Four warps bring a tile: 8-bit values out of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the tensor cores read them
+// (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); a thread makes weights
+// of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest of the
+// sequence so far: p = 2^(s - m + 11 + e_t - E).
+// Two groups of four warps take the even and the odd tiles: the weights of one tile are made while the products of the other run.  S of tile j + 2 is made when P of tile j has
+// been used; a group hands its P over when O of the tile before is complete, which is also when O may be rescaled; a row's running maximum goes from group to group through
+// shared memory, sums stay with the groups.  K is written a tile ahead of V, or the weights of a tile wait for a value tile that waits for them.
+// Every wait is bounded.
 #include "quantized_attention.cuh"
 #include <atomic>
 
@@ -14,7 +16,7 @@ namespace relaxkv {
 
 using namespace ptx;
 
-constexpr int kQrTile = 128, kQrThreads = 384;           // tokens of a tile; warps 0-3: a row per thread, 4-7: tiles, 8: products, three idle
+constexpr int kQrTile = 128, kQrThreads = 512;           // tokens of a tile; warps 0-3 and 4-7: a row per thread, 8-11: tiles, 12: products, three idle
 constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
 constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
 using QrWalk = Walk<kQrTile, 2, 2, 128>;
@@ -27,9 +29,11 @@ struct QrSmem {
   static constexpr int kRaw = kScale + 4 * 2 * kQrTile * 4;      // 8-bit values of two tiles as they come, K and V: every piece is one thread's
   static constexpr int kRawTile = 2 * kQrTile * D;
   static constexpr int kBar = kRaw + 2 * kRawTile;
-  // full_k[2], full_v[2], empty_k[2], empty_v[2], s[2], free[2], scale[4], p, o, q
-  static constexpr int kNumBars = 19;
-  static constexpr int kTotal = kBar + 8 * kNumBars;
+  // full_k[2], full_v[2], empty_k[2], empty_v[2], s[2], m[2], o[2], scale[4], p, q: those of two or four belong to every second or fourth tile, so that nobody who
+  // waits for one phase can be two behind
+  static constexpr int kNumBars = 20;
+  static constexpr int kMax = kBar + 8 * kNumBars + 8;   // running maximum of every row; its sums, by group
+  static constexpr int kTotal = kMax + 3 * 4 * kQrRows;
   static constexpr int kDynamic = kTotal + 1024;
   static_assert(kDynamic <= 232448 - 1024, "shared memory of a block");
 };
@@ -59,31 +63,31 @@ template <int D, int TYPE>
 __global__ void __launch_bounds__(kQrThreads, 1)
 quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
   using L = QrSmem<D>;
-  constexpr uint32_t kTmemCols = 512, kO = 256, kP = 384, kQ = 448;      // tensor memory: S of even tiles | of odd tiles | O | P | Q
+  constexpr uint32_t kTmemCols = 512, kO = 256, kQ = 384;      // tensor memory: S, then P, of even tiles | of odd tiles | O | Q
   extern __shared__ uint8_t smem_raw[];
   __shared__ QrWalk::Shared walk_s;
   __shared__ volatile uint32_t tmem_slot;
   __shared__ volatile int abort_s;
-  __shared__ int largest_s[2][4], e_s[4];                  // largest exponents: of each of the four warps' tokens; of the values up to the last four tiles
+  __shared__ int largest_s[2][4], e_s[8];                 // largest exponents: of each of the four warps' tokens; of the values up to the last eight tiles
   __shared__ uint32_t gone_s[4][4];                      // tokens of the last four tiles whose blocks do not exist, or that are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t full_k = base + L::kBar, full_v = full_k + 16, empty_k = full_v + 16, empty_v = empty_k + 16, bar_s = empty_v + 16, bar_free = bar_s + 16,
-                 bar_scale = bar_free + 16, bar_p = bar_scale + 32, bar_o = bar_p + 8, bar_q = bar_o + 8;
+  const uint32_t full_k = base + L::kBar, full_v = full_k + 16, empty_k = full_v + 16, empty_v = empty_k + 16, bar_s = empty_v + 16, bar_m = bar_s + 16,
+                 bar_o = bar_m + 16, bar_scale = bar_o + 16, bar_p = bar_scale + 32, bar_q = bar_p + 8;
   volatile int* abort_flag = &abort_s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(full_k + 8 * i, 128); mbar_init(full_v + 8 * i, 128); mbar_init(empty_k + 8 * i, 1); mbar_init(empty_v + 8 * i, 1);
-      mbar_init(bar_s + 8 * i, 1); mbar_init(bar_free + 8 * i, 128);
+      mbar_init(bar_s + 8 * i, 1); mbar_init(bar_m + 8 * i, 128); mbar_init(bar_o + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(bar_scale + 8 * i, 128);
-    mbar_init(bar_p, 128); mbar_init(bar_o, 1); mbar_init(bar_q, 128);
+    mbar_init(bar_p, 128); mbar_init(bar_q, 256);
     abort_s = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
   }
-  if (warp == 8) { tmem_alloc(smem_u32(const_cast<uint32_t*>(&tmem_slot)), kTmemCols); tmem_relinquish(); }
+  if (warp == 12) { tmem_alloc(smem_u32(const_cast<uint32_t*>(&tmem_slot)), kTmemCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -96,70 +100,72 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   if (!any || status == RELAXKV_ERR_TIMEOUT) {
     if (tid == 0) a.chain[blockIdx.x].c0 = -1;
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tmem_base, kTmemCols);
+    if (warp == 12) tmem_dealloc(tmem_base, kTmemCols);
     return;
   }
   const int G = a.G, rpt = a.rows_per_tile, bs_mask = (1 << a.block_shift) - 1;
 
-  // Registers: 12 warps x 168 at launch = 4 x 240 + 4 x 200 + 4 x 64.
-  if (warp < 4) {
-    reg_alloc<240>();
-    // ================= weights: thread = (row of the sequence, head) = lane of tensor memory =================
-    const int t_local = tid / G, in_group = tid - t_local * G;
-    const uint32_t lane_base = tmem_base + ((uint32_t)(warp * 32) << 16), t_o = lane_base + kO;
+  // Registers: 16 warps x 128 at launch = 8 x 176 + 4 x 104 + 4 x 56.
+  if (warp < 8) {
+    reg_alloc<176>();
+    // ================= weights: thread = (row of the sequence, head) = lane of tensor memory; x: even or odd tiles =================
+    const int x = warp >> 2, t = tid & 127, t_local = t / G, in_group = t - t_local * G;
+    const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16), t_s = lane_base + x * 128, t_o = lane_base + kO;
+    volatile float* max_s = reinterpret_cast<volatile float*>(base_ptr + L::kMax);
+    volatile float* sum_s = max_s + kQrRows;
     bool ok = true;
     uint32_t jj = 0;                                     // tiles so far, over all tasks
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, abort_flag)); };
     for (bool more = true; more && ok;) {
       const long long row = (long long)g.s.first + (long long)g.tile * rpt + t_local;
       const int head = g.hd * G + in_group;
       const bool exists = t_local < min(rpt, g.s.n - g.tile * rpt);
-      const int seen = exists ? row_tokens(a, g.seq, g.s, row, in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
-      // ---- Q: as fp16 times 2^-exponent, two dims to a word ----
+      const int seen = exists ? row_tokens(a, g.seq, g.s, row, x == 0 && in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
+      // ---- Q: as fp16 times 2^-exponent, two dims to a word; each group brings half of them ----
       float qs;
       {
-        uint32_t w[D / 2], top = 0;
+        uint32_t w[D / 4], top = 0;
         const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D);
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 v = exists ? q[c] : make_uint4(0, 0, 0, 0);
-          w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
-        }
+        for (int h = 0; h < 2; ++h) {                    // (its own half last)
+          const int from = (h ^ x ^ 1) * (D / 16);
 #pragma unroll
-        for (int c = 0; c < D / 2; ++c) top = __vmaxu2(top, w[c] & 0x7fff7fffu);
+          for (int c = 0; c < D / 16; ++c) {
+            const uint4 v = exists ? q[from + c] : make_uint4(0, 0, 0, 0);
+            w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
+          }
+#pragma unroll
+          for (int c = 0; c < D / 4; ++c) top = __vmaxu2(top, w[c] & 0x7fff7fffu);
+        }
         top = max(top & 0xffffu, top >> 16);
         const bool finite = top < 0x7f80u;
         const int e = max((int)(top >> 7) - 127 - 14, -120);
         const float inv = __uint_as_float((uint32_t)(127 - (finite ? e : 0)) << 23);
 #pragma unroll
-        for (int c = 0; c < D / 2; ++c) {
-          const __half2 x = __floats2half2_rn(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xffff0000u) * inv);
-          w[c] = finite ? *reinterpret_cast<const uint32_t*>(&x) : 0u;
+        for (int c = 0; c < D / 4; ++c) {
+          const __half2 y = __floats2half2_rn(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xffff0000u) * inv);
+          w[c] = finite ? *reinterpret_cast<const uint32_t*>(&y) : 0u;
         }
         qs = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) tmem_st32(lane_base + kQ + 32 * c, w + 32 * c);
+        if constexpr (D == 128) tmem_st32(lane_base + kQ + 32 * x, w); else tmem_st16(lane_base + kQ + 16 * x, w);
         tmem_wait_st();
         tc_fence_before();
       }
       mbar_arrive(bar_q);
       const bool busy = __any_sync(0xffffffffu, seen >= 0);          // a warp without rows only keeps step
-      float m = kNothing, z = 0.f;
-      int e_last = 0;
-      for (int j = g.j0; j < g.j1; ++j, ++jj) {
-        const uint32_t x = jj & 1, ph = (jj >> 1) & 1;
-        const int ring = jj & 3;
-        ok = mbar_wait(bar_scale + 8 * ring, (jj >> 2) & 1, abort_flag) && mbar_wait(bar_s + 8 * x, ph, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
+      const int n = g.j1 - g.j0;
+      const uint32_t jj0 = jj;
+      float m = kNothing, z = 0.f;                       // the row's maximum when this group last saw it, the group's sum relative to that
+      for (int i = (int)((jj0 ^ x) & 1); i < n; i += 2) {
+        jj = jj0 + i;
+        const int j = g.j0 + i, ring = jj & 3;
+        if (!(ok = wait(bar_scale + 8 * ring, jj >> 2)) || !(ok = wait(bar_s + 8 * x, jj >> 1))) break;
         tc_fence_after();
-        const int e_now = e_s[ring];
         if (!busy) {
-          mbar_arrive(bar_free + 8 * x);
-          if (jj > 0) ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
-          if (ok) mbar_arrive(bar_p);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          e_last = e_now;
+          if (jj > 0 && !(ok = wait(bar_m + 8 * (x ^ 1), (jj - 1) >> 1))) break;
+          mbar_arrive(bar_m + 8 * x);
+          if (jj > 0 && !(ok = wait(bar_o + 8 * (x ^ 1), (jj - 1) >> 1))) break;
+          mbar_arrive(bar_p);
           continue;
         }
         const float* ks = reinterpret_cast<const float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
@@ -169,21 +175,21 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         // 32 scores times their keys' scales; what the row does not see (its tokens from `limit` on, tokens without a block) becomes -inf
         auto scores = [&](int c, float* y) -> uint32_t {
           uint32_t w[32];
-          tmem_ld32(lane_base + x * 128 + c * 32, w);
+          tmem_ld32(t_s + c * 32, w);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 k4 = *reinterpret_cast<const float4*>(ks + c * 32 + i);
-            mul2(y[i], y[i + 1], __uint_as_float(w[i]), __uint_as_float(w[i + 1]), k4.x, k4.y);
-            mul2(y[i + 2], y[i + 3], __uint_as_float(w[i + 2]), __uint_as_float(w[i + 3]), k4.z, k4.w);
+          for (int e = 0; e < 32; e += 4) {
+            const float4 k4 = *reinterpret_cast<const float4*>(ks + c * 32 + e);
+            mul2(y[e], y[e + 1], __uint_as_float(w[e]), __uint_as_float(w[e + 1]), k4.x, k4.y);
+            mul2(y[e + 2], y[e + 3], __uint_as_float(w[e + 2]), __uint_as_float(w[e + 3]), k4.z, k4.w);
           }
           uint32_t hidden = 0;
           if (slow) {
             hidden = limit >= 32 * (c + 1) ? 0u : limit <= 32 * c ? 0xffffffffu : 0xffffffffu << (limit - 32 * c);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              if (ks[c * 32 + i] == -INFINITY) hidden |= 1u << i;
-              if (hidden >> i & 1) y[i] = -INFINITY;
+            for (int e = 0; e < 32; ++e) {
+              if (ks[c * 32 + e] == -INFINITY) hidden |= 1u << e;
+              if (hidden >> e & 1) y[e] = -INFINITY;
             }
           }
           return hidden;
@@ -198,36 +204,23 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx[e] = fmaxf(y[2 * e], y[2 * e + 1]);
 #pragma unroll
-          for (int i = 8; i < 32; i += 2) mx[(i >> 1) & 3] = fmax3(mx[(i >> 1) & 3], y[i], y[i + 1]);
+          for (int e = 8; e < 32; e += 2) mx[(e >> 1) & 3] = fmax3(mx[(e >> 1) & 3], y[e], y[e + 1]);
           top = fmax3(top, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         }
-        const float m_tile = top * qs, m_old = m;        // (qs > 0)
-        const bool grows = m_tile > m + kQrGrow;
-        if (grows) m = m_tile;
-        z *= fast_exp2(m_old - m);
+        if (jj > 0 && !(ok = wait(bar_m + 8 * (x ^ 1), (jj - 1) >> 1))) break;      // the other group's maximum of the tile before
+        const float m_tile = top * qs;                   // (qs > 0)
+        float m_old = kNothing;
+        if (i > 0) m_old = max_s[t];
+        const bool grows = m_tile > m_old + kQrGrow;
+        const float m_new = grows ? m_tile : m_old;
+        max_s[t] = m_new;
+        mbar_arrive(bar_m + 8 * x);
+        z *= fast_exp2(m - m_new);
+        m = m_new;
         // s * qs - m in one rounding keeps what the rounding of m has cut off: the same factor on all weights of the row, which their sum takes out again; very large logits are
         // rounded first, or the factor would leave the range of fp16
         const bool large = __any_sync(0xffffffffu, fabsf(m_tile) > kQrExact);
         const float q2 = large ? 1.f : qs;
-        if (jj > 0) {                                    // O of the tile before is complete, its P is not needed any more
-          ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-        }
-        if (j > g.j0 && __any_sync(0xffffffffu, grows || e_now != e_last)) {
-          const float alpha = fast_exp2(m_old - m + (float)(e_last - e_now));
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(t_o + c * 32, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-            tmem_st32(t_o + c * 32, o);
-          }
-        }
-        e_last = e_now;
         float z0 = 0.f, z1 = 0.f, z2 = 0.f, z3 = 0.f;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
@@ -236,42 +229,64 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           const uint32_t hidden = scores(c, y);
           if (large) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] *= qs;
+            for (int e = 0; e < 32; ++e) y[e] *= qs;
           }
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
+          for (int e = 0; e < 32; e += 4) {
             float p[4];
-            const float4 v4 = *reinterpret_cast<const float4*>(vs + c * 32 + i);
-            fma2(p[0], p[1], y[i], y[i + 1], q2, q2, -m, -m);
-            fma2(p[2], p[3], y[i + 2], y[i + 3], q2, q2, -m, -m);
+            const float4 v4 = *reinterpret_cast<const float4*>(vs + c * 32 + e);
+            fma2(p[0], p[1], y[e], y[e + 1], q2, q2, -m, -m);
+            fma2(p[2], p[3], y[e + 2], y[e + 3], q2, q2, -m, -m);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = fast_exp2(p[e]);
+            for (int u = 0; u < 4; ++u) p[u] = fast_exp2(p[u]);
             add2(z0, z1, p[0], p[1]);
             add2(z2, z3, p[2], p[3]);
             mul2(p[0], p[1], p[0], p[1], v4.x, v4.y);
             mul2(p[2], p[3], p[2], p[3], v4.z, v4.w);
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              const __half2 h = __floats2half2_rn(p[e], p[e + 1]);
-              pk[(i + e) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int u = 0; u < 4; u += 2) {
+              const __half2 h = __floats2half2_rn(p[u], p[u + 1]);
+              pk[(e + u) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
           }
           if (slow) {                                    // what is not seen weighs nothing, whatever its factor
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (hidden >> i & 1) pk[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+            for (int e = 0; e < 32; ++e)
+              if (hidden >> e & 1) pk[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
           }
-          tmem_st16(lane_base + kP + c * 16, pk);
+          tmem_st16(t_s + c * 16, pk);                   // (where scores were that have been read)
         }
         z += (z0 + z1) + (z2 + z3);
+        if (jj > 0) {                                    // O of the tile before is complete
+          if (!(ok = wait(bar_o + 8 * (x ^ 1), (jj - 1) >> 1))) break;
+          tc_fence_after();
+        }
+        const int e_now = e_s[jj & 7], e_was = i > 0 ? e_s[(jj - 1) & 7] : e_now;
+        if (i > 0 && __any_sync(0xffffffffu, grows || e_now != e_was)) {
+          const float alpha = fast_exp2(m_old - m_new + (float)(e_was - e_now));
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(t_o + c * 32, o);
+          }
+        }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(bar_free + 8 * x);                   // S and the factors have been read
         mbar_arrive(bar_p);
       }
-      // ---- the results ----
-      if (ok) ok = mbar_wait(bar_o, (jj - 1) & 1, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
+      // ---- the results, each group half the dims ----
+      jj = jj0 + n;
+      if (ok && jj > 1) ok = wait(bar_o + 8 * (jj & 1), (jj - 2) >> 1);
+      if (ok) ok = wait(bar_o + 8 * (~jj & 1), (jj - 1) >> 1);
+      const int e_last = e_s[(jj - 1) & 7];
+      const float m_end = max_s[t];                      // (of a warp without rows: anything)
+      sum_s[x * kQrRows + t] = z * fast_exp2(m - m_end);
+      asm volatile("bar.sync 2, 256;" ::: "memory");
+      ok = __all_sync(0xffffffffu, ok && !*abort_flag);
       const bool whole = g.whole();
       const int slot = g.slot();
       if (tid == 0) {
@@ -281,79 +296,82 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       }
       if (ok && busy) {
         tc_fence_after();
-        const bool none = z == 0.f;                      // no token, or none of a logit above -inf (NaN stays NaN)
-        const float inv = none ? 0.f : __uint_as_float((uint32_t)(127 - (int)kQrShift) << 23) / z, grow = __uint_as_float((uint32_t)(e_last + 127) << 23);
-        const float lse2 = none ? -INFINITY : m + log2_of(z);
-        const int col = tid;
+        const float zz = sum_s[t] + sum_s[kQrRows + t];
+        const bool none = zz == 0.f;                     // no token, or none of a logit above -inf (NaN stays NaN)
+        const float inv = none ? 0.f : one_over(zz * 2048.f), grow = __uint_as_float((uint32_t)(e_last + 127) << 23);
+        static_assert(kQrShift == 11.f, "2^11");
+        const float lse2 = none ? -INFINITY : m_end + log2_of(zz);
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = x * (D / 64); c < (x + 1) * (D / 64); ++c) {
           uint32_t o[32];
           tmem_ld32(t_o + c * 32, o);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = none ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv * grow);
+          for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv * grow);
           if (seen >= 0 && !whole) {
-            float* p = a.part_o + ((long long)slot * kQrRows + col) * D + c * 32;
+            float* p = a.part_o + ((long long)slot * kQrRows + t) * D + c * 32;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(p + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(p + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           } else if (seen >= 0) {
             uint16_t* p = a.out + (row * a.H + head) * D + c * 32;
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
+            for (int e = 0; e < 32; e += 8) {
               uint32_t w[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
-                w[e] = *reinterpret_cast<const uint32_t*>(&h2);
+              for (int u = 0; u < 4; ++u) {
+                const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(o[e + 2 * u]), __uint_as_float(o[e + 2 * u + 1]));
+                w[u] = *reinterpret_cast<const uint32_t*>(&h2);
               }
-              *reinterpret_cast<uint4*>(p + i) = make_uint4(w[0], w[1], w[2], w[3]);
+              *reinterpret_cast<uint4*>(p + e) = make_uint4(w[0], w[1], w[2], w[3]);
             }
           }
         }
-        if (seen >= 0) {
-          if (!whole) a.part_s[(long long)slot * kQrRows + col] = lse2;
+        if (seen >= 0 && x == 0) {
+          if (!whole) a.part_s[(long long)slot * kQrRows + t] = lse2;
           else if (a.lse_out) a.lse_out[(long long)head * a.n_rows + row] = lse2 * 0.6931471805599453f;
         }
         tc_fence_before();
       }
+      asm volatile("bar.sync 2, 256;" ::: "memory");       // O and the sums have been read by both groups
       more = g.next(a, st);
     }
-  } else if (warp < 8) {
-    reg_alloc<200>();
+  } else if (warp < 12) {
+    reg_dealloc<104>();
     // ================= tiles: 8 bits -> fp16 in shared memory =================
     constexpr int kPieces = D / 16, kAtOnce = 128 / kPieces, kTrips = kQrTile / kAtOnce;      // 16-byte pieces of a token; tokens that four warps bring at once
-    const int ct = tid - 128, my_token = ct / kPieces, my_piece = ct % kPieces, cw = ct >> 5;
+    const int ct = tid - 256, my_token = ct / kPieces, my_piece = ct % kPieces, cw = ct >> 5;
     // a piece becomes two chunks of 16 bytes; the lanes of the upper dims write theirs the other way round, so that eight lanes meet in no bank
     static_assert(kAtOnce % 8 == 0, "rows of the same swizzle");
     const int half = my_piece / 4, place0 = (((my_piece & 3) * 2 + half) ^ (my_token & 7)) << 4, place1 = place0 ^ 16;
-    const uint32_t raw = base + L::kRaw + ct * 16;        // this thread's pieces: kTrips of K, kTrips of V, 128 x 16 bytes apart
+    // this thread's pieces, kTrips of a tile, 128 x 16 bytes apart: K of even and odd tiles, V of those
+    constexpr int kRawHalf = L::kRawTile / 2;
+    const uint32_t raw = base + L::kRaw + ct * 16;
     const uint8_t* raw_ptr = base_ptr + L::kRaw + ct * 16;
     bool ok = true;
     uint32_t jj = 0;
     for (bool more = true; more && ok; more = ok && g.next(a, st)) {
       const int* pages = a.table + g.seq * a.table_stride;
-      const uint8_t* k_lane = a.k + g.hd * a.head_stride + my_piece * 16;
-      const long long v_off = a.v - a.k;
+      const long long to_lane = g.hd * (long long)a.head_stride + my_piece * 16;
+      const uint8_t *k_lane = a.k + to_lane, *v_lane = a.v + to_lane;
       auto block_numbers = [&](int j) -> int {           // of 16 tokens of tile j, for lanes 0 to 7; -1: behind the end
         const long long t = (long long)j * kQrTile + lane * 16;
         return lane < 8 && j < g.j1 && t < g.s.len ? pages[t >> a.block_shift] : -1;
       };
-      auto issue = [&](int j, int ids, uint32_t buffer) {
-        const uint32_t dst = raw + buffer * L::kRawTile;
-        const int left = (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile);
-#pragma unroll 1
+      auto issue = [&](int j, int ids, const uint8_t* from, uint32_t dst) {       // K or V of tile j
+        const int left = j < g.j1 ? (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile) : 0;
+        if (j < g.j1)
+#pragma unroll 4
         for (int i = 0; i < kTrips; ++i) {
           const int token = i * kAtOnce + my_token, id = __shfl_sync(0xffffffffu, ids, token >> 4);
           const bool there = token < left && (unsigned)id < (unsigned)a.n_blocks;
-          const uint8_t* p = there ? k_lane + id * a.block_stride + ((j * kQrTile + token) & bs_mask) * a.token_stride : a.k;
+          const uint8_t* p = there ? from + id * a.block_stride + ((j * kQrTile + token) & bs_mask) * a.token_stride : a.k;
           copy_16(dst + i * 2048, p, there ? 16 : 0);
-          copy_16(dst + (kTrips + i) * 2048, p + v_off, there ? 16 : 0);
         }
         copies_commit();
       };
       auto write = [&](uint32_t at, const uint8_t* from) {
         uint8_t* to = base_ptr + at + half * L::kHalfBytes + my_token * 128;
-#pragma unroll 2
+#pragma unroll 4
         for (int i = 0; i < kTrips; ++i) {               // (kAtOnce tokens on, a row's chunks lie in the same order)
           uint4 h[2];
           to_half_16<TYPE>(*reinterpret_cast<const uint4*>(from + i * 2048), h);
@@ -375,60 +393,71 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         }
         return there;
       };
-      int ids0 = block_numbers(g.j0), ids1 = block_numbers(g.j0 + 1), ids2;
-      issue(g.j0, ids0, jj & 1);
-      int ek, ev, ek_next, ev_next;
-      bool there = exponents(g.j0, ids0, &ek, &ev), there_next;
-      issue(g.j0 + 1, ids1, (jj + 1) & 1);
-      int e_run = -200;
-      for (int j = g.j0; j < g.j1; ++j, ++jj) {
-        const uint32_t x = jj & 1, ph = (jj >> 1) & 1;
-        const int ring = jj & 3;
-        ids2 = block_numbers(j + 2);
-        there_next = exponents(j + 1, ids1, &ek_next, &ev_next);
-        const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
-        if (lane == 0) largest_s[x][cw] = ev_max;        // (two: a warp may be a tile ahead)
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
-        const int e_now = max(e_run, kExpLeast);         // (no token yet: anything)
-        copies_wait<1>();                                // (of this thread's own pieces)
-        if (jj > 1) {
-          ok = mbar_wait(empty_k + 8 * x, ph ^ 1u, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
+      // K of tile i and V of the tile before, for i = 0 .. n; the copies of either are asked for two trips ahead (K0 K1 V0 | K2 V1 | K3 V2 | ..)
+      const int n = g.j1 - g.j0;
+      int e_run = -200, ek, ev, ids1 = block_numbers(g.j0), ids2 = block_numbers(g.j0 + 1);
+      issue(g.j0, ids1, k_lane, raw + (jj & 1) * kRawHalf);
+      issue(g.j0 + 1, ids2, k_lane, raw + (~jj & 1) * kRawHalf);
+      issue(g.j0, ids1, v_lane, raw + (2 + (jj & 1)) * kRawHalf);
+      bool there = exponents(g.j0, ids1, &ek, &ev);
+      ids1 = ids2;                                       // of tile i + 1
+      ids2 = block_numbers(g.j0 + 2);                    // of tile i + 2
+      for (int i = 0; i <= n; ++i) {
+        const uint32_t u = jj + i, x = u & 1;
+        const int ids3 = block_numbers(g.j0 + i + 3);
+        if (i < n) {
+          const int ring = u & 3;
+          const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
+          if (lane == 0) largest_s[x][cw] = ev_max;      // (two: a warp may be a tile ahead)
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+          e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
+          const int e_now = max(e_run, kExpLeast);       // (no token yet: anything)
+          if (i == 0) copies_wait<2>(); else copies_wait<3>();        // K of this tile (this thread's own pieces)
+          if (u > 1) {
+            ok = mbar_wait(empty_k + 8 * x, ((u >> 1) & 1) ^ 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+          }
+          write(x * L::kTileBytes, raw_ptr + x * kRawHalf);
+          float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
+          const float nan = __uint_as_float(0x7fc00000u);
+          const int down = ev - e_now + (int)kQrShift;   // (far below: nothing)
+          ks[ct] = there ? exp_scale(ek) : -INFINITY;
+          ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
+          const uint32_t odd = __ballot_sync(0xffffffffu, !there || ek == kExpNone || ev == kExpNone);
+          if (lane == 0) gone_s[ring][cw] = odd;
+          if (ct == 0) e_s[u & 7] = e_now;
+          mbar_arrive(bar_scale + 8 * ring);
+          fence_proxy_async_smem();
+          mbar_arrive(full_k + 8 * x);
+          there = exponents(g.j0 + i + 1, ids1, &ek, &ev);
         }
-        if (!ok) break;
-        write(x * L::kTileBytes, raw_ptr + x * L::kRawTile);
-        float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
-        const float nan = __uint_as_float(0x7fc00000u);
-        const int down = ev - e_now + (int)kQrShift;     // (far below: nothing)
-        ks[ct] = there ? exp_scale(ek) : -INFINITY;
-        ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
-        const uint32_t odd = __ballot_sync(0xffffffffu, !there || ek == kExpNone || ev == kExpNone);
-        if (lane == 0) gone_s[ring][cw] = odd;
-        if (ct == 0) e_s[ring] = e_now;
-        mbar_arrive(bar_scale + 8 * ring);
-        fence_proxy_async_smem();
-        mbar_arrive(full_k + 8 * x);
-        if (jj > 1) {
-          ok = mbar_wait(empty_v + 8 * x, ph ^ 1u, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
+        issue(g.j0 + i + 2, ids2, k_lane, raw + x * kRawHalf);
+        if (i > 0) {
+          const uint32_t v = u - 1, y = v & 1;
+          copies_wait<3>();                              // V of the tile before
+          if (v > 1) {
+            ok = mbar_wait(empty_v + 8 * y, ((v >> 1) & 1) ^ 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+          }
+          write(L::kV + y * L::kTileBytes, raw_ptr + (2 + y) * kRawHalf);
+          fence_proxy_async_smem();
+          mbar_arrive(full_v + 8 * y);
         }
-        if (!ok) break;
-        write(L::kV + x * L::kTileBytes, raw_ptr + x * L::kRawTile + kTrips * 2048);
-        fence_proxy_async_smem();
-        mbar_arrive(full_v + 8 * x);
-        issue(j + 2, ids2, x);                           // (behind the end: zeros)
+        issue(g.j0 + i + 1, ids1, v_lane, raw + (2 + (~x & 1)) * kRawHalf);
         ids1 = ids2;
-        ek = ek_next; ev = ev_next; there = there_next;
+        ids2 = ids3;
       }
+      jj += n;
       copies_wait<0>();
     }
     // the last products' arrivals come before the block goes
     for (uint32_t b = jj > 2 ? jj - 2 : 0; ok && b < jj; ++b)
       ok = mbar_wait(empty_k + 8 * (b & 1), (b >> 1) & 1, abort_flag) && mbar_wait(empty_v + 8 * (b & 1), (b >> 1) & 1, abort_flag);
   } else {
-    reg_dealloc<64>();
-    if (warp == 8) {
+    reg_dealloc<56>();
+    if (warp == 12) {
     // ================= products: the whole warp, one lane issues =================
     constexpr uint32_t idesc_qk = idesc_f16_f32(kQrRows, kQrTile, 0), idesc_pv = idesc_f16_f32(kQrRows, D, 1);
     constexpr uint32_t hi = desc_hi_sw128(1024);
@@ -440,7 +469,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       auto scores = [&](uint32_t u) -> bool {             // S = Q K^T of tile u
         const uint32_t x = u & 1, ph = u >> 1;
         if (!wait(full_k + 8 * x, ph)) return false;
-        if (u > 1 && !wait(bar_free + 8 * x, ph - 1u)) return false;
+        if (u > 1 && !wait(bar_o + 8 * x, ph - 1u)) return false;   // P of the tile that had this place has been used
         tc_fence_after();
         warp_mma_ts_kmajor<L::kHalves>(tmem_base + x * 128, tmem_base + kQ, desc_lo(base + x * L::kTileBytes, 16), hi, idesc_qk);
         warp_mma_commit(empty_k + 8 * x);
@@ -455,9 +484,9 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         if (!(ok = wait(full_v + 8 * x, ph))) break;
         if (!(ok = wait(bar_p, jj))) break;
         tc_fence_after();
-        warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + kP, desc_lo(base + L::kV + x * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
+        warp_mma_ts_mnmajor(tmem_base + kO, tmem_base + x * 128, desc_lo(base + L::kV + x * L::kTileBytes, L::kHalfBytes), hi, idesc_pv, j > 0 ? 1u : 0u);
         warp_mma_commit(empty_v + 8 * x);
-        warp_mma_commit(bar_o);
+        warp_mma_commit(bar_o + 8 * x);
       }
       more = g.next(a, st);
     }
@@ -472,7 +501,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
     while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 8) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
+  if (warp == 12) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
 }
 
 // The parts of tasks that went over several blocks: a row's parts weighed by their log-sum-exps, one warp per row at a time.  The blocks c0 <= b < c1 of a task share its rows.
