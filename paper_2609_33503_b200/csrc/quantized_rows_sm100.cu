@@ -1,7 +1,7 @@
 // Attention of many rows of a sequence over its tokens in the 8-bit store: a question, a long draft (relaxkv_quantized_attention).
 //
 // Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of one sequence), one KV head and a run of
-// 128-token tiles.  Four warps bring a tile: 8-bit values out of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the tensor cores read them
+// 128-token tiles.  Eight warps bring a tile, four its K and four its V: 8-bit values out of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the tensor cores read them
 // (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); a thread makes weights
 // of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest of the
 // sequence so far: p = 2^(s - m + 11 + e_t - E).
@@ -16,7 +16,7 @@ namespace relaxkv {
 
 using namespace ptx;
 
-constexpr int kQrTile = 128, kQrThreads = 512;           // tokens of a tile; warps 0-3 and 4-7: a row per thread, 8-11: tiles, 12: products, three idle
+constexpr int kQrTile = 128, kQrThreads = 640;           // tokens of a tile; warps 0-3 and 4-7: a row per thread, 8-11: K, 12-15: V, 16: products, three idle
 constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
 constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
 using QrWalk = Walk<kQrTile, 2, 2, 128>;
@@ -59,6 +59,15 @@ __device__ __forceinline__ void to_half_16(const uint4& r, uint4* out) {
   out[1] = make_uint4(h[4], h[5], h[6], h[7]);
 }
 
+// A barrier of some of the warps at which they also agree whether to go on: none waits for one that has left after a wait that ran out.
+template <int ID, int THREADS>
+__device__ __forceinline__ bool meet(bool ok) {
+  int all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, %3, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+               : "=r"(all) : "r"((int)ok), "n"(ID), "n"(THREADS) : "memory");
+  return all != 0;
+}
+
 template <int D, int TYPE>
 __global__ void __launch_bounds__(kQrThreads, 1)
 quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
@@ -87,7 +96,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
     fence_barrier_init();
     fence_proxy_async_smem();
   }
-  if (warp == 12) { tmem_alloc(smem_u32(const_cast<uint32_t*>(&tmem_slot)), kTmemCols); tmem_relinquish(); }
+  if (warp == 16) { tmem_alloc(smem_u32(const_cast<uint32_t*>(&tmem_slot)), kTmemCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -100,14 +109,14 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   if (!any || status == RELAXKV_ERR_TIMEOUT) {
     if (tid == 0) a.chain[blockIdx.x].c0 = -1;
     __syncthreads();
-    if (warp == 12) tmem_dealloc(tmem_base, kTmemCols);
+    if (warp == 16) tmem_dealloc(tmem_base, kTmemCols);
     return;
   }
   const int G = a.G, rpt = a.rows_per_tile, bs_mask = (1 << a.block_shift) - 1;
 
-  // Registers: 16 warps x 128 at launch = 8 x 176 + 4 x 104 + 4 x 56.
+  // Registers: 20 warps x 96 at launch = 8 x 136 + 8 x 80 + 4 x 48.
   if (warp < 8) {
-    reg_alloc<176>();
+    reg_alloc<136>();
     // ================= weights: thread = (row of the sequence, head) = lane of tensor memory; x: even or odd tiles =================
     const int x = warp >> 2, t = tid & 127, t_local = t / G, in_group = t - t_local * G;
     const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16), t_s = lane_base + x * 128, t_o = lane_base + kO;
@@ -170,7 +179,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         }
         const float* ks = reinterpret_cast<const float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
         const float* vs = ks + kQrTile;
-        const int limit = seen - j * kQrTile;
+        const int limit = seen < 0 ? kQrTile : seen - j * kQrTile;      // (rows that are not written see all: nothing to hide costs half as much)
         const bool slow = __any_sync(0xffffffffu, limit < kQrTile || (gone_s[ring][0] | gone_s[ring][1] | gone_s[ring][2] | gone_s[ring][3]) != 0);
         // 32 scores times their keys' scales; what the row does not see (its tokens from `limit` on, tokens without a block) becomes -inf
         auto scores = [&](int c, float* y) -> uint32_t {
@@ -198,9 +207,8 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         float top = kNothing;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
-          float y[32];
+          float y[32], mx[4];
           scores(c, y);
-          float mx[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx[e] = fmaxf(y[2 * e], y[2 * e + 1]);
 #pragma unroll
@@ -285,8 +293,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       const int e_last = e_s[(jj - 1) & 7];
       const float m_end = max_s[t];                      // (of a warp without rows: anything)
       sum_s[x * kQrRows + t] = z * fast_exp2(m - m_end);
-      asm volatile("bar.sync 2, 256;" ::: "memory");
-      ok = __all_sync(0xffffffffu, ok && !*abort_flag);
+      ok = meet<2, 256>(ok && !*abort_flag);
       const bool whole = g.whole();
       const int slot = g.slot();
       if (tid == 0) {
@@ -335,50 +342,44 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       asm volatile("bar.sync 2, 256;" ::: "memory");       // O and the sums have been read by both groups
       more = g.next(a, st);
     }
-  } else if (warp < 12) {
-    reg_dealloc<104>();
-    // ================= tiles: 8 bits -> fp16 in shared memory =================
+  } else if (warp < 16) {
+    reg_dealloc<80>();
+    // ================= tiles: 8 bits -> fp16 in shared memory; four warps for K, four for V =================
     constexpr int kPieces = D / 16, kAtOnce = 128 / kPieces, kTrips = kQrTile / kAtOnce;      // 16-byte pieces of a token; tokens that four warps bring at once
-    const int ct = tid - 256, my_token = ct / kPieces, my_piece = ct % kPieces, cw = ct >> 5;
-    // a piece becomes two chunks of 16 bytes; the lanes of the upper dims write theirs the other way round, so that eight lanes meet in no bank
     static_assert(kAtOnce % 8 == 0, "rows of the same swizzle");
-    const int half = my_piece / 4, place0 = (((my_piece & 3) * 2 + half) ^ (my_token & 7)) << 4, place1 = place0 ^ 16;
-    // this thread's pieces, kTrips of a tile, 128 x 16 bytes apart: K of even and odd tiles, V of those
-    constexpr int kRawHalf = L::kRawTile / 2;
-    const uint32_t raw = base + L::kRaw + ct * 16;
-    const uint8_t* raw_ptr = base_ptr + L::kRaw + ct * 16;
+    const bool of_k = warp < 12;
+    const int ct = tid & 127, cw = warp & 3;
+    // A piece becomes two chunks of 16 bytes.  Eight lanes: two tokens of four pieces (64 dims), whose chunks lie in eight different groups of banks.
+    const int my_token = D == 128 ? (ct >> 4) * 2 + ((ct >> 2) & 1) : ct >> 2, half = D == 128 ? (ct >> 3) & 1 : 0, my_piece = (ct & 3) + 4 * half;
+    const uint32_t place0 = (uint32_t)(((ct & 3) * 2) ^ (my_token & 7)) << 4;
+    const uint32_t full = of_k ? full_k : full_v, empty = of_k ? empty_k : empty_v;
+    const uint32_t raw_at = L::kRaw + (of_k ? 0 : L::kRawTile) + ct * 16;       // this thread's pieces, kTrips of a tile, 128 x 16 bytes apart; two tiles
+    uint8_t* to_tile = base_ptr + (of_k ? 0 : L::kV) + half * L::kHalfBytes + my_token * 128;
     bool ok = true;
     uint32_t jj = 0;
     for (bool more = true; more && ok; more = ok && g.next(a, st)) {
       const int* pages = a.table + g.seq * a.table_stride;
-      const long long to_lane = g.hd * (long long)a.head_stride + my_piece * 16;
-      const uint8_t *k_lane = a.k + to_lane, *v_lane = a.v + to_lane;
-      auto block_numbers = [&](int j) -> int {           // of 16 tokens of tile j, for lanes 0 to 7; -1: behind the end
+      const uint8_t* from = (of_k ? a.k : a.v) + g.hd * (long long)a.head_stride;
+      const long long lane_off = my_token % 16 * a.token_stride + my_piece * 16;
+      auto block_number = [&](int j) -> int {            // of 16 tokens of tile j, for lanes 0 to 7; -1: behind the end
         const long long t = (long long)j * kQrTile + lane * 16;
         return lane < 8 && j < g.j1 && t < g.s.len ? pages[t >> a.block_shift] : -1;
       };
-      auto issue = [&](int j, int ids, const uint8_t* from, uint32_t dst) {       // K or V of tile j
-        const int left = j < g.j1 ? (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile) : 0;
-        if (j < g.j1)
+      auto issue = [&](int j, int id) {                  // id: of this lane's 16 tokens
+        const uint32_t dst = base + raw_at + ((jj + j - g.j0) & 1) * (L::kRawTile / 2);
+        if (j < g.j1) {
+          const int left = (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile);
+          const bool known = (unsigned)id < (unsigned)a.n_blocks;
+          const unsigned long long mine = known ? reinterpret_cast<unsigned long long>(from + id * a.block_stride + ((j * kQrTile + (lane & 7) * 16) & bs_mask) * a.token_stride) : 0ull;
 #pragma unroll 4
-        for (int i = 0; i < kTrips; ++i) {
-          const int token = i * kAtOnce + my_token, id = __shfl_sync(0xffffffffu, ids, token >> 4);
-          const bool there = token < left && (unsigned)id < (unsigned)a.n_blocks;
-          const uint8_t* p = there ? from + id * a.block_stride + ((j * kQrTile + token) & bs_mask) * a.token_stride : a.k;
-          copy_16(dst + i * 2048, p, there ? 16 : 0);
+          for (int i = 0; i < kTrips; ++i) {
+            const int token = i * kAtOnce + my_token;
+            const unsigned long long p = __shfl_sync(0xffffffffu, mine, token >> 4);
+            const bool there = token < left && p != 0;
+            copy_16(dst + i * 2048, there ? reinterpret_cast<const uint8_t*>(p) + lane_off : a.k, there ? 16 : 0);
+          }
         }
         copies_commit();
-      };
-      auto write = [&](uint32_t at, const uint8_t* from) {
-        uint8_t* to = base_ptr + at + half * L::kHalfBytes + my_token * 128;
-#pragma unroll 4
-        for (int i = 0; i < kTrips; ++i) {               // (kAtOnce tokens on, a row's chunks lie in the same order)
-          uint4 h[2];
-          to_half_16<TYPE>(*reinterpret_cast<const uint4*>(from + i * 2048), h);
-          *reinterpret_cast<uint4*>(to + place0) = half ? h[1] : h[0];
-          *reinterpret_cast<uint4*>(to + place1) = half ? h[0] : h[1];
-          to += kAtOnce * 128;
-        }
       };
       auto exponents = [&](int j, int ids, int* ek, int* ev) -> bool {       // of token ct; false: none
         const int id = __shfl_sync(0xffffffffu, ids, ct >> 4);
@@ -393,32 +394,40 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         }
         return there;
       };
-      // K of tile i and V of the tile before, for i = 0 .. n; the copies of either are asked for two trips ahead (K0 K1 V0 | K2 V1 | K3 V2 | ..)
       const int n = g.j1 - g.j0;
-      int e_run = -200, ek, ev, ids1 = block_numbers(g.j0), ids2 = block_numbers(g.j0 + 1);
-      issue(g.j0, ids1, k_lane, raw + (jj & 1) * kRawHalf);
-      issue(g.j0 + 1, ids2, k_lane, raw + (~jj & 1) * kRawHalf);
-      issue(g.j0, ids1, v_lane, raw + (2 + (jj & 1)) * kRawHalf);
-      bool there = exponents(g.j0, ids1, &ek, &ev);
-      ids1 = ids2;                                       // of tile i + 1
-      ids2 = block_numbers(g.j0 + 2);                    // of tile i + 2
-      for (int i = 0; i <= n; ++i) {
+      int e_run = -200, ek = 0, ev = 0, id1 = block_number(g.j0), id2 = block_number(g.j0 + 1);
+      issue(g.j0, id1);
+      issue(g.j0 + 1, id2);
+      bool there = of_k ? exponents(g.j0, id1, &ek, &ev) : false;
+      id1 = id2;                                         // of tile i + 1
+      id2 = block_number(g.j0 + 2);                      // of tile i + 2
+      for (int i = 0; i < n; ++i) {
         const uint32_t u = jj + i, x = u & 1;
-        const int ids3 = block_numbers(g.j0 + i + 3);
-        if (i < n) {
-          const int ring = u & 3;
+        const int ring = u & 3, id3 = block_number(g.j0 + i + 3);
+        copies_wait<1>();                                // (of this thread's own pieces)
+        if (u > 1) {
+          ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * x, ((u >> 1) & 1) ^ 1u, abort_flag));
+          if (!ok && !of_k) break;
+        }
+        uint8_t* to = to_tile + x * L::kTileBytes;
+        const uint8_t* raw = base_ptr + raw_at + x * (L::kRawTile / 2);
+#pragma unroll 4
+        for (int c = 0; c < (ok ? kTrips : 0); ++c) {    // (kAtOnce tokens on, a row's chunks lie in the same order)
+          uint4 h[2];
+          to_half_16<TYPE>(*reinterpret_cast<const uint4*>(raw + c * 2048), h);
+          *reinterpret_cast<uint4*>(to + c * kAtOnce * 128 + place0) = h[0];
+          *reinterpret_cast<uint4*>(to + c * kAtOnce * 128 + (place0 ^ 16)) = h[1];
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(full + 8 * x);
+        issue(g.j0 + i + 2, id2);
+        if (of_k) {
           const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
           if (lane == 0) largest_s[x][cw] = ev_max;      // (two: a warp may be a tile ahead)
-          asm volatile("bar.sync 1, 128;" ::: "memory");
+          ok = meet<1, 128>(ok);
+          if (!ok) break;
           e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
           const int e_now = max(e_run, kExpLeast);       // (no token yet: anything)
-          if (i == 0) copies_wait<2>(); else copies_wait<3>();        // K of this tile (this thread's own pieces)
-          if (u > 1) {
-            ok = mbar_wait(empty_k + 8 * x, ((u >> 1) & 1) ^ 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-          }
-          write(x * L::kTileBytes, raw_ptr + x * kRawHalf);
           float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
           const float nan = __uint_as_float(0x7fc00000u);
           const int down = ev - e_now + (int)kQrShift;   // (far below: nothing)
@@ -428,36 +437,20 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           if (lane == 0) gone_s[ring][cw] = odd;
           if (ct == 0) e_s[u & 7] = e_now;
           mbar_arrive(bar_scale + 8 * ring);
-          fence_proxy_async_smem();
-          mbar_arrive(full_k + 8 * x);
-          there = exponents(g.j0 + i + 1, ids1, &ek, &ev);
+          there = exponents(g.j0 + i + 1, id1, &ek, &ev);
         }
-        issue(g.j0 + i + 2, ids2, k_lane, raw + x * kRawHalf);
-        if (i > 0) {
-          const uint32_t v = u - 1, y = v & 1;
-          copies_wait<3>();                              // V of the tile before
-          if (v > 1) {
-            ok = mbar_wait(empty_v + 8 * y, ((v >> 1) & 1) ^ 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-          }
-          write(L::kV + y * L::kTileBytes, raw_ptr + (2 + y) * kRawHalf);
-          fence_proxy_async_smem();
-          mbar_arrive(full_v + 8 * y);
-        }
-        issue(g.j0 + i + 1, ids1, v_lane, raw + (2 + (~x & 1)) * kRawHalf);
-        ids1 = ids2;
-        ids2 = ids3;
+        id1 = id2;
+        id2 = id3;
       }
       jj += n;
       copies_wait<0>();
     }
     // the last products' arrivals come before the block goes
     for (uint32_t b = jj > 2 ? jj - 2 : 0; ok && b < jj; ++b)
-      ok = mbar_wait(empty_k + 8 * (b & 1), (b >> 1) & 1, abort_flag) && mbar_wait(empty_v + 8 * (b & 1), (b >> 1) & 1, abort_flag);
+      ok = mbar_wait(empty + 8 * (b & 1), (b >> 1) & 1, abort_flag);
   } else {
-    reg_dealloc<56>();
-    if (warp == 12) {
+    reg_dealloc<48>();
+    if (warp == 16) {
     // ================= products: the whole warp, one lane issues =================
     constexpr uint32_t idesc_qk = idesc_f16_f32(kQrRows, kQrTile, 0), idesc_pv = idesc_f16_f32(kQrRows, D, 1);
     constexpr uint32_t hi = desc_hi_sw128(1024);
@@ -501,7 +494,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
     while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 12) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
+  if (warp == 16) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
 }
 
 // The parts of tasks that went over several blocks: a row's parts weighed by their log-sum-exps, one warp per row at a time.  The blocks c0 <= b < c1 of a task share its rows.
