@@ -652,14 +652,13 @@ static cudaError_t launch_attend(const QuantAttnArgs& a, long long blocks, Devic
 template <int D, int NT>
 static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a, int sms, DeviceStatus* st, cudaStream_t stream) {
   const bool int8 = type == RELAXKV_INT8;
-  if constexpr (NT < 4)                                    // (more columns of long sequences go to the kernel of many rows)
-    if (!whole) {
-      const int blocks = std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
-      const cudaError_t e = int8 ? launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
-      if (e != cudaSuccess) return e;
-      auto kern = quantized_join_kernel<D, NT>;
-      return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
-    }
+  if (!whole) {
+    const int blocks = std::min(kQaBlocks, QaSmem<D, NT>::kBlocksPerSm * sms);
+    const cudaError_t e = int8 ? launch_attend<D, RELAXKV_INT8, NT, false>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, false>(a, blocks, st, stream);
+    if (e != cudaSuccess) return e;
+    auto kern = quantized_join_kernel<D, NT>;
+    return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
+  }
   const long long blocks = a.n_rows * a.Hkv * a.split;
   return int8 ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream);
 }
@@ -718,7 +717,9 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   while (a.split < 8 && 2 * a.split * items <= 2 * sms && 2 * a.split * kQaWarps <= tiles) a.split *= 2;
   const bool whole = tiles <= (a.split > 1 ? 16LL * a.split : 32) && items * a.split <= 0x7fffffffLL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (!whole && cols > 16) {
+  // More columns than one block holds, of long sequences: 128 at a time on the tensor cores, which takes less time than tokens brought several times (200 rows over 3000 tokens
+  // 58.7 against 74.8 us, 16 over 8 x 4 K 56.8 against 68; of up to 32 columns it takes more: 6 rows over 16 x 3000 tokens 69 against 56 us, over 8 K 24.7 against 22.1).
+  if (!whole && cols > kQaColsMost) {
     a.rows_per_tile = kQrRows / a.G;
     return cuda_ok(launch_quantized_rows(a, head_dim, store->type, sms, st, s));
   }
