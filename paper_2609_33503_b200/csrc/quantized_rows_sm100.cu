@@ -78,7 +78,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   __shared__ volatile uint32_t tmem_slot;
   __shared__ volatile int abort_s;
   __shared__ int largest_s[2][4], e_s[8];                 // largest exponents: of each of the four warps' tokens; of the values up to the last eight tiles
-  __shared__ uint32_t gone_s[4][4];                      // tokens of the last four tiles whose blocks do not exist, or that are NaN
+  __shared__ uint32_t gone_s[4][4], nan_s[4][4];          // tokens of the last four tiles whose blocks do not exist; whose values are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t full_k = base + L::kBar, full_v = full_k + 16, empty_k = full_v + 16, empty_v = empty_k + 16, bar_s = empty_v + 16, bar_m = bar_s + 16,
@@ -181,6 +181,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         const float* vs = ks + kQrTile;
         const int limit = seen < 0 ? kQrTile : seen - j * kQrTile;      // (rows that are not written see all: nothing to hide costs half as much)
         const bool slow = __any_sync(0xffffffffu, limit < kQrTile || (gone_s[ring][0] | gone_s[ring][1] | gone_s[ring][2] | gone_s[ring][3]) != 0);
+        const bool factors = slow && (nan_s[ring][0] | nan_s[ring][1] | nan_s[ring][2] | nan_s[ring][3]) != 0;
         // 32 scores times their keys' scales; what the row does not see (its tokens from `limit` on, tokens without a block) becomes -inf
         auto scores = [&](int c, float* y) -> uint32_t {
           uint32_t w[32];
@@ -194,12 +195,10 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           }
           uint32_t hidden = 0;
           if (slow) {
-            hidden = limit >= 32 * (c + 1) ? 0u : limit <= 32 * c ? 0xffffffffu : 0xffffffffu << (limit - 32 * c);
+            hidden = (limit >= 32 * (c + 1) ? 0u : limit <= 32 * c ? 0xffffffffu : 0xffffffffu << (limit - 32 * c)) | gone_s[ring][c];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              if (ks[c * 32 + e] == -INFINITY) hidden |= 1u << e;
+            for (int e = 0; e < 32; ++e)
               if (hidden >> e & 1) y[e] = -INFINITY;
-            }
           }
           return hidden;
         };
@@ -257,7 +256,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
               pk[(e + u) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
           }
-          if (slow) {                                    // what is not seen weighs nothing, whatever its factor
+          if (factors) {                                 // what is not seen weighs nothing, whatever its factor
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (hidden >> e & 1) pk[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
@@ -297,10 +296,13 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       const bool whole = g.whole();
       const int slot = g.slot();
       if (tid == 0) {
-        Chain c = {-1, 0, g.s.first + g.tile * rpt, g.hd, min(rpt, g.s.n - g.tile * rpt) * G};
-        if (g.j1 < g.tiles) g.blocks_of(&c.c0, &c.c1);
-        a.chain[blockIdx.x] = c;                         // (the last task's stays)
+        Chain* c = a.chain + blockIdx.x;                 // (the last task's stays)
+        int c0 = -1, c1 = 0;
+        if (g.j1 < g.tiles) g.blocks_of(&c0, &c1);
+        c->c0 = c0; c->c1 = c1; c->row = g.s.first + g.tile * rpt; c->head = g.hd; c->cols = min(rpt, g.s.n - g.tile * rpt) * G;
       }
+      const uint32_t live = __ballot_sync(0xffffffffu, seen >= 0);
+      if (x == 0 && lane == 0) a.chain[blockIdx.x].live[warp] = live;
       if (ok && busy) {
         tc_fence_after();
         const float zz = sum_s[t] + sum_s[kQrRows + t];
@@ -431,10 +433,10 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
           const float nan = __uint_as_float(0x7fc00000u);
           const int down = ev - e_now + (int)kQrShift;   // (far below: nothing)
-          ks[ct] = there ? exp_scale(ek) : -INFINITY;
+          ks[ct] = there ? exp_scale(ek) : 0.f;
           ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
-          const uint32_t odd = __ballot_sync(0xffffffffu, !there || ek == kExpNone || ev == kExpNone);
-          if (lane == 0) gone_s[ring][cw] = odd;
+          const uint32_t gone = __ballot_sync(0xffffffffu, !there), no_number = __ballot_sync(0xffffffffu, there && ev == kExpNone);
+          if (lane == 0) { gone_s[ring][cw] = gone; nan_s[ring][cw] = no_number; }
           if (ct == 0) e_s[u & 7] = e_now;
           mbar_arrive(bar_scale + 8 * ring);
           there = exponents(g.j0 + i + 1, id1, &ek, &ev);
@@ -497,8 +499,10 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   if (warp == 16) { tc_fence_after(); tmem_dealloc(tmem_base, kTmemCols); }
 }
 
-// The parts of tasks that went over several blocks: a row's parts weighed by their log-sum-exps, one warp per row at a time.  The blocks c0 <= b < c1 of a task share its rows.
-constexpr int kQrJoinWarps = 8, kQrJoinBatch = 4;
+// The parts of tasks that went over several blocks: a row's parts weighed by their log-sum-exps, one warp per row at a time.  The blocks c0 <= b < c1 of a task share its rows
+// (of 32 warps: a row is a chain of dependent reads, and a task of two parts has one block for its 128 rows; 8 warps and a look at each row's length took 15 us more for 200
+// rows over 900 tokens).
+constexpr int kQrJoinWarps = 32, kQrJoinBatch = 4;
 template <int D>
 __global__ void __launch_bounds__(kQrJoinWarps * 32)
 quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st) {
@@ -515,7 +519,7 @@ quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
     const int r = col / a.G, head = ch.head * a.G + col - r * a.G;
     const long long row = ch.row + r;
-    bool live = false;
+    if (!(a.chain[blockIdx.x].live[col >> 5] >> (col & 31) & 1)) continue;           // (the row is left alone)
     for (int p0 = 0; p0 < parts; p0 += kQrJoinBatch) {
       float l[kQrJoinBatch], v[kQrJoinBatch][kPer];
 #pragma unroll
@@ -526,15 +530,6 @@ quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         l[b] = a.part_s[at];
         if constexpr (kPer == 4) *reinterpret_cast<float4*>(v[b]) = *reinterpret_cast<const float4*>(a.part_o + at * D + lane * kPer);
         else *reinterpret_cast<float2*>(v[b]) = *reinterpret_cast<const float2*>(a.part_o + at * D + lane * kPer);
-      }
-      if (p0 == 0) {                                     // (rows that are left alone have no parts: what was read is not looked at)
-        const int seq = a.row_seq[row];
-        live = seq >= 0 && seq < a.n_seq;
-        if (live) {
-          const SeqRows s = rows_of(a, seq, -1, 0, false, st);
-          live = row >= s.first && row < s.first + s.n && row_tokens(a, seq, s, row, false, st) >= 0;
-        }
-        if (!live) break;
       }
 #pragma unroll
       for (int b = 0; b < kQrJoinBatch; ++b) {
@@ -547,7 +542,6 @@ quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         m = now;
       }
     }
-    if (!live) continue;
     const bool none = den == 0.f;
     const float inv = none ? 0.f : one_over(den);
     uint32_t packed[kPer / 2];
