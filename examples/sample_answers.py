@@ -3,6 +3,7 @@
 
     python examples/sample_answers.py                       # 16 samples of a 16K context, 4 layers of 32 / 8 heads
     python examples/sample_answers.py --select 64           # each row reads the 64 context blocks it may need most
+    python examples/sample_answers.py --store int8          # every sample has the repaired context in 8 bits
 """
 from __future__ import annotations
 
@@ -29,6 +30,7 @@ def main() -> None:
     ap.add_argument("--steps", type=int, default=16, help="decoded tokens per sample")
     ap.add_argument("--question", type=int, default=8, help="tokens of the question that every sample begins with")
     ap.add_argument("--select", type=int, default=0, help="context blocks that a row reads (0: the whole context)")
+    ap.add_argument("--store", choices=["bf16", "int8", "e4m3"], default="bf16", help="what the samples' store holds; in 8 bits it holds their contexts as well")
     a = ap.parse_args()
     H, Hkv, D, L, ctx = 32, 8, 128, a.layers, a.ctx
     blk = inputs.BlockShape(hidden=1024, inter=2048, rope_theta=5.0e5, eps=1.0e-5)
@@ -63,9 +65,14 @@ def main() -> None:
 
     # ---- the samples: the question once each, then one token of each per step ----
     n = a.samples
-    c = Continuations(H, Hkv, D, [ctx], [n], L, blk, n_blocks=n * (-(-(a.question + a.steps) // 16)), max_len=a.question + a.steps, block_size=16,
-                      max_rows=n * max(1, a.question), n_select=a.select)
-    span("bounds", lambda: c.context_bounds(caches))
+    dtype = {"bf16": None, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[a.store]
+    kept = 0 if dtype is None else ctx
+    c = Continuations(H, Hkv, D, [ctx], [n], L, blk, n_blocks=n * (-(-(kept + a.question + a.steps) // 16)), max_len=a.question + a.steps, block_size=16,
+                      max_rows=max(n * max(1, a.question), min(kept, 4096)), n_select=a.select, store_dtype=dtype)
+    if dtype is None:
+        span("bounds", lambda: c.context_bounds(caches))
+    else:
+        span("keep", lambda: c.keep_contexts(caches))
     g = torch.Generator(device="cuda").manual_seed(7)
     embed = lambda rows: torch.randn(rows, blk.hidden, generator=g, device="cuda").to(torch.bfloat16)
     question = embed(a.question).repeat(n, 1)

@@ -285,6 +285,10 @@ class CacheView:
     def ref(self):
         return ctypes.byref(self.c)
 
+    def start(self, req: int) -> int:
+        """Token row at which a request begins."""
+        return int(self._off[req])
+
 
 class PagedStore:
     """Host-side relaxkv_paged_cache over torch tensors k, v of logical shape [n_blocks, block_size, H_kv, D] (any block, token and head

@@ -7,6 +7,10 @@ tables and slot maps once for all layers, then per layer the decoder block, with
 launch and attention over [the shared context, the sequence's own tokens].  The context is read once for all its rows; with
 `n_select` only the blocks that each row may need most are read (8-bit bounds of the keys' blocks choose them).
 
+With `store_dtype` (int8 or e4m3) the repaired contexts move into the store themselves, in 8 bits (`keep_contexts`), and the caches are free for
+the next repair: half the bytes to hold, and to read at each step.  Then every sequence has its own copy of its context, and all its rows' attention
+reads the store alone.
+
 Call sequencing over torch buffers only; every operation runs in the CUDA kernels behind `binding`.
 """
 from __future__ import annotations
@@ -25,7 +29,10 @@ class Continuations:
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, ctx_lens: Sequence[int], seqs: Sequence[int], n_layers: int,
                  blk: BlockShape, n_blocks: int, max_len: int, block_size: int = 64, max_rows: Optional[int] = None, n_select: int = 0,
-                 n_first: int = 1, n_last: int = 2, ctx_block: int = 64, device="cuda", softmax_scale: Optional[float] = None):
+                 n_first: int = 1, n_last: int = 2, ctx_block: int = 64, device="cuda", softmax_scale: Optional[float] = None,
+                 store_dtype: Optional[torch.dtype] = None):
+        if store_dtype is not None and (store_dtype not in B.QuantizedStore.TYPES or n_select > 0):
+            raise ValueError("contexts are kept in int8 or float8_e4m3fn, and read whole" if n_select > 0 else f"no store of {store_dtype}")
         self.H, self.Hkv, self.D, self.blk, self.n_layers = n_q_heads, n_kv_heads, head_dim, blk, int(n_layers)
         self.device = torch.device(device)
         self.ctx_lens, self.seqs = [int(x) for x in ctx_lens], [int(x) for x in seqs]
@@ -37,14 +44,25 @@ class Continuations:
         self.shape = B.Shape(self.H, self.Hkv, self.D, self.ctx_lens, None, softmax_scale)
         bf = dict(dtype=torch.bfloat16, device=self.device)
         i32 = dict(dtype=torch.int32, device=self.device)
-        self.stores = [B.PagedStore(*(torch.empty(n_blocks, self.block_size, self.Hkv, self.D, **bf) for _ in range(2)))
-                       for _ in range(self.n_layers)]
+        self.store_dtype = store_dtype
+        if store_dtype is None:
+            self.stores = [B.PagedStore(*(torch.empty(n_blocks, self.block_size, self.Hkv, self.D, **bf) for _ in range(2)))
+                           for _ in range(self.n_layers)]
+        else:
+            self.stores = [B.QuantizedStore.empty(n_blocks, self.block_size, self.Hkv, self.D, store_dtype, self.device) for _ in range(self.n_layers)]
+            max_len += max((t for t, n in zip(self.ctx_lens, self.seqs) if n > 0), default=0)
+        self.rotary = blk.rotary
+        if self.rotary is None and store_dtype is not None:
+            self.rotary = B.Rotary.scaled(self.D, blk.rope_theta, device=self.device)
+        self.softmax_scale = softmax_scale
         self.width = -(-int(max_len) // self.block_size)
         self.table = torch.full((n_seq, self.width), -1, **i32)
         self.free = torch.arange(n_blocks - 1, -1, -1, **i32)
         self._n_free = [torch.full((1,), n_blocks, **i32), torch.empty(1, **i32)]          # before and after a step, in turn
         self._len = [torch.zeros(n_seq, **i32), torch.empty(n_seq, **i32)]
-        self.base = torch.cat([torch.full((n,), t, **i32) for t, n in zip(self.ctx_lens, self.seqs)] or [torch.empty(0, **i32)])
+        # what lies before a sequence's tokens in the store: its context, unless that is in the store as well
+        self.base = torch.cat([torch.full((n,), 0 if store_dtype is not None else t, **i32) for t, n in zip(self.ctx_lens, self.seqs)] or [torch.empty(0, **i32)])
+        self.zeros = torch.zeros(self.max_rows, **i32) if store_dtype is None and blk.rotary is not None else None
         self.lens = [0] * n_seq                        # the host's copy of the lengths: what it asks for is what it gets
         self.n_free = int(n_blocks)
         self._new: Dict[tuple, torch.Tensor] = {}
@@ -63,9 +81,12 @@ class Continuations:
             self.bounds = [torch.empty(nb, self.Hkv, 2, self.D, dtype=torch.int8, device=self.device) for _ in range(self.n_layers)]
             self.scale = [torch.empty(nb, self.Hkv, dtype=torch.float32, device=self.device) for _ in range(self.n_layers)]
             self.blocks = torch.empty(R, self.Hkv, self.n_select, **i32)
-        nbytes = B.relaxkv_continuation_workspace_bytes(self.shape, R, self.ctx_block if self.n_select else 0)
+        if store_dtype is None:
+            nbytes = B.relaxkv_continuation_workspace_bytes(self.shape, R, self.ctx_block if self.n_select else 0)
+        else:
+            nbytes = B.relaxkv_quantized_workspace_bytes(self.H, self.Hkv, self.D)
         if nbytes == 0:
-            raise B.RelaxKVError(B.ERR_INVALID_ARG, "relaxkv_continuation_workspace_bytes")
+            raise B.RelaxKVError(B.ERR_INVALID_ARG, "relaxkv_continuation_workspace_bytes" if store_dtype is None else "relaxkv_quantized_workspace_bytes")
         ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         off = (-ws.data_ptr()) % 256
         self.workspace = ws[off:off + nbytes]
@@ -131,8 +152,60 @@ class Continuations:
         self.rows = B.ContinuationRows(self.seq_cu, per_ctx, longest, self.row_cu, self.row_seq[:rows], self.row_len[:rows], self.table)
         return rows
 
+    def keep_contexts(self, caches: Sequence[B.CacheView], sequences: Optional[Sequence[int]] = None) -> None:
+        """The contexts of these sequences (all, where None) as they stand in the caches of every layer, into the store, in steps of max_rows tokens: once
+        the repair is through, and again for sequences that have ended.  The next step's rows follow them."""
+        if self.store_dtype is None:
+            raise ValueError("contexts are kept in the store only where it has a store_dtype")
+        owner = [b for b, n in enumerate(self.seqs) for _ in range(n)]
+        which = list(range(self.n_seq)) if sequences is None else sorted({int(i) for i in sequences})
+        if any(not 0 <= i < self.n_seq for i in which) or any(self.lens[i] for i in which):
+            raise ValueError("contexts are kept for sequences that have no tokens yet")
+        short = sum(self._blocks(self.ctx_lens[owner[i]]) for i in which) - self.n_free
+        if short > 0:
+            raise ValueError(f"{short} blocks short: let sequences end, or give the store more")
+        which = [i for i in which if self.ctx_lens[owner[i]] > 0]
+        if which and (len(caches) != self.n_layers or any(c is None or c.v is None or c.heads != self.Hkv or c.dim != self.D or c.room[b] < self.ctx_lens[b]
+                                                          for c in caches for b in {owner[i] for i in which})):
+            raise ValueError(f"caches of {self.n_layers} layers with {self.Hkv} heads of {self.D} that hold the contexts expected")
+        done = {i: 0 for i in which}
+        while True:
+            new, room = [0] * self.n_seq, self.max_rows
+            for i in which:
+                new[i] = min(room, self.ctx_lens[owner[i]] - done[i])
+                room -= new[i]
+            if not any(new):
+                break
+            self.begin(new)
+            for l, cache in enumerate(caches):
+                at = 0
+                for i in which:
+                    if new[i]:
+                        t = cache.start(owner[i]) + done[i]
+                        B.relaxkv_append_quantized(self.stores[l], cache.k[t:t + new[i]], cache.v[t:t + new[i]], self.row_slot[at:at + new[i]])
+                        at += new[i]
+            for i in which:
+                done[i] += new[i]
+        self.rows, self.n_rows = None, 0
+
+    def _append(self, layer: int, w: Dict[str, torch.Tensor], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Norm and rotation of the step's q and k, the append of k and v."""
+        blk, n, store = self.blk, q.shape[0], self.stores[layer]
+        q_norm, k_norm = w.get("w_q_norm"), w.get("w_k_norm")
+        if self.store_dtype is not None:
+            B.relaxkv_append_quantized(store, k, v, self.row_slot[:n], q, q, self.row_pos[:n], self.rotary, q_norm, k_norm, blk.eps)
+        elif self.rotary is not None:
+            B.relaxkv_qk_norm_rotate(q, k, self.row_pos[:n], self.rotary, None, None, q_norm, k_norm, blk.eps)
+            B.relaxkv_qk_norm_rope_append_paged(store, q, k, v, self.zeros, self.row_slot, blk.rope_theta, q)      # (position 0: as they are)
+        else:
+            B.relaxkv_qk_norm_rope_append_paged(store, q, k, v, self.row_pos, self.row_slot, blk.rope_theta, q, q_norm, k_norm, blk.eps)
+
     def attention(self, layer: int, cache: Optional[B.CacheView], q: torch.Tensor, out: torch.Tensor, lse_out=None, stream=None) -> None:
-        """Attention of the step's rows at one layer, their own K/V appended: over the whole contexts, or over n_select blocks of them."""
+        """Attention of the step's rows at one layer, their own K/V appended: over the whole contexts, or over n_select blocks of them (`cache` is not looked
+        at where the store has the contexts)."""
+        if self.store_dtype is not None:
+            B.relaxkv_quantized_attention(self.stores[layer], self.rows, q, out, self.workspace, lse_out=lse_out, softmax_scale=self.softmax_scale, stream=stream)
+            return
         if self.n_select == 0:
             B.relaxkv_shared_prefix_attention(self.shape, cache, self.stores[layer], self.rows, q, out, self.workspace, lse_out=lse_out, stream=stream)
             return
@@ -142,9 +215,11 @@ class Continuations:
         B.relaxkv_block_sparse_attention(self.shape, cache, self.stores[layer], self.rows, self.ctx_block, blocks, q, out, self.workspace,
                                          lse_out=lse_out, stream=stream)
 
-    def run(self, h0: torch.Tensor, weights: List[Dict[str, torch.Tensor]], caches: Sequence[Optional[B.CacheView]]) -> torch.Tensor:
+    def run(self, h0: torch.Tensor, weights: List[Dict[str, torch.Tensor]], caches: Optional[Sequence[Optional[B.CacheView]]] = None) -> torch.Tensor:
         """The step's rows through the decoder: h0 [n_rows, hidden] = their input representations (rows behind them are not looked
-        at).  Returns the hidden rows after the last layer (one of this object's buffers)."""
+        at); no caches where the store has the contexts.  Returns the hidden rows after the last layer (one of this object's buffers)."""
+        if caches is None and self.store_dtype is None:
+            raise ValueError("the contexts' caches are missing")
         n, blk = self.n_rows, self.blk
         if n == 0:
             return h0
@@ -158,9 +233,8 @@ class Continuations:
             h_out = self.h[l % 2][:n]
             B.relaxkv_rmsnorm(h, w["w_in_norm"], x, blk.eps)
             B.relaxkv_linear_qkv(x, w["w_qkv"], q, k, v)
-            B.relaxkv_qk_norm_rope_append_paged(self.stores[l], q, k, v, self.row_pos, self.row_slot, blk.rope_theta, q, w.get("w_q_norm"),
-                                                w.get("w_k_norm"), blk.eps)
-            self.attention(l, caches[l], q, o)
+            self._append(l, w, q, k, v)
+            self.attention(l, None if caches is None else caches[l], q, o)
             B.relaxkv_linear(o, w["wo"], a, residual=h)
             B.relaxkv_rmsnorm(a, w["w_post_norm"], x, blk.eps)
             if blk.inter % 128 == 0:

@@ -233,12 +233,14 @@ NAMED: Dict[str, object] = {
 @dataclasses.dataclass(frozen=True)
 class BlockShape:
     """Llama-style pre-norm decoder block: hidden size, SwiGLU width, rotary base, RMSNorm epsilon; `qk_norm`
-    adds the per-head RMSNorm of the projected queries and keys (Qwen3)."""
+    adds the per-head RMSNorm of the projected queries and keys (Qwen3).  `rotary` (a binding.Rotary) takes the place of
+    the rotary embedding of `rope_theta` over whole heads: scaled frequencies, parts of a head, interleaved pairs."""
     hidden: int
     inter: int
     rope_theta: float = 1.0e6
     eps: float = 1.0e-6
     qk_norm: bool = False
+    rotary: Optional[object] = None
 
 
 QWEN3_14B_BLOCK = BlockShape(hidden=5120, inter=17408, qk_norm=True)

@@ -62,7 +62,8 @@ class LayerLoop:
             # per-head RMSNorm of the projected queries and keys (models that have one) and the rotary embedding at the
             # targets' original positions: one pass over q and k
             rec("rope", lambda: (B.relaxkv_target_positions(s.shape, s.u_pos, s.u_cu, s.r_rank, s.r_cu_layer(l), n_r[l], pos),
-                                 B.relaxkv_qk_norm_rope(q, k, pos, blk.rope_theta, w.get("w_q_norm"), w.get("w_k_norm"), blk.eps)))
+                                 B.relaxkv_qk_norm_rope(q, k, pos, blk.rope_theta, w.get("w_q_norm"), w.get("w_k_norm"), blk.eps) if blk.rotary is None else
+                                 B.relaxkv_qk_norm_rotate(q, k, pos, blk.rotary, None, None, w.get("w_q_norm"), w.get("w_k_norm"), blk.eps)))
             rec("attention", lambda: s.attention(l, caches[l], q, k, v, o, n_r[l], n_u))
             rec("scatter", lambda: s.scatter(l, caches[l], k, v, n_r[l]))
             rec("o_proj", lambda: B.relaxkv_linear(o, w["wo"], a, residual=h))

@@ -90,8 +90,12 @@ class QueryPass:
         if "w_qkv" not in w:                            # weight-loading step, once per layer: [Wq; Wk; Wv] stacked
             w["w_qkv"] = B.stack_qkv(w["wq"], w["wk"], w["wv"])
         rec("qkv_proj", lambda: B.relaxkv_linear_qkv(x, w["w_qkv"], q, k, v))
-        rec("rope_append", lambda: B.relaxkv_qk_norm_rope_append(shape, cache, q, k, v, pos, cu, counts, blk.rope_theta,
-                                                                 w.get("w_q_norm"), w.get("w_k_norm"), blk.eps))
+        if blk.rotary is None:
+            rec("rope_append", lambda: B.relaxkv_qk_norm_rope_append(shape, cache, q, k, v, pos, cu, counts, blk.rope_theta,
+                                                                     w.get("w_q_norm"), w.get("w_k_norm"), blk.eps))
+        else:
+            rec("rope_append", lambda: (B.relaxkv_qk_norm_rotate(q, k, pos, blk.rotary, None, None, w.get("w_q_norm"), w.get("w_k_norm"), blk.eps),
+                                        B.relaxkv_scatter_kv_lists(shape, cache, k, v, pos, cu, counts)))
         rec("attention", attend)
         rec("o_proj", lambda: B.relaxkv_linear(o, w["wo"], a, residual=h))
         rec("norm", lambda: B.relaxkv_rmsnorm(a, w["w_post_norm"], x, blk.eps))
