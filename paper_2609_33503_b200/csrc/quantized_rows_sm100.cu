@@ -19,7 +19,7 @@ using namespace ptx;
 constexpr int kQrTile = 128, kQrThreads = 640;           // tokens of a tile; warps 0-3 and 4-7: a row per thread, 8-11: K, 12-15: V, 16: products, three idle
 constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
 constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
-using QrWalk = Walk<kQrTile, 2, 2, 128>;
+using QrWalk = Walk<kQrTile, 4, 2, 128>;                 // a task's start and end take as long as four tiles (57 rows over 16 K: of two 68 us, of three to six 64)
 
 template <int D>
 struct QrSmem {
@@ -78,6 +78,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   __shared__ volatile uint32_t tmem_slot;
   __shared__ volatile int abort_s;
   __shared__ int largest_s[2][4], e_s[8];                 // largest exponents: of each of the four warps' tokens; of the values up to the last eight tiles
+  __shared__ uint32_t top_s[2][kQrRows];                 // largest bits of a row's dims, by half
   __shared__ uint32_t gone_s[4][4], nan_s[4][4];          // tokens of the last four tiles whose blocks do not exist; whose values are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -130,23 +131,22 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       const int head = g.hd * G + in_group;
       const bool exists = t_local < min(rpt, g.s.n - g.tile * rpt);
       const int seen = exists ? row_tokens(a, g.seq, g.s, row, x == 0 && in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
-      // ---- Q: as fp16 times 2^-exponent, two dims to a word; each group brings half of them ----
+      // ---- Q: as fp16 times 2^-exponent, two dims to a word; each group brings half of them, and both know the largest ----
       float qs;
       {
         uint32_t w[D / 4], top = 0;
-        const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D);
+        const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D) + x * (D / 16);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {                    // (its own half last)
-          const int from = (h ^ x ^ 1) * (D / 16);
-#pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint4 v = exists ? q[from + c] : make_uint4(0, 0, 0, 0);
-            w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
-          }
-#pragma unroll
-          for (int c = 0; c < D / 4; ++c) top = __vmaxu2(top, w[c] & 0x7fff7fffu);
+        for (int c = 0; c < D / 16; ++c) {
+          const uint4 v = exists ? q[c] : make_uint4(0, 0, 0, 0);
+          w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
         }
+#pragma unroll
+        for (int c = 0; c < D / 4; ++c) top = __vmaxu2(top, w[c] & 0x7fff7fffu);
         top = max(top & 0xffffu, top >> 16);
+        top_s[x][t] = top;
+        if (!(ok = meet<2, 256>(ok))) break;
+        top = max(top, top_s[x ^ 1][t]);
         const bool finite = top < 0x7f80u;
         const int e = max((int)(top >> 7) - 127 - 14, -120);
         const float inv = __uint_as_float((uint32_t)(127 - (finite ? e : 0)) << 23);
@@ -320,7 +320,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           if (seen >= 0 && !whole) {
             float* p = a.part_o + ((long long)slot * kQrRows + t) * D + c * 32;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(p + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 32; e += 8) st_global_32b(p + e, o + e);
           } else if (seen >= 0) {
             uint16_t* p = a.out + (row * a.H + head) * D + c * 32;
 #pragma unroll
