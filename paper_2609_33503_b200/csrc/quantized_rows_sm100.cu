@@ -373,7 +373,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           const int left = (int)min((long long)kQrTile, g.s.len - (long long)j * kQrTile);
           const bool known = (unsigned)id < (unsigned)a.n_blocks;
           const unsigned long long mine = known ? reinterpret_cast<unsigned long long>(from + id * a.block_stride + ((j * kQrTile + (lane & 7) * 16) & bs_mask) * a.token_stride) : 0ull;
-#pragma unroll 4
+#pragma unroll 8
           for (int i = 0; i < kTrips; ++i) {
             const int token = i * kAtOnce + my_token;
             const unsigned long long p = __shfl_sync(0xffffffffu, mine, token >> 4);
@@ -413,7 +413,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         }
         uint8_t* to = to_tile + x * L::kTileBytes;
         const uint8_t* raw = base_ptr + raw_at + x * (L::kRawTile / 2);
-#pragma unroll 4
+#pragma unroll 8
         for (int c = 0; c < (ok ? kTrips : 0); ++c) {    // (kAtOnce tokens on, a row's chunks lie in the same order)
           uint4 h[2];
           to_half_16<TYPE>(*reinterpret_cast<const uint4*>(raw + c * 2048), h);
