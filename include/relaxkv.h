@@ -587,7 +587,7 @@ typedef enum {
 
 /* The 8-bit store of one layer.  Token t of block x of KV head g: values at k + x * block_stride + t * token_stride + g * head_stride (bytes = elements;
  * head_dim of them side by side), same for V, strides multiples of 16, that of heads below 2^31; exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V.
- * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN.  All pointers 16-byte aligned. */
+ * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN; others are -100 to 127.  All pointers 16-byte aligned. */
 typedef struct {
   void* k;
   void* v;
@@ -659,10 +659,11 @@ size_t relaxkv_quantized_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, 
  * Attention of a step's rows over their sequence's tokens in the 8-bit store: row r of sequence i sees the first row_len[r] tokens of the blocks block_table[i, ..],
  *   out[r,h,:] = softmax over t < row_len[r] of softmax_scale * <q[r,h,:], K[t]>, times V        (keys and values as the store's bytes stand for them)
  * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits, and to 2^-38 of the
- * row's largest (weight times value's scale), before they meet the values.  Any number of rows to a sequence; a sequence's tokens are
- * read once for 8 / G to 32 / G rows of it, G = n_q_heads / n_kv_heads <= 16.  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
+ * row's largest (weight times value's scale), before they meet the values.  Any number of rows to a sequence.  With G = n_q_heads / n_kv_heads <= 16 and G times the sequences' rows on
+ * average up to 32, a sequence's tokens are read once for 8 / G to 32 / G rows of it; beyond that once for 128 / G, and weights are rounded to 2^-35 of (the row's largest
+ * weight times the largest value's scale of the sequence's tokens).  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
  * n_seq <= 4096; row_len does not fall within a sequence.  A row that sees no token gets zeros and lse = -inf.
- *   q, out  device bf16 [n_rows, n_q_heads, head_dim] (16-byte aligned); lse_out NULL or device fp32 [n_q_heads, n_rows]
+ *   q, out  device bf16 [n_rows, n_q_heads, head_dim] (16-byte aligned, not the same); lse_out NULL or device fp32 [n_q_heads, n_rows]
  * Rows with row_seq -1 and rows behind row_cu[n_seq] are left alone.  Reported and left alone: rows of a sequence whose row_cu, or whose last row_len, is out of range, rows whose row_seq is another
  * sequence, whose row_len is negative or above the sequence's last.  A block number out of range is reported, its tokens are passed over.  max_len up to 2^31 - 256.
  */

@@ -9,9 +9,16 @@
 // product as rows of tokens and goes into the second as columns of them: one 8 x 8 transposition per 8 tokens.
 //
 // A warp streams 32 tokens at a time through a ring of its own in shared memory (16-byte asynchronous copies, no barrier between warps; what lies behind a
-// sequence's end is filled with zeros and never read), eight warps to an SM with two tiles of 8 KB in flight each.  The work of a call - (sequence, KV head, row tile, 32
-// tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths: a block's first and last task may be
-// parts of one, whose results a second small kernel joins in the order of the blocks.
+// sequence's end is filled with zeros and never read): twelve warps to an SM with two tiles of 8 KB in flight each, eight with three where a block has more than eight columns.
+// The work of a call - (sequence, KV head, row tile, 32 tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths; a task counts eight
+// units more, the time of its start and end.  A block's first and last task may be parts of one, whose results a second small kernel joins in the order of the blocks.  The next
+// task's first copies are on their way while a task's results are added up.  Calls of few short sequences give a cluster of up to eight blocks to each row tile and KV head, which
+// joins within itself: one launch.  More than 32 columns to a sequence go to the kernel of many rows (quantized_rows_sm100.cu).
+//
+// Measured (int8, D 128, one row a sequence, L2 flushed): one sequence of 128 K of 32 / 8 heads 62 us (4.4 TB/s; 55 us with the heads' tokens side by side), 64 of up to 4 K of 40 / 8
+// heads 61.6 (4.75 TB/s), 16 of up to 8 K 41, three rows of eight sequences of 8 K to 64 K 105.5 (4.9 TB/s), 1 K of 4 / 1 heads 7.1.  Between its first and last copies a call is at
+// 5.4 to 6.5 TB/s of the 6.57 that a plain copy makes; its start takes 3.3 us (arguments, lengths and block numbers, one read behind the other), its end some 12 (blocks that had more of
+// the late copies, the four warps' results, the join).
 #include "quantized_attention.cuh"
 
 namespace relaxkv {
@@ -124,6 +131,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     rank = (int)blockIdx.x - unit * a.split;
     g.hd = unit - (int)row * a.Hkv;
     g.seq = a.row_seq[row];
+    const int before = rpt > 1 && row > 0 ? a.row_seq[row - 1] : -1;
     const bool tell = tid == 0 && g.hd == 0 && rank == 0;
     bool mine = row < a.row_cu[a.n_seq] && g.seq != -1;
     if (mine && (g.seq < 0 || g.seq >= a.n_seq)) {
@@ -131,6 +139,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       mine = false;
     }
     if (!mine) return;
+    if (before == g.seq) {                                            // (what most blocks see first, and enough for them)
+      const int first = a.row_cu[g.seq];
+      if (first >= 0 && row > first && (row - first) % rpt != 0) return;
+    }
     g.s = rows_of(a, g.seq, -1, 0, tell, st);
     if (g.s.n == 0) return;
     if (row < g.s.first || row >= g.s.first + g.s.n) {

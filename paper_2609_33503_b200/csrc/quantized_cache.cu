@@ -7,6 +7,10 @@
 // remainder in fp64 (a float of position 100000 would be off by 2^-8 radians), sine and cosine of that in fp32.  Everything else stays in fp32 until the one rounding at the
 // end.  The scale of 8 bits is a power of two: the division by it is exact, values of two eighths of bf16's bits stay exact when read back, and the
 // bytes do not depend on the order of anything.
+//
+// Measured (L2 flushed): 8205 rows of 40 / 8 heads with norms, half the head turned, 40 us (5.0 TB/s of bytes that have to move); 16 K rows of 8 heads written as e4m3 and read back
+// 44.8 us; 32 K rows read and turned 41.4 (4.9 TB/s); 64 rows of 32 / 8 heads turned 5.4, written and read back 9.8.  For many rows the schedulers issue in 78 % of their cycles: norm, turn and
+// rounding of eight elements are some 160 instructions with their addresses.  Sixteen elements to a lane took longer (50.7 us; 45.9 read), fewer heads being in flight.
 #include "quantized_cache.cuh"
 #include "sm100_ptx.cuh"
 #include <cmath>
