@@ -339,11 +339,12 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
 }
 
 // Rows that go to the store, or come from it, as they are.  A warp has a row's key heads and value heads, which lie alike, side by side: one address, one exchange of the largest
-// elements (16 bits each) for both.  (As a case of the kernels above, 170 instructions for eight elements of two heads in place of 50: 16 K rows of 8 heads to e4m3 29 us.)
+// elements (16 bits each) for both.  (As a case of the kernels above, 170 instructions for eight elements of two heads in place of 50; 16 K rows of 8 heads to
+// e4m3 and back 45 us, so 34.5.  Two or four heads ahead of the one at work 35.4.)
 template <int D, int STORE, int ROWS>
 __global__ void __launch_bounds__(kTurnThreads)
 store_plain_rows_kernel(const TurnArgs a, DeviceStatus* st) {
-  constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kWarps = kTurnThreads / 32 / ROWS, kUnits = kWarps * kPerWarp, U = 2;
+  constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kWarps = kTurnThreads / 32 / ROWS, kUnits = kWarps * kPerWarp;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane % kLanes, h0 = (warp % kWarps) * kPerWarp;
   const long long row = (long long)blockIdx.x * ROWS + warp / kWarps;
   griddep_launch();
@@ -355,45 +356,35 @@ store_plain_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   if (!stored && slot != -1 && h0 == 0 && lane == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ROWS, (int)row, slot);
   const int block = slot >> a.block_shift, token = slot & ((1 << a.block_shift) - 1);
   const long long at = block * a.block_stride + token * a.token_stride + gl * 8, exp_at = (((long long)block * a.Hkv) << a.block_shift) + token;
-  for (int h1 = h0; h1 < a.Hkv; h1 += U * kUnits) {          // (the same for all lanes)
-    uint4 k[U], v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h1 + u * kUnits + lane / kLanes;
-      k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < a.Hkv) {
-        const long long off = (long long)h * a.k_head;
-        k[u] = *reinterpret_cast<const uint4*>(pk + off);
-        v[u] = *reinterpret_cast<const uint4*>(pv + off);
-      }
+  for (int h1 = h0; h1 < a.Hkv; h1 += kUnits) {              // (the same for all lanes)
+    const int h = h1 + lane / kLanes;
+    uint4 x[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+    if (h < a.Hkv) {                                         // (read for the last time: what L2 keeps is the store)
+      x[0] = __ldcs(reinterpret_cast<const uint4*>(pk + (long long)h * a.k_head));
+      x[1] = __ldcs(reinterpret_cast<const uint4*>(pv + (long long)h * a.k_head));
     }
+    uint32_t top[2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h1 + u * kUnits + lane / kLanes;
-      const uint4 x[2] = {k[u], v[u]};
-      uint32_t top[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        constexpr uint32_t kNoSign = 0x7fff7fffu;
-        top[t] = __vmaxu2(__vmaxu2(x[t].x & kNoSign, x[t].y & kNoSign), __vmaxu2(x[t].z & kNoSign, x[t].w & kNoSign));
-      }
-      uint32_t both = __vmaxu2(__byte_perm(top[0], top[1], 0x5410), __byte_perm(top[0], top[1], 0x7632));      // keys below, values above
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
-      if (!stored || h >= a.Hkv) continue;
-      const int e[2] = {store_exponent<STORE>(both << 16), store_exponent<STORE>(both & 0xffff0000u)};
-      const long long off = at + (long long)h * a.head_stride;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float f[8];
-        unpack_8(make_uint2(x[t].x, x[t].y), make_uint2(x[t].z, x[t].w), f);
-        const float inv = __uint_as_float((uint32_t)(127 - e[t]) << 23);
-        uint2 b = make_uint2(store_bytes<STORE>(f, inv), store_bytes<STORE>(f + 4, inv));
-        if (e[t] == kExpNone) b = make_uint2(0u, 0u);
-        *reinterpret_cast<uint2*>((t == 0 ? a.store_k : a.store_v) + off) = b;
-      }
-      if (gl < 2) (gl == 0 ? a.exp_k : a.exp_v)[exp_at + (h << a.block_shift)] = (int8_t)(gl == 0 ? e[0] : e[1]);
+    for (int t = 0; t < 2; ++t) {
+      constexpr uint32_t kNoSign = 0x7fff7fffu;
+      top[t] = __vmaxu2(__vmaxu2(x[t].x & kNoSign, x[t].y & kNoSign), __vmaxu2(x[t].z & kNoSign, x[t].w & kNoSign));
     }
+    uint32_t both = __vmaxu2(__byte_perm(top[0], top[1], 0x5410), __byte_perm(top[0], top[1], 0x7632));      // keys below, values above
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+    if (!stored || h >= a.Hkv) continue;
+    const int e[2] = {store_exponent<STORE>(both << 16), store_exponent<STORE>(both & 0xffff0000u)};
+    const long long off = at + (long long)h * a.head_stride;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float f[8];
+      unpack_8(make_uint2(x[t].x, x[t].y), make_uint2(x[t].z, x[t].w), f);
+      const float inv = __uint_as_float((uint32_t)(127 - e[t]) << 23);
+      uint2 b = make_uint2(store_bytes<STORE>(f, inv), store_bytes<STORE>(f + 4, inv));
+      if (e[t] == kExpNone) b = make_uint2(0u, 0u);
+      *reinterpret_cast<uint2*>((t == 0 ? a.store_k : a.store_v) + off) = b;
+    }
+    if (gl < 2) (gl == 0 ? a.exp_k : a.exp_v)[exp_at + (h << a.block_shift)] = (int8_t)(gl == 0 ? e[0] : e[1]);
   }
 }
 
