@@ -264,12 +264,12 @@ __device__ __forceinline__ void scaled_8(const uint32_t* w, float scale, float* 
   }
 }
 
-// Rows of the store as bf16, the keys turned: units are the key heads, then the value heads of a row.
+// Rows of the store as bf16, the keys turned.  A key head and its value head lie alike, in the store and in the rows: one address for both.
 template <int D, bool HALF, int TYPE, int ROWS>
 __global__ void __launch_bounds__(kTurnThreads, 4)
 read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kHalf = D / 2;
-  constexpr int kWarps = kTurnThreads / 32 / ROWS, kUnits = kWarps * kPerWarp, U = 2 * kTurnAhead;
+  constexpr int kWarps = kTurnThreads / 32 / ROWS, kUnits = kWarps * kPerWarp, U = kTurnAhead;
   __shared__ __align__(16) float cos_s[ROWS][kHalf], sin_s[ROWS][kHalf];
   const int tid = threadIdx.x, lane = tid & 31, gl = lane % kLanes, rr = (tid >> 5) / kWarps;
   const int unit0 = ((tid >> 5) % kWarps) * kPerWarp + lane / kLanes;
@@ -281,34 +281,33 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   griddep_wait();
   const int slot = row < a.n_rows ? a.slots[row] : -1;
   const bool stored = slot >= 0 && (slot >> a.block_shift) < a.n_blocks;
-  const int total = stored ? 2 * a.Hkv : 0;
+  const int heads = stored ? a.Hkv : 0;
   const int block = stored ? slot >> a.block_shift : 0, token = stored ? slot & ((1 << a.block_shift) - 1) : 0;
-  const long long at = block * a.block_stride + token * a.token_stride, exp_at = (((long long)block * a.Hkv) << a.block_shift) + token;
+  const long long at = block * a.block_stride + token * a.token_stride + dlo, exp_at = (((long long)block * a.Hkv) << a.block_shift) + token;
   if (!stored && slot != -1 && unit0 == 0 && gl == 0) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ROWS, (int)row, slot);
-  const uint8_t *pk = a.store_k + at + dlo, *pv = a.store_v + at - (long long)a.Hkv * a.head_stride + dlo;      // (value heads behind the key heads)
-  const int8_t *ek = a.exp_k + exp_at, *ev = a.exp_v + exp_at - (a.Hkv << a.block_shift);
   const int dd = dhi - dlo;
-  auto load = [&](int u, uint32_t& w0, uint32_t& w1, int& e) {
-    w0 = w1 = 0u; e = 0;
-    if (u >= total) return;
-    const uint8_t* p = (u < a.Hkv ? pk : pv) + (long long)u * a.head_stride;
-    if constexpr (HALF) {
-      w0 = *reinterpret_cast<const uint32_t*>(p);
-      w1 = *reinterpret_cast<const uint32_t*>(p + dd);
-    } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(p);
-      w0 = w.x; w1 = w.y;
-    }
-    e = (u < a.Hkv ? ek : ev)[u << a.block_shift];
-  };
-  uint32_t w0[U], w1[U];
-  int e[U];
+  uint32_t w[U][2][2];
+  int e[U][2];
+  auto load = [&](int u, int h) {
+    if (h >= heads) return;
+    const long long off = at + (long long)h * a.head_stride, eo = exp_at + (h << a.block_shift);
 #pragma unroll
-  for (int u = 0; u < U; ++u) load(unit0 + u * kUnits, w0[u], w1[u], e[u]);
-  if (a.part > 0) {
-    make_angles<ROWS>(a.positions, a.freq, a.part / 2, a.amplitude, row0, a.n_rows, cos_s, sin_s);
-    __syncthreads();
-  }
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t* p = (t == 0 ? a.store_k : a.store_v) + off;
+      if constexpr (HALF) {
+        w[u][t][0] = *reinterpret_cast<const uint32_t*>(p);
+        w[u][t][1] = *reinterpret_cast<const uint32_t*>(p + dd);
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        w[u][t][0] = x.x; w[u][t][1] = x.y;
+      }
+      e[u][t] = (t == 0 ? a.exp_k : a.exp_v)[eo];
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) load(u, unit0 + u * kUnits);
+  make_angles<ROWS>(a.positions, a.freq, a.part / 2, a.amplitude, row0, a.n_rows, cos_s, sin_s);
+  __syncthreads();
   float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f}, ns[4];
   if (turned) {
     *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(&cos_s[rr][gl * 4]);
@@ -316,24 +315,26 @@ read_rows_kernel(const TurnArgs a, DeviceStatus* st) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) ns[i] = -s[i];
-  const long long k_at = row * a.k_token + dlo;
-  uint16_t *ok = a.k_out + k_at, *ov = a.v_out + k_at - (long long)a.Hkv * a.k_head;
-  for (int u0 = unit0; u0 < total; u0 += U * kUnits) {
+  uint16_t *ok = a.k_out + row * a.k_token + dlo, *ov = a.v_out + row * a.k_token + dlo;
+  for (int h0 = unit0; h0 < heads; h0 += U * kUnits) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int h = u0 + u * kUnits;
-      if (h >= total) break;
-      float f[8];
-      const uint32_t w[2] = {w0[u], w1[u]};
-      scaled_8<TYPE>(w, exp_scale(e[u]), f);
-      if (turned && h < a.Hkv) turn_8<HALF>(f, c, s, ns);
-      uint16_t* out = (h < a.Hkv ? ok : ov) + (long long)h * a.k_head;
-      const uint2 r0 = pack_bf16(f), r1 = pack_bf16(f + 4);
-      if constexpr (HALF) {
-        *reinterpret_cast<uint2*>(out) = r0;
-        *reinterpret_cast<uint2*>(out + dd) = r1;
-      } else *reinterpret_cast<uint4*>(out) = make_uint4(r0.x, r0.y, r1.x, r1.y);
-      load(h + U * kUnits, w0[u], w1[u], e[u]);
+      const int h = h0 + u * kUnits;
+      if (h >= heads) break;
+      const long long off = (long long)h * a.k_head;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float f[8];
+        scaled_8<TYPE>(w[u][t], exp_scale(e[u][t]), f);
+        if (t == 0 && turned) turn_8<HALF>(f, c, s, ns);
+        uint16_t* out = (t == 0 ? ok : ov) + off;
+        const uint2 r0 = pack_bf16(f), r1 = pack_bf16(f + 4);
+        if constexpr (HALF) {
+          *reinterpret_cast<uint2*>(out) = r0;
+          *reinterpret_cast<uint2*>(out + dd) = r1;
+        } else *reinterpret_cast<uint4*>(out) = make_uint4(r0.x, r0.y, r1.x, r1.y);
+      }
+      load(u, h + U * kUnits);
     }
   }
 }
