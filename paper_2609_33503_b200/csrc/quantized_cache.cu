@@ -59,15 +59,23 @@ __device__ __forceinline__ void lane_dims(int gl, int part, int* lo, int* hi) {
 // Eight elements by the four angles (cosine c, sine s, -s) of their pairs: element i and i + 4, or 2 i and 2 i + 1.
 template <bool HALF>
 __device__ __forceinline__ void turn_8(float* f, const float* c, const float* s, const float* ns) {
+  if constexpr (HALF) {
 #pragma unroll
-  for (int i = 0; i < 4; i += 2) {
-    float &a0 = f[HALF ? i : 2 * i], &b0 = f[HALF ? i + 4 : 2 * i + 1], &a1 = f[HALF ? i + 1 : 2 * i + 2], &b1 = f[HALF ? i + 5 : 2 * i + 3];
-    float x0, x1, y0, y1;
-    ptx::mul2(x0, x1, b0, b1, ns[i], ns[i + 1]);
-    ptx::fma2(x0, x1, a0, a1, c[i], c[i + 1], x0, x1);
-    ptx::mul2(y0, y1, a0, a1, s[i], s[i + 1]);
-    ptx::fma2(y0, y1, b0, b1, c[i], c[i + 1], y0, y1);
-    a0 = x0; a1 = x1; b0 = y0; b1 = y1;
+    for (int i = 0; i < 4; i += 2) {
+      float x0, x1, y0, y1;
+      ptx::mul2(x0, x1, f[i + 4], f[i + 5], ns[i], ns[i + 1]);
+      ptx::fma2(x0, x1, f[i], f[i + 1], c[i], c[i + 1], x0, x1);
+      ptx::mul2(y0, y1, f[i], f[i + 1], s[i], s[i + 1]);
+      ptx::fma2(y0, y1, f[i + 4], f[i + 5], c[i], c[i + 1], y0, y1);
+      f[i] = x0; f[i + 1] = x1; f[i + 4] = y0; f[i + 5] = y1;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = f[2 * i], b = f[2 * i + 1];
+      f[2 * i] = fmaf(a, c[i], b * ns[i]);
+      f[2 * i + 1] = fmaf(b, c[i], a * s[i]);
+    }
   }
 }
 
