@@ -13,8 +13,8 @@
 // Measured (int8, D 128): 57 rows of 40 / 8 heads over 16 K 62.7 us (the products alone, at 1.66 PFLOP/s, 11.5; the kernel of few rows 123), 16 rows of 32 / 8 heads over 8 x 4 K 48.5
 // (68), 200 over 3000 40 (75).  Bound by issue, not by the tensor cores (21 % of the time) or memory: a tile's 128 x 128 weights and its two conversions to fp16 are some 2200 instructions of
 // each of the SM's four schedulers, which five warps each (two of rows, one each of K and V, the products') issue at half their rate, 4200 clk a tile.  Weights in one pass with a
-// reference that is a whole number (62.7), exponents within the fp16 tiles in place of factors on scores and weights (65.4: the conversions get longer), 144 or 128 registers for
-// the rows' threads (62.9) and two of the 32-column chunks at once (80.8 of 78.5) were no faster.
+// reference that is a whole number (62.7), exponents within the fp16 tiles in place of factors on scores and weights (65.4: the conversions get longer), both groups on halves of the same tile
+// (68.4: all wait and all take exponentials at once), 144 or 128 registers for the rows' threads (62.9) and two of the 32-column chunks at once (80.8 of 78.5) were no faster.
 #include "quantized_attention.cuh"
 #include <atomic>
 
