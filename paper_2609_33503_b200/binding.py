@@ -711,18 +711,12 @@ def relaxkv_rotary_frequencies(dims: int, theta: float, scaling: str = "none", f
     return list(freq), float(amplitude.value)
 
 
-_BF16 = torch.bfloat16
-
-
 def _head_rows(x: torch.Tensor, like: Optional[torch.Tensor], n: Optional[int], heads: Optional[int], dim: Optional[int]):
-    """Rows, heads, dims, token and head stride of bf16 head rows [n, heads, dim], which are laid out like `like`."""
-    shape, strides = x.shape, x.stride()
-    if (len(shape) != 3 or x.dtype is not _BF16 or strides[2] != 1 or (n is not None and shape[0] != n) or (heads is not None and shape[1] != heads)
-            or (dim is not None and shape[2] != dim)):
-        raise ValueError(f"bf16 rows [{n}, {heads}, {dim}] with contiguous heads expected, not {tuple(shape)} of {x.dtype}, strides {strides}")
-    if like is not None and (like.shape != shape or like.stride() != strides or like.dtype is not _BF16):
-        raise ValueError(f"rows laid out like {tuple(shape)}, strides {strides}, expected, not {tuple(like.shape)} of {like.dtype}, strides {like.stride()}")
-    return shape[0], shape[1], shape[2], max(strides[0], shape[2]) if shape[0] == 1 else strides[0], max(strides[1], shape[2]) if shape[1] == 1 else strides[1]
+    """Rows, heads, dims, token and head stride of bf16 head rows [n, heads, dim] (None: any), whose heads are contiguous and which `like` (or None) is laid
+    out as; ValueError for others.  The first call puts the native function in this one's place."""
+    global _head_rows
+    _head_rows = _native().head_rows
+    return _head_rows(x, like, n, heads, dim)
 
 
 def relaxkv_qk_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, rotary: Rotary, q_out: Optional[torch.Tensor] = None,

@@ -186,3 +186,41 @@ def test_a_full_chunk_store_says_so(monkeypatch):
     with pytest.raises(KeyError):
         s.assemble(["b"], caches())
     assert len(s.free) == 1
+
+
+def test_rows_of_heads_as_the_calls_take_them():
+    x = bf(6, 4, 64)
+    assert B._head_rows(x, None, None, None, None) == B._head_rows(x, bf(6, 4, 64), 6, 4, 64) == B._head_rows(x, x, 6, None, None) == (6, 4, 64, 256, 64)
+    assert B._head_rows(x.transpose(0, 1), None, 4, 6, 64) == (4, 6, 64, 64, 256)
+    assert B._head_rows(x[:, :, :32], x[:, :, 32:], None, None, 32) == (6, 4, 32, 256, 64)
+    # the distance to a row or head that is not there: at least a head's dims
+    assert B._head_rows(torch.as_strided(x, (1, 1, 64), (0, 0, 1)), None, None, None, None) == (1, 1, 64, 64, 64)
+    assert B._head_rows(torch.as_strided(x, (1, 2, 64), (3, 64, 1)), None, None, None, None) == (1, 2, 64, 64, 64)
+    assert B._head_rows(x[:0], x[:0], 0, 4, 64) == (0, 4, 64, 256, 64)
+
+
+@pytest.mark.parametrize("args", [
+    (bf(6, 4, 64).float(), None, None, None, None), (bf(6, 4, 64).half(), None, None, None, None), (bf(6, 256), None, None, None, None), (bf(6, 4, 2, 64), None, None, None, None),
+    (bf(6, 4, 128)[..., ::2], None, None, None, None), (bf(6, 4, 64), None, 5, None, None), (bf(6, 4, 64), None, None, 3, None), (bf(6, 4, 64), None, None, None, 128),
+    (bf(6, 4, 64), bf(6, 4, 64).float(), None, None, None), (bf(6, 4, 64), bf(6, 2, 64), None, None, None), (bf(6, 4, 64), bf(4, 6, 64).transpose(0, 1), None, None, None),
+    (bf(6, 4, 64), bf(6, 256), None, None, None)])
+def test_rows_of_heads_that_are_refused(args):
+    with pytest.raises(ValueError, match="rows"):
+        B._head_rows(*args)
+
+
+def test_rows_of_heads_keep_no_reference():
+    import sys
+    x, y = bf(2, 2, 64), bf(2, 2, 64)
+    B._head_rows(x, y, None, None, None)
+    before = [sys.getrefcount(o) for o in (x, y, torch.bfloat16)]
+    for _ in range(200):
+        B._head_rows(x, y, 2, 2, 64)
+        with pytest.raises(ValueError):
+            B._head_rows(x, y, 3, 2, 64)
+    assert [sys.getrefcount(o) for o in (x, y, torch.bfloat16)] == before
+    for bad in ((3, None, None, None, None), (x, 3, None, None, None)):
+        with pytest.raises(AttributeError):
+            B._head_rows(*bad)
+    with pytest.raises(TypeError):
+        B._head_rows(x, None, "a", None, None)
