@@ -130,6 +130,11 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     const long long row = unit / a.Hkv;
     rank = (int)blockIdx.x - unit * a.split;
     g.hd = unit - (int)row * a.Hkv;
+    // (of as many sequences as rows, each row is mostly the only one of its sequence: what is known then comes with its number, not behind it; 64 x 300 tokens 18.8 us in
+    // place of 20.5.  The same for any number of rows, all alike, gained nothing: 19.6, and 25.9 of 25.6 for six rows of 43 short sequences.)
+    const bool one_each = a.n_rows == a.n_seq;
+    int first1 = 0, end1 = 0, len1 = 0;
+    if (one_each) { first1 = a.row_cu[row]; end1 = a.row_cu[row + 1]; len1 = a.row_len[row]; }
     g.seq = a.row_seq[row];
     const int before = rpt > 1 && row > 0 ? a.row_seq[row - 1] : -1;
     const bool tell = tid == 0 && g.hd == 0 && rank == 0;
@@ -143,7 +148,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       const int first = a.row_cu[g.seq];
       if (first >= 0 && row > first && (row - first) % rpt != 0) return;
     }
-    g.s = rows_of(a, g.seq, -1, 0, tell, st);
+    g.s = one_each && g.seq == row && first1 == row && end1 == row + 1 ? rows_with(a, g.seq, first1, end1, len1, tell, st) : rows_of(a, g.seq, -1, 0, tell, st);
     if (g.s.n == 0) return;
     if (row < g.s.first || row >= g.s.first + g.s.n) {
       if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);

@@ -48,6 +48,16 @@ constexpr float kNothing = -3.4028234663852886e38f;
 
 // Rows and tokens of a sequence; rows 0: none to work on.
 struct SeqRows { int first, n, len; };
+// Rows first to end - 1 with the last one's length.
+__device__ __forceinline__ SeqRows rows_with(const QuantAttnArgs& a, int seq, int first, int end, int len, bool tell, DeviceStatus* st) {
+  SeqRows s = {first, 0, len};
+  if (len < 0 || len > a.max_len || len > ((long long)a.table_width << a.block_shift)) {
+    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, len, seq);
+    return s;
+  }
+  s.n = end - first;
+  return s;
+}
 // guess_len: row_len[guess], read before it is known to be the last row's.
 __device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, int guess, int guess_len, bool tell, DeviceStatus* st) {
   SeqRows s = {a.row_cu[seq], 0, 0};
@@ -57,13 +67,7 @@ __device__ __forceinline__ SeqRows rows_of(const QuantAttnArgs& a, int seq, int 
     return s;
   }
   if (end == s.first) return s;
-  s.len = end - 1 == guess ? guess_len : a.row_len[end - 1];
-  if (s.len < 0 || s.len > a.max_len || s.len > ((long long)a.table_width << a.block_shift)) {
-    if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, s.len, seq);
-    return s;
-  }
-  s.n = end - s.first;
-  return s;
+  return rows_with(a, seq, s.first, end, end - 1 == guess ? guess_len : a.row_len[end - 1], tell, st);
 }
 // Tokens that a row of a sequence sees; -1: the row is left alone.
 __device__ __forceinline__ int row_tokens(const QuantAttnArgs& a, int seq, const SeqRows& s, long long row, bool tell, DeviceStatus* st) {
