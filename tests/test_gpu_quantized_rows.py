@@ -36,6 +36,18 @@ def test_many_rows(lens, new, H, Hkv, D, block, layout, kind):
     assert status() == B().OK
 
 
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,new,H,Hkv,D", [
+    ([300, 250], [3, 3], 16, 2, 128), ([2500, 1100], [4, 4], 20, 4, 128), ([1500, 40], [6, 5], 8, 2, 64), ([130], [24], 2, 2, 64), ([1300, 1200], [8, 7], 8, 2, 128), ([64, 31], [6, 6], 10, 2, 64),
+    ([1030], [2], 16, 1, 128)])
+def test_rows_of_three_and_four_column_tiles(lens, new, H, Hkv, D, kind):
+    """17 to 32 columns: short sequences a block to each row tile and head, long ones in shares; what the largest calls of few rows take."""
+    store = make_store(sum(-(-t // 16) for t in lens) + 2, 16, Hkv, D, kind, "head" if D == 64 else "token", seed=sum(lens))
+    r = attend(store, lens, new, H, 16, seed=3, gaps=len(lens) > 1)
+    check(r, D)
+    assert status() == B().OK
+
+
 def test_rows_that_see_nothing_and_sequences_without_tokens():
     """Rows before a sequence's first tokens (zeros and -inf), a sequence of rows without any token, one without rows."""
     store = make_store(20, 16, 2, 64, "int8", seed=4)
