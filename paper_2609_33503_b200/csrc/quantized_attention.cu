@@ -737,7 +737,7 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // More columns than one block holds: 128 at a time on the tensor cores, which takes less time than tokens brought several times (57 rows of 4 heads a group over 8 x 900
   // tokens 46 against 78 us, 20 over 16 x 300 19 against 40, 16 over 8 x 4 K 51 against 68, 30 over 3000 23.4 against 24.5; of up to 32 columns it takes more: 6 rows over 16 x 3000
-  // tokens 69 against 56 us, over 8 K 24.7 against 22.1).
+  // tokens 69 against 49.5 us, over 8 K 24.7 against 20.7).
   if (cols > kQaColsMost) {
     a.rows_per_tile = kQrRows / a.G;
     return cuda_ok(launch_quantized_rows(a, head_dim, store->type, sms, st, s));
