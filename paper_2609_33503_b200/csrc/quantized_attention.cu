@@ -125,42 +125,50 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   // ---- this block's share ----
   QaWalk g;
   int rank = 0;                                                       // of this block in its cluster
-  if constexpr (WHOLE) {                                              // a block, or a cluster, per row and KV head: the first of a tile's rows takes them all
+  // WHOLE: a block, or a cluster, per rows_at_once rows and KV head; the first of a row tile's rows takes them all.
+  long long row = 0, row_end = 0;
+  auto find = [&]() -> bool {                                         // the next such row
+    for (bool once = true; NT > 1 ? row < row_end : once; ++row, once = false) {      // (NT 1: one row)
+      // (of as many sequences as rows, each row is mostly the only one of its sequence: what is known then comes with its number, not behind it; 64 x 300 tokens 18.8 us in
+      // place of 20.5.  The same for any number of rows, all alike, gained nothing: 19.6, and 25.9 of 25.6 for six rows of 43 short sequences.)
+      const bool one_each = a.n_rows == a.n_seq;
+      int first1 = 0, end1 = 0, len1 = 0;
+      if (one_each) { first1 = a.row_cu[row]; end1 = a.row_cu[row + 1]; len1 = a.row_len[row]; }
+      g.seq = a.row_seq[row];
+      const bool tell = tid == 0 && g.hd == 0 && rank == 0;
+      if (row >= a.row_cu[a.n_seq] || g.seq == -1) continue;
+      if (g.seq < 0 || g.seq >= a.n_seq) {
+        if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
+        continue;
+      }
+      g.s = one_each && g.seq == row && first1 == row && end1 == row + 1 ? rows_with(a, g.seq, first1, end1, len1, tell, st) : rows_of(a, g.seq, -1, 0, tell, st);
+      if (g.s.n == 0) continue;
+      if (row < g.s.first || row >= g.s.first + g.s.n) {
+        if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
+        continue;
+      }
+      g.tile = (int)(row - g.s.first) / rpt;
+      const long long first = g.s.first + (long long)g.tile * rpt;
+      bool another = false;
+      for (long long r = first; r < row && !another; ++r) another = a.row_seq[r] == g.seq;
+      if (another) continue;
+      g.tiles = QaWalk::tiles_of(g.s.len);
+      const int each = (g.tiles + a.split - 1) / a.split;
+      g.j0 = min(g.tiles, rank * each);
+      g.j1 = min(g.tiles, g.j0 + each);
+      row = min(first + rpt, (long long)g.s.first + g.s.n);           // (what is between is of this tile, or reported with it)
+      return true;
+    }
+    return false;
+  };
+  if constexpr (WHOLE) {
     const int unit = (int)blockIdx.x / a.split;
-    const long long row = unit / a.Hkv;
+    const long long rows = unit / a.Hkv;
     rank = (int)blockIdx.x - unit * a.split;
-    g.hd = unit - (int)row * a.Hkv;
-    // (of as many sequences as rows, each row is mostly the only one of its sequence: what is known then comes with its number, not behind it; 64 x 300 tokens 18.8 us in
-    // place of 20.5.  The same for any number of rows, all alike, gained nothing: 19.6, and 25.9 of 25.6 for six rows of 43 short sequences.)
-    const bool one_each = a.n_rows == a.n_seq;
-    int first1 = 0, end1 = 0, len1 = 0;
-    if (one_each) { first1 = a.row_cu[row]; end1 = a.row_cu[row + 1]; len1 = a.row_len[row]; }
-    g.seq = a.row_seq[row];
-    const int before = rpt > 1 && row > 0 ? a.row_seq[row - 1] : -1;
-    const bool tell = tid == 0 && g.hd == 0 && rank == 0;
-    bool mine = row < a.row_cu[a.n_seq] && g.seq != -1;
-    if (mine && (g.seq < 0 || g.seq >= a.n_seq)) {
-      if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
-      mine = false;
-    }
-    if (!mine) return;
-    if (before == g.seq) {                                            // (what most blocks see first, and enough for them)
-      const int first = a.row_cu[g.seq];
-      if (first >= 0 && row > first && (row - first) % rpt != 0) return;
-    }
-    g.s = one_each && g.seq == row && first1 == row && end1 == row + 1 ? rows_with(a, g.seq, first1, end1, len1, tell, st) : rows_of(a, g.seq, -1, 0, tell, st);
-    if (g.s.n == 0) return;
-    if (row < g.s.first || row >= g.s.first + g.s.n) {
-      if (tell) report(st, RELAXKV_ERR_BAD_INDEX, KID_QUANTIZED_ATTN, g.seq, (int)row);
-      return;                                                         // (with it the other blocks of its cluster)
-    }
-    g.tile = (int)(row - g.s.first) / rpt;
-    for (long long r = g.s.first + (long long)g.tile * rpt; r < row; ++r)
-      if (a.row_seq[r] == g.seq) return;
-    g.tiles = QaWalk::tiles_of(g.s.len);
-    const int each = (g.tiles + a.split - 1) / a.split;
-    g.j0 = min(g.tiles, rank * each);
-    g.j1 = min(g.tiles, g.j0 + each);
+    g.hd = unit - (int)rows * a.Hkv;
+    row = rows * a.rows_at_once;
+    row_end = min(row + a.rows_at_once, a.n_rows);
+    if (!find()) return;                                              // (with it the other blocks of its cluster)
   } else {
     if (!g.begin(a, walk_s, st)) {                                    // (or it ends before the first tile of its only task)
       if (tid == 0) a.chain[blockIdx.x].c0 = -1;
@@ -507,6 +515,8 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         left.c0 = -1;
         if (g.j1 < g.tiles) g.blocks_of(&left.c0, &left.c1);
         more = g.next(a, st);
+      } else if constexpr (NT > 1) {
+        if (a.split == 1) more = find();
       }
       n_mine = more ? tiles_mine() : 0;
       stage = 0;
@@ -676,7 +686,7 @@ static cudaError_t launch_attend_n(int type, bool whole, const QuantAttnArgs& a,
     auto kern = quantized_join_kernel<D, NT>;
     return launch_chained(kern, dim3((unsigned)blocks), kQjWarps * 32, 0, stream, a);
   }
-  const long long blocks = a.n_rows * a.Hkv * a.split;
+  const long long blocks = (a.n_rows + a.rows_at_once - 1) / a.rows_at_once * a.Hkv * a.split;
   return int8 ? launch_attend<D, RELAXKV_INT8, NT, true>(a, blocks, st, stream) : launch_attend<D, RELAXKV_E4M3, NT, true>(a, blocks, st, stream);
 }
 template <int D>
@@ -733,6 +743,9 @@ extern "C" relaxkv_status relaxkv_quantized_attention(
   const long long items = r->n_rows * a.Hkv, tiles = (r->max_len + kQaTile - 1LL) / kQaTile;
   a.split = 1;
   while (a.split < 8 && 2 * a.split * items <= 2 * sms && 2 * a.split * kQaWarps <= tiles) a.split *= 2;
+  // Where sequences have as many rows each, the next row tile begins as many further on: a block for each row would mostly be one that has nothing to do (six rows of 29 sequences of 12
+  // tokens 12.0 us, so 18.6; three of 13 of 600 13.0, 15.3).  One column tile: little difference, and such blocks leave soon (two rows of 64 of 500 tokens 25.8, so 25.2).
+  a.rows_at_once = nt > 1 && a.split == 1 ? (int)std::max(1LL, (long long)r->n_rows / r->n_seq) : 1;
   const bool whole = tiles <= (a.split > 1 ? 16LL * a.split : 32) && items * a.split <= 0x7fffffffLL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // More columns than one block holds: 128 at a time on the tensor cores, which takes less time than tokens brought several times (57 rows of 4 heads a group over 8 x 900

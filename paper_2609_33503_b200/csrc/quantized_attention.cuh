@@ -24,6 +24,7 @@ struct QuantAttnArgs {
   int table_width, n_seq, n_blocks, block_shift, max_len;
   int H, Hkv, G, rows_per_tile;
   int split;                             // blocks of a cluster that share a row tile and KV head
+  int rows_at_once;                      // rows that a block, or cluster, looks through for the first ones of row tiles
   float scale_log2;
 };
 
