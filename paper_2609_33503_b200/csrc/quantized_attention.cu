@@ -15,8 +15,8 @@
 // task's first copies are on their way while a task's results are added up.  Calls of few short sequences give a cluster of up to eight blocks to each row tile and KV head, which
 // joins within itself: one launch.  More than 32 columns to a sequence go to the kernel of many rows (quantized_rows_sm100.cu).
 //
-// Measured (int8, D 128, one row a sequence, L2 flushed): one sequence of 128 K of 32 / 8 heads 62 us (4.4 TB/s; 55 us with the heads' tokens side by side), 64 of up to 4 K of 40 / 8
-// heads 61.6 (4.75 TB/s), 16 of up to 8 K 41, three rows of eight sequences of 8 K to 64 K 105.5 (4.9 TB/s), 1 K of 4 / 1 heads 7.1.  Between its first and last copies a call is at
+// Measured (int8, D 128, one row a sequence, L2 flushed): one sequence of 128 K of 32 / 8 heads 61 us (4.4 TB/s; 55 us with the heads' tokens side by side), 64 of up to 4 K of 40 / 8
+// heads 61.6 (4.75 TB/s), 16 of up to 8 K 40, three rows of eight sequences of 8 K to 64 K 106 (4.9 TB/s), 1 K of 4 / 1 heads 6.6.  Between its first and last copies a call is at
 // 5.4 to 6.5 TB/s of the 6.57 that a plain copy makes; its start takes 3.3 us (arguments, lengths and block numbers, one read behind the other), its end some 12 (blocks that had more of
 // the late copies, the four warps' results, the join).
 #include "quantized_attention.cuh"
