@@ -587,7 +587,8 @@ typedef enum {
 
 /* The 8-bit store of one layer.  Token t of block x of KV head g: values at k + x * block_stride + t * token_stride + g * head_stride (bytes = elements;
  * head_dim of them side by side), same for V, strides multiples of 16, that of heads below 2^31; exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V.
- * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN; others are -100 to 127.  All pointers 16-byte aligned. */
+ * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN; others are -100 to 127.
+ * No value byte is a NaN of e4m3 (relaxkv_append_quantized writes none).  All pointers 16-byte aligned. */
 typedef struct {
   void* k;
   void* v;
