@@ -198,3 +198,31 @@ def test_rows_of_blocks_far_into_a_store():
     back = [torch.empty_like(k), torch.empty_like(v)]
     B().relaxkv_read_quantized(store, slots, *back)
     assert torch.equal(back[0], v) and torch.equal(back[1], k) and status() == B().OK
+
+
+def test_calls_at_once_on_two_streams():
+    """Many rows on one stream, few rows, an append and a matrix product on another, each with its own workspace: every call gives what it gives by itself."""
+    store, other = make_store(300, 16, 4, 128, "int8", seed=20), make_store(300, 16, 4, 128, "e4m3", seed=21)
+    many = attend(store, [2000, 900], [70, 90], 16, 16, seed=22)
+    few = attend(other, [1500, 300, 40], [3, 2, 1], 16, 16, seed=23)
+    check_rows(many, store, 128, 2000)
+    check(few, 128)
+    w, x, y = rnd(1024, 512, seed=24, scale=0.05), rnd(300, 512, seed=25), torch.empty(300, 1024, dtype=torch.bfloat16, device="cuda")
+    B().relaxkv_linear(x, w, y)
+    spare = B().QuantizedStore.empty(4, 16, 4, 128, device="cuda")
+    k, v = rnd(50, 4, 128, seed=26), rnd(50, 4, 128, seed=27)
+    B().relaxkv_append_quantized(spare, k, v, i32(range(50)))
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (many["out"], many["lse"], few["out"], few["lse"], y, spare.k, spare.k_exp)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(50):
+        many["run"]()
+        with torch.cuda.stream(side):
+            few["run"]()
+            B().relaxkv_linear(x, w, y)
+            B().relaxkv_append_quantized(spare, k, v, i32(range(50)))
+    torch.cuda.synchronize()
+    for a, b in zip((many["out"], many["lse"], few["out"], few["lse"], y, spare.k, spare.k_exp), want):
+        assert torch.equal(a, b)
+    assert status() == B().OK
