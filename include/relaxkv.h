@@ -639,7 +639,8 @@ relaxkv_status relaxkv_qk_norm_rotate(
  * Append of rows to the 8-bit store: row r of K (normed and rotated as above where weights and a rotary are given, NULL: as it is) and of V goes to slot
  * slots[r] = block * block_size + token; q_out = rotated norm of q as above (q NULL: none).  For each row and KV head, with y in fp32 before any rounding and M = 127 or 448:
  *   exponent = the smallest e >= -100 with max |y| <= M 2^e (-100 where all are 0);  value = y 2^-e to the nearest, ties to even
- * (an infinite or NaN element makes the exponent -128 and the values 0).  What relaxkv_read_quantized returns without a rotation stands for the same values when it is appended again.
+ * (an infinite or NaN element makes the exponent -128 and the values 0).  What relaxkv_read_quantized returns without a rotation stands for the same values when it is appended again,
+ * but for heads with an element of almost 2^128 that the rounding to 8 bits has taken there: in bf16 that is infinite.
  * v is laid out like k.  Slots are distinct; a row with slot -1 is turned and not stored, another slot outside the store is reported and not stored.
  */
 relaxkv_status relaxkv_append_quantized(
@@ -648,7 +649,7 @@ relaxkv_status relaxkv_append_quantized(
     const void* w_k_norm, float eps, const int32_t* positions, const relaxkv_rotary* rotary, const int32_t* slots, relaxkv_stream stream);
 
 /* Rows of the 8-bit store in bf16: k_out, v_out row r (laid out as k above, v_out like k_out) = the token at slots[r], its keys turned by positions[r] positions more (positions
- * and rotary both NULL: as they are, which is exact).  A row with slot -1 is left alone, another slot outside the store is reported and left alone. */
+ * and rotary both NULL: as they are, which is exact; what stands for 2^128 or more is infinite).  A row with slot -1 is left alone, another slot outside the store is reported and left alone. */
 relaxkv_status relaxkv_read_quantized(
     const relaxkv_quantized_cache* store, const int32_t* slots, int64_t n_rows, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions,
     const relaxkv_rotary* rotary, void* k_out, void* v_out, int64_t token_stride, int64_t head_stride, relaxkv_stream stream);

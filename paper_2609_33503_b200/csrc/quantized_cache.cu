@@ -258,11 +258,16 @@ template <int TYPE>
 __device__ __forceinline__ void scaled_8(const uint32_t* w, float scale, float* f) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if constexpr (TYPE == RELAXKV_INT8) {                      // 2^23 + 128 + value, less 2^23 + 128, times the scale: products and sum are exact
+    if constexpr (TYPE == RELAXKV_INT8) {                      // 2^23 + 128 + value, less 2^23 + 128: exact, and only then the scale, which is up to 2^127
       const uint32_t b = w[i] ^ 0x80808080u;
-      const float less = -8388736.f * scale;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[4 * i + j] = fmaf(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7550 | j)), scale, less);
+      for (int j = 0; j < 4; j += 2) {
+        float* x = f + 4 * i + j;
+        x[0] = __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7550 | j));
+        x[1] = __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7550 | (j + 1)));
+        ptx::add2(x[0], x[1], -8388736.f, -8388736.f);
+        ptx::mul2(x[0], x[1], x[0], x[1], scale, scale);
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
