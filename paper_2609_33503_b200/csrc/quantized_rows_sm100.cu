@@ -138,7 +138,9 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       const bool exists = t_local < min(rpt, g.s.n - g.tile * rpt);
       const int seen = exists ? row_tokens(a, g.seq, g.s, row, x == 0 && in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
       // ---- Q: as fp16 times 2^-exponent, two dims to a word; each group brings half of them, and both know the largest ----
+      // A row that is no number meets the keys as zeros, so that what it does not see weighs nothing; its result becomes NaN at the end, where it has seen a token.
       float qs;
+      bool finite;
       {
         uint32_t w[D / 4], top = 0;
         const uint4* q = reinterpret_cast<const uint4*>(a.q + (row * a.H + head) * D) + x * (D / 16);
@@ -153,7 +155,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         top_s[x][t] = top;
         if (!(ok = meet<2, 256>(ok))) break;
         top = max(top, top_s[x ^ 1][t]);
-        const bool finite = top < 0x7f80u;
+        finite = top < 0x7f80u;
         const int e = max((int)(top >> 7) - 127 - 14, -120);
         const float inv = __uint_as_float((uint32_t)(127 - (finite ? e : 0)) << 23);
 #pragma unroll
@@ -161,7 +163,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           const __half2 y = __floats2half2_rn(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xffff0000u) * inv);
           w[c] = finite ? *reinterpret_cast<const uint32_t*>(&y) : 0u;
         }
-        qs = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
+        qs = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : 1.f;
         if constexpr (D == 128) tmem_st32(lane_base + kQ + 32 * x, w); else tmem_st16(lane_base + kQ + 16 * x, w);
         tmem_wait_st();
         tc_fence_before();
@@ -313,9 +315,10 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         tc_fence_after();
         const float zz = sum_s[t] + sum_s[kQrRows + t];
         const bool none = zz == 0.f;                     // no token, or none of a logit above -inf (NaN stays NaN)
-        const float inv = none ? 0.f : one_over(zz * 2048.f), grow = __uint_as_float((uint32_t)(e_last + 127) << 23);
+        const float nan = __uint_as_float(0x7fc00000u);
+        const float inv = none ? 0.f : finite ? one_over(zz * 2048.f) : nan, grow = __uint_as_float((uint32_t)(e_last + 127) << 23);
         static_assert(kQrShift == 11.f, "2^11");
-        const float lse2 = none ? -INFINITY : m_end + log2_of(zz);
+        const float lse2 = none ? -INFINITY : finite ? m_end + log2_of(zz) : nan;
 #pragma unroll 1
         for (int c = x * (D / 64); c < (x + 1) * (D / 64); ++c) {
           uint32_t o[32];

@@ -1,0 +1,45 @@
+"""Attention over the 8-bit store at the ends of its documented range: exponents, queries that are no numbers, tokens that a row does not see."""
+import numpy as np
+import pytest
+import torch
+
+from tests import quantized_oracle as orc
+from tests.test_gpu_quantized import B, attend, check, f64, i32, make_store, rnd, status, store_values, value_scale, workspace
+from tests.test_gpu_quantized_rows import check_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("lens,new", [([3, 0], [5, 2]), ([2000, 0], [2, 1]), ([100, 0, 700], [110, 60, 30]), ([4000, 0], [40, 40])])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_no_number_weighs_nothing_where_nothing_is_seen(lens, new, bad):
+    """Zeros and -inf for a row without tokens, whatever its query; NaN for one that sees a token; the others as they were."""
+    Hkv, D, block, H = 2, 64, 16, 8
+    store = make_store(sum(-(-t // block) for t in lens) + 2, block, Hkv, D, "int8", seed=1)
+    r = attend(store, lens, new, H, block, seed=3)
+    clean = r["out"].clone(), r["lse"].clone()
+    row_len = r["rows"]._keep[4]
+    hit = torch.zeros(r["n"], dtype=torch.bool, device="cuda")
+    hit[::2] = True
+    empty = row_len[:r["n"]] == 0
+    assert (hit & empty).any() and (hit & ~empty).any()
+    r["q"][:r["n"]][hit] = bad
+    r["out"].fill_(7)
+    r["lse"].fill_(7)
+    r["run"]()
+    out, lse = r["out"][:r["n"]], r["lse"][:, :r["n"]]
+    assert (out[empty] == 0).all() and (lse[:, empty] == -float("inf")).all()
+    assert torch.isnan(out[hit & ~empty]).all() and torch.isnan(lse[:, hit & ~empty]).all()
+    assert torch.equal(out[~hit], clean[0][:r["n"]][~hit]) and torch.equal(lse[:, ~hit], clean[1][:, :r["n"]][:, ~hit]) and status() == B().OK
+
+
+@pytest.mark.parametrize("T,n", [(90, 2), (90, 40), (300, 60)])
+def test_a_query_that_is_no_number_over_blocks_that_are_none(T, n):
+    """All of a sequence's blocks out of range: reported, and its rows see nothing."""
+    Hkv, D, block, H = 2, 64, 16, 8
+    store = make_store(20, block, Hkv, D, "int8", seed=1)
+    q = torch.full((n, H, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 7), torch.full((H, n), 7.0, device="cuda")
+    rows = B().ContinuationRows([0, 1], [n], T, i32([0, n]), i32([0] * n), i32([T - n + 1 + j for j in range(n)]), i32([[-1] * 19]))
+    B().relaxkv_quantized_attention(store, rows, q, out, workspace(H, Hkv, D), lse_out=lse)
+    assert status() == B().ERR_BAD_INDEX and (out == 0).all() and (lse == -float("inf")).all()
