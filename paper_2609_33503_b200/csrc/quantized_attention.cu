@@ -233,7 +233,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       float vexp[4], w[NT][2][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float ks = __uint_as_float(__byte_perm(ke, 0, 0x0444 | i << 12) >> 1);         // 2^(e + 1)
+        const float ks = __uint_as_float((__byte_perm(ke, 0, 0x0444 | i << 12) >> 1) - 0x800000u);      // 2^e (of a key that is none, or no number: replaced below)
         vexp[i] = __uint_as_float(__byte_perm(ve, 0x4b000000u, 0x7550 | i)) - 8388736.f;     // 2^23 + byte, less 2^23 + 128
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -435,8 +435,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
             if constexpr (kQInRegs) qf[c][nt] = h2;
             else q_s[c][nt][lane] = h2;
           }
-          // (half of it: the scale of a key is made with one more)
-          if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * (0.5f * a.scale_log2) : __uint_as_float(0x7fc00000u);
+          if (warp == 0 && tig == 0) qscale_s[col] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : __uint_as_float(0x7fc00000u);
         }
       }
       __syncthreads();

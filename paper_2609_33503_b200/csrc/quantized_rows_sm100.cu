@@ -24,6 +24,8 @@ using namespace ptx;
 
 constexpr int kQrTile = 128, kQrThreads = 640;           // tokens of a tile; warps 0-3 and 4-7: a row per thread, 8-11: K, 12-15: V, 16: products, three idle
 constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
+// Factors of keys are up to 2^90, what is above that of a tile's largest goes to the rows' scales: a product of Q and key values (2^31 at most) stays within fp32 before its row's scale.
+constexpr int kQrKeyMost = 90;
 constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
 using QrWalk = Walk<kQrTile, 4, 2, 128>;                 // a task's start and end take as long as four tiles (57 rows over 16 K: of two 68 us, of three to six 64)
 
@@ -83,7 +85,8 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   __shared__ QrWalk::Shared walk_s;
   __shared__ volatile uint32_t tmem_slot;
   __shared__ volatile int abort_s;
-  __shared__ int largest_s[2][4], e_s[8];                 // largest exponents: of each of the four warps' tokens; of the values up to the last eight tiles
+  __shared__ int largest_s[2][4], e_s[8];                 // largest exponents of the values: of each of the four warps' tokens; up to the last eight tiles
+  __shared__ int largest_k_s[2][4], over_s[4];            // of the keys: of each warp's tokens; by how much the last four tiles' are above kQrKeyMost
   __shared__ uint32_t top_s[2][kQrRows];                 // largest bits of a row's dims, by half
   __shared__ uint32_t gone_s[4][4], nan_s[4][4];          // tokens of the last four tiles whose blocks do not exist; whose values are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -139,7 +142,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       const int seen = exists ? row_tokens(a, g.seq, g.s, row, x == 0 && in_group == 0 && g.hd == 0 && g.j0 == 0, st) : -1;
       // ---- Q: as fp16 times 2^-exponent, two dims to a word; each group brings half of them, and both know the largest ----
       // A row that is no number meets the keys as zeros, so that what it does not see weighs nothing; its result becomes NaN at the end, where it has seen a token.
-      float qs;
+      int qe;                                            // exponent of the row's scale
       bool finite;
       {
         uint32_t w[D / 4], top = 0;
@@ -163,7 +166,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           const __half2 y = __floats2half2_rn(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xffff0000u) * inv);
           w[c] = finite ? *reinterpret_cast<const uint32_t*>(&y) : 0u;
         }
-        qs = finite ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : 1.f;
+        qe = finite && top != 0 ? e : 0;                 // (zeros are zeros by any scale)
         if constexpr (D == 128) tmem_st32(lane_base + kQ + 32 * x, w); else tmem_st16(lane_base + kQ + 16 * x, w);
         tmem_wait_st();
         tc_fence_before();
@@ -190,6 +193,8 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         const int limit = seen < 0 ? kQrTile : seen - j * kQrTile;      // (rows that are not written see all: nothing to hide costs half as much)
         const bool slow = __any_sync(0xffffffffu, limit < kQrTile || (gone_s[ring][0] | gone_s[ring][1] | gone_s[ring][2] | gone_s[ring][3]) != 0);
         const bool factors = slow && (nan_s[ring][0] | nan_s[ring][1] | nan_s[ring][2] | nan_s[ring][3]) != 0;
+        // (never 0: what is not seen stays -inf)
+        const float qs = fmaxf(__uint_as_float((uint32_t)(127 + min(qe + over_s[ring], 127)) << 23) * a.scale_log2, 1.4e-45f);
         // 32 scores times their keys' scales; what the row does not see (its tokens from `limit` on, tokens without a block) becomes -inf
         auto scores = [&](int c, float* y) -> uint32_t {
           uint32_t w[32];
@@ -434,7 +439,8 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         issue(g.j0 + i + 2, id2);
         if (of_k) {
           const int ev_max = __reduce_max_sync(0xffffffffu, ev == kExpNone ? -200 : ev);
-          if (lane == 0) largest_s[x][cw] = ev_max;      // (two: a warp may be a tile ahead)
+          const int ek_max = __reduce_max_sync(0xffffffffu, ek);
+          if (lane == 0) { largest_s[x][cw] = ev_max; largest_k_s[x][cw] = ek_max; }      // (two: a warp may be a tile ahead)
           ok = meet<1, 128>(ok);
           if (!ok) break;
           e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
@@ -442,11 +448,13 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
           const float nan = __uint_as_float(0x7fc00000u);
           const int down = ev - e_now + (int)kQrShift;   // (far below: nothing)
-          ks[ct] = there ? exp_scale(ek) : 0.f;
+          const int over = max(0, max(max(largest_k_s[x][0], largest_k_s[x][1]), max(largest_k_s[x][2], largest_k_s[x][3])) - kQrKeyMost);
+          const float key_scale = over == 0 || ek == kExpNone ? exp_scale(ek) : ek - over > -127 ? __uint_as_float((uint32_t)(ek - over + 127) << 23) : __uint_as_float(1u << (ek - over + 149));
+          ks[ct] = there ? key_scale : 0.f;
           ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
           const uint32_t gone = __ballot_sync(0xffffffffu, !there), no_number = __ballot_sync(0xffffffffu, there && ev == kExpNone);
           if (lane == 0) { gone_s[ring][cw] = gone; nan_s[ring][cw] = no_number; }
-          if (ct == 0) e_s[u & 7] = e_now;
+          if (ct == 0) { e_s[u & 7] = e_now; over_s[ring] = over; }
           mbar_arrive(bar_scale + 8 * ring);
           there = exponents(g.j0 + i + 1, id1, &ek, &ev);
         }

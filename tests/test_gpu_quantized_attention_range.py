@@ -43,3 +43,31 @@ def test_a_query_that_is_no_number_over_blocks_that_are_none(T, n):
     rows = B().ContinuationRows([0, 1], [n], T, i32([0, n]), i32([0] * n), i32([T - n + 1 + j for j in range(n)]), i32([[-1] * 19]))
     B().relaxkv_quantized_attention(store, rows, q, out, workspace(H, Hkv, D), lse_out=lse)
     assert status() == B().ERR_BAD_INDEX and (out == 0).all() and (lse == -float("inf")).all()
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,new", [([250, 3], [2, 1]), ([3000, 40], [2, 2]), ([700, 90], [6, 5]), ([700], [40]), ([3000, 200], [60, 33])])
+def test_keys_of_the_largest_exponents(lens, new, kind):
+    """Keys up to 127 * 2^127 and queries as small: logits of ordinary size, in both kernels; others that only just weigh beside them."""
+    Hkv, D, block, H = 1, 64, 16, 4
+    store = make_store(sum(-(-t // block) for t in lens) + 1, block, Hkv, D, kind, seed=1)
+    rng = np.random.default_rng(0)
+    for low in (127, 121, 96):
+        store.k_exp.copy_(i32(rng.integers(low, 128, tuple(store.k_exp.shape))).to(torch.int8))
+        r = attend(store, lens, new, H, block, q=rnd(sum(new) + 2, H, D, seed=4, scale=2.0 ** -120), scale=2.0 ** -12 if kind == "int8" else 2.0 ** -14)
+        check_rows(r, store, D, max(lens))
+    store.k_exp.fill_(127)
+    store.k.view(torch.int8).zero_()                                        # elements of nothing, whatever their exponent
+    check_rows(attend(store, lens, new, H, block), store, D, max(lens))
+    assert status() == B().OK
+
+
+@pytest.mark.parametrize("lens,new", [([250, 3], [2, 1]), ([700, 20], [40, 30])])
+@pytest.mark.parametrize("q_scale,scale", [(0.0, 0.125), (0.0, 1e-12), (2.0 ** -110, 1e-12), (2.0 ** -110, 1e-30), (1.0, 1e-30)])
+def test_logits_of_nothing(lens, new, q_scale, scale):
+    """Queries or scales so small that all logits are nothing: what is seen weighs alike, what is not seen nothing."""
+    Hkv, D, block, H = 2, 64, 16, 8
+    store = make_store(sum(-(-t // block) for t in lens) + 1, block, Hkv, D, "int8", seed=2)
+    r = attend(store, lens, new, H, block, q=rnd(sum(new) + 2, H, D, seed=4, scale=q_scale), scale=scale)
+    check_rows(r, store, D, max(lens))
+    assert status() == B().OK
