@@ -663,7 +663,7 @@ size_t relaxkv_quantized_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, 
  * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits, and to 2^-38 of the
  * row's largest (weight times value's scale), before they meet the values.  Any number of rows to a sequence.  With G = n_q_heads / n_kv_heads <= 16 and G times the sequences' rows on
  * average up to 32, a sequence's tokens are read once for 8 / G to 32 / G rows of it; beyond that once for 128 / G, and weights are rounded to 2^-35 of (the row's largest
- * weight times the largest value's scale of the sequence's tokens).  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
+ * weight times the largest value's scale of the tokens that it sees).  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
  * n_seq <= 4096; row_len does not fall within a sequence.  A row that sees no token gets zeros and lse = -inf.
  *   q, out  device bf16 [n_rows, n_q_heads, head_dim] (16-byte aligned, not the same); lse_out NULL or device fp32 [n_q_heads, n_rows]
  * Rows with row_seq -1 and rows behind row_cu[n_seq] are left alone.  Reported and left alone: rows of a sequence whose row_cu, or whose last row_len, is out of range, rows whose row_seq is another

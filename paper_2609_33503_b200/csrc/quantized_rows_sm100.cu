@@ -3,8 +3,8 @@
 // Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of one sequence), one KV head and a run of
 // 128-token tiles.  Eight warps bring a tile, four its K and four its V: 8-bit values out of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the
 // tensor cores read them (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); a thread makes weights
-// of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest of the
-// sequence so far: p = 2^(s - m + 11 + e_t - E).
+// of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest so far
+// of the tokens that a row sees: p = 2^(s - m + 11 + e_t - E).
 // Two groups of four warps take the even and the odd tiles: the weights of one tile are made while the products of the other run.  S of tile j + 2 is made when P of tile j has
 // been used; a group hands its P over when O of the tile before is complete, which is also when O may be rescaled; a row's running maximum goes from group to group through
 // shared memory, sums stay with the groups.  K is written a tile ahead of V, or the weights of a tile wait for a value tile that waits for them.
@@ -26,6 +26,8 @@ constexpr int kQrTile = 128, kQrThreads = 640;           // tokens of a tile; wa
 constexpr float kQrShift = 11.f, kQrGrow = 4.f;          // weights begin at 2^11 and are rescaled when a row's maximum grew by 2^4
 // Factors of keys are up to 2^90, what is above that of a tile's largest goes to the rows' scales: a product of Q and key values (2^31 at most) stays within fp32 before its row's scale.
 constexpr int kQrKeyMost = 90;
+// Values' factors are relative to the largest exponent so far, a second set to one 2^120 below: for rows that do not see tokens whose exponents are more than 100 above what they see.
+constexpr int kQrBelow = 120, kQrNear = 100;
 constexpr float kQrExact = 32768.f;                      // logits (in log2 units) up to this are not rounded by themselves: 2^-9 of a weight
 using QrWalk = Walk<kQrTile, 4, 2, 128>;                 // a task's start and end take as long as four tiles (57 rows over 16 K: of two 68 us, of three to six 64)
 
@@ -33,8 +35,8 @@ template <int D>
 struct QrSmem {
   static constexpr int kHalves = D / 64, kHalfBytes = kQrTile * 128, kTileBytes = kHalves * kHalfBytes;
   static constexpr int kV = 2 * kTileBytes;              // K[2] | V[2]
-  static constexpr int kScale = 4 * kTileBytes;          // of the last four tiles: factors of the keys' scores, of the values' weights
-  static constexpr int kRaw = kScale + 4 * 2 * kQrTile * 4;      // 8-bit values of two tiles as they come, K and V: every piece is one thread's
+  static constexpr int kScale = 4 * kTileBytes;          // of the last four tiles: factors of the keys' scores, of the values' weights, these 2^kQrBelow times as large
+  static constexpr int kRaw = kScale + 4 * 3 * kQrTile * 4;      // 8-bit values of two tiles as they come, K and V: every piece is one thread's
   static constexpr int kRawTile = 2 * kQrTile * D;
   static constexpr int kBar = kRaw + 2 * kRawTile;
   // full_k[2], full_v[2], empty_k[2], empty_v[2], s[2], m[2], o[2], scale[4], p, q: those of two or four belong to every second or fourth tile, so that nobody who
@@ -88,6 +90,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
   __shared__ int largest_s[2][4], e_s[8];                 // largest exponents of the values: of each of the four warps' tokens; up to the last eight tiles
   __shared__ int largest_k_s[2][4], over_s[4];            // of the keys: of each warp's tokens; by how much the last four tiles' are above kQrKeyMost
   __shared__ uint32_t top_s[2][kQrRows];                 // largest bits of a row's dims, by half
+  __shared__ int e_part_s[kQrRows];                       // what O of a row is relative to that does not see the last tile, or not all of it
   __shared__ uint32_t gone_s[4][4], nan_s[4][4];          // tokens of the last four tiles whose blocks do not exist; whose values are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -188,7 +191,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           mbar_arrive(bar_p);
           continue;
         }
-        const float* ks = reinterpret_cast<const float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
+        const float* ks = reinterpret_cast<const float*>(base_ptr + L::kScale) + ring * 3 * kQrTile;
         const float* vs = ks + kQrTile;
         const int limit = seen < 0 ? kQrTile : seen - j * kQrTile;      // (rows that are not written see all: nothing to hide costs half as much)
         const bool slow = __any_sync(0xffffffffu, limit < kQrTile || (gone_s[ring][0] | gone_s[ring][1] | gone_s[ring][2] | gone_s[ring][3]) != 0);
@@ -237,6 +240,40 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
         mbar_arrive(bar_m + 8 * x);
         z *= fast_exp2(m - m_new);
         m = m_new;
+        // The values' exponents are weighed relative to the largest so far of the tokens that the row sees: of the last tile that it sees, when that is a part of it, the part's largest,
+        // e_less below the tile's.  The weights of that tile grow by as much (2^e_grow with the factors that they meet), and their sum comes down again.
+        const bool cut = limit > 0 && limit < kQrTile;
+        int e_less = 0, e_grow = 0;
+        bool second = false;
+        // (only where the tile has a larger one than all before it)
+        if (slow && __any_sync(0xffffffffu, cut) && (i == 0 || e_s[jj & 7] != e_s[(jj - 1) & 7])) {
+          // a value's exponent, less that of the tile, + kQrShift + 127: from its factor, or from the second one where that is 0
+          auto exponent = [&](int at) -> int {
+            const int f = (int)(__float_as_uint(vs[at]) >> 23);
+            if (f == 255) return -1000;                  // (NaN)
+            return f > 0 ? f : (int)(__float_as_uint(vs[at + kQrTile]) >> 23) - kQrBelow;      // (none: far below)
+          };
+          int upto = -1000;                              // of tokens up to 4 lane + 3
+#pragma unroll 1
+          for (int b = 0; b < 4; ++b) upto = max(upto, exponent(4 * lane + b));
+#pragma unroll 1
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto = max(upto, y);
+          }
+          const int some = min(max(limit, 0), kQrTile - 1), words = some >> 2;
+          int most = __shfl_sync(0xffffffffu, upto, max(words - 1, 0));
+          if (words == 0) most = -1000;
+#pragma unroll 1
+          for (int b = 0; b < (some & 3); ++b) most = max(most, exponent(4 * words + b));
+          most -= (int)kQrShift + 127;
+          const int e_tile = e_s[jj & 7], e_before = i > 0 ? e_s[(jj - 1) & 7] : kExpLeast;       // (a row that sees some of it has seen all of the tiles before)
+          if (cut) e_less = e_tile - max(e_before, e_tile + most);
+          e_grow = e_less > kQrNear ? e_less - kQrBelow : e_less;
+          if (e_less > kQrNear) vs += kQrTile;
+          second = __any_sync(0xffffffffu, e_less > kQrNear);
+        }
+        const float m_less = m - (float)e_grow;
         // s * qs - m in one rounding keeps what the rounding of m has cut off: the same factor on all weights of the row, which their sum takes out again; very large logits are
         // rounded first, or the factor would leave the range of fp16
         const bool large = __any_sync(0xffffffffu, fabsf(m_tile) > kQrExact);
@@ -255,8 +292,8 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           for (int e = 0; e < 32; e += 4) {
             float p[4];
             const float4 v4 = *reinterpret_cast<const float4*>(vs + c * 32 + e);
-            fma2(p[0], p[1], y[e], y[e + 1], q2, q2, -m, -m);
-            fma2(p[2], p[3], y[e + 2], y[e + 3], q2, q2, -m, -m);
+            fma2(p[0], p[1], y[e], y[e + 1], q2, q2, -m_less, -m_less);
+            fma2(p[2], p[3], y[e + 2], y[e + 3], q2, q2, -m_less, -m_less);
 #pragma unroll
             for (int u = 0; u < 4; ++u) p[u] = fast_exp2(p[u]);
             add2(z0, z1, p[0], p[1]);
@@ -269,21 +306,25 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
               pk[(e + u) >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
           }
-          if (factors) {                                 // what is not seen weighs nothing, whatever its factor
+          if (factors || second) {                       // what is not seen weighs nothing, whatever its factor
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (hidden >> e & 1) pk[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
           }
           tmem_st16(t_s + c * 16, pk);                   // (where scores were that have been read)
         }
-        z += (z0 + z1) + (z2 + z3);
+        z = fmaf((z0 + z1) + (z2 + z3), __uint_as_float((uint32_t)(127 - e_grow) << 23), z);
         if (jj > 0) {                                    // O of the tile before is complete
           if (!(ok = wait(bar_o + 8 * (x ^ 1), (jj - 1) >> 1))) break;
           tc_fence_after();
         }
-        const int e_now = e_s[jj & 7], e_was = i > 0 ? e_s[(jj - 1) & 7] : e_now;
-        if (i > 0 && __any_sync(0xffffffffu, grows || e_now != e_was)) {
-          const float alpha = fast_exp2(m_old - m_new + (float)(e_was - e_now));
+        int e_up = i > 0 ? e_s[jj & 7] - e_s[(jj - 1) & 7] : 0;
+        if (slow) {
+          if (limit >= 0 && limit < kQrTile) e_part_s[t] = cut ? e_s[jj & 7] - e_less : e_s[(jj - 1) & 7];      // (of the last tile that the row sees)
+          e_up = cut ? e_up - e_less : limit > 0 ? e_up : 0;
+        }
+        if (i > 0 && __any_sync(0xffffffffu, grows || e_up != 0)) {
+          const float alpha = fast_exp2(m_old - m_new - (float)e_up);
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
@@ -302,10 +343,10 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
       jj = jj0 + n;
       if (ok && jj > 1) ok = wait(bar_o + 8 * (jj & 1), (jj - 2) >> 1);
       if (ok) ok = wait(bar_o + 8 * (~jj & 1), (jj - 1) >> 1);
-      const int e_last = e_s[(jj - 1) & 7];
       const float m_end = max_s[t];                      // (of a warp without rows: anything)
       sum_s[x * kQrRows + t] = z * fast_exp2(m - m_end);
       ok = meet<2, 256>(ok && !*abort_flag);
+      const int e_last = seen >= 0 && seen < (long long)g.j1 * kQrTile ? e_part_s[t] : e_s[(jj - 1) & 7];      // (of a row that has seen no token: anything)
       const bool whole = g.whole();
       const int slot = g.slot();
       if (tid == 0) {
@@ -445,13 +486,16 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           if (!ok) break;
           e_run = max(max(e_run, max(largest_s[x][0], largest_s[x][1])), max(largest_s[x][2], largest_s[x][3]));
           const int e_now = max(e_run, kExpLeast);       // (no token yet: anything)
-          float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 2 * kQrTile;
+          float* ks = reinterpret_cast<float*>(base_ptr + L::kScale) + ring * 3 * kQrTile;
           const float nan = __uint_as_float(0x7fc00000u);
           const int down = ev - e_now + (int)kQrShift;   // (far below: nothing)
           const int over = max(0, max(max(largest_k_s[x][0], largest_k_s[x][1]), max(largest_k_s[x][2], largest_k_s[x][3])) - kQrKeyMost);
           const float key_scale = over == 0 || ek == kExpNone ? exp_scale(ek) : ek - over > -127 ? __uint_as_float((uint32_t)(ek - over + 127) << 23) : __uint_as_float(1u << (ek - over + 149));
           ks[ct] = there ? key_scale : 0.f;
           ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
+          // (who reads the second factors sees nothing of a warp that has none to write)
+          if (__any_sync(0xffffffffu, !there || (ev != kExpNone && down < (int)kQrShift - kQrNear)))
+            ks[2 * kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : __uint_as_float((uint32_t)(min(down + kQrBelow, 127) + 127) << 23);
           const uint32_t gone = __ballot_sync(0xffffffffu, !there), no_number = __ballot_sync(0xffffffffu, there && ev == kExpNone);
           if (lane == 0) { gone_s[ring][cw] = gone; nan_s[ring][cw] = no_number; }
           if (ct == 0) { e_s[u & 7] = e_now; over_s[ring] = over; }

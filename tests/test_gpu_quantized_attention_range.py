@@ -71,3 +71,27 @@ def test_logits_of_nothing(lens, new, q_scale, scale):
     r = attend(store, lens, new, H, block, q=rnd(sum(new) + 2, H, D, seed=4, scale=q_scale), scale=scale)
     check_rows(r, store, D, max(lens))
     assert status() == B().OK
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("T,n,H,Hkv,D", [(650, 40, 8, 2, 128), (640, 40, 8, 2, 64), (5000, 60, 4, 1, 128), (130, 130, 4, 2, 64), (1290, 200, 2, 1, 128)])
+def test_tokens_behind_a_row_take_none_of_its_bits(T, n, H, Hkv, D, kind):
+    """Values behind a row, up to 2^190 times as large as those that it sees: its weights are rounded relative to what it sees."""
+    block = 16
+    store = make_store(-(-T // block) + 2, block, Hkv, D, kind, seed=T)
+    ids = np.random.default_rng(3).permutation(store.k.shape[0])[:-(-T // block)]              # (the blocks that attend() hands out)
+    low = -90 if D == 64 else -9
+    store.v_exp.add_(low + 9)
+    for token, e in ((T - 37, 5), (T - 25, 30), (T - 12, 70), (T - 10, 60), (T - 2, 100)):
+        store.v_exp[int(ids[token // block]), :, token % block] = e
+    r = attend(store, [T], [n], H, block, seed=3)
+    slots = (r["keep"][0][0, :len(ids), None] * block + np.arange(block)).reshape(-1)[:T].astype(int)
+    top = np.maximum.accumulate(value_scale(store)[slots], 0)               # [T, H_kv]: of what a row of so many tokens sees
+    lens = [max(0, T - n + 1 + j) for j in range(n)]
+    want, lse, mass, most, _ = r["wants"][0]
+    # the row's largest weight is at 2^11 or above before it meets its value's scale: off by up to 2^-36 of the largest weight times the largest scale that the row sees, for each of its
+    # tokens and values of up to 448
+    lost = 2.0 ** -36 * T * 448 * np.stack([top[max(t, 1) - 1].repeat(H // Hkv) * (t > 0) for t in lens], 1)
+    r["wants"] = [(want, lse, mass, most, lost)]
+    check(r, D)
+    assert status() == B().OK
