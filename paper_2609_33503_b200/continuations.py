@@ -64,6 +64,9 @@ class Continuations:
         self.base = torch.cat([torch.full((n,), 0 if store_dtype is not None else t, **i32) for t, n in zip(self.ctx_lens, self.seqs)] or [torch.empty(0, **i32)])
         self.zeros = torch.zeros(self.max_rows, **i32) if store_dtype is None and blk.rotary is not None else None
         self.lens = [0] * n_seq                        # the host's copy of the lengths: what it asks for is what it gets
+        self.owner = [b for b, n in enumerate(self.seqs) for _ in range(n)]
+        # whether what a sequence's rows are to see of its context is where the attention looks for it
+        self.kept = [store_dtype is None or self.ctx_lens[b] == 0 for b in self.owner]
         self.n_free = int(n_blocks)
         self._new: Dict[tuple, torch.Tensor] = {}
         self._captured: List[torch.Tensor] = []
@@ -126,11 +129,18 @@ class Continuations:
         return self._new[key]
 
     def begin(self, new: Sequence[int]) -> int:
-        """Begins a step: new[i] tokens of sequence i follow (0: it waits, -1: it ends and gives its blocks back).  Block tables, positions and
-        slots of the rows are made on the device, on the current stream; the rows are those of the sequences in order.  Returns their number."""
+        """Begins a step: new[i] tokens of sequence i follow (0: it waits, -1: it ends and gives its blocks back; with a store_dtype its context goes with
+        them, and comes again by keep_contexts).  Block tables, positions and slots of the rows are made on the device, on the current stream; the rows are those of the
+        sequences in order.  Returns their number."""
         new = [int(x) for x in new]
         if len(new) != self.n_seq or any(n < -1 for n in new):
             raise ValueError(f"a step of {self.n_seq} sequences takes as many counts, -1 or more each")
+        without = [i for i, n in enumerate(new) if n > 0 and not self.kept[i]]
+        if without:
+            raise ValueError(f"the contexts of the sequences {without} are not in the store: keep_contexts brings them there")
+        return self._begin(new)
+
+    def _begin(self, new: List[int]) -> int:
         lens = [0 if n < 0 else t + n for t, n in zip(self.lens, new)]
         rows = sum(n for n in new if n > 0)
         # what the device would refuse is refused here, before anything has changed
@@ -147,6 +157,7 @@ class Continuations:
         self._len.reverse()
         self._n_free.reverse()
         self.lens, self.n_free, self.n_rows = lens, n_free, rows
+        self.kept = [k and (n >= 0 or self.store_dtype is None or self.ctx_lens[b] == 0) for k, n, b in zip(self.kept, new, self.owner)]
         per_ctx = [sum(n for n in new[a:b] if n > 0) for a, b in zip(self.seq_cu, self.seq_cu[1:])]
         longest = max([t for t, n in zip(lens, new) if n > 0], default=0)
         self.rows = B.ContinuationRows(self.seq_cu, per_ctx, longest, self.row_cu, self.row_seq[:rows], self.row_len[:rows], self.table)
@@ -157,7 +168,7 @@ class Continuations:
         the repair is through, and again for sequences that have ended.  The next step's rows follow them."""
         if self.store_dtype is None:
             raise ValueError("contexts are kept in the store only where it has a store_dtype")
-        owner = [b for b, n in enumerate(self.seqs) for _ in range(n)]
+        owner = self.owner
         which = list(range(self.n_seq)) if sequences is None else sorted({int(i) for i in sequences})
         if any(not 0 <= i < self.n_seq for i in which) or any(self.lens[i] for i in which):
             raise ValueError("contexts are kept for sequences that have no tokens yet")
@@ -176,7 +187,7 @@ class Continuations:
                 room -= new[i]
             if not any(new):
                 break
-            self.begin(new)
+            self._begin(new)
             for l, cache in enumerate(caches):
                 at = 0
                 for i in which:
@@ -186,6 +197,8 @@ class Continuations:
                         at += new[i]
             for i in which:
                 done[i] += new[i]
+        for i in which:
+            self.kept[i] = True
         self.rows, self.n_rows = None, 0
 
     def _append(self, layer: int, w: Dict[str, torch.Tensor], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
