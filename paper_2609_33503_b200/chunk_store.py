@@ -57,11 +57,12 @@ class ChunkStore:
         need = -(-n // self.block_size)
         if need > len(self.free):
             raise ValueError(f"{need - len(self.free)} blocks short: let chunks go, or give the store more")
-        blocks = [self.free.pop() for _ in range(need)]
+        blocks = self.free[-1:-need - 1:-1]             # (taken when every layer has its rows: a call may be refused)
         slots = torch.tensor([b * self.block_size + t for b in blocks for t in range(self.block_size)][:n], dtype=torch.int32).to(self.device)
         for cache, store in zip(caches, self.stores):
             t = cache.start(req) + first
             B.relaxkv_append_quantized(store, cache.k[t:t + n], cache.v[t:t + n], slots)
+        del self.free[-need:]
         self.chunks[key] = _Chunk(tuple(blocks), slots, int(position))
 
     def drop(self, key: Hashable) -> None:
