@@ -289,6 +289,11 @@ class CacheView:
         """Token row at which a request begins."""
         return int(self._off[req])
 
+    def tokens(self, req: int) -> int:
+        """Token rows from where a request begins to where the next one does, or to the end."""
+        start = self._off[req]
+        return max(0, min([int(self.k.shape[0]), *(x for x in self._off if x > start)]) - start)
+
 
 class PagedStore:
     """Host-side relaxkv_paged_cache over torch tensors k, v of logical shape [n_blocks, block_size, H_kv, D] (any block, token and head

@@ -44,7 +44,7 @@ class ChunkStore:
         if len(caches) != len(self.stores):
             raise ValueError(f"caches of {len(self.stores)} layers expected, not {len(caches)}")
         for c, s in zip(caches, self.stores):
-            if c.v is None or c.heads != s.heads or c.dim != s.dim or not 0 <= req < len(c.room) or first < 0 or first + n > c.room[req]:
+            if c.v is None or c.heads != s.heads or c.dim != s.dim or not 0 <= req < len(c.room) or first < 0 or first + n > c.tokens(req):
                 raise ValueError(f"tokens {first} to {first + n} of request {req} in caches of {s.heads} heads of {s.dim} expected")
 
     def put(self, key: Hashable, caches: Sequence[B.CacheView], req: int, first: int, n: int, position: int) -> None:
@@ -71,7 +71,7 @@ class ChunkStore:
 
     def assemble(self, keys: Sequence[Hashable], caches: Sequence[B.CacheView], req: int = 0, first: int = 0) -> int:
         """Writes chunks one behind the other into a request's context, from its token `first` on, their keys turned for the positions there (token i of a
-        request has position i).  Returns the number of tokens."""
+        request has position i).  A request reaches to where the next one of the cache begins.  Returns the number of tokens."""
         parts: List[_Chunk] = [self.chunks[k] for k in keys]
         n = sum(int(c.slots.numel()) for c in parts)
         self._caches(caches, req, first, n)
