@@ -205,14 +205,15 @@ PyObject* head_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Held shape2{PyObject_GetAttr(like, g_shape)}, strides2{shape2.p ? PyObject_CallMethodNoArgs(like, g_stride) : nullptr},
         dtype2{strides2.p ? PyObject_GetAttr(like, g_dtype) : nullptr};
     if (!dtype2.p) return nullptr;
-    const bool same = three(shape2.p, ld) && three(strides2.p, ls) && dtype2.p == bf16 && !memcmp(d, ld, sizeof d) && !memcmp(s, ls, sizeof s);
+    const bool same = three(shape2.p, ld) && three(strides2.p, ls) && dtype2.p == bf16 && !memcmp(d, ld, sizeof d) && (d[0] < 2 || s[0] == ls[0]) &&
+                      (d[1] < 2 || s[1] == ls[1]) && s[2] == ls[2];
     if (PyErr_Occurred()) return nullptr;
     if (!same)
       return PyErr_Format(PyExc_ValueError, "rows laid out like %S, strides %S, expected, not %S of %S, strides %S", shape.p, strides.p, shape2.p, dtype2.p, strides2.p);
   }
   // (of one row, or one head, the distance to the next is whatever it happens to be)
-  if (d[0] == 1 && s[0] < d[2]) s[0] = d[2];
-  if (d[1] == 1 && s[1] < d[2]) s[1] = d[2];
+  if (d[0] == 1) s[0] = d[2];
+  if (d[1] == 1) s[1] = d[2];
   PyObject* out = PyTuple_New(5);
   const long long v[5] = {d[0], d[1], d[2], s[0], s[1]};
   for (int i = 0; out && i < 5; ++i) {
