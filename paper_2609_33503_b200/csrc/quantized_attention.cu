@@ -188,6 +188,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
   float qs[NT][2], m[NT][2], mp[NT][2], z[NT][2], o[kChunks][NT][4];
   uint2 qf[kQInRegs ? kChunks : 1][kQInRegs ? NT : 1];                // the columns of Q as fragments
   int seen[NT][2], seen_all = 0;
+  bool huge = false;
   // The task before, whose results are still to be added up.
   bool pending = false, pending_whole = false, more = true;
   int pending_slot = 0;
@@ -230,6 +231,15 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
         }
       }
       // ---- scores of this lane: tokens 4 gid + i, i = 2 h + y, columns 2 tig (+ 1); w: with the exponents of the values ----
+      // (queries so large that a score would leave fp32 before its key's scale brings it back take 2^-64 of it first)
+      if (huge) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) sc[h][nt][y] *= 0x1p-64f;
+      }
       float vexp[4], w[NT][2][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -241,6 +251,7 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           for (int x = 0; x < 2; ++x) {
             float& v = sc[i >> 1][nt][2 * (i & 1) + x];
             v = v * qs[nt][x] * ks;
+            if (huge) v *= 0x1p64f;
             w[nt][x][i] = v + vexp[i];
           }
       }
@@ -451,6 +462,10 @@ quantized_attention_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
           m[nt][x] = mp[nt][x] = kNothing;
           z[nt][x] = 0.f;
         }
+      bool far = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) far |= fmaxf(qs[nt][0], qs[nt][1]) > 0x1p90f;
+      huge = __any_sync(0xffffffffu, far);
       seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 1));
       seen_all = min(seen_all, __shfl_xor_sync(0xffffffffu, seen_all, 2));
 #pragma unroll

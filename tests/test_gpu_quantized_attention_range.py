@@ -95,3 +95,26 @@ def test_tokens_behind_a_row_take_none_of_its_bits(T, n, H, Hkv, D, kind):
     r["wants"] = [(want, lse, mass, most, lost)]
     check(r, D)
     assert status() == B().OK
+
+
+@pytest.mark.parametrize("lens,new", [([250, 3], [2, 1]), ([3000, 40], [2, 2]), ([700, 90], [6, 5]), ([700, 90], [40, 30])])
+def test_queries_of_the_largest_numbers(lens, new):
+    """Queries up to bf16's largest number over keys as small: logits of ordinary size, and queries of ordinary size beside them."""
+    Hkv, D, block, H = 1, 64, 16, 4
+    store = make_store(sum(-(-t // block) for t in lens) + 1, block, Hkv, D, "int8", seed=1)
+    store.k_exp.fill_(-100)
+    for power, scale in ((124, 2.0 ** -34), (112, 2.0 ** -22)):
+        q = rnd(sum(new) + 2, H, D, seed=4, scale=2.0 ** power)
+        q[:, 1] = rnd(sum(new) + 2, D, seed=5)
+        assert torch.isfinite(q).all()
+        check_rows(attend(store, lens, new, H, block, q=q, scale=scale), store, D, max(lens))
+    q[0, 2, 3] = torch.finfo(torch.bfloat16).max
+    check_rows(attend(store, lens, new, H, block, q=q, scale=2.0 ** -40), store, D, max(lens))
+    # logits of 2^31 and more: one key's weight alone, whichever fp32 finds the largest; a score is off by its sums' roundings, (D + 8) 2^-24 of the sum of its products' sizes
+    q[:, 1] = 0
+    r = attend(store, lens, new, H, block, q=q)
+    out, lse = f64(r["out"]), f64(r["lse"])
+    assert np.isfinite(out).all()
+    for (_, want, _, most, _), a, b in zip(r["wants"], r["cu"], r["cu"][1:]):
+        assert (np.abs(lse[:, a:b] - want) <= (D + 8) * 2.0 ** -24 * most + 2.0 ** -18 + 2.0 ** -21 * np.abs(want)).all()
+    assert status() == B().OK
