@@ -494,7 +494,7 @@ quantized_rows_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus* st)
           ks[ct] = there ? key_scale : 0.f;
           ks[kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : down < -126 ? 0.f : __uint_as_float((uint32_t)(down + 127) << 23);
           // (who reads the second factors sees nothing of a warp that has none to write)
-          if (__any_sync(0xffffffffu, !there || (ev != kExpNone && down < (int)kQrShift - kQrNear)))
+          if (__any_sync(0xffffffffu, !there || ev == kExpNone || down < (int)kQrShift - kQrNear))
             ks[2 * kQrTile + ct] = !there ? 0.f : ev == kExpNone ? nan : __uint_as_float((uint32_t)(min(down + kQrBelow, 127) + 127) << 23);
           const uint32_t gone = __ballot_sync(0xffffffffu, !there), no_number = __ballot_sync(0xffffffffu, there && ev == kExpNone);
           if (lane == 0) { gone_s[ring][cw] = gone; nan_s[ring][cw] = no_number; }

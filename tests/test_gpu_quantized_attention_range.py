@@ -118,3 +118,23 @@ def test_queries_of_the_largest_numbers(lens, new):
     for (_, want, _, most, _), a, b in zip(r["wants"], r["cu"], r["cu"][1:]):
         assert (np.abs(lse[:, a:b] - want) <= (D + 8) * 2.0 ** -24 * most + 2.0 ** -18 + 2.0 ** -21 * np.abs(want)).all()
     assert status() == B().OK
+
+
+def test_a_value_that_is_no_number_beside_tokens_that_are_not_seen():
+    """A row that sees tokens 2^130 times smaller than those behind it, the last of them NaN."""
+    T, n, H, D, block = 128, 64, 4, 64, 16
+    store = make_store(8, block, 1, D, "int8", seed=1)
+    store.v_exp.copy_(i32([-90] * 64 + [-128] + [40] * 63).to(torch.int8).view(8, 1, block))
+    q, out, lse = rnd(n, H, D, seed=2), torch.empty(n, H, D, dtype=torch.bfloat16, device="cuda"), torch.empty(H, n, device="cuda")
+    lens = [T - n + 1 + j for j in range(n)]
+    rows = B().ContinuationRows([0, 1], [n], T, i32([0, n]), i32([0] * n), i32(lens), i32([list(range(8))]))
+    for _ in range(3):
+        B().relaxkv_quantized_attention(store, rows, q, out, workspace(H, 1, D), lse_out=lse)
+        assert torch.isnan(out).all() and torch.isfinite(lse).all()
+    store.v_exp[4, 0, 0] = -90
+    kk, vv = store_values(store)
+    B().relaxkv_quantized_attention(store, rows, q, out, workspace(H, 1, D), lse_out=lse)
+    want, want_lse, mass, most, _ = orc.attention(f64(q), kk, vv, lens, D ** -0.5)
+    top = np.maximum.accumulate(value_scale(store)[:, 0])[np.array(lens) - 1]
+    tol, lse_tol = orc.attention_tolerance(want, want_lse, mass, most, 2.0 ** -36 * T * 448 * np.tile(top, (H, 1)), D)
+    assert (np.abs(f64(out) - want) <= tol).all() and (np.abs(f64(lse) - want_lse) <= lse_tol).all() and status() == B().OK
