@@ -596,10 +596,10 @@ quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
       for (int b = 0; b < kQrJoinBatch; ++b) {
         if (p0 + b >= parts) break;
         if (l[b] == -INFINITY) continue;
-        const float now = fmaxf(m, l[b]), was = fast_exp2(m - now), w = fast_exp2(l[b] - now);
+        const float now = fmaxf(m, l[b]), was = fast_exp2(m - now), w = fast_exp2(l[b] - now), w8 = w * 0x1p-8f;      // (the sum of 148 parts at most stays within fp32)
         den = den * was + w;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = acc[e] * was + v[b][e] * w;
+        for (int e = 0; e < kPer; ++e) acc[e] = acc[e] * was + v[b][e] * w8;
         m = now;
       }
     }
@@ -608,7 +608,7 @@ quantized_rows_join_kernel(const __grid_constant__ QuantAttnArgs a, DeviceStatus
     uint32_t packed[kPer / 2];
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) {
-      const __nv_bfloat162 h2 = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+      const __nv_bfloat162 h2 = __floats2bfloat162_rn(acc[e] * inv * 0x1p8f, acc[e + 1] * inv * 0x1p8f);
       packed[e / 2] = *reinterpret_cast<const uint32_t*>(&h2);
     }
     uint16_t* o = a.out + (row * a.H + head) * D + lane * kPer;

@@ -138,3 +138,15 @@ def test_a_value_that_is_no_number_beside_tokens_that_are_not_seen():
     top = np.maximum.accumulate(value_scale(store)[:, 0])[np.array(lens) - 1]
     tol, lse_tol = orc.attention_tolerance(want, want_lse, mass, most, 2.0 ** -36 * T * 448 * np.tile(top, (H, 1)), D)
     assert (np.abs(f64(out) - want) <= tol).all() and (np.abs(f64(lse) - want_lse) <= lse_tol).all() and status() == B().OK
+
+
+@pytest.mark.parametrize("kind,e", [("int8", 120), ("e4m3", 118)])
+@pytest.mark.parametrize("lens,new", [([250, 3], [2, 1]), ([3000, 40], [2, 2]), ([900], [50]), ([4000], [33])])
+def test_values_of_the_largest_numbers(lens, new, kind, e):
+    """Outputs of up to 2^127, joined from several parts: no sum on the way leaves fp32."""
+    Hkv, D, block, H = 1, 64, 16, 4
+    store = make_store(sum(-(-t // block) for t in lens) + 1, block, Hkv, D, kind, seed=1)
+    store.v_exp.fill_(e)
+    store.v.view(torch.int8).fill_(127 if kind == "int8" else 0x7d)         # 127, 416
+    check_rows(attend(store, lens, new, H, block), store, D, max(lens))
+    assert status() == B().OK
