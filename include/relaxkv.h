@@ -575,9 +575,10 @@ relaxkv_status relaxkv_block_sparse_attention(
     relaxkv_stream stream);
 
 /*
- * ---- Contexts kept in 8 bits.  (The paper reuses chunk caches without saying how they are kept.)  Chunks, repaired contexts and what sequences add to
- * them live in blocks of a paged store with one byte per element and one power of two per token and head; they are written as they come
- * (out of a cache, or a step's rows with norm and rotation), read back at any position, and attended to where they are.  ----
+ * ---- Contexts kept in 8 bits.  (The paper reuses chunk caches without saying how they are kept.)  Chunks, repaired contexts and
+ * what sequences add to them live in blocks of a paged store with one byte per element and one power of two per token and head; they
+ * are written as they come (out of a cache, or a step's rows with norm and rotation), read back at any position, and attended to
+ * where they are.  ----
  */
 
 typedef enum {
@@ -585,10 +586,13 @@ typedef enum {
   RELAXKV_E4M3 = 1                     /* 8-bit floating point, 4 bits of exponent, 3 of mantissa, up to 448    */
 } relaxkv_quantized_type;
 
-/* The 8-bit store of one layer.  Token t of block x of KV head g: values at k + x * block_stride + t * token_stride + g * head_stride (bytes = elements;
- * head_dim of them side by side), same for V, strides multiples of 16, that of heads below 2^31; exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V.
- * An element stands for value * 2^exponent; exponent -128 says that all elements of the token and head are NaN; others are -100 to 127.
- * No value byte is a NaN of e4m3 (relaxkv_append_quantized writes none).  All pointers 16-byte aligned. */
+/*
+ * The 8-bit store of one layer.  Token t of block x of KV head g: values at k + x * block_stride + t * token_stride + g *
+ * head_stride (bytes = elements; head_dim of them side by side), same for V, strides multiples of 16, that of heads below 2^31;
+ * exponents at k_exp + (x * n_kv_heads + g) * block_size + t, same for V. An element stands for value * 2^exponent; exponent -128
+ * says that all elements of the token and head are NaN; others are -100 to 127. No value byte is a NaN of e4m3
+ * (relaxkv_append_quantized writes none).  All pointers 16-byte aligned.
+ */
 typedef struct {
   void* k;
   void* v;
@@ -603,8 +607,10 @@ typedef struct {
   int32_t type;                        /* relaxkv_quantized_type                                                */
 } relaxkv_quantized_cache;
 
-/* A rotary embedding.  The first `dims` dims of a head (a multiple of 8) are dims / 2 pairs, pair i of them (i, i + dims / 2), or (2i, 2i + 1) where interleaved;
- * at position p it turns by p * freq[i], and grows by amplitude.  Dims behind them stay as they are. */
+/*
+ * A rotary embedding.  The first `dims` dims of a head (a multiple of 8) are dims / 2 pairs, pair i of them (i, i + dims / 2), or
+ * (2i, 2i + 1) where interleaved; at position p it turns by p * freq[i], and grows by amplitude.  Dims behind them stay as they are.
+ */
 typedef struct {
   const double* freq;                  /* device [dims / 2]: radians per position                               */
   int32_t dims;
@@ -626,30 +632,38 @@ typedef enum {
 relaxkv_status relaxkv_rotary_frequencies(int32_t dims, double theta, int32_t scaling, double factor, int32_t original_len, double low, double high,
                                           double* h_freq_out, float* h_amplitude_out);
 
-/* relaxkv_qk_norm_rope for any rotary embedding and any strides: q_out = rotated norm of q, k_out likewise, one rounding to bf16 (angles in fp64 up to their
- * remainder, the rest in fp32).  Head h of row r: q + r * q_token_stride + h * q_head_stride, head_dim elements side by side; q_out is laid out like q and may be q
- * itself, k_out like k.  q or k may be NULL, its output with it (only the other one is turned).  Norm weights [head_dim] as in relaxkv_qk_norm_rope.  head_dim 64 or 128,
- * strides multiples of 8, those of heads below 2^31; positions device int32 [n_rows], negative ones turn backwards. */
+/*
+ * relaxkv_qk_norm_rope for any rotary embedding and any strides: q_out = rotated norm of q, k_out likewise, one rounding to bf16
+ * (angles in fp64 up to their remainder, the rest in fp32).  Head h of row r: q + r * q_token_stride + h * q_head_stride, head_dim
+ * elements side by side; q_out is laid out like q and may be q itself, k_out like k.  q or k may be NULL, its output with it (only
+ * the other one is turned).  Norm weights [head_dim] as in relaxkv_qk_norm_rope.  head_dim 64 or 128, strides multiples of 8, those
+ * of heads below 2^31; positions device int32 [n_rows], negative ones turn backwards.
+ */
 relaxkv_status relaxkv_qk_norm_rotate(
     const void* q, void* q_out, int64_t q_token_stride, int64_t q_head_stride, const void* k, void* k_out, int64_t k_token_stride, int64_t k_head_stride,
     int64_t n_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* w_q_norm, const void* w_k_norm, float eps, const int32_t* positions,
     const relaxkv_rotary* rotary, relaxkv_stream stream);
 
 /*
- * Append of rows to the 8-bit store: row r of K (normed and rotated as above where weights and a rotary are given, NULL: as it is) and of V goes to slot
- * slots[r] = block * block_size + token; q_out = rotated norm of q as above (q NULL: none).  For each row and KV head, with y in fp32 before any rounding and M = 127 or 448:
+ * Append of rows to the 8-bit store: row r of K (normed and rotated as above where weights and a rotary are given, NULL: as it is)
+ * and of V goes to slot slots[r] = block * block_size + token; q_out = rotated norm of q as above (q NULL: none).  For each row and
+ * KV head, with y in fp32 before any rounding and M = 127 or 448:
  *   exponent = the smallest e >= -100 with max |y| <= M 2^e (-100 where all are 0);  value = y 2^-e to the nearest, ties to even
- * (an infinite or NaN element makes the exponent -128 and the values 0).  What relaxkv_read_quantized returns without a rotation stands for the same values when it is appended again,
- * but for heads with an element of almost 2^128 that the rounding to 8 bits has taken there: in bf16 that is infinite.
- * v is laid out like k.  Slots are distinct; a row with slot -1 is turned and not stored, another slot outside the store is reported and not stored.
+ * (an infinite or NaN element makes the exponent -128 and the values 0).  What relaxkv_read_quantized returns without a rotation
+ * stands for the same values when it is appended again, but for heads with an element of almost 2^128 that the rounding to 8 bits
+ * has taken there: in bf16 that is infinite. v is laid out like k.  Slots are distinct; a row with slot -1 is turned and not stored,
+ * another slot outside the store is reported and not stored.
  */
 relaxkv_status relaxkv_append_quantized(
     const relaxkv_quantized_cache* store, const void* q, void* q_out, int64_t q_token_stride, int64_t q_head_stride, const void* k, const void* v,
     int64_t k_token_stride, int64_t k_head_stride, int64_t n_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* w_q_norm,
     const void* w_k_norm, float eps, const int32_t* positions, const relaxkv_rotary* rotary, const int32_t* slots, relaxkv_stream stream);
 
-/* Rows of the 8-bit store in bf16: k_out, v_out row r (laid out as k above, v_out like k_out) = the token at slots[r], its keys turned by positions[r] positions more (positions
- * and rotary both NULL: as they are, which is exact; what stands for 2^128 or more is infinite).  A row with slot -1 is left alone, another slot outside the store is reported and left alone. */
+/*
+ * Rows of the 8-bit store in bf16: k_out, v_out row r (laid out as k above, v_out like k_out) = the token at slots[r], its keys
+ * turned by positions[r] positions more (positions and rotary both NULL: as they are, which is exact; what stands for 2^128 or more
+ * is infinite).  A row with slot -1 is left alone, another slot outside the store is reported and left alone.
+ */
 relaxkv_status relaxkv_read_quantized(
     const relaxkv_quantized_cache* store, const int32_t* slots, int64_t n_rows, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions,
     const relaxkv_rotary* rotary, void* k_out, void* v_out, int64_t token_stride, int64_t head_stride, relaxkv_stream stream);
@@ -658,16 +672,19 @@ relaxkv_status relaxkv_read_quantized(
 size_t relaxkv_quantized_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 
 /*
- * Attention of a step's rows over their sequence's tokens in the 8-bit store: row r of sequence i sees the first row_len[r] tokens of the blocks block_table[i, ..],
+ * Attention of a step's rows over their sequence's tokens in the 8-bit store: row r of sequence i sees the first row_len[r] tokens
+ * of the blocks block_table[i, ..],
  *   out[r,h,:] = softmax over t < row_len[r] of softmax_scale * <q[r,h,:], K[t]>, times V        (keys and values as the store's bytes stand for them)
- * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits, and to 2^-38 of the
- * row's largest (weight times value's scale), before they meet the values.  Any number of rows to a sequence.  With G = n_q_heads / n_kv_heads <= 16 and G times the sequences' rows on
- * average up to 32, a sequence's tokens are read once for 8 / G to 32 / G rows of it; beyond that once for 128 / G, and weights are rounded to 2^-35 of (the row's largest
- * weight times the largest value's scale of the tokens that it sees).  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
+ * q and the keys meet as they are (exact products, fp32 sums); weights are rounded to 11 bits, and to 2^-38 of the row's largest
+ * (weight times value's scale), before they meet the values.  Any number of rows to a sequence.  With G = n_q_heads / n_kv_heads <=
+ * 16 and G times the sequences' rows on average up to 32, a sequence's tokens are read once for 8 / G to 32 / G rows of it; beyond
+ * that once for 128 / G, and weights are rounded to 2^-35 of (the row's largest weight times the largest value's scale of the tokens
+ * that it sees).  Of rows n_seq, table_width, table_stride, n_rows, max_len, row_cu, row_seq, row_len and block_table are read;
  * n_seq <= 4096; row_len does not fall within a sequence.  A row that sees no token gets zeros and lse = -inf.
  *   q, out  device bf16 [n_rows, n_q_heads, head_dim] (16-byte aligned, not the same); lse_out NULL or device fp32 [n_q_heads, n_rows]
- * Rows with row_seq -1 and rows behind row_cu[n_seq] are left alone.  Reported and left alone: rows of a sequence whose row_cu, or whose last row_len, is out of range, rows whose row_seq is another
- * sequence, whose row_len is negative or above the sequence's last.  A block number out of range is reported, its tokens are passed over.  max_len up to 2^31 - 256.
+ * Rows with row_seq -1 and rows behind row_cu[n_seq] are left alone.  Reported and left alone: rows of a sequence whose row_cu, or
+ * whose last row_len, is out of range, rows whose row_seq is another sequence, whose row_len is negative or above the sequence's
+ * last.  A block number out of range is reported, its tokens are passed over.  max_len up to 2^31 - 256.
  */
 relaxkv_status relaxkv_quantized_attention(
     const relaxkv_quantized_cache* store, const relaxkv_continuation_rows* rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale,

@@ -8,8 +8,8 @@ launch and attention over [the shared context, the sequence's own tokens].  The 
 `n_select` only the blocks that each row may need most are read (8-bit bounds of the keys' blocks choose them).
 
 With `store_dtype` (int8 or e4m3) the repaired contexts move into the store themselves, in 8 bits (`keep_contexts`), and the caches are free for
-the next repair: half the bytes to hold, and to read at each step.  Then every sequence has its own copy of its context, and all its rows' attention
-reads the store alone.
+the next repair.  Then every sequence has a copy of its context of its own, and all its rows' attention reads the store alone: for a context that one
+sequence continues half the bytes to hold, and to read at each step, for n samples of one context n / 2 times those of the shared bf16 form.
 
 Call sequencing over torch buffers only; every operation runs in the CUDA kernels behind `binding`.
 """
@@ -25,7 +25,8 @@ from .inputs import BlockShape
 
 class Continuations:
     """Sequences over the contexts of a batch: `seqs[b]` of them continue context b (`ctx_lens[b]` tokens; 0: none).  Room for
-    `n_blocks` blocks of `block_size` own tokens in all, `max_len` to a sequence, and steps of up to `max_rows` rows."""
+    `n_blocks` blocks of `block_size` own tokens in all, `max_len` to a sequence, and steps of up to `max_rows` rows.  With a store_dtype the
+    blocks hold every sequence's context as well, which `max_len` does not count."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, ctx_lens: Sequence[int], seqs: Sequence[int], n_layers: int,
                  blk: BlockShape, n_blocks: int, max_len: int, block_size: int = 64, max_rows: Optional[int] = None, n_select: int = 0,

@@ -1,24 +1,30 @@
 // Attention of a step's rows over their sequence's tokens in the 8-bit store (relaxkv_quantized_attention).
 //
-// Every key and value meets the few rows and heads that read its KV head once: bound by the bytes of K and V.  Tokens are the 16 rows of the warp-level MMA and
-// (row, head) pairs its 8 columns, S^T = K Q^T and O^T += V^T P^T: a group of 4 or 5 heads fills half of it (as the 16 rows of the usual order a quarter), and what
-// is made of a byte of K or V is used for NT column tiles.  Bytes become fp16 in registers, exactly: two instructions for two of them (the byte under the exponent of
-// 1024, minus that; or the hardware's conversion of e4m3).  Q becomes fp16 exactly, too, scaled by a power of two per head; scores get the exponent
-// of their token's keys behind the product.  The exponents of the values are weighed with the scores: p'_t = 2^(s_t + e_t - max of that + 14), so that weights stay within
-// fp16 whatever the exponents are, and are rounded to 11 bits; the sum of the weights is kept beside it in fp32, with a maximum of its own.  P^T comes out of the first
-// product as rows of tokens and goes into the second as columns of them: one 8 x 8 transposition per 8 tokens.
+// Every key and value meets the few rows and heads that read its KV head once: bound by the bytes of K and V.  Tokens are the 16
+// rows of the warp-level MMA and (row, head) pairs its 8 columns, S^T = K Q^T and O^T += V^T P^T: a group of 4 or 5 heads fills
+// half of it (as the 16 rows of the usual order a quarter), and what is made of a byte of K or V is used for NT column tiles.
+// Bytes become fp16 in registers, exactly: two instructions for two of them (the byte under the exponent of 1024, minus that; or
+// the hardware's conversion of e4m3).  Q becomes fp16 exactly, too, scaled by a power of two per head; scores get the exponent of
+// their token's keys behind the product.  The exponents of the values are weighed with the scores: p'_t = 2^(s_t + e_t - max of
+// that + 14), so that weights stay within fp16 whatever the exponents are, and are rounded to 11 bits; the sum of the weights is
+// kept beside it in fp32, with a maximum of its own.  P^T comes out of the first product as rows of tokens and goes into the second
+// as columns of them: one 8 x 8 transposition per 8 tokens.
 //
-// A warp streams 32 tokens at a time through a ring of its own in shared memory (16-byte asynchronous copies, no barrier between warps; what lies behind a
-// sequence's end is filled with zeros and never read): twelve warps to an SM with two tiles of 8 KB in flight each, eight with three where a block has more than eight columns.
-// The work of a call - (sequence, KV head, row tile, 32 tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths; a task counts eight
-// units more, the time of its start and end.  A block's first and last task may be parts of one, whose results a second small kernel joins in the order of the blocks.  The next
-// task's first copies are on their way while a task's results are added up.  Calls of few short sequences give a cluster of up to eight blocks to each row tile and KV head, which
-// joins within itself: one launch.  More than 32 columns to a sequence go to the kernel of many rows (quantized_rows_sm100.cu).
+// A warp streams 32 tokens at a time through a ring of its own in shared memory (16-byte asynchronous copies, no barrier between
+// warps; what lies behind a sequence's end is filled with zeros and never read): twelve warps to an SM with two tiles of 8 KB in
+// flight each, eight with three where a block has more than eight columns. The work of a call - (sequence, KV head, row tile, 32
+// tokens), in this order - is cut into equal shares, one per block, found on the device from the lengths; a task counts eight units
+// more, the time of its start and end.  A block's first and last task may be parts of one, whose results a second small kernel
+// joins in the order of the blocks.  The next task's first copies are on their way while a task's results are added up.  Calls of
+// few short sequences give a cluster of up to eight blocks to each row tile and KV head, which joins within itself: one launch.
+// More than 32 columns to a sequence go to the kernel of many rows (quantized_rows_sm100.cu).
 //
-// Measured (int8, D 128, one row a sequence, L2 flushed): one sequence of 128 K of 32 / 8 heads 61 us (4.4 TB/s; 55 us with the heads' tokens side by side), 64 of up to 4 K of 40 / 8
-// heads 61.6 (4.75 TB/s), 16 of up to 8 K 40, three rows of eight sequences of 8 K to 64 K 106 (4.9 TB/s), 1 K of 4 / 1 heads 6.6.  Between its first and last copies a call is at
-// 5.4 to 6.5 TB/s of the 6.57 that a plain copy makes; its start takes 3.3 us (arguments, lengths and block numbers, one read behind the other), its end some 12 (blocks that had more of
-// the late copies, the four warps' results, the join).
+// Measured (D 128, calls among others on changing inputs): one sequence of 128 K of 32 / 8 heads 60 to 63 us
+// (4.3 to 4.5 TB/s), 64 of up to 4 K of 40 / 8 heads, tokens of a head side by side, 62 (4.7 TB/s), 16 of up to 8 K 40, three rows
+// of eight sequences of 8 K to 64 K 112 to 118 (4.4 to 4.6 TB/s), 1 K of 4 / 1 heads 6.5. Blocks ask for their first copies 3.8 us
+// after they may begin (arguments, lengths and block numbers, one read behind the other), half of them have done their last tile 10
+// us before the last one has (64 of up to 4 K: 8; they began alike, but had fewer of the late copies), the last results take 1.5 us
+// more and the join 4 to 5.
 #include "quantized_attention.cuh"
 
 namespace relaxkv {

@@ -1,17 +1,22 @@
-// Rotary embeddings of every form (relaxkv_qk_norm_rotate), rows into the 8-bit store (relaxkv_append_quantized) and back (relaxkv_read_quantized).
+// Rotary embeddings of every form (relaxkv_qk_norm_rotate), rows into the 8-bit store (relaxkv_append_quantized) and back
+// (relaxkv_read_quantized).
 //
-// All three read and write every element once and are bound by HBM for many rows, by their latencies (row values, then slot or angle) for few.  D / 8 lanes hold
-// a head, eight dims each, chosen so that a pair always meets in one lane: dims 8 i .. 8 i + 7 where pairs are neighbours or nothing turns; where pair i is
-// (i, i + part / 2), dims 4 i .. and part / 2 + 4 i .. of the part that turns, and the dims behind it eight at a time.  Lane i has the pairs 4 i .. 4 i + 3
-// either way.  All heads of a row turn by the same angles, which are made once per row, one per thread: the turns p freq / 2 pi are rounded to their
-// remainder in fp64 (a float of position 100000 would be off by 2^-8 radians), sine and cosine of that in fp32, with what its own rounding cuts off (which moved a third of the keys
-// that land on the other side of a rounding to 8 bits than the formula's: 18 of 4 million e4m3 values for 32).  Everything else stays in fp32 until the one rounding at the
-// end.  The scale of 8 bits is a power of two: the division by it is exact, values of two eighths of bf16's bits stay exact when read back, and the
-// bytes do not depend on the order of anything.
+// All three read and write every element once and are bound by HBM for many rows, by their latencies (row values, then slot or
+// angle) for few.  D / 8 lanes hold a head, eight dims each, chosen so that a pair always meets in one lane: dims 8 i .. 8 i + 7
+// where pairs are neighbours or nothing turns; where pair i is (i, i + part / 2), dims 4 i .. and part / 2 + 4 i .. of the part
+// that turns, and the dims behind it eight at a time.  Lane i has the pairs 4 i .. 4 i + 3 either way.  All heads of a row turn by
+// the same angles, which are made once per row, one per thread: the turns p freq / 2 pi are rounded to their remainder in fp64 (a
+// float of position 100000 would be off by 2^-8 radians), sine and cosine of that in fp32, with what its own rounding cuts off
+// (which moved a third of the keys that land on the other side of a rounding to 8 bits than the formula's: 18 of 4 million e4m3
+// values for 32).  Everything else stays in fp32 until the one rounding at the end.  The scale of 8 bits is a power of two: the
+// division by it is exact, values of two eighths of bf16's bits stay exact when read back, and the bytes do not depend on the order
+// of anything.
 //
-// Measured (L2 flushed): 8205 rows of 40 / 8 heads with norms, half the head turned, 40 us (5.0 TB/s of bytes that have to move); 16 K rows of 8 heads written as e4m3 and read back
-// 34.5 us (by themselves 19 and 18); 32 K rows read and turned 40 (5.1 TB/s); 64 rows of 32 / 8 heads turned 5.2, written and read back 9.6.  Many rows with norm and rotation issue in
-// 78 % of the schedulers' cycles: some 160 instructions for eight elements with their addresses.  Sixteen elements to a lane took longer (50.7 us; 45.9 read), fewer heads being in flight.
+// Measured (L2 flushed): 8205 rows of 40 / 8 heads with norms, half the head turned, 40 us (5.0 TB/s of bytes that have to move);
+// 16 K rows of 8 heads written as e4m3 and read back 34.5 us (by themselves 19 and 18); 32 K rows read and turned 40 (5.1 TB/s); 64
+// rows of 32 / 8 heads turned 5.2, written and read back 9.6.  Many rows with norm and rotation issue in 78 % of the schedulers'
+// cycles: some 160 instructions for eight elements with their addresses.  Sixteen elements to a lane took longer (50.7 us; 45.9
+// read), fewer heads being in flight.
 #include "quantized_cache.cuh"
 #include "sm100_ptx.cuh"
 #include <cmath>

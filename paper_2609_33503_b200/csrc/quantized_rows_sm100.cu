@@ -1,20 +1,24 @@
 // Attention of many rows of a sequence over its tokens in the 8-bit store: a question, a long draft (relaxkv_quantized_attention).
 //
-// Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of one sequence), one KV head and a run of
-// 128-token tiles.  Eight warps bring a tile, four its K and four its V: 8-bit values out of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the
-// tensor cores read them (K as rows of dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two per row); a thread makes weights
-// of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the scores, those of the values on the weights, relative to the largest so far
-// of the tokens that a row sees: p = 2^(s - m + 11 + e_t - E).
-// Two groups of four warps take the even and the odd tiles: the weights of one tile are made while the products of the other run.  S of tile j + 2 is made when P of tile j has
-// been used; a group hands its P over when O of the tile before is complete, which is also when O may be rescaled; a row's running maximum goes from group to group through
-// shared memory, sums stay with the groups.  K is written a tile ahead of V, or the weights of a tile wait for a value tile that waits for them.
-// Every wait is bounded.
+// Rows x heads of a group meet the same keys, so they are the rows of a matrix product: a block owns 128 of them (128 / G rows of
+// one sequence), one KV head and a run of 128-token tiles.  Eight warps bring a tile, four its K and four its V: 8-bit values out
+// of the pages in 16-byte pieces, two tiles ahead, made fp16, exactly, and written where the tensor cores read them (K as rows of
+// dims, V as rows of the contraction, 128-byte swizzle).  S = Q K^T with Q in tensor memory as fp16 (exactly, times a power of two
+// per row); a thread makes weights of a row of S, which take its place as fp16; O += P V.  The exponents of the keys go on the
+// scores, those of the values on the weights, relative to the largest so far of the tokens that a row sees: p = 2^(s - m + 11 + e_t
+// - E). Two groups of four warps take the even and the odd tiles: the weights of one tile are made while the products of the other
+// run.  S of tile j + 2 is made when P of tile j has been used; a group hands its P over when O of the tile before is complete,
+// which is also when O may be rescaled; a row's running maximum goes from group to group through shared memory, sums stay with the
+// groups.  K is written a tile ahead of V, or the weights of a tile wait for a value tile that waits for them. Every wait is
+// bounded.
 //
-// Measured (int8, D 128): 57 rows of 40 / 8 heads over 16 K 62.7 us (the products alone, at 1.66 PFLOP/s, 11.5; the kernel of few rows 123), 16 rows of 32 / 8 heads over 8 x 4 K 48.5
-// (68), 200 over 3000 40 (75).  Bound by issue, not by the tensor cores (21 % of the time) or memory: a tile's 128 x 128 weights and its two conversions to fp16 are some 2200 instructions of
-// each of the SM's four schedulers, which five warps each (two of rows, one each of K and V, the products') issue at half their rate, 4200 clk a tile.  Weights in one pass with a
-// reference that is a whole number (62.7), exponents within the fp16 tiles in place of factors on scores and weights (65.4: the conversions get longer), both groups on halves of the same tile
-// (68.4: all wait and all take exponentials at once), 144 or 128 registers for the rows' threads (62.9) and two of the 32-column chunks at once (80.8 of 78.5) were no faster.
+// Measured (int8, D 128): 57 rows of 40 / 8 heads over 16 K 62.9 us (the products alone, at 1.66 PFLOP/s, 11.5; the kernel of few
+// rows 123).  Bound by issue, not by the tensor cores (21 % of the time) or memory: a tile's 128 x 128 weights and its two
+// conversions to fp16 are some 2100 instructions of each of the SM's four schedulers, which five warps each (two of rows, one each
+// of K and V, the products') issue at half their rate, 4200 clk a tile.  No faster, at 62.7 us then: weights in one pass with a
+// reference that is a whole number (62.7), exponents within the fp16 tiles in place of factors on scores and weights (65.4: the
+// conversions get longer), both groups on halves of the same tile (68.4: all wait and all take exponentials at once), 144 or 128
+// registers for the rows' threads (62.9). Weighing the last tile of a row relative to what the row sees of it took 1 us.
 #include "quantized_attention.cuh"
 #include <atomic>
 
